@@ -31,6 +31,11 @@
  *   derf_set_encoding  gamma(x) fused into the MLP or stored by its
  *                 own pass (the ablation of the fusion)          (Sec. 4)
  *   derf_render_noalloc  derf_render for callers that cannot allocate
+ *   derf_route, derf_dispatch, derf_combine, derf_combine_backward,
+ *   derf_heads_linear, derf_heads_linear_backward, derf_adamw_*
+ *                 operators of training: samples to their heads and back,
+ *                 the heads' layers, their gradients, the AdamW step
+ *                 (Sec. 3.2 Eq. 4-5, Sec. 3.4)
  *
  * All functions return a derf_status (0 on success, negative on error),
  * never abort and never print.  derf_last_error() returns a thread-local
@@ -375,6 +380,146 @@ int derf_set_timing(derf_handle *h, int on);
 /* Waits for the last render's stream, then fills *out. */
 int derf_get_stats(derf_handle *h, derf_stats *out);
 int derf_reset_stats(derf_handle *h);
+
+/* ---- Operators of training ---------------------------------------------------
+ * The mixture of heads sigma = sum_n w^n sigma_n, c = sum_n w^n c_n of Sec. 3.2
+ * (Eq. 4-5) with a few heads per sample, layer by layer and with gradients: a
+ * sample's rows go to the heads that a weight function picked for it (the
+ * largest soft Voronoi weights, a gate's), each head's layers run on its rows,
+ * the results come back weighted, and AdamW updates the weights.
+ *
+ * These calls take no handle (but for the optimizer's).  All arrays are device
+ * memory of the current device unless they are called host; work is enqueued on
+ * hip_stream (a hipStream_t, NULL: the default stream) and the calls return
+ * without waiting.  They allocate nothing, run nothing on other streams and may
+ * be captured into HIP graphs.  A workspace belongs to the caller, holds nothing
+ * between calls, and is 16-byte aligned.  Results do not depend on the run:
+ * every sum has a fixed order.
+ *   precision    a derf_precision: the type of the rows (float or bf16)
+ *   *_stride     elements from a row to the next, >= the row length; rows need
+ *                the alignment of their type only (rows and strides that are
+ *                multiples of 16 bytes are read fastest)
+ * Products and sums are taken in fp32; results in bf16 are rounded once, to
+ * nearest even. */
+#define DERF_MAX_TOP_K 16
+
+/* Sort (sample, slot) pairs by head.
+ *   heads        int [T][top_k]: each pair's head; outside [0, num_heads): the
+ *                pair has none (a masked slot)
+ *   out_offsets  int [num_heads + 1]: head h's rows are [offsets[h],
+ *                offsets[h + 1]); from offsets[num_heads] on, pairs without head
+ *   out_pair     int [T * top_k]: the pair t * top_k + j at each row (stable:
+ *                a head's pairs ascend)
+ *   out_row      int [T][top_k]: each pair's row r, or -1 - r without a head
+ *   workspace    derf_route_workspace(...) bytes (-1 for invalid sizes)
+ * 1 <= num_heads <= 256, 1 <= top_k <= DERF_MAX_TOP_K, T * top_k < 2^31. */
+long long derf_route_workspace(long long num_tokens, int top_k, int num_heads);
+int derf_route(const int *heads, long long num_tokens, int top_k, int num_heads, int *out_offsets,
+               int *out_pair, int *out_row, void *workspace, long long workspace_bytes,
+               void *hip_stream);
+
+/* Samples' rows into the heads' order: out[row[t][j]] = x[t]; rows without a
+ * head are zero (out has T * top_k rows, all written).  row: derf_route's.  The
+ * gradient is derf_combine of the output's gradient without weights. */
+int derf_dispatch(const void *x, long long x_stride, const int *row, long long num_tokens,
+                  int top_k, int dim, int precision, void *out, long long out_stride,
+                  void *hip_stream);
+
+/* Rows back to their samples (Eq. 4-5): out[t] = sum_j weights[t][j] *
+ * rows[row[t][j]] over the pairs that have a head, in the order of j.
+ *   weights  float [T][top_k], NULL: ones.  Weights and rows of pairs without a
+ *            head are not looked at. */
+int derf_combine(const void *rows, long long rows_stride, const float *weights, const int *row,
+                 long long num_tokens, int top_k, int dim, int precision, void *out,
+                 long long out_stride, void *hip_stream);
+
+/* Gradients of derf_combine: out_rows[row[t][j]] = weights[t][j] * dout[t] and
+ * out_weights[t][j] = <rows[row[t][j]], dout[t]>; both zero for pairs without a
+ * head.  out_weights (float [T][top_k]) may be NULL, and then rows too. */
+int derf_combine_backward(const void *dout, long long dout_stride, const void *rows,
+                          long long rows_stride, const float *weights, const int *row,
+                          long long num_tokens, int top_k, int dim, int precision,
+                          void *out_rows, long long out_rows_stride, float *out_weights,
+                          void *hip_stream);
+
+/* One linear layer of every head on its rows (the heads' networks of Sec. 4.1):
+ * y[r] = act(W_h x[r] + b_h) for r in [offsets[h], offsets[h + 1]), zero for
+ * rows from offsets[num_heads] on.
+ *   w        [num_heads][fan_out][fan_in] of the rows' type, as in
+ *            derf_weights_count's order; contiguous
+ *   bias     float [num_heads][fan_out], or NULL
+ *   offsets  int [num_heads + 1], ascending within [0, num_rows] (values outside
+ *            are taken as the nearest inside)
+ *   relu     1: act = ReLU (a NaN stays NaN), 0: none
+ * num_heads <= 256; num_rows < 2^31; fan_in, fan_out in [1, 65536]. */
+int derf_heads_linear(const void *x, long long x_stride, const void *w, const float *bias,
+                      const int *offsets, long long num_rows, int num_heads, int fan_in,
+                      int fan_out, int relu, int precision, void *y, long long y_stride,
+                      void *hip_stream);
+
+/* Gradients of derf_heads_linear.  With dz = dy, or with y (the layer's output,
+ * where it had a ReLU) dz = dy where y > 0 and 0 elsewhere:
+ *   out_x     dx[r] = W_h^T dz[r]; zero for rows from offsets[num_heads] on
+ *   out_w     float [num_heads][fan_out][fan_in]: dW_h = sum_r dz[r] x[r]^T
+ *   out_bias  float [num_heads][fan_out]: sum_r dz[r]
+ * Heads without rows get zeros.  Any of the three outputs may be NULL (then
+ * what only it needs may be NULL too: w for out_x, x for out_w).
+ *   workspace  derf_heads_linear_workspace(...) bytes (-1 for invalid sizes) */
+long long derf_heads_linear_workspace(long long num_rows, int num_heads, int fan_in, int fan_out,
+                                      int precision);
+int derf_heads_linear_backward(const void *dy, long long dy_stride, const void *x,
+                               long long x_stride, const void *w, const void *y,
+                               long long y_stride, const int *offsets, long long num_rows,
+                               int num_heads, int fan_in, int fan_out, int precision, void *out_x,
+                               long long out_x_stride, float *out_w, float *out_bias,
+                               void *workspace, long long workspace_bytes, void *hip_stream);
+
+/* AdamW over many tensors in one launch (the heads are trained with a
+ * first-order optimizer, Sec. 3.4).  Per value, with g = *grad_scale * grad:
+ *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,
+ *   p = (1 - lr weight_decay) p
+ *       - lr / (1 - beta1^t) * m / (sqrt(v) / sqrt(1 - beta2^t) + eps)
+ * in fp32, each operation rounded on its own.
+ * A tensor:
+ *   param, grad   n values, float or bf16 each (a derf_precision)
+ *   copy          NULL, or bf16 [n]: the updated parameters rounded (for a float
+ *                 param whose layers run in bf16)
+ *   m, v          state_bits 32: float [n] each.
+ *                 state_bits 8: one byte a value in OCP e4m3, and m_scale and
+ *                 v_scale a float for each 256 values (from the tensor's first
+ *                 one on): m = code * scale and sqrt(v) = code * scale.  A scale
+ *                 is its block's largest magnitude / 448 (at least 2^-120), a
+ *                 positive sqrt(v) keeps at least the smallest code, and a value
+ *                 that is not finite is kept as NaN and left out of the scale.
+ *                 The step uses m and v as they are before they are rounded.
+ *                 All zeros is the initial state of both forms.
+ *   n             values, >= 0 */
+typedef struct {
+    void *param;
+    const void *grad;
+    void *m;
+    void *v;
+    float *m_scale;
+    float *v_scale;
+    void *copy;
+    long long n;
+    int param_precision;
+    int grad_precision;
+} derf_adamw_tensor;
+typedef struct derf_adamw derf_adamw;
+/* tensors: host [num_tensors] (copied to the device; the call synchronises it).
+ * The optimizer keeps the addresses, not the memory: every tensor stays valid
+ * until derf_adamw_destroy, gradients are written to the same place each step.
+ * num_tensors <= 65536, their sum of n < 2^40. */
+int derf_adamw_create(derf_adamw **out, const derf_adamw_tensor *tensors, int num_tensors,
+                      int state_bits);
+/* step: t above, >= 1.  grad_scale: device float or NULL (1): an unscaling or a
+ * clipping factor that is computed on the device. */
+int derf_adamw_step(derf_adamw *opt, double lr, double beta1, double beta2, double eps,
+                    double weight_decay, long long step, const float *grad_scale,
+                    void *hip_stream);
+/* Waits for the device, then frees the table.  NULL is a no-op. */
+void derf_adamw_destroy(derf_adamw *opt);
 
 /* Waits for the handle's last stream, then frees everything.  NULL is a no-op. */
 void derf_destroy(derf_handle *h);

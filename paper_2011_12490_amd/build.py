@@ -22,7 +22,8 @@ ARCH = "gfx950"
 SOURCES = ["mlp_8x256.hip", "mlp_8x128.hip", "mlp_8x128_split.hip", "mlp_8x128_f32.hip",
            "mlp_6x64.hip", "mlp_6x64_split.hip", "mlp_6x64_f32.hip", "mlp_4x64.hip",
            "mlp_4x64_split.hip", "mlp_4x64_f32.hip", "kernels_sample.hip",
-           "kernels_fine.hip", "kernels_soft.hip", "kernels_gate.hip", "derf_api.cpp"]
+           "kernels_fine.hip", "kernels_soft.hip", "kernels_gate.hip", "kernels_route.hip",
+           "kernels_linear.hip", "kernels_adamw.hip", "ops_api.cpp", "derf_api.cpp"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=" + ARCH,
           "-I" + os.path.join(ROOT, "include"), "-I" + CSRC,

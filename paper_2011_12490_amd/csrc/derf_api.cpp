@@ -18,6 +18,7 @@
 
 #include "derf_internal.h"
 #include "derf_cull.h"
+#include "ops_internal.h"
 
 using namespace derf;
 
@@ -248,6 +249,18 @@ size_t layout(char *base, unsigned S, unsigned Sf, unsigned R, unsigned nblk, in
 }
 
 }  // namespace
+
+int derf::report(int status, const char *fmt, ...)
+{
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(g_last_error, sizeof(g_last_error), fmt, ap);
+    va_end(ap);
+    return status;
+}
+
+hipError_t derf::device_alloc(void **p, size_t bytes) { return dev_alloc(p, bytes); }
+hipError_t derf::device_free(void *p) { return dev_free(p); }
 
 // The grouped-MLP variant of a head architecture, or nullptr if none is built.
 const MlpVariant *derf::find_mlp_variant(const HeadArch &a, bool bf16)

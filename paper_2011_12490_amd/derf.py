@@ -54,12 +54,24 @@ class derf_stats(ctypes.Structure):
                 ("walk_rays", ctypes.c_longlong), ("walk_fallback_rays", ctypes.c_longlong)]
 
 
+class derf_adamw_tensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("m_scale", ctypes.c_void_p),
+                ("v_scale", ctypes.c_void_p), ("copy", ctypes.c_void_p),
+                ("n", ctypes.c_longlong), ("param_precision", ctypes.c_int),
+                ("grad_precision", ctypes.c_int)]
+
+
 EXPORTS = ("derf_weights_count", "derf_create", "derf_create_mixed", "derf_head_arithmetic", "derf_render",
            "derf_render_debug", "derf_render_noalloc",
            "derf_render_soft", "derf_render_culled", "derf_set_empty_heads", "derf_set_gate",
            "derf_gate_weights_count", "derf_render_gated", "derf_set_encoding", "derf_set_timing",
            "derf_get_stats",
            "derf_reset_stats", "derf_destroy",
+           "derf_route_workspace", "derf_route", "derf_dispatch", "derf_combine",
+           "derf_combine_backward", "derf_heads_linear", "derf_heads_linear_workspace",
+           "derf_heads_linear_backward", "derf_adamw_create", "derf_adamw_step",
+           "derf_adamw_destroy",
            "derf_status_string", "derf_last_error")
 
 _lib: Optional[ctypes.CDLL] = None
@@ -124,6 +136,22 @@ def lib() -> ctypes.CDLL:
         L.derf_get_stats.restype = ctypes.c_int
         L.derf_reset_stats.argtypes = [P]
         L.derf_reset_stats.restype = ctypes.c_int
+        N, I, D = ctypes.c_longlong, ctypes.c_int, ctypes.c_double
+        for name, restype, argtypes in (
+                ("derf_route_workspace", N, [N, I, I]),
+                ("derf_route", I, [P, N, I, I, P, P, P, P, N, P]),
+                ("derf_dispatch", I, [P, N, P, N, I, I, I, P, N, P]),
+                ("derf_combine", I, [P, N, P, P, N, I, I, I, P, N, P]),
+                ("derf_combine_backward", I, [P, N, P, N, P, P, N, I, I, I, P, N, P, P]),
+                ("derf_heads_linear", I, [P, N, P, P, P, N, I, I, I, I, I, P, N, P]),
+                ("derf_heads_linear_workspace", N, [N, I, I, I, I]),
+                ("derf_heads_linear_backward", I,
+                 [P, N, P, N, P, P, N, P, N, I, I, I, I, P, N, P, P, P, N, P]),
+                ("derf_adamw_create", I, [ctypes.POINTER(P), P, I, I]),
+                ("derf_adamw_step", I, [P, D, D, D, D, D, N, P, P]),
+                ("derf_adamw_destroy", None, [P])):
+            getattr(L, name).restype = restype
+            getattr(L, name).argtypes = argtypes
         L.derf_destroy.argtypes = [P]
         L.derf_destroy.restype = None
         L.derf_status_string.argtypes = [ctypes.c_int]
@@ -402,6 +430,10 @@ def derf_reset_stats(h):
 
 def derf_destroy(h):
     lib().derf_destroy(h)
+
+
+def derf_adamw_destroy(opt):
+    lib().derf_adamw_destroy(opt)
 
 
 # ---- convenience ----------------------------------------------------------------
