@@ -451,7 +451,8 @@ int derf_combine_backward(const void *dout, long long dout_stride, const void *r
  *   offsets  int [num_heads + 1], ascending within [0, num_rows] (values outside
  *            are taken as the nearest inside)
  *   relu     1: act = ReLU (a NaN stays NaN), 0: none
- * num_heads <= 256; num_rows < 2^31; fan_in, fan_out in [1, 65536]. */
+ * num_heads <= 256; num_rows < 2^31; fan_in, fan_out in [1, 65536]; row strides
+ * below 2^21. */
 int derf_heads_linear(const void *x, long long x_stride, const void *w, const float *bias,
                       const int *offsets, long long num_rows, int num_heads, int fan_in,
                       int fan_out, int relu, int precision, void *y, long long y_stride,

@@ -1,5 +1,15 @@
 // The heads' linear layers and their gradients: products of matrices whose
 // rows come in groups, one group a head, with bounds known on the device only.
+//
+//   layer      y[r][o]  = act(sum_i x[r][i] W[o][i] + b[o])
+//   rows       dx[r][i] = sum_o dz[r][o] W[o][i]
+//   weights    dW[o][i] = sum_r dz[r][o] x[r][i],  db[o] = sum_r dz[r][o]
+//
+// One tile product serves all three (tile_product below): operand P (TP
+// rows of the matrix unit's first operand) times operand Q (TQ of its second),
+// reduced over steps of 128 bytes of depth.  Each operand lies in memory either
+// with its depth side by side ("deep": x, dz, and W for a layer) or with its
+// tile's rows side by side (W for the rows' gradient; dz and x for the weights').
 #include "ops_internal.h"
 
 namespace derf {
@@ -7,10 +17,15 @@ namespace derf {
 namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kThreads = 256;
-constexpr int kTile = 64;  // rows and columns of a workgroup's tile of the result
+__device__ __forceinline__ unsigned uniform(unsigned x)
+{
+    return (unsigned)__builtin_amdgcn_readfirstlane((int)x);
+}
 
 struct Problem {
     const int *offsets;
@@ -24,239 +39,902 @@ __device__ __forceinline__ unsigned bound(const Problem &p, int h)
     return v < 0 ? 0u : (unsigned)v < p.rows ? (unsigned)v : p.rows;
 }
 
-// The rows [first, last) of tile `tile` and their head (p.heads: rows without
-// one, p.heads + 1: there is no such tile).  256 threads, all call it.
-struct TileRows {
+// ---- which rows a workgroup takes ---------------------------------------------
+
+// Rows [first, last) of one head (or of none: head = number of heads).
+struct RowTile {
     unsigned first, last;
     int head;
 };
-__device__ TileRows find_tile(const Problem &p, unsigned tile, unsigned tile_rows, TileRows *found,
-                              unsigned *tmp)
+
+// The heads' numbers of tiles of `tile_rows` rows, summed: thread h < 256 keeps
+// the tiles before head h's.  At least 256 threads, all call it.
+struct Spread {
+    unsigned first, last, before, mine;  // of head threadIdx.x
+    unsigned total;                      // of all heads
+};
+__device__ __forceinline__ Spread spread_tiles(const Problem &p, unsigned tile_rows, unsigned *tmp)
 {
     const int h = threadIdx.x, lane = h & 63, wave = h >> 6;
-    unsigned a = 0, b = 0;
+    Spread s = {0, 0, 0, 0, 0};
     if (h < p.heads) {
-        a = bound(p, h);
-        b = bound(p, h + 1);
+        s.first = bound(p, h);
+        s.last = bound(p, h + 1);
+        s.mine = s.last > s.first ? (s.last - s.first + tile_rows - 1) / tile_rows : 0;
     }
-    const unsigned mine = b > a ? (b - a + tile_rows - 1) / tile_rows : 0;
-    unsigned incl = mine;
+    unsigned incl = s.mine;
     for (int off = 1; off < 64; off <<= 1) {
         const unsigned y = __shfl_up(incl, off);
         if (lane >= off)
             incl += y;
     }
-    if (lane == 63)
+    if (lane == 63 && wave < 4)
         tmp[wave] = incl;
     __syncthreads();
-    if (h == 0)
-        found->head = p.heads + 1;  // until the tile's thread says otherwise, below
-    __syncthreads();
-    unsigned before = incl - mine, total = 0;
-    for (int w = 0; w < kThreads / 64; ++w) {
+    s.before = incl - s.mine;
+    for (int w = 0; w < 4; ++w) {
         if (w < wave)
-            before += tmp[w];
-        total += tmp[w];
-    }
-    if (tile >= before && tile - before < mine) {
-        found->first = a + (tile - before) * tile_rows;
-        found->last = found->first + tile_rows < b ? found->first + tile_rows : b;
-        found->head = h;
-    }
-    if (h == 0 && tile >= total) {
-        const unsigned from = bound(p, p.heads);
-        const unsigned long long at = from + (unsigned long long)(tile - total) * tile_rows;
-        if (at < p.rows) {
-            found->first = (unsigned)at;
-            found->last = at + tile_rows < p.rows ? (unsigned)at + tile_rows : p.rows;
-            found->head = p.heads;
-        }
+            s.before += tmp[w];
+        s.total += tmp[w];
     }
     __syncthreads();
-    return *found;
+    return s;
 }
 
-template <class T>
-struct Kind;
-template <>
-struct Kind<__bf16> {
-    static constexpr int kDepth = 32;  // of one step through LDS
-    static __device__ __forceinline__ f32x4 step(const __bf16 *a, const __bf16 *b, int q, f32x4 c)
-    {
-        bf16x8 x, y;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            x[i] = a[q * 8 + i];
-            y[i] = b[q * 8 + i];
-        }
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(x, y, c, 0, 0, 0);
+// Tile number `tile` (one of the heads'); all threads call it.
+__device__ __forceinline__ RowTile head_tile(const Spread &s, unsigned tile, unsigned tile_rows,
+                                             RowTile *found)
+{
+    __syncthreads();
+    if (tile >= s.before && tile - s.before < s.mine) {
+        found->first = s.first + (tile - s.before) * tile_rows;
+        found->last = s.last - found->first > tile_rows ? found->first + tile_rows : s.last;
+        found->head = threadIdx.x;
     }
+    __syncthreads();
+    return {uniform(found->first), uniform(found->last), (int)uniform((unsigned)found->head)};
+}
+
+// Workgroup b of at least `all`: which of `all` tiles it takes.  Consecutive
+// workgroups go to the 8 XCDs in turn; each XCD gets runs of up to 32 tiles (its
+// compute units), neighbours that share operands in its L2, and short ones where
+// there are few tiles, so that none gets much more than another.
+constexpr unsigned kXcds = 8, kRun = 32;
+__device__ __forceinline__ unsigned long long by_xcd(unsigned long long b, unsigned long long all)
+{
+    const unsigned run = all >= 64 * kRun ? kRun : all >= 64 ? (unsigned)all / 64 : 1;
+    const unsigned long long j = b / kXcds;
+    return (j / run * kXcds + b % kXcds) * run + j % run;
+}
+
+// Tile `at` of rows x cols ones: in groups of 4 rows, a group column by column.
+struct Place2 {
+    unsigned a, b;
+};
+__device__ __forceinline__ Place2 in_groups(unsigned long long at, unsigned rows, unsigned cols)
+{
+    const unsigned group = (unsigned)(at / (4ull * cols));
+    const unsigned in = (unsigned)(at - (unsigned long long)group * 4 * cols);
+    const unsigned tall = rows - group * 4 < 4 ? rows - group * 4 : 4;
+    return {group * 4 + in % tall, in / tall};
+}
+
+// ---- operands -------------------------------------------------------------------
+
+template <class T>
+struct Type;
+template <>
+struct Type<__bf16> {
+    static constexpr int kVec = 8;     // elements of 16 bytes
+    static constexpr int kDepth = 64;  // of 128 bytes: a step's depth
 };
 template <>
-struct Kind<float> {
-    static constexpr int kDepth = 16;
-    static __device__ __forceinline__ f32x4 step(const float *a, const float *b, int q, f32x4 c)
+struct Type<float> {
+    static constexpr int kVec = 4;
+    static constexpr int kDepth = 32;
+};
+
+struct __attribute__((packed, aligned(2))) Bytes16 {
+    u32x4 v;
+};
+
+// x without its first `n` elements, zeros behind (n >= the elements: all zero).
+template <class T>
+__device__ __forceinline__ u32x4 drop_first(u32x4 x, int n)
+{
+    const int bits = n * (int)sizeof(T) * 8;
+    unsigned long long lo = x[0] | (unsigned long long)x[1] << 32;
+    unsigned long long hi = x[2] | (unsigned long long)x[3] << 32;
+    const int s = bits & 63;
+    if (bits >= 64) {
+        lo = hi;
+        hi = 0;
+    }
+    if (bits >= 128)
+        lo = 0;
+    if (s) {
+        lo = lo >> s | hi << (64 - s);
+        hi >>= s;
+    }
+    return u32x4{(unsigned)lo, (unsigned)(lo >> 32), (unsigned)hi, (unsigned)(hi >> 32)};
+}
+
+// x where y > 0, zero elsewhere (bf16: a value is positive and no NaN if its
+// bits less one are below those of infinity).
+__device__ __forceinline__ u32x4 where_positive(u32x4 x, u32x4 y, __bf16)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const unsigned lo = ((y[i] & 0xFFFFu) - 1u) < 0x7F80u ? 0xFFFFu : 0u;
+        const unsigned hi = ((y[i] >> 16) - 1u) < 0x7F80u ? 0xFFFF0000u : 0u;
+        x[i] &= lo | hi;
+    }
+    return x;
+}
+__device__ __forceinline__ u32x4 where_positive(u32x4 x, u32x4 y, float)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        x[i] = __uint_as_float(y[i]) > 0.0f ? x[i] : 0u;
+    return x;
+}
+
+// An operand in memory: element (row, col) at p[row * stride + col], `rows` by
+// `cols`; what lies outside counts as zero.  With a mask of the same shape,
+// elements count where the mask's are positive.  All of it is the same for the
+// whole workgroup.
+template <class T>
+struct Matrix {
+    const T *p;
+    long long stride;
+    const T *mask;
+    long long mask_stride;
+    unsigned rows;
+    int cols;
+};
+
+// A stretch of memory that a workgroup reads at 32-bit offsets: what starts at
+// or behind its end reads as zero, and no read that starts in front of it (a
+// whole 16-byte piece of a row) reaches over it.  At most 2^31 - 1 bytes, which
+// a tile's 256 rows do not exceed (row strides are below 2^21 elements); an
+// offset of kOutside is behind every window's end.
+typedef u32x4 Window;
+constexpr long long kMostBytes = 0x7FFFFFFF;
+constexpr unsigned kOutside = 0xFFFFFFF0u;
+template <class T>
+__device__ __forceinline__ Window window(const T *p, long long stride, unsigned rows, int cols,
+                                         unsigned row0, int col0)
+{
+    const unsigned long long at = reinterpret_cast<unsigned long long>(p + (row0 * stride + col0));
+    const long long end = row0 < rows && col0 < cols
+                              ? ((long long)(rows - row0 - 1) * stride + cols - col0) * (long long)sizeof(T)
+                              : 0;
+    const unsigned records = end < kMostBytes ? (unsigned)end : (unsigned)kMostBytes;
+    return Window{uniform((unsigned)at), uniform((unsigned)(at >> 32)), uniform(records), 0x00020000u};
+}
+__device__ __forceinline__ u32x4 read16(const Window &w, unsigned offset)
+{
+    const void *p = reinterpret_cast<const void *>(w[0] | (unsigned long long)w[1] << 32);
+    return __builtin_amdgcn_raw_buffer_load_b128(
+        __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, w[2], w[3]), offset, 0, 0);
+}
+// 64 x 16 bytes to LDS: lane l's piece at `offset` lands at lds + 16 l.  Written
+// as asm so that the compiler does not wait for it at the next read of LDS; it
+// is waited for where its tile is needed (async_done).
+__device__ __forceinline__ void read16_to_lds(const Window &w, unsigned offset, char *lds)
+{
+    const unsigned l = (unsigned)(unsigned long)(__attribute__((address_space(3))) char *)lds;
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 ::"s"(uniform(l)), "v"(offset), "s"(w)
+                 : "memory");
+}
+__device__ __forceinline__ void async_done() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
+// Tile of an operand: DEEP: TILE rows by kDepth columns, else kDepth rows by
+// TILE columns; one depth step's.  In LDS it lies row by row in 16-byte chunks,
+// a row's chunks permuted by the row: deep ones so that a column of chunks
+// touches all banks, the others in pairs so that what a transposing read takes
+// from four rows lies in four places.  A thread brings kShare chunks, all of
+// the same columns.
+template <class T, int TILE, bool DEEP, int THREADS, bool MASK>
+struct Tile {
+    static constexpr int V = Type<T>::kVec, D = Type<T>::kDepth;
+    static constexpr int kShare = TILE * 8 / THREADS;
+    static constexpr int kBytes = TILE * 128;
+    static constexpr int kPerRow = DEEP ? 8 : TILE / V;
+    static constexpr int kRowStep = THREADS / kPerRow;
+    static_assert(TILE * 8 % THREADS == 0 && kRowStep % (sizeof(T) == 2 && !DEEP ? 16 : 8) == 0,
+                  "whole shares, of one permutation");
+    struct S {
+        u32x4 x[kShare];
+        u32x4 y[MASK ? kShare : 1];
+    };
+
+    // the permutation of row r's chunks: chunk c lies at c ^ turn(r)
+    static __device__ __forceinline__ unsigned turn(unsigned r)
     {
+        if (DEEP)
+            return r & 7;
+        if (sizeof(T) == 2)
+            return (((r & 3) | (r >> 1 & 4)) & (TILE / 16 - 1)) << 1;
+        return 0;
+    }
+    static __device__ __forceinline__ unsigned my_row() { return threadIdx.x / kPerRow; }
+    static __device__ __forceinline__ int my_col()
+    {
+        return (int)((threadIdx.x % kPerRow) ^ turn(my_row())) * V;
+    }
+
+    // This workgroup's tiles of a matrix, from tile row (or column) t0 on.
+    struct Source {
+        Matrix<T> m;
+        unsigned t0;
+    };
+    // First column of the step at depth k, columns from there on, and its window.
+    static __device__ __forceinline__ int cols_left(const Source &s, unsigned k)
+    {
+        return s.m.cols - (int)(DEEP ? k : s.t0);
+    }
+    static __device__ __forceinline__ int first_col(const Source &s, unsigned k)
+    {
+        return (int)(DEEP ? k : s.t0);
+    }
+    // `back`: elements in front of the step's first column to see as well
+    static __device__ __forceinline__ Window view(const Source &s, const T *p, long long stride,
+                                                  unsigned k, int back = 0)
+    {
+        return window(p, stride, s.m.rows, s.m.cols, DEEP ? s.t0 : k, first_col(s, k) - back);
+    }
+
+    // Starts the loads of the step at depth k.
+    static __device__ __forceinline__ void load(S &s, const Source &src, unsigned k)
+    {
+        const int left = cols_left(src, k);
+        const int col = my_col();
+        if (src.m.cols >= V) {
+            // a chunk that reaches over its row's end is read where it ends with it
+            const int back = first_col(src, k) > 0 ? V : 0;
+            const unsigned c = (unsigned)(back + (col + V <= left ? col : left - V));
+            const unsigned row_bytes = (unsigned)src.m.stride * sizeof(T);
+            const Window w = view(src, src.m.p, src.m.stride, k, back);
+            const unsigned offset = my_row() * row_bytes + c * (unsigned)sizeof(T);
+#pragma unroll
+            for (int i = 0; i < kShare; ++i)
+                s.x[i] = read16(w, offset + i * kRowStep * row_bytes);
+            if (MASK) {
+                const unsigned mask_bytes = (unsigned)src.m.mask_stride * sizeof(T);
+                const Window y = view(src, src.m.mask, src.m.mask_stride, k, back);
+                const unsigned at = my_row() * mask_bytes + c * (unsigned)sizeof(T);
+#pragma unroll
+                for (int i = 0; i < kShare; ++i)
+                    s.y[i] = read16(y, at + i * kRowStep * mask_bytes);
+            }
+            return;
+        }
+        // rows shorter than 16 bytes
+        const unsigned row0 = (DEEP ? src.t0 : k) + my_row();
+#pragma unroll
+        for (int i = 0; i < kShare; ++i) {
+            const unsigned r = row0 + i * kRowStep;
+            const bool in = r < src.m.rows && col == 0 && left == src.m.cols;
+            unsigned x[V] = {}, y[V] = {};
+#pragma unroll
+            for (int e = 0; e < V; ++e)
+                if (in && e < src.m.cols) {
+                    x[e] = bits(src.m.p[r * src.m.stride + e]);
+                    if (MASK)
+                        y[e] = bits(src.m.mask[r * src.m.mask_stride + e]);
+                }
+            s.x[i] = pack(x);
+            if (MASK)
+                s.y[i] = pack(y);
+        }
+    }
+    static __device__ __forceinline__ unsigned bits(float x) { return __float_as_uint(x); }
+    static __device__ __forceinline__ unsigned bits(__bf16 x) { return __builtin_bit_cast(unsigned short, x); }
+    static __device__ __forceinline__ u32x4 pack(const unsigned (&x)[V])
+    {
+        u32x4 v;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-            c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[i * 4 + q], b[i * 4 + q], c, 0, 0, 0);
-        return c;
+            v[i] = V == 4 ? x[i] : x[2 * i] | x[(2 * i + 1) % V] << 16;
+        return v;
+    }
+
+    // What was loaded, zero outside the matrix and where its mask says so.
+    static __device__ __forceinline__ void settle(S &s, const Source &src, unsigned k)
+    {
+        if (MASK)
+#pragma unroll
+            for (int i = 0; i < kShare; ++i)
+                s.x[i] = where_positive(s.x[i], s.y[i], T{});
+        const int left = cols_left(src, k);
+        if (left < (DEEP ? D : TILE) && src.m.cols >= V) {
+            const int over = my_col() + V - left;
+            if (over > 0)
+#pragma unroll
+                for (int i = 0; i < kShare; ++i)
+                    s.x[i] = drop_first<T>(s.x[i], over);
+        }
+    }
+    static __device__ __forceinline__ void store(const S &s, char *lds)
+    {
+#pragma unroll
+        for (int i = 0; i < kShare; ++i)
+            *reinterpret_cast<u32x4 *>(lds + (threadIdx.x + i * THREADS) * 16) = s.x[i];
+    }
+
+    // The same without registers in between: for matrices without a mask whose
+    // rows start at multiples of 16 bytes and are as long.
+    static __device__ __forceinline__ void load_async(const Source &src, unsigned k, char *lds)
+    {
+        const Window w = view(src, src.m.p, src.m.stride, k);
+        const int col = my_col();
+        const unsigned row_bytes = (unsigned)src.m.stride * sizeof(T);
+        const bool in = col < cols_left(src, k);
+        const unsigned offset = my_row() * row_bytes + (unsigned)col * (unsigned)sizeof(T);
+#pragma unroll
+        for (int i = 0; i < kShare; ++i)
+            read16_to_lds(w, in ? offset + i * kRowStep * row_bytes : kOutside,
+                          lds + (uniform(threadIdx.x & ~63u) + i * THREADS) * 16);
+    }
+
+    // 16-byte chunk `c` of row `r`, in bytes.
+    static __device__ __forceinline__ unsigned at(unsigned r, unsigned c)
+    {
+        return (r * kPerRow + (c ^ turn(r))) * 16;
+    }
+
+    // The matrix unit's operand: tile rows [32 f, 32 f + 32), step `k` of four.
+    // bf16: 16 deep, 8 side by side a lane.  float: 8 deep, lane half h has depths
+    // 8 k + 4 h + (0 .. 3): the unit takes them two (one of each half) at a time.
+    static __device__ __forceinline__ u32x4 fragment(const char *lds, int f, int k)
+    {
+        const int lane = threadIdx.x & 63;
+        if (DEEP)
+            return *reinterpret_cast<const u32x4 *>(lds + at(f * 32 + (lane & 31), k * 2 + (lane >> 5)));
+        if constexpr (sizeof(T) == 2) {
+            // a group of 16 lanes reads 4 rows of 16 elements and gets them by columns
+            const int group = lane >> 4, l = lane & 15;
+            const unsigned r = k * 16 + (group >> 1) * 8 + (l >> 2);
+            const unsigned e = f * 32 + (group & 1) * 16 + (l & 3) * 4;
+            typedef __attribute__((address_space(3))) i16x4 *Lds;
+            const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(lds + at(r, e / 8) + (e & 4) * 2));
+            const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(lds + at(r + 4, e / 8) + (e & 4) * 2));
+            return __builtin_bit_cast(u32x4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+        } else {
+            u32x4 x;
+            const unsigned e = f * 32 + (lane & 31);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                x[j] = *reinterpret_cast<const unsigned *>(
+                    lds + at(k * 8 + (lane >> 5) * 4 + j, e / 4) + (e & 3) * 4);
+            return x;
+        }
     }
 };
 
-// C[m][n] = sum_k A(m, k) B(n, k) over a 64 x 64 tile, four waves of 16 rows.
-template <class T, class LoadA, class LoadB>
-__device__ __forceinline__ void tile_product(unsigned depth, LoadA load_a, LoadB load_b,
-                                             T (*As)[Kind<T>::kDepth + 8], T (*Bs)[Kind<T>::kDepth + 8],
-                                             f32x4 (&acc)[4], float *row_sum)
+__device__ __forceinline__ f32x16 multiply(u32x4 p, u32x4 q, f32x16 c, __bf16)
 {
-    constexpr int kDepth = Kind<T>::kDepth;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    for (unsigned k0 = 0; k0 < depth; k0 += kDepth) {
-        for (int i = threadIdx.x; i < kTile * kDepth; i += kThreads) {
-            const int r = i / kDepth, k = i % kDepth;
-            As[r][k] = k0 + k < depth ? load_a(r, k0 + k) : (T)0.0f;
-            Bs[r][k] = k0 + k < depth ? load_b(r, k0 + k) : (T)0.0f;
-        }
-        __syncthreads();
-        const T *a = As[wave * 16 + (lane & 15)];
+    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, p),
+                                                   __builtin_bit_cast(bf16x8, q), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 multiply(u32x4 p, u32x4 q, f32x16 c, float)
+{
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            acc[j] = Kind<T>::step(a, Bs[j * 16 + (lane & 15)], lane >> 4, acc[j]);
-        if (row_sum && threadIdx.x < kTile)
-            for (int k = 0; k < kDepth; ++k)
-                *row_sum += (float)As[threadIdx.x][k];
-        __syncthreads();
+    for (int j = 0; j < 4; ++j)
+        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(p[j]), __uint_as_float(q[j]), c, 0, 0, 0);
+    return c;
+}
+
+// Sizes of a product: a workgroup's tile TP x TQ, by WP x WQ waves.
+// ASYNC: operands go from memory to LDS by themselves (see load_async).  EACH_P:
+// tile_product shows its caller the P tiles.
+template <class T_, int TP_, int TQ_, int WP_, int WQ_, bool DEEP_P, bool DEEP_Q, bool MASK_P,
+          bool MASK_Q, bool ASYNC = false, bool EACH_P = false>
+struct Product {
+    using T = T_;
+    static constexpr int TP = TP_, TQ = TQ_, WP = WP_, WQ = WQ_;
+    static constexpr int kThreads = WP * WQ * 64;
+    static constexpr int kDepth = Type<T>::kDepth;
+    static constexpr bool kAsync = ASYNC, kEachP = EACH_P;
+    using P = Tile<T, TP, DEEP_P, kThreads, MASK_P>;
+    using Q = Tile<T, TQ, DEEP_Q, kThreads, MASK_Q>;
+    static constexpr int FP = TP / WP / 32, FQ = TQ / WQ / 32;  // a wave's 32 x 32 results
+    static constexpr int kStage = P::kBytes + Q::kBytes;
+    static_assert(FP * WP * 32 == TP && FQ * WQ * 32 == TQ, "whole results a wave");
+};
+
+// acc += P(p, k) Q(q, k) over one step's tiles in LDS.
+template <class C>
+__device__ __forceinline__ void step_product(const char *lds, int fp, int fq, f32x16 (&acc)[C::FP][C::FQ])
+{
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+        u32x4 p[C::FP], q[C::FQ];
+#pragma unroll
+        for (int i = 0; i < C::FP; ++i)
+            p[i] = C::P::fragment(lds, fp + i, s);
+#pragma unroll
+        for (int j = 0; j < C::FQ; ++j)
+            q[j] = C::Q::fragment(lds + C::P::kBytes, fq + j, s);
+#pragma unroll
+        for (int i = 0; i < C::FP; ++i)
+#pragma unroll
+            for (int j = 0; j < C::FQ; ++j)
+                acc[i][j] = multiply(p[i], q[j], acc[i][j], typename C::T{});
     }
 }
 
-// y = act(x W^T + b) (BACK = false), or dx = dz W (BACK = true).
-template <class T, bool BACK>
-__global__ __launch_bounds__(kThreads) void rows_kernel(Problem p, const T *x, long long xs,
-                                                        const T *w, const float *bias, bool relu,
-                                                        const T *mask, long long ms, T *y,
-                                                        long long ys)
+// acc = sum over `depth` of P(p, k) Q(q, k); each_p(share): called with each of
+// the P tiles that this thread brings to LDS.  lds: 2 * kStage bytes.
+template <class C, class EachP>
+__device__ __forceinline__ void tile_product(const Matrix<typename C::T> &mp, unsigned p0,
+                                             const Matrix<typename C::T> &mq, unsigned q0,
+                                             unsigned depth, char *lds,
+                                             f32x16 (&acc)[C::FP][C::FQ], EachP each_p)
 {
-    __shared__ T As[kTile][Kind<T>::kDepth + 8], Bs[kTile][Kind<T>::kDepth + 8];
-    __shared__ TileRows found;
-    __shared__ unsigned tmp[4];
-    const int depth = BACK ? p.fan_out : p.fan_in, width = BACK ? p.fan_in : p.fan_out;
-    const int n0 = blockIdx.y * kTile;
-  for (unsigned tile = blockIdx.x;; tile += gridDim.x) {
-    const TileRows t = find_tile(p, tile, kTile, &found, tmp);
-    if (t.head > p.heads)
+    const int wave = uniform(threadIdx.x >> 6);
+    const int fp = (wave % C::WP) * C::FP, fq = (wave / C::WP) * C::FQ;
+    const typename C::P::Source p = {mp, p0};
+    const typename C::Q::Source q = {mq, q0};
+    if (depth == 0)
         return;
-    f32x4 acc[4] = {};
-    const bool headed = t.head < p.heads;
-    if (headed) {
-        const T *wh = w + (size_t)t.head * p.fan_out * p.fan_in;
-        tile_product<T>(
-            depth,
-            [&](int r, int k) -> T {
-                if (t.first + r >= t.last)
-                    return (T)0.0f;
-                if (BACK && mask && !((float)mask[(t.first + r) * ms + k] > 0.0f))
-                    return (T)0.0f;
-                return x[(t.first + r) * xs + k];
-            },
-            [&](int r, int k) -> T {
-                if (n0 + r >= width)
-                    return (T)0.0f;
-                return BACK ? wh[(size_t)k * p.fan_in + n0 + r] : wh[(size_t)(n0 + r) * p.fan_in + k];
-            },
-            As, Bs, acc, nullptr);
-    }
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    for (int j = 0; j < 4; ++j) {
-        const int n = n0 + j * 16 + (lane & 15);
-        for (int i = 0; i < 4; ++i) {
-            const unsigned r = t.first + wave * 16 + (lane >> 4) * 4 + i;
-            if (r >= t.last || n >= width)
-                continue;
-            float v = acc[j][i];
-            if (!BACK && headed) {
-                if (bias)
-                    v += bias[(size_t)t.head * width + n];
-                if (relu)
-                    v = v < 0.0f ? 0.0f : v;
+    if constexpr (C::kAsync) {
+        auto load = [&](unsigned k, char *to) {
+            C::P::load_async(p, k, to);
+            C::Q::load_async(q, k, to + C::P::kBytes);
+        };
+        load(0, lds);
+        async_done();
+        unsigned stage = 0;
+        for (unsigned k = 0; k < depth; k += C::kDepth) {
+            const char *from = lds + stage * C::kStage;
+            stage ^= 1;
+            if (k + C::kDepth < depth)
+                load(k + C::kDepth, lds + stage * C::kStage);
+            if constexpr (C::kEachP) {
+                typename C::P::S share;
+#pragma unroll
+                for (int i = 0; i < C::P::kShare; ++i)
+                    share.x[i] = *reinterpret_cast<const u32x4 *>(from + (threadIdx.x + i * C::kThreads) * 16);
+                each_p(share);
             }
-            y[r * ys + n] = (T)v;
+            step_product<C>(from, fp, fq, acc);
+            async_done();
+        }
+    } else {
+        typename C::P::S sp;
+        typename C::Q::S sq;
+        auto load = [&](unsigned k) {
+            C::P::load(sp, p, k);
+            C::Q::load(sq, q, k);
+        };
+        auto bring = [&](unsigned k, char *to) {
+            C::P::settle(sp, p, k);
+            C::Q::settle(sq, q, k);
+            if constexpr (C::kEachP)
+                each_p(sp);
+            C::P::store(sp, to);
+            C::Q::store(sq, to + C::P::kBytes);
+        };
+        load(0);
+        bring(0, lds);
+        __syncthreads();
+        unsigned stage = 0;
+        for (unsigned k = 0; k < depth; k += C::kDepth) {
+            const unsigned next = k + C::kDepth;
+            if (next < depth)
+                load(next);
+            step_product<C>(lds + stage * C::kStage, fp, fq, acc);
+            stage ^= 1;
+            if (next < depth)
+                bring(next, lds + stage * C::kStage);
+            __syncthreads();
         }
     }
-  }
 }
 
-// dW[o][i] = sum_r dz[r][o] x[r][i] of head blockIdx.z, and db[o] = sum_r dz[r][o].
-template <class T>
-__global__ __launch_bounds__(kThreads) void weights_kernel(Problem p, const T *dy, long long ds,
-                                                           const T *x, long long xs, const T *mask,
-                                                           long long ms, float *dw, float *db)
+// ---- rows: the layer, and its rows' gradient --------------------------------------
+
+// A wave's results as rows of 32 FP elements: a lane has, of row 32 j + (lane &
+// 31) of Q, elements 8 i + 4 (lane >> 5) + (0 .. 3) of each 32 of P.  They go
+// through LDS to be written in 16-byte pieces.  Bytes of a row there (8 of 64
+// banks further on for the next row):
+template <class C>
+constexpr int kResultRow = C::FP * 32 * (int)sizeof(typename C::T) + 16;
+template <class C>
+constexpr int kResultBytes = C::WP * C::WQ * 32 * kResultRow<C>;
+template <class C>
+constexpr int kRowsLds = 2 * C::kStage > kResultBytes<C> ? 2 * C::kStage : kResultBytes<C>;
+
+__device__ __forceinline__ void store_values(char *to, const float (&v)[4], __bf16)
 {
-    __shared__ T As[kTile][Kind<T>::kDepth + 8], Bs[kTile][Kind<T>::kDepth + 8];
-    const int h = blockIdx.z, m0 = blockIdx.y * kTile, n0 = blockIdx.x * kTile;
-    const unsigned first = bound(p, h), last = bound(p, h + 1);
-    f32x4 acc[4] = {};
-    float sum = 0.0f;
-    tile_product<T>(
-        last > first ? last - first : 0,
-        [&](int m, unsigned k) -> T {
-            if (m0 + m >= p.fan_out)
-                return (T)0.0f;
-            if (mask && !((float)mask[(first + k) * ms + m0 + m] > 0.0f))
-                return (T)0.0f;
-            return dy[(first + k) * ds + m0 + m];
-        },
-        [&](int n, unsigned k) -> T {
-            return dw && n0 + n < p.fan_in ? x[(first + k) * xs + n0 + n] : (T)0.0f;
-        },
-        As, Bs, acc, db && n0 == 0 ? &sum : nullptr);
+    union {
+        __bf16 e[4];
+        unsigned long long u;
+    } x;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+        x.e[i] = (__bf16)v[i];
+    *reinterpret_cast<unsigned long long *>(to) = x.u;
+}
+__device__ __forceinline__ void store_values(char *to, const float (&v)[4], float)
+{
+    *reinterpret_cast<f32x4 *>(to) = f32x4{v[0], v[1], v[2], v[3]};
+}
+
+// P: the weights (width columns of the result), Q: rows.
+template <class C>
+__global__ __launch_bounds__(C::kThreads) void rows_kernel(
+    Problem p, Matrix<typename C::T> w, Matrix<typename C::T> x, const float *bias, int relu,
+    typename C::T *y, long long ys, int width, int depth, unsigned long long from)
+{
+    using T = typename C::T;
+    constexpr int V = Type<T>::kVec;
+    __shared__ __attribute__((aligned(16))) char lds[kRowsLds<C>];
+    __shared__ unsigned tmp[4];
+    __shared__ RowTile found;
+    const Spread s = spread_tiles(p, C::TQ, tmp);
+    const unsigned headless = bound(p, p.heads);
+    const unsigned tail = (unsigned)(((unsigned long long)(p.rows - headless) + C::TQ - 1) / C::TQ);
+    const unsigned row_tiles = s.total + tail, col_tiles = (width + C::TP - 1) / C::TP;
+    const unsigned long long all = (unsigned long long)row_tiles * col_tiles;
+    const size_t head_size = (size_t)p.fan_in * p.fan_out;
+    const unsigned long long at = by_xcd(from + blockIdx.x, all);
+    if (at >= all)
+        return;
+    const Place2 where = in_groups(at, row_tiles, col_tiles);
+    const unsigned tile = where.a;
+    const int n0 = (int)where.b * C::TP;
+    RowTile t;
+    if (tile < s.total) {
+        t = head_tile(s, tile, C::TQ, &found);
+    } else {
+        t.first = headless + (tile - s.total) * C::TQ;
+        t.last = p.rows - t.first > (unsigned)C::TQ ? t.first + C::TQ : p.rows;
+        t.head = p.heads;
+    }
+    const bool headed = t.head < p.heads;
+    f32x16 acc[C::FP][C::FQ] = {};
+    if (headed) {
+        Matrix<T> wh = w, xh = x;
+        wh.p += t.head * head_size;
+        xh.p += t.first * xh.stride;
+        xh.mask += t.first * xh.mask_stride;
+        xh.rows = t.last - t.first;
+        tile_product<C>(wh, n0, xh, 0, depth, lds, acc, [](auto &) {});
+    }
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    if (dw)
-        for (int j = 0; j < 4; ++j)
-            for (int i = 0; i < 4; ++i) {
-                const int m = m0 + wave * 16 + (lane >> 4) * 4 + i, n = n0 + j * 16 + (lane & 15);
-                if (m < p.fan_out && n < p.fan_in)
-                    dw[((size_t)h * p.fan_out + m) * p.fan_in + n] = acc[j][i];
+    const int wp = (wave % C::WP) * C::FP * 32, wq = (wave / C::WP) * C::FQ * 32;
+    char *mine = lds + wave * 32 * kResultRow<C>;
+    const float *bh = bias && headed ? bias + (size_t)t.head * width : nullptr;
+#pragma unroll
+    for (int j = 0; j < C::FQ; ++j) {
+#pragma unroll
+        for (int i = 0; i < C::FP; ++i)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const int e = i * 32 + q * 8 + (lane >> 5) * 4;
+                float v[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    v[k] = acc[i][j][q * 4 + k];
+                    if (bh && n0 + wp + e + k < width)
+                        v[k] += bh[n0 + wp + e + k];
+                    if (relu)
+                        v[k] = v[k] < 0.0f ? 0.0f : v[k];
+                }
+                store_values(mine + (lane & 31) * kResultRow<C> + e * sizeof(T), v, T{});
             }
-    if (db && n0 == 0 && threadIdx.x < kTile && m0 + (int)threadIdx.x < p.fan_out)
-        db[(size_t)h * p.fan_out + m0 + threadIdx.x] = sum;
+        __builtin_amdgcn_wave_barrier();
+        constexpr int kPieces = C::FP * 32 / V;  // of a row
+#pragma unroll
+        for (int i = 0; i < 32 * kPieces / 64; ++i) {
+            const int r = (i * 64 + lane) / kPieces, c = (i * 64 + lane) % kPieces * V;
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(mine + r * kResultRow<C> + c * sizeof(T));
+            const unsigned row = t.first + wq + j * 32 + r;
+            const int n = n0 + wp + c;
+            if (row >= t.last || n >= width)
+                continue;
+            T *to = y + (row * ys + n);
+            if (n + V <= width) {
+                reinterpret_cast<Bytes16 *>(to)->v = v;
+            } else {
+                union {
+                    u32x4 v;
+                    T e[V];
+                } piece = {v};
+#pragma unroll
+                for (int k = 0; k < V; ++k)
+                    if (n + k < width)
+                        to[k] = piece.e[k];
+            }
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
 }
 
-unsigned tiles(int n) { return (unsigned)((n + kTile - 1) / kTile); }
+// ---- weights ----------------------------------------------------------------------
 
-// Tiles of rows: each head's last one may be partly filled, and so may the last
-// of the rows without a head.
-unsigned row_tiles(const LinearShape &sh)
+// P: dz, Q: x, reduced over rows: a tile of a head's dW from a stretch of
+// `stretch` of its rows.  Where heads have more than one stretch (partial),
+// each has a place of its own in dw and db, and sum_kernel adds them up.
+template <class C>
+__global__ __launch_bounds__(C::kThreads) void weights_kernel(Problem p, Matrix<typename C::T> dz,
+                                                              Matrix<typename C::T> x, float *dw,
+                                                              float *db, unsigned stretch,
+                                                              bool partial, unsigned places,
+                                                              unsigned row_tiles, unsigned col_tiles,
+                                                              unsigned long long from)
 {
-    const unsigned n = sh.rows / kTile + sh.heads + 1;
-    return n < (1u << 20) ? n : 1u << 20;
+    using T = typename C::T;
+    constexpr int V = Type<T>::kVec;
+    __shared__ __attribute__((aligned(16))) char lds[2 * C::kStage];
+    __shared__ unsigned tmp[4];
+    __shared__ RowTile found;
+    const int I = p.fan_in, O = p.fan_out;
+    const unsigned each = row_tiles * col_tiles;  // of a place
+    const unsigned long long at = by_xcd(from + blockIdx.x, (unsigned long long)places * each);
+    const unsigned place = (unsigned)(at / each);
+    if (place >= places)
+        return;
+    const Place2 where = in_groups(at - (unsigned long long)place * each, row_tiles, col_tiles);
+    const int m0 = (int)where.a * C::TP, n0 = (int)where.b * C::TQ;
+    RowTile t;
+    if (partial) {
+        const Spread s = spread_tiles(p, stretch, tmp);
+        if (place >= s.total)
+            return;
+        t = head_tile(s, place, stretch, &found);
+    } else {
+        t.first = uniform(bound(p, place));
+        t.last = uniform(bound(p, place + 1));
+        t.last = t.last > t.first ? t.last : t.first;
+    }
+    Matrix<T> mz = dz, mx = x;
+    mz.p += t.first * mz.stride;
+    mz.mask += t.first * mz.mask_stride;
+    mx.p += t.first * mx.stride;
+    mz.rows = mx.rows = t.last - t.first;
+    const bool sum = db && n0 == 0;
+    float sums[V] = {};
+    f32x16 acc[C::FP][C::FQ] = {};
+    tile_product<C>(mz, m0, mx, n0, mz.rows, lds, acc, [&](const typename C::P::S &share) {
+        if (!sum)
+            return;
+#pragma unroll
+        for (int i = 0; i < C::P::kShare; ++i) {
+            union {
+                u32x4 v;
+                T e[V];
+            } piece = {share.x[i]};
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                sums[k] += (float)piece.e[k];
+        }
+    });
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int wp = (wave % C::WP) * C::FP * 32, wq = (wave / C::WP) * C::FQ * 32;
+    if (dw) {
+        float *to = dw + (size_t)place * O * I;
+#pragma unroll
+        for (int i = 0; i < C::FP; ++i)
+#pragma unroll
+            for (int j = 0; j < C::FQ; ++j)
+#pragma unroll
+                for (int q = 0; q < 16; ++q) {
+                    const int m = m0 + wp + i * 32 + (q >> 2) * 8 + (lane >> 5) * 4 + (q & 3);
+                    const int n = n0 + wq + j * 32 + (lane & 31);
+                    if (m < O && n < I)
+                        to[(size_t)m * I + n] = acc[i][j][q];
+                }
+    }
+    if (sum) {
+        // a thread's sums are over every (threads / kPerRow)-th row of its columns
+        constexpr int kRowsOfThreads = C::kThreads / C::P::kPerRow;
+        float(*part)[C::TP + 1] = reinterpret_cast<float(*)[C::TP + 1]>(lds);
+        static_assert(sizeof(float) * kRowsOfThreads * (C::TP + 1) <= 2 * C::kStage, "fits");
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            part[C::P::my_row()][C::P::my_col() + k] = sums[k];
+        __syncthreads();
+        for (int m = threadIdx.x; m < C::TP; m += C::kThreads) {
+            float v = 0.0f;
+            for (int r = 0; r < kRowsOfThreads; ++r)
+                v += part[r][m];
+            if (m0 + m < O)
+                db[(size_t)place * O + m0 + m] = v;
+        }
+    }
 }
+
+// out[h][e] = the sum of head h's stretches' parts, in order.
+__global__ __launch_bounds__(256) void sum_kernel(Problem p, unsigned stretch, const float *parts,
+                                                  size_t size, float *out)
+{
+    __shared__ unsigned tmp[4];
+    __shared__ unsigned range[2];
+    const Spread s = spread_tiles(p, stretch, tmp);
+    if (threadIdx.x == blockIdx.y) {
+        range[0] = s.before;
+        range[1] = s.before + s.mine;
+    }
+    __syncthreads();
+    const unsigned a = range[0], b = range[1];
+    for (size_t e = blockIdx.x * 256 + threadIdx.x; e < size; e += (size_t)gridDim.x * 256) {
+        float v = 0.0f;
+        for (unsigned i = a; i < b; ++i)
+            v += parts[i * size + e];
+        out[blockIdx.y * size + e] = v;
+    }
+}
+
+// ---- choice of a form ---------------------------------------------------------------
+
+constexpr unsigned kMostGroups = 1u << 22;  // workgroups of a launch
+
+unsigned tiles_of(long long n, int tile) { return (unsigned)((n + tile - 1) / tile); }
+
+template <class C>
+hipError_t launch_rows(const Problem &p, const Matrix<typename C::T> &w,
+                       const Matrix<typename C::T> &x, const float *bias, bool relu, Rows y,
+                       int width, int depth, hipStream_t s)
+{
+    using T = typename C::T;
+    // at most: every head's last tile and the headless rows' may be partly filled
+    unsigned long long all = ((unsigned long long)p.rows / C::TQ + p.heads + 1) * tiles_of(width, C::TP);
+    all += kXcds * kRun;
+    for (unsigned long long from = 0; from < all; from += kMostGroups)
+        rows_kernel<C><<<(unsigned)(all - from < kMostGroups ? all - from : kMostGroups), C::kThreads, 0, s>>>(
+            p, w, x, bias, relu, static_cast<T *>(const_cast<void *>(y.p)), y.stride, width, depth, from);
+    return hipGetLastError();
+}
+
+// Whether an operand can go from memory to LDS by itself (Tile::load_async).
+template <class T>
+bool goes_alone(const Matrix<T> &m)
+{
+    return !m.mask && reinterpret_cast<uintptr_t>(m.p) % 16 == 0 && m.stride % Type<T>::kVec == 0 &&
+           m.cols % Type<T>::kVec == 0;
+}
+
+// The rows' product with tiles for its width.
+template <class T, bool DEEP_W, bool MASK>
+hipError_t rows_product(const Problem &p, const Matrix<T> &w, const Matrix<T> &x, const float *bias,
+                        bool relu, Rows y, int width, int depth, hipStream_t s)
+{
+    const bool alone = goes_alone(w) && goes_alone(x);
+    if constexpr (sizeof(T) == 2)
+        if (width > 128 && (unsigned long long)p.rows * tiles_of(width, 256) >= 256 * 128) {
+            if constexpr (!MASK)
+                if (alone)
+                    return launch_rows<Product<T, 256, 256, 4, 2, DEEP_W, true, false, false, true>>(
+                        p, w, x, bias, relu, y, width, depth, s);
+            return launch_rows<Product<T, 256, 256, 4, 2, DEEP_W, true, false, MASK>>(
+                p, w, x, bias, relu, y, width, depth, s);
+        }
+    if (width > 64) {
+        if constexpr (!MASK)
+            if (alone)
+                return launch_rows<Product<T, 128, 128, 2, 2, DEEP_W, true, false, false, true>>(
+                    p, w, x, bias, relu, y, width, depth, s);
+        return launch_rows<Product<T, 128, 128, 2, 2, DEEP_W, true, false, MASK>>(
+            p, w, x, bias, relu, y, width, depth, s);
+    }
+    return launch_rows<Product<T, 64, 128, 2, 2, DEEP_W, true, false, MASK>>(p, w, x, bias, relu, y,
+                                                                             width, depth, s);
+}
+
+// Rows of a stretch of the weights' product, 0: each head as a whole.  Split
+// until 512 workgroups (2 a compute unit) have work.
+struct Split {
+    unsigned stretch, places;
+};
+Split split_rows(unsigned rows, int heads, int fan_in, int fan_out)
+{
+    const unsigned long long tiles =
+        (unsigned long long)tiles_of(fan_in, fan_in > 64 ? 128 : 64) * tiles_of(fan_out, fan_out > 64 ? 128 : 64);
+    const unsigned long long want = 512 / tiles;
+    if (want <= (unsigned)heads)
+        return {0, (unsigned)heads};
+    unsigned stretch = (unsigned)(rows / (want - heads));
+    stretch = (stretch + 255) / 256 * 256;
+    if (stretch < 256)
+        stretch = 256;
+    return {stretch, rows / stretch + heads};
+}
+
+template <class C>
+hipError_t launch_weights(const Problem &p, const Matrix<typename C::T> &dz,
+                          const Matrix<typename C::T> &x, float *dw, float *db, char *workspace,
+                          hipStream_t s)
+{
+    const Split split = split_rows(p.rows, p.heads, p.fan_in, p.fan_out);
+    const bool partial = split.stretch != 0;
+    const size_t size = (size_t)p.fan_in * p.fan_out;
+    float *wparts = reinterpret_cast<float *>(workspace);
+    float *bparts = wparts + (size_t)split.places * size;
+    float *to_w = dw ? (partial ? wparts : dw) : nullptr, *to_b = db ? (partial ? bparts : db) : nullptr;
+    const unsigned row_tiles = tiles_of(p.fan_out, C::TP), col_tiles = dw ? tiles_of(p.fan_in, C::TQ) : 1;
+    const unsigned long long all = (unsigned long long)split.places * row_tiles * col_tiles + kXcds * kRun;
+    for (unsigned long long from = 0; from < all; from += kMostGroups)
+        weights_kernel<C><<<(unsigned)(all - from < kMostGroups ? all - from : kMostGroups), C::kThreads, 0, s>>>(
+            p, dz, x, to_w, to_b, split.stretch, partial, split.places, row_tiles, col_tiles, from);
+    if (partial) {
+        if (dw) {
+            const unsigned blocks = tiles_of(size, 256);
+            sum_kernel<<<dim3(blocks < 1024 ? blocks : 1024, p.heads), 256, 0, s>>>(p, split.stretch, wparts, size, dw);
+        }
+        if (db)
+            sum_kernel<<<dim3(tiles_of(p.fan_out, 256), p.heads), 256, 0, s>>>(p, split.stretch, bparts, p.fan_out, db);
+    }
+    return hipGetLastError();
+}
+
+template <class T, bool MASK>
+hipError_t weights_product(const Problem &p, const Matrix<T> &dz, const Matrix<T> &x, float *dw,
+                           float *db, char *workspace, hipStream_t s)
+{
+    const bool wide_o = p.fan_out > 64, wide_i = p.fan_in > 64;
+    const bool alone = goes_alone(dz) && goes_alone(x);
+    if constexpr (sizeof(T) == 2)
+        if (p.fan_out > 128 && p.fan_in > 128 &&
+            (unsigned long long)tiles_of(p.fan_out, 256) * tiles_of(p.fan_in, 256) * p.heads >= 256) {
+            if constexpr (!MASK)
+                if (alone)
+                    return launch_weights<Product<T, 256, 256, 4, 2, false, false, false, false, true, true>>(
+                        p, dz, x, dw, db, workspace, s);
+            return launch_weights<Product<T, 256, 256, 4, 2, false, false, MASK, false, false, true>>(p, dz, x, dw, db, workspace, s);
+        }
+    if constexpr (!MASK)
+        if (wide_o && wide_i && alone)
+            return launch_weights<Product<T, 128, 128, 2, 2, false, false, false, false, true, true>>(
+                p, dz, x, dw, db, workspace, s);
+    if (wide_o && wide_i)
+        return launch_weights<Product<T, 128, 128, 2, 2, false, false, MASK, false, false, true>>(p, dz, x, dw, db, workspace, s);
+    if (wide_o)
+        return launch_weights<Product<T, 128, 64, 2, 2, false, false, MASK, false, false, true>>(p, dz, x, dw, db, workspace, s);
+    if (wide_i)
+        return launch_weights<Product<T, 64, 128, 2, 2, false, false, MASK, false, false, true>>(p, dz, x, dw, db, workspace, s);
+    return launch_weights<Product<T, 64, 64, 2, 2, false, false, MASK, false, false, true>>(p, dz, x, dw, db, workspace, s);
+}
+
+Problem problem(const LinearShape &sh) { return {sh.offsets, sh.rows, sh.heads, sh.fan_in, sh.fan_out}; }
 
 template <class T>
 hipError_t forward(const LinearShape &sh, Rows x, const void *w, const float *bias, bool relu,
                    Rows y, hipStream_t s)
 {
-    const Problem p = {sh.offsets, sh.rows, sh.heads, sh.fan_in, sh.fan_out};
-    rows_kernel<T, false><<<dim3(row_tiles(sh), tiles(sh.fan_out)), kThreads, 0, s>>>(
-        p, static_cast<const T *>(x.p), x.stride, static_cast<const T *>(w), bias, relu, nullptr, 0,
-        static_cast<T *>(const_cast<void *>(y.p)), y.stride);
-    return hipGetLastError();
+    const Matrix<T> mw = {static_cast<const T *>(w), sh.fan_in, nullptr, 0, (unsigned)sh.fan_out, sh.fan_in};
+    const Matrix<T> mx = {static_cast<const T *>(x.p), x.stride, nullptr, 0, sh.rows, sh.fan_in};
+    return rows_product<T, true, false>(problem(sh), mw, mx, bias, relu, y, sh.fan_out, sh.fan_in, s);
 }
 
 template <class T>
 hipError_t backward(const LinearShape &sh, Rows dy, Rows x, const void *w, Rows y, Rows dx,
-                    float *dw, float *db, hipStream_t s)
+                    float *dw, float *db, char *workspace, hipStream_t s)
 {
-    const Problem p = {sh.offsets, sh.rows, sh.heads, sh.fan_in, sh.fan_out};
-    const T *dyp = static_cast<const T *>(dy.p), *yp = static_cast<const T *>(y.p);
-    if (dx.p && sh.rows > 0)
-        rows_kernel<T, true><<<dim3(row_tiles(sh), tiles(sh.fan_in)), kThreads, 0, s>>>(
-            p, dyp, dy.stride, static_cast<const T *>(w), nullptr, false, yp, y.stride,
-            static_cast<T *>(const_cast<void *>(dx.p)), dx.stride);
-    if (dw || db)
-        weights_kernel<T><<<dim3(dw ? tiles(sh.fan_in) : 1, tiles(sh.fan_out), sh.heads), kThreads, 0, s>>>(
-            p, dyp, dy.stride, static_cast<const T *>(x.p), x.stride, yp, y.stride, dw, db);
-    return hipGetLastError();
+    const Problem p = problem(sh);
+    const Matrix<T> mz = {static_cast<const T *>(dy.p), dy.stride, static_cast<const T *>(y.p), y.stride, sh.rows, sh.fan_out};
+    const Matrix<T> mw = {static_cast<const T *>(w), sh.fan_in, nullptr, 0, (unsigned)sh.fan_out, sh.fan_in};
+    Matrix<T> mx = {static_cast<const T *>(x.p), x.stride, nullptr, 0, sh.rows, sh.fan_in};
+    if (dx.p && sh.rows > 0) {
+        const hipError_t e =
+            y.p ? rows_product<T, false, true>(p, mw, mz, nullptr, false, dx, sh.fan_in, sh.fan_out, s)
+                : rows_product<T, false, false>(p, mw, mz, nullptr, false, dx, sh.fan_in, sh.fan_out, s);
+        if (e != hipSuccess)
+            return e;
+    }
+    if (!dw && !db)
+        return hipSuccess;
+    if (!dw) {  // nothing needs x: the product's other operand is any matrix of these rows
+        mx = mz;
+        mx.mask = nullptr;
+    }
+    return y.p ? weights_product<T, true>(p, mz, mx, dw, db, workspace, s)
+               : weights_product<T, false>(p, mz, mx, dw, db, workspace, s);
 }
 
 }  // namespace
@@ -267,14 +945,19 @@ hipError_t launch_heads_linear(const LinearShape &sh, Rows x, const void *w, con
     return bf16 ? forward<__bf16>(sh, x, w, bias, relu, y, s) : forward<float>(sh, x, w, bias, relu, y, s);
 }
 
-size_t heads_linear_workspace_bytes(unsigned, int, int, int, bool) { return 0; }
+size_t heads_linear_workspace_bytes(unsigned rows, int heads, int fan_in, int fan_out, bool)
+{
+    const Split split = split_rows(rows, heads, fan_in, fan_out);
+    return split.stretch ? (size_t)split.places * fan_out * ((size_t)fan_in + 1) * sizeof(float) : 0;
+}
 
 hipError_t launch_heads_linear_backward(const LinearShape &sh, Rows dy, Rows x, const void *w,
                                         Rows y, bool bf16, Rows dx, float *dw, float *db,
-                                        void *, hipStream_t s)
+                                        void *workspace, hipStream_t s)
 {
-    return bf16 ? backward<__bf16>(sh, dy, x, w, y, dx, dw, db, s)
-                : backward<float>(sh, dy, x, w, y, dx, dw, db, s);
+    char *ws = static_cast<char *>(workspace);
+    return bf16 ? backward<__bf16>(sh, dy, x, w, y, dx, dw, db, ws, s)
+                : backward<float>(sh, dy, x, w, y, dx, dw, db, ws, s);
 }
 
 }  // namespace derf

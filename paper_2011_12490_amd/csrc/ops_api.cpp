@@ -41,6 +41,15 @@ int check_rows(const char *name, const void *p, long long stride, int dim, int p
     return DERF_OK;
 }
 
+// The rows of a linear layer: a tile of them is read at 32-bit offsets.
+constexpr long long kMaxLayerStride = 1LL << 21;
+int check_layer_rows(const char *name, const void *p, long long stride, int dim, int precision)
+{
+    if (stride >= kMaxLayerStride)
+        return report(DERF_ERR_INVALID_ARG, "%s: stride %lld, a layer takes less than 2^21", name, stride);
+    return check_rows(name, p, stride, dim, precision);
+}
+
 int check_array(const char *name, const void *p, unsigned align)
 {
     if (!p)
@@ -202,12 +211,12 @@ int derf_heads_linear(const void *x, long long x_stride, const void *w, const fl
     TRY(check_linear(num_rows, num_heads, fan_in, fan_out, precision));
     if (num_rows == 0)
         return DERF_OK;
-    TRY(check_rows("x", x, x_stride, fan_in, precision));
+    TRY(check_layer_rows("x", x, x_stride, fan_in, precision));
     TRY(check_array("w", w, precision == DERF_PREC_BF16 ? 2 : 4));
     if (bias)
         TRY(check_array("bias", bias, 4));
     TRY(check_array("offsets", offsets, 4));
-    TRY(check_rows("y", y, y_stride, fan_out, precision));
+    TRY(check_layer_rows("y", y, y_stride, fan_out, precision));
     const LinearShape sh = {offsets, (unsigned)num_rows, num_heads, fan_in, fan_out};
     return launched(launch_heads_linear(sh, {x, x_stride}, w, bias, relu != 0,
                                         precision == DERF_PREC_BF16, {y, y_stride},
@@ -233,15 +242,15 @@ int derf_heads_linear_backward(const void *dy, long long dy_stride, const void *
 {
     TRY(check_linear(num_rows, num_heads, fan_in, fan_out, precision));
     if (num_rows > 0) {
-        TRY(check_rows("dy", dy, dy_stride, fan_out, precision));
+        TRY(check_layer_rows("dy", dy, dy_stride, fan_out, precision));
         if (y)
-            TRY(check_rows("y", y, y_stride, fan_out, precision));
+            TRY(check_layer_rows("y", y, y_stride, fan_out, precision));
         if (out_x) {
             TRY(check_array("w", w, precision == DERF_PREC_BF16 ? 2 : 4));
-            TRY(check_rows("out_x", out_x, out_x_stride, fan_in, precision));
+            TRY(check_layer_rows("out_x", out_x, out_x_stride, fan_in, precision));
         }
         if (out_w)
-            TRY(check_rows("x", x, x_stride, fan_in, precision));
+            TRY(check_layer_rows("x", x, x_stride, fan_in, precision));
     }
     if (out_w)
         TRY(check_array("out_w", out_w, 4));
