@@ -13,12 +13,68 @@ namespace derf {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kItem = 1024;  // values of a work item: a workgroup's share
+constexpr int kItem = 4096;  // values of a work item, a workgroup's: 4 blocks a wave
 
-__device__ __forceinline__ float load_value(const void *p, long long i, int precision)
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+
+// Four values of an array at i, converted to and from float.  WHOLE: all of
+// them are there and lie at a multiple of their size; else those below n, one by one.
+template <bool WHOLE, class T>
+__device__ __forceinline__ f32x4 read4(const void *p, long long i, long long n)
 {
-    return precision == DERF_PREC_BF16 ? (float)static_cast<const __bf16 *>(p)[i]
-                                       : static_cast<const float *>(p)[i];
+    typedef T Four __attribute__((ext_vector_type(4)));
+    const T *a = static_cast<const T *>(p) + i;
+    if constexpr (WHOLE)
+        return __builtin_convertvector(__builtin_nontemporal_load(reinterpret_cast<const Four *>(a)), f32x4);
+    f32x4 x = {0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (i + j < n)
+            x[j] = (float)a[j];
+    return x;
+}
+template <bool WHOLE, class T>
+__device__ __forceinline__ void write4(void *p, long long i, long long n, f32x4 x)
+{
+    typedef T Four __attribute__((ext_vector_type(4)));
+    T *a = static_cast<T *>(p) + i;
+    const Four y = __builtin_convertvector(x, Four);
+    if constexpr (WHOLE) {
+        __builtin_nontemporal_store(y, reinterpret_cast<Four *>(a));
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (i + j < n)
+            a[j] = y[j];
+}
+// The same for four codes, one in each byte.
+template <bool WHOLE>
+__device__ __forceinline__ unsigned read_codes(const void *p, long long i, long long n)
+{
+    const unsigned char *a = static_cast<const unsigned char *>(p) + i;
+    if constexpr (WHOLE)
+        return __builtin_nontemporal_load(reinterpret_cast<const unsigned *>(a));
+    unsigned x = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (i + j < n)
+            x |= (unsigned)a[j] << 8 * j;
+    return x;
+}
+template <bool WHOLE>
+__device__ __forceinline__ void write_codes(void *p, long long i, long long n, unsigned x)
+{
+    unsigned char *a = static_cast<unsigned char *>(p) + i;
+    if constexpr (WHOLE) {
+        __builtin_nontemporal_store(x, reinterpret_cast<unsigned *>(a));
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (i + j < n)
+            a[j] = (unsigned char)(x >> 8 * j);
 }
 
 // The tensor that work item `item` belongs to: the last whose first is <= item.
@@ -42,93 +98,120 @@ __device__ __forceinline__ float wave_max(float x)
     return x;
 }
 
-__device__ __forceinline__ float finite_abs(float x) { return isfinite(x) ? fabsf(x) : 0.0f; }
-
-// x / scale as an e4m3 code; is_root: a positive value keeps the smallest code.
-__device__ __forceinline__ unsigned char encode8(float x, float inv_scale, bool is_root)
+__device__ __forceinline__ float finite_abs(float x)
 {
-    if (!isfinite(x))
-        return 0x7F;
-    float q = fminf(fmaxf(x * inv_scale, -448.0f), 448.0f);
-    if (is_root && x > 0.0f)
-        q = fmaxf(q, 0x1p-9f);
-    return (unsigned char)(__builtin_amdgcn_cvt_pk_fp8_f32(q, 0.0f, 0, false) & 0xFF);
+    const float a = fabsf(x);
+    return a < INFINITY ? a : 0.0f;  // a NaN compares false
 }
 
-__device__ __forceinline__ float decode8(unsigned char c, float scale)
+// Four values over their block's scale as e4m3 codes (what is not finite: NaN);
+// is_root: a positive value keeps the smallest code.
+__device__ __forceinline__ unsigned encode8(f32x4 x, float inv_scale, bool is_root)
 {
-    return __builtin_amdgcn_cvt_f32_fp8((int)c, 0) * scale;
+    float q[4];
+    unsigned bad = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        q[j] = fminf(fmaxf(x[j] * inv_scale, -448.0f), 448.0f);
+        if (is_root && x[j] > 0.0f)
+            q[j] = fmaxf(q[j], 0x1p-9f);
+        if (!(fabsf(x[j]) < INFINITY))
+            bad |= 0x7Fu << 8 * j;
+    }
+    int c = __builtin_amdgcn_cvt_pk_fp8_f32(q[0], q[1], 0, false);
+    c = __builtin_amdgcn_cvt_pk_fp8_f32(q[2], q[3], c, true);
+    return (unsigned)c | bad;
+}
+__device__ __forceinline__ f32x4 decode8(unsigned c, float scale)
+{
+    return f32x4{__builtin_amdgcn_cvt_f32_fp8((int)c, 0) * scale, __builtin_amdgcn_cvt_f32_fp8((int)c, 1) * scale,
+                 __builtin_amdgcn_cvt_f32_fp8((int)c, 2) * scale, __builtin_amdgcn_cvt_f32_fp8((int)c, 3) * scale};
 }
 
-// One wave takes 256 values (a moment block), four a lane.
+// One wave's step on the 256 values from `base` on, four a lane.
+template <int BITS, bool WHOLE, class P, class G>
+__device__ __forceinline__ void step_block(const derf_adamw_tensor &t, long long base, const AdamWScalars &c,
+                                           float gs)
+{
+    const int lane = threadIdx.x & 63;
+    const long long i = base + lane * 4, n = t.n, block = base / kMomentBlock;
+    const f32x4 g = read4<WHOLE, G>(t.grad, i, n) * gs;
+    f32x4 p = read4<WHOLE, P>(t.param, i, n);
+    f32x4 m, v;
+    if (BITS == 8) {
+        const float ms = t.m_scale[block], vs = t.v_scale[block];
+        m = decode8(read_codes<WHOLE>(t.m, i, n), ms);
+        v = decode8(read_codes<WHOLE>(t.v, i, n), vs);
+        v = v * v;
+    } else {
+        m = read4<WHOLE, float>(t.m, i, n);
+        v = read4<WHOLE, float>(t.v, i, n);
+    }
+    m = m * c.beta1 + g * c.one_minus_beta1;
+    v = v * c.beta2 + (g * g) * c.one_minus_beta2;
+    f32x4 root;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        root[j] = sqrtf(v[j]);
+    p = p * c.decay - m / (root * c.root_scale + c.eps) * c.rate;
+    write4<WHOLE, P>(t.param, i, n, p);
+    if (t.copy)
+        write4<WHOLE, __bf16>(t.copy, i, n, p);
+    if (BITS == 32) {
+        write4<WHOLE, float>(t.m, i, n, m);
+        write4<WHOLE, float>(t.v, i, n, v);
+        return;
+    }
+    // lanes past the end have zeros
+    float mmax = 0.0f, rmax = 0.0f;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        mmax = fmaxf(mmax, finite_abs(m[j]));
+        rmax = fmaxf(rmax, finite_abs(root[j]));
+    }
+    const float ms = fmaxf(wave_max(mmax) * (1.0f / 448.0f), 0x1p-120f);
+    const float vs = fmaxf(wave_max(rmax) * (1.0f / 448.0f), 0x1p-120f);
+    write_codes<WHOLE>(t.m, i, n, encode8(m, 1.0f / ms, false));
+    write_codes<WHOLE>(t.v, i, n, encode8(root, 1.0f / vs, true));
+    if (lane == 0) {
+        t.m_scale[block] = ms;
+        t.v_scale[block] = vs;
+    }
+}
+
+// A work item: each wave takes every fourth of its blocks.
+template <int BITS, class P, class G>
+__device__ __forceinline__ void step_item(const derf_adamw_tensor &t, bool aligned, long long base,
+                                          const AdamWScalars &c, float gs)
+{
+    base += (threadIdx.x >> 6) * kMomentBlock;
+#pragma unroll 1
+    for (int r = 0; r < kItem / kThreads / 4; ++r, base += 4 * kMomentBlock) {
+        if (base >= t.n)
+            return;
+        if (aligned && base + kMomentBlock <= t.n)
+            step_block<BITS, true, P, G>(t, base, c, gs);
+        else
+            step_block<BITS, false, P, G>(t, base, c, gs);
+    }
+}
+
 template <int BITS>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamWEntry *table, int tensors,
                                                          AdamWScalars c, const float *grad_scale)
 {
     const AdamWEntry &e = table[find_tensor(table, tensors, blockIdx.x)];
     const float gs = grad_scale ? *grad_scale : 1.0f;
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const long long block = (long long)(blockIdx.x - e.first) * (kItem / kMomentBlock) + wave;
-    const long long base = block * kMomentBlock;
-    const long long n = e.t.n;
-    if (base >= n)
-        return;
-    float ms = 0.0f, vs = 0.0f;
-    if (BITS == 8) {
-        ms = e.t.m_scale[block];
-        vs = e.t.v_scale[block];
-    }
-    float m[4], root[4];
-    float mmax = 0.0f, rmax = 0.0f;
-    for (int j = 0; j < 4; ++j) {
-        const long long i = base + lane * 4 + j;
-        m[j] = root[j] = 0.0f;
-        if (i >= n)
-            continue;
-        const float g = load_value(e.t.grad, i, e.t.grad_precision) * gs;
-        float p = load_value(e.t.param, i, e.t.param_precision);
-        float mo, vo;
-        if (BITS == 8) {
-            mo = decode8(static_cast<const unsigned char *>(e.t.m)[i], ms);
-            const float r = decode8(static_cast<const unsigned char *>(e.t.v)[i], vs);
-            vo = r * r;
-        } else {
-            mo = static_cast<const float *>(e.t.m)[i];
-            vo = static_cast<const float *>(e.t.v)[i];
-        }
-        m[j] = mo * c.beta1 + g * c.one_minus_beta1;
-        const float v = vo * c.beta2 + (g * g) * c.one_minus_beta2;
-        root[j] = sqrtf(v);
-        p = p * c.decay - m[j] / (root[j] * c.root_scale + c.eps) * c.rate;
-        if (e.t.param_precision == DERF_PREC_BF16)
-            static_cast<__bf16 *>(e.t.param)[i] = (__bf16)p;
-        else
-            static_cast<float *>(e.t.param)[i] = p;
-        if (e.t.copy)
-            static_cast<__bf16 *>(e.t.copy)[i] = (__bf16)p;
-        if (BITS == 32) {
-            static_cast<float *>(e.t.m)[i] = m[j];
-            static_cast<float *>(e.t.v)[i] = v;
-        }
-        mmax = fmaxf(mmax, finite_abs(m[j]));
-        rmax = fmaxf(rmax, finite_abs(root[j]));
-    }
-    if (BITS == 8) {
-        ms = fmaxf(wave_max(mmax) * (1.0f / 448.0f), 0x1p-120f);
-        vs = fmaxf(wave_max(rmax) * (1.0f / 448.0f), 0x1p-120f);
-        const float mi = 1.0f / ms, vi = 1.0f / vs;
-        for (int j = 0; j < 4; ++j) {
-            const long long i = base + lane * 4 + j;
-            if (i >= n)
-                continue;
-            static_cast<unsigned char *>(e.t.m)[i] = encode8(m[j], mi, false);
-            static_cast<unsigned char *>(e.t.v)[i] = encode8(root[j], vi, true);
-        }
-        if (lane == 0) {
-            e.t.m_scale[block] = ms;
-            e.t.v_scale[block] = vs;
-        }
-    }
+    const long long base = (long long)(blockIdx.x - e.first) * kItem;
+    const bool pb = e.t.param_precision == DERF_PREC_BF16, gb = e.t.grad_precision == DERF_PREC_BF16;
+    if (pb && gb)
+        step_item<BITS, __bf16, __bf16>(e.t, e.aligned, base, c, gs);
+    else if (pb)
+        step_item<BITS, __bf16, float>(e.t, e.aligned, base, c, gs);
+    else if (gb)
+        step_item<BITS, float, __bf16>(e.t, e.aligned, base, c, gs);
+    else
+        step_item<BITS, float, float>(e.t, e.aligned, base, c, gs);
 }
 
 }  // namespace

@@ -23,6 +23,7 @@ row stride, on one GPU; what does not fit raises ValueError before any GPU work.
 from __future__ import annotations
 
 import ctypes
+import functools
 from typing import List, NamedTuple, Optional, Sequence
 
 import torch
@@ -43,8 +44,27 @@ class Routing(NamedTuple):
     num_heads: int
 
 
-def _stream(device):
-    return ctypes.c_void_p(torch.cuda.current_stream(device).cuda_stream)
+def _call(name: str, device: torch.device, *args) -> None:
+    """Call an entry point with the device's current stream as its last argument."""
+    f = getattr(derf.lib(), name)
+    index = device.index
+    stream = torch._C._cuda_getCurrentRawStream(index)  # without the Stream object
+    if torch.cuda.current_device() == index:
+        status = f(*args, stream)
+    else:
+        with torch.cuda.device(index):
+            status = f(*args, stream)
+    if status != derf.DERF_OK:
+        raise derf.DerfError(status, name)
+
+
+@functools.lru_cache(maxsize=256)
+def _workspace_bytes(name: str, *sizes: int) -> int:
+    return getattr(derf.lib(), name)(*sizes)
+
+
+def _ptr(x: Optional[torch.Tensor]):
+    return None if x is None else x.data_ptr()
 
 
 def _array(x, name, dtype, shape, device=None) -> None:
@@ -55,7 +75,7 @@ def _array(x, name, dtype, shape, device=None) -> None:
         raise ValueError("%s must be a tensor on %s" % (name, device or "a GPU"))
     if x.dtype != dtype:
         raise ValueError("%s must be %s, got %s" % (name, dtype, x.dtype))
-    if tuple(x.shape) != tuple(shape):
+    if x.shape != shape:
         raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(x.shape)))
     if not x.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
@@ -70,7 +90,7 @@ def _rows(x, name, shape=None, dtype=None, device=None) -> int:
         raise ValueError("%s must be a tensor on %s" % (name, device or "a GPU"))
     if x.dtype not in _PRECISION or (dtype is not None and x.dtype != dtype):
         raise ValueError("%s must be %s, got %s" % (name, dtype or "float32 or bfloat16", x.dtype))
-    if x.dim() != 2 or x.shape[1] < 1 or (shape is not None and tuple(x.shape) != tuple(shape)):
+    if x.dim() != 2 or x.shape[1] < 1 or (shape is not None and x.shape != shape):
         raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape) if shape else "[rows, dim]",
                                                            tuple(x.shape)))
     if x.shape[1] > 1 and x.stride(1) != 1:
@@ -94,7 +114,7 @@ def _out_array(out, name, shape, device):
 
 
 def _workspace(need: int, device):
-    return torch.empty((max(int(need), 1),), dtype=torch.uint8, device=device) if need else None
+    return torch.empty((need,), dtype=torch.uint8, device=device) if need else None
 
 
 def _routing(routing, device):
@@ -113,19 +133,17 @@ def route(ids: torch.Tensor, num_heads: int) -> Routing:
         raise ValueError("ids must be a tensor [T, k]")
     _array(ids, "ids", torch.int32, ids.shape)
     T, k = ids.shape
-    need = derf.lib().derf_route_workspace(T, k, num_heads)
+    need = _workspace_bytes("derf_route_workspace", T, k, num_heads)
     if need < 0:
         raise ValueError("invalid sizes: %d samples, %d pairs each, %d heads" % (T, k, num_heads))
     dev = ids.device
-    r = Routing(torch.empty((num_heads + 1,), dtype=torch.int32, device=dev),
-                torch.empty((T * k,), dtype=torch.int32, device=dev),
-                torch.empty((T, k), dtype=torch.int32, device=dev), num_heads)
+    offsets = torch.empty((num_heads + 1,), dtype=torch.int32, device=dev)
+    pair = torch.empty((T * k,), dtype=torch.int32, device=dev)
+    row = torch.empty((T, k), dtype=torch.int32, device=dev)
     ws = _workspace(need, dev)
-    with torch.cuda.device(dev):
-        derf._check(derf.lib().derf_route(
-            derf._dptr(ids), T, k, num_heads, derf._dptr(r.offsets), derf._dptr(r.pair),
-            derf._dptr(r.row), derf._dptr(ws), need, _stream(dev)), "derf_route")
-    return r
+    _call("derf_route", dev, ids.data_ptr(), T, k, num_heads, offsets.data_ptr(), pair.data_ptr(),
+          row.data_ptr(), _ptr(ws), need)
+    return Routing(offsets, pair, row, num_heads)
 
 
 def dispatch(x: torch.Tensor, routing: Routing, out: Optional[torch.Tensor] = None) -> torch.Tensor:
@@ -135,10 +153,8 @@ def dispatch(x: torch.Tensor, routing: Routing, out: Optional[torch.Tensor] = No
     if x.shape[0] != T:
         raise ValueError("x has %d rows, the routing %d samples" % (x.shape[0], T))
     out, out_stride = _out_rows(out, "out", T * k, x.shape[1], x)
-    with torch.cuda.device(x.device):
-        derf._check(derf.lib().derf_dispatch(
-            derf._dptr(x), stride, derf._dptr(routing.row), T, k, x.shape[1], _PRECISION[x.dtype],
-            derf._dptr(out), out_stride, _stream(x.device)), "derf_dispatch")
+    _call("derf_dispatch", x.device, x.data_ptr(), stride, routing.row.data_ptr(), T, k, x.shape[1],
+          _PRECISION[x.dtype], out.data_ptr(), out_stride)
     return out
 
 
@@ -153,11 +169,8 @@ def combine(rows: torch.Tensor, routing: Routing, weights: Optional[torch.Tensor
     if weights is not None:
         _array(weights, "weights", torch.float32, (T, k), rows.device)
     out, out_stride = _out_rows(out, "out", T, rows.shape[1], rows)
-    with torch.cuda.device(rows.device):
-        derf._check(derf.lib().derf_combine(
-            derf._dptr(rows), stride, derf._dptr(weights), derf._dptr(routing.row), T, k,
-            rows.shape[1], _PRECISION[rows.dtype], derf._dptr(out), out_stride,
-            _stream(rows.device)), "derf_combine")
+    _call("derf_combine", rows.device, rows.data_ptr(), stride, _ptr(weights), routing.row.data_ptr(),
+          T, k, rows.shape[1], _PRECISION[rows.dtype], out.data_ptr(), out_stride)
     return out
 
 
@@ -185,11 +198,9 @@ def combine_backward(dout: torch.Tensor, rows: Optional[torch.Tensor], routing: 
     if weights is not None:
         _array(weights, "weights", torch.float32, (T, k), dout.device)
     out, out_stride = _out_rows(out, "out", T * k, D, dout)
-    with torch.cuda.device(dout.device):
-        derf._check(derf.lib().derf_combine_backward(
-            derf._dptr(dout), stride, derf._dptr(rows), rows_stride, derf._dptr(weights),
-            derf._dptr(routing.row), T, k, D, _PRECISION[dout.dtype], derf._dptr(out), out_stride,
-            derf._dptr(out_weights), _stream(dout.device)), "derf_combine_backward")
+    _call("derf_combine_backward", dout.device, dout.data_ptr(), stride, _ptr(rows), rows_stride,
+          _ptr(weights), routing.row.data_ptr(), T, k, D, _PRECISION[dout.dtype], out.data_ptr(),
+          out_stride, _ptr(out_weights))
     return out, out_weights
 
 
@@ -215,11 +226,9 @@ def linear(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor],
     if bias is not None:
         _array(bias, "bias", torch.float32, (K, O), x.device)
     out, out_stride = _out_rows(out, "out", x.shape[0], O, x)
-    with torch.cuda.device(x.device):
-        derf._check(derf.lib().derf_heads_linear(
-            derf._dptr(x), stride, derf._dptr(weight), derf._dptr(bias), derf._dptr(offsets),
-            x.shape[0], K, I, O, int(bool(relu)), _PRECISION[x.dtype], derf._dptr(out), out_stride,
-            _stream(x.device)), "derf_heads_linear")
+    _call("derf_heads_linear", x.device, x.data_ptr(), stride, weight.data_ptr(), _ptr(bias),
+          offsets.data_ptr(), x.shape[0], K, I, O, int(bool(relu)), _PRECISION[x.dtype],
+          out.data_ptr(), out_stride)
     return out
 
 
@@ -246,16 +255,13 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor,
     out_weight = _out_array(out_weight, "out_weight", (K, O, I), dy.device)
     out_bias = _out_array(out_bias, "out_bias", (K, O), dy.device)
     prec = _PRECISION[dy.dtype]
-    need = derf.lib().derf_heads_linear_workspace(R, K, I, O, prec)
+    need = _workspace_bytes("derf_heads_linear_workspace", R, K, I, O, prec)
     if need < 0:
         raise ValueError("invalid sizes: %d rows, %d heads of %d to %d" % (R, K, I, O))
     ws = _workspace(need, dy.device)
-    with torch.cuda.device(dy.device):
-        derf._check(derf.lib().derf_heads_linear_backward(
-            derf._dptr(dy), dy_stride, derf._dptr(x), x_stride, derf._dptr(weight), derf._dptr(y),
-            y_stride, derf._dptr(offsets), R, K, I, O, prec, derf._dptr(out_x), dx_stride,
-            derf._dptr(out_weight), derf._dptr(out_bias), derf._dptr(ws), need,
-            _stream(dy.device)), "derf_heads_linear_backward")
+    _call("derf_heads_linear_backward", dy.device, dy.data_ptr(), dy_stride, x.data_ptr(), x_stride,
+          weight.data_ptr(), _ptr(y), y_stride, offsets.data_ptr(), R, K, I, O, prec, _ptr(out_x),
+          dx_stride, out_weight.data_ptr(), out_bias.data_ptr(), _ptr(ws), need)
     return out_x, out_weight, out_bias
 
 
@@ -337,10 +343,8 @@ class AdamW:
         if grad_scale is not None:
             _array(grad_scale, "grad_scale", torch.float32, (1,), self.device)
         step = self.steps + 1 if step is None else int(step)
-        with torch.cuda.device(self.device):
-            derf._check(derf.lib().derf_adamw_step(
-                self.handle, self.lr, self.betas[0], self.betas[1], self.eps, self.weight_decay,
-                step, derf._dptr(grad_scale), _stream(self.device)), "derf_adamw_step")
+        _call("derf_adamw_step", self.device, self.handle, self.lr, self.betas[0], self.betas[1],
+              self.eps, self.weight_decay, step, _ptr(grad_scale))
         self.steps = step
 
     def moments(self, i: int):
