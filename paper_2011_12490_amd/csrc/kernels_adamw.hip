@@ -93,6 +93,7 @@ __device__ __forceinline__ int find_tensor(const AdamWEntry *table, int tensors,
 
 __device__ __forceinline__ float wave_max(float x)
 {
+#pragma unroll
     for (int off = 32; off > 0; off >>= 1)
         x = fmaxf(x, __shfl_xor(x, off));
     return x;
@@ -128,24 +129,43 @@ __device__ __forceinline__ f32x4 decode8(unsigned c, float scale)
                  __builtin_amdgcn_cvt_f32_fp8((int)c, 2) * scale, __builtin_amdgcn_cvt_f32_fp8((int)c, 3) * scale};
 }
 
-// One wave's step on the 256 values from `base` on, four a lane.
+// What a lane reads of a block: four values of each array.
+struct Block {
+    f32x4 g, p, m, v;  // 8 bits: m[0], v[0] hold the codes
+    float ms, vs;
+};
 template <int BITS, bool WHOLE, class P, class G>
-__device__ __forceinline__ void step_block(const derf_adamw_tensor &t, long long base, const AdamWScalars &c,
-                                           float gs)
+__device__ __forceinline__ Block read_block(const derf_adamw_tensor &t, long long base)
+{
+    const long long i = base + (threadIdx.x & 63) * 4, block = base / kMomentBlock;
+    Block b;
+    b.g = read4<WHOLE, G>(t.grad, i, t.n);
+    b.p = read4<WHOLE, P>(t.param, i, t.n);
+    if (BITS == 8) {
+        b.ms = t.m_scale[block];
+        b.vs = t.v_scale[block];
+        b.m[0] = __uint_as_float(read_codes<WHOLE>(t.m, i, t.n));
+        b.v[0] = __uint_as_float(read_codes<WHOLE>(t.v, i, t.n));
+    } else {
+        b.m = read4<WHOLE, float>(t.m, i, t.n);
+        b.v = read4<WHOLE, float>(t.v, i, t.n);
+    }
+    return b;
+}
+
+// One wave's step on the 256 values from `base` on.
+template <int BITS, bool WHOLE, class P>
+__device__ __forceinline__ void step_block(const derf_adamw_tensor &t, long long base, const Block &b,
+                                           const AdamWScalars &c, float gs)
 {
     const int lane = threadIdx.x & 63;
     const long long i = base + lane * 4, n = t.n, block = base / kMomentBlock;
-    const f32x4 g = read4<WHOLE, G>(t.grad, i, n) * gs;
-    f32x4 p = read4<WHOLE, P>(t.param, i, n);
-    f32x4 m, v;
+    const f32x4 g = b.g * gs;
+    f32x4 m = b.m, v = b.v;
     if (BITS == 8) {
-        const float ms = t.m_scale[block], vs = t.v_scale[block];
-        m = decode8(read_codes<WHOLE>(t.m, i, n), ms);
-        v = decode8(read_codes<WHOLE>(t.v, i, n), vs);
+        m = decode8(__float_as_uint(b.m[0]), b.ms);
+        v = decode8(__float_as_uint(b.v[0]), b.vs);
         v = v * v;
-    } else {
-        m = read4<WHOLE, float>(t.m, i, n);
-        v = read4<WHOLE, float>(t.v, i, n);
     }
     m = m * c.beta1 + g * c.one_minus_beta1;
     v = v * c.beta2 + (g * g) * c.one_minus_beta2;
@@ -153,7 +173,7 @@ __device__ __forceinline__ void step_block(const derf_adamw_tensor &t, long long
 #pragma unroll
     for (int j = 0; j < 4; ++j)
         root[j] = sqrtf(v[j]);
-    p = p * c.decay - m / (root * c.root_scale + c.eps) * c.rate;
+    const f32x4 p = b.p * c.decay - m / (root * c.root_scale + c.eps) * c.rate;
     write4<WHOLE, P>(t.param, i, n, p);
     if (t.copy)
         write4<WHOLE, __bf16>(t.copy, i, n, p);
@@ -179,28 +199,35 @@ __device__ __forceinline__ void step_block(const derf_adamw_tensor &t, long long
     }
 }
 
-// A work item: each wave takes every fourth of its blocks.
+// A work item: each wave takes every fourth of its blocks, and reads one ahead.
 template <int BITS, class P, class G>
 __device__ __forceinline__ void step_item(const derf_adamw_tensor &t, bool aligned, long long base,
                                           const AdamWScalars &c, float gs)
 {
+    constexpr int kStep = 4 * kMomentBlock;
+    const long long end = base + kItem < t.n ? base + kItem : t.n;
     base += (threadIdx.x >> 6) * kMomentBlock;
+    if (aligned && base + kMomentBlock <= end) {
+        Block b = read_block<BITS, true, P, G>(t, base);
 #pragma unroll 1
-    for (int r = 0; r < kItem / kThreads / 4; ++r, base += 4 * kMomentBlock) {
-        if (base >= t.n)
-            return;
-        if (aligned && base + kMomentBlock <= t.n)
-            step_block<BITS, true, P, G>(t, base, c, gs);
-        else
-            step_block<BITS, false, P, G>(t, base, c, gs);
+        for (; base + kStep + kMomentBlock <= end; base += kStep) {
+            const Block next = read_block<BITS, true, P, G>(t, base + kStep);
+            step_block<BITS, true, P>(t, base, b, c, gs);
+            b = next;
+        }
+        step_block<BITS, true, P>(t, base, b, c, gs);
+        base += kStep;
     }
+#pragma unroll 1
+    for (; base < end; base += kStep)
+        step_block<BITS, false, P>(t, base, read_block<BITS, false, P, G>(t, base), c, gs);
 }
 
 template <int BITS>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(const AdamWEntry *table, int tensors,
                                                          AdamWScalars c, const float *grad_scale)
 {
-    const AdamWEntry &e = table[find_tensor(table, tensors, blockIdx.x)];
+    const AdamWEntry e = table[find_tensor(table, tensors, blockIdx.x)];
     const float gs = grad_scale ? *grad_scale : 1.0f;
     const long long base = (long long)(blockIdx.x - e.first) * kItem;
     const bool pb = e.t.param_precision == DERF_PREC_BF16, gb = e.t.grad_precision == DERF_PREC_BF16;
