@@ -17,7 +17,6 @@ namespace derf {
 namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
-typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
@@ -125,13 +124,11 @@ template <class T>
 struct Type;
 template <>
 struct Type<__bf16> {
-    static constexpr int kVec = 8;     // elements of 16 bytes
-    static constexpr int kDepth = 64;  // of 128 bytes: a step's depth
+    static constexpr int kVec = 8;  // elements of 16 bytes
 };
 template <>
 struct Type<float> {
     static constexpr int kVec = 4;
-    static constexpr int kDepth = 32;
 };
 
 struct __attribute__((packed, aligned(2))) Bytes16 {
@@ -218,32 +215,43 @@ __device__ __forceinline__ u32x4 read16(const Window &w, unsigned offset)
     return __builtin_amdgcn_raw_buffer_load_b128(
         __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, w[2], w[3]), offset, 0, 0);
 }
-// 64 x 16 bytes to LDS: lane l's piece at `offset` lands at lds + 16 l.  Written
-// as asm so that the compiler does not wait for it at the next read of LDS; it
-// is waited for where its tile is needed (async_done).
-__device__ __forceinline__ void read16_to_lds(const Window &w, unsigned offset, char *lds)
+// 64 x 16 bytes to LDS: lane l's piece at `offset` lands at byte lds + 16 l of
+// LDS.  Written as asm so that the compiler does not wait for it at the next
+// read of LDS; it is waited for where its tile is needed (arrived).
+__device__ __forceinline__ void read16_to_lds(const Window &w, unsigned offset, unsigned lds)
 {
-    const unsigned l = (unsigned)(unsigned long)(__attribute__((address_space(3))) char *)lds;
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
-                 ::"s"(uniform(l)), "v"(offset), "s"(w)
+                 ::"s"(lds), "v"(offset), "s"(w)
                  : "memory");
 }
-__device__ __forceinline__ void async_done() { asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+__device__ __forceinline__ unsigned lds_byte(const char *p)
+{
+    return uniform((unsigned)(unsigned long)(__attribute__((address_space(3))) const char *)p);
+}
+// Waits until at most N of this wave's loads and none of its LDS accesses are
+// under way, and for the other waves to get here.
+template <int N>
+__device__ __forceinline__ void arrived()
+{
+    static_assert(N < 64, "the counter's range");
+    asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
+}
 
-// Tile of an operand: DEEP: TILE rows by kDepth columns, else kDepth rows by
-// TILE columns; one depth step's.  In LDS it lies row by row in 16-byte chunks,
-// a row's chunks permuted by the row: deep ones so that a column of chunks
-// touches all banks, the others in pairs so that what a transposing read takes
-// from four rows lies in four places.  A thread brings kShare chunks, all of
-// the same columns.
+// Tile of an operand: DEEP: TILE rows by D columns, else D rows by TILE columns;
+// one depth step's, D elements being 128 bytes.  In LDS it lies row by row in
+// 16-byte chunks, a row's chunks permuted by the row so that reads touch every
+// bank once (64 of 4 bytes; no conflicts counted): 16 lanes read 16 bytes at a
+// time (lanes 0-3, 12-15, 20-23, 24-27 for one), or 32 lanes 8 bytes where they
+// transpose.  A thread brings kShare chunks, all of the same columns.
+constexpr int kChunks = 8;
 template <class T, int TILE, bool DEEP, int THREADS, bool MASK>
 struct Tile {
-    static constexpr int V = Type<T>::kVec, D = Type<T>::kDepth;
-    static constexpr int kShare = TILE * 8 / THREADS;
-    static constexpr int kBytes = TILE * 128;
-    static constexpr int kPerRow = DEEP ? 8 : TILE / V;
+    static constexpr int V = Type<T>::kVec, D = kChunks * V;
+    static constexpr int kShare = TILE * kChunks / THREADS;
+    static constexpr int kBytes = TILE * kChunks * 16;
+    static constexpr int kPerRow = DEEP ? kChunks : TILE / V;
     static constexpr int kRowStep = THREADS / kPerRow;
-    static_assert(TILE * 8 % THREADS == 0 && kRowStep % (sizeof(T) == 2 && !DEEP ? 16 : 8) == 0,
+    static_assert(TILE * kChunks % THREADS == 0 && (kRowStep % 16 == 0 || (sizeof(T) == 4 && !DEEP)),
                   "whole shares, of one permutation");
     struct S {
         u32x4 x[kShare];
@@ -254,9 +262,9 @@ struct Tile {
     static __device__ __forceinline__ unsigned turn(unsigned r)
     {
         if (DEEP)
-            return r & 7;
-        if (sizeof(T) == 2)
-            return (((r & 3) | (r >> 1 & 4)) & (TILE / 16 - 1)) << 1;
+            return r >> 1 & 7;
+        if (sizeof(T) == 2)  // in pairs of chunks: rows 0-3 and 8-11 are read at once
+            return (TILE == 64 ? (r >> 1 & 1) | (r >> 2 & 2) : (r & 3) | (r >> 1 & 4)) << 1;
         return 0;
     }
     static __device__ __forceinline__ unsigned my_row() { return threadIdx.x / kPerRow; }
@@ -364,20 +372,52 @@ struct Tile {
             *reinterpret_cast<u32x4 *>(lds + (threadIdx.x + i * THREADS) * 16) = s.x[i];
     }
 
-    // The same without registers in between: for matrices without a mask whose
-    // rows start at multiples of 16 bytes and are as long.
-    static __device__ __forceinline__ void load_async(const Source &src, unsigned k, char *lds)
-    {
-        const Window w = view(src, src.m.p, src.m.stride, k);
-        const int col = my_col();
-        const unsigned row_bytes = (unsigned)src.m.stride * sizeof(T);
-        const bool in = col < cols_left(src, k);
-        const unsigned offset = my_row() * row_bytes + (unsigned)col * (unsigned)sizeof(T);
+    // The same without registers in between, for matrices without a mask whose
+    // rows start at multiples of 16 bytes and are as long: steps one after
+    // another, with little work for each.
+    struct Feed {
+        Window w;
+        long long left;  // bytes of the matrix from the window's start on
+        unsigned step, more;
+        int cols;
+        unsigned offset[kShare];
+        __device__ __forceinline__ void start(const Source &s)
+        {
+            w = view(s, s.m.p, s.m.stride, 0);
+            const unsigned row_bytes = (unsigned)s.m.stride * sizeof(T);
+            const int col = my_col();
+            cols = cols_left(s, 0);
+            more = 0;
+            left = s.m.rows ? ((long long)(s.m.rows - 1) * s.m.stride + cols) * (long long)sizeof(T) : 0;
+            step = D * row_bytes;
+            // a tile's columns that are not the matrix's are outside in every step
 #pragma unroll
-        for (int i = 0; i < kShare; ++i)
-            read16_to_lds(w, in ? offset + i * kRowStep * row_bytes : kOutside,
-                          lds + (uniform(threadIdx.x & ~63u) + i * THREADS) * 16);
-    }
+            for (int i = 0; i < kShare; ++i)
+                offset[i] = DEEP || col < cols ? (my_row() + i * kRowStep) * row_bytes + col * (unsigned)sizeof(T) : kOutside;
+        }
+        // Brings piece i of the step to the LDS tile that starts at byte `lds`.
+        __device__ __forceinline__ void piece(int i, unsigned lds) const
+        {
+            const unsigned to = lds + uniform(threadIdx.x & ~63u) * 16 + i * THREADS * 16;
+            if (DEEP)
+                read16_to_lds(w, my_col() < cols ? offset[i] + more : kOutside, to);
+            else
+                read16_to_lds(w, offset[i], to);
+        }
+        __device__ __forceinline__ void advance()
+        {
+            if (DEEP) {
+                cols -= D;
+                more += D * sizeof(T);
+            } else {
+                const unsigned long long at = (w[0] | (unsigned long long)w[1] << 32) + step;
+                left -= step;
+                w[0] = (unsigned)at;
+                w[1] = (unsigned)(at >> 32);
+                w[2] = left > kMostBytes ? (unsigned)kMostBytes : left > 0 ? (unsigned)left : 0u;
+            }
+        }
+    };
 
     // 16-byte chunk `c` of row `r`, in bytes.
     static __device__ __forceinline__ unsigned at(unsigned r, unsigned c)
@@ -385,168 +425,221 @@ struct Tile {
         return (r * kPerRow + (c ^ turn(r))) * 16;
     }
 
-    // The matrix unit's operand: tile rows [32 f, 32 f + 32), step `k` of four.
-    // bf16: 16 deep, 8 side by side a lane.  float: 8 deep, lane half h has depths
-    // 8 k + 4 h + (0 .. 3): the unit takes them two (one of each half) at a time.
-    static __device__ __forceinline__ u32x4 fragment(const char *lds, int f, int k)
+    // The matrix unit's operand: tile rows [16 f, 16 f + 16), half `part` of the
+    // step.  bf16: 32 deep, 8 side by side a lane.  float: 16 deep, lane quarter h
+    // has depths 4 h + (0 .. 3): the unit takes them four (one of each) at a time.
+    static __device__ __forceinline__ u32x4 fragment(const char *lds, int f, int part)
     {
-        const int lane = threadIdx.x & 63;
+        const int quarter = (threadIdx.x & 63) >> 4, l = threadIdx.x & 15;
         if (DEEP)
-            return *reinterpret_cast<const u32x4 *>(lds + at(f * 32 + (lane & 31), k * 2 + (lane >> 5)));
+            return *reinterpret_cast<const u32x4 *>(lds + at(f * 16 + l, part * 4 + quarter));
         if constexpr (sizeof(T) == 2) {
-            // a group of 16 lanes reads 4 rows of 16 elements and gets them by columns
-            const int group = lane >> 4, l = lane & 15;
-            const unsigned r = k * 16 + (group >> 1) * 8 + (l >> 2);
-            const unsigned e = f * 32 + (group & 1) * 16 + (l & 3) * 4;
+            // 16 lanes read 4 rows of 16 elements and get them by columns
+            const unsigned r = part * 32 + quarter * 8 + (l >> 2);
+            const unsigned e = f * 16 + (l & 3) * 4;
             typedef __attribute__((address_space(3))) i16x4 *Lds;
             const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(lds + at(r, e / 8) + (e & 4) * 2));
             const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((Lds)(lds + at(r + 4, e / 8) + (e & 4) * 2));
             return __builtin_bit_cast(u32x4, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
         } else {
             u32x4 x;
-            const unsigned e = f * 32 + (lane & 31);
+            const unsigned e = f * 16 + l;
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 x[j] = *reinterpret_cast<const unsigned *>(
-                    lds + at(k * 8 + (lane >> 5) * 4 + j, e / 4) + (e & 3) * 4);
+                    lds + at(part * 16 + quarter * 4 + j, e / 4) + (e & 3) * 4);
             return x;
         }
     }
 };
 
-__device__ __forceinline__ f32x16 multiply(u32x4 p, u32x4 q, f32x16 c, __bf16)
+// 16 x 16 results: of the matrix unit's forms the one of least power, which is
+// what bounds it (random bf16 values in registers: 2,060 TFLOP/s, 32 x 32 x 16:
+// 1,780).  Lane 16 h + l has column l (of Q), rows 4 h + (0 .. 3) (of P).
+__device__ __forceinline__ f32x4 multiply(u32x4 p, u32x4 q, f32x4 c, __bf16)
 {
-    return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, p),
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, p),
                                                    __builtin_bit_cast(bf16x8, q), c, 0, 0, 0);
 }
-__device__ __forceinline__ f32x16 multiply(u32x4 p, u32x4 q, f32x16 c, float)
+__device__ __forceinline__ f32x4 multiply(u32x4 p, u32x4 q, f32x4 c, float)
 {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
-        c = __builtin_amdgcn_mfma_f32_32x32x2f32(__uint_as_float(p[j]), __uint_as_float(q[j]), c, 0, 0, 0);
+        c = __builtin_amdgcn_mfma_f32_16x16x4f32(__uint_as_float(p[j]), __uint_as_float(q[j]), c, 0, 0, 0);
     return c;
 }
 
-// Sizes of a product: a workgroup's tile TP x TQ, by WP x WQ waves.
-// ASYNC: operands go from memory to LDS by themselves (see load_async).  EACH_P:
-// tile_product shows its caller the P tiles.
-template <class T_, int TP_, int TQ_, int WP_, int WQ_, bool DEEP_P, bool DEEP_Q, bool MASK_P,
-          bool MASK_Q, bool ASYNC = false, bool EACH_P = false>
+// Sizes of a product: a workgroup's tile TP x TQ, by WP x WQ waves.  MASK: Q has
+// a mask.  ASYNC: operands go from memory to LDS by themselves (Tile::Feed).
+// EACH_Q: tile_product shows its caller the Q tiles.
+template <class T_, int TP_, int TQ_, int WP_, int WQ_, bool DEEP_P, bool DEEP_Q, bool MASK,
+          bool ASYNC = false, bool EACH_Q = false>
 struct Product {
     using T = T_;
     static constexpr int TP = TP_, TQ = TQ_, WP = WP_, WQ = WQ_;
     static constexpr int kThreads = WP * WQ * 64;
-    static constexpr int kDepth = Type<T>::kDepth;
-    static constexpr bool kAsync = ASYNC, kEachP = EACH_P;
-    using P = Tile<T, TP, DEEP_P, kThreads, MASK_P>;
-    using Q = Tile<T, TQ, DEEP_Q, kThreads, MASK_Q>;
-    static constexpr int FP = TP / WP / 32, FQ = TQ / WQ / 32;  // a wave's 32 x 32 results
-    static constexpr int kStage = P::kBytes + Q::kBytes;
-    static_assert(FP * WP * 32 == TP && FQ * WQ * 32 == TQ, "whole results a wave");
+    static constexpr bool kAsync = ASYNC, kEachQ = EACH_Q;
+    using P = Tile<T, TP, DEEP_P, kThreads, false>;
+    using Q = Tile<T, TQ, DEEP_Q, kThreads, MASK>;
+    static constexpr int kDepth = P::D;
+    static constexpr int FP = TP / WP / 16, FQ = TQ / WQ / 16;  // a wave's 16 x 16 results
+    static constexpr int kStage = P::kBytes + Q::kBytes, kLds = 2 * kStage;
+    static constexpr int kLoads = P::kShare + Q::kShare;  // of a thread for a step
+    static_assert(FP * WP * 16 == TP && FQ * WQ * 16 == TQ, "whole results a wave");
 };
 
-// acc += P(p, k) Q(q, k) over one step's tiles in LDS.
-template <class C>
-__device__ __forceinline__ void step_product(const char *lds, int fp, int fq, f32x16 (&acc)[C::FP][C::FQ])
+// What of `all` things to do in turn n of `turns`, spread evenly: do_one(i).
+template <class F>
+__device__ __forceinline__ void share_out(int n, int turns, int all, F do_one)
 {
 #pragma unroll
-    for (int s = 0; s < 4; ++s) {
-        u32x4 p[C::FP], q[C::FQ];
-#pragma unroll
-        for (int i = 0; i < C::FP; ++i)
-            p[i] = C::P::fragment(lds, fp + i, s);
-#pragma unroll
-        for (int j = 0; j < C::FQ; ++j)
-            q[j] = C::Q::fragment(lds + C::P::kBytes, fq + j, s);
-#pragma unroll
-        for (int i = 0; i < C::FP; ++i)
-#pragma unroll
-            for (int j = 0; j < C::FQ; ++j)
-                acc[i][j] = multiply(p[i], q[j], acc[i][j], typename C::T{});
-    }
+    for (int i = 0; i < all; ++i)
+        if (i * turns / all == n)
+            do_one(i);
 }
 
-// acc = sum over `depth` of P(p, k) Q(q, k); each_p(share): called with each of
-// the P tiles that this thread brings to LDS.  lds: 2 * kStage bytes.
-template <class C, class EachP>
+// acc += the products of p and q.  Meanwhile the next part's operands come from
+// half `part` of the stage at `lds` to p_next and, each where it has been used, to q
+// (READ), and load(i) is called for each of kLoads (LOAD).
+template <class C, bool LOAD, class Load>
+__device__ __forceinline__ void multiply_part(const u32x4 (&p)[C::FP], u32x4 (&q)[C::FQ], u32x4 (&p_next)[C::FP],
+                                              bool read, const char *lds, int fp, int fq, int part,
+                                              f32x4 (&acc)[C::FP][C::FQ], Load load)
+{
+    constexpr int kAll = C::FP * C::FQ;
+#pragma unroll
+    for (int j = 0; j < C::FQ; ++j)
+#pragma unroll
+        for (int i = 0; i < C::FP; ++i) {
+            const int n = j * C::FP + i;
+            acc[i][j] = multiply(p[i], q[j], acc[i][j], typename C::T{});
+            if (read) {
+                if (i == C::FP - 1)
+                    q[j] = C::Q::fragment(lds + C::P::kBytes, fq + j, part);
+                share_out(n, kAll, C::FP, [&](int k) { p_next[k] = C::P::fragment(lds, fp + k, part); });
+            }
+            if (LOAD)
+                share_out(n, kAll, C::kLoads, load);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+}
+
+// acc = sum over `depth` of P(p, k) Q(q, k); each_q(share): called with each of
+// the Q tiles that this thread brings to LDS.  lds: kLds bytes, two steps.
+//
+// A step has two parts; operands are read a part ahead of their products, the
+// next step's first behind the barrier between the parts.  There all of the step
+// has been read, so the loads of the step after the next can overwrite it.
+template <class C, class EachQ>
 __device__ __forceinline__ void tile_product(const Matrix<typename C::T> &mp, unsigned p0,
                                              const Matrix<typename C::T> &mq, unsigned q0,
                                              unsigned depth, char *lds,
-                                             f32x16 (&acc)[C::FP][C::FQ], EachP each_p)
+                                             f32x4 (&acc)[C::FP][C::FQ], EachQ each_q)
 {
     const int wave = uniform(threadIdx.x >> 6);
     const int fp = (wave % C::WP) * C::FP, fq = (wave / C::WP) * C::FQ;
-    const typename C::P::Source p = {mp, p0};
-    const typename C::Q::Source q = {mq, q0};
+    const typename C::P::Source ps = {mp, p0};
+    const typename C::Q::Source qs = {mq, q0};
     if (depth == 0)
         return;
-    if constexpr (C::kAsync) {
-        auto load = [&](unsigned k, char *to) {
-            C::P::load_async(p, k, to);
-            C::Q::load_async(q, k, to + C::P::kBytes);
-        };
-        load(0, lds);
-        async_done();
-        unsigned stage = 0;
-        for (unsigned k = 0; k < depth; k += C::kDepth) {
-            const char *from = lds + stage * C::kStage;
-            stage ^= 1;
-            if (k + C::kDepth < depth)
-                load(k + C::kDepth, lds + stage * C::kStage);
-            if constexpr (C::kEachP) {
-                typename C::P::S share;
+    typename C::Q::S sq;
+    u32x4 p0f[C::FP], p1f[C::FP], q[C::FQ];
+    auto read_first = [&]() {
 #pragma unroll
-                for (int i = 0; i < C::P::kShare; ++i)
-                    share.x[i] = *reinterpret_cast<const u32x4 *>(from + (threadIdx.x + i * C::kThreads) * 16);
-                each_p(share);
-            }
-            step_product<C>(from, fp, fq, acc);
-            async_done();
-        }
-    } else {
-        typename C::P::S sp;
-        typename C::Q::S sq;
-        auto load = [&](unsigned k) {
-            C::P::load(sp, p, k);
-            C::Q::load(sq, q, k);
+        for (int i = 0; i < C::FP; ++i)
+            p0f[i] = C::P::fragment(lds, fp + i, 0);
+#pragma unroll
+        for (int j = 0; j < C::FQ; ++j)
+            q[j] = C::Q::fragment(lds + C::P::kBytes, fq + j, 0);
+    };
+    unsigned stage = 0;
+    if constexpr (C::kAsync) {
+        typename C::P::Feed pf;
+        typename C::Q::Feed qf;
+        pf.start(ps);
+        qf.start(qs);
+        const unsigned lds0 = lds_byte(lds);
+        auto piece = [&](int i, unsigned to) {
+            if (i < C::P::kShare)
+                pf.piece(i, to);
+            else
+                qf.piece(i - C::P::kShare, to + C::P::kBytes);
         };
-        auto bring = [&](unsigned k, char *to) {
-            C::P::settle(sp, p, k);
-            C::Q::settle(sq, q, k);
-            if constexpr (C::kEachP)
-                each_p(sp);
-            C::P::store(sp, to);
-            C::Q::store(sq, to + C::P::kBytes);
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+#pragma unroll
+            for (int i = 0; i < C::kLoads; ++i)
+                piece(i, lds0 + n * C::kStage);
+            pf.advance();
+            qf.advance();
+        }
+        arrived<C::kLoads>();
+        read_first();
+#pragma unroll 1
+        for (unsigned k = 0; k < depth; k += C::kDepth) {
+            const unsigned used = stage * C::kStage;
+            if constexpr (C::kEachQ) {
+#pragma unroll
+                for (int i = 0; i < C::Q::kShare; ++i)
+                    sq.x[i] = *reinterpret_cast<const u32x4 *>(lds + used + C::P::kBytes + (threadIdx.x + i * C::kThreads) * 16);
+                each_q(sq);
+            }
+            multiply_part<C, false>(p0f, q, p1f, true, lds + used, fp, fq, 1, acc, [](int) {});
+            arrived<0>();
+            stage ^= 1;
+            multiply_part<C, true>(p1f, q, p0f, true, lds + stage * C::kStage, fp, fq, 0, acc,
+                                   [&](int i) { piece(i, lds0 + used); });
+            pf.advance();
+            qf.advance();
+        }
+        arrived<0>();
+    } else {
+        // Through registers: a step's loads begin a step before they are stored.
+        typename C::P::S sp;
+        auto load = [&](unsigned k) {
+            C::P::load(sp, ps, k);
+            C::Q::load(sq, qs, k);
+        };
+        auto bring = [&](unsigned k, unsigned to) {
+            C::P::settle(sp, ps, k);
+            C::Q::settle(sq, qs, k);
+            if constexpr (C::kEachQ)
+                each_q(sq);
+            C::P::store(sp, lds + to * C::kStage);
+            C::Q::store(sq, lds + to * C::kStage + C::P::kBytes);
         };
         load(0);
-        bring(0, lds);
-        __syncthreads();
-        unsigned stage = 0;
+        bring(0, 0);
+        arrived<0>();
+        read_first();
+#pragma unroll 1
         for (unsigned k = 0; k < depth; k += C::kDepth) {
-            const unsigned next = k + C::kDepth;
-            if (next < depth)
-                load(next);
-            step_product<C>(lds + stage * C::kStage, fp, fq, acc);
+            const char *from = lds + stage * C::kStage;
+            const bool more = k + C::kDepth < depth;
+            if (more)
+                load(k + C::kDepth);
+            multiply_part<C, false>(p0f, q, p1f, true, from, fp, fq, 1, acc, [](int) {});
             stage ^= 1;
-            if (next < depth)
-                bring(next, lds + stage * C::kStage);
-            __syncthreads();
+            if (more)
+                bring(k + C::kDepth, stage);
+            arrived<0>();
+            multiply_part<C, false>(p1f, q, p0f, more, lds + stage * C::kStage, fp, fq, 0, acc, [](int) {});
         }
     }
 }
 
 // ---- rows: the layer, and its rows' gradient --------------------------------------
 
-// A wave's results as rows of 32 FP elements: a lane has, of row 32 j + (lane &
-// 31) of Q, elements 8 i + 4 (lane >> 5) + (0 .. 3) of each 32 of P.  They go
-// through LDS to be written in 16-byte pieces.  Bytes of a row there (8 of 64
-// banks further on for the next row):
+// A wave's results as rows of 16 FP elements: lane 16 h + l has, of row 16 j + l
+// of Q, elements 4 h + (0 .. 3) of each 16 of P.  They go through LDS, 16 rows at
+// a time, to be written in 16-byte pieces.  Bytes of a row there (4 of 64 banks
+// further on for the next row):
 template <class C>
-constexpr int kResultRow = C::FP * 32 * (int)sizeof(typename C::T) + 16;
+constexpr int kResultRow = C::FP * 16 * (int)sizeof(typename C::T) + 16;
 template <class C>
-constexpr int kResultBytes = C::WP * C::WQ * 32 * kResultRow<C>;
+constexpr int kResultBytes = C::WP * C::WQ * 16 * kResultRow<C>;
 template <class C>
-constexpr int kRowsLds = 2 * C::kStage > kResultBytes<C> ? 2 * C::kStage : kResultBytes<C>;
+constexpr int kRowsLds = C::kLds > kResultBytes<C> ? C::kLds : kResultBytes<C>;
 
 __device__ __forceinline__ void store_values(char *to, const float (&v)[4], __bf16)
 {
@@ -566,7 +659,7 @@ __device__ __forceinline__ void store_values(char *to, const float (&v)[4], floa
 
 // P: the weights (width columns of the result), Q: rows.
 template <class C>
-__global__ __launch_bounds__(C::kThreads) void rows_kernel(
+__global__ __launch_bounds__(C::kThreads, 2) void rows_kernel(
     Problem p, Matrix<typename C::T> w, Matrix<typename C::T> x, const float *bias, int relu,
     typename C::T *y, long long ys, int width, int depth, unsigned long long from)
 {
@@ -596,7 +689,7 @@ __global__ __launch_bounds__(C::kThreads) void rows_kernel(
         t.head = p.heads;
     }
     const bool headed = t.head < p.heads;
-    f32x16 acc[C::FP][C::FQ] = {};
+    f32x4 acc[C::FP][C::FQ] = {};
     if (headed) {
         Matrix<T> wh = w, xh = x;
         wh.p += t.head * head_size;
@@ -606,34 +699,34 @@ __global__ __launch_bounds__(C::kThreads) void rows_kernel(
         tile_product<C>(wh, n0, xh, 0, depth, lds, acc, [](auto &) {});
     }
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int wp = (wave % C::WP) * C::FP * 32, wq = (wave / C::WP) * C::FQ * 32;
-    char *mine = lds + wave * 32 * kResultRow<C>;
+    const int wp = (wave % C::WP) * C::FP * 16, wq = (wave / C::WP) * C::FQ * 16;
+    char *mine = lds + wave * 16 * kResultRow<C>;
     const float *bh = bias && headed ? bias + (size_t)t.head * width : nullptr;
 #pragma unroll
     for (int j = 0; j < C::FQ; ++j) {
 #pragma unroll
-        for (int i = 0; i < C::FP; ++i)
+        for (int i = 0; i < C::FP; ++i) {
+            const int e = i * 16 + (lane >> 4) * 4;
+            float v[4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int e = i * 32 + q * 8 + (lane >> 5) * 4;
-                float v[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    v[k] = acc[i][j][q * 4 + k];
-                    if (bh && n0 + wp + e + k < width)
-                        v[k] += bh[n0 + wp + e + k];
-                    if (relu)
-                        v[k] = v[k] < 0.0f ? 0.0f : v[k];
-                }
-                store_values(mine + (lane & 31) * kResultRow<C> + e * sizeof(T), v, T{});
+            for (int k = 0; k < 4; ++k) {
+                v[k] = acc[i][j][k];
+                if (bh && n0 + wp + e + k < width)
+                    v[k] += bh[n0 + wp + e + k];
+                if (relu)
+                    v[k] = v[k] < 0.0f ? 0.0f : v[k];
             }
+            store_values(mine + (lane & 15) * kResultRow<C> + e * sizeof(T), v, T{});
+        }
         __builtin_amdgcn_wave_barrier();
-        constexpr int kPieces = C::FP * 32 / V;  // of a row
+        constexpr int kPieces = C::FP * 16 / V;  // of a row
 #pragma unroll
-        for (int i = 0; i < 32 * kPieces / 64; ++i) {
+        for (int i = 0; i < (16 * kPieces + 63) / 64; ++i) {
             const int r = (i * 64 + lane) / kPieces, c = (i * 64 + lane) % kPieces * V;
+            if (16 * kPieces % 64 && r >= 16)
+                continue;
             const u32x4 v = *reinterpret_cast<const u32x4 *>(mine + r * kResultRow<C> + c * sizeof(T));
-            const unsigned row = t.first + wq + j * 32 + r;
+            const unsigned row = t.first + wq + j * 16 + r;
             const int n = n0 + wp + c;
             if (row >= t.last || n >= width)
                 continue;
@@ -657,11 +750,11 @@ __global__ __launch_bounds__(C::kThreads) void rows_kernel(
 
 // ---- weights ----------------------------------------------------------------------
 
-// P: dz, Q: x, reduced over rows: a tile of a head's dW from a stretch of
+// P: x, Q: dz, reduced over rows: a tile of a head's dW from a stretch of
 // `stretch` of its rows.  Where heads have more than one stretch (partial),
 // each has a place of its own in dw and db, and sum_kernel adds them up.
 template <class C>
-__global__ __launch_bounds__(C::kThreads) void weights_kernel(Problem p, Matrix<typename C::T> dz,
+__global__ __launch_bounds__(C::kThreads, 2) void weights_kernel(Problem p, Matrix<typename C::T> dz,
                                                               Matrix<typename C::T> x, float *dw,
                                                               float *db, unsigned stretch,
                                                               bool partial, unsigned places,
@@ -670,7 +763,7 @@ __global__ __launch_bounds__(C::kThreads) void weights_kernel(Problem p, Matrix<
 {
     using T = typename C::T;
     constexpr int V = Type<T>::kVec;
-    __shared__ __attribute__((aligned(16))) char lds[2 * C::kStage];
+    __shared__ __attribute__((aligned(16))) char lds[C::kLds];
     __shared__ unsigned tmp[4];
     __shared__ RowTile found;
     const int I = p.fan_in, O = p.fan_out;
@@ -680,7 +773,7 @@ __global__ __launch_bounds__(C::kThreads) void weights_kernel(Problem p, Matrix<
     if (place >= places)
         return;
     const Place2 where = in_groups(at - (unsigned long long)place * each, row_tiles, col_tiles);
-    const int m0 = (int)where.a * C::TP, n0 = (int)where.b * C::TQ;
+    const int m0 = (int)where.a * C::TQ, n0 = (int)where.b * C::TP;  // of dz, of x
     RowTile t;
     if (partial) {
         const Spread s = spread_tiles(p, stretch, tmp);
@@ -699,12 +792,12 @@ __global__ __launch_bounds__(C::kThreads) void weights_kernel(Problem p, Matrix<
     mz.rows = mx.rows = t.last - t.first;
     const bool sum = db && n0 == 0;
     float sums[V] = {};
-    f32x16 acc[C::FP][C::FQ] = {};
-    tile_product<C>(mz, m0, mx, n0, mz.rows, lds, acc, [&](const typename C::P::S &share) {
+    f32x4 acc[C::FP][C::FQ] = {};
+    tile_product<C>(mx, n0, mz, m0, mz.rows, lds, acc, [&](const typename C::Q::S &share) {
         if (!sum)
             return;
 #pragma unroll
-        for (int i = 0; i < C::P::kShare; ++i) {
+        for (int i = 0; i < C::Q::kShare; ++i) {
             union {
                 u32x4 v;
                 T e[V];
@@ -715,32 +808,40 @@ __global__ __launch_bounds__(C::kThreads) void weights_kernel(Problem p, Matrix<
         }
     });
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int wp = (wave % C::WP) * C::FP * 32, wq = (wave / C::WP) * C::FQ * 32;
+    const int wp = (wave % C::WP) * C::FP * 16, wq = (wave / C::WP) * C::FQ * 16;
     if (dw) {
         float *to = dw + (size_t)place * O * I;
 #pragma unroll
-        for (int i = 0; i < C::FP; ++i)
+        for (int j = 0; j < C::FQ; ++j) {
+            const int m = m0 + wq + j * 16 + (lane & 15);
 #pragma unroll
-            for (int j = 0; j < C::FQ; ++j)
+            for (int i = 0; i < C::FP; ++i) {
+                const int n = n0 + wp + i * 16 + (lane >> 4) * 4;
+                if (m >= O || n >= I)
+                    continue;
+                float *at = to + ((size_t)m * I + n);
+                if (n + 4 <= I) {
+                    reinterpret_cast<Bytes16 *>(at)->v = __builtin_bit_cast(u32x4, acc[i][j]);
+                } else {
 #pragma unroll
-                for (int q = 0; q < 16; ++q) {
-                    const int m = m0 + wp + i * 32 + (q >> 2) * 8 + (lane >> 5) * 4 + (q & 3);
-                    const int n = n0 + wq + j * 32 + (lane & 31);
-                    if (m < O && n < I)
-                        to[(size_t)m * I + n] = acc[i][j][q];
+                    for (int k = 0; k < 4; ++k)
+                        if (n + k < I)
+                            at[k] = acc[i][j][k];
                 }
+            }
+        }
     }
     if (sum) {
         // a thread's sums are over every (threads / kPerRow)-th row of its columns
-        constexpr int kRowsOfThreads = C::kThreads / C::P::kPerRow;
-        float(*part)[C::TP + 1] = reinterpret_cast<float(*)[C::TP + 1]>(lds);
-        static_assert(sizeof(float) * kRowsOfThreads * (C::TP + 1) <= 2 * C::kStage, "fits");
+        constexpr int kRowsOfThreads = C::kThreads / C::Q::kPerRow;
+        float(*part)[C::TQ + 1] = reinterpret_cast<float(*)[C::TQ + 1]>(lds);
+        static_assert(sizeof(float) * kRowsOfThreads * (C::TQ + 1) <= C::kLds, "fits");
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < V; ++k)
-            part[C::P::my_row()][C::P::my_col() + k] = sums[k];
+            part[C::Q::my_row()][C::Q::my_col() + k] = sums[k];
         __syncthreads();
-        for (int m = threadIdx.x; m < C::TP; m += C::kThreads) {
+        for (int m = threadIdx.x; m < C::TQ; m += C::kThreads) {
             float v = 0.0f;
             for (int r = 0; r < kRowsOfThreads; ++r)
                 v += part[r][m];
@@ -810,20 +911,20 @@ hipError_t rows_product(const Problem &p, const Matrix<T> &w, const Matrix<T> &x
         if (width > 128 && (unsigned long long)p.rows * tiles_of(width, 256) >= 256 * 128) {
             if constexpr (!MASK)
                 if (alone)
-                    return launch_rows<Product<T, 256, 256, 4, 2, DEEP_W, true, false, false, true>>(
+                    return launch_rows<Product<T, 256, 256, 4, 2, DEEP_W, true, false, true>>(
                         p, w, x, bias, relu, y, width, depth, s);
-            return launch_rows<Product<T, 256, 256, 4, 2, DEEP_W, true, false, MASK>>(
+            return launch_rows<Product<T, 256, 256, 4, 2, DEEP_W, true, MASK>>(
                 p, w, x, bias, relu, y, width, depth, s);
         }
     if (width > 64) {
         if constexpr (!MASK)
             if (alone)
-                return launch_rows<Product<T, 128, 128, 2, 2, DEEP_W, true, false, false, true>>(
+                return launch_rows<Product<T, 128, 128, 2, 2, DEEP_W, true, false, true>>(
                     p, w, x, bias, relu, y, width, depth, s);
-        return launch_rows<Product<T, 128, 128, 2, 2, DEEP_W, true, false, MASK>>(
+        return launch_rows<Product<T, 128, 128, 2, 2, DEEP_W, true, MASK>>(
             p, w, x, bias, relu, y, width, depth, s);
     }
-    return launch_rows<Product<T, 64, 128, 2, 2, DEEP_W, true, false, MASK>>(p, w, x, bias, relu, y,
+    return launch_rows<Product<T, 64, 128, 2, 2, DEEP_W, true, MASK>>(p, w, x, bias, relu, y,
                                                                              width, depth, s);
 }
 
@@ -857,7 +958,7 @@ hipError_t launch_weights(const Problem &p, const Matrix<typename C::T> &dz,
     float *wparts = reinterpret_cast<float *>(workspace);
     float *bparts = wparts + (size_t)split.places * size;
     float *to_w = dw ? (partial ? wparts : dw) : nullptr, *to_b = db ? (partial ? bparts : db) : nullptr;
-    const unsigned row_tiles = tiles_of(p.fan_out, C::TP), col_tiles = dw ? tiles_of(p.fan_in, C::TQ) : 1;
+    const unsigned row_tiles = tiles_of(p.fan_out, C::TQ), col_tiles = dw ? tiles_of(p.fan_in, C::TP) : 1;
     const unsigned long long all = (unsigned long long)split.places * row_tiles * col_tiles + kXcds * kRun;
     for (unsigned long long from = 0; from < all; from += kMostGroups)
         weights_kernel<C><<<(unsigned)(all - from < kMostGroups ? all - from : kMostGroups), C::kThreads, 0, s>>>(
@@ -884,21 +985,21 @@ hipError_t weights_product(const Problem &p, const Matrix<T> &dz, const Matrix<T
             (unsigned long long)tiles_of(p.fan_out, 256) * tiles_of(p.fan_in, 256) * p.heads >= 256) {
             if constexpr (!MASK)
                 if (alone)
-                    return launch_weights<Product<T, 256, 256, 4, 2, false, false, false, false, true, true>>(
+                    return launch_weights<Product<T, 256, 256, 4, 2, false, false, false, true, true>>(
                         p, dz, x, dw, db, workspace, s);
-            return launch_weights<Product<T, 256, 256, 4, 2, false, false, MASK, false, false, true>>(p, dz, x, dw, db, workspace, s);
+            return launch_weights<Product<T, 256, 256, 4, 2, false, false, MASK, false, true>>(p, dz, x, dw, db, workspace, s);
         }
     if constexpr (!MASK)
         if (wide_o && wide_i && alone)
-            return launch_weights<Product<T, 128, 128, 2, 2, false, false, false, false, true, true>>(
+            return launch_weights<Product<T, 128, 128, 2, 2, false, false, false, true, true>>(
                 p, dz, x, dw, db, workspace, s);
     if (wide_o && wide_i)
-        return launch_weights<Product<T, 128, 128, 2, 2, false, false, MASK, false, false, true>>(p, dz, x, dw, db, workspace, s);
+        return launch_weights<Product<T, 128, 128, 2, 2, false, false, MASK, false, true>>(p, dz, x, dw, db, workspace, s);
     if (wide_o)
-        return launch_weights<Product<T, 128, 64, 2, 2, false, false, MASK, false, false, true>>(p, dz, x, dw, db, workspace, s);
+        return launch_weights<Product<T, 64, 128, 2, 2, false, false, MASK, false, true>>(p, dz, x, dw, db, workspace, s);
     if (wide_i)
-        return launch_weights<Product<T, 64, 128, 2, 2, false, false, MASK, false, false, true>>(p, dz, x, dw, db, workspace, s);
-    return launch_weights<Product<T, 64, 64, 2, 2, false, false, MASK, false, false, true>>(p, dz, x, dw, db, workspace, s);
+        return launch_weights<Product<T, 128, 64, 2, 2, false, false, MASK, false, true>>(p, dz, x, dw, db, workspace, s);
+    return launch_weights<Product<T, 64, 64, 2, 2, false, false, MASK, false, true>>(p, dz, x, dw, db, workspace, s);
 }
 
 Problem problem(const LinearShape &sh) { return {sh.offsets, sh.rows, sh.heads, sh.fan_in, sh.fan_out}; }
