@@ -46,74 +46,82 @@ struct RowTile {
     int head;
 };
 
-// The heads' numbers of tiles of `tile_rows` rows, summed: thread h < 256 keeps
-// the tiles before head h's.  At least 256 threads, all call it.
-struct Spread {
-    unsigned first, last, before, mine;  // of head threadIdx.x
-    unsigned total;                      // of all heads
-};
-__device__ __forceinline__ Spread spread_tiles(const Problem &p, unsigned tile_rows, unsigned *tmp)
+// before[h] (h <= heads): the tiles of `tile_rows` rows of the heads before h, in
+// LDS.  At least 256 threads, all call it.
+constexpr int kMaxHeads = 256;
+__device__ __forceinline__ void count_tiles(const Problem &p, unsigned tile_rows, unsigned *before)
 {
     const int h = threadIdx.x, lane = h & 63, wave = h >> 6;
-    Spread s = {0, 0, 0, 0, 0};
+    unsigned mine = 0;
     if (h < p.heads) {
-        s.first = bound(p, h);
-        s.last = bound(p, h + 1);
-        s.mine = s.last > s.first ? (s.last - s.first + tile_rows - 1) / tile_rows : 0;
+        const unsigned a = bound(p, h), b = bound(p, h + 1);
+        mine = b > a ? (b - a + tile_rows - 1) / tile_rows : 0;
     }
-    unsigned incl = s.mine;
+    unsigned incl = mine;
+#pragma unroll
     for (int off = 1; off < 64; off <<= 1) {
         const unsigned y = __shfl_up(incl, off);
         if (lane >= off)
             incl += y;
     }
-    if (lane == 63 && wave < 4)
+    __shared__ unsigned tmp[kMaxHeads / 64];
+    if (lane == 63 && wave < kMaxHeads / 64)
         tmp[wave] = incl;
     __syncthreads();
-    s.before = incl - s.mine;
-    for (int w = 0; w < 4; ++w) {
-        if (w < wave)
-            s.before += tmp[w];
-        s.total += tmp[w];
-    }
+    for (int w = 0; w < wave && w < kMaxHeads / 64; ++w)
+        incl += tmp[w];
+    if (h < p.heads)
+        before[h + 1] = incl;
+    if (h == 0)
+        before[0] = 0;
     __syncthreads();
-    return s;
 }
 
-// Tile number `tile` (one of the heads'); all threads call it.
-__device__ __forceinline__ RowTile head_tile(const Spread &s, unsigned tile, unsigned tile_rows,
-                                             RowTile *found)
+// Rows of tile number `tile`, which is below before[heads].
+__device__ __forceinline__ RowTile head_tile(const Problem &p, const unsigned *before, unsigned tile,
+                                             unsigned tile_rows)
 {
-    __syncthreads();
-    if (tile >= s.before && tile - s.before < s.mine) {
-        found->first = s.first + (tile - s.before) * tile_rows;
-        found->last = s.last - found->first > tile_rows ? found->first + tile_rows : s.last;
-        found->head = threadIdx.x;
+    int lo = 0, hi = p.heads - 1;  // the last head with before[h] <= tile
+    while (lo < hi) {
+        const int mid = (lo + hi + 1) >> 1;
+        if (uniform(before[mid]) <= tile)
+            lo = mid;
+        else
+            hi = mid - 1;
     }
-    __syncthreads();
-    return {uniform(found->first), uniform(found->last), (int)uniform((unsigned)found->head)};
+    const unsigned first = uniform(bound(p, lo)) + (tile - uniform(before[lo])) * tile_rows;
+    const unsigned last = uniform(bound(p, lo + 1));
+    return {first, last - first > tile_rows ? first + tile_rows : last, lo};
 }
 
-// Workgroup b of at least `all`: which of `all` tiles it takes.  Consecutive
+// Number b, in the order in which they are taken, of `all` tiles: consecutive
 // workgroups go to the 8 XCDs in turn; each XCD gets runs of up to 32 tiles (its
 // compute units), neighbours that share operands in its L2, and short ones where
-// there are few tiles, so that none gets much more than another.
+// there are few tiles, so that none gets much more than another.  Some b beyond
+// `all` give tiles too, and some below none; none from runs_end(all) on does.
 constexpr unsigned kXcds = 8, kRun = 32;
-__device__ __forceinline__ unsigned long long by_xcd(unsigned long long b, unsigned long long all)
+__device__ __forceinline__ unsigned run_of(unsigned all)
 {
-    const unsigned run = all >= 64 * kRun ? kRun : all >= 64 ? (unsigned)all / 64 : 1;
-    const unsigned long long j = b / kXcds;
+    return all >= 64 * kRun ? kRun : all >= 64 ? all / 64 : 1;
+}
+__device__ __forceinline__ unsigned by_xcd(unsigned b, unsigned all)
+{
+    const unsigned run = run_of(all), j = b / kXcds;
     return (j / run * kXcds + b % kXcds) * run + j % run;
+}
+__device__ __forceinline__ unsigned runs_end(unsigned all)
+{
+    const unsigned round = run_of(all) * kXcds;
+    return (all + round - 1) / round * round;
 }
 
 // Tile `at` of rows x cols ones: in groups of 4 rows, a group column by column.
 struct Place2 {
     unsigned a, b;
 };
-__device__ __forceinline__ Place2 in_groups(unsigned long long at, unsigned rows, unsigned cols)
+__device__ __forceinline__ Place2 in_groups(unsigned at, unsigned rows, unsigned cols)
 {
-    const unsigned group = (unsigned)(at / (4ull * cols));
-    const unsigned in = (unsigned)(at - (unsigned long long)group * 4 * cols);
+    const unsigned group = at / (4 * cols), in = at - group * 4 * cols;
     const unsigned tall = rows - group * 4 < 4 ? rows - group * 4 : 4;
     return {group * 4 + in % tall, in / tall};
 }
@@ -198,6 +206,7 @@ struct Matrix {
 typedef u32x4 Window;
 constexpr long long kMostBytes = 0x7FFFFFFF;
 constexpr unsigned kOutside = 0xFFFFFFF0u;
+constexpr unsigned kWindowFlags = 0x00020000u;  // untyped, rows of no fixed length
 template <class T>
 __device__ __forceinline__ Window window(const T *p, long long stride, unsigned rows, int cols,
                                          unsigned row0, int col0)
@@ -207,7 +216,7 @@ __device__ __forceinline__ Window window(const T *p, long long stride, unsigned 
                               ? ((long long)(rows - row0 - 1) * stride + cols - col0) * (long long)sizeof(T)
                               : 0;
     const unsigned records = end < kMostBytes ? (unsigned)end : (unsigned)kMostBytes;
-    return Window{uniform((unsigned)at), uniform((unsigned)(at >> 32)), uniform(records), 0x00020000u};
+    return Window{uniform((unsigned)at), uniform((unsigned)(at >> 32)), uniform(records), kWindowFlags};
 }
 __device__ __forceinline__ u32x4 read16(const Window &w, unsigned offset)
 {
@@ -221,6 +230,13 @@ __device__ __forceinline__ u32x4 read16(const Window &w, unsigned offset)
 __device__ __forceinline__ void read16_to_lds(const Window &w, unsigned offset, unsigned lds)
 {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 ::"s"(lds), "v"(offset), "s"(w)
+                 : "memory");
+}
+// The same with 64 x 4 bytes.
+__device__ __forceinline__ void read4_to_lds(const Window &w, unsigned offset, unsigned lds)
+{
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tbuffer_load_dword %1, %2, 0 offen lds"
                  ::"s"(lds), "v"(offset), "s"(w)
                  : "memory");
 }
@@ -395,6 +411,18 @@ struct Tile {
             for (int i = 0; i < kShare; ++i)
                 offset[i] = DEEP || col < cols ? (my_row() + i * kRowStep) * row_bytes + col * (unsigned)sizeof(T) : kOutside;
         }
+        // The steps from here on bring zeros: an empty window, whether or not
+        // there was a tile before.
+        __device__ __forceinline__ void stop()
+        {
+            w = Window{0u, 0u, 0u, kWindowFlags};
+            left = 0;
+            step = more = 0;
+            cols = 0;
+#pragma unroll
+            for (int i = 0; i < kShare; ++i)
+                offset[i] = kOutside;
+        }
         // Brings piece i of the step to the LDS tile that starts at byte `lds`.
         __device__ __forceinline__ void piece(int i, unsigned lds) const
         {
@@ -524,107 +552,149 @@ __device__ __forceinline__ void multiply_part(const u32x4 (&p)[C::FP], u32x4 (&q
         }
 }
 
-// acc = sum over `depth` of P(p, k) Q(q, k); each_q(share): called with each of
-// the Q tiles that this thread brings to LDS.  lds: kLds bytes, two steps.
-//
+// The first part's operands, from the stage at `lds`.
+template <class C>
+__device__ __forceinline__ void read_first(u32x4 (&p)[C::FP], u32x4 (&q)[C::FQ], const char *lds, int fp, int fq)
+{
+#pragma unroll
+    for (int i = 0; i < C::FP; ++i)
+        p[i] = C::P::fragment(lds, fp + i, 0);
+#pragma unroll
+    for (int j = 0; j < C::FQ; ++j)
+        q[j] = C::Q::fragment(lds + C::P::kBytes, fq + j, 0);
+}
+
 // A step has two parts; operands are read a part ahead of their products, the
 // next step's first behind the barrier between the parts.  There all of the step
-// has been read, so the loads of the step after the next can overwrite it.
+// has been read, and the loads of the step after the next overwrite it.
+
+// Products whose operands go to LDS by themselves: a workgroup's tiles one after
+// another, with the loads two steps ahead of the products, across the tiles.
+template <class C>
+struct Pipe {
+    char *lds;
+    unsigned lds0, stage, left;  // left: steps of the tile being loaded that are not yet
+    int fp, fq;
+    typename C::P::Feed pf;
+    typename C::Q::Feed qf;
+    u32x4 pa[C::FP], pb[C::FP], q[C::FQ];
+
+    __device__ __forceinline__ void piece(int i, unsigned to)
+    {
+        if (i < C::P::kShare)
+            pf.piece(i, to);
+        else
+            qf.piece(i - C::P::kShare, to + C::P::kBytes);
+    }
+    // next_tile(*this): calls load_tile with the next tile of more than no steps, or
+    // load_nothing.
+    __device__ __forceinline__ void load_tile(const typename C::P::Source &p, const typename C::Q::Source &q_,
+                                              unsigned depth)
+    {
+        pf.start(p);
+        qf.start(q_);
+        left = (depth + C::kDepth - 1) / C::kDepth;
+    }
+    __device__ __forceinline__ void load_nothing()
+    {
+        pf.stop();
+        qf.stop();
+        left = 0xFFFFFFFFu;
+    }
+    template <class Next>
+    __device__ __forceinline__ void start(char *lds_, Next next_tile)
+    {
+        const int wave = uniform(threadIdx.x >> 6);
+        fp = (wave % C::WP) * C::FP;
+        fq = (wave / C::WP) * C::FQ;
+        lds = lds_;
+        lds0 = lds_byte(lds);
+        stage = 0;
+        left = 0;
+        for (int n = 0; n < 2; ++n) {
+            if (left == 0)
+                next_tile(*this);
+#pragma unroll
+            for (int i = 0; i < C::kLoads; ++i)
+                piece(i, lds0 + n * C::kStage);
+            advance();
+        }
+        arrived<C::kLoads>();
+        read_first<C>(pa, q, lds, fp, fq);
+    }
+    __device__ __forceinline__ void advance()
+    {
+        pf.advance();
+        qf.advance();
+        --left;
+    }
+    // The next step's products.
+    template <class Next, class EachQ>
+    __device__ __forceinline__ void step(f32x4 (&acc)[C::FP][C::FQ], Next next_tile, EachQ each_q)
+    {
+        const unsigned used = stage * C::kStage;
+        if constexpr (C::kEachQ) {
+            typename C::Q::S s;
+#pragma unroll
+            for (int i = 0; i < C::Q::kShare; ++i)
+                s.x[i] = *reinterpret_cast<const u32x4 *>(lds + used + C::P::kBytes + (threadIdx.x + i * C::kThreads) * 16);
+            each_q(s);
+        }
+        if (left == 0)
+            next_tile(*this);
+        multiply_part<C, false>(pa, q, pb, true, lds + used, fp, fq, 1, acc, [](int) {});
+        arrived<0>();
+        stage ^= 1;
+        multiply_part<C, true>(pb, q, pa, true, lds + stage * C::kStage, fp, fq, 0, acc,
+                               [&](int i) { piece(i, lds0 + used); });
+        advance();
+    }
+};
+
+// Through registers, one tile: acc = sum over `depth` of P(p, k) Q(q, k).  A step's
+// loads begin a step before they are stored.  each_q(share): called with each
+// of the Q tiles that this thread brings.
 template <class C, class EachQ>
-__device__ __forceinline__ void tile_product(const Matrix<typename C::T> &mp, unsigned p0,
-                                             const Matrix<typename C::T> &mq, unsigned q0,
+__device__ __forceinline__ void tile_product(const typename C::P::Source &ps, const typename C::Q::Source &qs,
                                              unsigned depth, char *lds,
                                              f32x4 (&acc)[C::FP][C::FQ], EachQ each_q)
 {
     const int wave = uniform(threadIdx.x >> 6);
     const int fp = (wave % C::WP) * C::FP, fq = (wave / C::WP) * C::FQ;
-    const typename C::P::Source ps = {mp, p0};
-    const typename C::Q::Source qs = {mq, q0};
     if (depth == 0)
         return;
+    typename C::P::S sp;
     typename C::Q::S sq;
-    u32x4 p0f[C::FP], p1f[C::FP], q[C::FQ];
-    auto read_first = [&]() {
-#pragma unroll
-        for (int i = 0; i < C::FP; ++i)
-            p0f[i] = C::P::fragment(lds, fp + i, 0);
-#pragma unroll
-        for (int j = 0; j < C::FQ; ++j)
-            q[j] = C::Q::fragment(lds + C::P::kBytes, fq + j, 0);
+    u32x4 pa[C::FP], pb[C::FP], q[C::FQ];
+    auto load = [&](unsigned k) {
+        C::P::load(sp, ps, k);
+        C::Q::load(sq, qs, k);
     };
+    auto bring = [&](unsigned k, unsigned to) {
+        C::P::settle(sp, ps, k);
+        C::Q::settle(sq, qs, k);
+        if constexpr (C::kEachQ)
+            each_q(sq);
+        C::P::store(sp, lds + to * C::kStage);
+        C::Q::store(sq, lds + to * C::kStage + C::P::kBytes);
+    };
+    load(0);
+    bring(0, 0);
+    arrived<0>();
+    read_first<C>(pa, q, lds, fp, fq);
     unsigned stage = 0;
-    if constexpr (C::kAsync) {
-        typename C::P::Feed pf;
-        typename C::Q::Feed qf;
-        pf.start(ps);
-        qf.start(qs);
-        const unsigned lds0 = lds_byte(lds);
-        auto piece = [&](int i, unsigned to) {
-            if (i < C::P::kShare)
-                pf.piece(i, to);
-            else
-                qf.piece(i - C::P::kShare, to + C::P::kBytes);
-        };
-#pragma unroll
-        for (int n = 0; n < 2; ++n) {
-#pragma unroll
-            for (int i = 0; i < C::kLoads; ++i)
-                piece(i, lds0 + n * C::kStage);
-            pf.advance();
-            qf.advance();
-        }
-        arrived<C::kLoads>();
-        read_first();
 #pragma unroll 1
-        for (unsigned k = 0; k < depth; k += C::kDepth) {
-            const unsigned used = stage * C::kStage;
-            if constexpr (C::kEachQ) {
-#pragma unroll
-                for (int i = 0; i < C::Q::kShare; ++i)
-                    sq.x[i] = *reinterpret_cast<const u32x4 *>(lds + used + C::P::kBytes + (threadIdx.x + i * C::kThreads) * 16);
-                each_q(sq);
-            }
-            multiply_part<C, false>(p0f, q, p1f, true, lds + used, fp, fq, 1, acc, [](int) {});
-            arrived<0>();
-            stage ^= 1;
-            multiply_part<C, true>(p1f, q, p0f, true, lds + stage * C::kStage, fp, fq, 0, acc,
-                                   [&](int i) { piece(i, lds0 + used); });
-            pf.advance();
-            qf.advance();
-        }
+    for (unsigned k = 0; k < depth; k += C::kDepth) {
+        const char *from = lds + stage * C::kStage;
+        const bool more = k + C::kDepth < depth;
+        if (more)
+            load(k + C::kDepth);
+        multiply_part<C, false>(pa, q, pb, true, from, fp, fq, 1, acc, [](int) {});
+        stage ^= 1;
+        if (more)
+            bring(k + C::kDepth, stage);
         arrived<0>();
-    } else {
-        // Through registers: a step's loads begin a step before they are stored.
-        typename C::P::S sp;
-        auto load = [&](unsigned k) {
-            C::P::load(sp, ps, k);
-            C::Q::load(sq, qs, k);
-        };
-        auto bring = [&](unsigned k, unsigned to) {
-            C::P::settle(sp, ps, k);
-            C::Q::settle(sq, qs, k);
-            if constexpr (C::kEachQ)
-                each_q(sq);
-            C::P::store(sp, lds + to * C::kStage);
-            C::Q::store(sq, lds + to * C::kStage + C::P::kBytes);
-        };
-        load(0);
-        bring(0, 0);
-        arrived<0>();
-        read_first();
-#pragma unroll 1
-        for (unsigned k = 0; k < depth; k += C::kDepth) {
-            const char *from = lds + stage * C::kStage;
-            const bool more = k + C::kDepth < depth;
-            if (more)
-                load(k + C::kDepth);
-            multiply_part<C, false>(p0f, q, p1f, true, from, fp, fq, 1, acc, [](int) {});
-            stage ^= 1;
-            if (more)
-                bring(k + C::kDepth, stage);
-            arrived<0>();
-            multiply_part<C, false>(p1f, q, p0f, more, lds + stage * C::kStage, fp, fq, 0, acc, [](int) {});
-        }
+        multiply_part<C, false>(pb, q, pa, more, lds + stage * C::kStage, fp, fq, 0, acc, [](int) {});
     }
 }
 
@@ -638,10 +708,7 @@ template <class C>
 constexpr int kResultRow = C::FP * 16 * (int)sizeof(typename C::T) + 16;
 template <class C>
 constexpr int kResultBytes = C::WP * C::WQ * 16 * kResultRow<C>;
-template <class C>
-constexpr int kRowsLds = C::kLds > kResultBytes<C> ? C::kLds : kResultBytes<C>;
-
-__device__ __forceinline__ void store_values(char *to, const float (&v)[4], __bf16)
+__device__ __forceinline__ void store_values(char *to, f32x4 v, __bf16)
 {
     union {
         __bf16 e[4];
@@ -652,70 +719,31 @@ __device__ __forceinline__ void store_values(char *to, const float (&v)[4], __bf
         x.e[i] = (__bf16)v[i];
     *reinterpret_cast<unsigned long long *>(to) = x.u;
 }
-__device__ __forceinline__ void store_values(char *to, const float (&v)[4], float)
-{
-    *reinterpret_cast<f32x4 *>(to) = f32x4{v[0], v[1], v[2], v[3]};
-}
+__device__ __forceinline__ void store_values(char *to, f32x4 v, float) { *reinterpret_cast<f32x4 *>(to) = v; }
 
-// P: the weights (width columns of the result), Q: rows.
+// A tile of the result: rows [t.first, t.last), columns from n0 on.
 template <class C>
-__global__ __launch_bounds__(C::kThreads, 2) void rows_kernel(
-    Problem p, Matrix<typename C::T> w, Matrix<typename C::T> x, const float *bias, int relu,
-    typename C::T *y, long long ys, int width, int depth, unsigned long long from)
+__device__ __forceinline__ void write_rows(const RowTile &t, int n0, int width, const f32x4 (&acc)[C::FP][C::FQ],
+                                           const float *bias, bool relu, char *results,
+                                           typename C::T *y, long long ys)
 {
     using T = typename C::T;
     constexpr int V = Type<T>::kVec;
-    __shared__ __attribute__((aligned(16))) char lds[kRowsLds<C>];
-    __shared__ unsigned tmp[4];
-    __shared__ RowTile found;
-    const Spread s = spread_tiles(p, C::TQ, tmp);
-    const unsigned headless = bound(p, p.heads);
-    const unsigned tail = (unsigned)(((unsigned long long)(p.rows - headless) + C::TQ - 1) / C::TQ);
-    const unsigned row_tiles = s.total + tail, col_tiles = (width + C::TP - 1) / C::TP;
-    const unsigned long long all = (unsigned long long)row_tiles * col_tiles;
-    const size_t head_size = (size_t)p.fan_in * p.fan_out;
-    const unsigned long long at = by_xcd(from + blockIdx.x, all);
-    if (at >= all)
-        return;
-    const Place2 where = in_groups(at, row_tiles, col_tiles);
-    const unsigned tile = where.a;
-    const int n0 = (int)where.b * C::TP;
-    RowTile t;
-    if (tile < s.total) {
-        t = head_tile(s, tile, C::TQ, &found);
-    } else {
-        t.first = headless + (tile - s.total) * C::TQ;
-        t.last = p.rows - t.first > (unsigned)C::TQ ? t.first + C::TQ : p.rows;
-        t.head = p.heads;
-    }
-    const bool headed = t.head < p.heads;
-    f32x4 acc[C::FP][C::FQ] = {};
-    if (headed) {
-        Matrix<T> wh = w, xh = x;
-        wh.p += t.head * head_size;
-        xh.p += t.first * xh.stride;
-        xh.mask += t.first * xh.mask_stride;
-        xh.rows = t.last - t.first;
-        tile_product<C>(wh, n0, xh, 0, depth, lds, acc, [](auto &) {});
-    }
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int wp = (wave % C::WP) * C::FP * 16, wq = (wave / C::WP) * C::FQ * 16;
-    char *mine = lds + wave * 16 * kResultRow<C>;
-    const float *bh = bias && headed ? bias + (size_t)t.head * width : nullptr;
+    char *mine = results + wave * 16 * kResultRow<C>;
 #pragma unroll
     for (int j = 0; j < C::FQ; ++j) {
 #pragma unroll
         for (int i = 0; i < C::FP; ++i) {
             const int e = i * 16 + (lane >> 4) * 4;
-            float v[4];
+            f32x4 v = acc[i][j];
+            if (bias)
+                v += *reinterpret_cast<const f32x4 *>(bias + wp + e);
+            if (relu)
 #pragma unroll
-            for (int k = 0; k < 4; ++k) {
-                v[k] = acc[i][j][k];
-                if (bh && n0 + wp + e + k < width)
-                    v[k] += bh[n0 + wp + e + k];
-                if (relu)
+                for (int k = 0; k < 4; ++k)
                     v[k] = v[k] < 0.0f ? 0.0f : v[k];
-            }
             store_values(mine + (lane & 15) * kResultRow<C> + e * sizeof(T), v, T{});
         }
         __builtin_amdgcn_wave_barrier();
@@ -748,6 +776,108 @@ __global__ __launch_bounds__(C::kThreads, 2) void rows_kernel(
     }
 }
 
+// P: the weights (width columns of the result), Q: rows.
+template <class C>
+__global__ __launch_bounds__(C::kThreads, 2) void rows_kernel(
+    Problem p, Matrix<typename C::T> w, Matrix<typename C::T> x, const float *bias, int relu,
+    typename C::T *y, long long ys, int width, int depth, unsigned from)
+{
+    using T = typename C::T;
+    constexpr int kBiases = C::kAsync ? 4 : 1;  // of the tiles under way
+    __shared__ __attribute__((aligned(16))) char lds[C::kLds];
+    __shared__ __attribute__((aligned(16))) char results[C::kAsync ? kResultBytes<C> : 16];
+    __shared__ __attribute__((aligned(16))) float biases[kBiases][C::TP];
+    __shared__ unsigned before[kMaxHeads + 1];
+    static_assert(C::kAsync || kResultBytes<C> <= C::kLds, "results take the stages' place");
+    count_tiles(p, C::TQ, before);
+    const unsigned headed = uniform(before[p.heads]), headless = bound(p, p.heads);
+    const unsigned tail = (unsigned)(((unsigned long long)(p.rows - headless) + C::TQ - 1) / C::TQ);
+    const unsigned row_tiles = headed + tail, col_tiles = (width + C::TP - 1) / C::TP;
+    const unsigned all = row_tiles * col_tiles, end = runs_end(all);
+    const size_t head_size = (size_t)p.fan_in * p.fan_out;
+    // what workgroup number b does: false if nothing
+    auto tile_at = [&](unsigned b, RowTile &t, int &n0) {
+        const unsigned at = by_xcd(b, all);
+        if (at >= all)
+            return false;
+        const Place2 where = in_groups(at, row_tiles, col_tiles);
+        n0 = (int)where.b * C::TP;
+        if (where.a < headed) {
+            t = head_tile(p, before, where.a, C::TQ);
+        } else {
+            t.first = headless + (where.a - headed) * C::TQ;
+            t.last = p.rows - t.first > (unsigned)C::TQ ? t.first + C::TQ : p.rows;
+            t.head = p.heads;
+        }
+        return true;
+    };
+    auto sources = [&](const RowTile &t, int n0, typename C::P::Source &ps, typename C::Q::Source &qs) {
+        ps = {w, (unsigned)n0};
+        ps.m.p += t.head * head_size;
+        qs = {x, 0};
+        qs.m.p += t.first * x.stride;
+        qs.m.mask += t.first * x.mask_stride;
+        qs.m.rows = t.last - t.first;
+    };
+    RowTile t;
+    int n0;
+    if constexpr (C::kAsync) {
+        unsigned ahead = blockIdx.x, loaded = 0, done = 0;
+        auto next_tile = [&](Pipe<C> &pipe) {
+            RowTile u;
+            int m0;
+            for (; ahead < end; ahead += gridDim.x) {
+                if (!tile_at(ahead, u, m0) || u.head >= p.heads)
+                    continue;
+                ahead += gridDim.x;
+                // its biases too: the first waves bring 64 each
+                if (bias && threadIdx.x < C::TP) {
+                    const Window b = window(bias + (size_t)u.head * width, width, 1, width, 0, m0);
+                    const unsigned wave = uniform(threadIdx.x >> 6);
+                    read4_to_lds(b, threadIdx.x * 4, lds_byte(reinterpret_cast<const char *>(biases[loaded & 3])) + wave * 256);
+                }
+                ++loaded;
+                typename C::P::Source ps;
+                typename C::Q::Source qs;
+                sources(u, m0, ps, qs);
+                pipe.load_tile(ps, qs, depth);
+                return;
+            }
+            pipe.load_nothing();
+        };
+        Pipe<C> pipe;
+        pipe.start(lds, next_tile);
+        for (unsigned b = blockIdx.x; b < end; b += gridDim.x) {
+            if (!tile_at(b, t, n0))
+                continue;
+            f32x4 acc[C::FP][C::FQ] = {};
+            const bool has = t.head < p.heads;
+            if (has)
+#pragma unroll 1
+                for (int k = 0; k < depth; k += C::kDepth)
+                    pipe.step(acc, next_tile, [](auto &) {});
+            write_rows<C>(t, n0, width, acc, has && bias ? biases[done & 3] : nullptr, has && relu, results, y, ys);
+            done += has;
+        }
+        arrived<0>();
+    } else {
+        if (!tile_at(from + blockIdx.x, t, n0))
+            return;
+        f32x4 acc[C::FP][C::FQ] = {};
+        const bool has = t.head < p.heads;
+        if (has) {
+            if (bias && threadIdx.x < C::TP)
+                biases[0][threadIdx.x] =
+                    n0 + (int)threadIdx.x < width ? bias[(size_t)t.head * width + n0 + threadIdx.x] : 0.0f;
+            typename C::P::Source ps;
+            typename C::Q::Source qs;
+            sources(t, n0, ps, qs);
+            tile_product<C>(ps, qs, depth, lds, acc, [](auto &) {});
+        }
+        write_rows<C>(t, n0, width, acc, has && bias ? biases[0] : nullptr, has && relu, lds, y, ys);
+    }
+}
+
 // ---- weights ----------------------------------------------------------------------
 
 // P: x, Q: dz, reduced over rows: a tile of a head's dW from a stretch of
@@ -755,45 +885,58 @@ __global__ __launch_bounds__(C::kThreads, 2) void rows_kernel(
 // each has a place of its own in dw and db, and sum_kernel adds them up.
 template <class C>
 __global__ __launch_bounds__(C::kThreads, 2) void weights_kernel(Problem p, Matrix<typename C::T> dz,
-                                                              Matrix<typename C::T> x, float *dw,
-                                                              float *db, unsigned stretch,
-                                                              bool partial, unsigned places,
-                                                              unsigned row_tiles, unsigned col_tiles,
-                                                              unsigned long long from)
+                                                                 Matrix<typename C::T> x, float *dw,
+                                                                 float *db, unsigned stretch,
+                                                                 unsigned places, unsigned row_tiles,
+                                                                 unsigned col_tiles, unsigned from)
 {
     using T = typename C::T;
     constexpr int V = Type<T>::kVec;
+    // a thread's sums are over every (threads / kPerRow)-th row of its columns
+    constexpr int kRowsOfThreads = C::kThreads / C::Q::kPerRow;
+    constexpr int kSumsBytes = kRowsOfThreads * (C::TQ + 1) * (int)sizeof(float);
     __shared__ __attribute__((aligned(16))) char lds[C::kLds];
-    __shared__ unsigned tmp[4];
-    __shared__ RowTile found;
+    __shared__ __attribute__((aligned(16))) char sums_lds[C::kAsync ? kSumsBytes : 16];
+    __shared__ unsigned before[kMaxHeads + 1];
+    static_assert(C::kAsync || kSumsBytes <= C::kLds, "sums take the stages' place");
     const int I = p.fan_in, O = p.fan_out;
     const unsigned each = row_tiles * col_tiles;  // of a place
-    const unsigned long long at = by_xcd(from + blockIdx.x, (unsigned long long)places * each);
-    const unsigned place = (unsigned)(at / each);
-    if (place >= places)
-        return;
-    const Place2 where = in_groups(at - (unsigned long long)place * each, row_tiles, col_tiles);
-    const int m0 = (int)where.a * C::TQ, n0 = (int)where.b * C::TP;  // of dz, of x
-    RowTile t;
-    if (partial) {
-        const Spread s = spread_tiles(p, stretch, tmp);
-        if (place >= s.total)
-            return;
-        t = head_tile(s, place, stretch, &found);
-    } else {
-        t.first = uniform(bound(p, place));
-        t.last = uniform(bound(p, place + 1));
-        t.last = t.last > t.first ? t.last : t.first;
+    if (stretch) {
+        count_tiles(p, stretch, before);
+        places = uniform(before[p.heads]);
     }
-    Matrix<T> mz = dz, mx = x;
-    mz.p += t.first * mz.stride;
-    mz.mask += t.first * mz.mask_stride;
-    mx.p += t.first * mx.stride;
-    mz.rows = mx.rows = t.last - t.first;
-    const bool sum = db && n0 == 0;
-    float sums[V] = {};
-    f32x4 acc[C::FP][C::FQ] = {};
-    tile_product<C>(mx, n0, mz, m0, mz.rows, lds, acc, [&](const typename C::Q::S &share) {
+    const unsigned all = places * each, end = runs_end(all);
+    auto tile_at = [&](unsigned b, unsigned &place, RowTile &t, int &m0, int &n0) {
+        const unsigned at = by_xcd(b, all);
+        if (at >= all)
+            return false;
+        place = at / each;
+        const Place2 where = in_groups(at - place * each, row_tiles, col_tiles);
+        m0 = (int)where.a * C::TQ;  // of dz
+        n0 = (int)where.b * C::TP;  // of x
+        if (stretch) {
+            t = head_tile(p, before, place, stretch);
+        } else {
+            t.first = uniform(bound(p, place));
+            t.last = uniform(bound(p, place + 1));
+            t.last = t.last > t.first ? t.last : t.first;
+        }
+        return true;
+    };
+    auto sources = [&](const RowTile &t, int m0, int n0, typename C::P::Source &ps, typename C::Q::Source &qs) {
+        ps = {x, (unsigned)n0};
+        ps.m.p += t.first * x.stride;
+        qs = {dz, (unsigned)m0};
+        qs.m.p += t.first * dz.stride;
+        qs.m.mask += t.first * dz.mask_stride;
+        ps.m.rows = qs.m.rows = t.last - t.first;
+    };
+    unsigned place;
+    RowTile t;
+    int m0, n0;
+    float sums[V];
+    bool sum;
+    auto add_sums = [&](const typename C::Q::S &share) {
         if (!sum)
             return;
 #pragma unroll
@@ -806,36 +949,41 @@ __global__ __launch_bounds__(C::kThreads, 2) void weights_kernel(Problem p, Matr
             for (int k = 0; k < V; ++k)
                 sums[k] += (float)piece.e[k];
         }
-    });
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const int wp = (wave % C::WP) * C::FP * 16, wq = (wave / C::WP) * C::FQ * 16;
-    if (dw) {
-        float *to = dw + (size_t)place * O * I;
+    };
+    auto begin = [&]() {
+        sum = db && n0 == 0;
 #pragma unroll
-        for (int j = 0; j < C::FQ; ++j) {
-            const int m = m0 + wq + j * 16 + (lane & 15);
+        for (int k = 0; k < V; ++k)
+            sums[k] = 0.0f;
+    };
+    auto write = [&](const f32x4(&acc)[C::FP][C::FQ], char *sums_at) {
+        const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
+        const int wp = (wave % C::WP) * C::FP * 16, wq = (wave / C::WP) * C::FQ * 16;
+        if (dw) {
+            float *to = dw + (size_t)place * O * I;
 #pragma unroll
-            for (int i = 0; i < C::FP; ++i) {
-                const int n = n0 + wp + i * 16 + (lane >> 4) * 4;
-                if (m >= O || n >= I)
-                    continue;
-                float *at = to + ((size_t)m * I + n);
-                if (n + 4 <= I) {
-                    reinterpret_cast<Bytes16 *>(at)->v = __builtin_bit_cast(u32x4, acc[i][j]);
-                } else {
+            for (int j = 0; j < C::FQ; ++j) {
+                const int m = m0 + wq + j * 16 + (lane & 15);
 #pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        if (n + k < I)
-                            at[k] = acc[i][j][k];
+                for (int i = 0; i < C::FP; ++i) {
+                    const int n = n0 + wp + i * 16 + (lane >> 4) * 4;
+                    if (m >= O || n >= I)
+                        continue;
+                    float *at = to + ((size_t)m * I + n);
+                    if (n + 4 <= I) {
+                        reinterpret_cast<Bytes16 *>(at)->v = __builtin_bit_cast(u32x4, acc[i][j]);
+                    } else {
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (n + k < I)
+                                at[k] = acc[i][j][k];
+                    }
                 }
             }
         }
-    }
-    if (sum) {
-        // a thread's sums are over every (threads / kPerRow)-th row of its columns
-        constexpr int kRowsOfThreads = C::kThreads / C::Q::kPerRow;
-        float(*part)[C::TQ + 1] = reinterpret_cast<float(*)[C::TQ + 1]>(lds);
-        static_assert(sizeof(float) * kRowsOfThreads * (C::TQ + 1) <= C::kLds, "fits");
+        if (!sum)
+            return;
+        float(*part)[C::TQ + 1] = reinterpret_cast<float(*)[C::TQ + 1]>(sums_at);
         __syncthreads();
 #pragma unroll
         for (int k = 0; k < V; ++k)
@@ -848,25 +996,77 @@ __global__ __launch_bounds__(C::kThreads, 2) void weights_kernel(Problem p, Matr
             if (m0 + m < O)
                 db[(size_t)place * O + m0 + m] = v;
         }
+    };
+    if constexpr (C::kAsync) {
+        unsigned ahead = blockIdx.x;
+        auto next_tile = [&](Pipe<C> &pipe) {
+            unsigned pl;
+            RowTile u;
+            int a, b;
+            for (; ahead < end; ahead += gridDim.x) {
+                if (!tile_at(ahead, pl, u, a, b) || u.first == u.last)
+                    continue;
+                ahead += gridDim.x;
+                typename C::P::Source ps;
+                typename C::Q::Source qs;
+                sources(u, a, b, ps, qs);
+                pipe.load_tile(ps, qs, u.last - u.first);
+                return;
+            }
+            pipe.load_nothing();
+        };
+        Pipe<C> pipe;
+        pipe.start(lds, next_tile);
+        for (unsigned b = blockIdx.x; b < end; b += gridDim.x) {
+            if (!tile_at(b, place, t, m0, n0))
+                continue;
+            begin();
+            f32x4 acc[C::FP][C::FQ] = {};
+#pragma unroll 1
+            for (unsigned k = t.first; k < t.last; k += C::kDepth)
+                pipe.step(acc, next_tile, add_sums);
+            write(acc, sums_lds);
+        }
+        arrived<0>();
+    } else {
+        if (!tile_at(from + blockIdx.x, place, t, m0, n0))
+            return;
+        begin();
+        f32x4 acc[C::FP][C::FQ] = {};
+        typename C::P::Source ps;
+        typename C::Q::Source qs;
+        sources(t, m0, n0, ps, qs);
+        tile_product<C>(ps, qs, t.last - t.first, lds, acc, add_sums);
+        write(acc, lds);
     }
 }
 
-// out[h][e] = the sum of head h's stretches' parts, in order.
-__global__ __launch_bounds__(256) void sum_kernel(Problem p, unsigned stretch, const float *parts,
-                                                  size_t size, float *out)
+// out[h][e] = the sum of head h's stretches' parts, in order: the weights' in the
+// first blocks of a head, the biases' in its last.
+__global__ __launch_bounds__(256) void sum_kernel(Problem p, unsigned stretch, const float *wparts, size_t wsize, float *dw,
+                                                  const float *bparts, float *db, unsigned wblocks)
 {
-    __shared__ unsigned tmp[4];
-    __shared__ unsigned range[2];
-    const Spread s = spread_tiles(p, stretch, tmp);
-    if (threadIdx.x == blockIdx.y) {
-        range[0] = s.before;
-        range[1] = s.before + s.mine;
-    }
-    __syncthreads();
-    const unsigned a = range[0], b = range[1];
-    for (size_t e = blockIdx.x * 256 + threadIdx.x; e < size; e += (size_t)gridDim.x * 256) {
+    __shared__ unsigned before[kMaxHeads + 1];
+    count_tiles(p, stretch, before);
+    const unsigned a = uniform(before[blockIdx.y]), b = uniform(before[blockIdx.y + 1]);
+    const bool biases = blockIdx.x >= wblocks;
+    const float *parts = biases ? bparts : wparts;
+    float *out = biases ? db : dw;
+    const size_t size = biases ? (size_t)p.fan_out : wsize;
+    const unsigned block = biases ? blockIdx.x - wblocks : blockIdx.x, blocks = biases ? gridDim.x - wblocks : wblocks;
+    for (size_t e = block * 256 + threadIdx.x; e < size; e += (size_t)blocks * 256) {
         float v = 0.0f;
-        for (unsigned i = a; i < b; ++i)
+        unsigned i = a;
+        for (; i + 8 <= b; i += 8) {
+            float x[8];
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                x[k] = parts[(i + k) * size + e];
+#pragma unroll
+            for (int k = 0; k < 8; ++k)
+                v += x[k];
+        }
+        for (; i < b; ++i)
             v += parts[i * size + e];
         out[blockIdx.y * size + e] = v;
     }
@@ -874,9 +1074,33 @@ __global__ __launch_bounds__(256) void sum_kernel(Problem p, unsigned stretch, c
 
 // ---- choice of a form ---------------------------------------------------------------
 
-constexpr unsigned kMostGroups = 1u << 22;  // workgroups of a launch
-
 unsigned tiles_of(long long n, int tile) { return (unsigned)((n + tile - 1) / tile); }
+
+// Launches for at most `all` tiles: launch(workgroups, from).  Where workgroups
+// take tiles one after another (ASYNC), as many as run at once; else one a tile,
+// within a launch's limits.
+template <class C, class F>
+hipError_t launch_for(unsigned long long all, F launch)
+{
+    if (all >= 1ull << 31)  // more than any memory holds
+        return hipErrorInvalidConfiguration;
+    const unsigned end = (unsigned)all + kXcds * kRun;  // runs_end of as many or fewer is not above it
+    if (C::kAsync) {
+        int device, cus;
+        hipError_t e = hipGetDevice(&device);
+        if (e == hipSuccess)
+            e = hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, device);
+        if (e != hipSuccess)
+            return e;
+        const unsigned most = (unsigned)cus * (C::kThreads >= 512 ? 1 : 2);
+        launch(end < most ? end : most, 0u);
+    } else {
+        constexpr unsigned kMost = 1u << 22;
+        for (unsigned from = 0; from < end; from += kMost)
+            launch(end - from < kMost ? end - from : kMost, from);
+    }
+    return hipGetLastError();
+}
 
 template <class C>
 hipError_t launch_rows(const Problem &p, const Matrix<typename C::T> &w,
@@ -885,12 +1109,11 @@ hipError_t launch_rows(const Problem &p, const Matrix<typename C::T> &w,
 {
     using T = typename C::T;
     // at most: every head's last tile and the headless rows' may be partly filled
-    unsigned long long all = ((unsigned long long)p.rows / C::TQ + p.heads + 1) * tiles_of(width, C::TP);
-    all += kXcds * kRun;
-    for (unsigned long long from = 0; from < all; from += kMostGroups)
-        rows_kernel<C><<<(unsigned)(all - from < kMostGroups ? all - from : kMostGroups), C::kThreads, 0, s>>>(
-            p, w, x, bias, relu, static_cast<T *>(const_cast<void *>(y.p)), y.stride, width, depth, from);
-    return hipGetLastError();
+    return launch_for<C>(((unsigned long long)p.rows / C::TQ + p.heads + 1) * tiles_of(width, C::TP),
+                         [&](unsigned groups, unsigned from) {
+                             rows_kernel<C><<<groups, C::kThreads, 0, s>>>(
+                                 p, w, x, bias, relu, static_cast<T *>(const_cast<void *>(y.p)), y.stride, width, depth, from);
+                         });
 }
 
 // Whether an operand can go from memory to LDS by itself (Tile::load_async).
@@ -959,17 +1182,16 @@ hipError_t launch_weights(const Problem &p, const Matrix<typename C::T> &dz,
     float *bparts = wparts + (size_t)split.places * size;
     float *to_w = dw ? (partial ? wparts : dw) : nullptr, *to_b = db ? (partial ? bparts : db) : nullptr;
     const unsigned row_tiles = tiles_of(p.fan_out, C::TQ), col_tiles = dw ? tiles_of(p.fan_in, C::TP) : 1;
-    const unsigned long long all = (unsigned long long)split.places * row_tiles * col_tiles + kXcds * kRun;
-    for (unsigned long long from = 0; from < all; from += kMostGroups)
-        weights_kernel<C><<<(unsigned)(all - from < kMostGroups ? all - from : kMostGroups), C::kThreads, 0, s>>>(
-            p, dz, x, to_w, to_b, split.stretch, partial, split.places, row_tiles, col_tiles, from);
+    const hipError_t e = launch_for<C>(
+        (unsigned long long)split.places * row_tiles * col_tiles, [&](unsigned groups, unsigned from) {
+            weights_kernel<C><<<groups, C::kThreads, 0, s>>>(p, dz, x, to_w, to_b, split.stretch, split.places, row_tiles, col_tiles, from);
+        });
+    if (e != hipSuccess)
+        return e;
     if (partial) {
-        if (dw) {
-            const unsigned blocks = tiles_of(size, 256);
-            sum_kernel<<<dim3(blocks < 1024 ? blocks : 1024, p.heads), 256, 0, s>>>(p, split.stretch, wparts, size, dw);
-        }
-        if (db)
-            sum_kernel<<<dim3(tiles_of(p.fan_out, 256), p.heads), 256, 0, s>>>(p, split.stretch, bparts, p.fan_out, db);
+        const unsigned blocks = dw ? tiles_of(size, 256) : 0, wblocks = blocks < 1024 ? blocks : 1024;
+        const unsigned bblocks = db ? tiles_of(p.fan_out, 256) : 0;
+        sum_kernel<<<dim3(wblocks + bblocks, p.heads), 256, 0, s>>>(p, split.stretch, wparts, size, dw, bparts, db, wblocks);
     }
     return hipGetLastError();
 }
