@@ -179,16 +179,29 @@ template <class T, int V>
 struct __attribute__((packed, aligned(sizeof(T)))) Vec {
     T v[V];
 };
+typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
+typedef u32x4 __attribute__((aligned(2))) Any16;  // 16 bytes at any element
 
-template <class T, int V>
+// ONCE: what is read once, or written and not read again before much else is,
+// goes past the caches (nontemporal).  For rows of whole 128-byte lines: there
+// 524,288 rows of 1,024 bf16 are written in the order of heads in 215 us, 432 with
+// ordinary stores, and summed back in 222, 264 with ordinary loads; 262,144 rows
+// of 63 float, whose lines are shared, take 31 and 21 us so, 29 and 19 without.
+template <class T, int V, bool ONCE = false>
 __device__ __forceinline__ Vec<T, V> load_vec(const T *p)
 {
-    return *reinterpret_cast<const Vec<T, V> *>(p);
+    if constexpr (ONCE)
+        return __builtin_bit_cast(Vec<T, V>, (u32x4)__builtin_nontemporal_load(reinterpret_cast<const Any16 *>(p)));
+    else
+        return *reinterpret_cast<const Vec<T, V> *>(p);
 }
-template <class T, int V>
+template <class T, int V, bool ONCE>
 __device__ __forceinline__ void store_vec(T *p, const Vec<T, V> &x)
 {
-    *reinterpret_cast<Vec<T, V> *>(p) = x;
+    if constexpr (ONCE)
+        __builtin_nontemporal_store(__builtin_bit_cast(u32x4, x), reinterpret_cast<Any16 *>(p));
+    else
+        *reinterpret_cast<Vec<T, V> *>(p) = x;
 }
 
 // First element of vector c of a row of D elements.
@@ -214,7 +227,11 @@ __device__ __forceinline__ Lane lane_of(int group_log2)
 // The place of a pair's row, and whether it has a head.
 __device__ __forceinline__ unsigned place_of(int row) { return row < 0 ? (unsigned)(-1 - row) : (unsigned)row; }
 
-template <class T, int V>
+// Vectors of a row that a lane has under way at once.
+constexpr int kAhead = 4;
+
+// A row is read once and written top_k times, whole rows one after another.
+template <class T, int V, bool ONCE>
 __global__ __launch_bounds__(kRowThreads) void dispatch_kernel(const T *x, long long xs,
                                                                const int *row, long long tokens,
                                                                int top_k, int D, T *out,
@@ -226,52 +243,88 @@ __global__ __launch_bounds__(kRowThreads) void dispatch_kernel(const T *x, long 
     for (long long t = l.item; t < tokens; t += l.stride) {
         const T *xr = x + t * xs;
         const int *rr = row + t * top_k;
-        for (int c = l.at; c < vecs; c += l.step) {
-            const int e = vec_at<V>(c, D);
-            const Vec<T, V> v = load_vec<T, V>(xr + e);
+        for (int c0 = l.at; c0 < vecs; c0 += kAhead * l.step) {
+            Vec<T, V> v[kAhead];
+#pragma unroll
+            for (int i = 0; i < kAhead; ++i)
+                if (c0 + i * l.step < vecs)
+                    v[i] = load_vec<T, V>(xr + vec_at<V>(c0 + i * l.step, D));
             for (int j = 0; j < top_k; ++j) {
                 const int r = rr[j];
-                store_vec<T, V>(out + (long long)place_of(r) * os + e, r < 0 ? zero : v);
+                T *to = out + (long long)place_of(r) * os;
+#pragma unroll
+                for (int i = 0; i < kAhead; ++i)
+                    if (c0 + i * l.step < vecs)
+                        store_vec<T, V, ONCE>(to + vec_at<V>(c0 + i * l.step, D), r < 0 ? zero : v[i]);
             }
         }
     }
 }
 
-template <class T, int V>
+// Vectors of four of a sample's rows are read at once; the sum goes in the
+// order of j.
+template <class T, int V, bool ONCE>
 __global__ __launch_bounds__(kRowThreads) void combine_kernel(const T *rows, long long rs,
                                                               const float *weights, const int *row,
                                                               long long tokens, int top_k, int D,
                                                               T *out, long long os, int group_log2)
 {
+    constexpr int kRows = 4, kVecs = ONCE ? 2 : 1;  // short rows leave the second idle
     const Lane l = lane_of(group_log2);
     const int vecs = (D + V - 1) / V;
     for (long long t = l.item; t < tokens; t += l.stride) {
         const int *rr = row + t * top_k;
         const float *wr = weights ? weights + t * top_k : nullptr;
-        for (int c = l.at; c < vecs; c += l.step) {
-            const int e = vec_at<V>(c, D);
-            float sum[V] = {};
-            for (int j = 0; j < top_k; ++j) {
-                const int r = rr[j];
-                if (r < 0)
-                    continue;
-                const float w = wr ? wr[j] : 1.0f;
-                const Vec<T, V> v = load_vec<T, V>(rows + (long long)r * rs + e);
+        for (int c0 = l.at; c0 < vecs; c0 += kVecs * l.step) {
+            int e[kVecs];
+            float sum[kVecs][V];
+#pragma unroll
+            for (int k = 0; k < kVecs; ++k) {
+                e[k] = c0 + k * l.step < vecs ? vec_at<V>(c0 + k * l.step, D) : -1;
 #pragma unroll
                 for (int i = 0; i < V; ++i)
-                    sum[i] = fmaf(w, (float)v.v[i], sum[i]);
+                    sum[k][i] = 0.0f;
             }
-            Vec<T, V> y;
+            for (int j0 = 0; j0 < top_k; j0 += kRows) {
+                int r[kRows];
+                float w[kRows];
+                Vec<T, V> v[kRows][kVecs];
 #pragma unroll
-            for (int i = 0; i < V; ++i)
-                y.v[i] = (T)sum[i];
-            store_vec<T, V>(out + t * os + e, y);
+                for (int j = 0; j < kRows; ++j) {
+                    r[j] = j0 + j < top_k ? rr[j0 + j] : -1;
+                    w[j] = r[j] >= 0 && wr ? wr[j0 + j] : 1.0f;
+                }
+#pragma unroll
+                for (int j = 0; j < kRows; ++j)
+                    if (r[j] >= 0)
+#pragma unroll
+                        for (int k = 0; k < kVecs; ++k)
+                            if (k == 0 || e[k] >= 0)
+                                v[j][k] = load_vec<T, V, ONCE>(rows + (long long)r[j] * rs + e[k]);
+#pragma unroll
+                for (int j = 0; j < kRows; ++j)
+                    if (r[j] >= 0)
+#pragma unroll
+                        for (int k = 0; k < kVecs; ++k)
+#pragma unroll
+                            for (int i = 0; i < V; ++i)
+                                sum[k][i] = fmaf(w[j], (float)v[j][k].v[i], sum[k][i]);
+            }
+#pragma unroll
+            for (int k = 0; k < kVecs; ++k) {
+                Vec<T, V> y;
+#pragma unroll
+                for (int i = 0; i < V; ++i)
+                    y.v[i] = (T)sum[k][i];
+                if (k == 0 || e[k] >= 0)
+                    store_vec<T, V, ONCE>(out + t * os + e[k], y);
+            }
         }
     }
 }
 
 // A group of lanes takes one pair.
-template <class T, int V>
+template <class T, int V, bool ONCE>
 __global__ __launch_bounds__(kRowThreads) void combine_backward_kernel(
     const T *dout, long long ds, const T *rows, long long rs, const float *weights, const int *row,
     long long pairs, int top_k, int D, T *drows, long long os, float *dweights, int group_log2)
@@ -298,7 +351,7 @@ __global__ __launch_bounds__(kRowThreads) void combine_backward_kernel(
                     for (int i = 0; i < V; ++i)
                         y.v[i] = (T)(w * (float)d.v[i]);
                     if (dweights) {
-                        const Vec<T, V> v = load_vec<T, V>(xr + e);
+                        const Vec<T, V> v = load_vec<T, V, ONCE>(xr + e);
                         const int skip = c * V - e;  // elements that the vector before has too
 #pragma unroll
                         for (int i = 0; i < V; ++i)
@@ -306,7 +359,7 @@ __global__ __launch_bounds__(kRowThreads) void combine_backward_kernel(
                                 dot = fmaf((float)d.v[i], (float)v.v[i], dot);
                     }
                 }
-                store_vec<T, V>(drows + place * os + e, y);
+                store_vec<T, V, ONCE>(drows + place * os + e, y);
             }
         }
         if (dweights) {
@@ -334,14 +387,27 @@ unsigned groups_grid(long long items, int group_log2)
     return (unsigned)(blocks < (1 << 22) ? blocks : 1 << 22);
 }
 
-// Calls f(T{}, V) with the rows' type and the vector length for rows of D.
-template <class F>
-hipError_t with_rows(bool bf16, int D, F f)
+// Whole 128-byte lines.
+bool whole_lines(const Rows &r, int D, int size)
 {
+    return D * size % 128 == 0 && r.stride * size % 128 == 0 && reinterpret_cast<uintptr_t>(r.p) % 128 == 0;
+}
+
+// Calls f(T{}, V, ONCE) with the rows' type, the vector length for rows of D and
+// whether they are whole lines.
+template <class F>
+hipError_t with_rows(bool bf16, int D, bool lines, F f)
+{
+    using Yes = std::true_type;
+    using No = std::false_type;
     if (bf16)
-        D >= 8 ? f(__bf16{}, std::integral_constant<int, 8>{}) : f(__bf16{}, std::integral_constant<int, 1>{});
+        lines ? f(__bf16{}, std::integral_constant<int, 8>{}, Yes{})
+        : D >= 8 ? f(__bf16{}, std::integral_constant<int, 8>{}, No{})
+                 : f(__bf16{}, std::integral_constant<int, 1>{}, No{});
     else
-        D >= 4 ? f(float{}, std::integral_constant<int, 4>{}) : f(float{}, std::integral_constant<int, 1>{});
+        lines ? f(float{}, std::integral_constant<int, 4>{}, Yes{})
+        : D >= 4 ? f(float{}, std::integral_constant<int, 4>{}, No{})
+                 : f(float{}, std::integral_constant<int, 1>{}, No{});
     return hipGetLastError();
 }
 
@@ -375,11 +441,14 @@ hipError_t launch_route(const int *heads, unsigned pairs, int num_heads, int *of
 hipError_t launch_dispatch(Rows x, const int *row, long long tokens, int top_k, int dim, bool bf16,
                            Rows out, hipStream_t s)
 {
-    return with_rows(bf16, dim, [&](auto t, auto v) {
+    const int size = bf16 ? 2 : 4;
+    const bool lines = whole_lines(out, dim, size);
+    return with_rows(bf16, dim, lines, [&](auto t, auto v, auto once) {
         using T = decltype(t);
         constexpr int V = decltype(v)::value;
+        constexpr bool ONCE = decltype(once)::value;
         const int g = group_log2_of((dim + V - 1) / V);
-        dispatch_kernel<T, V><<<groups_grid(tokens, g), kRowThreads, 0, s>>>(
+        dispatch_kernel<T, V, ONCE><<<groups_grid(tokens, g), kRowThreads, 0, s>>>(
             static_cast<const T *>(x.p), x.stride, row, tokens, top_k, dim,
             static_cast<T *>(const_cast<void *>(out.p)), out.stride, g);
     });
@@ -388,11 +457,14 @@ hipError_t launch_dispatch(Rows x, const int *row, long long tokens, int top_k, 
 hipError_t launch_combine(Rows rows, const float *weights, const int *row, long long tokens,
                           int top_k, int dim, bool bf16, Rows out, hipStream_t s)
 {
-    return with_rows(bf16, dim, [&](auto t, auto v) {
+    const int size = bf16 ? 2 : 4;
+    const bool lines = whole_lines(rows, dim, size) && whole_lines(out, dim, size);
+    return with_rows(bf16, dim, lines, [&](auto t, auto v, auto once) {
         using T = decltype(t);
         constexpr int V = decltype(v)::value;
+        constexpr bool ONCE = decltype(once)::value;
         const int g = group_log2_of((dim + V - 1) / V);
-        combine_kernel<T, V><<<groups_grid(tokens, g), kRowThreads, 0, s>>>(
+        combine_kernel<T, V, ONCE><<<groups_grid(tokens, g), kRowThreads, 0, s>>>(
             static_cast<const T *>(rows.p), rows.stride, weights, row, tokens, top_k, dim,
             static_cast<T *>(const_cast<void *>(out.p)), out.stride, g);
     });
@@ -402,11 +474,14 @@ hipError_t launch_combine_backward(Rows dout, Rows rows, const float *weights, c
                                    long long tokens, int top_k, int dim, bool bf16, Rows drows,
                                    float *dweights, hipStream_t s)
 {
-    return with_rows(bf16, dim, [&](auto t, auto v) {
+    const int size = bf16 ? 2 : 4;
+    const bool lines = whole_lines(drows, dim, size) && (!dweights || whole_lines(rows, dim, size));
+    return with_rows(bf16, dim, lines, [&](auto t, auto v, auto once) {
         using T = decltype(t);
         constexpr int V = decltype(v)::value;
+        constexpr bool ONCE = decltype(once)::value;
         const int g = group_log2_of((dim + V - 1) / V);
-        combine_backward_kernel<T, V><<<groups_grid(tokens * top_k, g), kRowThreads, 0, s>>>(
+        combine_backward_kernel<T, V, ONCE><<<groups_grid(tokens * top_k, g), kRowThreads, 0, s>>>(
             static_cast<const T *>(dout.p), dout.stride, static_cast<const T *>(rows.p),
             rows.stride, weights, row, tokens * top_k, top_k, dim,
             static_cast<T *>(const_cast<void *>(drows.p)), drows.stride, dweights, g);
