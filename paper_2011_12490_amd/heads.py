@@ -44,12 +44,17 @@ class Routing(NamedTuple):
     num_heads: int
 
 
+_entry = {}  # entry points by name
+
+
 def _call(name: str, device: torch.device, *args) -> None:
     """Call an entry point with the device's current stream as its last argument."""
-    f = getattr(derf.lib(), name)
+    f = _entry.get(name)
+    if f is None:
+        f = _entry[name] = getattr(derf.lib(), name)
     index = device.index
     stream = torch._C._cuda_getCurrentRawStream(index)  # without the Stream object
-    if torch.cuda.current_device() == index:
+    if torch._C._cuda_getDevice() == index:
         status = f(*args, stream)
     else:
         with torch.cuda.device(index):
@@ -90,19 +95,23 @@ def _rows(x, name, shape=None, dtype=None, device=None) -> int:
         raise ValueError("%s must be a tensor on %s" % (name, device or "a GPU"))
     if x.dtype not in _PRECISION or (dtype is not None and x.dtype != dtype):
         raise ValueError("%s must be %s, got %s" % (name, dtype or "float32 or bfloat16", x.dtype))
-    if x.dim() != 2 or x.shape[1] < 1 or (shape is not None and x.shape != shape):
+    size = x.shape
+    if len(size) != 2 or size[1] < 1 or (shape is not None and size != shape):
         raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape) if shape else "[rows, dim]",
-                                                           tuple(x.shape)))
-    if x.shape[1] > 1 and x.stride(1) != 1:
+                                                           tuple(size)))
+    stride, step = x.stride()
+    if step != 1 and size[1] > 1:
         raise ValueError("%s: the elements of a row must lie side by side" % name)
-    if x.shape[0] > 1 and x.stride(0) < x.shape[1]:
-        raise ValueError("%s: rows overlap" % name)
-    return max(x.stride(0), x.shape[1])
+    if stride < size[1]:
+        if size[0] > 1:
+            raise ValueError("%s: rows overlap" % name)
+        return size[1]
+    return stride
 
 
 def _out_rows(out, name, rows, dim, like):
     if out is None:
-        return torch.empty((rows, dim), dtype=like.dtype, device=like.device), dim
+        return like.new_empty((rows, dim)), dim
     return out, _rows(out, name, (rows, dim), like.dtype, like.device)
 
 
@@ -120,10 +129,12 @@ def _workspace(need: int, device):
 def _routing(routing, device):
     if not isinstance(routing, Routing):
         raise ValueError("routing must be a Routing")
-    if not isinstance(routing.row, torch.Tensor) or routing.row.dim() != 2:
+    row = routing.row
+    if not isinstance(row, torch.Tensor) or row.dim() != 2:
         raise ValueError("routing.row must be a tensor [T, k]")
-    _array(routing.row, "routing.row", torch.int32, routing.row.shape, device)
-    return routing.row.shape
+    if row.dtype != torch.int32 or row.device != device or not row.is_contiguous():
+        raise ValueError("routing.row must be a contiguous int32 tensor on %s" % device)
+    return row.shape
 
 
 def route(ids: torch.Tensor, num_heads: int) -> Routing:
@@ -137,9 +148,7 @@ def route(ids: torch.Tensor, num_heads: int) -> Routing:
     if need < 0:
         raise ValueError("invalid sizes: %d samples, %d pairs each, %d heads" % (T, k, num_heads))
     dev = ids.device
-    offsets = torch.empty((num_heads + 1,), dtype=torch.int32, device=dev)
-    pair = torch.empty((T * k,), dtype=torch.int32, device=dev)
-    row = torch.empty((T, k), dtype=torch.int32, device=dev)
+    offsets, pair, row = ids.new_empty((num_heads + 1,)), ids.new_empty((T * k,)), torch.empty_like(ids)
     ws = _workspace(need, dev)
     _call("derf_route", dev, ids.data_ptr(), T, k, num_heads, offsets.data_ptr(), pair.data_ptr(),
           row.data_ptr(), _ptr(ws), need)
