@@ -465,9 +465,10 @@ int derf_heads_linear(const void *x, long long x_stride, const void *w, const fl
  *   out_bias  float [num_heads][fan_out]: sum_r dz[r]
  * Heads without rows get zeros.  Any of the three outputs may be NULL (then
  * what only it needs may be NULL too: w for out_x, x for out_w).
- *   workspace  derf_heads_linear_workspace(...) bytes (-1 for invalid sizes) */
+ *   workspace  derf_heads_linear_workspace(...) bytes (-1 for invalid sizes);
+ *              relu: whether y will be given */
 long long derf_heads_linear_workspace(long long num_rows, int num_heads, int fan_in, int fan_out,
-                                      int precision);
+                                      int relu, int precision);
 int derf_heads_linear_backward(const void *dy, long long dy_stride, const void *x,
                                long long x_stride, const void *w, const void *y,
                                long long y_stride, const int *offsets, long long num_rows,

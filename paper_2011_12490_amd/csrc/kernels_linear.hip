@@ -253,6 +253,9 @@ __device__ __forceinline__ void arrived()
     asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(N) : "memory");
 }
 
+// The same for LDS accesses alone.
+__device__ __forceinline__ void stored() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+
 // Tile of an operand: DEEP: TILE rows by D columns, else D rows by TILE columns;
 // one depth step's, D elements being 128 bytes.  In LDS it lies row by row in
 // 16-byte chunks, a row's chunks permuted by the row so that reads touch every
@@ -513,6 +516,10 @@ struct Product {
     static constexpr int FP = TP / WP / 16, FQ = TQ / WQ / 16;  // a wave's 16 x 16 results
     static constexpr int kStage = P::kBytes + Q::kBytes, kLds = 2 * kStage;
     static constexpr int kLoads = P::kShare + Q::kShare;  // of a thread for a step
+    // tile_product's sets of registers: a second one costs masked 128 x 128 tiles
+    // spills and narrow ones a workgroup more on the compute unit (262,144 rows of
+    // 64 to 64 24 us, 18 with one; of 319 to 256 132, 147 with one)
+    static constexpr int kSets = !MASK && FP * FQ >= 16 ? 2 : 1;
     static_assert(FP * WP * 16 == TP && FQ * WQ * 16 == TQ, "whole results a wave");
 };
 
@@ -652,8 +659,9 @@ struct Pipe {
 };
 
 // Through registers, one tile: acc = sum over `depth` of P(p, k) Q(q, k).  A step's
-// loads begin a step before they are stored.  each_q(share): called with each
-// of the Q tiles that this thread brings.
+// loads begin two steps before it is stored, into two sets of registers in turn
+// (one step is shorter than a load takes), or one where there is no room for two.
+// each_q(share): called with each of the Q tiles that this thread brings.
 template <class C, class EachQ>
 __device__ __forceinline__ void tile_product(const typename C::P::Source &ps, const typename C::Q::Source &qs,
                                              unsigned depth, char *lds,
@@ -663,38 +671,48 @@ __device__ __forceinline__ void tile_product(const typename C::P::Source &ps, co
     const int fp = (wave % C::WP) * C::FP, fq = (wave / C::WP) * C::FQ;
     if (depth == 0)
         return;
-    typename C::P::S sp;
-    typename C::Q::S sq;
+    struct Set {
+        typename C::P::S p;
+        typename C::Q::S q;
+    } sets[C::kSets];
+    Set &even = sets[0], &odd = sets[C::kSets - 1];  // steps 0, 2, ... and 1, 3, ...
     u32x4 pa[C::FP], pb[C::FP], q[C::FQ];
-    auto load = [&](unsigned k) {
-        C::P::load(sp, ps, k);
-        C::Q::load(sq, qs, k);
+    auto load = [&](Set &s, unsigned k) {
+        if (k < depth) {
+            C::P::load(s.p, ps, k);
+            C::Q::load(s.q, qs, k);
+        }
     };
-    auto bring = [&](unsigned k, unsigned to) {
-        C::P::settle(sp, ps, k);
-        C::Q::settle(sq, qs, k);
+    auto bring = [&](Set &s, unsigned k, unsigned to) {
+        if (k >= depth)
+            return;
+        C::P::settle(s.p, ps, k);
+        C::Q::settle(s.q, qs, k);
         if constexpr (C::kEachQ)
-            each_q(sq);
-        C::P::store(sp, lds + to * C::kStage);
-        C::Q::store(sq, lds + to * C::kStage + C::P::kBytes);
+            each_q(s.q);
+        C::P::store(s.p, lds + to * C::kStage);
+        C::Q::store(s.q, lds + to * C::kStage + C::P::kBytes);
     };
-    load(0);
-    bring(0, 0);
-    arrived<0>();
+    // the step at k, whose successor is in `next`
+    auto step = [&](unsigned k, unsigned stage, Set &next) {
+        multiply_part<C, false>(pa, q, pb, true, lds + stage * C::kStage, fp, fq, 1, acc, [](int) {});
+        bring(next, k + C::kDepth, stage ^ 1);
+        load(next, k + (1 + C::kSets) * C::kDepth);
+        stored();
+        multiply_part<C, false>(pb, q, pa, k + C::kDepth < depth, lds + (stage ^ 1) * C::kStage, fp, fq, 0, acc, [](int) {});
+    };
+    load(even, 0);
+    if constexpr (C::kSets == 2)
+        load(odd, C::kDepth);
+    bring(even, 0, 0);
+    load(even, C::kSets * C::kDepth);
+    stored();
     read_first<C>(pa, q, lds, fp, fq);
-    unsigned stage = 0;
 #pragma unroll 1
-    for (unsigned k = 0; k < depth; k += C::kDepth) {
-        const char *from = lds + stage * C::kStage;
-        const bool more = k + C::kDepth < depth;
-        if (more)
-            load(k + C::kDepth);
-        multiply_part<C, false>(pa, q, pb, true, from, fp, fq, 1, acc, [](int) {});
-        stage ^= 1;
-        if (more)
-            bring(k + C::kDepth, stage);
-        arrived<0>();
-        multiply_part<C, false>(pb, q, pa, more, lds + stage * C::kStage, fp, fq, 0, acc, [](int) {});
+    for (unsigned k = 0; k < depth; k += 2 * C::kDepth) {
+        step(k, 0, odd);
+        if (k + C::kDepth < depth)
+            step(k + C::kDepth, 1, even);
     }
 }
 
@@ -1072,6 +1090,21 @@ __global__ __launch_bounds__(256) void sum_kernel(Problem p, unsigned stretch, c
     }
 }
 
+// ---- a masked copy -------------------------------------------------------------------
+
+// out[r][c] = x[r][c] where y[r][c] > 0, else zero; rows of `cols`, a multiple of 8.
+__global__ __launch_bounds__(256) void mask_kernel(const __bf16 *x, long long xs, const __bf16 *y, long long ys,
+                                                   unsigned rows, int cols, __bf16 *out)
+{
+    const unsigned vecs = cols / 8;
+    for (unsigned r = blockIdx.x; r < rows; r += gridDim.x)
+        for (unsigned c = threadIdx.x; c < vecs; c += 256) {
+            const u32x4 a = reinterpret_cast<const Bytes16 *>(x + r * xs + c * 8)->v;
+            const u32x4 b = reinterpret_cast<const Bytes16 *>(y + r * ys + c * 8)->v;
+            *reinterpret_cast<u32x4 *>(out + (size_t)r * cols + c * 8) = where_positive(a, b, __bf16{});
+        }
+}
+
 // ---- choice of a form ---------------------------------------------------------------
 
 unsigned tiles_of(long long n, int tile) { return (unsigned)((n + tile - 1) / tile); }
@@ -1124,21 +1157,30 @@ bool goes_alone(const Matrix<T> &m)
            m.cols % Type<T>::kVec == 0;
 }
 
+// 256 x 256 tiles, one workgroup a compute unit, or 128 x 128 ones, two: a large
+// one does the work of four in the time of 3.5, but the last round of tiles is a
+// larger part of the whole.  us with large and small tiles: 4,096 rows of 2,048 to
+// 4,096 100, 89; 32,768 of 1,024 to 1,024 92, 85; 65,536 of 1,024 to 1,024 179,
+// 207; 65,536 of 512 to 1,024 103, 107; and 262,144 of 256 to 256, where the depth
+// is too short to pay for a large tile's start, 84, 75.
+bool large_tiles(const Problem &p, int width)
+{
+    constexpr unsigned kCus = 256;
+    const unsigned long long large = (p.rows / 256ull + p.heads / 2) * tiles_of(width, 256);
+    const unsigned long long small = (p.rows / 128ull + p.heads / 2) * tiles_of(width, 128);
+    return 8 * ((large + kCus - 1) / kCus) <= 4.6 * ((small + 2 * kCus - 1) / (2 * kCus));
+}
+
 // The rows' product with tiles for its width.
 template <class T, bool DEEP_W, bool MASK>
 hipError_t rows_product(const Problem &p, const Matrix<T> &w, const Matrix<T> &x, const float *bias,
                         bool relu, Rows y, int width, int depth, hipStream_t s)
 {
     const bool alone = goes_alone(w) && goes_alone(x);
-    if constexpr (sizeof(T) == 2)
-        if (width > 128 && (unsigned long long)p.rows * tiles_of(width, 256) >= 256 * 128) {
-            if constexpr (!MASK)
-                if (alone)
-                    return launch_rows<Product<T, 256, 256, 4, 2, DEEP_W, true, false, true>>(
-                        p, w, x, bias, relu, y, width, depth, s);
-            return launch_rows<Product<T, 256, 256, 4, 2, DEEP_W, true, MASK>>(
-                p, w, x, bias, relu, y, width, depth, s);
-        }
+    if constexpr (sizeof(T) == 2 && !MASK)
+        if (alone && depth >= 512 && large_tiles(p, width))
+            return launch_rows<Product<T, 256, 256, 4, 2, DEEP_W, true, false, true>>(p, w, x, bias, relu, y, width,
+                                                                                    depth, s);
     if (width > 64) {
         if constexpr (!MASK)
             if (alone)
@@ -1202,15 +1244,11 @@ hipError_t weights_product(const Problem &p, const Matrix<T> &dz, const Matrix<T
 {
     const bool wide_o = p.fan_out > 64, wide_i = p.fan_in > 64;
     const bool alone = goes_alone(dz) && goes_alone(x);
-    if constexpr (sizeof(T) == 2)
-        if (p.fan_out > 128 && p.fan_in > 128 &&
-            (unsigned long long)tiles_of(p.fan_out, 256) * tiles_of(p.fan_in, 256) * p.heads >= 256) {
-            if constexpr (!MASK)
-                if (alone)
-                    return launch_weights<Product<T, 256, 256, 4, 2, false, false, false, true, true>>(
-                        p, dz, x, dw, db, workspace, s);
-            return launch_weights<Product<T, 256, 256, 4, 2, false, false, MASK, false, true>>(p, dz, x, dw, db, workspace, s);
-        }
+    if constexpr (sizeof(T) == 2 && !MASK)
+        if (alone && p.fan_out > 128 && p.fan_in > 128 &&
+            (unsigned long long)tiles_of(p.fan_out, 256) * tiles_of(p.fan_in, 256) * p.heads >= 256)
+            return launch_weights<Product<T, 256, 256, 4, 2, false, false, false, true, true>>(p, dz, x, dw, db,
+                                                                                             workspace, s);
     if constexpr (!MASK)
         if (wide_o && wide_i && alone)
             return launch_weights<Product<T, 128, 128, 2, 2, false, false, false, true, true>>(
@@ -1235,18 +1273,39 @@ hipError_t forward(const LinearShape &sh, Rows x, const void *w, const float *bi
     return rows_product<T, true, false>(problem(sh), mw, mx, bias, relu, y, sh.fan_out, sh.fan_in, s);
 }
 
+size_t masked_bytes(unsigned rows, int fan_out) { return ((size_t)rows * fan_out * 2 + 255) / 256 * 256; }
+
+// Whether a masked dz is laid out by a pass of its own, so that the products'
+// operands go to LDS by themselves: where both read it often.  us without and
+// with: 16,384 rows of 512 to 1,024 123, 103; 262,144 rows of 256 to 256 218, 234.
+bool mask_apart(int fan_in, int fan_out, bool bf16)
+{
+    return bf16 && fan_in >= 512 && fan_out >= 512 && fan_in % 8 == 0 && fan_out % 8 == 0;
+}
+
 template <class T>
 hipError_t backward(const LinearShape &sh, Rows dy, Rows x, const void *w, Rows y, Rows dx,
                     float *dw, float *db, char *workspace, hipStream_t s)
 {
     const Problem p = problem(sh);
-    const Matrix<T> mz = {static_cast<const T *>(dy.p), dy.stride, static_cast<const T *>(y.p), y.stride, sh.rows, sh.fan_out};
+    Matrix<T> mz = {static_cast<const T *>(dy.p), dy.stride, static_cast<const T *>(y.p), y.stride, sh.rows, sh.fan_out};
     const Matrix<T> mw = {static_cast<const T *>(w), sh.fan_in, nullptr, 0, (unsigned)sh.fan_out, sh.fan_in};
     Matrix<T> mx = {static_cast<const T *>(x.p), x.stride, nullptr, 0, sh.rows, sh.fan_in};
+    if constexpr (sizeof(T) == 2)
+        if (y.p && sh.rows > 0 && mask_apart(sh.fan_in, sh.fan_out, true)) {
+            __bf16 *dz = reinterpret_cast<__bf16 *>(workspace);
+            mask_kernel<<<sh.rows < (1u << 20) ? sh.rows : 1u << 20, 256, 0, s>>>(mz.p, mz.stride, mz.mask, mz.mask_stride,
+                                                                                 sh.rows, sh.fan_out, dz);
+            const hipError_t e = hipGetLastError();
+            if (e != hipSuccess)
+                return e;
+            workspace += masked_bytes(sh.rows, sh.fan_out);
+            mz = {dz, sh.fan_out, nullptr, 0, sh.rows, sh.fan_out};
+        }
     if (dx.p && sh.rows > 0) {
         const hipError_t e =
-            y.p ? rows_product<T, false, true>(p, mw, mz, nullptr, false, dx, sh.fan_in, sh.fan_out, s)
-                : rows_product<T, false, false>(p, mw, mz, nullptr, false, dx, sh.fan_in, sh.fan_out, s);
+            mz.mask ? rows_product<T, false, true>(p, mw, mz, nullptr, false, dx, sh.fan_in, sh.fan_out, s)
+                    : rows_product<T, false, false>(p, mw, mz, nullptr, false, dx, sh.fan_in, sh.fan_out, s);
         if (e != hipSuccess)
             return e;
     }
@@ -1256,8 +1315,8 @@ hipError_t backward(const LinearShape &sh, Rows dy, Rows x, const void *w, Rows 
         mx = mz;
         mx.mask = nullptr;
     }
-    return y.p ? weights_product<T, true>(p, mz, mx, dw, db, workspace, s)
-               : weights_product<T, false>(p, mz, mx, dw, db, workspace, s);
+    return mz.mask ? weights_product<T, true>(p, mz, mx, dw, db, workspace, s)
+                   : weights_product<T, false>(p, mz, mx, dw, db, workspace, s);
 }
 
 }  // namespace
@@ -1268,10 +1327,11 @@ hipError_t launch_heads_linear(const LinearShape &sh, Rows x, const void *w, con
     return bf16 ? forward<__bf16>(sh, x, w, bias, relu, y, s) : forward<float>(sh, x, w, bias, relu, y, s);
 }
 
-size_t heads_linear_workspace_bytes(unsigned rows, int heads, int fan_in, int fan_out, bool)
+size_t heads_linear_workspace_bytes(unsigned rows, int heads, int fan_in, int fan_out, bool relu, bool bf16)
 {
     const Split split = split_rows(rows, heads, fan_in, fan_out);
-    return split.stretch ? (size_t)split.places * fan_out * ((size_t)fan_in + 1) * sizeof(float) : 0;
+    return (relu && mask_apart(fan_in, fan_out, bf16) ? masked_bytes(rows, fan_out) : 0) +
+           (split.stretch ? (size_t)split.places * fan_out * ((size_t)fan_in + 1) * sizeof(float) : 0);
 }
 
 hipError_t launch_heads_linear_backward(const LinearShape &sh, Rows dy, Rows x, const void *w,

@@ -225,12 +225,12 @@ int derf_heads_linear(const void *x, long long x_stride, const void *w, const fl
 }
 
 long long derf_heads_linear_workspace(long long num_rows, int num_heads, int fan_in, int fan_out,
-                                      int precision)
+                                      int relu, int precision)
 {
     if (!linear_sizes_valid(num_rows, num_heads, fan_in, fan_out) || !is_precision(precision))
         return -1;
     return (long long)heads_linear_workspace_bytes((unsigned)num_rows, num_heads, fan_in, fan_out,
-                                                   precision == DERF_PREC_BF16);
+                                                   relu != 0, precision == DERF_PREC_BF16);
 }
 
 int derf_heads_linear_backward(const void *dy, long long dy_stride, const void *x,
@@ -259,7 +259,7 @@ int derf_heads_linear_backward(const void *dy, long long dy_stride, const void *
     TRY(check_array("offsets", offsets, 4));
     TRY(check_workspace(workspace, workspace_bytes,
                         derf_heads_linear_workspace(num_rows, num_heads, fan_in, fan_out,
-                                                    precision)));
+                                                    y != nullptr, precision)));
     const LinearShape sh = {offsets, (unsigned)num_rows, num_heads, fan_in, fan_out};
     return launched(launch_heads_linear_backward(sh, {dy, dy_stride}, {x, x_stride}, w,
                                                  {y, y_stride}, precision == DERF_PREC_BF16,

@@ -41,7 +41,7 @@ struct LinearShape {
 };
 hipError_t launch_heads_linear(const LinearShape &sh, Rows x, const void *w, const float *bias,
                                bool relu, bool bf16, Rows y, hipStream_t s);
-size_t heads_linear_workspace_bytes(unsigned rows, int heads, int fan_in, int fan_out, bool bf16);
+size_t heads_linear_workspace_bytes(unsigned rows, int heads, int fan_in, int fan_out, bool relu, bool bf16);
 // y.p: null without ReLU.  dx.p, dw, db may be null.
 hipError_t launch_heads_linear_backward(const LinearShape &sh, Rows dy, Rows x, const void *w,
                                         Rows y, bool bf16, Rows dx, float *dw, float *db,

@@ -144,7 +144,7 @@ def lib() -> ctypes.CDLL:
                 ("derf_combine", I, [P, N, P, P, N, I, I, I, P, N, P]),
                 ("derf_combine_backward", I, [P, N, P, N, P, P, N, I, I, I, P, N, P, P]),
                 ("derf_heads_linear", I, [P, N, P, P, P, N, I, I, I, I, I, P, N, P]),
-                ("derf_heads_linear_workspace", N, [N, I, I, I, I]),
+                ("derf_heads_linear_workspace", N, [N, I, I, I, I, I]),
                 ("derf_heads_linear_backward", I,
                  [P, N, P, N, P, P, N, P, N, I, I, I, I, P, N, P, P, P, N, P]),
                 ("derf_adamw_create", I, [ctypes.POINTER(P), P, I, I]),

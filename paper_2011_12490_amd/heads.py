@@ -264,7 +264,7 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor,
     out_weight = _out_array(out_weight, "out_weight", (K, O, I), dy.device)
     out_bias = _out_array(out_bias, "out_bias", (K, O), dy.device)
     prec = _PRECISION[dy.dtype]
-    need = _workspace_bytes("derf_heads_linear_workspace", R, K, I, O, prec)
+    need = _workspace_bytes("derf_heads_linear_workspace", R, K, I, O, int(y is not None), prec)
     if need < 0:
         raise ValueError("invalid sizes: %d rows, %d heads of %d to %d" % (R, K, I, O))
     ws = _workspace(need, dy.device)

@@ -69,7 +69,7 @@ def test_rows_arrays():
                                           (8, 4, 0, 8, 0), (8, 4, 8, 65537, 0), (8, 4, 8, 8, 3)])
 def test_linear_sizes(R, K, I, O, prec):
     L = lib()
-    assert L.derf_heads_linear_workspace(R, K, I, O, prec) == -1
+    assert L.derf_heads_linear_workspace(R, K, I, O, 1, prec) == -1
     assert L.derf_heads_linear(P, 1 << 17, P, P, P, R, K, I, O, 0, prec, P, 1 << 17, None) == INVALID
     assert L.derf_heads_linear_backward(P, 1 << 17, P, 1 << 17, P, None, 0, P, R, K, I, O, prec, P, 1 << 17, P, P,
                                         P, 1 << 40, None) == INVALID
@@ -100,7 +100,7 @@ def test_linear_arrays():
     refused(backward(dxs=15), b"stride")
     refused(backward(dw=P + 2), b"out_w is not aligned")
     refused(backward(db=P + 1), b"out_bias is not aligned")
-    if L.derf_heads_linear_workspace(8, 4, 16, 24, 1) > 0:
+    if L.derf_heads_linear_workspace(8, 4, 16, 24, 1, 1) > 0:
         refused(backward(n=0), b"workspace")
 
 
