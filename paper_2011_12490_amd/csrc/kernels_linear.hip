@@ -47,7 +47,8 @@ struct RowTile {
 };
 
 // before[h] (h <= heads): the tiles of `tile_rows` rows of the heads before h, in
-// LDS.  At least 256 threads, all call it.
+// LDS; never more than rows / tile_rows + heads in all, what grids and workspaces
+// are made for, whatever the offsets.  At least 256 threads, all call it.
 constexpr int kMaxHeads = 256;
 __device__ __forceinline__ void count_tiles(const Problem &p, unsigned tile_rows, unsigned *before)
 {
@@ -70,8 +71,9 @@ __device__ __forceinline__ void count_tiles(const Problem &p, unsigned tile_rows
     __syncthreads();
     for (int w = 0; w < wave && w < kMaxHeads / 64; ++w)
         incl += tmp[w];
+    const unsigned most = p.rows / tile_rows + p.heads;
     if (h < p.heads)
-        before[h + 1] = incl;
+        before[h + 1] = incl < most ? incl : most;
     if (h == 0)
         before[0] = 0;
     __syncthreads();
@@ -284,7 +286,7 @@ struct Tile {
             return r >> 1 & 7;
         if (sizeof(T) == 2)  // in pairs of chunks: rows 0-3 and 8-11 are read at once
             return (TILE == 64 ? (r >> 1 & 1) | (r >> 2 & 2) : (r & 3) | (r >> 1 & 4)) << 1;
-        return 0;
+        return kRowStep % 16 == 0 ? ((r & 3) | (r >> 1 & 4)) << 1 : 0;
     }
     static __device__ __forceinline__ unsigned my_row() { return threadIdx.x / kPerRow; }
     static __device__ __forceinline__ int my_col()
@@ -454,6 +456,15 @@ struct Tile {
     static __device__ __forceinline__ unsigned at(unsigned r, unsigned c)
     {
         return (r * kPerRow + (c ^ turn(r))) * 16;
+    }
+
+    // Of an operand whose tile's rows lie side by side, read as a deep one: rows
+    // [16 f, 16 f + 16), 64 bytes from byte 64 part on.
+    static __device__ __forceinline__ u32x4 row_fragment(const char *lds, int f, int part)
+    {
+        static_assert(!DEEP, "the other kind");
+        const int quarter = (threadIdx.x & 63) >> 4, l = threadIdx.x & 15;
+        return *reinterpret_cast<const u32x4 *>(lds + at(f * 16 + l, part * 4 + quarter));
     }
 
     // The matrix unit's operand: tile rows [16 f, 16 f + 16), half `part` of the
@@ -739,6 +750,25 @@ __device__ __forceinline__ void store_values(char *to, f32x4 v, __bf16)
 }
 __device__ __forceinline__ void store_values(char *to, f32x4 v, float) { *reinterpret_cast<f32x4 *>(to) = v; }
 
+// The first `left` (at most 16 bytes' worth) elements of v.
+template <class T>
+__device__ __forceinline__ void write_piece(T *to, u32x4 v, int left, T)
+{
+    constexpr int V = Type<T>::kVec;
+    if (left >= V) {
+        reinterpret_cast<Bytes16 *>(to)->v = v;
+        return;
+    }
+    union {
+        u32x4 v;
+        T e[V];
+    } piece = {v};
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+        if (k < left)
+            to[k] = piece.e[k];
+}
+
 // A tile of the result: rows [t.first, t.last), columns from n0 on.
 template <class C>
 __device__ __forceinline__ void write_rows(const RowTile &t, int n0, int width, const f32x4 (&acc)[C::FP][C::FQ],
@@ -776,19 +806,7 @@ __device__ __forceinline__ void write_rows(const RowTile &t, int n0, int width, 
             const int n = n0 + wp + c;
             if (row >= t.last || n >= width)
                 continue;
-            T *to = y + (row * ys + n);
-            if (n + V <= width) {
-                reinterpret_cast<Bytes16 *>(to)->v = v;
-            } else {
-                union {
-                    u32x4 v;
-                    T e[V];
-                } piece = {v};
-#pragma unroll
-                for (int k = 0; k < V; ++k)
-                    if (n + k < width)
-                        to[k] = piece.e[k];
-            }
+            write_piece(y + (row * ys + n), v, width - n, T{});
         }
         __builtin_amdgcn_wave_barrier();
     }
@@ -964,15 +982,7 @@ __device__ __forceinline__ void write_weights(float *to, int m0, int n0, int O, 
             const int n = n0 + wp + i * 16 + (lane >> 4) * 4;
             if (m >= O || n >= I)
                 continue;
-            float *at = to + ((size_t)m * I + n);
-            if (n + 4 <= I) {
-                reinterpret_cast<Bytes16 *>(at)->v = __builtin_bit_cast(u32x4, acc[i][j]);
-            } else {
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    if (n + k < I)
-                        at[k] = acc[i][j][k];
-            }
+            write_piece(to + ((size_t)m * I + n), __builtin_bit_cast(u32x4, acc[i][j]), I - n, 0.0f);
         }
     }
 }
@@ -1205,6 +1215,194 @@ __global__ __launch_bounds__(CR::kThreads, 2) void gradients_kernel(Problem p, M
     arrived<0>();
 }
 
+// ---- both gradients of narrow layers, in one pass over the rows --------------------------
+
+// Layers of at most 128 to 128 move more than they compute: here every row is
+// read once for both gradients.  A workgroup (one a compute unit) keeps its
+// head's weights in LDS and its part of dW in registers and goes through a
+// stretch of the head's rows, RT at a time, the next ones' loads under way.  dz
+// lies in LDS once: dx reads it by rows, dW by columns.  128 to 128 with ReLU on
+// 131,072 rows of bf16: 45 us, 66 with a pass for each gradient.
+template <class T_, int TI_, int TO_, bool MASK>
+struct Narrow {
+    using T = T_;
+    static constexpr int TI = TI_, TO = TO_, kThreads = 512, RT = sizeof(T) == 2 ? 128 : 64;
+    using X = Tile<T, TI, false, kThreads, false>;   // x
+    using Z = Tile<T, TO, false, kThreads, MASK>;    // dz
+    static constexpr int kSteps = RT / X::D;         // tiles of D rows
+    static constexpr int kSpan = X::D / 2;           // depth of a fragment
+    // dW: 4 waves over fan_in, 2 over fan_out
+    static constexpr int FP = TI / 64, FQ = TO / 32;
+    // dx: a wave takes 16 rows; where there are fewer of them than waves, half the columns
+    static constexpr int kColGroups = 8 / (RT / 16), FX = TI / 16 / kColGroups;
+    static constexpr int kRowBytes = FX * 16 * (int)sizeof(T) + 16;
+    static constexpr int kResults = sizeof(T) == 2 ? 8 * 16 * kRowBytes : 0;
+    static constexpr int kZ = 0, kX = kZ + RT * TO * (int)sizeof(T), kW = kX + RT * TI * (int)sizeof(T);
+    static constexpr int kOut = kW + TO * TI * (int)sizeof(T), kLds = kOut + kResults;
+    static constexpr int kRowsOfThreads = kThreads / Z::kPerRow;
+    static_assert(kRowsOfThreads * (TO + 1) * 4 <= kW, "sums take the rows' place");
+};
+
+template <class C>
+__global__ __launch_bounds__(C::kThreads, 2) void narrow_kernel(Problem p, Matrix<typename C::T> w, Matrix<typename C::T> dz,
+                                                                Matrix<typename C::T> x, typename C::T *dx, long long dxs,
+                                                                float *dw, float *db, unsigned stretch)
+{
+    using T = typename C::T;
+    constexpr int V = Type<T>::kVec;
+    __shared__ __attribute__((aligned(16))) char lds[C::kLds];
+    __shared__ unsigned before[kMaxHeads + 1];
+    const int I = p.fan_in, O = p.fan_out, lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    count_tiles(p, stretch, before);
+    const unsigned places = uniform(before[p.heads]), place = blockIdx.x;
+    if (place >= places) {  // rows without a head: zeros
+        const unsigned headless = bound(p, p.heads);
+        const unsigned long long from = headless + (unsigned long long)(place - places) * stretch;
+        if (dx)
+            for (unsigned long long r = from + wave; r < from + stretch && r < p.rows; r += C::kThreads / 64)
+                for (int c = lane; c < I; c += 64)
+                    dx[r * dxs + c] = (T)0.0f;
+        return;
+    }
+    const RowTile t = head_tile(p, before, place, stretch);
+    typename C::X::Source xs = {x, 0}, ws = {w, 0};
+    typename C::Z::Source zs = {dz, 0};
+    xs.m.p += t.first * x.stride;
+    zs.m.p += t.first * dz.stride;
+    zs.m.mask += t.first * dz.mask_stride;
+    xs.m.rows = zs.m.rows = t.last - t.first;
+    ws.m.p += t.head * ((size_t)I * O);
+    typename C::X::S sx[C::kSteps];
+    typename C::Z::S sz[C::kSteps];
+    auto load = [&](unsigned k) {
+#pragma unroll
+        for (int i = 0; i < C::kSteps; ++i) {
+            C::Z::load(sz[i], zs, k + i * C::Z::D);
+            C::X::load(sx[i], xs, k + i * C::X::D);
+        }
+    };
+    typename C::X::S sw[C::TO / C::X::D];
+    if (dx)
+#pragma unroll
+        for (int i = 0; i < C::TO / C::X::D; ++i)
+            C::X::load(sw[i], ws, i * C::X::D);
+    load(0);
+    if (dx)
+#pragma unroll
+        for (int i = 0; i < C::TO / C::X::D; ++i) {
+            C::X::settle(sw[i], ws, i * C::X::D);
+            C::X::store(sw[i], lds + C::kW + i * C::X::kBytes);
+        }
+    float sums[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+        sums[k] = 0.0f;
+    f32x4 acc[C::FP][C::FQ] = {};
+    const int fp = (wave % 4) * C::FP, fq = (wave / 4) * C::FQ;
+    const int fr = wave / C::kColGroups, fc = (wave % C::kColGroups) * C::FX;  // of dx
+#pragma unroll 1
+    for (unsigned k = 0; k < t.last - t.first; k += C::RT) {
+        stored();
+#pragma unroll
+        for (int i = 0; i < C::kSteps; ++i) {
+            C::Z::settle(sz[i], zs, k + i * C::Z::D);
+            C::X::settle(sx[i], xs, k + i * C::X::D);
+            C::Z::store(sz[i], lds + C::kZ + i * C::Z::kBytes);
+            C::X::store(sx[i], lds + C::kX + i * C::X::kBytes);
+#pragma unroll
+            for (int j = 0; j < C::Z::kShare; ++j) {
+                union {
+                    u32x4 v;
+                    T e[V];
+                } piece = {sz[i].x[j]};
+#pragma unroll
+                for (int e = 0; e < V; ++e)
+                    sums[e] += (float)piece.e[e];
+            }
+        }
+        stored();
+        if (k + C::RT < t.last - t.first)
+            load(k + C::RT);
+        if (dx) {
+            f32x4 rows[C::FX] = {};
+#pragma unroll
+            for (int part = 0; part < C::TO / C::kSpan; ++part) {
+                const u32x4 q = C::Z::row_fragment(lds + C::kZ, fr, part);
+#pragma unroll
+                for (int i = 0; i < C::FX; ++i)
+                    rows[i] = multiply(C::X::fragment(lds + C::kW, fc + i, part), q, rows[i], T{});
+            }
+            const unsigned first = t.first + k + fr * 16;
+            if constexpr (C::kResults > 0) {
+                char *mine = lds + C::kOut + wave * 16 * C::kRowBytes;
+#pragma unroll
+                for (int i = 0; i < C::FX; ++i)
+                    store_values(mine + (lane & 15) * C::kRowBytes + (i * 16 + (lane >> 4) * 4) * (int)sizeof(T), rows[i], T{});
+                __builtin_amdgcn_wave_barrier();
+                constexpr int kPieces = C::FX * 16 / V;  // of a row
+#pragma unroll
+                for (int i = 0; i < 16 * kPieces / 64; ++i) {
+                    const int r = (i * 64 + lane) / kPieces, c = (i * 64 + lane) % kPieces * V;
+                    const u32x4 v = *reinterpret_cast<const u32x4 *>(mine + r * C::kRowBytes + c * (int)sizeof(T));
+                    const int n = fc * 16 + c;
+                    if (first + r < t.last && n < I)
+                        write_piece(dx + ((first + r) * dxs + n), v, I - n, T{});
+                }
+                __builtin_amdgcn_wave_barrier();
+            } else {
+#pragma unroll
+                for (int i = 0; i < C::FX; ++i) {
+                    const int n = (fc + i) * 16 + (lane >> 4) * 4;
+                    if (first + (lane & 15) < t.last && n < I)
+                        write_piece(dx + ((first + (lane & 15)) * dxs + n), __builtin_bit_cast(u32x4, rows[i]), I - n, T{});
+                }
+            }
+        }
+        if (dw)
+#pragma unroll
+            for (int part = 0; part < C::RT / C::kSpan; ++part) {
+                u32x4 q[C::FQ];
+#pragma unroll
+                for (int j = 0; j < C::FQ; ++j)
+                    q[j] = C::Z::fragment(lds + C::kZ, fq + j, part);
+#pragma unroll
+                for (int i = 0; i < C::FP; ++i) {
+                    const u32x4 f = C::X::fragment(lds + C::kX, fp + i, part);
+#pragma unroll
+                    for (int j = 0; j < C::FQ; ++j)
+                        acc[i][j] = multiply(f, q[j], acc[i][j], T{});
+                }
+            }
+    }
+    if (dw) {
+        float *to = dw + (size_t)place * O * I;
+#pragma unroll
+        for (int j = 0; j < C::FQ; ++j) {
+            const int m = (fq + j) * 16 + (lane & 15);
+#pragma unroll
+            for (int i = 0; i < C::FP; ++i) {
+                const int n = (fp + i) * 16 + (lane >> 4) * 4;
+                if (m < O && n < I)
+                    write_piece(to + ((size_t)m * I + n), __builtin_bit_cast(u32x4, acc[i][j]), I - n, 0.0f);
+            }
+        }
+    }
+    if (db) {
+        float(*part)[C::TO + 1] = reinterpret_cast<float(*)[C::TO + 1]>(lds);
+        __syncthreads();
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            part[C::Z::my_row()][C::Z::my_col() + k] = sums[k];
+        __syncthreads();
+        if ((int)threadIdx.x < O) {
+            float v = 0.0f;
+            for (int r = 0; r < C::kRowsOfThreads; ++r)
+                v += part[r][threadIdx.x];
+            db[(size_t)place * O + threadIdx.x] = v;
+        }
+    }
+}
+
 // out[h][e] = the sum of head h's stretches' parts, in order: the weights' in the
 // first blocks of a head, the biases' in its last.
 __global__ __launch_bounds__(256) void sum_kernel(Problem p, unsigned stretch, const float *wparts, size_t wsize, float *dw,
@@ -1358,6 +1556,17 @@ Split split_rows(unsigned rows, int heads, int fan_in, int fan_out)
     return {stretch, rows / stretch + heads};
 }
 
+// The stretches' parts added up.
+hipError_t launch_sums(const Problem &p, const Split &split, const float *wparts, float *dw, const float *bparts, float *db,
+                       hipStream_t s)
+{
+    const size_t size = (size_t)p.fan_in * p.fan_out;
+    const unsigned blocks = dw ? tiles_of(size, 256) : 0, wblocks = blocks < 1024 ? blocks : 1024;
+    const unsigned bblocks = db ? tiles_of(p.fan_out, 256) : 0;
+    sum_kernel<<<dim3(wblocks + bblocks, p.heads), 256, 0, s>>>(p, split.stretch, wparts, size, dw, bparts, db, wblocks);
+    return hipGetLastError();
+}
+
 template <class C>
 hipError_t launch_weights(const Problem &p, const Matrix<typename C::T> &dz,
                           const Matrix<typename C::T> &x, float *dw, float *db, char *workspace,
@@ -1376,12 +1585,7 @@ hipError_t launch_weights(const Problem &p, const Matrix<typename C::T> &dz,
         });
     if (e != hipSuccess)
         return e;
-    if (partial) {
-        const unsigned blocks = dw ? tiles_of(size, 256) : 0, wblocks = blocks < 1024 ? blocks : 1024;
-        const unsigned bblocks = db ? tiles_of(p.fan_out, 256) : 0;
-        sum_kernel<<<dim3(wblocks + bblocks, p.heads), 256, 0, s>>>(p, split.stretch, wparts, size, dw, bparts, db, wblocks);
-    }
-    return hipGetLastError();
+    return partial ? launch_sums(p, split, wparts, dw, bparts, db, s) : hipSuccess;
 }
 
 template <class T, bool MASK>
@@ -1427,6 +1631,44 @@ size_t masked_bytes(unsigned rows, int fan_out) { return ((size_t)rows * fan_out
 bool mask_apart(int fan_in, int fan_out, bool bf16)
 {
     return bf16 && fan_in >= 512 && fan_out >= 512 && fan_in % 8 == 0 && fan_out % 8 == 0;
+}
+
+// Layers that narrow_kernel takes, and its stretches: a workgroup for each, one
+// a compute unit.
+bool is_narrow(int fan_in, int fan_out) { return fan_in <= 128 && fan_out <= 128; }
+Split narrow_split(unsigned rows, int heads)
+{
+    constexpr unsigned kPlaces = 256;
+    const unsigned most = (unsigned)heads < kPlaces / 2 ? kPlaces - heads : kPlaces / 2;
+    unsigned stretch = (rows / most + 32) / 32 * 32;
+    if (stretch < 128)
+        stretch = 128;
+    return {stretch, rows / stretch + heads};
+}
+
+template <class C>
+hipError_t launch_narrow(const Problem &p, const Matrix<typename C::T> &w, const Matrix<typename C::T> &dz,
+                         const Matrix<typename C::T> &x, Rows dx, float *dw, float *db, char *workspace, hipStream_t s)
+{
+    using T = typename C::T;
+    const Split split = narrow_split(p.rows, p.heads);
+    float *wparts = reinterpret_cast<float *>(workspace);
+    float *bparts = wparts + (size_t)split.places * p.fan_in * p.fan_out;
+    narrow_kernel<C><<<split.places + 1, C::kThreads, 0, s>>>(p, w, dz, x, static_cast<T *>(const_cast<void *>(dx.p)), dx.stride,
+                                                              dw ? wparts : nullptr, db ? bparts : nullptr, split.stretch);
+    const hipError_t e = hipGetLastError();
+    return e != hipSuccess || (!dw && !db) ? e : launch_sums(p, split, wparts, dw, bparts, db, s);
+}
+
+template <class T, bool MASK>
+hipError_t narrow(const Problem &p, const Matrix<T> &w, const Matrix<T> &dz, const Matrix<T> &x, Rows dx, float *dw,
+                  float *db, char *workspace, hipStream_t s)
+{
+    if (p.fan_in <= 64)
+        return p.fan_out <= 64 ? launch_narrow<Narrow<T, 64, 64, MASK>>(p, w, dz, x, dx, dw, db, workspace, s)
+                               : launch_narrow<Narrow<T, 64, 128, MASK>>(p, w, dz, x, dx, dw, db, workspace, s);
+    return p.fan_out <= 64 ? launch_narrow<Narrow<T, 128, 64, MASK>>(p, w, dz, x, dx, dw, db, workspace, s)
+                           : launch_narrow<Narrow<T, 128, 128, MASK>>(p, w, dz, x, dx, dw, db, workspace, s);
 }
 
 template <class CR, class CW>
@@ -1477,6 +1719,12 @@ hipError_t backward(const LinearShape &sh, Rows dy, Rows x, const void *w, Rows 
         if (dx.p && dw && sh.rows > 0 && goes_alone(mz) && goes_alone(mw) && goes_alone(mx) && gradients_together(p))
             return launch_gradients<Product<T, 256, 256, 4, 2, false, true, false, true>,
                                     Product<T, 256, 256, 4, 2, false, false, false, true, true>>(p, mw, mz, mx, dx, dw, db, s);
+    if (is_narrow(sh.fan_in, sh.fan_out) && sh.rows > 0 && (dx.p ? dw || db : dw != nullptr)) {
+        if (!dw)  // nothing needs x
+            mx = {mz.p, mz.stride, nullptr, 0, mz.rows, mz.cols};
+        return mz.mask ? narrow<T, true>(p, mw, mz, mx, dx, dw, db, workspace, s)
+                       : narrow<T, false>(p, mw, mz, mx, dx, dw, db, workspace, s);
+    }
     if (dx.p && sh.rows > 0) {
         const hipError_t e =
             mz.mask ? rows_product<T, false, true>(p, mw, mz, nullptr, false, dx, sh.fan_in, sh.fan_out, s)
@@ -1504,9 +1752,12 @@ hipError_t launch_heads_linear(const LinearShape &sh, Rows x, const void *w, con
 
 size_t heads_linear_workspace_bytes(unsigned rows, int heads, int fan_in, int fan_out, bool relu, bool bf16)
 {
-    const Split split = split_rows(rows, heads, fan_in, fan_out);
+    const Split split = split_rows(rows, heads, fan_in, fan_out), narrow = narrow_split(rows, heads);
+    size_t places = split.stretch ? split.places : 0;
+    if (is_narrow(fan_in, fan_out) && narrow.places > places)
+        places = narrow.places;
     return (relu && mask_apart(fan_in, fan_out, bf16) ? masked_bytes(rows, fan_out) : 0) +
-           (split.stretch ? (size_t)split.places * fan_out * ((size_t)fan_in + 1) * sizeof(float) : 0);
+           places * fan_out * ((size_t)fan_in + 1) * sizeof(float);
 }
 
 hipError_t launch_heads_linear_backward(const LinearShape &sh, Rows dy, Rows x, const void *w,
