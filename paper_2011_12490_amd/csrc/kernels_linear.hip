@@ -1223,20 +1223,24 @@ __global__ __launch_bounds__(CR::kThreads, 2) void gradients_kernel(Problem p, M
 // stretch of the head's rows, RT at a time, the next ones' loads under way.  dz
 // lies in LDS once: dx reads it by rows, dW by columns.  128 to 128 with ReLU on
 // 131,072 rows of bf16: 45 us, 66 with a pass for each gradient.
+// float's products take about as long as its rows: two workgroups of half the
+// waves and rows a compute unit, where their weights fit, compute in turns.
 template <class T_, int TI_, int TO_, bool MASK>
 struct Narrow {
     using T = T_;
-    static constexpr int TI = TI_, TO = TO_, kThreads = 512, RT = sizeof(T) == 2 ? 128 : 64;
+    static constexpr bool kTwo = sizeof(T) == 4 && TI_ + TO_ < 256;  // workgroups a compute unit
+    static constexpr int TI = TI_, TO = TO_, kThreads = kTwo ? 256 : 512, kWaves = kThreads / 64;
+    static constexpr int RT = sizeof(T) == 2 ? 128 : kTwo ? 32 : 64;
     using X = Tile<T, TI, false, kThreads, false>;   // x
     using Z = Tile<T, TO, false, kThreads, MASK>;    // dz
     static constexpr int kSteps = RT / X::D;         // tiles of D rows
     static constexpr int kSpan = X::D / 2;           // depth of a fragment
-    // dW: 4 waves over fan_in, 2 over fan_out
-    static constexpr int FP = TI / 64, FQ = TO / 32;
-    // dx: a wave takes 16 rows; where there are fewer of them than waves, half the columns
-    static constexpr int kColGroups = 8 / (RT / 16), FX = TI / 16 / kColGroups;
+    // dW: 4 waves over fan_in, the rest over fan_out
+    static constexpr int FP = TI / 64, FQ = TO / (kWaves / 4) / 16;
+    // dx: a wave takes 16 rows; where there are fewer of them than waves, part of the columns
+    static constexpr int kColGroups = kWaves / (RT / 16), FX = TI / 16 / kColGroups;
     static constexpr int kRowBytes = FX * 16 * (int)sizeof(T) + 16;
-    static constexpr int kResults = sizeof(T) == 2 ? 8 * 16 * kRowBytes : 0;
+    static constexpr int kResults = sizeof(T) == 2 ? kWaves * 16 * kRowBytes : 0;
     static constexpr int kZ = 0, kX = kZ + RT * TO * (int)sizeof(T), kW = kX + RT * TI * (int)sizeof(T);
     static constexpr int kOut = kW + TO * TI * (int)sizeof(T), kLds = kOut + kResults;
     static constexpr int kRowsOfThreads = kThreads / Z::kPerRow;
@@ -1633,12 +1637,12 @@ bool mask_apart(int fan_in, int fan_out, bool bf16)
     return bf16 && fan_in >= 512 && fan_out >= 512 && fan_in % 8 == 0 && fan_out % 8 == 0;
 }
 
-// Layers that narrow_kernel takes, and its stretches: a workgroup for each, one
-// a compute unit.
+// Layers that narrow_kernel takes, and its stretches: a workgroup for each, as
+// many as run at once.
 bool is_narrow(int fan_in, int fan_out) { return fan_in <= 128 && fan_out <= 128; }
-Split narrow_split(unsigned rows, int heads)
+Split narrow_split(unsigned rows, int heads, int fan_in, int fan_out, bool bf16)
 {
-    constexpr unsigned kPlaces = 256;
+    const unsigned kPlaces = !bf16 && (fan_in <= 64 || fan_out <= 64) ? 512 : 256;
     const unsigned most = (unsigned)heads < kPlaces / 2 ? kPlaces - heads : kPlaces / 2;
     unsigned stretch = (rows / most + 32) / 32 * 32;
     if (stretch < 128)
@@ -1651,7 +1655,7 @@ hipError_t launch_narrow(const Problem &p, const Matrix<typename C::T> &w, const
                          const Matrix<typename C::T> &x, Rows dx, float *dw, float *db, char *workspace, hipStream_t s)
 {
     using T = typename C::T;
-    const Split split = narrow_split(p.rows, p.heads);
+    const Split split = narrow_split(p.rows, p.heads, p.fan_in, p.fan_out, sizeof(T) == 2);
     float *wparts = reinterpret_cast<float *>(workspace);
     float *bparts = wparts + (size_t)split.places * p.fan_in * p.fan_out;
     narrow_kernel<C><<<split.places + 1, C::kThreads, 0, s>>>(p, w, dz, x, static_cast<T *>(const_cast<void *>(dx.p)), dx.stride,
@@ -1752,7 +1756,7 @@ hipError_t launch_heads_linear(const LinearShape &sh, Rows x, const void *w, con
 
 size_t heads_linear_workspace_bytes(unsigned rows, int heads, int fan_in, int fan_out, bool relu, bool bf16)
 {
-    const Split split = split_rows(rows, heads, fan_in, fan_out), narrow = narrow_split(rows, heads);
+    const Split split = split_rows(rows, heads, fan_in, fan_out), narrow = narrow_split(rows, heads, fan_in, fan_out, bf16);
     size_t places = split.stretch ? split.places : 0;
     if (is_narrow(fan_in, fan_out) && narrow.places > places)
         places = narrow.places;
