@@ -514,3 +514,62 @@ def test_python_refusals():
         with pytest.raises(ValueError):
             call()
             print("case", i)
+
+
+# ---- beyond 32 bits ------------------------------------------------------------------
+
+def far_rows(rows, dim, stride, dtype):
+    """Rows so far apart that the last ones start behind 2^32 bytes."""
+    buf = torch.empty((rows * stride,), dtype=dtype, device="cuda")
+    view = buf.view(rows, stride)[:, :dim]
+    assert (rows - 1) * stride * dtype.itemsize > 1 << 32
+    return view
+
+
+@pytest.mark.parametrize("dtype,stride", [(BF16, 1 << 20), (FP32, (1 << 19) + 1)])
+def test_rows_beyond_32_bits(dtype, stride):
+    """Dispatch, combine and a layer with its gradients on rows behind 2^32 bytes give
+    what they give on rows side by side."""
+    R, I, O = 2304, 40, 72
+    g = gen(40)
+    x = far_rows(R, I, stride, dtype)
+    x.copy_(rand(g, R, I).to(dtype))
+    near = x.contiguous()
+    w, b = (rand(g, 2, O, I) / 6).to(dtype), rand(g, 2, O)
+    offsets = torch.tensor([0, 1000, R], dtype=torch.int32, device="cuda")
+    y = heads.linear(near, w, b, offsets, True)
+    far_y = heads.linear(x, w, b, offsets, True, far_rows(R, O, stride, dtype))
+    dy = rand(g, R, O).to(dtype)
+    want = heads.linear_backward(dy, near, w, offsets, y)
+    got = heads.linear_backward(dy, x, w, offsets, far_y, out_x=far_rows(R, I, stride, dtype))
+    # the order of sums goes by the form that a stride's alignment allows
+    assert_near(far_y, y.double(), y.double().abs() + 10, I)
+    assert_near(got[0], want[0].double(), want[0].double().abs() + 10, O)
+    for a, c in zip(got[1:], want[1:]):
+        assert_near(a, c.double(), c.double().abs() + 100, R)
+    ids = torch.from_numpy(some_ids(1, R // 2, 2, 3, "some")).cuda()
+    r = heads.route(ids, 3)
+    half = x[:R // 2]
+    assert torch.equal(heads.dispatch(half, r, far_rows(R, I, stride, dtype)), heads.dispatch(near[:R // 2], r))
+    weights = torch.rand(R // 2, 2, generator=g, device="cuda")
+    assert torch.equal(heads.combine(x, r, weights), heads.combine(near, r, weights))
+    for a, c in zip(heads.combine_backward(half, x, r, weights), heads.combine_backward(near[:R // 2], near, r, weights)):
+        assert torch.equal(a, c)
+
+
+def test_adamw_of_more_than_2_31_values():
+    """The last values of a tensor of 2^31 + 1000 in 8 bits are updated as a tensor of
+    their own is."""
+    n, tail = (1 << 31) + 1000, (1 << 31) - 512
+    p, grad = torch.zeros(n, dtype=BF16, device="cuda"), torch.zeros(n, dtype=BF16, device="cuda")
+    g = gen(41)
+    p[tail:] = (rand(g, n - tail) * 0.1).to(BF16)
+    grad[tail:] = (rand(g, n - tail) * 0.1).to(BF16)
+    q = p[tail:].clone()
+    opt, ref = heads.AdamW([p], [grad], state_bits=8), heads.AdamW([q], [grad[tail:].clone()], state_bits=8)
+    for _ in range(2):
+        opt.step()
+        ref.step()
+    assert torch.equal(p[tail:], q) and not bool(p[:256].any()) and not bool(p[tail - 512:tail].any())
+    assert torch.equal(opt.m[0][tail:].view(torch.uint8), ref.m[0].view(torch.uint8))
+    assert torch.equal(opt.v_scale[0][tail // 256:], ref.v_scale[0])
