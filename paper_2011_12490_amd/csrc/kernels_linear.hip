@@ -1087,6 +1087,129 @@ __global__ __launch_bounds__(C::kThreads, 2) void weights_kernel(Problem p, Matr
     }
 }
 
+// ---- shallow products, their weights in LDS ---------------------------------------------
+
+// Layers of at most STEPS x 128 bytes of depth on many rows, or their rows'
+// gradient (DEEP_W false: the weights' columns are its outputs): a workgroup
+// keeps TO of its head's outputs' weights in LDS and goes through a stretch of
+// the head's rows, RT at a time, the next ones' loads under way: the rows stream,
+// whatever their alignment, and nothing is read again but by the other columns'
+// workgroups beside it.  Rows of bf16, us here and tile by tile: 319 to 256 on
+// 262,139 113, 132; 128 to 128 on 262,144 25 (5.3 TB/s), 31; 63 to 64 15, 20.
+template <class T_, int TO_, int STEPS, bool DEEP_W, bool MASK>
+struct Shallow {
+    using T = T_;
+    static constexpr int TO = TO_, kSteps = STEPS, kThreads = 512, kColGroups = TO / 64, RT = 16 * 8 / kColGroups;
+    using W = Tile<T, TO, DEEP_W, kThreads, false>;
+    using X = Tile<T, RT, true, kThreads, MASK>;
+    static constexpr int FP = 4;  // a wave's: 64 outputs of 16 rows
+    static constexpr int kRowBytes = 64 * (int)sizeof(T) + 16;
+    static constexpr int kX = STEPS * W::kBytes, kOut = kX + STEPS * X::kBytes, kLds = kOut + 8 * 16 * kRowBytes;
+    // workgroups a compute unit: by LDS, and 4 waves a SIMD
+    static constexpr int kAtOnce = 2 * (kLds + 4096) <= 160 * 1024 ? 2 : 1;
+};
+
+template <class C>
+__global__ __launch_bounds__(C::kThreads, 2 * C::kAtOnce) void shallow_kernel(Problem p, Matrix<typename C::T> w,
+                                                                              Matrix<typename C::T> x, const float *bias,
+                                                                              int relu, typename C::T *y, long long ys, int width,
+                                                                              unsigned stretch)
+{
+    using T = typename C::T;
+    constexpr int V = Type<T>::kVec;
+    __shared__ __attribute__((aligned(16))) char lds[C::kLds];
+    __shared__ __attribute__((aligned(16))) float biases[C::TO];
+    __shared__ unsigned before[kMaxHeads + 1];
+    const int O = width, lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    count_tiles(p, stretch, before);
+    // the columns of a stretch on one XCD, at about the same time
+    const unsigned cols = (O + C::TO - 1) / C::TO, j = blockIdx.x / kXcds;
+    const unsigned places = uniform(before[p.heads]), place = j / cols * kXcds + blockIdx.x % kXcds;
+    const int n0 = (int)(j % cols) * C::TO;
+    if (place >= places) {  // rows without a head: zeros
+        const unsigned headless = bound(p, p.heads);
+        const unsigned long long from = headless + (unsigned long long)(place - places) * stretch;
+        for (unsigned long long r = from + wave; r < from + stretch && r < p.rows; r += C::kThreads / 64)
+            for (int c = n0 + lane; c < n0 + C::TO && c < O; c += 64)
+                y[r * ys + c] = (T)0.0f;
+        return;
+    }
+    const RowTile t = head_tile(p, before, place, stretch);
+    typename C::W::Source ws = {w, (unsigned)n0};
+    ws.m.p += t.head * ((size_t)p.fan_in * p.fan_out);
+    typename C::X::Source xs = {x, 0};
+    xs.m.p += t.first * x.stride;
+    xs.m.mask += t.first * x.mask_stride;
+    xs.m.rows = t.last - t.first;
+    typename C::W::S sw[C::kSteps];
+    typename C::X::S sx[C::kSteps];
+    auto load = [&](unsigned r) {
+        xs.t0 = r;
+#pragma unroll
+        for (int i = 0; i < C::kSteps; ++i)
+            C::X::load(sx[i], xs, i * C::X::D);
+    };
+#pragma unroll
+    for (int i = 0; i < C::kSteps; ++i)
+        C::W::load(sw[i], ws, i * C::W::D);
+    load(0);
+    if (threadIdx.x < C::TO)
+        biases[threadIdx.x] =
+            bias && n0 + (int)threadIdx.x < O ? bias[(size_t)t.head * O + n0 + threadIdx.x] : 0.0f;
+#pragma unroll
+    for (int i = 0; i < C::kSteps; ++i) {
+        C::W::settle(sw[i], ws, i * C::W::D);
+        C::W::store(sw[i], lds + i * C::W::kBytes);
+    }
+    const int fp = (wave % C::kColGroups) * C::FP, fq = wave / C::kColGroups;
+    char *mine = lds + C::kOut + wave * 16 * C::kRowBytes;
+#pragma unroll 1
+    for (unsigned r0 = 0; r0 < t.last - t.first; r0 += C::RT) {
+        stored();
+        xs.t0 = r0;
+#pragma unroll
+        for (int i = 0; i < C::kSteps; ++i) {
+            C::X::settle(sx[i], xs, i * C::X::D);
+            C::X::store(sx[i], lds + C::kX + i * C::X::kBytes);
+        }
+        stored();
+        if (r0 + C::RT < t.last - t.first)
+            load(r0 + C::RT);
+        f32x4 acc[C::FP] = {};
+#pragma unroll
+        for (int i = 0; i < C::kSteps; ++i)
+#pragma unroll
+            for (int part = 0; part < 2; ++part) {
+                const u32x4 q = C::X::fragment(lds + C::kX + i * C::X::kBytes, fq, part);
+#pragma unroll
+                for (int f = 0; f < C::FP; ++f)
+                    acc[f] = multiply(C::W::fragment(lds + i * C::W::kBytes, fp + f, part), q, acc[f], T{});
+            }
+#pragma unroll
+        for (int f = 0; f < C::FP; ++f) {
+            const int e = f * 16 + (lane >> 4) * 4;
+            f32x4 v = acc[f] + *reinterpret_cast<const f32x4 *>(biases + fp * 16 + e);
+            if (relu)
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    v[k] = v[k] < 0.0f ? 0.0f : v[k];
+            store_values(mine + (lane & 15) * C::kRowBytes + e * (int)sizeof(T), v, T{});
+        }
+        __builtin_amdgcn_wave_barrier();
+        constexpr int kPieces = 64 / V;  // of a row
+#pragma unroll
+        for (int i = 0; i < 16 * kPieces / 64; ++i) {
+            const int r = (i * 64 + lane) / kPieces, c = (i * 64 + lane) % kPieces * V;
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(mine + r * C::kRowBytes + c * (int)sizeof(T));
+            const unsigned row = t.first + r0 + fq * 16 + r;
+            const int n = n0 + fp * 16 + c;
+            if (row < t.last && n < O)
+                write_piece(y + (row * ys + n), v, O - n, T{});
+        }
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
 // ---- both gradients in one launch -----------------------------------------------------
 
 // One tile of dx (CR) or of a head's dW (CW) a workgroup, the longest first: the
@@ -1519,11 +1642,61 @@ bool large_tiles(const Problem &p, int width)
     return 8 * ((large + kCus - 1) / kCus) <= 4.6 * ((small + 2 * kCus - 1) / (2 * kCus));
 }
 
+template <class C>
+hipError_t launch_shallow(const Problem &p, const Matrix<typename C::T> &w, const Matrix<typename C::T> &x,
+                          const float *bias, bool relu, Rows y, int width, hipStream_t s)
+{
+    using T = typename C::T;
+    const unsigned cols = tiles_of(width, C::TO), want = 256 * C::kAtOnce / cols;
+    // stretches for `want` places, some of which the heads' last ones take
+    unsigned stretch = (unsigned)p.heads < want / 2 ? p.rows / (want - p.heads) : p.rows / (want / 2);
+    stretch = (stretch + 32) / 32 * 32;
+    const unsigned places = p.rows / stretch + p.heads + 1;
+    const unsigned groups = (places + kXcds - 1) / kXcds * kXcds * cols;
+    shallow_kernel<C><<<groups, C::kThreads, 0, s>>>(p, w, x, bias, relu, static_cast<T *>(const_cast<void *>(y.p)), y.stride,
+                                                     width, stretch);
+    return hipGetLastError();
+}
+
+template <class T, int TO, bool DEEP_W, bool MASK>
+hipError_t shallow(const Problem &p, const Matrix<T> &w, const Matrix<T> &x, const float *bias, bool relu, Rows y,
+                   int width, hipStream_t s)
+{
+    const unsigned steps = tiles_of((long long)x.cols * sizeof(T), 128);
+    if constexpr (DEEP_W) {
+        if (steps == 3)
+            return launch_shallow<Shallow<T, TO, 3, DEEP_W, MASK>>(p, w, x, bias, relu, y, width, s);
+        if (steps == 4)
+            return launch_shallow<Shallow<T, TO, 4, DEEP_W, MASK>>(p, w, x, bias, relu, y, width, s);
+        if (steps == 5)
+            return launch_shallow<Shallow<T, TO, 5, DEEP_W, MASK>>(p, w, x, bias, relu, y, width, s);
+    }
+    return steps == 1 ? launch_shallow<Shallow<T, TO, 1, DEEP_W, MASK>>(p, w, x, bias, relu, y, width, s)
+                      : launch_shallow<Shallow<T, TO, 2, DEEP_W, MASK>>(p, w, x, bias, relu, y, width, s);
+}
+
+// Whether a product goes with its weights in LDS: not too wide (its rows are read
+// for each 128 columns), on rows for all of the chip, and shallow: up to 2 steps,
+// or 5 for a layer, but not where bf16 operands of more than two go to LDS by
+// themselves (262,144 rows of 256 to 256: 72 us, 80 here; their gradients with
+// ReLU take 220 us, 227 with dx here).
+template <class T, bool DEEP_W>
+bool is_shallow(const Problem &p, const Matrix<T> &w, const Matrix<T> &x, int width, int depth)
+{
+    const unsigned steps = tiles_of((long long)depth * sizeof(T), 128);
+    if (width > 512 || p.rows < 32768 || steps > 5)
+        return false;
+    return steps <= 2 || (DEEP_W && (sizeof(T) == 4 || !goes_alone(w) || !goes_alone(x)));
+}
+
 // The rows' product with tiles for its width.
 template <class T, bool DEEP_W, bool MASK>
 hipError_t rows_product(const Problem &p, const Matrix<T> &w, const Matrix<T> &x, const float *bias,
                         bool relu, Rows y, int width, int depth, hipStream_t s)
 {
+    if (is_shallow<T, DEEP_W>(p, w, x, width, depth))
+        return width <= 64 ? shallow<T, 64, DEEP_W, MASK>(p, w, x, bias, relu, y, width, s)
+                           : shallow<T, 128, DEEP_W, MASK>(p, w, x, bias, relu, y, width, s);
     const bool alone = goes_alone(w) && goes_alone(x);
     if constexpr (sizeof(T) == 2 && !MASK)
         if (alone && depth >= 512 && large_tiles(p, width))

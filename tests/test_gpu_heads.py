@@ -152,7 +152,9 @@ LINEAR_CASES = [  # counts by head, rows without a head, fan_in, fan_out, pad, s
     ([40, 300, 8], 5, 128, 128, 8, 0), ([33] * 9, 0, 72, 264, 0, 1), ([5] * 256, 9, 24, 40, 0, 0), ([2, 1100], 0, 283, 136, 0, 0),
     ([9000, 10], 4, 64, 64, 0, 0), ([31, 600], 50, 512, 520, 0, 0), ([2, 3, 0, 1], 1, 1030, 300, 0, 0), ([700, 900], 0, 520, 1032, 0, 0),
     ([9000, 2100, 1], 130, 264, 520, 0, 0), ([9000, 2100, 1], 130, 263, 519, 2, 1), ([40] * 255 + [300], 9, 136, 144, 0, 0),
-    ([40] * 256, 0, 131, 137, 0, 0), ([100] * 30 + [0, 1500], 20, 1024, 1032, 0, 0)]
+    ([40] * 256, 0, 131, 137, 0, 0), ([100] * 30 + [0, 1500], 20, 1024, 1032, 0, 0),
+    ([20000, 0, 13000, 5], 70, 319, 256, 0, 0), ([20000, 0, 13000, 5], 300, 63, 64, 1, 1), ([33000], 5, 128, 300, 0, 0),
+    ([11000, 11100, 11200], 0, 40, 5, 0, 0), ([300] * 120, 0, 190, 130, 2, 1), ([1] * 200 + [33000], 1, 250, 128, 6, 0)]
 
 
 def layer(counts, tail, I, O, pad, shift, dtype, seed):
