@@ -733,10 +733,11 @@ __device__ __forceinline__ void tile_product(const typename C::P::Source &ps, co
 // of Q, elements 4 h + (0 .. 3) of each 16 of P.  They go through LDS, 16 rows at
 // a time, to be written in 16-byte pieces.  Bytes of a row there (4 of 64 banks
 // further on for the next row):
+// (float results are written from the registers, 16 bytes a lane.)
 template <class C>
 constexpr int kResultRow = C::FP * 16 * (int)sizeof(typename C::T) + 16;
 template <class C>
-constexpr int kResultBytes = C::WP * C::WQ * 16 * kResultRow<C>;
+constexpr int kResultBytes = sizeof(typename C::T) == 2 ? C::WP * C::WQ * 16 * kResultRow<C> : 16;
 __device__ __forceinline__ void store_values(char *to, f32x4 v, __bf16)
 {
     union {
@@ -792,8 +793,17 @@ __device__ __forceinline__ void write_rows(const RowTile &t, int n0, int width, 
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
                     v[k] = v[k] < 0.0f ? 0.0f : v[k];
-            store_values(mine + (lane & 15) * kResultRow<C> + e * sizeof(T), v, T{});
+            if constexpr (sizeof(T) == 4) {
+                const unsigned row = t.first + wq + j * 16 + (lane & 15);
+                const int n = n0 + wp + e;
+                if (row < t.last && n < width)
+                    write_piece(y + (row * ys + n), __builtin_bit_cast(u32x4, v), width - n, T{});
+            } else {
+                store_values(mine + (lane & 15) * kResultRow<C> + e * sizeof(T), v, T{});
+            }
         }
+        if constexpr (sizeof(T) == 4)
+            continue;
         __builtin_amdgcn_wave_barrier();
         constexpr int kPieces = C::FP * 16 / V;  // of a row
 #pragma unroll
@@ -1675,6 +1685,14 @@ hipError_t shallow(const Problem &p, const Matrix<T> &w, const Matrix<T> &x, con
                       : launch_shallow<Shallow<T, TO, 2, DEEP_W, MASK>>(p, w, x, bias, relu, y, width, s);
 }
 
+// 128 columns a tile, or 64: for narrow matrices, and for float, which is bound by
+// its products, where 128 would pad more than a seventh.
+template <class T>
+bool wide_tile(int width)
+{
+    return width > 64 && (sizeof(T) == 2 || 8 * 64 * tiles_of(width, 64) > 7 * 128 * tiles_of(width, 128));
+}
+
 // Whether a product goes with its weights in LDS: not too wide (its rows are read
 // for each 128 columns), on rows for all of the chip, and shallow: up to 2 steps,
 // or 5 for a layer, but not where bf16 operands of more than two go to LDS by
@@ -1702,7 +1720,7 @@ hipError_t rows_product(const Problem &p, const Matrix<T> &w, const Matrix<T> &x
         if (alone && depth >= 512 && large_tiles(p, width))
             return launch_rows<Product<T, 256, 256, 4, 2, DEEP_W, true, false, true>>(p, w, x, bias, relu, y, width,
                                                                                     depth, s);
-    if (width > 64) {
+    if (wide_tile<T>(width)) {
         if constexpr (!MASK)
             if (alone)
                 return launch_rows<Product<T, 128, 128, 2, 2, DEEP_W, true, false, true>>(
@@ -1714,16 +1732,19 @@ hipError_t rows_product(const Problem &p, const Matrix<T> &w, const Matrix<T> &x
                                                                              width, depth, s);
 }
 
-// Rows of a stretch of the weights' product, 0: each head as a whole.  Split
-// until 512 workgroups (2 a compute unit) have work.
+// Rows of a stretch of the weights' product, 0: each head as a whole.  Split until
+// there are 512 tiles, a round of them, or 1024 in float32, whose tiles take so
+// long that heads of many rows would hold up the rest (191 to 576 on 242,086 rows of
+// 26 heads, weights' part: 820 us, 1448 with 512).  In bfloat16 the parts' traffic
+// costs more (256 to 256 on 65,536 rows of 8, both gradients: 149 us, 165 with 1024).
 struct Split {
     unsigned stretch, places;
 };
-Split split_rows(unsigned rows, int heads, int fan_in, int fan_out)
+Split split_rows(unsigned rows, int heads, int fan_in, int fan_out, bool bf16)
 {
     const unsigned long long tiles =
         (unsigned long long)tiles_of(fan_in, fan_in > 64 ? 128 : 64) * tiles_of(fan_out, fan_out > 64 ? 128 : 64);
-    const unsigned long long want = 512 / tiles;
+    const unsigned long long want = (bf16 ? 512 : 1024) / tiles;
     if (want <= (unsigned)heads)
         return {0, (unsigned)heads};
     unsigned stretch = (unsigned)(rows / (want - heads));
@@ -1749,7 +1770,7 @@ hipError_t launch_weights(const Problem &p, const Matrix<typename C::T> &dz,
                           const Matrix<typename C::T> &x, float *dw, float *db, char *workspace,
                           hipStream_t s)
 {
-    const Split split = split_rows(p.rows, p.heads, p.fan_in, p.fan_out);
+    const Split split = split_rows(p.rows, p.heads, p.fan_in, p.fan_out, sizeof(typename C::T) == 2);
     const bool partial = split.stretch != 0;
     const size_t size = (size_t)p.fan_in * p.fan_out;
     float *wparts = reinterpret_cast<float *>(workspace);
@@ -1769,7 +1790,7 @@ template <class T, bool MASK>
 hipError_t weights_product(const Problem &p, const Matrix<T> &dz, const Matrix<T> &x, float *dw,
                            float *db, char *workspace, hipStream_t s)
 {
-    const bool wide_o = p.fan_out > 64, wide_i = p.fan_in > 64;
+    const bool wide_o = wide_tile<T>(p.fan_out), wide_i = wide_tile<T>(p.fan_in);
     const bool alone = goes_alone(dz) && goes_alone(x);
     if constexpr (sizeof(T) == 2 && !MASK)
         if (alone && p.fan_out > 128 && p.fan_in > 128 &&
@@ -1870,7 +1891,7 @@ bool gradients_together(const Problem &p)
     const unsigned long long x_tiles = p.rows / 256ull * tiles_of(p.fan_in, 256);
     const unsigned long long w_tiles = (unsigned long long)p.heads * tiles_of(p.fan_out, 256) * tiles_of(p.fan_in, 256);
     return p.fan_in >= 512 && p.fan_out >= 512 && x_tiles + w_tiles < 1u << 16 && x_tiles + w_tiles >= 512 &&
-           split_rows(p.rows, p.heads, p.fan_in, p.fan_out).stretch == 0;
+           split_rows(p.rows, p.heads, p.fan_in, p.fan_out, true).stretch == 0;
 }
 
 template <class T>
@@ -1929,7 +1950,7 @@ hipError_t launch_heads_linear(const LinearShape &sh, Rows x, const void *w, con
 
 size_t heads_linear_workspace_bytes(unsigned rows, int heads, int fan_in, int fan_out, bool relu, bool bf16)
 {
-    const Split split = split_rows(rows, heads, fan_in, fan_out), narrow = narrow_split(rows, heads, fan_in, fan_out, bf16);
+    const Split split = split_rows(rows, heads, fan_in, fan_out, bf16), narrow = narrow_split(rows, heads, fan_in, fan_out, bf16);
     size_t places = split.stretch ? split.places : 0;
     if (is_narrow(fan_in, fan_out) && narrow.places > places)
         places = narrow.places;
