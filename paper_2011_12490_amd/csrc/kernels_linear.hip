@@ -288,10 +288,11 @@ struct Tile {
             return (TILE == 64 ? (r >> 1 & 1) | (r >> 2 & 2) : (r & 3) | (r >> 1 & 4)) << 1;
         return kRowStep % 16 == 0 ? ((r & 3) | (r >> 1 & 4)) << 1 : 0;
     }
-    static __device__ __forceinline__ unsigned my_row() { return threadIdx.x / kPerRow; }
+    static __device__ __forceinline__ unsigned my_thread() { return threadIdx.x % THREADS; }  // of a team
+    static __device__ __forceinline__ unsigned my_row() { return my_thread() / kPerRow; }
     static __device__ __forceinline__ int my_col()
     {
-        return (int)((threadIdx.x % kPerRow) ^ turn(my_row())) * V;
+        return (int)((my_thread() % kPerRow) ^ turn(my_row())) * V;
     }
 
     // This workgroup's tiles of a matrix, from tile row (or column) t0 on.
@@ -390,7 +391,7 @@ struct Tile {
     {
 #pragma unroll
         for (int i = 0; i < kShare; ++i)
-            *reinterpret_cast<u32x4 *>(lds + (threadIdx.x + i * THREADS) * 16) = s.x[i];
+            *reinterpret_cast<u32x4 *>(lds + (my_thread() + i * THREADS) * 16) = s.x[i];
     }
 
     // The same without registers in between, for matrices without a mask whose
@@ -513,24 +514,26 @@ __device__ __forceinline__ f32x4 multiply(u32x4 p, u32x4 q, f32x4 c, float)
 
 // Sizes of a product: a workgroup's tile TP x TQ, by WP x WQ waves.  MASK: Q has
 // a mask.  ASYNC: operands go from memory to LDS by themselves (Tile::Feed).
-// EACH_Q: tile_product shows its caller the Q tiles.
+// EACH_Q: tile_product shows its caller the Q tiles.  TEAMS: of so many waves each;
+// they take the depth's steps in turn, in LDS of their own, and add up at the end.
 template <class T_, int TP_, int TQ_, int WP_, int WQ_, bool DEEP_P, bool DEEP_Q, bool MASK,
-          bool ASYNC = false, bool EACH_Q = false>
+          bool ASYNC = false, bool EACH_Q = false, int TEAMS = 1>
 struct Product {
     using T = T_;
     static constexpr int TP = TP_, TQ = TQ_, WP = WP_, WQ = WQ_;
-    static constexpr int kThreads = WP * WQ * 64;
+    static constexpr int kTeams = TEAMS, kTeam = WP * WQ * 64, kThreads = kTeam * TEAMS;
     static constexpr bool kAsync = ASYNC, kEachQ = EACH_Q;
-    using P = Tile<T, TP, DEEP_P, kThreads, false>;
-    using Q = Tile<T, TQ, DEEP_Q, kThreads, MASK>;
+    static_assert(TEAMS == 1 || !ASYNC, "teams bring their operands through registers");
+    using P = Tile<T, TP, DEEP_P, kTeam, false>;
+    using Q = Tile<T, TQ, DEEP_Q, kTeam, MASK>;
     static constexpr int kDepth = P::D;
     static constexpr int FP = TP / WP / 16, FQ = TQ / WQ / 16;  // a wave's 16 x 16 results
-    static constexpr int kStage = P::kBytes + Q::kBytes, kLds = 2 * kStage;
+    static constexpr int kStage = P::kBytes + Q::kBytes, kLds = 2 * kStage * TEAMS;
     static constexpr int kLoads = P::kShare + Q::kShare;  // of a thread for a step
     // tile_product's sets of registers: a second one costs masked 128 x 128 tiles
     // spills and narrow ones a workgroup more on the compute unit (262,144 rows of
     // 64 to 64 24 us, 18 with one; of 319 to 256 132, 147 with one)
-    static constexpr int kSets = !MASK && FP * FQ >= 16 ? 2 : 1;
+    static constexpr int kSets = TEAMS > 1 || (!MASK && FP * FQ >= 16) ? 2 : 1;
     static_assert(FP * WP * 16 == TP && FQ * WQ * 16 == TQ, "whole results a wave");
 };
 
@@ -672,16 +675,20 @@ struct Pipe {
 // Through registers, one tile: acc = sum over `depth` of P(p, k) Q(q, k).  A step's
 // loads begin two steps before it is stored, into two sets of registers in turn
 // (one step is shorter than a load takes), or one where there is no room for two.
-// each_q(share): called with each of the Q tiles that this thread brings.
+// each_q(share): called with each of the Q tiles that this thread brings.  A team's
+// steps are every kTeams-th; all teams make as many, of zeros behind the last.
 template <class C, class EachQ>
 __device__ __forceinline__ void tile_product(const typename C::P::Source &ps, const typename C::Q::Source &qs,
                                              unsigned depth, char *lds,
                                              f32x4 (&acc)[C::FP][C::FQ], EachQ each_q)
 {
-    const int wave = uniform(threadIdx.x >> 6);
+    constexpr unsigned kStep = C::kDepth * C::kTeams;
+    const int wave = uniform(threadIdx.x >> 6) % (C::kTeam / 64);
     const int fp = (wave % C::WP) * C::FP, fq = (wave / C::WP) * C::FQ;
     if (depth == 0)
         return;
+    const unsigned team = C::kTeams > 1 ? uniform(threadIdx.x / C::kTeam) : 0, mine = team * C::kDepth;
+    lds += team * 2 * C::kStage;
     struct Set {
         typename C::P::S p;
         typename C::Q::S q;
@@ -689,16 +696,20 @@ __device__ __forceinline__ void tile_product(const typename C::P::Source &ps, co
     Set &even = sets[0], &odd = sets[C::kSets - 1];  // steps 0, 2, ... and 1, 3, ...
     u32x4 pa[C::FP], pb[C::FP], q[C::FQ];
     auto load = [&](Set &s, unsigned k) {
-        if (k < depth) {
-            C::P::load(s.p, ps, k);
-            C::Q::load(s.q, qs, k);
+        if (k + mine < depth) {
+            C::P::load(s.p, ps, k + mine);
+            C::Q::load(s.q, qs, k + mine);
+        } else if (C::kTeams > 1) {
+            s = Set{};
         }
     };
     auto bring = [&](Set &s, unsigned k, unsigned to) {
         if (k >= depth)
             return;
-        C::P::settle(s.p, ps, k);
-        C::Q::settle(s.q, qs, k);
+        if (C::kTeams == 1 || k + mine < depth) {
+            C::P::settle(s.p, ps, k + mine);
+            C::Q::settle(s.q, qs, k + mine);
+        }
         if constexpr (C::kEachQ)
             each_q(s.q);
         C::P::store(s.p, lds + to * C::kStage);
@@ -707,25 +718,51 @@ __device__ __forceinline__ void tile_product(const typename C::P::Source &ps, co
     // the step at k, whose successor is in `next`
     auto step = [&](unsigned k, unsigned stage, Set &next) {
         multiply_part<C, false>(pa, q, pb, true, lds + stage * C::kStage, fp, fq, 1, acc, [](int) {});
-        bring(next, k + C::kDepth, stage ^ 1);
-        load(next, k + (1 + C::kSets) * C::kDepth);
+        bring(next, k + kStep, stage ^ 1);
+        load(next, k + (1 + C::kSets) * kStep);
         stored();
-        multiply_part<C, false>(pb, q, pa, k + C::kDepth < depth, lds + (stage ^ 1) * C::kStage, fp, fq, 0, acc, [](int) {});
+        multiply_part<C, false>(pb, q, pa, k + kStep < depth, lds + (stage ^ 1) * C::kStage, fp, fq, 0, acc, [](int) {});
     };
     load(even, 0);
     if constexpr (C::kSets == 2)
-        load(odd, C::kDepth);
+        load(odd, kStep);
     bring(even, 0, 0);
-    load(even, C::kSets * C::kDepth);
+    load(even, C::kSets * kStep);
     stored();
     read_first<C>(pa, q, lds, fp, fq);
 #pragma unroll 1
-    for (unsigned k = 0; k < depth; k += 2 * C::kDepth) {
+    for (unsigned k = 0; k < depth; k += 2 * kStep) {
         step(k, 0, odd);
-        if (k + C::kDepth < depth)
-            step(k + C::kDepth, 1, even);
+        if (k + kStep < depth)
+            step(k + kStep, 1, even);
     }
 }
+
+// The teams' results added up in the first one's registers, in the teams' order.
+// `lds` is that of the stages, which all have been read.  True for the first team.
+template <class C>
+__device__ __forceinline__ bool join_teams(char *lds, f32x4 (&acc)[C::FP][C::FQ])
+{
+    constexpr int kAll = C::FP * C::FQ;
+    const int team = uniform(threadIdx.x / C::kTeam);
+    f32x4 *parts = reinterpret_cast<f32x4 *>(lds) + threadIdx.x % C::kTeam;
+    stored();
+    if (team > 0)
+#pragma unroll
+        for (int n = 0; n < kAll; ++n)
+            parts[((team - 1) * kAll + n) * C::kTeam] = acc[n / C::FQ][n % C::FQ];
+    stored();
+    if (team > 0)
+        return false;
+#pragma unroll
+    for (int t = 0; t < C::kTeams - 1; ++t)
+#pragma unroll
+        for (int n = 0; n < kAll; ++n)
+            acc[n / C::FQ][n % C::FQ] += parts[(t * kAll + n) * C::kTeam];
+    return true;
+}
+template <class C>
+constexpr int kJoinBytes = (C::kTeams - 1) * C::FP * C::FQ * C::kTeam * 16;
 
 // ---- rows: the layer, and its rows' gradient --------------------------------------
 
@@ -834,7 +871,7 @@ __global__ __launch_bounds__(C::kThreads, 2) void rows_kernel(
     __shared__ __attribute__((aligned(16))) char results[C::kAsync ? kResultBytes<C> : 16];
     __shared__ __attribute__((aligned(16))) float biases[kBiases][C::TP];
     __shared__ unsigned before[kMaxHeads + 1];
-    static_assert(C::kAsync || kResultBytes<C> <= C::kLds, "results take the stages' place");
+    static_assert(C::kAsync || kJoinBytes<C> + kResultBytes<C> <= C::kLds, "parts and results take the stages' place");
     count_tiles(p, C::TQ, before);
     const unsigned headed = uniform(before[p.heads]), headless = bound(p, p.heads);
     const unsigned tail = (unsigned)(((unsigned long long)(p.rows - headless) + C::TQ - 1) / C::TQ);
@@ -920,7 +957,10 @@ __global__ __launch_bounds__(C::kThreads, 2) void rows_kernel(
             sources(t, n0, ps, qs);
             tile_product<C>(ps, qs, depth, lds, acc, [](auto &) {});
         }
-        write_rows<C>(t, n0, width, acc, has && bias ? biases[0] : nullptr, has && relu, lds, y, ys);
+        if constexpr (C::kTeams > 1)
+            if (!join_teams<C>(lds, acc))
+                return;
+        write_rows<C>(t, n0, width, acc, has && bias ? biases[0] : nullptr, has && relu, lds + kJoinBytes<C>, y, ys);
     }
 }
 
@@ -1707,6 +1747,19 @@ bool is_shallow(const Problem &p, const Matrix<T> &w, const Matrix<T> &x, int wi
     return steps <= 2 || (DEEP_W && (sizeof(T) == 4 || !goes_alone(w) || !goes_alone(x)));
 }
 
+// Few rows: tiles of 64 x 32, whose depth four teams of two waves share, while that
+// is a round of workgroups, or two and a half in float, whose products of 128 rows
+// take longer, if it is not shallow.  us of large tiles and of these: float32 of 128
+// to 2,816, 1,024 rows, dx 182, 40; of 1,024 to 1,024, 1,024 rows (544 tiles) 72, 52,
+// 2,048 rows (1,056) 74, 83; dx of 319 to 155, 2,048 rows (330) 12.6, 15; bfloat16 of
+// 2,816 to 128, 2,048 rows 34, 14; of 1,024 to 1,024, 512 rows (288) 13, 16.
+template <class T>
+bool few_rows(const Problem &p, int width, int depth)
+{
+    const unsigned long long tiles = (p.rows / 32ull + p.heads / 2) * tiles_of(width, 64);
+    return tiles <= (sizeof(T) == 4 && depth >= 256 ? 640 : 256);
+}
+
 // The rows' product with tiles for its width.
 template <class T, bool DEEP_W, bool MASK>
 hipError_t rows_product(const Problem &p, const Matrix<T> &w, const Matrix<T> &x, const float *bias,
@@ -1715,6 +1768,9 @@ hipError_t rows_product(const Problem &p, const Matrix<T> &w, const Matrix<T> &x
     if (is_shallow<T, DEEP_W>(p, w, x, width, depth))
         return width <= 64 ? shallow<T, 64, DEEP_W, MASK>(p, w, x, bias, relu, y, width, s)
                            : shallow<T, 128, DEEP_W, MASK>(p, w, x, bias, relu, y, width, s);
+    if (few_rows<T>(p, width, depth))
+        return launch_rows<Product<T, 64, 32, 2, 1, DEEP_W, true, MASK, false, false, 4>>(p, w, x, bias, relu, y, width,
+                                                                                      depth, s);
     const bool alone = goes_alone(w) && goes_alone(x);
     if constexpr (sizeof(T) == 2 && !MASK)
         if (alone && depth >= 512 && large_tiles(p, width))
