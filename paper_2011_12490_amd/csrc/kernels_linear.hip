@@ -807,6 +807,25 @@ __device__ __forceinline__ void write_piece(T *to, u32x4 v, int left, T)
             to[k] = piece.e[k];
 }
 
+// Whether results go past the caches (nontemporal): their rows are whole 128-byte
+// lines.  bf16 us so and with ordinary stores: 2,048 to 4,096 on 32,768 rows 482, 513;
+// 256 to 256 on 262,144 63, 72; 319 to 256 on 262,139 94, 108; but rows of 319, whose
+// lines are shared, 280, 270.
+template <class T>
+__host__ __device__ __forceinline__ bool past_caches(const T *y, long long ys, int width)
+{
+    return ((unsigned)reinterpret_cast<unsigned long long>(y) | (unsigned)ys * (unsigned)sizeof(T) |
+            (unsigned)width * (unsigned)sizeof(T)) % 128 == 0;
+}
+template <class T>
+__device__ __forceinline__ void write_result(T *to, u32x4 v, int left, bool past)
+{
+    if (past)
+        __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(to));
+    else
+        write_piece(to, v, left, T{});
+}
+
 // A tile of the result: rows [t.first, t.last), columns from n0 on.
 template <class C>
 __device__ __forceinline__ void write_rows(const RowTile &t, int n0, int width, const f32x4 (&acc)[C::FP][C::FQ],
@@ -818,6 +837,7 @@ __device__ __forceinline__ void write_rows(const RowTile &t, int n0, int width, 
     const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int wp = (wave % C::WP) * C::FP * 16, wq = (wave / C::WP) * C::FQ * 16;
     char *mine = results + wave * 16 * kResultRow<C>;
+    const bool past = past_caches(y, ys, width);
 #pragma unroll
     for (int j = 0; j < C::FQ; ++j) {
 #pragma unroll
@@ -853,7 +873,7 @@ __device__ __forceinline__ void write_rows(const RowTile &t, int n0, int width, 
             const int n = n0 + wp + c;
             if (row >= t.last || n >= width)
                 continue;
-            write_piece(y + (row * ys + n), v, width - n, T{});
+            write_result(y + (row * ys + n), v, width - n, past);
         }
         __builtin_amdgcn_wave_barrier();
     }
@@ -1144,11 +1164,13 @@ __global__ __launch_bounds__(C::kThreads, 2) void weights_kernel(Problem p, Matr
 // keeps TO of its head's outputs' weights in LDS and goes through a stretch of
 // the head's rows, RT at a time, the next ones' loads under way: the rows stream,
 // whatever their alignment, and nothing is read again but by the other columns'
-// workgroups beside it.  Rows of bf16, us here and tile by tile: 319 to 256 on
-// 262,139 113, 132; 128 to 128 on 262,144 25 (5.3 TB/s), 31; 63 to 64 15, 20.
-template <class T_, int TO_, int STEPS, bool DEEP_W, bool MASK>
+// workgroups beside it.  Rows of bf16, us here and tile by tile, both with ordinary
+// stores: 319 to 256 on 262,139 113, 132; 128 to 128 on 262,144 25 (5.3 TB/s), 31; 63
+// to 64 15, 20.  PAST: results past the caches (past_caches): the first takes 94 so.
+template <class T_, int TO_, int STEPS, bool DEEP_W, bool MASK, bool PAST>
 struct Shallow {
     using T = T_;
+    static constexpr bool kPast = PAST;  // asked in the loop instead, it costs what it brings
     static constexpr int TO = TO_, kSteps = STEPS, kThreads = 512, kColGroups = TO / 64, RT = 16 * 8 / kColGroups;
     using W = Tile<T, TO, DEEP_W, kThreads, false>;
     using X = Tile<T, RT, true, kThreads, MASK>;
@@ -1254,7 +1276,7 @@ __global__ __launch_bounds__(C::kThreads, 2 * C::kAtOnce) void shallow_kernel(Pr
             const unsigned row = t.first + r0 + fq * 16 + r;
             const int n = n0 + fp * 16 + c;
             if (row < t.last && n < O)
-                write_piece(y + (row * ys + n), v, O - n, T{});
+                write_result(y + (row * ys + n), v, O - n, C::kPast);
         }
         __builtin_amdgcn_wave_barrier();
     }
@@ -1416,6 +1438,9 @@ struct Narrow {
     static constexpr int kResults = sizeof(T) == 2 ? kWaves * 16 * kRowBytes : 0;
     static constexpr int kZ = 0, kX = kZ + RT * TO * (int)sizeof(T), kW = kX + RT * TI * (int)sizeof(T);
     static constexpr int kOut = kW + TO * TI * (int)sizeof(T), kLds = kOut + kResults;
+    // dx past the caches: us so and with ordinary stores, of 128 to 128 on 262,144 rows
+    // with ReLU 56, 62, without 47, 46; of 64 to 64 with ReLU 31.6, 31.0
+    static constexpr bool kPast = MASK && TI == 128;
     static constexpr int kRowsOfThreads = kThreads / Z::kPerRow;
     static_assert(kRowsOfThreads * (TO + 1) * 4 <= kW, "sums take the rows' place");
 };
@@ -1449,6 +1474,7 @@ __global__ __launch_bounds__(C::kThreads, 2) void narrow_kernel(Problem p, Matri
     zs.m.mask += t.first * dz.mask_stride;
     xs.m.rows = zs.m.rows = t.last - t.first;
     ws.m.p += t.head * ((size_t)I * O);
+    const bool past = C::kPast && past_caches(dx, dxs, I);
     typename C::X::S sx[C::kSteps];
     typename C::Z::S sz[C::kSteps];
     auto load = [&](unsigned k) {
@@ -1523,7 +1549,7 @@ __global__ __launch_bounds__(C::kThreads, 2) void narrow_kernel(Problem p, Matri
                     const u32x4 v = *reinterpret_cast<const u32x4 *>(mine + r * C::kRowBytes + c * (int)sizeof(T));
                     const int n = fc * 16 + c;
                     if (first + r < t.last && n < I)
-                        write_piece(dx + ((first + r) * dxs + n), v, I - n, T{});
+                        write_result(dx + ((first + r) * dxs + n), v, I - n, past);
                 }
                 __builtin_amdgcn_wave_barrier();
             } else {
@@ -1733,21 +1759,21 @@ hipError_t launch_shallow(const Problem &p, const Matrix<typename C::T> &w, cons
     return hipGetLastError();
 }
 
-template <class T, int TO, bool DEEP_W, bool MASK>
+template <class T, int TO, bool DEEP_W, bool MASK, bool PAST>
 hipError_t shallow(const Problem &p, const Matrix<T> &w, const Matrix<T> &x, const float *bias, bool relu, Rows y,
                    int width, hipStream_t s)
 {
     const unsigned steps = tiles_of((long long)x.cols * sizeof(T), 128);
     if constexpr (DEEP_W) {
         if (steps == 3)
-            return launch_shallow<Shallow<T, TO, 3, DEEP_W, MASK>>(p, w, x, bias, relu, y, width, s);
+            return launch_shallow<Shallow<T, TO, 3, DEEP_W, MASK, PAST>>(p, w, x, bias, relu, y, width, s);
         if (steps == 4)
-            return launch_shallow<Shallow<T, TO, 4, DEEP_W, MASK>>(p, w, x, bias, relu, y, width, s);
+            return launch_shallow<Shallow<T, TO, 4, DEEP_W, MASK, PAST>>(p, w, x, bias, relu, y, width, s);
         if (steps == 5)
-            return launch_shallow<Shallow<T, TO, 5, DEEP_W, MASK>>(p, w, x, bias, relu, y, width, s);
+            return launch_shallow<Shallow<T, TO, 5, DEEP_W, MASK, PAST>>(p, w, x, bias, relu, y, width, s);
     }
-    return steps == 1 ? launch_shallow<Shallow<T, TO, 1, DEEP_W, MASK>>(p, w, x, bias, relu, y, width, s)
-                      : launch_shallow<Shallow<T, TO, 2, DEEP_W, MASK>>(p, w, x, bias, relu, y, width, s);
+    return steps == 1 ? launch_shallow<Shallow<T, TO, 1, DEEP_W, MASK, PAST>>(p, w, x, bias, relu, y, width, s)
+                      : launch_shallow<Shallow<T, TO, 2, DEEP_W, MASK, PAST>>(p, w, x, bias, relu, y, width, s);
 }
 
 // 128 columns a tile, or 64: for narrow matrices, and for float, which is bound by
@@ -1790,9 +1816,14 @@ template <class T, bool DEEP_W, bool MASK>
 hipError_t rows_product(const Problem &p, const Matrix<T> &w, const Matrix<T> &x, const float *bias,
                         bool relu, Rows y, int width, int depth, hipStream_t s)
 {
-    if (is_shallow<T, DEEP_W>(p, w, x, width, depth))
-        return width <= 64 ? shallow<T, 64, DEEP_W, MASK>(p, w, x, bias, relu, y, width, s)
-                           : shallow<T, 128, DEEP_W, MASK>(p, w, x, bias, relu, y, width, s);
+    if (is_shallow<T, DEEP_W>(p, w, x, width, depth)) {
+        const bool past = past_caches(static_cast<const T *>(y.p), y.stride, width);
+        if (width <= 64)
+            return past ? shallow<T, 64, DEEP_W, MASK, true>(p, w, x, bias, relu, y, width, s)
+                        : shallow<T, 64, DEEP_W, MASK, false>(p, w, x, bias, relu, y, width, s);
+        return past ? shallow<T, 128, DEEP_W, MASK, true>(p, w, x, bias, relu, y, width, s)
+                    : shallow<T, 128, DEEP_W, MASK, false>(p, w, x, bias, relu, y, width, s);
+    }
     if (few_rows<T>(p, width, depth))
         return launch_rows<Product<T, 64, 32, 2, 1, DEEP_W, true, MASK, false, false, 4>>(p, w, x, bias, relu, y, width,
                                                                                       depth, s);
@@ -1817,7 +1848,7 @@ hipError_t rows_product(const Problem &p, const Matrix<T> &w, const Matrix<T> &x
 // there are 512 tiles, a round of them, or 1024 in float32, whose tiles take so
 // long that heads of many rows would hold up the rest (191 to 576 on 242,086 rows of
 // 26 heads, weights' part: 820 us, 1448 with 512).  In bfloat16 the parts' traffic
-// costs more (256 to 256 on 65,536 rows of 8, both gradients: 149 us, 165 with 1024).
+// costs more (256 to 256 on 262,144 rows of 16, both gradients: 149 us, 165 with 1024).
 struct Split {
     unsigned stretch, places;
 };
