@@ -154,7 +154,14 @@ LINEAR_CASES = [  # counts by head, rows without a head, fan_in, fan_out, pad, s
     ([9000, 2100, 1], 130, 264, 520, 0, 0), ([9000, 2100, 1], 130, 263, 519, 2, 1), ([40] * 255 + [300], 9, 136, 144, 0, 0),
     ([40] * 256, 0, 131, 137, 0, 0), ([100] * 30 + [0, 1500], 20, 1024, 1032, 0, 0),
     ([20000, 0, 13000, 5], 70, 319, 256, 0, 0), ([20000, 0, 13000, 5], 300, 63, 64, 1, 1), ([33000], 5, 128, 300, 0, 0),
-    ([11000, 11100, 11200], 0, 40, 5, 0, 0), ([300] * 120, 0, 190, 130, 2, 1), ([1] * 200 + [33000], 1, 250, 128, 6, 0)]
+    ([11000, 11100, 11200], 0, 40, 5, 0, 0), ([300] * 120, 0, 190, 130, 2, 1), ([1] * 200 + [33000], 1, 250, 128, 6, 0),
+    # few rows and long depths
+    ([3, 0, 60, 1], 2, 40, 1500, 0, 0), ([149], 0, 155, 2816, 3, 1), ([7] * 20, 3, 1601, 70, 0, 0), ([33, 31, 32], 0, 1152, 136, 0, 0),
+    # too many rows for those, too few to stream
+    ([5000, 0, 1300], 40, 300, 333, 0, 0), ([5000, 1300], 40, 264, 328, 0, 0), ([5000, 1300], 40, 263, 331, 2, 1),
+    ([21000, 9000], 20, 400, 40, 0, 0), ([21000, 9000], 20, 40, 400, 0, 0), ([21000, 9000], 20, 39, 401, 2, 1),
+    # results in whole lines of longer rows
+    ([32000, 1000], 5, 128, 256, 64, 0), ([5000, 7000], 5, 512, 640, 64, 0)]
 
 
 def layer(counts, tail, I, O, pad, shift, dtype, seed):

@@ -1,6 +1,9 @@
 """What the training operators refuse, before any GPU work: sizes, strides,
 alignment and null arrays at the C entries, tensors that do not fit in Python."""
 import ctypes
+import os
+import shutil
+import subprocess
 
 import pytest
 import torch
@@ -153,3 +156,21 @@ def test_python_refuses_host_tensors():
                  lambda: heads.linear_backward(x, x, w, off), lambda: heads.AdamW([x], [x])):
         with pytest.raises(ValueError):
             call()
+
+
+def test_adamw_tensor_has_the_headers_layout(tmp_path):
+    """A C program prints the struct's size and offsets; the binding's mirror has the same."""
+    cc = shutil.which("gcc")
+    if cc is None:
+        pytest.skip("no gcc")
+    mirror = derf.derf_adamw_tensor
+    names = [f[0] for f in mirror._fields_]
+    prints = "".join('printf(" %%zu", offsetof(derf_adamw_tensor, %s));\n' % n for n in names)
+    source = tmp_path / "layout.c"
+    source.write_text('#include <stddef.h>\n#include <stdio.h>\n#include "derf.h"\n'
+                      'int main(void) {\nprintf("%zu", sizeof(derf_adamw_tensor));\n' + prints + "return 0;\n}\n")
+    program = str(tmp_path / "layout")
+    include = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include")
+    subprocess.run([cc, "-I", include, str(source), "-o", program], check=True)
+    got = [int(v) for v in subprocess.run([program], check=True, capture_output=True, text=True).stdout.split()]
+    assert got == [ctypes.sizeof(mirror)] + [getattr(mirror, n).offset for n in names]
