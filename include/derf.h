@@ -392,8 +392,10 @@ int derf_reset_stats(derf_handle *h);
  * memory of the current device unless they are called host; work is enqueued on
  * hip_stream (a hipStream_t, NULL: the default stream) and the calls return
  * without waiting.  They allocate nothing, run nothing on other streams and may
- * be captured into HIP graphs.  A workspace belongs to the caller, holds nothing
- * between calls, and is 16-byte aligned.  Results do not depend on the run:
+ * be captured into HIP graphs (not so the optimizer: derf_adamw_create allocates and
+ * waits, derf_adamw_step refuses a capturing stream, derf_adamw_destroy waits).  A
+ * workspace belongs to the caller, holds nothing between calls, and is 16-byte
+ * aligned.  Results do not depend on the run:
  * every sum has a fixed order.
  *   precision    a derf_precision: the type of the rows (float or bf16)
  *   *_stride     elements from a row to the next, >= the row length; rows need
@@ -516,7 +518,9 @@ typedef struct derf_adamw derf_adamw;
 int derf_adamw_create(derf_adamw **out, const derf_adamw_tensor *tensors, int num_tensors,
                       int state_bits);
 /* step: t above, >= 1.  grad_scale: device float or NULL (1): an unscaling or a
- * clipping factor that is computed on the device. */
+ * clipping factor that is computed on the device.  DERF_ERR_INVALID_ARG while
+ * hip_stream is being captured, with nothing recorded: step, lr and the other
+ * scalars are the call's, and a graph would repeat them at every replay. */
 int derf_adamw_step(derf_adamw *opt, double lr, double beta1, double beta2, double eps,
                     double weight_decay, long long step, const float *grad_scale,
                     void *hip_stream);

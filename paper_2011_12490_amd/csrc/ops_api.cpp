@@ -356,6 +356,13 @@ int derf_adamw_step(derf_adamw *opt, double lr, double beta1, double beta2, doub
         return report(DERF_ERR_INVALID_ARG, "grad_scale is not aligned to its elements");
     if (opt->items == 0)
         return DERF_OK;
+    // Step number and rates go into the launch, which a graph would repeat as it is.  Where
+    // the runtime does not tell (another stream's capture), the launch says what is wrong.
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(static_cast<hipStream_t>(hip_stream), &capture) != hipSuccess)
+        (void)hipGetLastError();
+    else if (capture != hipStreamCaptureStatusNone)
+        return report(DERF_ERR_INVALID_ARG, "the stream is being captured: a graph would repeat step %lld", step);
     AdamWScalars c;
     c.decay = (float)(1.0 - lr * weight_decay);
     c.beta1 = (float)beta1;

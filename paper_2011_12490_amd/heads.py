@@ -346,7 +346,9 @@ class AdamW:
 
     def step(self, step: Optional[int] = None, grad_scale: Optional[torch.Tensor] = None) -> None:
         """One step, number `step` (None: one more than the last).  grad_scale:
-        float32 [1] on the GPU, a factor on every gradient."""
+        float32 [1] on the GPU, a factor on every gradient.  Not while the stream
+        is being captured: a graph would repeat this step's number and rate, so it
+        raises; capture the rest of a training step and call this beside the replay."""
         if self.handle is None:
             raise ValueError("the optimizer is closed")
         if grad_scale is not None:
