@@ -102,10 +102,10 @@ def _rows(x, name, shape=None, dtype=None, device=None) -> int:
     stride, step = x.stride()
     if step != 1 and size[1] > 1:
         raise ValueError("%s: the elements of a row must lie side by side" % name)
-    if stride < size[1]:
-        if size[0] > 1:
-            raise ValueError("%s: rows overlap" % name)
+    if size[0] <= 1:  # no next row
         return size[1]
+    if stride < size[1]:
+        raise ValueError("%s: rows overlap" % name)
     return stride
 
 
