@@ -18,7 +18,8 @@ Sec. 3.2 is
 
 Argument checks and marshalling only; all work is done by libderf.so, on torch's
 current stream of the tensors' device.  Tensors are float32 or bfloat16, of any
-row stride, on one GPU; what does not fit raises ValueError before any GPU work.
+row stride (the layers': below 2^21 elements), on one GPU; what does not fit, and
+what the library itself refuses, raises ValueError before any GPU work.
 """
 from __future__ import annotations
 
@@ -44,6 +45,15 @@ class Routing(NamedTuple):
     num_heads: int
 
 
+class Refused(derf.DerfError, ValueError):
+    """Arguments that the library refuses (DERF_ERR_INVALID_ARG)."""
+
+
+def _check(status: int, name: str) -> None:
+    if status != derf.DERF_OK:
+        raise (Refused if status == derf.DERF_ERR_INVALID_ARG else derf.DerfError)(status, name)
+
+
 _entry = {}  # entry points by name
 
 
@@ -60,7 +70,7 @@ def _call(name: str, device: torch.device, *args) -> None:
         with torch.cuda.device(index):
             status = f(*args, stream)
     if status != derf.DERF_OK:
-        raise derf.DerfError(status, name)
+        _check(status, name)
 
 
 @functools.lru_cache(maxsize=256)
@@ -321,7 +331,7 @@ class AdamW:
                                               _PRECISION[p.dtype], _PRECISION[g.dtype])
         handle = ctypes.c_void_p()
         with torch.cuda.device(self.device):
-            derf._check(derf.lib().derf_adamw_create(
+            _check(derf.lib().derf_adamw_create(
                 ctypes.byref(handle), ctypes.cast(table, ctypes.c_void_p), len(self.params),
                 state_bits), "derf_adamw_create")
         self.handle = handle

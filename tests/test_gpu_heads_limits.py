@@ -1,5 +1,5 @@
 """What the training operators take and refuse at their edges: graphs that would
-repeat a step, one row of a wide buffer."""
+repeat a step, one row of a wide buffer, sizes beyond the limits."""
 import pytest
 import torch
 
@@ -64,3 +64,38 @@ def test_one_row_of_a_wide_buffer(dtype):
     weights = torch.full((1, 1), 0.5, device="cuda")
     assert torch.equal(heads.dispatch(one_row(x), r, one_row(torch.zeros_like(x))), x)
     assert torch.equal(heads.combine(one_row(x), r, weights), heads.combine(x, r, weights))
+
+
+# ---- sizes beyond the limits ----------------------------------------------------------
+
+def test_what_does_not_fit_raises_value_error():
+    z = lambda *shape, dtype=FP32: torch.zeros(shape, dtype=dtype, device="cuda")  # noqa: E731
+    ints = lambda *shape: z(*shape, dtype=torch.int32)  # noqa: E731
+    wide, many, two = 65537, 17, ints(2)
+    far = torch.empty((1 << 21) + 64, device="cuda").as_strided((2, 8), (1 << 21, 1))  # rows 2^21 apart
+    p = z(10)
+    opt = heads.AdamW([p], [z(10)])
+    pairs = heads.Routing(ints(3), ints(4), ints(2, 2), 2)
+    slots = heads.Routing(ints(3), ints(2 * many), ints(2, many), 2)
+    bad = [
+        lambda: heads.dispatch(z(2, wide), pairs), lambda: heads.combine(z(4, wide), pairs),
+        lambda: heads.combine_backward(z(2, wide), None, pairs),
+        lambda: heads.dispatch(z(2, 4), slots), lambda: heads.combine(z(2 * many, 4), slots),
+        lambda: heads.combine_backward(z(2, 4), None, slots), lambda: heads.route(ints(2, many), 2),
+        lambda: heads.linear(z(2, 8), z(257, 4, 8), None, ints(258)), lambda: heads.linear(z(2, wide), z(1, 1, wide), None, two),
+        lambda: heads.linear(z(2, 1), z(1, wide, 1), None, two), lambda: heads.linear(far, z(1, 4, 8), None, two),
+        lambda: heads.linear(z(2, 4), z(1, 8, 4), None, two, out=far),
+        lambda: heads.linear_backward(z(2, 4), z(2, 8), z(257, 4, 8), ints(258)),
+        lambda: heads.linear_backward(far, z(2, 4), z(1, 8, 4), two), lambda: heads.linear_backward(z(2, 4), far, z(1, 4, 8), two),
+        lambda: opt.step(step=0),
+    ]
+    for i, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+            pytest.fail("case %d was taken" % i)
+    for lr, betas, eps, decay in ((-1.0, (0.9, 0.99), 1e-8, 0.0), (1e-3, (1.0, 0.99), 1e-8, 0.0), (1e-3, (0.9, 0.99), float("nan"), 0.0),
+                                  (1e-3, (0.9, 0.99), 1e-8, -0.1)):
+        opt.lr, opt.betas, opt.eps, opt.weight_decay = lr, betas, eps, decay
+        with pytest.raises(ValueError):
+            opt.step()
+    assert opt.steps == 0 and not bool(p.any())
