@@ -307,8 +307,15 @@ class AdamW:
             raise ValueError("need parameters and as many gradients")
         self.lr, self.betas, self.eps, self.weight_decay = lr, tuple(betas), eps, weight_decay
         self.state_bits, self.steps = state_bits, 0
-        self.device = self.params[0].device
         self.copies = self._list(copies, "copies") if copies is not None else [None] * len(self.params)
+        for i, (p, g, c) in enumerate(zip(self.params, self.grads, self.copies)):
+            for name, x in (("params", p), ("grads", g)):
+                if not isinstance(x, torch.Tensor) or x.dtype not in _PRECISION:
+                    raise ValueError("%s[%d] must be a float32 or bfloat16 tensor" % (name, i))
+                _array(x, "%s[%d]" % (name, i), x.dtype, p.shape, self.params[0].device)
+            if c is not None:
+                _array(c, "copies[%d]" % i, torch.bfloat16, p.shape, self.params[0].device)
+        self.device = self.params[0].device
         state = torch.float32 if state_bits == 32 else torch.float8_e4m3fn
         self.m, self.v = self._state(m, "m", state), self._state(v, "v", state)
         self.m_scale = self.v_scale = None
@@ -319,12 +326,6 @@ class AdamW:
             raise ValueError("scales belong to 8-bit moments")
         table = (derf.derf_adamw_tensor * len(self.params))()
         for i, (p, g, c) in enumerate(zip(self.params, self.grads, self.copies)):
-            for name, x in (("params", p), ("grads", g)):
-                if not isinstance(x, torch.Tensor) or x.dtype not in _PRECISION:
-                    raise ValueError("%s[%d] must be a float32 or bfloat16 tensor" % (name, i))
-                _array(x, "%s[%d]" % (name, i), x.dtype, p.shape, self.device)
-            if c is not None:
-                _array(c, "copies[%d]" % i, torch.bfloat16, p.shape, self.device)
             ptr = [x.data_ptr() for x in (p, g, self.m[i], self.v[i])]
             ptr += [0, 0] if state_bits == 32 else [self.m_scale[i].data_ptr(), self.v_scale[i].data_ptr()]
             table[i] = derf.derf_adamw_tensor(*ptr, 0 if c is None else c.data_ptr(), p.numel(),
