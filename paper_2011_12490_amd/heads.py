@@ -19,7 +19,10 @@ Sec. 3.2 is
 Argument checks and marshalling only; all work is done by libderf.so, on torch's
 current stream of the tensors' device.  Tensors are float32 or bfloat16, of any
 row stride (the layers': below 2^21 elements), on one GPU; what does not fit, and
-what the library itself refuses, raises ValueError before any GPU work.
+what the library itself refuses, raises ValueError before any GPU work.  No
+autograd graph is recorded: while one is (torch.is_grad_enabled()), a tensor that
+requires a gradient is refused, but for the optimizer's, since its gradient would
+be lost.
 """
 from __future__ import annotations
 
@@ -82,8 +85,15 @@ def _ptr(x: Optional[torch.Tensor]):
     return None if x is None else x.data_ptr()
 
 
-def _array(x, name, dtype, shape, device=None) -> None:
-    """Check a contiguous GPU array of a given type and shape."""
+def _no_graph(x, name) -> None:
+    """Refuse a tensor that requires a gradient, which autograd would silently not get."""
+    if torch.is_grad_enabled():
+        raise ValueError("%s requires a gradient and autograd would not see it: detach it or call under "
+                         "torch.no_grad()" % name)
+
+
+def _array(x, name, dtype, shape, device=None, leaf=False) -> None:
+    """Check a contiguous GPU array of a given type and shape; leaf: autograd may follow it."""
     if not isinstance(x, torch.Tensor):
         raise ValueError("%s must be a torch tensor" % name)
     if not x.is_cuda or (device is not None and x.device != device):
@@ -94,6 +104,8 @@ def _array(x, name, dtype, shape, device=None) -> None:
         raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(x.shape)))
     if not x.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
+    if x.requires_grad and not leaf:
+        _no_graph(x, name)
 
 
 def _rows(x, name, shape=None, dtype=None, device=None) -> int:
@@ -112,6 +124,8 @@ def _rows(x, name, shape=None, dtype=None, device=None) -> int:
     stride, step = x.stride()
     if step != 1 and size[1] > 1:
         raise ValueError("%s: the elements of a row must lie side by side" % name)
+    if x.requires_grad:
+        _no_graph(x, name)
     if size[0] <= 1:  # no next row
         return size[1]
     if stride < size[1]:
@@ -312,9 +326,9 @@ class AdamW:
             for name, x in (("params", p), ("grads", g)):
                 if not isinstance(x, torch.Tensor) or x.dtype not in _PRECISION:
                     raise ValueError("%s[%d] must be a float32 or bfloat16 tensor" % (name, i))
-                _array(x, "%s[%d]" % (name, i), x.dtype, p.shape, self.params[0].device)
+                _array(x, "%s[%d]" % (name, i), x.dtype, p.shape, self.params[0].device, leaf=True)
             if c is not None:
-                _array(c, "copies[%d]" % i, torch.bfloat16, p.shape, self.params[0].device)
+                _array(c, "copies[%d]" % i, torch.bfloat16, p.shape, self.params[0].device, leaf=True)
         self.device = self.params[0].device
         state = torch.float32 if state_bits == 32 else torch.float8_e4m3fn
         self.m, self.v = self._state(m, "m", state), self._state(v, "v", state)
@@ -350,7 +364,7 @@ class AdamW:
                                 device=self.device).view(dtype) for n in counts]
         given = self._list(given, name)
         for i, (x, n) in enumerate(zip(given, counts)):
-            _array(x, "%s[%d]" % (name, i), dtype, (n,) if block > 1 else getattr(x, "shape", ()), self.device)
+            _array(x, "%s[%d]" % (name, i), dtype, (n,) if block > 1 else getattr(x, "shape", ()), self.device, leaf=True)
             if x.numel() != n:
                 raise ValueError("%s[%d] holds %d values, %d needed" % (name, i, x.numel(), n))
         return given
@@ -363,7 +377,7 @@ class AdamW:
         if self.handle is None:
             raise ValueError("the optimizer is closed")
         if grad_scale is not None:
-            _array(grad_scale, "grad_scale", torch.float32, (1,), self.device)
+            _array(grad_scale, "grad_scale", torch.float32, (1,), self.device, leaf=True)
         step = self.steps + 1 if step is None else int(step)
         _call("derf_adamw_step", self.device, self.handle, self.lr, self.betas[0], self.betas[1],
               self.eps, self.weight_decay, step, _ptr(grad_scale))

@@ -1,5 +1,6 @@
 """What the training operators take and refuse at their edges: graphs that would
-repeat a step, one row of a wide buffer, sizes beyond the limits."""
+repeat a step, one row of a wide buffer, sizes beyond the limits, tensors that
+autograd follows."""
 import pytest
 import torch
 
@@ -99,3 +100,33 @@ def test_what_does_not_fit_raises_value_error():
         with pytest.raises(ValueError):
             opt.step()
     assert opt.steps == 0 and not bool(p.any())
+
+
+# ---- autograd ---------------------------------------------------------------------------
+
+def test_tensors_that_autograd_follows():
+    """No graph is recorded, so a tensor that requires a gradient is refused where one
+    would be expected; without autograd, and in the optimizer, it is as any other."""
+    g = gen(2)
+    x, w, b, offsets, _ = layer([3, 2], 0, 8, 6, 0, 0, FP32, 3)
+    dy, dout, weights = rand(g, 5, 6), rand(g, 5, 8), rand(g, 5, 1)
+    r = heads.route(torch.zeros((5, 1), dtype=torch.int32, device="cuda"), 2)
+    leaf = lambda t: t.clone().requires_grad_()  # noqa: E731
+    calls = [lambda f: heads.linear(f(x), w, b, offsets), lambda f: heads.linear(x, f(w), b, offsets),
+             lambda f: heads.linear(x, w, f(b), offsets), lambda f: heads.linear_backward(f(dy), x, w, offsets)[0],
+             lambda f: heads.linear_backward(dy, x, f(w), offsets)[0], lambda f: heads.dispatch(f(x), r),
+             lambda f: heads.combine(f(x), r, weights), lambda f: heads.combine(x, r, f(weights)),
+             lambda f: heads.combine_backward(f(dout), x, r, weights)[0],
+             lambda f: heads.combine_backward(dout, f(x), r, weights)[1], lambda f: heads.dispatch_backward(f(x), r)]
+    for i, call in enumerate(calls):
+        with pytest.raises(ValueError, match="autograd"):
+            call(leaf)
+            pytest.fail("case %d was taken" % i)
+        with torch.no_grad():
+            got = call(leaf)
+        assert torch.equal(got, call(lambda t: t)), i
+        assert torch.equal(call(lambda t: leaf(t).detach()), got), i
+    p, q = torch.nn.Parameter(x.clone()), x.clone()
+    for v in (p, q):
+        heads.AdamW([v], [dout]).step(grad_scale=leaf(torch.ones(1, device="cuda")))
+    assert torch.equal(p, q) and p.requires_grad
