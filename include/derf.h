@@ -389,9 +389,9 @@ int derf_reset_stats(derf_handle *h);
  * the results come back weighted, and AdamW updates the weights.
  *
  * These calls take no handle (but for the optimizer's).  All arrays are device
- * memory of the current device unless they are called host; work is enqueued on
- * hip_stream (a hipStream_t, NULL: the default stream) and the calls return
- * without waiting.  They allocate nothing, run nothing on other streams and may
+ * memory of the current device (the optimizer's: of its own) unless they are called
+ * host; work is enqueued on hip_stream (a hipStream_t, NULL: the default stream) and
+ * the calls return without waiting.  They allocate nothing, run nothing on other streams and may
  * be captured into HIP graphs (not so the optimizer: derf_adamw_create allocates and
  * waits, derf_adamw_step refuses a capturing stream, derf_adamw_destroy waits).  A
  * workspace belongs to the caller, holds nothing between calls, and is 16-byte
@@ -512,6 +512,8 @@ typedef struct {
 } derf_adamw_tensor;
 typedef struct derf_adamw derf_adamw;
 /* tensors: host [num_tensors] (copied to the device; the call synchronises it).
+ * The optimizer belongs to the device that is current now: its steps and its end
+ * run there and leave the current device as it is.
  * The optimizer keeps the addresses, not the memory: every tensor stays valid
  * until derf_adamw_destroy, gradients are written to the same place each step.
  * num_tensors <= 65536, their sum of n < 2^40. */
@@ -524,7 +526,7 @@ int derf_adamw_create(derf_adamw **out, const derf_adamw_tensor *tensors, int nu
 int derf_adamw_step(derf_adamw *opt, double lr, double beta1, double beta2, double eps,
                     double weight_decay, long long step, const float *grad_scale,
                     void *hip_stream);
-/* Waits for the device, then frees the table.  NULL is a no-op. */
+/* Waits for the optimizer's device, then frees the table.  NULL is a no-op. */
 void derf_adamw_destroy(derf_adamw *opt);
 
 /* Waits for the handle's last stream, then frees everything.  NULL is a no-op. */

@@ -98,6 +98,23 @@ int check_workspace(const void *p, long long have, long long need)
     return DERF_OK;
 }
 
+// Makes a device the current one, and the one before again at its end.
+struct OnDevice {
+    int device, before = -1;
+    hipError_t status;
+    explicit OnDevice(int device_) : device(device_)
+    {
+        status = hipGetDevice(&before);
+        if (status == hipSuccess && before != device)
+            status = hipSetDevice(device);
+    }
+    ~OnDevice()
+    {
+        if (before >= 0 && before != device)
+            (void)hipSetDevice(before);
+    }
+};
+
 #define TRY(expr)                  \
     do {                           \
         const int rc_ = (expr);    \
@@ -108,7 +125,8 @@ int check_workspace(const void *p, long long have, long long need)
 }  // namespace
 
 struct derf_adamw {
-    AdamWEntry *table = nullptr;  // device
+    AdamWEntry *table = nullptr;  // device memory
+    int device = -1;              // of the table
     int tensors = 0;
     int state_bits = 32;
     unsigned items = 0;
@@ -319,7 +337,12 @@ int derf_adamw_create(derf_adamw **out, const derf_adamw_tensor *tensors, int nu
         opt->items = (unsigned)items;
         if (!table.empty()) {
             const size_t bytes = table.size() * sizeof(AdamWEntry);
-            hipError_t e = device_alloc(reinterpret_cast<void **>(&opt->table), bytes);
+            hipError_t e = hipGetDevice(&opt->device);
+            if (e != hipSuccess) {
+                delete opt;
+                return report(DERF_ERR_HIP, "hipGetDevice: %s", hipGetErrorString(e));
+            }
+            e = device_alloc(reinterpret_cast<void **>(&opt->table), bytes);
             if (e != hipSuccess) {
                 (void)hipGetLastError();
                 delete opt;
@@ -356,6 +379,9 @@ int derf_adamw_step(derf_adamw *opt, double lr, double beta1, double beta2, doub
         return report(DERF_ERR_INVALID_ARG, "grad_scale is not aligned to its elements");
     if (opt->items == 0)
         return DERF_OK;
+    const OnDevice on(opt->device);
+    if (on.status != hipSuccess)
+        return launched(on.status, "the optimizer's device");
     // Step number and rates go into the launch, which a graph would repeat as it is.  Where
     // the runtime does not tell (another stream's capture), the launch says what is wrong.
     hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
@@ -381,9 +407,11 @@ void derf_adamw_destroy(derf_adamw *opt)
 {
     if (!opt)
         return;
-    if (opt->table)
+    if (opt->table) {
+        const OnDevice on(opt->device);
         (void)hipDeviceSynchronize();
-    (void)device_free(opt->table);
+        (void)device_free(opt->table);
+    }
     delete opt;
 }
 

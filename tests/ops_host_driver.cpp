@@ -13,6 +13,7 @@
 namespace {
 
 int current = 0;                                                     // device
+int waited_for = -1, freed_on = -1, launched_on = -1;                // the device that was current
 hipStreamCaptureStatus capture_status = hipStreamCaptureStatusNone;  // of every stream
 hipError_t capture_query = hipSuccess;
 int launches = 0;
@@ -43,7 +44,11 @@ hipError_t hipSetDevice(int device)
     current = device;
     return hipSuccess;
 }
-hipError_t hipDeviceSynchronize(void) { return hipSuccess; }
+hipError_t hipDeviceSynchronize(void)
+{
+    waited_for = current;
+    return hipSuccess;
+}
 hipError_t hipMemcpy(void *to, const void *from, size_t bytes, hipMemcpyKind)
 {
     memcpy(to, from, bytes);
@@ -77,6 +82,7 @@ hipError_t device_alloc(void **p, size_t bytes)
 }
 hipError_t device_free(void *p)
 {
+    freed_on = current;
     free(p);
     return hipSuccess;
 }
@@ -85,6 +91,7 @@ unsigned adamw_items(long long n) { return (unsigned)((n + 4095) / 4096); }
 hipError_t launch_adamw(const AdamWEntry *, int, unsigned, int, const AdamWScalars &, const float *, hipStream_t)
 {
     ++launches;
+    launched_on = current;
     return hipSuccess;
 }
 
@@ -151,11 +158,28 @@ void capture()
     derf_adamw_destroy(opt);
 }
 
+// An optimizer works on the device that it was made on, whichever is current, and
+// leaves the current one as it was.
+void devices()
+{
+    current = 1;
+    derf_adamw *opt = optimizer();
+    current = 0;
+    launched_on = waited_for = freed_on = -1;
+    expect(step(opt) == DERF_OK && launched_on == 1, "a step runs on the optimizer's device");
+    expect(current == 0, "a step leaves the current device");
+    derf_adamw_destroy(opt);
+    expect(waited_for == 1, "destroy waits for the optimizer's device");
+    expect(freed_on == 1, "destroy frees there");
+    expect(current == 0, "destroy leaves the current device");
+}
+
 }  // namespace
 
 int main()
 {
     capture();
+    devices();
     printf("ops host driver: %d failure(s)\n", failures);
     return failures != 0;
 }
