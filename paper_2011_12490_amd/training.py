@@ -160,8 +160,9 @@ class HeadTrainer:
         return torch.cat(parts, dim=1).cpu().numpy()
 
     def renderer(self) -> derf.Renderer:
-        """A renderer of the heads as they are."""
-        return derf.Renderer(self.host_sites, self.arch, self.packed(), self.precision)
+        """A renderer of the heads as they are, on the trainer's device."""
+        with torch.cuda.device(self.device):
+            return derf.Renderer(self.host_sites, self.arch, self.packed(), self.precision)
 
 
 def start_weights(num_heads: int, arch: scenes.HeadArch, seed: int) -> np.ndarray:

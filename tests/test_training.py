@@ -37,3 +37,26 @@ def test_trainer_refusals():
     for kw in (dict(precision="fp16"), dict(top_k=0), dict(top_k=4)):
         with pytest.raises(ValueError):
             training.HeadTrainer(np.zeros((3, 3)), scenes.ARCH_TINY, w, device="cpu", **kw)
+
+
+def test_renderer_is_made_on_the_trainers_device(monkeypatch):
+    """derf.Renderer binds to the current device, which need not be the trainer's."""
+    current, seen = ["another"], []
+
+    class Device:
+        def __init__(self, device):
+            self.device = device
+
+        def __enter__(self):
+            self.before, current[0] = current[0], self.device
+
+        def __exit__(self, *_):
+            current[0] = self.before
+
+    monkeypatch.setattr(torch.cuda, "device", Device)
+    monkeypatch.setattr(training.derf, "Renderer", lambda *args: seen.append((current[0],) + args[3:]))
+    t = object.__new__(training.HeadTrainer)
+    t.device, t.host_sites, t.arch, t.precision = torch.device("cuda:1"), None, None, "fp32"
+    t.packed = lambda: None
+    t.renderer()
+    assert seen == [(torch.device("cuda:1"), "fp32")] and current == ["another"]
