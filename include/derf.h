@@ -391,12 +391,13 @@ int derf_reset_stats(derf_handle *h);
  * These calls take no handle (but for the optimizer's).  All arrays are device
  * memory of the current device (the optimizer's: of its own) unless they are called
  * host; work is enqueued on hip_stream (a hipStream_t, NULL: the default stream) and
- * the calls return without waiting.  They allocate nothing, run nothing on other streams and may
- * be captured into HIP graphs (not so the optimizer: derf_adamw_create allocates and
- * waits, derf_adamw_step refuses a capturing stream, derf_adamw_destroy waits).  A
- * workspace belongs to the caller, holds nothing between calls, and is 16-byte
- * aligned.  Results do not depend on the run:
- * every sum has a fixed order.
+ * the calls return without waiting.  They allocate nothing, run nothing on other
+ * streams and may be captured into HIP graphs (not so the optimizer:
+ * derf_adamw_create allocates and waits, derf_adamw_step refuses a capturing stream,
+ * derf_adamw_destroy waits).  A workspace belongs to the caller, holds nothing between
+ * calls, and is 16-byte aligned.  Outputs overlap neither inputs nor each other (the
+ * optimizer's arrays are updated in place).  Results do not depend on the run: every
+ * sum has a fixed order.
  *   precision    a derf_precision: the type of the rows (float or bf16)
  *   *_stride     elements from a row to the next, >= the row length; rows need
  *                the alignment of their type only (rows and strides that are

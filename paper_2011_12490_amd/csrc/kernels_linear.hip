@@ -99,8 +99,11 @@ __device__ __forceinline__ RowTile head_tile(const Problem &p, const unsigned *b
 // Number b, in the order in which they are taken, of `all` tiles: consecutive
 // workgroups go to the 8 XCDs in turn; each XCD gets runs of up to 32 tiles (its
 // compute units), neighbours that share operands in its L2, and short ones where
-// there are few tiles, so that none gets much more than another.  Some b beyond
-// `all` give tiles too, and some below none; none from runs_end(all) on does.
+// there are few tiles, so that none gets much more than another.  us with runs of 32
+// and of 1: bf16 256 to 256 on 262,144 rows 68, 73, both gradients 130, 163; gradients
+// of 2,048 to 4,096 on 16,384 498, 511, the layer on 32,768 489, 480 (of 128: 461);
+// float32 319 to 640 on 65,536 272, 282 (of 128: 290).  Some b beyond `all` give tiles
+// too, and some below none; none from runs_end(all) on does.
 constexpr unsigned kXcds = 8, kRun = 32;
 __device__ __forceinline__ unsigned run_of(unsigned all)
 {
@@ -767,10 +770,10 @@ constexpr int kJoinBytes = (C::kTeams - 1) * C::FP * C::FQ * C::kTeam * 16;
 // ---- rows: the layer, and its rows' gradient --------------------------------------
 
 // A wave's results as rows of 16 FP elements: lane 16 h + l has, of row 16 j + l
-// of Q, elements 4 h + (0 .. 3) of each 16 of P.  They go through LDS, 16 rows at
-// a time, to be written in 16-byte pieces.  Bytes of a row there (4 of 64 banks
-// further on for the next row):
-// (float results are written from the registers, 16 bytes a lane.)
+// of Q, elements 4 h + (0 .. 3) of each 16 of P.  float results are written from the
+// registers, 16 bytes a lane.  bf16 ones go through LDS, 16 rows at a time, to be
+// written in 16-byte pieces; kResultRow: bytes of a row there (4 of 64 banks further
+// on for the next row).
 template <class C>
 constexpr int kResultRow = C::FP * 16 * (int)sizeof(typename C::T) + 16;
 template <class C>
@@ -808,9 +811,10 @@ __device__ __forceinline__ void write_piece(T *to, u32x4 v, int left, T)
 }
 
 // Whether results go past the caches (nontemporal): their rows are whole 128-byte
-// lines.  bf16 us so and with ordinary stores: 2,048 to 4,096 on 32,768 rows 482, 513;
-// 256 to 256 on 262,144 63, 72; 319 to 256 on 262,139 94, 108; but rows of 319, whose
-// lines are shared, 280, 270.
+// lines.  bf16 us so and with ordinary stores: 2,048 to 4,096 on 32,768 rows 468, 521;
+// 256 to 256 on 262,139 67, 76, its dx alone 62, 71; 319 to 256 83, 103.  Rows that
+// share lines: both gradients of 319 to 256 252 either way, with ReLU 319, 318, though
+// dx alone would take 124 instead of 147 and a layer of 256 to 319 97 instead of 118.
 template <class T>
 __host__ __device__ __forceinline__ bool past_caches(const T *y, long long ys, int width)
 {
@@ -1065,9 +1069,8 @@ __device__ __forceinline__ void write_weights(float *to, int m0, int n0, int O, 
 // P: x, Q: dz, reduced over rows: a tile of a head's dW from a stretch of
 // `stretch` of its rows.  Where heads have more than one stretch (partial),
 // each has a place of its own in dw and db, and sum_kernel adds them up.  db comes from
-// the dz tiles on their way, no pass of its own.  2,048 to 4,096 on 32,768 rows of bf16,
-// with dx by rows_kernel: 940 us, 1,170 TFLOP/s, bound by the matrix units' power
-// (zeros 815).
+// the dz tiles on their way, no pass of its own.  dW and db of 2,048 to 4,096 on 32,768
+// rows of bf16: 499 us, 1,100 TFLOP/s, bound by the matrix units' power.
 template <class C>
 __global__ __launch_bounds__(C::kThreads, 2) void weights_kernel(Problem p, Matrix<typename C::T> dz,
                                                                  Matrix<typename C::T> x, float *dw,
@@ -1427,7 +1430,8 @@ __global__ __launch_bounds__(CR::kThreads, 2) void gradients_kernel(Problem p, M
 // lies in LDS once: dx reads it by rows, dW by columns.  128 to 128 with ReLU on
 // 131,072 rows of bf16: 45 us, 66 with a pass for each gradient.
 // float's products take about as long as its rows: two workgroups of half the
-// waves and rows a compute unit, where their weights fit, compute in turns.
+// waves and rows a compute unit, where their weights fit, compute in turns.  63 to 128
+// with ReLU, us so and with one: 262,144 rows 109, 120, 65,536 41, 43, 32,768 34, 31.
 template <class T_, int TI_, int TO_, bool MASK>
 struct Narrow {
     using T = T_;
@@ -1730,7 +1734,7 @@ hipError_t launch_rows(const Problem &p, const Matrix<typename C::T> &w,
                          });
 }
 
-// Whether an operand can go from memory to LDS by itself (Tile::load_async).
+// Whether an operand can go from memory to LDS by itself (Tile::Feed).
 template <class T>
 bool goes_alone(const Matrix<T> &m)
 {
@@ -1786,7 +1790,9 @@ hipError_t shallow(const Problem &p, const Matrix<T> &w, const Matrix<T> &x, con
 }
 
 // 128 columns a tile, or 64: for narrow matrices, and for float, which is bound by
-// its products, where 128 would pad more than a seventh.
+// its products, where 128 would pad a seventh or more.  float32 us with 64 and 128, 20,000
+// rows: 400 to 155 38, 58; 319 to 400 67, 97; dx of 400 to 319 64, 79; but 400 to 319 71,
+// 60 and 400 to 283 71, 60.
 template <class T>
 bool wide_tile(int width)
 {
@@ -1797,7 +1803,14 @@ bool wide_tile(int width)
 // for each 128 columns), on rows for all of the chip, and shallow: up to 2 steps,
 // or 5 for a layer, but not where bf16 operands of more than two go to LDS by
 // themselves (262,144 rows of 256 to 256: 72 us, 80 here; their gradients with
-// ReLU take 220 us, 227 with dx here).
+// ReLU take 220 us, 227 with dx here).  us here and by tiles (of few rows below 32,768):
+//   rows   bf16 319 to 256, 8,192 to 262,144: 10, 12; 12, 15 (16,384); 16, 23 (32,768);
+//          85, 102; 63 to 64 8.2, 8.9 (16,384); 13, 20; float32 63 to 128 10, 13 (16,384);
+//          13, 19 (32,768); 56, 75; 128 to 128 92, 92; dx of 256 to 64 109, 114
+//   width  bf16 on 65,536, 100 to 512 22, 35; to 768 30, 49; to 1,024 41, 63; float32
+//          100 to 512 111, 93; 128 to 768 194, 133
+// So bf16 would gain on fewer rows and beyond 512 columns; float32 loses at 512 on more
+// than 32,768 rows (57, 56 there).
 template <class T, bool DEEP_W>
 bool is_shallow(const Problem &p, const Matrix<T> &w, const Matrix<T> &x, int width, int depth)
 {
@@ -1907,6 +1920,11 @@ hipError_t launch_weights(const Problem &p, const Matrix<typename C::T> &dz,
     return partial ? launch_sums(p, split, wparts, dw, bparts, db, s) : hipSuccess;
 }
 
+// 256 x 256 tiles from 256 of them on, one a compute unit.  dW and db, us with large and
+// small tiles: 2,048 to 4,096 on 32,768 rows of 8 heads (1,024 tiles) 499, 612; 1,024 to
+// 1,024 on 16,384 of 8 (128) 115, 70; 512 to 512 on 65,536 of 16 (64) 111, 80; at the line
+// small ones would win: 1,024 to 2,048 on 16,384 of 8 119, 101; 1,024 to 1,024 on 65,536 of
+// 16 387, 271.
 template <class T, bool MASK>
 hipError_t weights_product(const Problem &p, const Matrix<T> &dz, const Matrix<T> &x, float *dw,
                            float *db, char *workspace, hipStream_t s)
@@ -1953,7 +1971,10 @@ bool mask_apart(int fan_in, int fan_out, bool bf16)
 }
 
 // Layers that narrow_kernel takes, and its stretches: a workgroup for each, as
-// many as run at once.
+// many as run at once.  us with half as many, with these, and with twice as many, 16
+// heads with ReLU: bf16 128 to 128 on 65,536 rows 33, 29, 39, on 262,144 85, 57, 70; 64 to
+// 64 on 131,072 28, 23, 23; float32 63 to 128 on 131,072 69, 62, 75, on 32,768 29, 34, 34;
+// 128 to 128 on 131,072 189, 107, 128.
 bool is_narrow(int fan_in, int fan_out) { return fan_in <= 128 && fan_out <= 128; }
 Split narrow_split(unsigned rows, int heads, int fan_in, int fan_out, bool bf16)
 {
@@ -2005,8 +2026,12 @@ hipError_t launch_gradients(const Problem &p, const Matrix<typename CR::T> &w, c
     return hipGetLastError();
 }
 
-// Whether both gradients go in one launch: where each of them has a few rounds
-// of tiles, so that filling up the last ones matters, and heads as a whole.
+// Whether both gradients go in one launch: where they have two rounds of tiles, so that
+// filling up the last one matters, and heads as a whole.  us in one and in two launches,
+// 8 heads: 1,024 to 2,048 on 16,384 rows (512 tiles) 131, 177; 1,024 to 1,024 on 32,768
+// (640) 164, 180, on 16,384 (384) 106, 103; 512 to 1,024 on 16,384 (192) 86, 84; 16 heads:
+// 512 to 1,024 on 32,768 (384) 95, 102.  Where heads would be split: 512 to 512 on 262,144
+// rows of 16 915, 474; 256 to 512 on 131,072 531, 117.
 bool gradients_together(const Problem &p)
 {
     const unsigned long long x_tiles = p.rows / 256ull * tiles_of(p.fan_in, 256);

@@ -19,10 +19,10 @@ Sec. 3.2 is
 Argument checks and marshalling only; all work is done by libderf.so, on torch's
 current stream of the tensors' device.  Tensors are float32 or bfloat16, of any
 row stride (the layers': below 2^21 elements), on one GPU; what does not fit, and
-what the library itself refuses, raises ValueError before any GPU work.  No
-autograd graph is recorded: while one is (torch.is_grad_enabled()), a tensor that
-requires a gradient is refused, but for the optimizer's, since its gradient would
-be lost.
+what the library itself refuses, raises ValueError before any GPU work.  An out=
+tensor shares no memory with the call's other tensors.  No autograd graph is
+recorded: while autograd records (torch.is_grad_enabled()), a tensor that requires a
+gradient is refused, but for the optimizer's, since its gradient would be lost.
 """
 from __future__ import annotations
 
