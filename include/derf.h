@@ -479,6 +479,46 @@ int derf_heads_linear_backward(const void *dy, long long dy_stride, const void *
                                long long out_x_stride, float *out_w, float *out_bias,
                                void *workspace, long long workspace_bytes, void *hip_stream);
 
+/* A gated layer of every head on its rows: with the gates g = Wg_h x[r] + bg_h and the
+ * ups u = Wu_h x[r] + bu_h, y[r] = act(g) * u for r in [offsets[h], offsets[h + 1]),
+ * zero for rows from offsets[num_heads] on.
+ *   w        [num_heads][2][fan_out][fan_in] of the rows' type: Wg, then Wu; contiguous
+ *   bias     float [num_heads][2][fan_out], or NULL
+ *   act      a derf_activation
+ *   pre      [num_rows][2 * fan_out] of the rows' type, or NULL: g, then u of each row,
+ *            which the gradients need (zero for rows without a head)
+ * Limits as for derf_heads_linear, and a head's w below 2^31 bytes. */
+enum derf_activation {
+    DERF_ACT_SILU = 0,    /* g / (1 + exp(-g))                            */
+    DERF_ACT_GELU = 1,    /* g Phi(g), Phi the normal distribution's      */
+    DERF_ACT_RELU = 2,    /* max(g, 0), a NaN stays NaN                   */
+    DERF_ACT_SIGMOID = 3  /* 1 / (1 + exp(-g))                            */
+};
+int derf_heads_gated(const void *x, long long x_stride, const void *w, const float *bias,
+                     const int *offsets, long long num_rows, int num_heads, int fan_in,
+                     int fan_out, int act, int precision, void *y, long long y_stride, void *pre,
+                     long long pre_stride, void *hip_stream);
+
+/* Gradients of derf_heads_gated at the gates and ups that it kept.  With
+ * dg = dy u act'(g) and du = dy act(g) (taken in fp32, rounded to the rows' type once,
+ * for the products; the biases' sums take them unrounded):
+ *   out_x     dx[r] = Wg_h^T dg[r] + Wu_h^T du[r]; zero for rows from
+ *             offsets[num_heads] on
+ *   out_w     [num_heads][2][fan_out][fan_in] of the rows' type: sum_r dg[r] x[r]^T, then
+ *             sum_r du[r] x[r]^T, summed in fp32
+ *   out_bias  float [num_heads][2][fan_out]: sum_r dg[r], then sum_r du[r]
+ * Heads without rows get zeros.  act' of a ReLU is 0 at 0.  Any of the three outputs may
+ * be NULL (then what only it needs may be NULL too: w for out_x, x for out_w).
+ *   workspace  derf_heads_gated_workspace(...) bytes (-1 for invalid sizes) */
+long long derf_heads_gated_workspace(long long num_rows, int num_heads, int fan_in, int fan_out,
+                                     int precision);
+int derf_heads_gated_backward(const void *dy, long long dy_stride, const void *pre,
+                              long long pre_stride, const void *x, long long x_stride,
+                              const void *w, const int *offsets, long long num_rows,
+                              int num_heads, int fan_in, int fan_out, int act, int precision,
+                              void *out_x, long long out_x_stride, void *out_w, float *out_bias,
+                              void *workspace, long long workspace_bytes, void *hip_stream);
+
 /* AdamW over many tensors in one launch (the heads are trained with a
  * first-order optimizer, Sec. 3.4).  Per value, with g = *grad_scale * grad:
  *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,

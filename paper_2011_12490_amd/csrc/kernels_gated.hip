@@ -1,0 +1,55 @@
+// The heads' gated layers: y[r][o] = act(g) u with the gates and ups
+//
+//   g = sum_i x[r][i] Wg[o][i] + bg[o],   u = sum_i x[r][i] Wu[o][i] + bu[o]
+//
+// The layer of kernels_linear.hip with both weights in one matrix of 2 fan_out rows:
+// a tile takes 16 rows of Wg and the 16 of Wu that belong to them in turn, so a lane
+// holds a gate and its up in the same place of two results, and the activation and the
+// product are taken on the way out of the registers.  x is read once for both.
+#include "layers.h"
+
+namespace derf {
+
+namespace {
+
+// The forms of a layer of 2 fan_out outputs (rows_product), with tiles of pairs.
+template <class T>
+hipError_t gated(const LinearShape &sh, Rows x, const void *w, const float *bias, int act, Rows y, Rows pre, hipStream_t s)
+{
+    const Problem p = {sh.offsets, sh.rows, sh.heads, sh.fan_in, sh.fan_out};
+    const int O = sh.fan_out, depth = sh.fan_in;
+    const Matrix<T> mw = {static_cast<const T *>(w), depth, nullptr, 0, 2 * (unsigned)O, depth};
+    const Matrix<T> mx = {static_cast<const T *>(x.p), x.stride, nullptr, 0, sh.rows, depth};
+    if (is_shallow<T, true>(p, mw, mx, 2 * O, depth)) {
+        if (O <= 32)
+            return shallow<T, 64, true, false, false, true>(p, mw, mx, bias, act, y, O, s, pre);
+        return shallow<T, 128, true, false, false, true>(p, mw, mx, bias, act, y, O, s, pre);
+    }
+    if (few_rows<T>(p, 2 * O, depth))
+        return launch_rows<Product<T, 64, 32, 2, 1, true, true, false, false, false, 4, true>>(p, mw, mx, bias, act, y, O, depth,
+                                                                                            s, pre);
+    const bool alone = goes_alone(mw) && goes_alone(mx);
+    if constexpr (sizeof(T) == 2)
+        if (alone && depth >= 512 && large_tiles(p, 2 * O))
+            return launch_rows<Product<T, 256, 256, 2, 4, true, true, false, true, false, 1, true>>(p, mw, mx, bias, act, y, O,
+                                                                                                 depth, s, pre);
+    if (wide_tile<T>(2 * O)) {
+        if (alone)
+            return launch_rows<Product<T, 128, 128, 2, 2, true, true, false, true, false, 1, true>>(p, mw, mx, bias, act, y, O,
+                                                                                                 depth, s, pre);
+        return launch_rows<Product<T, 128, 128, 2, 2, true, true, false, false, false, 1, true>>(p, mw, mx, bias, act, y, O,
+                                                                                              depth, s, pre);
+    }
+    return launch_rows<Product<T, 64, 128, 2, 2, true, true, false, false, false, 1, true>>(p, mw, mx, bias, act, y, O, depth, s,
+                                                                                         pre);
+}
+
+}  // namespace
+
+hipError_t launch_heads_gated(const LinearShape &sh, Rows x, const void *w, const float *bias, int act, bool bf16, Rows y,
+                              Rows pre, hipStream_t s)
+{
+    return bf16 ? gated<__bf16>(sh, x, w, bias, act, y, pre, s) : gated<float>(sh, x, w, bias, act, y, pre, s);
+}
+
+}  // namespace derf

@@ -108,12 +108,8 @@ hipError_t launch_heads_linear(const LinearShape &sh, Rows x, const void *w, con
 
 size_t heads_linear_workspace_bytes(unsigned rows, int heads, int fan_in, int fan_out, bool relu, bool bf16)
 {
-    const Split split = split_rows(rows, heads, fan_in, fan_out, bf16), narrow = narrow_split(rows, heads, fan_in, fan_out, bf16);
-    size_t places = split.stretch ? split.places : 0;
-    if (is_narrow(fan_in, fan_out) && narrow.places > places)
-        places = narrow.places;
     return (relu && mask_apart(fan_in, fan_out, bf16) ? masked_bytes(rows, fan_out) : 0) +
-           places * fan_out * ((size_t)fan_in + 1) * sizeof(float);
+           parts_bytes(rows, heads, fan_in, fan_out, bf16);
 }
 
 hipError_t launch_heads_linear_backward(const LinearShape &sh, Rows dy, Rows x, const void *w,

@@ -4,6 +4,8 @@
 #pragma once
 #include "product.h"
 
+#include <type_traits>
+
 namespace derf {
 
 namespace {
@@ -61,18 +63,142 @@ __device__ __forceinline__ void write_rows(const RowTile &t, int n0, int width, 
     }
 }
 
+// ---- gated layers: their result ---------------------------------------------------
+
+// act(g) and, for the gradient, its slope.  bf16 rows take the exponential and the
+// reciprocal of the hardware (a unit in the last place of float each, and the
+// exponent's rounding, 2^-24 |g| of the value): far below bf16's half step of 2^-9.
+__device__ __forceinline__ float exp_of(float x, float) { return expf(x); }
+__device__ __forceinline__ float exp_of(float x, __bf16) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+__device__ __forceinline__ float logistic(float g, float) { return 1.0f / (1.0f + expf(-g)); }
+__device__ __forceinline__ float logistic(float g, __bf16 t) { return __builtin_amdgcn_rcpf(1.0f + exp_of(-g, t)); }
+__device__ __forceinline__ float below(float g) { return 0.5f * erfcf(g * -0.70710678f); }  // of the normal distribution
+template <class T>
+__device__ __forceinline__ f32x4 activate(f32x4 g, int act)
+{
+    f32x4 v;
+    if (act == DERF_ACT_RELU) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            v[k] = g[k] < 0.0f ? 0.0f : g[k];
+    } else if (act == DERF_ACT_GELU) {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            v[k] = g[k] * below(g[k]);
+    } else {
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            v[k] = logistic(g[k], T{});
+        if (act == DERF_ACT_SILU)
+            v = v * g;
+    }
+    return v;
+}
+
+// 16 rows from row0 on of a wave's COLS results from column n0 on, below `last` and
+// `width`: lane 16 h + l has, of row l, columns 4 h + (0 .. 3) of each 16.  bf16 through
+// the wave's place in LDS (kPieceRow a row), for pieces of 16 bytes.
+template <class T, int COLS>
+constexpr int kPieceRow = sizeof(T) == 2 ? COLS * 2 + 16 : 1;
+template <class T, int COLS>
+__device__ __forceinline__ void write_16_rows(const f32x4 (&v)[COLS / 16], char *mine, unsigned row0, unsigned last, int n0,
+                                              int width, T *y, long long ys)
+{
+    constexpr int V = Type<T>::kVec, kPieces = COLS / V;  // of a row
+    const int lane = threadIdx.x & 63;
+    if constexpr (sizeof(T) == 4) {
+        const unsigned row = row0 + (lane & 15);
+#pragma unroll
+        for (int i = 0; i < COLS / 16; ++i) {
+            const int n = n0 + i * 16 + (lane >> 4) * 4;
+            if (row < last && n < width)
+                write_piece(y + (row * ys + n), __builtin_bit_cast(u32x4, v[i]), width - n, T{});
+        }
+        return;
+    }
+    const bool past = COLS * sizeof(T) >= 128 && past_caches(y, ys, width);
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < COLS / 16; ++i)
+        store_values(mine + (lane & 15) * kPieceRow<T, COLS> + (i * 16 + (lane >> 4) * 4) * (int)sizeof(T), v[i], T{});
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < (16 * kPieces + 63) / 64; ++i) {
+        const int r = (i * 64 + lane) / kPieces, c = (i * 64 + lane) % kPieces * V;
+        if (16 * kPieces % 64 && r >= 16)
+            continue;
+        const u32x4 piece = *reinterpret_cast<const u32x4 *>(mine + r * kPieceRow<T, COLS> + c * (int)sizeof(T));
+        const unsigned row = row0 + r;
+        const int n = n0 + c;
+        if (row < last && n < width)
+            write_result(y + (row * ys + n), piece, width - n, past);
+    }
+    __builtin_amdgcn_wave_barrier();
+}
+
+// Of 16 rows: gates in the even results of acc, ups in the odd ones.  y = act(gate) up,
+// and, where `pre` is wanted, both as they are, the ups `width` columns behind the gates.
+template <class T, int PAIRS>
+__device__ __forceinline__ void write_gated(const f32x4 (&acc)[2 * PAIRS], const float *gate_bias, const float *up_bias, int act,
+                                            char *mine, unsigned row0, unsigned last, int n0, int width, T *y, long long ys,
+                                            T *pre, long long pres)
+{
+    f32x4 g[PAIRS], u[PAIRS], v[PAIRS];
+#pragma unroll
+    for (int i = 0; i < PAIRS; ++i) {
+        const int e = i * 16 + (threadIdx.x & 63) / 16 * 4;
+        g[i] = acc[2 * i];
+        u[i] = acc[2 * i + 1];
+        if (gate_bias) {
+            g[i] += *reinterpret_cast<const f32x4 *>(gate_bias + e);
+            u[i] += *reinterpret_cast<const f32x4 *>(up_bias + e);
+        }
+        v[i] = activate<T>(g[i], act) * u[i];
+    }
+    write_16_rows<T, PAIRS * 16>(v, mine, row0, last, n0, width, y, ys);
+    if (pre) {
+        write_16_rows<T, PAIRS * 16>(g, mine, row0, last, n0, width, pre, pres);
+        write_16_rows<T, PAIRS * 16>(u, mine, row0, last, n0, width, pre + width, pres);
+    }
+}
+
+// A tile of a gated layer's result: rows [t.first, t.last), columns from n0 on.
+// bias: TP values, the gates' first.
+template <class C>
+__device__ __forceinline__ void write_pairs(const RowTile &t, int n0, int width, const f32x4 (&acc)[C::FP][C::FQ],
+                                            const float *bias, int act, char *results, typename C::T *y, long long ys,
+                                            typename C::T *pre, long long pres)
+{
+    using T = typename C::T;
+    constexpr int PAIRS = C::FP / 2;
+    const int wave = uniform(threadIdx.x >> 6);
+    const int wp = (wave % C::WP) * PAIRS * 16, wq = (wave / C::WP) * C::FQ * 16;
+    char *mine = results + wave * 16 * kPieceRow<T, PAIRS * 16>;
+#pragma unroll
+    for (int j = 0; j < C::FQ; ++j) {
+        f32x4 column[C::FP];
+#pragma unroll
+        for (int i = 0; i < C::FP; ++i)
+            column[i] = acc[i][j];
+        write_gated<T, PAIRS>(column, bias ? bias + wp : nullptr, bias ? bias + C::kCols + wp : nullptr, act, mine,
+                              t.first + wq + j * 16, t.last, n0 + wp, width, y, ys, pre, pres);
+    }
+}
+
+// ---- rows: the layer, and its rows' gradient --------------------------------------
+
 // P: the weights (width columns of the result), Q: rows.  Where operands go to LDS by
 // themselves a workgroup goes on from tile to tile with its loads two steps ahead;
 // tiles that share rows or weights run on one XCD.  2,048 to 4,096 on 32,768 rows of
 // bf16: 493 us, 1,115 TFLOP/s; what depth adds runs at 1,430, the rest is a tile's
 // start and its results' stores.  1,024 to 4,096 on 26 rows of 16 heads, the weights'
-// reading: 18 us.
+// reading: 18 us.  act: a ReLU or none, or (kPair, a gated layer) a derf_activation; pre:
+// kPair's gates and ups, or null.
 template <class C>
 __global__ __launch_bounds__(C::kThreads, 2) void rows_kernel(
-    Problem p, Matrix<typename C::T> w, Matrix<typename C::T> x, const float *bias, int relu,
-    typename C::T *y, long long ys, int width, int depth, unsigned from)
+    Problem p, Matrix<typename C::T> w, Matrix<typename C::T> x, const float *bias, int act,
+    typename C::T *y, long long ys, typename C::T *pre, long long pres, int width, int depth, unsigned from)
 {
-    using T = typename C::T;
     constexpr int kBiases = C::kAsync ? 4 : 1;  // of the tiles under way
     __shared__ __attribute__((aligned(16))) char lds[C::kLds];
     __shared__ __attribute__((aligned(16))) char results[C::kAsync ? kResultBytes<C> : 16];
@@ -82,16 +208,16 @@ __global__ __launch_bounds__(C::kThreads, 2) void rows_kernel(
     count_tiles(p, C::TQ, before);
     const unsigned headed = uniform(before[p.heads]), headless = bound(p, p.heads);
     const unsigned tail = (unsigned)(((unsigned long long)(p.rows - headless) + C::TQ - 1) / C::TQ);
-    const unsigned row_tiles = headed + tail, col_tiles = (width + C::TP - 1) / C::TP;
+    const unsigned row_tiles = headed + tail, col_tiles = (width + C::kCols - 1) / C::kCols;
     const unsigned all = row_tiles * col_tiles, end = runs_end(all);
-    const size_t head_size = (size_t)p.fan_in * p.fan_out;
+    const size_t head_size = (size_t)p.fan_in * p.fan_out * (C::kPair ? 2 : 1);
     // what workgroup number b does: false if nothing
     auto tile_at = [&](unsigned b, RowTile &t, int &n0) {
         const unsigned at = by_xcd(b, all);
         if (at >= all)
             return false;
         const Place2 where = in_groups(at, row_tiles, col_tiles);
-        n0 = (int)where.b * C::TP;
+        n0 = (int)where.b * C::kCols;
         if (where.a < headed) {
             t = head_tile(p, before, where.a, C::TQ);
         } else {
@@ -102,7 +228,7 @@ __global__ __launch_bounds__(C::kThreads, 2) void rows_kernel(
         return true;
     };
     auto sources = [&](const RowTile &t, int n0, typename C::P::Source &ps, typename C::Q::Source &qs) {
-        ps = {w, (unsigned)n0};
+        ps = {w, (unsigned)n0, C::kPair ? (unsigned)width : 0u};
         ps.m.p += t.head * head_size;
         qs = {x, 0};
         qs.m.p += t.first * x.stride;
@@ -122,9 +248,9 @@ __global__ __launch_bounds__(C::kThreads, 2) void rows_kernel(
                 ahead += gridDim.x;
                 // its biases too: the first waves bring 64 each
                 if (bias && threadIdx.x < C::TP) {
-                    const Window b = window(bias + (size_t)u.head * width, width, 1, width, 0, m0);
-                    const unsigned wave = uniform(threadIdx.x >> 6);
-                    read4_to_lds(b, threadIdx.x * 4, lds_byte(reinterpret_cast<const char *>(biases[loaded & 3])) + wave * 256);
+                    const unsigned wave = uniform(threadIdx.x >> 6), half = wave * 64 / C::kCols;  // kPair: of the ups
+                    const Window b = window(bias + ((size_t)u.head * (C::kPair ? 2 : 1) + half) * width, width, 1, width, 0, m0);
+                    read4_to_lds(b, (threadIdx.x % C::kCols) * 4, lds_byte(reinterpret_cast<const char *>(biases[loaded & 3])) + wave * 256);
                 }
                 ++loaded;
                 typename C::P::Source ps;
@@ -146,7 +272,10 @@ __global__ __launch_bounds__(C::kThreads, 2) void rows_kernel(
 #pragma unroll 1
                 for (int k = 0; k < depth; k += C::kDepth)
                     pipe.step(acc, next_tile, [](auto &) {});
-            write_rows<C>(t, n0, width, acc, has && bias ? biases[done & 3] : nullptr, has && relu, results, y, ys);
+            if constexpr (C::kPair)
+                write_pairs<C>(t, n0, width, acc, has && bias ? biases[done & 3] : nullptr, act, results, y, ys, pre, pres);
+            else
+                write_rows<C>(t, n0, width, acc, has && bias ? biases[done & 3] : nullptr, has && act, results, y, ys);
             done += has;
         }
         arrived<0>();
@@ -156,9 +285,11 @@ __global__ __launch_bounds__(C::kThreads, 2) void rows_kernel(
         f32x4 acc[C::FP][C::FQ] = {};
         const bool has = t.head < p.heads;
         if (has) {
-            if (bias && threadIdx.x < C::TP)
+            if (bias && threadIdx.x < C::TP) {
+                const int n = n0 + (int)threadIdx.x % C::kCols, half = (int)threadIdx.x / C::kCols;  // kPair: of the ups
                 biases[0][threadIdx.x] =
-                    n0 + (int)threadIdx.x < width ? bias[(size_t)t.head * width + n0 + threadIdx.x] : 0.0f;
+                    n < width ? bias[((size_t)t.head * (C::kPair ? 2 : 1) + half) * width + n] : 0.0f;
+            }
             typename C::P::Source ps;
             typename C::Q::Source qs;
             sources(t, n0, ps, qs);
@@ -167,7 +298,10 @@ __global__ __launch_bounds__(C::kThreads, 2) void rows_kernel(
         if constexpr (C::kTeams > 1)
             if (!join_teams<C>(lds, acc))
                 return;
-        write_rows<C>(t, n0, width, acc, has && bias ? biases[0] : nullptr, has && relu, lds + kJoinBytes<C>, y, ys);
+        if constexpr (C::kPair)
+            write_pairs<C>(t, n0, width, acc, has && bias ? biases[0] : nullptr, act, lds + kJoinBytes<C>, y, ys, pre, pres);
+        else
+            write_rows<C>(t, n0, width, acc, has && bias ? biases[0] : nullptr, has && act, lds + kJoinBytes<C>, y, ys);
     }
 }
 
@@ -225,9 +359,28 @@ struct RowSums {
     }
 };
 
-// A tile of dW [O][I], rows from m0 on, columns from n0 on.
-template <class C>
-__device__ __forceinline__ void write_weights(float *to, int m0, int n0, int O, int I, const f32x4 (&acc)[C::FP][C::FQ])
+// V's values as four of a type, and the first `left` of them to memory.
+__device__ __forceinline__ void write_four(float *to, f32x4 v, int left) { write_piece(to, __builtin_bit_cast(u32x4, v), left, 0.0f); }
+struct __attribute__((packed, aligned(2))) Bytes8 {
+    unsigned long long v;
+};
+__device__ __forceinline__ void write_four(__bf16 *to, f32x4 v, int left)
+{
+    if (left >= 4) {
+        unsigned long long four;
+        store_values(reinterpret_cast<char *>(&four), v, __bf16{});
+        reinterpret_cast<Bytes8 *>(to)->v = four;
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+        if (k < left)
+            to[k] = (__bf16)v[k];
+}
+
+// A tile of dW [O][I], rows from m0 on, columns from n0 on, in float or rounded once.
+template <class C, class W>
+__device__ __forceinline__ void write_weights(W *to, int m0, int n0, int O, int I, const f32x4 (&acc)[C::FP][C::FQ])
 {
     const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
     const int wp = (wave % C::WP) * C::FP * 16, wq = (wave / C::WP) * C::FQ * 16;
@@ -239,7 +392,7 @@ __device__ __forceinline__ void write_weights(float *to, int m0, int n0, int O, 
             const int n = n0 + wp + i * 16 + (lane >> 4) * 4;
             if (m >= O || n >= I)
                 continue;
-            write_piece(to + ((size_t)m * I + n), __builtin_bit_cast(u32x4, acc[i][j]), I - n, 0.0f);
+            write_four(to + ((size_t)m * I + n), acc[i][j], I - n);
         }
     }
 }
@@ -249,9 +402,9 @@ __device__ __forceinline__ void write_weights(float *to, int m0, int n0, int O, 
 // each has a place of its own in dw and db, and sum_kernel adds them up.  db comes from
 // the dz tiles on their way, no pass of its own.  dW and db of 2,048 to 4,096 on 32,768
 // rows of bf16: 499 us, 1,100 TFLOP/s, bound by the matrix units' power.
-template <class C>
+template <class C, class W>
 __global__ __launch_bounds__(C::kThreads, 2) void weights_kernel(Problem p, Matrix<typename C::T> dz,
-                                                                 Matrix<typename C::T> x, float *dw,
+                                                                 Matrix<typename C::T> x, W *dw,
                                                                  float *db, unsigned stretch,
                                                                  unsigned places, unsigned row_tiles,
                                                                  unsigned col_tiles, unsigned from)
@@ -356,12 +509,14 @@ __global__ __launch_bounds__(C::kThreads, 2) void weights_kernel(Problem p, Matr
 // workgroups beside it.  Rows of bf16, us here and tile by tile, both with ordinary
 // stores: 319 to 256 on 262,139 113, 132; 128 to 128 on 262,144 25 (5.3 TB/s), 31; 63
 // to 64 15, 20.  PAST: results past the caches (past_caches): the first takes 94 so.
-template <class T_, int TO_, int STEPS, bool DEEP_W, bool MASK, bool PAST>
+// PAIR: a gated layer, TO / 2 columns of its result.
+template <class T_, int TO_, int STEPS, bool DEEP_W, bool MASK, bool PAST, bool PAIR = false>
 struct Shallow {
     using T = T_;
     static constexpr bool kPast = PAST;  // asked in the loop instead, it costs what it brings
-    static constexpr int TO = TO_, kSteps = STEPS, kThreads = 512, kColGroups = TO / 64, RT = 16 * 8 / kColGroups;
-    using W = Tile<T, TO, DEEP_W, kThreads, false>;
+    static constexpr bool kPair = PAIR;
+    static constexpr int TO = TO_, kCols = PAIR ? TO / 2 : TO, kSteps = STEPS, kThreads = 512, kColGroups = TO / 64, RT = 16 * 8 / kColGroups;
+    using W = Tile<T, TO, DEEP_W, kThreads, false, PAIR>;
     using X = Tile<T, RT, true, kThreads, MASK>;
     static constexpr int FP = 4;  // a wave's: 64 outputs of 16 rows
     static constexpr int kRowBytes = 64 * (int)sizeof(T) + 16;
@@ -373,7 +528,7 @@ struct Shallow {
 template <class C>
 __global__ __launch_bounds__(C::kThreads, 2 * C::kAtOnce) void shallow_kernel(Problem p, Matrix<typename C::T> w,
                                                                               Matrix<typename C::T> x, const float *bias,
-                                                                              int relu, typename C::T *y, long long ys, int width,
+                                                                              int act, typename C::T *y, long long ys, typename C::T *pre, long long pres, int width,
                                                                               unsigned stretch)
 {
     using T = typename C::T;
@@ -384,20 +539,23 @@ __global__ __launch_bounds__(C::kThreads, 2 * C::kAtOnce) void shallow_kernel(Pr
     const int O = width, lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
     count_tiles(p, stretch, before);
     // the columns of a stretch on one XCD, at about the same time
-    const unsigned cols = (O + C::TO - 1) / C::TO, j = blockIdx.x / kXcds;
+    const unsigned cols = (O + C::kCols - 1) / C::kCols, j = blockIdx.x / kXcds;
     const unsigned places = uniform(before[p.heads]), place = j / cols * kXcds + blockIdx.x % kXcds;
-    const int n0 = (int)(j % cols) * C::TO;
+    const int n0 = (int)(j % cols) * C::kCols;
     if (place >= places) {  // rows without a head: zeros
         const unsigned headless = bound(p, p.heads);
         const unsigned long long from = headless + (unsigned long long)(place - places) * stretch;
         for (unsigned long long r = from + wave; r < from + stretch && r < p.rows; r += C::kThreads / 64)
-            for (int c = n0 + lane; c < n0 + C::TO && c < O; c += 64)
+            for (int c = n0 + lane; c < n0 + C::kCols && c < O; c += 64) {
                 y[r * ys + c] = (T)0.0f;
+                if (C::kPair && pre)
+                    pre[r * pres + c] = pre[r * pres + O + c] = (T)0.0f;
+            }
         return;
     }
     const RowTile t = head_tile(p, before, place, stretch);
-    typename C::W::Source ws = {w, (unsigned)n0};
-    ws.m.p += t.head * ((size_t)p.fan_in * p.fan_out);
+    typename C::W::Source ws = {w, (unsigned)n0, C::kPair ? (unsigned)O : 0u};
+    ws.m.p += t.head * ((size_t)p.fan_in * p.fan_out * (C::kPair ? 2 : 1));
     typename C::X::Source xs = {x, 0};
     xs.m.p += t.first * x.stride;
     xs.m.mask += t.first * x.mask_stride;
@@ -414,9 +572,10 @@ __global__ __launch_bounds__(C::kThreads, 2 * C::kAtOnce) void shallow_kernel(Pr
     for (int i = 0; i < C::kSteps; ++i)
         C::W::load(sw[i], ws, i * C::W::D);
     load(0);
-    if (threadIdx.x < C::TO)
-        biases[threadIdx.x] =
-            bias && n0 + (int)threadIdx.x < O ? bias[(size_t)t.head * O + n0 + threadIdx.x] : 0.0f;
+    if (threadIdx.x < C::TO) {
+        const int n = n0 + (int)threadIdx.x % C::kCols, half = (int)threadIdx.x / C::kCols;  // kPair: of the ups
+        biases[threadIdx.x] = bias && n < O ? bias[((size_t)t.head * (C::kPair ? 2 : 1) + half) * O + n] : 0.0f;
+    }
 #pragma unroll
     for (int i = 0; i < C::kSteps; ++i) {
         C::W::settle(sw[i], ws, i * C::W::D);
@@ -446,11 +605,16 @@ __global__ __launch_bounds__(C::kThreads, 2 * C::kAtOnce) void shallow_kernel(Pr
                 for (int f = 0; f < C::FP; ++f)
                     acc[f] = multiply(C::W::fragment(lds + i * C::W::kBytes, fp + f, part), q, acc[f], T{});
             }
+        if constexpr (C::kPair) {
+            write_gated<T, C::FP / 2>(acc, biases + fp * 8, biases + C::kCols + fp * 8, act, mine, t.first + r0 + fq * 16,
+                                      t.last, n0 + fp * 8, O, y, ys, pre, pres);
+            continue;
+        }
 #pragma unroll
         for (int f = 0; f < C::FP; ++f) {
             const int e = f * 16 + (lane >> 4) * 4;
             f32x4 v = acc[f] + *reinterpret_cast<const f32x4 *>(biases + fp * 16 + e);
-            if (relu)
+            if (act)
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
                     v[k] = v[k] < 0.0f ? 0.0f : v[k];
@@ -477,10 +641,10 @@ __global__ __launch_bounds__(C::kThreads, 2 * C::kAtOnce) void shallow_kernel(Pr
 // last rounds of one fill up with tiles of the other, and what comes last is
 // short.  Both gradients of 2,048 to 4,096 on 16,384 rows: 509 us, 617 in two
 // launches.
-template <class CR, class CW>
+template <class CR, class CW, class W>
 __global__ __launch_bounds__(CR::kThreads, 2) void gradients_kernel(Problem p, Matrix<typename CR::T> w,
                                                                     Matrix<typename CR::T> dz, Matrix<typename CR::T> x,
-                                                                    typename CR::T *dx, long long dxs, float *dw, float *db)
+                                                                    typename CR::T *dx, long long dxs, W *dw, float *db)
 {
     static_assert(CR::kThreads == CW::kThreads && CR::kAsync && CW::kAsync && CR::kLds == CW::kLds, "one workgroup for both");
     constexpr int kExtra = kResultBytes<CR> > RowSums<CW>::kBytes ? kResultBytes<CR> : RowSums<CW>::kBytes;
@@ -801,7 +965,8 @@ __global__ __launch_bounds__(C::kThreads, 2) void narrow_kernel(Problem p, Matri
 // 256 elements, in order, and add up at the end: heads of many rows have so many
 // parts that one wave would wait for them in turn (16 heads, 272 parts of 128 x 128:
 // 5.7 us, 6.8 with a thread for each element).
-__global__ __launch_bounds__(256) void sum_kernel(Problem p, unsigned stretch, const float *wparts, size_t wsize, float *dw,
+template <class W>
+__global__ __launch_bounds__(256) void sum_kernel(Problem p, unsigned stretch, const float *wparts, size_t wsize, W *dw,
                                                   const float *bparts, float *db, unsigned wblocks)
 {
     constexpr unsigned kWaves = 4, kAtOnce = 8;
@@ -811,7 +976,6 @@ __global__ __launch_bounds__(256) void sum_kernel(Problem p, unsigned stretch, c
     const unsigned a = uniform(before[blockIdx.y]), b = uniform(before[blockIdx.y + 1]);
     const bool biases = blockIdx.x >= wblocks;
     const float *parts = biases ? bparts : wparts;
-    float *out = biases ? db : dw;
     const size_t size = biases ? (size_t)p.fan_out : wsize;
     const unsigned block = biases ? blockIdx.x - wblocks : blockIdx.x, blocks = biases ? gridDim.x - wblocks : wblocks;
     const unsigned wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
@@ -846,7 +1010,10 @@ __global__ __launch_bounds__(256) void sum_kernel(Problem p, unsigned stretch, c
         __syncthreads();
         if (wave == 0) {
             v = sums[0][lane] + sums[1][lane] + sums[2][lane] + sums[3][lane];
-            write_piece(out + (blockIdx.y * size + e), __builtin_bit_cast(u32x4, v), here, 0.0f);
+            if (biases)
+                write_four(db + (blockIdx.y * size + e), v, here);
+            else
+                write_four(dw + (blockIdx.y * size + e), v, here);
         }
         __syncthreads();
     }
@@ -856,15 +1023,16 @@ __global__ __launch_bounds__(256) void sum_kernel(Problem p, unsigned stretch, c
 
 template <class C>
 hipError_t launch_rows(const Problem &p, const Matrix<typename C::T> &w,
-                       const Matrix<typename C::T> &x, const float *bias, bool relu, Rows y,
-                       int width, int depth, hipStream_t s)
+                       const Matrix<typename C::T> &x, const float *bias, int act, Rows y,
+                       int width, int depth, hipStream_t s, Rows pre = {nullptr, 0})
 {
     using T = typename C::T;
     // at most: every head's last tile and the headless rows' may be partly filled
-    return launch_for<C>(((unsigned long long)p.rows / C::TQ + p.heads + 1) * tiles_of(width, C::TP),
+    return launch_for<C>(((unsigned long long)p.rows / C::TQ + p.heads + 1) * tiles_of(width, C::kCols),
                          [&](unsigned groups, unsigned from) {
                              rows_kernel<C><<<groups, C::kThreads, 0, s>>>(
-                                 p, w, x, bias, relu, static_cast<T *>(const_cast<void *>(y.p)), y.stride, width, depth, from);
+                                 p, w, x, bias, act, static_cast<T *>(const_cast<void *>(y.p)), y.stride,
+                                 static_cast<T *>(const_cast<void *>(pre.p)), pre.stride, width, depth, from);
                          });
 }
 
@@ -884,35 +1052,35 @@ bool large_tiles(const Problem &p, int width)
 
 template <class C>
 hipError_t launch_shallow(const Problem &p, const Matrix<typename C::T> &w, const Matrix<typename C::T> &x,
-                          const float *bias, bool relu, Rows y, int width, hipStream_t s)
+                          const float *bias, int act, Rows y, int width, hipStream_t s, Rows pre = {nullptr, 0})
 {
     using T = typename C::T;
-    const unsigned cols = tiles_of(width, C::TO), want = 256 * C::kAtOnce / cols;
+    const unsigned cols = tiles_of(width, C::kCols), want = 256 * C::kAtOnce / cols;
     // stretches for `want` places, some of which the heads' last ones take
     unsigned stretch = (unsigned)p.heads < want / 2 ? p.rows / (want - p.heads) : p.rows / (want / 2);
     stretch = (stretch + 32) / 32 * 32;
     const unsigned places = p.rows / stretch + p.heads + 1;
     const unsigned groups = (places + kXcds - 1) / kXcds * kXcds * cols;
-    shallow_kernel<C><<<groups, C::kThreads, 0, s>>>(p, w, x, bias, relu, static_cast<T *>(const_cast<void *>(y.p)), y.stride,
-                                                     width, stretch);
+    shallow_kernel<C><<<groups, C::kThreads, 0, s>>>(p, w, x, bias, act, static_cast<T *>(const_cast<void *>(y.p)), y.stride,
+                                                     static_cast<T *>(const_cast<void *>(pre.p)), pre.stride, width, stretch);
     return hipGetLastError();
 }
 
-template <class T, int TO, bool DEEP_W, bool MASK, bool PAST>
-hipError_t shallow(const Problem &p, const Matrix<T> &w, const Matrix<T> &x, const float *bias, bool relu, Rows y,
-                   int width, hipStream_t s)
+template <class T, int TO, bool DEEP_W, bool MASK, bool PAST, bool PAIR = false>
+hipError_t shallow(const Problem &p, const Matrix<T> &w, const Matrix<T> &x, const float *bias, int act, Rows y,
+                   int width, hipStream_t s, Rows pre = {nullptr, 0})
 {
     const unsigned steps = tiles_of((long long)x.cols * sizeof(T), 128);
     if constexpr (DEEP_W) {
         if (steps == 3)
-            return launch_shallow<Shallow<T, TO, 3, DEEP_W, MASK, PAST>>(p, w, x, bias, relu, y, width, s);
+            return launch_shallow<Shallow<T, TO, 3, DEEP_W, MASK, PAST, PAIR>>(p, w, x, bias, act, y, width, s, pre);
         if (steps == 4)
-            return launch_shallow<Shallow<T, TO, 4, DEEP_W, MASK, PAST>>(p, w, x, bias, relu, y, width, s);
+            return launch_shallow<Shallow<T, TO, 4, DEEP_W, MASK, PAST, PAIR>>(p, w, x, bias, act, y, width, s, pre);
         if (steps == 5)
-            return launch_shallow<Shallow<T, TO, 5, DEEP_W, MASK, PAST>>(p, w, x, bias, relu, y, width, s);
+            return launch_shallow<Shallow<T, TO, 5, DEEP_W, MASK, PAST, PAIR>>(p, w, x, bias, act, y, width, s, pre);
     }
-    return steps == 1 ? launch_shallow<Shallow<T, TO, 1, DEEP_W, MASK, PAST>>(p, w, x, bias, relu, y, width, s)
-                      : launch_shallow<Shallow<T, TO, 2, DEEP_W, MASK, PAST>>(p, w, x, bias, relu, y, width, s);
+    return steps == 1 ? launch_shallow<Shallow<T, TO, 1, DEEP_W, MASK, PAST, PAIR>>(p, w, x, bias, act, y, width, s, pre)
+                      : launch_shallow<Shallow<T, TO, 2, DEEP_W, MASK, PAST, PAIR>>(p, w, x, bias, act, y, width, s, pre);
 }
 
 // 128 columns a tile, or 64: for narrow matrices, and for float, which is bound by
@@ -1015,19 +1183,20 @@ Split split_rows(unsigned rows, int heads, int fan_in, int fan_out, bool bf16)
 }
 
 // The stretches' parts added up.
-hipError_t launch_sums(const Problem &p, const Split &split, const float *wparts, float *dw, const float *bparts, float *db,
+template <class W>
+hipError_t launch_sums(const Problem &p, const Split &split, const float *wparts, W *dw, const float *bparts, float *db,
                        hipStream_t s)
 {
     const size_t size = (size_t)p.fan_in * p.fan_out;
     const unsigned blocks = dw ? tiles_of(size, 256) : 0, wblocks = blocks < 1024 ? blocks : 1024;
     const unsigned bblocks = db ? tiles_of(p.fan_out, 256) : 0;
-    sum_kernel<<<dim3(wblocks + bblocks, p.heads), 256, 0, s>>>(p, split.stretch, wparts, size, dw, bparts, db, wblocks);
+    sum_kernel<W><<<dim3(wblocks + bblocks, p.heads), 256, 0, s>>>(p, split.stretch, wparts, size, dw, bparts, db, wblocks);
     return hipGetLastError();
 }
 
-template <class C>
+template <class C, class W>
 hipError_t launch_weights(const Problem &p, const Matrix<typename C::T> &dz,
-                          const Matrix<typename C::T> &x, float *dw, float *db, char *workspace,
+                          const Matrix<typename C::T> &x, W *dw, float *db, char *workspace,
                           hipStream_t s)
 {
     const Split split = split_rows(p.rows, p.heads, p.fan_in, p.fan_out, sizeof(typename C::T) == 2);
@@ -1035,15 +1204,18 @@ hipError_t launch_weights(const Problem &p, const Matrix<typename C::T> &dz,
     const size_t size = (size_t)p.fan_in * p.fan_out;
     float *wparts = reinterpret_cast<float *>(workspace);
     float *bparts = wparts + (size_t)split.places * size;
-    float *to_w = dw ? (partial ? wparts : dw) : nullptr, *to_b = db ? (partial ? bparts : db) : nullptr;
     const unsigned row_tiles = tiles_of(p.fan_out, C::TQ), col_tiles = dw ? tiles_of(p.fan_in, C::TP) : 1;
-    const hipError_t e = launch_for<C>(
-        (unsigned long long)split.places * row_tiles * col_tiles, [&](unsigned groups, unsigned from) {
-            weights_kernel<C><<<groups, C::kThreads, 0, s>>>(p, dz, x, to_w, to_b, split.stretch, split.places, row_tiles, col_tiles, from);
+    const unsigned long long tiles = (unsigned long long)split.places * row_tiles * col_tiles;
+    auto launch = [&](auto *to_w, float *to_b) {
+        using To = std::remove_pointer_t<decltype(to_w)>;
+        return launch_for<C>(tiles, [&](unsigned groups, unsigned from) {
+            weights_kernel<C, To><<<groups, C::kThreads, 0, s>>>(p, dz, x, to_w, to_b, split.stretch, split.places, row_tiles, col_tiles, from);
         });
-    if (e != hipSuccess)
-        return e;
-    return partial ? launch_sums(p, split, wparts, dw, bparts, db, s) : hipSuccess;
+    };
+    if (!partial)
+        return launch(dw, db);
+    const hipError_t e = launch(dw ? wparts : nullptr, db ? bparts : nullptr);
+    return e != hipSuccess ? e : launch_sums(p, split, wparts, dw, bparts, db, s);
 }
 
 // 256 x 256 tiles from 256 of them on, one a compute unit.  dW and db, us with large and
@@ -1051,8 +1223,8 @@ hipError_t launch_weights(const Problem &p, const Matrix<typename C::T> &dz,
 // 1,024 on 16,384 of 8 (128) 115, 70; 512 to 512 on 65,536 of 16 (64) 111, 80; at the line
 // small ones would win: 1,024 to 2,048 on 16,384 of 8 119, 101; 1,024 to 1,024 on 65,536 of
 // 16 387, 271.
-template <class T, bool MASK>
-hipError_t weights_product(const Problem &p, const Matrix<T> &dz, const Matrix<T> &x, float *dw,
+template <class T, bool MASK, class W>
+hipError_t weights_product(const Problem &p, const Matrix<T> &dz, const Matrix<T> &x, W *dw,
                            float *db, char *workspace, hipStream_t s)
 {
     const bool wide_o = wide_tile<T>(p.fan_out), wide_i = wide_tile<T>(p.fan_in);
@@ -1091,9 +1263,19 @@ Split narrow_split(unsigned rows, int heads, int fan_in, int fan_out, bool bf16)
     return {stretch, rows / stretch + heads};
 }
 
-template <class C>
+// Bytes that the products of the gradients need for their stretches' parts.
+size_t parts_bytes(unsigned rows, int heads, int fan_in, int fan_out, bool bf16)
+{
+    const Split split = split_rows(rows, heads, fan_in, fan_out, bf16), narrow = narrow_split(rows, heads, fan_in, fan_out, bf16);
+    size_t places = split.stretch ? split.places : 0;
+    if (is_narrow(fan_in, fan_out) && narrow.places > places)
+        places = narrow.places;
+    return places * fan_out * ((size_t)fan_in + 1) * sizeof(float);
+}
+
+template <class C, class W>
 hipError_t launch_narrow(const Problem &p, const Matrix<typename C::T> &w, const Matrix<typename C::T> &dz,
-                         const Matrix<typename C::T> &x, Rows dx, float *dw, float *db, char *workspace, hipStream_t s)
+                         const Matrix<typename C::T> &x, Rows dx, W *dw, float *db, char *workspace, hipStream_t s)
 {
     using T = typename C::T;
     const Split split = narrow_split(p.rows, p.heads, p.fan_in, p.fan_out, sizeof(T) == 2);
@@ -1105,8 +1287,8 @@ hipError_t launch_narrow(const Problem &p, const Matrix<typename C::T> &w, const
     return e != hipSuccess || (!dw && !db) ? e : launch_sums(p, split, wparts, dw, bparts, db, s);
 }
 
-template <class T, bool MASK>
-hipError_t narrow(const Problem &p, const Matrix<T> &w, const Matrix<T> &dz, const Matrix<T> &x, Rows dx, float *dw,
+template <class T, bool MASK, class W>
+hipError_t narrow(const Problem &p, const Matrix<T> &w, const Matrix<T> &dz, const Matrix<T> &x, Rows dx, W *dw,
                   float *db, char *workspace, hipStream_t s)
 {
     if (p.fan_in <= 64)
@@ -1116,9 +1298,9 @@ hipError_t narrow(const Problem &p, const Matrix<T> &w, const Matrix<T> &dz, con
                            : launch_narrow<Narrow<T, 128, 128, MASK>>(p, w, dz, x, dx, dw, db, workspace, s);
 }
 
-template <class CR, class CW>
+template <class CR, class CW, class W>
 hipError_t launch_gradients(const Problem &p, const Matrix<typename CR::T> &w, const Matrix<typename CR::T> &dz,
-                            const Matrix<typename CR::T> &x, Rows dx, float *dw, float *db, hipStream_t s)
+                            const Matrix<typename CR::T> &x, Rows dx, W *dw, float *db, hipStream_t s)
 {
     using T = typename CR::T;
     const unsigned long long all =
@@ -1126,7 +1308,7 @@ hipError_t launch_gradients(const Problem &p, const Matrix<typename CR::T> &w, c
         (unsigned long long)p.heads * tiles_of(p.fan_out, CW::TQ) * tiles_of(p.fan_in, CW::TP) + 3 * kXcds * kRun;
     if (all >= 1ull << 23)
         return hipErrorInvalidConfiguration;
-    gradients_kernel<CR, CW><<<(unsigned)all, CR::kThreads, 0, s>>>(
+    gradients_kernel<CR, CW, W><<<(unsigned)all, CR::kThreads, 0, s>>>(
         p, w, dz, x, static_cast<T *>(const_cast<void *>(dx.p)), dx.stride, dw, db);
     return hipGetLastError();
 }

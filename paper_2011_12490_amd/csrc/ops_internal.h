@@ -47,6 +47,15 @@ hipError_t launch_heads_linear_backward(const LinearShape &sh, Rows dy, Rows x, 
                                         Rows y, bool bf16, Rows dx, float *dw, float *db,
                                         void *workspace, hipStream_t s);
 
+// ---- the heads' gated layers (kernels_gated.hip, kernels_gated_back.hip) -------
+// pre.p may be null.
+hipError_t launch_heads_gated(const LinearShape &sh, Rows x, const void *w, const float *bias, int act, bool bf16, Rows y,
+                              Rows pre, hipStream_t s);
+size_t heads_gated_workspace_bytes(unsigned rows, int heads, int fan_in, int fan_out, bool bf16);
+// dx.p, dw, db may be null.
+hipError_t launch_heads_gated_backward(const LinearShape &sh, Rows dy, Rows pre, Rows x, const void *w, int act, bool bf16,
+                                       Rows dx, void *dw, float *db, void *workspace, hipStream_t s);
+
 // ---- AdamW (kernels_adamw.hip) ----------------------------------------------
 // Values of an 8-bit moment that share a scale.
 constexpr int kMomentBlock = 256;

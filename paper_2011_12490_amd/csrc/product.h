@@ -264,9 +264,12 @@ __device__ __forceinline__ void stored() { asm volatile("s_waitcnt lgkmcnt(0)\n\
 // bank once (64 of 4 bytes; no conflicts counted): 16 lanes read 16 bytes at a
 // time (lanes 0-3, 12-15, 20-23, 24-27 for one), or 32 lanes 8 bytes where they
 // transpose.  A thread brings kShare chunks, all of the same columns.
+// PAIR: a deep tile of rows of two halves of a matrix, 16 of the first and 16 of the
+// second in turn, so that a wave has both results of a column in the same lanes.
 constexpr int kChunks = 8;
-template <class T, int TILE, bool DEEP, int THREADS, bool MASK>
+template <class T, int TILE, bool DEEP, int THREADS, bool MASK, bool PAIR = false>
 struct Tile {
+    static_assert(DEEP || !PAIR, "pairs are of rows");
     static constexpr int V = Type<T>::kVec, D = kChunks * V;
     static constexpr int kShare = TILE * kChunks / THREADS;
     static constexpr int kBytes = TILE * kChunks * 16;
@@ -299,7 +302,13 @@ struct Tile {
     struct Source {
         Matrix<T> m;
         unsigned t0;
+        unsigned half;  // PAIR: rows from a row of the first half to the second's
     };
+    // Row of the matrix, from t0 on, that is the tile's row r.
+    static __device__ __forceinline__ unsigned matrix_row(const Source &s, unsigned r)
+    {
+        return PAIR ? (r >> 5) * 16 + (r & 15) + (r & 16 ? s.half : 0) : r;
+    }
     // First column of the step at depth k, columns from there on, and its window.
     static __device__ __forceinline__ int cols_left(const Source &s, unsigned k)
     {
@@ -327,10 +336,10 @@ struct Tile {
             const unsigned c = (unsigned)(back + (col + V <= left ? col : left - V));
             const unsigned row_bytes = (unsigned)src.m.stride * sizeof(T);
             const Window w = view(src, src.m.p, src.m.stride, k, back);
-            const unsigned offset = my_row() * row_bytes + c * (unsigned)sizeof(T);
+            const unsigned offset = (PAIR ? 0 : my_row() * row_bytes) + c * (unsigned)sizeof(T);
 #pragma unroll
             for (int i = 0; i < kShare; ++i)
-                s.x[i] = read16(w, offset + i * kRowStep * row_bytes);
+                s.x[i] = read16(w, offset + (PAIR ? matrix_row(src, my_row() + i * kRowStep) : i * kRowStep) * row_bytes);
             if (MASK) {
                 const unsigned mask_bytes = (unsigned)src.m.mask_stride * sizeof(T);
                 const Window y = view(src, src.m.mask, src.m.mask_stride, k, back);
@@ -345,7 +354,7 @@ struct Tile {
         const unsigned row0 = (DEEP ? src.t0 : k) + my_row();
 #pragma unroll
         for (int i = 0; i < kShare; ++i) {
-            const unsigned r = row0 + i * kRowStep;
+            const unsigned r = PAIR ? src.t0 + matrix_row(src, my_row() + i * kRowStep) : row0 + i * kRowStep;
             const bool in = r < src.m.rows && col == 0 && left == src.m.cols;
             unsigned x[V] = {}, y[V] = {};
 #pragma unroll
@@ -415,7 +424,7 @@ struct Tile {
             // a tile's columns that are not the matrix's are outside in every step
 #pragma unroll
             for (int i = 0; i < kShare; ++i)
-                offset[i] = DEEP || col < cols ? (my_row() + i * kRowStep) * row_bytes + col * (unsigned)sizeof(T) : kOutside;
+                offset[i] = DEEP || col < cols ? matrix_row(s, my_row() + i * kRowStep) * row_bytes + col * (unsigned)sizeof(T) : kOutside;
         }
         // The steps from here on bring zeros: an empty window, whether or not
         // there was a tile before.
@@ -516,15 +525,16 @@ __device__ __forceinline__ f32x4 multiply(u32x4 p, u32x4 q, f32x4 c, float)
 // a mask.  ASYNC: operands go from memory to LDS by themselves (Tile::Feed).
 // EACH_Q: tile_product shows its caller the Q tiles.  TEAMS: of so many waves each;
 // they take the depth's steps in turn, in LDS of their own, and add up at the end.
+// PAIR: P's tiles are of pairs (Tile).
 template <class T_, int TP_, int TQ_, int WP_, int WQ_, bool DEEP_P, bool DEEP_Q, bool MASK,
-          bool ASYNC = false, bool EACH_Q = false, int TEAMS = 1>
+          bool ASYNC = false, bool EACH_Q = false, int TEAMS = 1, bool PAIR = false>
 struct Product {
     using T = T_;
     static constexpr int TP = TP_, TQ = TQ_, WP = WP_, WQ = WQ_;
     static constexpr int kTeams = TEAMS, kTeam = WP * WQ * 64, kThreads = kTeam * TEAMS;
-    static constexpr bool kAsync = ASYNC, kEachQ = EACH_Q;
+    static constexpr bool kAsync = ASYNC, kEachQ = EACH_Q, kPair = PAIR;
     static_assert(TEAMS == 1 || !ASYNC, "teams bring their operands through registers");
-    using P = Tile<T, TP, DEEP_P, kTeam, false>;
+    using P = Tile<T, TP, DEEP_P, kTeam, false, PAIR>;
     using Q = Tile<T, TQ, DEEP_Q, kTeam, MASK>;
     static constexpr int kDepth = P::D;
     static constexpr int FP = TP / WP / 16, FQ = TQ / WQ / 16;  // a wave's 16 x 16 results
@@ -534,7 +544,8 @@ struct Product {
     // spills and narrow ones a workgroup more on the compute unit (262,144 rows of
     // 64 to 64 24 us, 18 with one; of 319 to 256 132, 147 with one)
     static constexpr int kSets = TEAMS > 1 || (!MASK && FP * FQ >= 16) ? 2 : 1;
-    static_assert(FP * WP * 16 == TP && FQ * WQ * 16 == TQ, "whole results a wave");
+    static constexpr int kCols = PAIR ? TP / 2 : TP;  // of a result's row
+    static_assert(FP * WP * 16 == TP && FQ * WQ * 16 == TQ && (!PAIR || FP % 2 == 0), "whole results a wave");
 };
 
 // What of `all` things to do in turn n of `turns`, spread evenly: do_one(i).
@@ -772,7 +783,7 @@ constexpr int kJoinBytes = (C::kTeams - 1) * C::FP * C::FQ * C::kTeam * 16;
 // written in 16-byte pieces; kResultRow: bytes of a row there (4 of 64 banks further
 // on for the next row).
 template <class C>
-constexpr int kResultRow = C::FP * 16 * (int)sizeof(typename C::T) + 16;
+constexpr int kResultRow = C::FP * (C::kPair ? 8 : 16) * (int)sizeof(typename C::T) + 16;
 template <class C>
 constexpr int kResultBytes = sizeof(typename C::T) == 2 ? C::WP * C::WQ * 16 * kResultRow<C> : 16;
 __device__ __forceinline__ void store_values(char *to, f32x4 v, __bf16)

@@ -70,7 +70,8 @@ EXPORTS = ("derf_weights_count", "derf_create", "derf_create_mixed", "derf_head_
            "derf_reset_stats", "derf_destroy",
            "derf_route_workspace", "derf_route", "derf_dispatch", "derf_combine",
            "derf_combine_backward", "derf_heads_linear", "derf_heads_linear_workspace",
-           "derf_heads_linear_backward", "derf_adamw_create", "derf_adamw_step",
+           "derf_heads_linear_backward", "derf_heads_gated",
+           "derf_heads_gated_workspace", "derf_heads_gated_backward", "derf_adamw_create", "derf_adamw_step",
            "derf_adamw_destroy",
            "derf_status_string", "derf_last_error")
 
@@ -147,6 +148,10 @@ def lib() -> ctypes.CDLL:
                 ("derf_heads_linear_workspace", N, [N, I, I, I, I, I]),
                 ("derf_heads_linear_backward", I,
                  [P, N, P, N, P, P, N, P, N, I, I, I, I, P, N, P, P, P, N, P]),
+                ("derf_heads_gated", I, [P, N, P, P, P, N, I, I, I, I, I, P, N, P, N, P]),
+                ("derf_heads_gated_workspace", N, [N, I, I, I, I]),
+                ("derf_heads_gated_backward", I,
+                 [P, N, P, N, P, N, P, P, N, I, I, I, I, I, P, N, P, P, P, N, P]),
                 ("derf_adamw_create", I, [ctypes.POINTER(P), P, I, I]),
                 ("derf_adamw_step", I, [P, D, D, D, D, D, N, P, P]),
                 ("derf_adamw_destroy", None, [P])):

@@ -36,6 +36,7 @@ from . import derf
 
 MAX_TOP_K = 16
 MOMENT_BLOCK = 256  # values of an 8-bit moment that share a scale
+ACTIVATIONS = {"silu": 0, "gelu": 1, "relu": 2, "sigmoid": 3}  # derf_activation
 _PRECISION = {torch.float32: derf.DERF_PREC_FP32, torch.bfloat16: derf.DERF_PREC_BF16}
 
 
@@ -295,6 +296,77 @@ def linear_backward(dy: torch.Tensor, x: torch.Tensor, weight: torch.Tensor,
     _call("derf_heads_linear_backward", dy.device, dy.data_ptr(), dy_stride, x.data_ptr(), x_stride,
           weight.data_ptr(), _ptr(y), y_stride, offsets.data_ptr(), R, K, I, O, prec, _ptr(out_x),
           dx_stride, out_weight.data_ptr(), out_bias.data_ptr(), _ptr(ws), need)
+    return out_x, out_weight, out_bias
+
+
+def _gated_layer(w, offsets, like, act):
+    if not isinstance(w, torch.Tensor) or w.dim() != 4 or w.shape[1] != 2:
+        raise ValueError("weight must be a tensor [heads, 2, fan_out, fan_in]")
+    _array(w, "weight", like.dtype, w.shape, like.device)
+    K, _, O, I = w.shape
+    _array(offsets, "offsets", torch.int32, (K + 1,), like.device)
+    if act not in ACTIVATIONS:
+        raise ValueError("act is %r, not one of %s" % (act, ", ".join(ACTIVATIONS)))
+    return K, O, I
+
+
+def gated(x: torch.Tensor, weight: torch.Tensor, bias: Optional[torch.Tensor],
+          offsets: torch.Tensor, act: str = "silu", keep: bool = False,
+          out: Optional[torch.Tensor] = None, out_pre: Optional[torch.Tensor] = None):
+    """Every head's gated layer on its rows: (y, pre) with y[r] = act(g) * u, g = weight[h, 0] @
+    x[r] + bias[h, 0] and u = weight[h, 1] @ x[r] + bias[h, 1], zero from offsets[-1] on.
+    weight [heads, 2, fan_out, fan_in] of x's type, bias float32 [heads, 2, fan_out] or
+    None; act one of ACTIVATIONS.  pre [R, 2 * fan_out], g then u, is what the gradients
+    need: with keep (or out_pre), else None."""
+    stride = _rows(x, "x")
+    K, O, I = _gated_layer(weight, offsets, x, act)
+    if x.shape[1] != I:
+        raise ValueError("x has rows of %d, the layer takes %d" % (x.shape[1], I))
+    if bias is not None:
+        _array(bias, "bias", torch.float32, (K, 2, O), x.device)
+    out, out_stride = _out_rows(out, "out", x.shape[0], O, x)
+    pre_stride = 0
+    if keep or out_pre is not None:
+        out_pre, pre_stride = _out_rows(out_pre, "out_pre", x.shape[0], 2 * O, x)
+    _call("derf_heads_gated", x.device, x.data_ptr(), stride, weight.data_ptr(), _ptr(bias),
+          offsets.data_ptr(), x.shape[0], K, I, O, ACTIVATIONS[act], _PRECISION[x.dtype],
+          out.data_ptr(), out_stride, _ptr(out_pre), pre_stride)
+    return out, out_pre
+
+
+def gated_backward(dy: torch.Tensor, pre: torch.Tensor, x: torch.Tensor, weight: torch.Tensor,
+                   offsets: torch.Tensor, act: str = "silu", need_dx: bool = True,
+                   out_x: Optional[torch.Tensor] = None, out_weight: Optional[torch.Tensor] = None,
+                   out_bias: Optional[torch.Tensor] = None):
+    """Gradients of gated at the gates and ups that it kept: (dx, dweight, dbias).
+    dweight [heads, 2, fan_out, fan_in] is of the weights' type (its factors carry that
+    type's rounding), dbias [heads, 2, fan_out] float32; need_dx False: dx is None and
+    not computed."""
+    dy_stride = _rows(dy, "dy")
+    K, O, I = _gated_layer(weight, offsets, dy, act)
+    R = dy.shape[0]
+    if dy.shape[1] != O:
+        raise ValueError("dy has rows of %d, the layer gives %d" % (dy.shape[1], O))
+    pre_stride = _rows(pre, "pre", (R, 2 * O), dy.dtype, dy.device)
+    x_stride = _rows(x, "x", (R, I), dy.dtype, dy.device)
+    dx_stride = 0
+    if need_dx:
+        out_x, dx_stride = _out_rows(out_x, "out_x", R, I, dy)
+    elif out_x is not None:
+        raise ValueError("out_x without need_dx")
+    if out_weight is None:
+        out_weight = torch.empty_like(weight, requires_grad=False)
+    else:
+        _array(out_weight, "out_weight", weight.dtype, weight.shape, dy.device)
+    out_bias = _out_array(out_bias, "out_bias", (K, 2, O), dy.device)
+    prec = _PRECISION[dy.dtype]
+    need = _workspace_bytes("derf_heads_gated_workspace", R, K, I, O, prec)
+    if need < 0:
+        raise ValueError("invalid sizes: %d rows, %d heads of %d to 2 x %d" % (R, K, I, O))
+    ws = _workspace(need, dy.device)
+    _call("derf_heads_gated_backward", dy.device, dy.data_ptr(), dy_stride, pre.data_ptr(), pre_stride,
+          x.data_ptr(), x_stride, weight.data_ptr(), offsets.data_ptr(), R, K, I, O, ACTIVATIONS[act],
+          prec, _ptr(out_x), dx_stride, out_weight.data_ptr(), out_bias.data_ptr(), _ptr(ws), need)
     return out_x, out_weight, out_bias
 
 
