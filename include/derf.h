@@ -519,6 +519,26 @@ int derf_heads_gated_backward(const void *dy, long long dy_stride, const void *p
                               void *out_x, long long out_x_stride, void *out_w, float *out_bias,
                               void *workspace, long long workspace_bytes, void *hip_stream);
 
+/* Rows of a table picked by the samples' ids (a code for each image, features of a
+ * cell): out[t] = scale * table[ids[t]], zero where ids[t] is outside [0, num_rows).
+ *   table   [num_rows] rows of dim elements, table_stride apart
+ *   ids     int [num_samples]
+ * 1 <= num_rows < 2^31, num_samples < 2^31, 1 <= dim <= 65536. */
+int derf_lookup(const void *table, long long table_stride, const int *ids, long long num_samples,
+                long long num_rows, int dim, float scale, int precision, void *out,
+                long long out_stride, void *hip_stream);
+
+/* Gradient of derf_lookup: out[v] = scale * sum of dout[t] over the samples with
+ * ids[t] = v, zero where there is none.  The samples are sorted by id, stably; the sums
+ * are taken in fp32 in an order that the ids alone fix.
+ *   out        float [num_rows][dim], contiguous, all written
+ *   workspace  derf_lookup_workspace(...) bytes (-1 for invalid sizes) */
+long long derf_lookup_workspace(long long num_samples, long long num_rows, int dim);
+int derf_lookup_backward(const void *dout, long long dout_stride, const int *ids,
+                         long long num_samples, long long num_rows, int dim, float scale,
+                         int precision, float *out, void *workspace, long long workspace_bytes,
+                         void *hip_stream);
+
 /* AdamW over many tensors in one launch (the heads are trained with a
  * first-order optimizer, Sec. 3.4).  Per value, with g = *grad_scale * grad:
  *   m = beta1 m + (1 - beta1) g,   v = beta2 v + (1 - beta2) g^2,

@@ -2,6 +2,8 @@
 // declared in include/derf.h: argument checks before any HIP call, then the launches.
 #include "ops_checks.h"
 
+#include <math.h>
+
 using namespace derf;
 
 namespace {
@@ -20,6 +22,22 @@ int check_gated(long long rows, int heads, int fan_in, int fan_out, int act, int
         return report(DERF_ERR_INVALID_ARG, "a head's weights from %d to 2 x %d take 2^31 bytes or more", fan_in, fan_out);
     if (act < DERF_ACT_SILU || act > DERF_ACT_SIGMOID)
         return report(DERF_ERR_INVALID_ARG, "unknown activation %d", act);
+    return DERF_OK;
+}
+
+bool lookup_sizes_valid(long long samples, long long rows, int dim)
+{
+    return samples >= 0 && samples < kMaxRows && rows >= 1 && rows < kMaxRows && dim >= 1 && dim <= kMaxDim;
+}
+
+int check_lookup(long long samples, long long rows, int dim, float scale, int precision)
+{
+    if (!lookup_sizes_valid(samples, rows, dim))
+        return report(DERF_ERR_INVALID_ARG, "need 0 <= num_samples < 2^31, 1 <= num_rows < 2^31, 1 <= dim <= %d", kMaxDim);
+    if (!is_precision(precision))
+        return report(DERF_ERR_INVALID_ARG, "unknown precision %d", precision);
+    if (!isfinite(scale))
+        return report(DERF_ERR_INVALID_ARG, "scale is not finite");
     return DERF_OK;
 }
 
@@ -89,6 +107,45 @@ int derf_heads_gated_backward(const void *dy, long long dy_stride, const void *p
                                                 precision == DERF_PREC_BF16, {out_x, out_x_stride}, out_w, out_bias,
                                                 workspace, static_cast<hipStream_t>(hip_stream)),
                     "derf_heads_gated_backward");
+}
+
+int derf_lookup(const void *table, long long table_stride, const int *ids, long long num_samples,
+                long long num_rows, int dim, float scale, int precision, void *out,
+                long long out_stride, void *hip_stream)
+{
+    TRY(check_lookup(num_samples, num_rows, dim, scale, precision));
+    if (num_samples == 0)
+        return DERF_OK;
+    TRY(check_rows("table", table, table_stride, dim, precision));
+    TRY(check_array("ids", ids, 4));
+    TRY(check_rows("out", out, out_stride, dim, precision));
+    return launched(launch_lookup({table, table_stride}, ids, num_samples, num_rows, dim, scale, precision == DERF_PREC_BF16,
+                                  {out, out_stride}, static_cast<hipStream_t>(hip_stream)),
+                    "derf_lookup");
+}
+
+long long derf_lookup_workspace(long long num_samples, long long num_rows, int dim)
+{
+    if (!lookup_sizes_valid(num_samples, num_rows, dim))
+        return -1;
+    return (long long)lookup_workspace_bytes((unsigned)num_samples, (unsigned)num_rows, dim);
+}
+
+int derf_lookup_backward(const void *dout, long long dout_stride, const int *ids,
+                         long long num_samples, long long num_rows, int dim, float scale,
+                         int precision, float *out, void *workspace, long long workspace_bytes,
+                         void *hip_stream)
+{
+    TRY(check_lookup(num_samples, num_rows, dim, scale, precision));
+    if (num_samples > 0) {
+        TRY(check_rows("dout", dout, dout_stride, dim, precision));
+        TRY(check_array("ids", ids, 4));
+    }
+    TRY(check_array("out", out, 4));
+    TRY(check_workspace(workspace, workspace_bytes, derf_lookup_workspace(num_samples, num_rows, dim)));
+    return launched(launch_lookup_backward({dout, dout_stride}, ids, (unsigned)num_samples, (unsigned)num_rows, dim, scale,
+                                           precision == DERF_PREC_BF16, out, workspace, static_cast<hipStream_t>(hip_stream)),
+                    "derf_lookup_backward");
 }
 
 }  // extern "C"

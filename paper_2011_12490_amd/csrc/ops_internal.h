@@ -56,6 +56,13 @@ size_t heads_gated_workspace_bytes(unsigned rows, int heads, int fan_in, int fan
 hipError_t launch_heads_gated_backward(const LinearShape &sh, Rows dy, Rows pre, Rows x, const void *w, int act, bool bf16,
                                        Rows dx, void *dw, float *db, void *workspace, hipStream_t s);
 
+// ---- table lookups (kernels_lookup.hip) -----------------------------------------
+hipError_t launch_lookup(Rows table, const int *ids, long long samples, long long rows, int dim, float scale, bool bf16, Rows out,
+                         hipStream_t s);
+size_t lookup_workspace_bytes(unsigned samples, unsigned rows, int dim);
+hipError_t launch_lookup_backward(Rows dout, const int *ids, unsigned samples, unsigned rows, int dim, float scale, bool bf16,
+                                  float *out, void *workspace, hipStream_t s);
+
 // ---- AdamW (kernels_adamw.hip) ----------------------------------------------
 // Values of an 8-bit moment that share a scale.
 constexpr int kMomentBlock = 256;

@@ -71,7 +71,8 @@ EXPORTS = ("derf_weights_count", "derf_create", "derf_create_mixed", "derf_head_
            "derf_route_workspace", "derf_route", "derf_dispatch", "derf_combine",
            "derf_combine_backward", "derf_heads_linear", "derf_heads_linear_workspace",
            "derf_heads_linear_backward", "derf_heads_gated",
-           "derf_heads_gated_workspace", "derf_heads_gated_backward", "derf_adamw_create", "derf_adamw_step",
+           "derf_heads_gated_workspace", "derf_heads_gated_backward",
+           "derf_lookup", "derf_lookup_workspace", "derf_lookup_backward", "derf_adamw_create", "derf_adamw_step",
            "derf_adamw_destroy",
            "derf_status_string", "derf_last_error")
 
@@ -137,7 +138,7 @@ def lib() -> ctypes.CDLL:
         L.derf_get_stats.restype = ctypes.c_int
         L.derf_reset_stats.argtypes = [P]
         L.derf_reset_stats.restype = ctypes.c_int
-        N, I, D = ctypes.c_longlong, ctypes.c_int, ctypes.c_double
+        N, I, D, F = ctypes.c_longlong, ctypes.c_int, ctypes.c_double, ctypes.c_float
         for name, restype, argtypes in (
                 ("derf_route_workspace", N, [N, I, I]),
                 ("derf_route", I, [P, N, I, I, P, P, P, P, N, P]),
@@ -152,6 +153,9 @@ def lib() -> ctypes.CDLL:
                 ("derf_heads_gated_workspace", N, [N, I, I, I, I]),
                 ("derf_heads_gated_backward", I,
                  [P, N, P, N, P, N, P, P, N, I, I, I, I, I, P, N, P, P, P, N, P]),
+                ("derf_lookup", I, [P, N, P, N, N, I, F, I, P, N, P]),
+                ("derf_lookup_workspace", N, [N, N, I]),
+                ("derf_lookup_backward", I, [P, N, P, N, N, I, F, I, P, P, N, P]),
                 ("derf_adamw_create", I, [ctypes.POINTER(P), P, I, I]),
                 ("derf_adamw_step", I, [P, D, D, D, D, D, N, P, P]),
                 ("derf_adamw_destroy", None, [P])):

@@ -370,6 +370,40 @@ def gated_backward(dy: torch.Tensor, pre: torch.Tensor, x: torch.Tensor, weight:
     return out_x, out_weight, out_bias
 
 
+def lookup(table: torch.Tensor, ids: torch.Tensor, scale: float = 1.0,
+           out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Rows of a table [V, D] picked by ids (int32 [T]): out[t] = scale * table[ids[t]], zero
+    where an id is outside [0, V)."""
+    stride = _rows(table, "table")
+    V, D = table.shape
+    if V < 1:
+        raise ValueError("table has no rows")
+    if not isinstance(ids, torch.Tensor) or ids.dim() != 1:
+        raise ValueError("ids must be a tensor [T]")
+    _array(ids, "ids", torch.int32, ids.shape, table.device)
+    out, out_stride = _out_rows(out, "out", ids.shape[0], D, table)
+    _call("derf_lookup", table.device, table.data_ptr(), stride, ids.data_ptr(), ids.shape[0], V, D,
+          scale, _PRECISION[table.dtype], out.data_ptr(), out_stride)
+    return out
+
+
+def lookup_backward(dout: torch.Tensor, ids: torch.Tensor, num_rows: int, scale: float = 1.0,
+                    out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Gradient of lookup in the table, float32 [num_rows, D]: each row's samples summed, times
+    scale; zero without any.  Samples go in a fixed order, so the sums repeat bit for bit."""
+    stride = _rows(dout, "dout")
+    T, D = dout.shape
+    _array(ids, "ids", torch.int32, (T,), dout.device)
+    need = _workspace_bytes("derf_lookup_workspace", T, num_rows, D)
+    if need < 0:
+        raise ValueError("invalid sizes: %d samples, %d rows of %d" % (T, num_rows, D))
+    out = _out_array(out, "out", (num_rows, D), dout.device)
+    ws = _workspace(need, dout.device)
+    _call("derf_lookup_backward", dout.device, dout.data_ptr(), stride, ids.data_ptr(), T, num_rows, D,
+          scale, _PRECISION[dout.dtype], out.data_ptr(), _ptr(ws), need)
+    return out
+
+
 class AdamW:
     """AdamW over lists of tensors, in one launch a step (derf_adamw_create).
 

@@ -1,4 +1,4 @@
-"""What the heads' gated layers refuse at the C entries and in Python, before any GPU work."""
+"""What the heads' gated layers and table lookups refuse at the C entries and in Python, before any GPU work."""
 import pytest
 import torch
 
@@ -72,5 +72,52 @@ def test_gated_arrays():
 def test_gated_refuses_host_tensors():
     x, w, off = torch.zeros((4, 8)), torch.zeros((3, 2, 5, 8)), torch.zeros(4, dtype=torch.int32)
     for call in (lambda: heads.gated(x, w, None, off), lambda: heads.gated_backward(x, x, x, w, off)):
+        with pytest.raises(ValueError):
+            call()
+
+
+# ---- lookups --------------------------------------------------------------------------
+
+@pytest.mark.parametrize("T,V,D,scale,prec", [(-1, 4, 8, 1.0, 0), (1 << 31, 4, 8, 1.0, 0), (4, 0, 8, 1.0, 0), (4, 1 << 31, 8, 1.0, 0),
+                                              (4, 4, 0, 1.0, 0), (4, 4, 65537, 1.0, 1)])
+def test_lookup_sizes(T, V, D, scale, prec):
+    L = lib()
+    assert L.derf_lookup_workspace(T, V, D) == -1
+    assert L.derf_lookup(P, 1 << 17, P, T, V, D, scale, prec, P, 1 << 17, None) == INVALID
+    assert L.derf_lookup_backward(P, 1 << 17, P, T, V, D, scale, prec, P, P, 1 << 60, None) == INVALID
+
+
+def test_lookup_arrays():
+    L = lib()
+
+    def forward(table=P, ts=8, ids=P, scale=1.0, prec=0, out=P, os=8):
+        return L.derf_lookup(table, ts, ids, 4, 5, 8, scale, prec, out, os, None)
+
+    def backward(dout=P, ds=8, ids=P, scale=1.0, prec=0, out=P, ws=P, n=1 << 40):
+        return L.derf_lookup_backward(dout, ds, ids, 4, 5, 8, scale, prec, out, ws, n, None)
+
+    refused(forward(table=None), b"null table")
+    refused(forward(ts=7), b"stride")
+    refused(forward(ids=P + 2), b"ids is not aligned")
+    refused(forward(ids=None), b"null ids")
+    refused(forward(scale=float("nan")), b"scale")
+    refused(forward(prec=2), b"precision")
+    refused(forward(out=None), b"null out")
+    refused(forward(os=7), b"stride")
+    refused(backward(dout=None), b"null dout")
+    refused(backward(ds=-8), b"stride")
+    refused(backward(ids=None), b"null ids")
+    refused(backward(scale=float("inf")), b"scale")
+    refused(backward(out=P + 2), b"out is not aligned")
+    need = L.derf_lookup_workspace(4, 5, 8)
+    assert need > 0
+    refused(backward(n=need - 1), b"workspace")
+    refused(backward(ws=None), b"workspace")
+    assert L.derf_lookup(None, 8, None, 0, 5, 8, 1.0, 0, None, 8, None) == derf.DERF_OK
+
+
+def test_lookup_refuses_host_tensors():
+    x, ids = torch.zeros((4, 8)), torch.zeros(4, dtype=torch.int32)
+    for call in (lambda: heads.lookup(x, ids), lambda: heads.lookup_backward(x, ids, 5)):
         with pytest.raises(ValueError):
             call()
