@@ -590,6 +590,57 @@ int derf_adamw_step(derf_adamw *opt, double lr, double beta1, double beta2, doub
 /* Waits for the optimizer's device, then frees the table.  NULL is a no-op. */
 void derf_adamw_destroy(derf_adamw *opt);
 
+/* Matrices orthogonalised: x / (|x| + 1e-7), |x| the Frobenius norm, then `iterations`
+ * times X = a X + (b S + c S^2) X with S = X X^T (of the transpose where fan_out >
+ * fan_in) and (a, b, c) = (3.4445, -4.7750, 2.0315), which brings the singular values
+ * near 1 (five iterations: those above a few hundredths of the norm into about
+ * [0.7, 1.2]) and keeps the directions.
+ *   x, out   [num_matrices][fan_out][fan_in] of one type, contiguous
+ *   float: as exact as the iteration in fp32; bf16: operands of 11 bits, sums in fp32.
+ *   Entries of X count down to 2^-36 (a norm far below 1e-7 leaves smaller ones)
+ *   workspace  derf_orthogonalise_workspace(...) bytes (-1 for invalid sizes)
+ * 0 <= num_matrices <= 32768, fan_out, fan_in in [1, 16384], iterations in [1, 20]. */
+long long derf_orthogonalise_workspace(long long num_matrices, int fan_out, int fan_in,
+                                       int precision);
+int derf_orthogonalise(const void *x, long long num_matrices, int fan_out, int fan_in,
+                       int iterations, int precision, void *out, void *workspace,
+                       long long workspace_bytes, void *hip_stream);
+
+/* Steps along orthogonalised directions, for the heads' weight matrices (biases and
+ * other vectors go with AdamW).  Per matrix, with g = *grad_scale * grad:
+ *   m = momentum m + g,   u = g + momentum m (nesterov) or m,
+ *   p = (1 - lr weight_decay) p - lr sqrt(max(1, fan_out / fan_in)) X,
+ * X being u after derf_orthogonalise's iteration, with its exactness by the type of
+ * param.
+ * A tensor:
+ *   param, grad   [num_matrices][fan_out][fan_in], float or bf16 each
+ *   m             float, the same shape; zeros at the start
+ *   copy          NULL, or bf16: the updated parameters rounded
+ * num_matrices <= 32768 in all tensors together, fan_out, fan_in in [1, 16384]. */
+typedef struct {
+    void *param;
+    const void *grad;
+    float *m;
+    void *copy;
+    int num_matrices;
+    int fan_out;
+    int fan_in;
+    int param_precision;
+    int grad_precision;
+} derf_muon_tensor;
+typedef struct derf_muon derf_muon;
+/* As derf_adamw_create: the optimizer belongs to the current device and keeps the
+ * addresses; it holds the steps' workspace (matrices of one padded shape together, at
+ * most 8 GiB of them or one at a time), so its steps follow one another: on one stream,
+ * or waited for. */
+int derf_muon_create(derf_muon **out, const derf_muon_tensor *tensors, int num_tensors);
+/* momentum in [0, 1).  As derf_adamw_step: grad_scale a device float or NULL,
+ * DERF_ERR_INVALID_ARG while hip_stream is being captured (lr is the call's). */
+int derf_muon_step(derf_muon *opt, double lr, double momentum, int nesterov, double weight_decay,
+                   int iterations, const float *grad_scale, void *hip_stream);
+/* Waits for the optimizer's device, then frees its memory.  NULL is a no-op. */
+void derf_muon_destroy(derf_muon *opt);
+
 /* Waits for the handle's last stream, then frees everything.  NULL is a no-op. */
 void derf_destroy(derf_handle *h);
 

@@ -24,7 +24,7 @@ SOURCES = ["mlp_8x256.hip", "mlp_8x128.hip", "mlp_8x128_split.hip", "mlp_8x128_f
            "mlp_4x64_split.hip", "mlp_4x64_f32.hip", "kernels_sample.hip",
            "kernels_fine.hip", "kernels_soft.hip", "kernels_gate.hip", "kernels_route.hip",
            "kernels_linear.hip", "kernels_gated.hip", "kernels_gated_back.hip",
-           "kernels_lookup.hip", "kernels_adamw.hip", "ops_api.cpp", "heads_api.cpp", "derf_api.cpp"]
+           "kernels_lookup.hip", "kernels_muon.hip", "kernels_adamw.hip", "ops_api.cpp", "heads_api.cpp", "derf_api.cpp"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "--offload-arch=" + ARCH,
           "-I" + os.path.join(ROOT, "include"), "-I" + CSRC,

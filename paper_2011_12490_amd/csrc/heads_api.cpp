@@ -4,6 +4,10 @@
 
 #include <math.h>
 
+#include <algorithm>
+#include <new>
+#include <vector>
+
 using namespace derf;
 
 namespace {
@@ -39,6 +43,45 @@ int check_lookup(long long samples, long long rows, int dim, float scale, int pr
     if (!isfinite(scale))
         return report(DERF_ERR_INVALID_ARG, "scale is not finite");
     return DERF_OK;
+}
+
+constexpr long long kMaxMatrices = 32768;
+constexpr int kMaxSide = 16384;
+constexpr int kMaxIterations = 20;
+constexpr size_t kMostWorkspace = 8ull << 30;  // of an optimizer, but for a matrix that needs more
+
+bool matrices_valid(long long matrices, int fan_out, int fan_in)
+{
+    return matrices >= 0 && matrices <= kMaxMatrices && fan_out >= 1 && fan_out <= kMaxSide && fan_in >= 1 && fan_in <= kMaxSide;
+}
+
+// Matrices of a table that go together: of one padded shape and exactness.
+struct MuonGroup {
+    unsigned first, count;
+    int fan_out, fan_in;
+    bool split;
+};
+
+int padded_side(int n) { return (n + 63) / 64 * 64; }
+
+}  // namespace
+
+struct derf_muon {
+    MuonEntry *table = nullptr;  // device memory, as the workspace
+    void *workspace = nullptr;
+    int device = -1;
+    std::vector<MuonGroup> groups;
+};
+
+namespace {
+
+void free_muon(derf_muon *opt)
+{
+    if (opt->table)
+        (void)device_free(opt->table);
+    if (opt->workspace)
+        (void)device_free(opt->workspace);
+    delete opt;
 }
 
 }  // namespace
@@ -146,6 +189,153 @@ int derf_lookup_backward(const void *dout, long long dout_stride, const int *ids
     return launched(launch_lookup_backward({dout, dout_stride}, ids, (unsigned)num_samples, (unsigned)num_rows, dim, scale,
                                            precision == DERF_PREC_BF16, out, workspace, static_cast<hipStream_t>(hip_stream)),
                     "derf_lookup_backward");
+}
+
+long long derf_orthogonalise_workspace(long long num_matrices, int fan_out, int fan_in,
+                                       int precision)
+{
+    if (!matrices_valid(num_matrices, fan_out, fan_in) || !is_precision(precision))
+        return -1;
+    return (long long)muon_workspace_bytes(fan_out, fan_in, precision == DERF_PREC_FP32, (unsigned)num_matrices);
+}
+
+int derf_orthogonalise(const void *x, long long num_matrices, int fan_out, int fan_in,
+                       int iterations, int precision, void *out, void *workspace,
+                       long long workspace_bytes, void *hip_stream)
+{
+    if (!matrices_valid(num_matrices, fan_out, fan_in))
+        return report(DERF_ERR_INVALID_ARG, "need 0 <= num_matrices <= %lld, fan_out and fan_in in [1, %d]", kMaxMatrices, kMaxSide);
+    if (!is_precision(precision))
+        return report(DERF_ERR_INVALID_ARG, "unknown precision %d", precision);
+    if (iterations < 1 || iterations > kMaxIterations)
+        return report(DERF_ERR_INVALID_ARG, "iterations is %d, not in [1, %d]", iterations, kMaxIterations);
+    if (num_matrices == 0)
+        return DERF_OK;
+    const bool bf16 = precision == DERF_PREC_BF16;
+    TRY(check_array("x", x, bf16 ? 2 : 4));
+    TRY(check_array("out", out, bf16 ? 2 : 4));
+    TRY(check_workspace(workspace, workspace_bytes, derf_orthogonalise_workspace(num_matrices, fan_out, fan_in, precision)));
+    const MuonSet set = {nullptr, 0, {out, x, nullptr, nullptr, fan_out, fan_in, bf16, bf16, 1.0f}};
+    const MuonStep st = {0.0f, 1.0f, 0.0f, 0, 0, 0, iterations, nullptr};
+    return launched(launch_muon(set, (unsigned)num_matrices, fan_out, fan_in, !bf16, st, workspace,
+                                static_cast<hipStream_t>(hip_stream)),
+                    "derf_orthogonalise");
+}
+
+int derf_muon_create(derf_muon **out, const derf_muon_tensor *tensors, int num_tensors)
+{
+    if (!out)
+        return report(DERF_ERR_INVALID_ARG, "null out");
+    *out = nullptr;
+    if (num_tensors < 0 || num_tensors > 65536 || (num_tensors > 0 && !tensors))
+        return report(DERF_ERR_INVALID_ARG, "need 0 <= num_tensors <= 65536 and their array");
+    derf_muon *opt = nullptr;
+    try {
+        std::vector<MuonEntry> table;
+        long long matrices = 0;
+        for (int i = 0; i < num_tensors; ++i) {
+            const derf_muon_tensor &t = tensors[i];
+            if (!matrices_valid(t.num_matrices, t.fan_out, t.fan_in) || (matrices += t.num_matrices) > kMaxMatrices)
+                return report(DERF_ERR_INVALID_ARG, "tensor %d: %d matrices of %d x %d", i, t.num_matrices, t.fan_out, t.fan_in);
+            if (!is_precision(t.param_precision) || !is_precision(t.grad_precision))
+                return report(DERF_ERR_INVALID_ARG, "tensor %d: unknown precision", i);
+            const unsigned pa = t.param_precision == DERF_PREC_BF16 ? 2 : 4, ga = t.grad_precision == DERF_PREC_BF16 ? 2 : 4;
+            if (t.num_matrices > 0 && (!t.param || !t.grad || !t.m))
+                return report(DERF_ERR_INVALID_ARG, "tensor %d: a null array", i);
+            if (misaligned(t.param, pa) || misaligned(t.grad, ga) || misaligned(t.m, 4) || misaligned(t.copy, 2))
+                return report(DERF_ERR_INVALID_ARG, "tensor %d: an array is not aligned to its elements", i);
+            const long long size = (long long)t.fan_out * t.fan_in;
+            for (int k = 0; k < t.num_matrices; ++k)
+                table.push_back({static_cast<char *>(t.param) + k * size * pa, static_cast<const char *>(t.grad) + k * size * ga,
+                                 t.m + k * size, t.copy ? static_cast<char *>(t.copy) + k * size * 2 : nullptr, t.fan_out, t.fan_in,
+                                 t.param_precision == DERF_PREC_BF16, t.grad_precision == DERF_PREC_BF16,
+                                 (float)sqrt(std::max(1.0, (double)t.fan_out / t.fan_in))});
+        }
+        auto key = [](const MuonEntry &e) {
+            const int o = padded_side(e.fan_out), i = padded_side(e.fan_in);
+            return ((long long)std::min(o, i) << 32 | (long long)std::max(o, i) << 1) + (e.param_bf16 ? 0 : 1);
+        };
+        std::stable_sort(table.begin(), table.end(), [&](const MuonEntry &a, const MuonEntry &b) { return key(a) < key(b); });
+        opt = new derf_muon;
+        size_t workspace = 0;
+        for (size_t i = 0; i < table.size();) {
+            MuonGroup g = {(unsigned)i, 1, table[i].fan_out, table[i].fan_in, !table[i].param_bf16};
+            while (i + g.count < table.size() && key(table[i + g.count]) == key(table[i]) &&
+                   muon_workspace_bytes(g.fan_out, g.fan_in, g.split, g.count + 1) <= kMostWorkspace)
+                ++g.count;
+            workspace = std::max(workspace, muon_workspace_bytes(g.fan_out, g.fan_in, g.split, g.count));
+            opt->groups.push_back(g);
+            i += g.count;
+        }
+        hipError_t e = hipSuccess;
+        if (!table.empty()) {
+            const size_t bytes = table.size() * sizeof(MuonEntry);
+            e = hipGetDevice(&opt->device);
+            if (e == hipSuccess)
+                e = device_alloc(reinterpret_cast<void **>(&opt->table), bytes);
+            if (e == hipSuccess)
+                e = device_alloc(&opt->workspace, workspace);
+            if (e == hipSuccess)
+                e = hipMemcpy(opt->table, table.data(), bytes, hipMemcpyHostToDevice);
+        }
+        if (e != hipSuccess) {
+            (void)hipGetLastError();
+            free_muon(opt);
+            if (e == hipErrorOutOfMemory)
+                return report(DERF_ERR_OOM, "optimizer workspace of %zu bytes", workspace);
+            return report(DERF_ERR_HIP, "derf_muon_create: %s", hipGetErrorString(e));
+        }
+        *out = opt;
+        return DERF_OK;
+    } catch (const std::bad_alloc &) {
+        delete opt;  // nothing on the device yet
+        return report(DERF_ERR_OOM, "host memory");
+    }
+}
+
+int derf_muon_step(derf_muon *opt, double lr, double momentum, int nesterov, double weight_decay,
+                   int iterations, const float *grad_scale, void *hip_stream)
+{
+    if (!opt)
+        return report(DERF_ERR_INVALID_ARG, "null optimizer");
+    if (!(lr >= 0) || !isfinite(lr) || !(momentum >= 0 && momentum < 1) || !(weight_decay >= 0) || !isfinite(weight_decay))
+        return report(DERF_ERR_INVALID_ARG, "need finite lr, weight_decay >= 0 and momentum in [0, 1)");
+    if (iterations < 1 || iterations > kMaxIterations)
+        return report(DERF_ERR_INVALID_ARG, "iterations is %d, not in [1, %d]", iterations, kMaxIterations);
+    if (misaligned(grad_scale, 4))
+        return report(DERF_ERR_INVALID_ARG, "grad_scale is not aligned to its elements");
+    if (opt->groups.empty())
+        return DERF_OK;
+    const OnDevice on(opt->device);
+    if (on.status != hipSuccess)
+        return launched(on.status, "the optimizer's device");
+    // the rate goes into the launches, which a graph would repeat as it is
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    if (hipStreamIsCapturing(static_cast<hipStream_t>(hip_stream), &capture) != hipSuccess)
+        (void)hipGetLastError();
+    else if (capture != hipStreamCaptureStatusNone)
+        return report(DERF_ERR_INVALID_ARG, "the stream is being captured: a graph would repeat this step's rate");
+    const MuonStep st = {(float)momentum, (float)(1.0 - lr * weight_decay), (float)lr, 1, nesterov != 0, 1, iterations, grad_scale};
+    for (const MuonGroup &g : opt->groups) {
+        const MuonSet set = {opt->table, g.first, {}};
+        TRY(launched(launch_muon(set, g.count, g.fan_out, g.fan_in, g.split, st, opt->workspace,
+                                 static_cast<hipStream_t>(hip_stream)),
+                     "derf_muon_step"));
+    }
+    return DERF_OK;
+}
+
+void derf_muon_destroy(derf_muon *opt)
+{
+    if (!opt)
+        return;
+    if (opt->device >= 0) {
+        const OnDevice on(opt->device);
+        (void)hipDeviceSynchronize();
+        free_muon(opt);
+    } else {
+        delete opt;
+    }
 }
 
 }  // extern "C"

@@ -1,0 +1,497 @@
+// Orthogonalised updates.  A matrix u (a head's update) becomes X = u / (|u| + 1e-7), |u|
+// its Frobenius norm, and goes through steps
+//
+//   S = X X^T,   Q = a + b S + c S^2,   X = Q X,     (a, b, c) = (3.4445, -4.7750, 2.0315)
+//
+// which take every singular value s to a s + b s^3 + c s^5 and leave the directions: from
+// (0, 1] they come near 1.  X is taken with its shorter side as rows (u^T for a tall
+// matrix), padded with zeros to multiples of 64, which stay zeros.
+//
+// The products run on the fp16 matrix units.  All singular values stay below 1.21, so no
+// entry of X, S or Q is above 3.5 in magnitude, and they are held as fp16 values of 2^12
+// times themselves, far from fp16's limits.  For float32 updates each is held as two
+// fp16 values, the rounded one and the rest (22 bits), and a product is three: the steps
+// lose no more than they do in float32 (on matrices of 512 to 1,024 of normal values
+// 2.1e-6 of the result's norm off, 1.9e-6 in float32).  bf16 updates, whose own rounding
+// is 2^-9, take the first halves alone: 11 bits, 0.2 to 3e-3 off where bf16 products would
+// be 0.2 to 3e-2 off.
+#include "product.h"
+
+namespace derf {
+
+namespace {
+
+constexpr float kA = 3.4445f, kB = -4.7750f, kC = 2.0315f;
+constexpr float kUnit = 4096.0f;  // what 1 is held as
+constexpr double kNormEps = 1e-7;
+typedef _Float16 f16;
+typedef f16 f16x4 __attribute__((ext_vector_type(4)));
+
+// Matrix k of a set.
+__device__ __forceinline__ MuonEntry entry_of(const MuonSet &set, unsigned k)
+{
+    if (set.table)
+        return set.table[set.first + k];
+    MuonEntry t = set.one;
+    const long long at = (long long)k * t.fan_out * t.fan_in;
+    t.param = static_cast<char *>(t.param) + at * (t.param_bf16 ? 2 : 4);
+    t.grad = static_cast<const char *>(t.grad) + at * (t.grad_bf16 ? 2 : 4);
+    return t;
+}
+
+template <class T>
+struct __attribute__((packed, aligned(sizeof(T)))) Four {
+    T v[4];
+};
+__device__ __forceinline__ f32x4 read4(const void *p, bool bf16, long long i, int here)
+{
+    f32x4 x = {};
+    if (bf16) {
+        const __bf16 *a = static_cast<const __bf16 *>(p) + i;
+        if (here == 4) {
+            const Four<__bf16> f = *reinterpret_cast<const Four<__bf16> *>(a);
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                x[k] = (float)f.v[k];
+            return x;
+        }
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+            if (k < here)
+                x[k] = (float)a[k];
+        return x;
+    }
+    const float *a = static_cast<const float *>(p) + i;
+    if (here == 4) {
+        const Four<float> f = *reinterpret_cast<const Four<float> *>(a);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            x[k] = f.v[k];
+        return x;
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+        if (k < here)
+            x[k] = a[k];
+    return x;
+}
+template <class T>
+__device__ __forceinline__ void write4_as(T *a, f32x4 x, int here)
+{
+    if (here == 4) {
+        Four<T> f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            f.v[k] = (T)x[k];
+        *reinterpret_cast<Four<T> *>(a) = f;
+        return;
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k)
+        if (k < here)
+            a[k] = (T)x[k];
+}
+__device__ __forceinline__ void write4(void *p, bool bf16, long long i, f32x4 x, int here)
+{
+    if (bf16)
+        write4_as(static_cast<__bf16 *>(p) + i, x, here);
+    else
+        write4_as(static_cast<float *>(p) + i, x, here);
+}
+
+// The update of four values: u = g, or with momentum m = momentum m + g and u = g +
+// momentum m (nesterov) or m.  g: the gradient times *grad_scale.
+__device__ __forceinline__ f32x4 update_of(const MuonStep &st, f32x4 g, f32x4 m)
+{
+    if (!st.has_momentum)
+        return g;
+    return st.nesterov ? g + m * st.momentum : m;
+}
+
+// ---- momentum and norm ------------------------------------------------------------
+// A workgroup takes a chunk of a matrix: the new momentum is written and the squares of
+// the update summed, in 64 bits: no gradient is too large or too small for its norm.
+__global__ __launch_bounds__(256) void momentum_kernel(const MuonSet set, MuonStep st, unsigned chunk,
+                                                       double *squares)
+{
+    __shared__ double sums[4];
+    const MuonEntry t = entry_of(set, blockIdx.y);
+    const long long n = (long long)t.fan_out * t.fan_in;
+    const long long from = (long long)blockIdx.x * chunk, to = from + chunk < n ? from + chunk : n;
+    const float scale = st.grad_scale ? *st.grad_scale : 1.0f;
+    double sum = 0.0;
+    for (long long i = from + threadIdx.x * 4; i < to; i += 1024) {
+        const int here = to - i >= 4 ? 4 : (int)(to - i);
+        const f32x4 g = read4(t.grad, t.grad_bf16, i, here) * scale;
+        f32x4 m = {};
+        if (st.has_momentum) {
+            m = read4(t.m, false, i, here) * st.momentum + g;
+            write4(t.m, false, i, m, here);
+        }
+        const f32x4 u = update_of(st, g, m);
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            sum += (double)u[k] * (double)u[k];  // values that are not there are zero
+    }
+    for (int off = 32; off; off >>= 1)
+        sum += __shfl_xor(sum, off);
+    if ((threadIdx.x & 63) == 0)
+        sums[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    if (threadIdx.x == 0)
+        squares[(size_t)blockIdx.y * gridDim.x + blockIdx.x] = sums[0] + sums[1] + sums[2] + sums[3];
+}
+
+// 1 / (|u| + eps) from the chunks' squares, in every thread.
+__device__ __forceinline__ double inverse_norm(const double *squares, unsigned chunks)
+{
+    __shared__ double sums[4];
+    double sum = 0.0;
+    for (unsigned i = threadIdx.x; i < chunks; i += 256)
+        sum += squares[i];
+    for (int off = 32; off; off >>= 1)
+        sum += __shfl_xor(sum, off);
+    if ((threadIdx.x & 63) == 0)
+        sums[threadIdx.x >> 6] = sum;
+    __syncthreads();
+    return 1.0 / (sqrt(sums[0] + sums[1] + sums[2] + sums[3]) + kNormEps);
+}
+
+// ---- X's start, and the end -----------------------------------------------------------
+// A workgroup takes 64 x 64 values of the tensor; X holds tall matrices transposed.
+// Between the two forms they go through LDS, a row a few banks on from the one before.
+
+constexpr int kTurnRow = 68;  // floats
+
+// The planes of a matrix: rows x cols fp16 each, the rests behind the rounded values.
+struct Planes {
+    f16 *p;
+    long long matrix;  // values from a matrix to the next
+    unsigned rows, cols;
+};
+
+template <bool SPLIT>
+__global__ __launch_bounds__(256) void start_kernel(const MuonSet set, MuonStep st, const double *squares,
+                                                    unsigned chunks, Planes x)
+{
+    __shared__ __attribute__((aligned(16))) float tile[64][kTurnRow];
+    const MuonEntry t = entry_of(set, blockIdx.z);
+    const bool tall = t.fan_out > t.fan_in;
+    const unsigned r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;  // of X
+    const double inverse = inverse_norm(squares + (size_t)blockIdx.z * chunks, chunks);
+    const float scale = st.grad_scale ? *st.grad_scale : 1.0f;
+    const int o0 = (int)(tall ? c0 : r0), i0 = (int)(tall ? r0 : c0);  // of the tensor
+    const int c = (threadIdx.x & 15) * 4;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int r = k * 16 + threadIdx.x / 16;
+        const int left = t.fan_in - i0 - c, here = o0 + r < t.fan_out ? (left >= 4 ? 4 : left > 0 ? left : 0) : 0;
+        f32x4 v = {};
+        if (here > 0) {
+            const long long at = (long long)(o0 + r) * t.fan_in + i0 + c;
+            const f32x4 g = read4(t.grad, t.grad_bf16, at, here) * scale;
+            const f32x4 m = st.has_momentum ? read4(t.m, false, at, here) : f32x4{};
+            const f32x4 u = update_of(st, g, m);
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] = (float)((double)u[e] * inverse) * kUnit;
+        }
+        *reinterpret_cast<f32x4 *>(&tile[r][c]) = v;
+    }
+    __syncthreads();
+    f16 *out = x.p + blockIdx.z * x.matrix;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int r = k * 16 + threadIdx.x / 16;
+        f32x4 v;
+        if (tall)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] = tile[c + e][r];
+        else
+            v = *reinterpret_cast<const f32x4 *>(&tile[r][c]);
+        f16x4 hi, lo;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            hi[e] = (f16)v[e];
+            lo[e] = (f16)(v[e] - (float)hi[e]);
+        }
+        const size_t at = (size_t)(r0 + r) * x.cols + c0 + c;
+        *reinterpret_cast<f16x4 *>(out + at) = hi;
+        if (SPLIT)
+            *reinterpret_cast<f16x4 *>(out + (size_t)x.rows * x.cols + at) = lo;
+    }
+}
+
+// The parameters' step along X, or X itself as the result (no parameters).
+template <bool SPLIT>
+__global__ __launch_bounds__(256) void finish_kernel(const MuonSet set, MuonStep st, Planes x)
+{
+    __shared__ __attribute__((aligned(16))) float tile[64][kTurnRow];
+    const MuonEntry t = entry_of(set, blockIdx.z);
+    const bool tall = t.fan_out > t.fan_in;
+    const unsigned r0 = blockIdx.y * 64, c0 = blockIdx.x * 64;
+    const int o0 = (int)(tall ? c0 : r0), i0 = (int)(tall ? r0 : c0);
+    const int c = (threadIdx.x & 15) * 4;
+    const f16 *in = x.p + blockIdx.z * x.matrix;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int r = k * 16 + threadIdx.x / 16;
+        const size_t at = (size_t)(r0 + r) * x.cols + c0 + c;
+        f32x4 v = __builtin_convertvector(*reinterpret_cast<const f16x4 *>(in + at), f32x4);
+        if (SPLIT)
+            v += __builtin_convertvector(*reinterpret_cast<const f16x4 *>(in + (size_t)x.rows * x.cols + at), f32x4);
+        v *= 1.0f / kUnit;
+        if (tall)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                tile[c + e][r] = v[e];
+        else
+            *reinterpret_cast<f32x4 *>(&tile[r][c]) = v;
+    }
+    __syncthreads();
+    const float rate = st.rate * t.size;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+        const int r = k * 16 + threadIdx.x / 16;
+        const int left = t.fan_in - i0 - c, here = o0 + r < t.fan_out ? (left >= 4 ? 4 : left > 0 ? left : 0) : 0;
+        if (here <= 0)
+            continue;
+        const long long at = (long long)(o0 + r) * t.fan_in + i0 + c;
+        f32x4 v = *reinterpret_cast<const f32x4 *>(&tile[r][c]);
+        if (st.updates)
+            v = read4(t.param, t.param_bf16, at, here) * st.decay - v * rate;
+        write4(t.param, t.param_bf16, at, v, here);
+        if (t.copy)
+            write4(t.copy, true, at, v, here);
+    }
+}
+
+// ---- the steps' products ------------------------------------------------------------
+
+enum Kind { kGram, kSquare, kApply };
+
+// out = a product of P and Q for each matrix: S = X X^T (Gram: P, Q = X), Q = a + b S +
+// c S S (Square: P, Q = S; both results symmetric: tiles on and below the diagonal are
+// computed and written to both places), X = Q X (Apply: P = X, depth down its columns).
+// SPLIT: the product of the rounded values, and those of each with the other's rest, one
+// after the other into the same registers.
+template <class C, int KIND, bool SPLIT>
+__global__ __launch_bounds__(C::kThreads, 2) void step_kernel(Planes pm, Planes qm, Planes out, unsigned matrices)
+{
+    constexpr bool kSymmetric = KIND != kApply;
+    constexpr int kPasses = SPLIT ? 3 : 1, COLS = C::FP * 16;
+    __shared__ __attribute__((aligned(16))) char lds[C::kLds];
+    __shared__ __attribute__((aligned(16))) char results[C::WP * C::WQ * 16 * kPieceRow<f16, COLS>];
+    const unsigned row_tiles = (out.rows + C::TQ - 1) / C::TQ, col_tiles = (out.cols + C::TP - 1) / C::TP;
+    const unsigned each = kSymmetric ? row_tiles * (row_tiles + 1) / 2 : row_tiles * col_tiles;
+    const unsigned all = matrices * each, end = runs_end(all), depth = qm.cols;
+    static_assert(!kSymmetric || C::TP == C::TQ, "square tiles");
+    auto tile_at = [&](unsigned b, unsigned &matrix, unsigned &r0, unsigned &c0) {
+        const unsigned at = by_xcd(b, all);
+        if (at >= all)
+            return false;
+        matrix = at / each;
+        const unsigned in = at - matrix * each;
+        if (kSymmetric) {  // row by row of the triangle
+            unsigned row = (unsigned)((sqrtf(8.0f * (float)in + 1.0f) - 1.0f) * 0.5f);
+            while (row * (row + 1) / 2 > in)
+                --row;
+            while ((row + 1) * (row + 2) / 2 <= in)
+                ++row;
+            r0 = uniform(row) * C::TQ;
+            c0 = uniform(in - row * (row + 1) / 2) * C::TP;
+        } else {
+            const Place2 where = in_groups(in, row_tiles, col_tiles);
+            r0 = where.a * C::TQ;
+            c0 = where.b * C::TP;
+        }
+        return true;
+    };
+    unsigned ahead = blockIdx.x, pass = 0;
+    auto next_tile = [&](Pipe<C> &pipe) {
+        unsigned matrix, r0, c0;
+        for (; ahead < end; ahead += gridDim.x) {
+            if (!tile_at(ahead, matrix, r0, c0))
+                continue;
+            const f16 *p = pm.p + matrix * pm.matrix, *q = qm.p + matrix * qm.matrix;
+            if (pass == 1)
+                p += (size_t)pm.rows * pm.cols;
+            if (pass == 2)
+                q += (size_t)qm.rows * qm.cols;
+            const typename C::P::Source ps = {{p, pm.cols, nullptr, 0, pm.rows, (int)pm.cols}, c0};
+            const typename C::Q::Source qs = {{q, qm.cols, nullptr, 0, qm.rows, (int)qm.cols}, r0};
+            if (++pass == kPasses) {
+                pass = 0;
+                ahead += gridDim.x;
+            }
+            pipe.load_tile(ps, qs, depth);
+            return;
+        }
+        pipe.load_nothing();
+    };
+    const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int wp = (wave % C::WP) * COLS, wq = (wave / C::WP) * C::FQ * 16;
+    char *mine = results + wave * 16 * kPieceRow<f16, COLS>;
+    Pipe<C> pipe;
+    pipe.start(lds, next_tile);
+    for (unsigned b = blockIdx.x; b < end; b += gridDim.x) {
+        unsigned matrix, r0, c0;
+        if (!tile_at(b, matrix, r0, c0))
+            continue;
+        f32x4 acc[C::FP][C::FQ] = {};
+#pragma unroll 1
+        for (int n = 0; n < kPasses; ++n)
+#pragma unroll 1
+            for (unsigned k = 0; k < depth; k += C::kDepth)
+                pipe.step(acc, next_tile, [](auto &) {});
+        f16 *to = out.p + matrix * out.matrix;
+        const size_t rest = (size_t)out.rows * out.cols;
+        const f16 *s = qm.p + matrix * qm.matrix;
+#pragma unroll
+        for (int j = 0; j < C::FQ; ++j) {
+            const unsigned row = r0 + wq + j * 16 + (lane & 15);
+            f32x4 v[C::FP], lo[C::FP];
+#pragma unroll
+            for (int i = 0; i < C::FP; ++i) {
+                const unsigned col = c0 + wp + i * 16 + (lane >> 4) * 4;
+                v[i] = acc[i][j] * (1.0f / kUnit);
+                if (KIND == kSquare) {
+                    f32x4 old = {};
+                    if (row < out.rows && col < out.cols) {
+                        const size_t at = (size_t)row * out.cols + col;
+                        old = __builtin_convertvector(*reinterpret_cast<const f16x4 *>(s + at), f32x4);
+                        if (SPLIT)
+                            old += __builtin_convertvector(*reinterpret_cast<const f16x4 *>(s + rest + at), f32x4);
+                    }
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        v[i][k] = fmaf(kC, v[i][k], fmaf(kB, old[k], col + k == row ? kA * kUnit : 0.0f));
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    lo[i][k] = v[i][k] - (float)(f16)v[i][k];
+            }
+            write_16_rows<f16, COLS>(v, mine, r0 + wq + j * 16, out.rows, c0 + wp, out.cols, to, out.cols);
+            if (SPLIT)
+                write_16_rows<f16, COLS>(lo, mine, r0 + wq + j * 16, out.rows, c0 + wp, out.cols, to + rest, out.cols);
+            if (kSymmetric && r0 != c0)  // the same above the diagonal
+#pragma unroll
+                for (int i = 0; i < C::FP; ++i)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const unsigned col = c0 + wp + i * 16 + (lane >> 4) * 4 + k;
+                        if (row < out.rows && col < out.cols) {
+                            to[(size_t)col * out.cols + row] = (f16)v[i][k];
+                            if (SPLIT)
+                                to[rest + (size_t)col * out.cols + row] = (f16)lo[i][k];
+                        }
+                    }
+        }
+    }
+    arrived<0>();
+}
+
+// ---- launches --------------------------------------------------------------------------
+
+unsigned padded(int n) { return (unsigned)(n + 63) / 64 * 64; }
+size_t whole(size_t bytes) { return (bytes + 255) / 256 * 256; }
+
+// Sizes of a group of matrices of one padded shape.
+struct Sizes {
+    unsigned m, n;  // of X
+    unsigned chunk, chunks;
+    size_t squares, x, s;  // bytes of a matrix
+};
+Sizes sizes_of(int fan_out, int fan_in, bool split)
+{
+    Sizes z;
+    const unsigned o = padded(fan_out), i = padded(fan_in);
+    z.m = o < i ? o : i;
+    z.n = o < i ? i : o;
+    // chunks of the padded matrix, which are enough for every member of the group
+    const unsigned long long all = (unsigned long long)z.m * z.n;
+    unsigned long long chunk = (all / 256 + 1023) / 1024 * 1024;
+    z.chunk = (unsigned)(chunk < 4096 ? 4096 : chunk);
+    z.chunks = (unsigned)((all + z.chunk - 1) / z.chunk);
+    z.squares = z.chunks * sizeof(double);
+    z.x = all * (split ? 4 : 2);
+    z.s = (size_t)z.m * z.m * (split ? 4 : 2);
+    return z;
+}
+
+template <class C, int KIND, bool SPLIT>
+hipError_t launch_step(const Planes &p, const Planes &q, const Planes &out, unsigned matrices, hipStream_t s)
+{
+    const unsigned long long rows = (out.rows + C::TQ - 1) / C::TQ, cols = (out.cols + C::TP - 1) / C::TP;
+    const unsigned long long all = matrices * (KIND != kApply ? rows * (rows + 1) / 2 : rows * cols);
+    return launch_for<C>(all, [&](unsigned groups, unsigned) {
+        step_kernel<C, KIND, SPLIT><<<groups, C::kThreads, 0, s>>>(p, q, out, matrices);
+    });
+}
+
+template <int KIND, bool SPLIT>
+hipError_t step(const Planes &p, const Planes &q, const Planes &out, unsigned matrices, hipStream_t s)
+{
+    constexpr bool kDeep = KIND != kApply;
+    const unsigned long long large = (unsigned long long)matrices * ((out.rows + 255) / 256) * ((out.cols + 255) / 256);
+    if (large >= 256)
+        return launch_step<Product<f16, 256, 256, 4, 2, kDeep, true, false, true>, KIND, SPLIT>(p, q, out, matrices, s);
+    if (out.rows > 64)
+        return launch_step<Product<f16, 128, 128, 2, 2, kDeep, true, false, true>, KIND, SPLIT>(p, q, out, matrices, s);
+    return launch_step<Product<f16, 64, 64, 2, 2, kDeep, true, false, true>, KIND, SPLIT>(p, q, out, matrices, s);
+}
+
+template <bool SPLIT>
+hipError_t orthogonalise(const MuonSet &set, unsigned matrices, const Sizes &z, const MuonStep &st, char *ws,
+                         hipStream_t s)
+{
+    auto take = [&](size_t bytes) {
+        char *p = ws;
+        ws += whole(bytes * matrices);
+        return p;
+    };
+    double *squares = reinterpret_cast<double *>(take(z.squares));
+    auto planes = [&](size_t bytes, unsigned rows, unsigned cols) {
+        return Planes{reinterpret_cast<f16 *>(take(bytes)), (long long)(bytes / sizeof(f16)), rows, cols};
+    };
+    Planes x = planes(z.x, z.m, z.n), y = planes(z.x, z.m, z.n);
+    const Planes gram = planes(z.s, z.m, z.m), poly = planes(z.s, z.m, z.m);
+    momentum_kernel<<<dim3(z.chunks, matrices), 256, 0, s>>>(set, st, z.chunk, squares);
+    const dim3 tiles(z.n / 64, z.m / 64, matrices);
+    start_kernel<SPLIT><<<tiles, 256, 0, s>>>(set, st, squares, z.chunks, x);
+    hipError_t e = hipGetLastError();
+    for (int i = 0; i < st.iterations && e == hipSuccess; ++i) {
+        e = step<kGram, SPLIT>(x, x, gram, matrices, s);
+        if (e == hipSuccess)
+            e = step<kSquare, SPLIT>(gram, gram, poly, matrices, s);
+        if (e == hipSuccess)
+            e = step<kApply, SPLIT>(x, poly, y, matrices, s);
+        const Planes was = x;
+        x = y;
+        y = was;
+    }
+    if (e != hipSuccess)
+        return e;
+    finish_kernel<SPLIT><<<tiles, 256, 0, s>>>(set, st, x);
+    return hipGetLastError();
+}
+
+}  // namespace
+
+size_t muon_workspace_bytes(int fan_out, int fan_in, bool split, unsigned matrices)
+{
+    const Sizes z = sizes_of(fan_out, fan_in, split);
+    return whole(z.squares * matrices) + 2 * whole(z.x * matrices) + 2 * whole(z.s * matrices);
+}
+
+hipError_t launch_muon(const MuonSet &set, unsigned matrices, int fan_out, int fan_in, bool split,
+                       const MuonStep &st, void *workspace, hipStream_t s)
+{
+    const Sizes z = sizes_of(fan_out, fan_in, split);
+    char *ws = static_cast<char *>(workspace);
+    return split ? orthogonalise<true>(set, matrices, z, st, ws, s)
+                 : orthogonalise<false>(set, matrices, z, st, ws, s);
+}
+
+}  // namespace derf

@@ -95,47 +95,6 @@ __device__ __forceinline__ f32x4 activate(f32x4 g, int act)
     return v;
 }
 
-// 16 rows from row0 on of a wave's COLS results from column n0 on, below `last` and
-// `width`: lane 16 h + l has, of row l, columns 4 h + (0 .. 3) of each 16.  bf16 through
-// the wave's place in LDS (kPieceRow a row), for pieces of 16 bytes.
-template <class T, int COLS>
-constexpr int kPieceRow = sizeof(T) == 2 ? COLS * 2 + 16 : 1;
-template <class T, int COLS>
-__device__ __forceinline__ void write_16_rows(const f32x4 (&v)[COLS / 16], char *mine, unsigned row0, unsigned last, int n0,
-                                              int width, T *y, long long ys)
-{
-    constexpr int V = Type<T>::kVec, kPieces = COLS / V;  // of a row
-    const int lane = threadIdx.x & 63;
-    if constexpr (sizeof(T) == 4) {
-        const unsigned row = row0 + (lane & 15);
-#pragma unroll
-        for (int i = 0; i < COLS / 16; ++i) {
-            const int n = n0 + i * 16 + (lane >> 4) * 4;
-            if (row < last && n < width)
-                write_piece(y + (row * ys + n), __builtin_bit_cast(u32x4, v[i]), width - n, T{});
-        }
-        return;
-    }
-    const bool past = COLS * sizeof(T) >= 128 && past_caches(y, ys, width);
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-    for (int i = 0; i < COLS / 16; ++i)
-        store_values(mine + (lane & 15) * kPieceRow<T, COLS> + (i * 16 + (lane >> 4) * 4) * (int)sizeof(T), v[i], T{});
-    __builtin_amdgcn_wave_barrier();
-#pragma unroll
-    for (int i = 0; i < (16 * kPieces + 63) / 64; ++i) {
-        const int r = (i * 64 + lane) / kPieces, c = (i * 64 + lane) % kPieces * V;
-        if (16 * kPieces % 64 && r >= 16)
-            continue;
-        const u32x4 piece = *reinterpret_cast<const u32x4 *>(mine + r * kPieceRow<T, COLS> + c * (int)sizeof(T));
-        const unsigned row = row0 + r;
-        const int n = n0 + c;
-        if (row < last && n < width)
-            write_result(y + (row * ys + n), piece, width - n, past);
-    }
-    __builtin_amdgcn_wave_barrier();
-}
-
 // Of 16 rows: gates in the even results of acc, ups in the odd ones.  y = act(gate) up,
 // and, where `pre` is wanted, both as they are, the ups `width` columns behind the gates.
 template <class T, int PAIRS>

@@ -63,6 +63,36 @@ size_t lookup_workspace_bytes(unsigned samples, unsigned rows, int dim);
 hipError_t launch_lookup_backward(Rows dout, const int *ids, unsigned samples, unsigned rows, int dim, float scale, bool bf16,
                                   float *out, void *workspace, hipStream_t s);
 
+// ---- orthogonalised updates (kernels_muon.hip) ----------------------------------
+// A matrix: its parameters (or where the result goes), gradient, momentum and copy.
+struct MuonEntry {
+    void *param;
+    const void *grad;
+    float *m;
+    void *copy;
+    int fan_out, fan_in, param_bf16, grad_bf16;
+    float size;  // of its steps
+};
+// Matrices from table[first] on (device memory), or, without a table, some like `one`
+// that lie one after another.
+struct MuonSet {
+    const MuonEntry *table;
+    unsigned first;
+    MuonEntry one;
+};
+struct MuonStep {
+    float momentum, decay, rate;
+    int has_momentum, nesterov;
+    int updates;  // 0: the result itself is written
+    int iterations;
+    const float *grad_scale;  // device, or null
+};
+// Of matrices of one padded shape, those of fan_out x fan_in being one of them.  split:
+// products as exact as float32's.
+size_t muon_workspace_bytes(int fan_out, int fan_in, bool split, unsigned matrices);
+hipError_t launch_muon(const MuonSet &set, unsigned matrices, int fan_out, int fan_in, bool split, const MuonStep &st,
+                       void *workspace, hipStream_t s);
+
 // ---- AdamW (kernels_adamw.hip) ----------------------------------------------
 // Values of an 8-bit moment that share a scale.
 constexpr int kMomentBlock = 256;

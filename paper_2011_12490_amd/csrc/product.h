@@ -15,6 +15,7 @@ namespace {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
 typedef unsigned u32x4 __attribute__((ext_vector_type(4)));
 
@@ -135,6 +136,10 @@ struct Type;
 template <>
 struct Type<__bf16> {
     static constexpr int kVec = 8;  // elements of 16 bytes
+};
+template <>
+struct Type<_Float16> {
+    static constexpr int kVec = 8;
 };
 template <>
 struct Type<float> {
@@ -371,6 +376,7 @@ struct Tile {
     }
     static __device__ __forceinline__ unsigned bits(float x) { return __float_as_uint(x); }
     static __device__ __forceinline__ unsigned bits(__bf16 x) { return __builtin_bit_cast(unsigned short, x); }
+    static __device__ __forceinline__ unsigned bits(_Float16 x) { return __builtin_bit_cast(unsigned short, x); }
     static __device__ __forceinline__ u32x4 pack(const unsigned (&x)[V])
     {
         u32x4 v;
@@ -512,6 +518,10 @@ __device__ __forceinline__ f32x4 multiply(u32x4 p, u32x4 q, f32x4 c, __bf16)
 {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, p),
                                                    __builtin_bit_cast(bf16x8, q), c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x4 multiply(u32x4 p, u32x4 q, f32x4 c, _Float16)
+{
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, p), __builtin_bit_cast(f16x8, q), c, 0, 0, 0);
 }
 __device__ __forceinline__ f32x4 multiply(u32x4 p, u32x4 q, f32x4 c, float)
 {
@@ -786,15 +796,16 @@ template <class C>
 constexpr int kResultRow = C::FP * (C::kPair ? 8 : 16) * (int)sizeof(typename C::T) + 16;
 template <class C>
 constexpr int kResultBytes = sizeof(typename C::T) == 2 ? C::WP * C::WQ * 16 * kResultRow<C> : 16;
-__device__ __forceinline__ void store_values(char *to, f32x4 v, __bf16)
+template <class T>
+__device__ __forceinline__ void store_values(char *to, f32x4 v, T)
 {
     union {
-        __bf16 e[4];
+        T e[4];
         unsigned long long u;
     } x;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-        x.e[i] = (__bf16)v[i];
+        x.e[i] = (T)v[i];
     *reinterpret_cast<unsigned long long *>(to) = x.u;
 }
 __device__ __forceinline__ void store_values(char *to, f32x4 v, float) { *reinterpret_cast<f32x4 *>(to) = v; }
@@ -836,6 +847,47 @@ __device__ __forceinline__ void write_result(T *to, u32x4 v, int left, bool past
         __builtin_nontemporal_store(v, reinterpret_cast<u32x4 *>(to));
     else
         write_piece(to, v, left, T{});
+}
+
+// 16 rows from row0 on of a wave's COLS results from column n0 on, below `last` and
+// `width`: lane 16 h + l has, of row l, columns 4 h + (0 .. 3) of each 16.  bf16 through
+// the wave's place in LDS (kPieceRow a row), for pieces of 16 bytes.
+template <class T, int COLS>
+constexpr int kPieceRow = sizeof(T) == 2 ? COLS * 2 + 16 : 1;
+template <class T, int COLS>
+__device__ __forceinline__ void write_16_rows(const f32x4 (&v)[COLS / 16], char *mine, unsigned row0, unsigned last, int n0,
+                                              int width, T *y, long long ys)
+{
+    constexpr int V = Type<T>::kVec, kPieces = COLS / V;  // of a row
+    const int lane = threadIdx.x & 63;
+    if constexpr (sizeof(T) == 4) {
+        const unsigned row = row0 + (lane & 15);
+#pragma unroll
+        for (int i = 0; i < COLS / 16; ++i) {
+            const int n = n0 + i * 16 + (lane >> 4) * 4;
+            if (row < last && n < width)
+                write_piece(y + (row * ys + n), __builtin_bit_cast(u32x4, v[i]), width - n, T{});
+        }
+        return;
+    }
+    const bool past = COLS * sizeof(T) >= 128 && past_caches(y, ys, width);
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < COLS / 16; ++i)
+        store_values(mine + (lane & 15) * kPieceRow<T, COLS> + (i * 16 + (lane >> 4) * 4) * (int)sizeof(T), v[i], T{});
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < (16 * kPieces + 63) / 64; ++i) {
+        const int r = (i * 64 + lane) / kPieces, c = (i * 64 + lane) % kPieces * V;
+        if (16 * kPieces % 64 && r >= 16)
+            continue;
+        const u32x4 piece = *reinterpret_cast<const u32x4 *>(mine + r * kPieceRow<T, COLS> + c * (int)sizeof(T));
+        const unsigned row = row0 + r;
+        const int n = n0 + c;
+        if (row < last && n < width)
+            write_result(y + (row * ys + n), piece, width - n, past);
+    }
+    __builtin_amdgcn_wave_barrier();
 }
 
 // ---- launches ---------------------------------------------------------------------

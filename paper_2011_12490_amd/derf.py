@@ -62,6 +62,13 @@ class derf_adamw_tensor(ctypes.Structure):
                 ("grad_precision", ctypes.c_int)]
 
 
+class derf_muon_tensor(ctypes.Structure):
+    _fields_ = [("param", ctypes.c_void_p), ("grad", ctypes.c_void_p), ("m", ctypes.c_void_p),
+                ("copy", ctypes.c_void_p), ("num_matrices", ctypes.c_int), ("fan_out", ctypes.c_int),
+                ("fan_in", ctypes.c_int), ("param_precision", ctypes.c_int),
+                ("grad_precision", ctypes.c_int)]
+
+
 EXPORTS = ("derf_weights_count", "derf_create", "derf_create_mixed", "derf_head_arithmetic", "derf_render",
            "derf_render_debug", "derf_render_noalloc",
            "derf_render_soft", "derf_render_culled", "derf_set_empty_heads", "derf_set_gate",
@@ -72,7 +79,9 @@ EXPORTS = ("derf_weights_count", "derf_create", "derf_create_mixed", "derf_head_
            "derf_combine_backward", "derf_heads_linear", "derf_heads_linear_workspace",
            "derf_heads_linear_backward", "derf_heads_gated",
            "derf_heads_gated_workspace", "derf_heads_gated_backward",
-           "derf_lookup", "derf_lookup_workspace", "derf_lookup_backward", "derf_adamw_create", "derf_adamw_step",
+           "derf_lookup", "derf_lookup_workspace", "derf_lookup_backward",
+           "derf_orthogonalise_workspace", "derf_orthogonalise", "derf_muon_create",
+           "derf_muon_step", "derf_muon_destroy", "derf_adamw_create", "derf_adamw_step",
            "derf_adamw_destroy",
            "derf_status_string", "derf_last_error")
 
@@ -156,6 +165,11 @@ def lib() -> ctypes.CDLL:
                 ("derf_lookup", I, [P, N, P, N, N, I, F, I, P, N, P]),
                 ("derf_lookup_workspace", N, [N, N, I]),
                 ("derf_lookup_backward", I, [P, N, P, N, N, I, F, I, P, P, N, P]),
+                ("derf_orthogonalise_workspace", N, [N, I, I, I]),
+                ("derf_orthogonalise", I, [P, N, I, I, I, I, P, P, N, P]),
+                ("derf_muon_create", I, [ctypes.POINTER(P), P, I]),
+                ("derf_muon_step", I, [P, D, D, I, D, I, P, P]),
+                ("derf_muon_destroy", None, [P]),
                 ("derf_adamw_create", I, [ctypes.POINTER(P), P, I, I]),
                 ("derf_adamw_step", I, [P, D, D, D, D, D, N, P, P]),
                 ("derf_adamw_destroy", None, [P])):
@@ -443,6 +457,10 @@ def derf_destroy(h):
 
 def derf_adamw_destroy(opt):
     lib().derf_adamw_destroy(opt)
+
+
+def derf_muon_destroy(opt):
+    lib().derf_muon_destroy(opt)
 
 
 # ---- convenience ----------------------------------------------------------------

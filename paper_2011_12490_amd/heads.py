@@ -508,3 +508,99 @@ class AdamW:
             self.close()
         except Exception:
             pass
+
+
+def orthogonalise(x: torch.Tensor, iterations: int = 5, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """x's matrices (the last two dimensions) with their singular values brought near 1 and
+    their directions kept (derf_orthogonalise): float32 as exactly as the iteration in
+    float32, bfloat16 through operands of 11 bits.  x: contiguous, [fan_out, fan_in] or
+    [heads, fan_out, fan_in]; out: another tensor of its shape and type."""
+    if not isinstance(x, torch.Tensor) or x.dim() not in (2, 3) or x.dtype not in _PRECISION:
+        raise ValueError("x must be a float32 or bfloat16 tensor [fan_out, fan_in] or [heads, fan_out, fan_in]")
+    _array(x, "x", x.dtype, x.shape)
+    K, (O, I) = (x.shape[0] if x.dim() == 3 else 1), x.shape[-2:]
+    prec = _PRECISION[x.dtype]
+    need = _workspace_bytes("derf_orthogonalise_workspace", K, O, I, prec)
+    if need < 0:
+        raise ValueError("invalid sizes: %d matrices of %d x %d" % (K, O, I))
+    if out is None:
+        out = torch.empty_like(x)
+    else:
+        _array(out, "out", x.dtype, x.shape, x.device)
+    ws = _workspace(need, x.device)
+    _call("derf_orthogonalise", x.device, x.data_ptr(), K, O, I, iterations, prec, out.data_ptr(), _ptr(ws), need)
+    return out
+
+
+class Muon:
+    """Steps along orthogonalised directions over lists of weight tensors (derf_muon_create).
+
+    params and grads: contiguous float32 or bfloat16 tensors [fan_out, fan_in] or [heads,
+    fan_out, fan_in] of one GPU, each matrix orthogonalised for itself; the gradients are
+    read from these tensors at every step.  copies: bfloat16 tensors (or None in the place
+    of one) that receive the updated parameters rounded.  m: the momentum, float32 tensors
+    of the parameters' shapes, used in place; zeros unless given.  The optimizer holds its
+    workspace: its steps go on one stream, or are waited for.  Biases and other vectors
+    belong to AdamW."""
+
+    def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], lr: float = 0.02,
+                 momentum: float = 0.95, nesterov: bool = True, weight_decay: float = 0.0, iterations: int = 5,
+                 copies=None, m=None):
+        self.handle = None
+        self.params, self.grads = list(params), list(grads)
+        if not self.params or len(self.params) != len(self.grads):
+            raise ValueError("need parameters and as many gradients")
+        for name, given in (("copies", copies), ("m", m)):
+            if given is not None and len(given) != len(self.params):
+                raise ValueError("%s: one for each parameter" % name)
+        self.lr, self.momentum, self.nesterov = lr, momentum, bool(nesterov)
+        self.weight_decay, self.iterations = weight_decay, iterations
+        self.copies = list(copies) if copies is not None else [None] * len(self.params)
+        first = self.params[0]
+        if not isinstance(first, torch.Tensor):
+            raise ValueError("params[0] must be a torch tensor")
+        self.device = first.device
+        for i, (p, g, c) in enumerate(zip(self.params, self.grads, self.copies)):
+            for name, x in (("params", p), ("grads", g)):
+                if not isinstance(x, torch.Tensor) or x.dtype not in _PRECISION or x.dim() not in (2, 3):
+                    raise ValueError("%s[%d] must be a float32 or bfloat16 tensor of matrices" % (name, i))
+                _array(x, "%s[%d]" % (name, i), x.dtype, p.shape, self.device, leaf=True)
+            if c is not None:
+                _array(c, "copies[%d]" % i, torch.bfloat16, p.shape, self.device, leaf=True)
+        if m is None:
+            self.m = [torch.zeros(p.shape, dtype=torch.float32, device=self.device) for p in self.params]
+        else:
+            self.m = list(m)
+            for i, (p, x) in enumerate(zip(self.params, self.m)):
+                _array(x, "m[%d]" % i, torch.float32, p.shape, self.device, leaf=True)
+        table = (derf.derf_muon_tensor * len(self.params))()
+        for i, (p, g, c) in enumerate(zip(self.params, self.grads, self.copies)):
+            table[i] = derf.derf_muon_tensor(p.data_ptr(), g.data_ptr(), self.m[i].data_ptr(), _ptr(c),
+                                             p.shape[0] if p.dim() == 3 else 1, p.shape[-2], p.shape[-1],
+                                             _PRECISION[p.dtype], _PRECISION[g.dtype])
+        handle = ctypes.c_void_p()
+        with torch.cuda.device(self.device):
+            _check(derf.lib().derf_muon_create(ctypes.byref(handle), ctypes.cast(table, ctypes.c_void_p),
+                                               len(self.params)), "derf_muon_create")
+        self.handle = handle
+
+    def step(self, grad_scale: Optional[torch.Tensor] = None) -> None:
+        """One step.  grad_scale: float32 [1] on the GPU, a factor on every gradient.  Not while
+        the stream is being captured (a graph would repeat this step's rate): it raises."""
+        if self.handle is None:
+            raise ValueError("the optimizer is closed")
+        if grad_scale is not None:
+            _array(grad_scale, "grad_scale", torch.float32, (1,), self.device, leaf=True)
+        _call("derf_muon_step", self.device, self.handle, self.lr, self.momentum, int(self.nesterov),
+              self.weight_decay, self.iterations, _ptr(grad_scale))
+
+    def close(self):
+        if self.handle is not None and self.handle.value:
+            derf.derf_muon_destroy(self.handle)
+        self.handle = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass

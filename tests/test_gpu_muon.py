@@ -1,0 +1,238 @@
+"""Orthogonalised updates on the GPU against the iteration in float64.
+
+Tolerances are of norms (Frobenius), for each matrix.  The kernels' operands carry 22 bits
+(float32: two fp16 values) or 11 (bf16: one), sums are float32.  A plain float32 iteration
+has operands of 24 bits and the same sums, so what its roundings make of a matrix, the
+kernels' make 4 or 2^13 times as large; that much of the plain iteration's own error is
+allowed, and 2^-22 or 2^-11 for a matrix that it gets exactly.  Roundings r_k of a step reach
+the result as a sum of D_k r_k with the matrix's own sensitivities D_k, the same for both.
+Over many singular values a sum of squares of such sums is near its mean; of a matrix of few
+values one sample can be next to nothing (a 1 x 1 matrix of 1 comes out 3e-8 off in float32
+where its five steps' D_k r_k, 2^-24 each times up to 7.8 for the three terms of Q, make up to
+2e-6), so there the largest of 32 samples counts: the matrix and 31 others that differ by a
+factor of 1 + j 2^-18, whose D_k are the same to 2^-13.  Entries of X are held as fp16 values of
+2^12 times themselves, whose least step is 2^-24: each is off by up to 2^-37 however small it
+is (of a matrix whose norm is far below 1e-7 they are small), and a step takes that to 3.4445
+times as much at most, for small singular values: 3.4445^5 2^-37 in all.  Results in bf16 are rounded once
+more, 2^-8 of a value.  Momentum: three roundings of 2^-24 of the terms' magnitudes.
+"""
+import math
+
+import pytest
+import torch
+
+from paper_2011_12490_amd import heads
+from test_gpu_heads import BF16, FP32, HALF_ULP, gen, rand
+
+pytestmark = pytest.mark.gpu
+
+A, B, C = 3.4445, -4.7750, 2.0315
+SHAPES = [  # matrices, fan_out, fan_in
+    (1, 1, 1), (3, 1, 9), (2, 9, 1), (5, 8, 8), (1, 64, 64), (3, 63, 65), (2, 65, 64), (7, 128, 63), (16, 128, 128), (4, 100, 127),
+    (2, 128, 129), (2, 129, 128), (3, 64, 155), (2, 30, 700), (2, 700, 30), (2, 300, 701), (2, 701, 300), (1, 256, 256), (1, 257, 512),
+    (40, 192, 192), (70, 96, 200), (1, 1000, 1500), (9, 520, 512), (70, 260, 500), (300, 20, 30)]
+
+
+def iterated(x, iterations=5):
+    """In x's own type, matrix products and sums."""
+    x = x.mT if x.shape[-2] > x.shape[-1] else x
+    for _ in range(iterations):
+        s = x @ x.mT
+        x = A * x + (B * s + C * (s @ s)) @ x
+    return x
+
+
+def direction(u, dtype, iterations=5):
+    """The exact direction of each matrix of u (float64), and how far the kernels may be from it."""
+    x = u / (u.square().sum((-2, -1), keepdim=True).sqrt() + 1e-7)
+    want = iterated(x, iterations)
+    near = 32 if min(u.shape[-2:]) <= 32 else 1
+    of = 0.0
+    for j in range(near):
+        y = (x * (1 + j * 2.0 ** -18)).float()
+        off = iterated(y, iterations).double() - iterated(x * (1 + j * 2.0 ** -18), iterations)
+        of = torch.maximum(off.square().sum((-2, -1)).sqrt(), torch.as_tensor(of, dtype=torch.float64, device="cuda"))
+    norm = want.square().sum((-2, -1)).sqrt()
+    bits = 2 if dtype == FP32 else 13
+    floor = A ** iterations * 2.0 ** -37 * (u.shape[-2] * u.shape[-1]) ** 0.5
+    return want.mT if u.shape[-2] > u.shape[-1] else want, 2.0 ** bits * of + 2.0 ** (bits - 24) * norm + floor
+
+
+def spread(g, *shape):
+    """Matrices whose singular values span a few powers of e."""
+    K, O, I = shape
+    rank = min(O, I)
+    return rand(g, K, O, rank) * torch.exp(-4.0 * torch.arange(rank, device="cuda") / rank) @ rand(g, K, rank, I)
+
+
+def check(got, want, far, also=0.0):
+    off = (got.double() - want).square().sum((-2, -1)).sqrt()
+    bound = far + also + HALF_ULP[got.dtype] * want.square().sum((-2, -1)).sqrt()
+    assert bool((off <= bound).all()), "off by %s, allowed %s" % (off.tolist(), bound.tolist())
+
+
+@pytest.mark.parametrize("dtype", [FP32, BF16])
+@pytest.mark.parametrize("K,O,I", SHAPES)
+def test_orthogonalise(K, O, I, dtype):
+    g = gen(K + O + 3 * I)
+    x = (spread(g, K, O, I) * 10.0 ** rand(g, K, 1, 1)).to(dtype)
+    kept = x.clone()
+    got = heads.orthogonalise(x, out=torch.full_like(x, float("nan")))
+    check(got, *direction(x.double(), dtype))
+    assert torch.equal(x, kept)
+    want, far = direction(x[:1].double(), dtype)
+    check(heads.orthogonalise(x[0]), want[0], far[0])  # a matrix, alone
+
+
+def test_every_number_of_iterations():
+    g = gen(1)
+    for shape in ((2, 70, 150), (2, 60, 64)):
+        x = spread(g, *shape)
+        for n in (1, 2, 3, 8):
+            check(heads.orthogonalise(x, n), *direction(x.double(), FP32, n))
+
+
+def test_singular_values_come_near_one_and_directions_stay():
+    g = gen(2)
+    q, _ = torch.linalg.qr(rand(g, 200, 200).double())
+    r, _ = torch.linalg.qr(rand(g, 300, 300).double())
+    s = torch.linspace(0.05, 1.0, 200, dtype=torch.float64, device="cuda")  # above 2 % of the norm once divided by it
+    x = (q * s @ r[:200]).float()
+    y = heads.orthogonalise(x).double()
+    got = q.mT @ y @ r[:200].mT
+    values = got.diagonal()
+    # five steps take (0.0035, 1] into [0.68, 1.21]; here the smallest starts at 0.05 / 8.3
+    assert 0.65 < float(values.min()) and float(values.max()) < 1.21
+    assert float((got - torch.diag(values)).abs().max()) < 1e-3  # float32's input roundings, amplified up to 500 times
+
+
+@pytest.mark.parametrize("dtype", [FP32, BF16])
+@pytest.mark.parametrize("O,I", [(40, 100), (128, 128), (300, 200)])
+def test_zeros_extremes_and_matrices_that_are_not_finite(O, I, dtype):
+    g = gen(3)
+    x = spread(g, 8, O, I).to(dtype)
+    x[1] = 0
+    x[2] *= 1e30
+    x[3] *= 1e-20
+    x[4, 5, 7] = float("nan")
+    x[5, 0, 0] = float("inf")
+    x[6] = 0
+    x[6, 3, 4] = -2.0  # a single value: its matrix has one singular value
+    got = heads.orthogonalise(x)
+    want, far = direction(x.double(), dtype)
+    for k in (0, 1, 2, 3, 6, 7):
+        check(got[k], want[k], far[k])
+    assert not bool(got[1].any())
+    assert not bool(got[4].isfinite().any()) and bool(got[5].isnan().any())
+
+
+def formula(p, grad, m, scale, lr, momentum, nesterov, decay, dtype, iterations=5):
+    grad = grad.double() * scale
+    m = momentum * m.double() + grad
+    way, far = direction(grad + momentum * m if nesterov else m, dtype, iterations)
+    size = lr * math.sqrt(max(1.0, p.shape[-2] / p.shape[-1]))
+    return m, p.double() * (1 - lr * decay) - size * way, size * far
+
+
+@pytest.mark.parametrize("dtype,grad_dtype,copy,nesterov", [(FP32, FP32, True, True), (FP32, BF16, False, False),
+                                                            (BF16, BF16, False, True), (BF16, FP32, True, True)])
+def test_muon(dtype, grad_dtype, copy, nesterov):
+    """Tensors of many shapes, 2-D ones among them, over three steps with changing gradients."""
+    g = gen(4)
+    shapes = [(16, 128, 63), (3, 128, 128), (2, 70, 300), (300, 70), (5, 40, 24), (1, 256, 200), (64, 64), (2, 127, 120), (3, 33, 1)]
+    p = [(0.05 * rand(g, *s)).to(dtype) for s in shapes]
+    grads = [torch.empty(s, dtype=grad_dtype, device="cuda") for s in shapes]
+    copies = [torch.zeros(s, dtype=BF16, device="cuda") if i % 2 else None for i, s in enumerate(shapes)] if copy else None
+    lr, momentum, decay = 0.05, 0.9, 0.1
+    opt = heads.Muon(p, grads, lr, momentum, nesterov, decay, copies=copies)
+    scale = torch.tensor([0.7], device="cuda")
+    for step in range(3):
+        was = [(a.clone(), m.clone()) for a, m in zip(p, opt.m)]
+        for x in grads:
+            x.copy_(spread(g, *x.shape) if x.dim() == 3 else spread(g, 1, *x.shape)[0])
+        opt.step(scale if step != 1 else None)
+        for i, (a, m) in enumerate(was):
+            by = float(scale[0]) if step != 1 else 1.0
+            want_m, want, far = formula(a, grads[i], m, by, lr, momentum, nesterov, decay, dtype)
+            off = (opt.m[i].double() - want_m).abs()
+            assert bool((off <= 4 * 2.0 ** -24 * (momentum * m.double().abs() + by * grads[i].double().abs()) + 2.0 ** -126).all())
+            rounded = 3 * 2.0 ** -24 * want.square().sum((-2, -1)).sqrt()
+            check(p[i], want, far, rounded)
+            if copies and copies[i] is not None:
+                check(copies[i], want, far, rounded)
+                assert dtype == BF16 or torch.equal(copies[i], p[i].to(BF16))
+
+
+def test_a_head_whose_gradient_is_not_finite_hurts_no_other():
+    g = gen(5)
+    p, grad = [rand(g, 4, 70, 90), rand(g, 3, 64, 64)], [rand(g, 4, 70, 90), rand(g, 3, 64, 64)]
+    twin, twin_grad = [x.clone() for x in p], [x.clone() for x in grad]
+    grad[0][2, 3, 3] = float("nan")
+    grad[1][0] = 0
+    twin_grad[1][0] = 0
+    heads.Muon(p, grad, 0.1).step()
+    heads.Muon(twin, twin_grad, 0.1).step()
+    assert not bool(p[0][2].isfinite().any())
+    p[0][2] = twin[0][2]
+    assert all(torch.equal(a, c) for a, c in zip(p, twin))
+
+
+def test_same_bits_on_a_stream_and_from_a_graph():
+    """Eager, on another stream, and captured: twice into graphs that have workspaces of their own."""
+    g = gen(6)
+    for shape, dtype in (((3, 200, 130), FP32), ((5, 128, 100), BF16), ((2, 128, 128), FP32)):
+        x = spread(g, *shape).to(dtype)
+        want = heads.orthogonalise(x)
+        assert torch.equal(heads.orthogonalise(x), want)
+        s = torch.cuda.Stream()
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            there = heads.orthogonalise(x)
+        s.synchronize()
+        assert torch.equal(there, want)
+        graphs = [torch.cuda.CUDAGraph() for _ in range(2)]
+        outs = []
+        for graph in graphs:
+            with torch.cuda.graph(graph):
+                outs.append(heads.orthogonalise(x))
+        for _ in range(3):
+            x.copy_(spread(g, *shape))
+            want = heads.orthogonalise(x)
+            for graph in graphs:
+                graph.replay()
+            torch.cuda.synchronize()
+            assert all(torch.equal(out, want) for out in outs)
+
+
+def test_a_step_is_not_captured():
+    p, grad = [torch.ones(8, 8, device="cuda")], [torch.ones(8, 8, device="cuda")]
+    opt = heads.Muon(p, grad, 0.1)
+    other = torch.zeros(4, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        other += 1
+        with pytest.raises(ValueError):
+            opt.step()
+    before = p[0].clone()
+    graph.replay()
+    torch.cuda.synchronize()
+    assert torch.equal(p[0], before) and bool((other == 1).all())
+    opt.step()
+    assert not torch.equal(p[0], before)
+    opt.close()
+    with pytest.raises(ValueError):
+        opt.step()
+
+
+def test_python_refusals():
+    x = torch.ones(2, 8, 9, device="cuda")
+    vector = torch.ones(8, device="cuda")
+    for call in (lambda: heads.orthogonalise(vector), lambda: heads.orthogonalise(x.double()), lambda: heads.orthogonalise(x.mT),
+                 lambda: heads.orthogonalise(x, 0), lambda: heads.orthogonalise(x, 21), lambda: heads.orthogonalise(x, out=x[0]),
+                 lambda: heads.orthogonalise(x.clone().requires_grad_()), lambda: heads.Muon([], []), lambda: heads.Muon([x], []),
+                 lambda: heads.Muon([vector], [vector]), lambda: heads.Muon([x], [x[0]]), lambda: heads.Muon([x], [x], m=[x.bfloat16()]),
+                 lambda: heads.Muon([x], [x], copies=[x]), lambda: heads.Muon([x], [x], momentum=1.0).step(),
+                 lambda: heads.Muon([x], [x], lr=float("nan")).step(), lambda: heads.Muon([x], [x], iterations=0).step(),
+                 lambda: heads.Muon([x], [x]).step(grad_scale=vector)):
+        with pytest.raises(ValueError):
+            call()

@@ -1,4 +1,9 @@
-"""What the heads' gated layers and table lookups refuse at the C entries and in Python, before any GPU work."""
+"""What the heads' gated layers, table lookups and orthogonalised updates refuse at the C entries and in Python, before any GPU work."""
+import ctypes
+import os
+import shutil
+import subprocess
+
 import pytest
 import torch
 
@@ -119,5 +124,94 @@ def test_lookup_arrays():
 def test_lookup_refuses_host_tensors():
     x, ids = torch.zeros((4, 8)), torch.zeros(4, dtype=torch.int32)
     for call in (lambda: heads.lookup(x, ids), lambda: heads.lookup_backward(x, ids, 5)):
+        with pytest.raises(ValueError):
+            call()
+
+
+# ---- orthogonalised updates -------------------------------------------------------------
+
+@pytest.mark.parametrize("K,O,I,n,prec", [(-1, 8, 8, 5, 0), (32769, 8, 8, 5, 0), (4, 0, 8, 5, 0), (4, 8, 16385, 5, 0), (4, 8, 8, 5, 2)])
+def test_orthogonalise_sizes(K, O, I, n, prec):
+    L = lib()
+    assert L.derf_orthogonalise_workspace(K, O, I, prec) == -1
+    assert L.derf_orthogonalise(P, K, O, I, n, prec, P, P, 1 << 60, None) == INVALID
+
+
+def test_orthogonalise_arrays():
+    L = lib()
+
+    def call(x=P, n=5, out=P, ws=P, size=1 << 50):
+        return L.derf_orthogonalise(x, 3, 40, 50, n, 0, out, ws, size, None)
+
+    refused(call(x=None), b"null x")
+    refused(call(x=P + 2), b"x is not aligned")
+    refused(call(n=0), b"iterations")
+    refused(call(n=21), b"iterations")
+    refused(call(out=None), b"null out")
+    need = L.derf_orthogonalise_workspace(3, 40, 50, 0)
+    refused(call(size=need - 1), b"workspace")
+    refused(call(ws=P + 8), b"workspace")
+    assert L.derf_orthogonalise(None, 0, 40, 50, 5, 0, None, None, 1 << 30, None) == derf.DERF_OK
+
+
+def _matrices(**kw):
+    t = dict(param=P, grad=P, m=P, copy=None, num_matrices=2, fan_out=8, fan_in=9, param_precision=0, grad_precision=0)
+    t.update(kw)
+    return derf.derf_muon_tensor(**t)
+
+
+@pytest.mark.parametrize("kw,text", [
+    (dict(num_matrices=-1), b"matrices"), (dict(num_matrices=32769), b"matrices"), (dict(fan_out=0), b"matrices"),
+    (dict(fan_in=16385), b"matrices"), (dict(param=None), b"null array"), (dict(grad=None), b"null array"), (dict(m=None), b"null array"),
+    (dict(param_precision=2), b"precision"), (dict(grad_precision=-1), b"precision"), (dict(m=P + 2), b"aligned"),
+    (dict(copy=P + 1), b"aligned"), (dict(grad=P + 2), b"aligned")])
+def test_muon_tensors(kw, text):
+    h = ctypes.c_void_p(1)
+    t = _matrices(**kw)
+    refused(lib().derf_muon_create(ctypes.byref(h), ctypes.byref(t), 1), text)
+    assert not h.value
+
+
+def test_muon_calls():
+    L = lib()
+    h = ctypes.c_void_p(1)
+    refused(L.derf_muon_create(None, None, 0), b"null out")
+    refused(L.derf_muon_create(ctypes.byref(h), None, 1), b"num_tensors")
+    refused(L.derf_muon_create(ctypes.byref(h), None, -1), b"num_tensors")
+    refused(L.derf_muon_step(None, 0.1, 0.9, 1, 0.0, 5, None, None), b"null optimizer")
+    L.derf_muon_destroy(None)
+    # an optimizer of no matrices needs no GPU: its scalars are still checked
+    empty = _matrices(num_matrices=0, param=None, grad=None, m=None)
+    assert L.derf_muon_create(ctypes.byref(h), ctypes.byref(empty), 1) == derf.DERF_OK
+    good = dict(lr=0.02, momentum=0.9, nesterov=1, weight_decay=0.0, iterations=5)
+    for kw in (dict(lr=-1.0), dict(lr=float("nan")), dict(momentum=1.0), dict(momentum=-0.1), dict(weight_decay=float("inf")),
+               dict(iterations=0), dict(iterations=21)):
+        assert L.derf_muon_step(h, *dict(good, **kw).values(), None, None) == INVALID, kw
+    refused(L.derf_muon_step(h, *good.values(), P + 2, None), b"grad_scale")
+    assert L.derf_muon_step(h, *good.values(), None, None) == derf.DERF_OK
+    L.derf_muon_destroy(h)
+
+
+def test_muon_tensor_has_the_headers_layout(tmp_path):
+    """A C program prints the struct's size and offsets; the binding's mirror has the same."""
+    cc = shutil.which("gcc")
+    if cc is None:
+        pytest.skip("no gcc")
+    mirror = derf.derf_muon_tensor
+    names = [f[0] for f in mirror._fields_]
+    prints = "".join('printf(" %%zu", offsetof(derf_muon_tensor, %s));\n' % n for n in names)
+    source = tmp_path / "layout.c"
+    source.write_text('#include <stddef.h>\n#include <stdio.h>\n#include "derf.h"\n'
+                      'int main(void) {\nprintf("%zu", sizeof(derf_muon_tensor));\n' + prints + "return 0;\n}\n")
+    program = str(tmp_path / "layout")
+    include = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include")
+    subprocess.run([cc, "-I", include, str(source), "-o", program], check=True)
+    got = [int(v) for v in subprocess.run([program], check=True, capture_output=True, text=True).stdout.split()]
+    assert got == [ctypes.sizeof(mirror)] + [getattr(mirror, n).offset for n in names]
+
+
+def test_muon_refuses_host_tensors():
+    x = torch.zeros((4, 8))
+    for call in (lambda: heads.orthogonalise(x), lambda: heads.Muon([x], [x])):
         with pytest.raises(ValueError):
             call()
