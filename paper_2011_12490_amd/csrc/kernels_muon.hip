@@ -1,7 +1,7 @@
 // Orthogonalised updates.  A matrix u (a head's update) becomes X = u / (|u| + 1e-7), |u|
 // its Frobenius norm, and goes through steps
 //
-//   S = X X^T,   Q = a + b S + c S^2,   X = Q X,     (a, b, c) = (3.4445, -4.7750, 2.0315)
+//   S = X X^T,   Q = b S + c S^2,   X = a X + Q X,     (a, b, c) = (3.4445, -4.7750, 2.0315)
 //
 // which take every singular value s to a s + b s^3 + c s^5 and leave the directions: from
 // (0, 1] they come near 1.  X is taken with its shorter side as rows (u^T for a tall
@@ -12,7 +12,9 @@
 // times themselves, far from fp16's limits.  For float32 updates each is held as two
 // fp16 values, the rounded one and the rest (22 bits), and a product is three: the steps
 // lose no more than they do in float32 (on matrices of 512 to 1,024 of normal values
-// 2.1e-6 of the result's norm off, 1.9e-6 in float32).  bf16 updates, whose own rounding
+// 2.1e-6 of the result's norm off, 1.9e-6 in float32).  a X is added in float32: with a in
+// Q's diagonal the matrix units' sums, whose roundings are those of their largest terms,
+// lose twice as much.  bf16 updates, whose own rounding
 // is 2^-9, take the first halves alone: 11 bits, 0.2 to 3e-3 off where bf16 products would
 // be 0.2 to 3e-2 off.
 #include "product.h"
@@ -271,9 +273,10 @@ __global__ __launch_bounds__(256) void finish_kernel(const MuonSet set, MuonStep
 
 enum Kind { kGram, kSquare, kApply };
 
-// out = a product of P and Q for each matrix: S = X X^T (Gram: P, Q = X), Q = a + b S +
+// out = a product of P and Q for each matrix: S = X X^T (Gram: P, Q = X), Q = b S +
 // c S S (Square: P, Q = S; both results symmetric: tiles on and below the diagonal are
-// computed and written to both places), X = Q X (Apply: P = X, depth down its columns).
+// computed and written to both places), X = a X + Q X (Apply: P = X, depth down its
+// columns).
 // SPLIT: the product of the rounded values, and those of each with the other's rest, one
 // after the other into the same registers.
 template <class C, int KIND, bool SPLIT>
@@ -347,7 +350,7 @@ __global__ __launch_bounds__(C::kThreads, 2) void step_kernel(Planes pm, Planes 
                 pipe.step(acc, next_tile, [](auto &) {});
         f16 *to = out.p + matrix * out.matrix;
         const size_t rest = (size_t)out.rows * out.cols;
-        const f16 *s = qm.p + matrix * qm.matrix;
+        const f16 *was = pm.p + matrix * pm.matrix;  // S, or X: of the result's shape
 #pragma unroll
         for (int j = 0; j < C::FQ; ++j) {
             const unsigned row = r0 + wq + j * 16 + (lane & 15);
@@ -356,17 +359,14 @@ __global__ __launch_bounds__(C::kThreads, 2) void step_kernel(Planes pm, Planes 
             for (int i = 0; i < C::FP; ++i) {
                 const unsigned col = c0 + wp + i * 16 + (lane >> 4) * 4;
                 v[i] = acc[i][j] * (1.0f / kUnit);
-                if (KIND == kSquare) {
-                    f32x4 old = {};
-                    if (row < out.rows && col < out.cols) {
-                        const size_t at = (size_t)row * out.cols + col;
-                        old = __builtin_convertvector(*reinterpret_cast<const f16x4 *>(s + at), f32x4);
-                        if (SPLIT)
-                            old += __builtin_convertvector(*reinterpret_cast<const f16x4 *>(s + rest + at), f32x4);
-                    }
+                if (KIND != kGram && row < out.rows && col < out.cols) {
+                    const size_t at = (size_t)row * out.cols + col;
+                    f32x4 old = __builtin_convertvector(*reinterpret_cast<const f16x4 *>(was + at), f32x4);
+                    if (SPLIT)
+                        old += __builtin_convertvector(*reinterpret_cast<const f16x4 *>(was + rest + at), f32x4);
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
-                        v[i][k] = fmaf(kC, v[i][k], fmaf(kB, old[k], col + k == row ? kA * kUnit : 0.0f));
+                        v[i][k] = KIND == kSquare ? fmaf(kC, v[i][k], kB * old[k]) : fmaf(kA, old[k], v[i][k]);
                 }
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
