@@ -251,15 +251,22 @@ int derf_muon_create(derf_muon **out, const derf_muon_tensor *tensors, int num_t
                                  t.param_precision == DERF_PREC_BF16, t.grad_precision == DERF_PREC_BF16,
                                  (float)sqrt(std::max(1.0, (double)t.fan_out / t.fan_in))});
         }
-        auto key = [](const MuonEntry &e) {
-            const int o = padded_side(e.fan_out), i = padded_side(e.fan_in);
+        auto small = [](const MuonEntry &e) { return e.fan_out <= 128 && e.fan_in <= 128; };
+        // few small matrices run at once whatever their shapes: 128 of 128 x 128 and 16 of
+        // 128 x 63 in one launch of 128 x 128 places KEY_ONE us, in two KEY_TWO
+        const bool as_one = std::count_if(table.begin(), table.end(), small) <= 256;
+        auto key = [&](const MuonEntry &e) {
+            int o = padded_side(e.fan_out), i = padded_side(e.fan_in);
+            if (as_one && small(e))
+                o = i = 128;
             return ((long long)std::min(o, i) << 32 | (long long)std::max(o, i) << 1) + (e.param_bf16 ? 0 : 1);
         };
         std::stable_sort(table.begin(), table.end(), [&](const MuonEntry &a, const MuonEntry &b) { return key(a) < key(b); });
         opt = new derf_muon;
         size_t workspace = 0;
         for (size_t i = 0; i < table.size();) {
-            MuonGroup g = {(unsigned)i, 1, table[i].fan_out, table[i].fan_in, !table[i].param_bf16};
+            const long long shape = key(table[i]) >> 1;  // padded sides
+            MuonGroup g = {(unsigned)i, 1, (int)(shape >> 31), (int)(shape & 0x7FFFFFFF), !table[i].param_bf16};
             while (i + g.count < table.size() && key(table[i + g.count]) == key(table[i]) &&
                    muon_workspace_bytes(g.fan_out, g.fan_in, g.split, g.count + 1) <= kMostWorkspace)
                 ++g.count;
@@ -273,7 +280,7 @@ int derf_muon_create(derf_muon **out, const derf_muon_tensor *tensors, int num_t
             e = hipGetDevice(&opt->device);
             if (e == hipSuccess)
                 e = device_alloc(reinterpret_cast<void **>(&opt->table), bytes);
-            if (e == hipSuccess)
+            if (e == hipSuccess && workspace > 0)
                 e = device_alloc(&opt->workspace, workspace);
             if (e == hipSuccess)
                 e = hipMemcpy(opt->table, table.data(), bytes, hipMemcpyHostToDevice);

@@ -392,7 +392,267 @@ __global__ __launch_bounds__(C::kThreads, 2) void step_kernel(Planes pm, Planes 
     arrived<0>();
 }
 
+// ---- small matrices, all of it in one launch ----------------------------------------------
+
+// Matrices of up to 128 x 128: a workgroup takes one from its gradient to its parameters,
+// X and S (or Q in its place) in LDS.  Both lie row by row in 64-row tiles: their rows are
+// read as they lie, and X's columns for Q X by transposing reads.
+template <int M_, int N_, bool SPLIT>
+struct Small {
+    static constexpr int M = M_, N = N_, kPlanes = SPLIT ? 2 : 1, kThreads = M == 128 ? 512 : 256;
+    static constexpr int WP = 2, WQ = kThreads / 128, FQ = 2;  // waves over columns and rows, 16-row results of each
+    static_assert(WQ * FQ * 16 == M, "all rows");
+    using X = Tile<f16, N, false, kThreads, false>;
+    using S = Tile<f16, M, false, kThreads, false>;
+    static constexpr int kX = M * N * 2, kS = M * M * 2, kLds = kPlanes * (kX + kS);  // bytes
+    static constexpr int kVecs = M * N / 4 / kThreads;  // of a thread
+    // workgroups a compute unit by their LDS
+    static constexpr int kAtOnce = 160 * 1024 / (kLds + 256) < 4 ? 160 * 1024 / (kLds + 256) : 4;
+};
+
+// Four values side by side in a plane of tiles: row r, columns from c on.
+template <class TILE>
+__device__ __forceinline__ unsigned lds_at(int r, int c)
+{
+    return (r >> 6) * TILE::kBytes + TILE::at(r & 63, c >> 3) + (c & 4) * 2;
+}
+template <class TILE, bool SPLIT>
+__device__ __forceinline__ f32x4 read_lds(const char *plane, int plane_bytes, int r, int c)
+{
+    const unsigned at = lds_at<TILE>(r, c);
+    f32x4 v = __builtin_convertvector(*reinterpret_cast<const f16x4 *>(plane + at), f32x4);
+    if (SPLIT)
+        v += __builtin_convertvector(*reinterpret_cast<const f16x4 *>(plane + plane_bytes + at), f32x4);
+    return v;
+}
+template <class TILE, bool SPLIT>
+__device__ __forceinline__ void write_lds(char *plane, int plane_bytes, int r, int c, f32x4 v)
+{
+    const unsigned at = lds_at<TILE>(r, c);
+    const f16x4 hi = __builtin_convertvector(v, f16x4);
+    *reinterpret_cast<f16x4 *>(plane + at) = hi;
+    if (SPLIT)
+        *reinterpret_cast<f16x4 *>(plane + plane_bytes + at) = __builtin_convertvector(v - __builtin_convertvector(hi, f32x4), f16x4);
+}
+
+// acc[i][j] = sum over `depth` of P's and Q's 16-row results: P_READ, Q_READ (plane,
+// result, 32 deep part) give the matrix unit's operands.
+template <int FP, int FQ, bool SPLIT, class PRead, class QRead>
+__device__ __forceinline__ void small_product(int depth, f32x4 (&acc)[FP][FQ], PRead p_read, QRead q_read)
+{
+#pragma unroll 2
+    for (int part = 0; part < depth / 32; ++part) {
+        u32x4 p[FP], q[FQ];
+#pragma unroll
+        for (int j = 0; j < FQ; ++j)
+            q[j] = q_read(0, j, part);
+#pragma unroll
+        for (int i = 0; i < FP; ++i)
+            p[i] = p_read(0, i, part);
+#pragma unroll
+        for (int i = 0; i < FP; ++i)
+#pragma unroll
+            for (int j = 0; j < FQ; ++j)
+                acc[i][j] = multiply(p[i], q[j], acc[i][j], f16{});
+        if (SPLIT) {
+            u32x4 rest[FQ];
+#pragma unroll
+            for (int j = 0; j < FQ; ++j)
+                rest[j] = q_read(1, j, part);
+#pragma unroll
+            for (int i = 0; i < FP; ++i)
+#pragma unroll
+                for (int j = 0; j < FQ; ++j)
+                    acc[i][j] = multiply(p[i], rest[j], acc[i][j], f16{});
+#pragma unroll
+            for (int i = 0; i < FP; ++i)
+                p[i] = p_read(1, i, part);
+#pragma unroll
+            for (int i = 0; i < FP; ++i)
+#pragma unroll
+                for (int j = 0; j < FQ; ++j)
+                    acc[i][j] = multiply(p[i], q[j], acc[i][j], f16{});
+        }
+    }
+}
+
+template <class C, bool SPLIT>
+__global__ __launch_bounds__(C::kThreads, C::kAtOnce *C::kThreads / 256) void small_kernel(const MuonSet set, MuonStep st)
+{
+    using X = typename C::X;
+    using S = typename C::S;
+    constexpr int FQ = C::FQ, FS = C::M / 32, FX = C::N / 32;  // results of a wave: rows, columns of S, columns of X
+    __shared__ __attribute__((aligned(16))) char lds[C::kLds];
+    __shared__ double sums[C::kThreads / 64];
+    char *const x = lds, *const sq = lds + C::kPlanes * C::kX;
+    const MuonEntry t = entry_of(set, blockIdx.x);
+    const bool tall = t.fan_out > t.fan_in;
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const float scale = st.grad_scale ? *st.grad_scale : 1.0f;
+    const int vecs = (tall ? C::M : C::N) / 4;  // of a row of the tensor, padded
+    // vector k of this thread's: row o and column i of the tensor, elements there
+    auto place = [&](int k, int &o, int &i) {
+        const int n = k * C::kThreads + threadIdx.x;
+        o = n / vecs;
+        i = n % vecs * 4;
+        const int left = t.fan_in - i;
+        return o < t.fan_out && left > 0 ? (left < 4 ? left : 4) : 0;
+    };
+    {
+        f32x4 u[C::kVecs];
+        double sum = 0.0;
+#pragma unroll
+        for (int k = 0; k < C::kVecs; ++k) {
+            int o, i;
+            const int here = place(k, o, i);
+            u[k] = f32x4{};
+            if (here > 0) {
+                const long long at = (long long)o * t.fan_in + i;
+                const f32x4 g = read4(t.grad, t.grad_bf16, at, here) * scale;
+                f32x4 m = {};
+                if (st.has_momentum) {
+                    m = read4(t.m, false, at, here) * st.momentum + g;
+                    write4(t.m, false, at, m, here);
+                }
+                u[k] = update_of(st, g, m);
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                sum += (double)u[k][e] * (double)u[k][e];
+        }
+        for (int off = 32; off; off >>= 1)
+            sum += __shfl_xor(sum, off);
+        if (lane == 0)
+            sums[wave] = sum;
+        __syncthreads();
+        sum = 0.0;
+        for (int w = 0; w < C::kThreads / 64; ++w)
+            sum += sums[w];
+        const double inverse = 1.0 / (sqrt(sum) + kNormEps);
+#pragma unroll
+        for (int k = 0; k < C::kVecs; ++k) {
+            int o, i;
+            place(k, o, i);
+            f32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                v[e] = (float)((double)u[k][e] * inverse) * kUnit;
+            if (!tall) {
+                write_lds<X, SPLIT>(x, C::kX, o, i, v);
+                continue;
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                f16 *to = reinterpret_cast<f16 *>(x + lds_at<X>(i + e, o)) + (o & 3);
+                const f16 hi = (f16)v[e];
+                to[0] = hi;
+                if (SPLIT)
+                    to[C::kX / 2] = (f16)(v[e] - (float)hi);
+            }
+        }
+    }
+    __syncthreads();
+    const int wp = wave % C::WP, fq = wave / C::WP * FQ;
+    const int row = fq * 16 + (lane & 15), col = (lane >> 4) * 4;  // of the wave's first result; the next 16 on
+    auto x_rows = [&](int first) {
+        return [=](int plane, int i, int part) {
+            const int f = first + i;
+            return X::row_fragment(x + plane * C::kX + (f >> 2) * X::kBytes, f & 3, part);
+        };
+    };
+    auto s_rows = [&](int first) {
+        return [=](int plane, int i, int part) {
+            const int f = first + i;
+            return S::row_fragment(sq + plane * C::kS + (f >> 2) * S::kBytes, f & 3, part);
+        };
+    };
+#pragma unroll 1
+    for (int n = 0; n < st.iterations; ++n) {
+        {
+            f32x4 acc[FS][FQ] = {};
+            small_product<FS, FQ, SPLIT>(C::N, acc, x_rows(wp * FS), x_rows(fq));
+#pragma unroll
+            for (int i = 0; i < FS; ++i)
+#pragma unroll
+                for (int j = 0; j < FQ; ++j)
+                    write_lds<S, SPLIT>(sq, C::kS, row + j * 16, (wp * FS + i) * 16 + col, acc[i][j] * (1.0f / kUnit));
+        }
+        __syncthreads();
+        {
+            f32x4 acc[FS][FQ] = {};
+            small_product<FS, FQ, SPLIT>(C::M, acc, s_rows(wp * FS), s_rows(fq));
+#pragma unroll
+            for (int i = 0; i < FS; ++i)
+#pragma unroll
+                for (int j = 0; j < FQ; ++j) {
+                    const f32x4 old = read_lds<S, SPLIT>(sq, C::kS, row + j * 16, (wp * FS + i) * 16 + col);
+                    acc[i][j] = acc[i][j] * (kC / kUnit) + old * kB;
+                }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < FS; ++i)
+#pragma unroll
+                for (int j = 0; j < FQ; ++j)
+                    write_lds<S, SPLIT>(sq, C::kS, row + j * 16, (wp * FS + i) * 16 + col, acc[i][j]);
+        }
+        __syncthreads();
+        {
+            f32x4 acc[FX][FQ] = {};
+            auto x_columns = [&](int plane, int i, int part) {
+                return X::fragment(x + plane * C::kX + (part >> 1) * X::kBytes, wp * FX + i, part & 1);
+            };
+            small_product<FX, FQ, SPLIT>(C::M, acc, x_columns, s_rows(fq));
+#pragma unroll
+            for (int i = 0; i < FX; ++i)
+#pragma unroll
+                for (int j = 0; j < FQ; ++j) {
+                    const f32x4 old = read_lds<X, SPLIT>(x, C::kX, row + j * 16, (wp * FX + i) * 16 + col);
+                    acc[i][j] = acc[i][j] * (1.0f / kUnit) + old * kA;
+                }
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < FX; ++i)
+#pragma unroll
+                for (int j = 0; j < FQ; ++j)
+                    write_lds<X, SPLIT>(x, C::kX, row + j * 16, (wp * FX + i) * 16 + col, acc[i][j]);
+        }
+        __syncthreads();
+    }
+    const float rate = st.rate * t.size;
+#pragma unroll
+    for (int k = 0; k < C::kVecs; ++k) {
+        int o, i;
+        const int here = place(k, o, i);
+        if (here <= 0)
+            continue;
+        f32x4 v;
+        if (tall)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const f16 *from = reinterpret_cast<const f16 *>(x + lds_at<X>(i + e, o)) + (o & 3);
+                v[e] = (float)from[0] + (SPLIT ? (float)from[C::kX / 2] : 0.0f);
+            }
+        else
+            v = read_lds<X, SPLIT>(x, C::kX, o, i);
+        v *= 1.0f / kUnit;
+        const long long at = (long long)o * t.fan_in + i;
+        if (st.updates)
+            v = read4(t.param, t.param_bf16, at, here) * st.decay - v * rate;
+        write4(t.param, t.param_bf16, at, v, here);
+        if (t.copy)
+            write4(t.copy, true, at, v, here);
+    }
+}
+
 // ---- launches --------------------------------------------------------------------------
+
+template <int M, int N, bool SPLIT>
+hipError_t launch_small(const MuonSet &set, unsigned matrices, const MuonStep &st, hipStream_t s)
+{
+    using C = Small<M, N, SPLIT>;
+    small_kernel<C, SPLIT><<<matrices, C::kThreads, 0, s>>>(set, st);
+    return hipGetLastError();
+}
 
 unsigned padded(int n) { return (unsigned)(n + 63) / 64 * 64; }
 size_t whole(size_t bytes) { return (bytes + 255) / 256 * 256; }
@@ -482,6 +742,8 @@ hipError_t orthogonalise(const MuonSet &set, unsigned matrices, const Sizes &z, 
 size_t muon_workspace_bytes(int fan_out, int fan_in, bool split, unsigned matrices)
 {
     const Sizes z = sizes_of(fan_out, fan_in, split);
+    if (z.n <= 128)
+        return 0;  // all in LDS
     return whole(z.squares * matrices) + 2 * whole(z.x * matrices) + 2 * whole(z.s * matrices);
 }
 
@@ -489,6 +751,13 @@ hipError_t launch_muon(const MuonSet &set, unsigned matrices, int fan_out, int f
                        const MuonStep &st, void *workspace, hipStream_t s)
 {
     const Sizes z = sizes_of(fan_out, fan_in, split);
+    if (z.n <= 128) {
+        if (z.m == 128)
+            return split ? launch_small<128, 128, true>(set, matrices, st, s) : launch_small<128, 128, false>(set, matrices, st, s);
+        if (z.n == 128)
+            return split ? launch_small<64, 128, true>(set, matrices, st, s) : launch_small<64, 128, false>(set, matrices, st, s);
+        return split ? launch_small<64, 64, true>(set, matrices, st, s) : launch_small<64, 64, false>(set, matrices, st, s);
+    }
     char *ws = static_cast<char *>(workspace);
     return split ? orthogonalise<true>(set, matrices, z, st, ws, s)
                  : orthogonalise<false>(set, matrices, z, st, ws, s);
