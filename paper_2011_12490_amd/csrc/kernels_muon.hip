@@ -273,6 +273,71 @@ __global__ __launch_bounds__(256) void finish_kernel(const MuonSet set, MuonStep
 
 enum Kind { kGram, kSquare, kApply };
 
+// A wave's results, from row r and column c on, to both planes of `to` [rows][cols], with
+// what they are added to (was: S or X).  mirror: those of a symmetric matrix to the place
+// above the diagonal too.
+template <int KIND, bool SPLIT, int FP, int FQ>
+__device__ __forceinline__ void write_step(const f32x4 (&acc)[FP][FQ], const f16 *was, f16 *to, unsigned rows, unsigned cols, unsigned r,
+                                           unsigned c, char *mine, bool mirror)
+{
+    const int lane = threadIdx.x & 63;
+    const size_t rest = (size_t)rows * cols;
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) {
+        const unsigned row = r + j * 16 + (lane & 15);
+        f32x4 v[FP], lo[FP];
+#pragma unroll
+        for (int i = 0; i < FP; ++i) {
+            const unsigned col = c + i * 16 + (lane >> 4) * 4;
+            v[i] = acc[i][j] * (1.0f / kUnit);
+            if (KIND != kGram && row < rows && col < cols) {
+                const size_t at = (size_t)row * cols + col;
+                f32x4 old = __builtin_convertvector(*reinterpret_cast<const f16x4 *>(was + at), f32x4);
+                if (SPLIT)
+                    old += __builtin_convertvector(*reinterpret_cast<const f16x4 *>(was + rest + at), f32x4);
+#pragma unroll
+                for (int k = 0; k < 4; ++k)
+                    v[i][k] = KIND == kSquare ? fmaf(kC, v[i][k], kB * old[k]) : fmaf(kA, old[k], v[i][k]);
+            }
+            lo[i] = v[i] - __builtin_convertvector(__builtin_convertvector(v[i], f16x4), f32x4);
+        }
+        write_16_rows<f16, FP * 16>(v, mine, r + j * 16, rows, c, cols, to, cols);
+        if (SPLIT)
+            write_16_rows<f16, FP * 16>(lo, mine, r + j * 16, rows, c, cols, to + rest, cols);
+        if (KIND != kApply && mirror)
+#pragma unroll
+            for (int i = 0; i < FP; ++i)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const unsigned col = c + i * 16 + (lane >> 4) * 4 + k;
+                    if (row < rows && col < cols) {
+                        to[(size_t)col * cols + row] = (f16)v[i][k];
+                        if (SPLIT)
+                            to[rest + (size_t)col * cols + row] = (f16)lo[i][k];
+                    }
+                }
+    }
+}
+
+// Tile `in` of a matrix: of all row by row in groups, or of a triangle row by row.
+template <int TP, int TQ, bool SYMMETRIC>
+__device__ __forceinline__ void step_tile(unsigned in, unsigned row_tiles, unsigned col_tiles, unsigned &r0, unsigned &c0)
+{
+    if (SYMMETRIC) {
+        unsigned row = (unsigned)((sqrtf(8.0f * (float)in + 1.0f) - 1.0f) * 0.5f);
+        while (row * (row + 1) / 2 > in)
+            --row;
+        while ((row + 1) * (row + 2) / 2 <= in)
+            ++row;
+        r0 = uniform(row) * TQ;
+        c0 = uniform(in - row * (row + 1) / 2) * TP;
+    } else {
+        const Place2 where = in_groups(in, row_tiles, col_tiles);
+        r0 = where.a * TQ;
+        c0 = where.b * TP;
+    }
+}
+
 // out = a product of P and Q for each matrix: S = X X^T (Gram: P, Q = X), Q = b S +
 // c S S (Square: P, Q = S; both results symmetric: tiles on and below the diagonal are
 // computed and written to both places), X = a X + Q X (Apply: P = X, depth down its
@@ -295,20 +360,7 @@ __global__ __launch_bounds__(C::kThreads, 2) void step_kernel(Planes pm, Planes 
         if (at >= all)
             return false;
         matrix = at / each;
-        const unsigned in = at - matrix * each;
-        if (kSymmetric) {  // row by row of the triangle
-            unsigned row = (unsigned)((sqrtf(8.0f * (float)in + 1.0f) - 1.0f) * 0.5f);
-            while (row * (row + 1) / 2 > in)
-                --row;
-            while ((row + 1) * (row + 2) / 2 <= in)
-                ++row;
-            r0 = uniform(row) * C::TQ;
-            c0 = uniform(in - row * (row + 1) / 2) * C::TP;
-        } else {
-            const Place2 where = in_groups(in, row_tiles, col_tiles);
-            r0 = where.a * C::TQ;
-            c0 = where.b * C::TP;
-        }
+        step_tile<C::TP, C::TQ, kSymmetric>(at - matrix * each, row_tiles, col_tiles, r0, c0);
         return true;
     };
     unsigned ahead = blockIdx.x, pass = 0;
@@ -333,7 +385,7 @@ __global__ __launch_bounds__(C::kThreads, 2) void step_kernel(Planes pm, Planes 
         }
         pipe.load_nothing();
     };
-    const int wave = uniform(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const int wave = uniform(threadIdx.x >> 6);
     const int wp = (wave % C::WP) * COLS, wq = (wave / C::WP) * C::FQ * 16;
     char *mine = results + wave * 16 * kPieceRow<f16, COLS>;
     Pipe<C> pipe;
@@ -348,91 +400,10 @@ __global__ __launch_bounds__(C::kThreads, 2) void step_kernel(Planes pm, Planes 
 #pragma unroll 1
             for (unsigned k = 0; k < depth; k += C::kDepth)
                 pipe.step(acc, next_tile, [](auto &) {});
-        f16 *to = out.p + matrix * out.matrix;
-        const size_t rest = (size_t)out.rows * out.cols;
-        const f16 *was = pm.p + matrix * pm.matrix;  // S, or X: of the result's shape
-#pragma unroll
-        for (int j = 0; j < C::FQ; ++j) {
-            const unsigned row = r0 + wq + j * 16 + (lane & 15);
-            f32x4 v[C::FP], lo[C::FP];
-#pragma unroll
-            for (int i = 0; i < C::FP; ++i) {
-                const unsigned col = c0 + wp + i * 16 + (lane >> 4) * 4;
-                v[i] = acc[i][j] * (1.0f / kUnit);
-                if (KIND != kGram && row < out.rows && col < out.cols) {
-                    const size_t at = (size_t)row * out.cols + col;
-                    f32x4 old = __builtin_convertvector(*reinterpret_cast<const f16x4 *>(was + at), f32x4);
-                    if (SPLIT)
-                        old += __builtin_convertvector(*reinterpret_cast<const f16x4 *>(was + rest + at), f32x4);
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        v[i][k] = KIND == kSquare ? fmaf(kC, v[i][k], kB * old[k]) : fmaf(kA, old[k], v[i][k]);
-                }
-#pragma unroll
-                for (int k = 0; k < 4; ++k)
-                    lo[i][k] = v[i][k] - (float)(f16)v[i][k];
-            }
-            write_16_rows<f16, COLS>(v, mine, r0 + wq + j * 16, out.rows, c0 + wp, out.cols, to, out.cols);
-            if (SPLIT)
-                write_16_rows<f16, COLS>(lo, mine, r0 + wq + j * 16, out.rows, c0 + wp, out.cols, to + rest, out.cols);
-            if (kSymmetric && r0 != c0)  // the same above the diagonal
-#pragma unroll
-                for (int i = 0; i < C::FP; ++i)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const unsigned col = c0 + wp + i * 16 + (lane >> 4) * 4 + k;
-                        if (row < out.rows && col < out.cols) {
-                            to[(size_t)col * out.cols + row] = (f16)v[i][k];
-                            if (SPLIT)
-                                to[rest + (size_t)col * out.cols + row] = (f16)lo[i][k];
-                        }
-                    }
-        }
+        write_step<KIND, SPLIT, C::FP, C::FQ>(acc, pm.p + matrix * pm.matrix, out.p + matrix * out.matrix, out.rows, out.cols, r0 + wq,
+                                              c0 + wp, mine, r0 != c0);
     }
     arrived<0>();
-}
-
-// ---- small matrices, all of it in one launch ----------------------------------------------
-
-// Matrices of up to 128 x 128: a workgroup takes one from its gradient to its parameters,
-// X and S (or Q in its place) in LDS.  Both lie row by row in 64-row tiles: their rows are
-// read as they lie, and X's columns for Q X by transposing reads.
-template <int M_, int N_, bool SPLIT>
-struct Small {
-    static constexpr int M = M_, N = N_, kPlanes = SPLIT ? 2 : 1, kThreads = M == 128 ? 512 : 256;
-    static constexpr int WP = 2, WQ = kThreads / 128, FQ = 2;  // waves over columns and rows, 16-row results of each
-    static_assert(WQ * FQ * 16 == M, "all rows");
-    using X = Tile<f16, N, false, kThreads, false>;
-    using S = Tile<f16, M, false, kThreads, false>;
-    static constexpr int kX = M * N * 2, kS = M * M * 2, kLds = kPlanes * (kX + kS);  // bytes
-    static constexpr int kVecs = M * N / 4 / kThreads;  // of a thread
-    // workgroups a compute unit by their LDS
-    static constexpr int kAtOnce = 160 * 1024 / (kLds + 256) < 4 ? 160 * 1024 / (kLds + 256) : 4;
-};
-
-// Four values side by side in a plane of tiles: row r, columns from c on.
-template <class TILE>
-__device__ __forceinline__ unsigned lds_at(int r, int c)
-{
-    return (r >> 6) * TILE::kBytes + TILE::at(r & 63, c >> 3) + (c & 4) * 2;
-}
-template <class TILE, bool SPLIT>
-__device__ __forceinline__ f32x4 read_lds(const char *plane, int plane_bytes, int r, int c)
-{
-    const unsigned at = lds_at<TILE>(r, c);
-    f32x4 v = __builtin_convertvector(*reinterpret_cast<const f16x4 *>(plane + at), f32x4);
-    if (SPLIT)
-        v += __builtin_convertvector(*reinterpret_cast<const f16x4 *>(plane + plane_bytes + at), f32x4);
-    return v;
-}
-template <class TILE, bool SPLIT>
-__device__ __forceinline__ void write_lds(char *plane, int plane_bytes, int r, int c, f32x4 v)
-{
-    const unsigned at = lds_at<TILE>(r, c);
-    const f16x4 hi = __builtin_convertvector(v, f16x4);
-    *reinterpret_cast<f16x4 *>(plane + at) = hi;
-    if (SPLIT)
-        *reinterpret_cast<f16x4 *>(plane + plane_bytes + at) = __builtin_convertvector(v - __builtin_convertvector(hi, f32x4), f16x4);
 }
 
 // acc[i][j] = sum over `depth` of P's and Q's 16-row results: P_READ, Q_READ (plane,
@@ -474,6 +445,112 @@ __device__ __forceinline__ void small_product(int depth, f32x4 (&acc)[FP][FQ], P
                     acc[i][j] = multiply(p[i], q[j], acc[i][j], f16{});
         }
     }
+}
+
+// The same for split matrices of few tiles, one a workgroup: a step brings both planes of
+// both operands, so that it has three products to do while the next ones' loads are under
+// way, where the passes of step_kernel have one and wait.
+template <class C, int KIND>
+__global__ __launch_bounds__(C::kThreads, 2) void pair_kernel(Planes pm, Planes qm, Planes out, unsigned matrices)
+{
+    constexpr bool kSymmetric = KIND != kApply;
+    constexpr int kStage = 2 * C::kStage, kLoads = 2 * C::kLoads, COLS = C::FP * 16;
+    __shared__ __attribute__((aligned(16))) char lds[2 * kStage];
+    static_assert(C::WP * C::WQ * 16 * kPieceRow<f16, COLS> <= 2 * kStage, "results take the stages' place");
+    const unsigned row_tiles = (out.rows + C::TQ - 1) / C::TQ, col_tiles = (out.cols + C::TP - 1) / C::TP;
+    const unsigned each = kSymmetric ? row_tiles * (row_tiles + 1) / 2 : row_tiles * col_tiles;
+    const unsigned at = by_xcd(blockIdx.x, matrices * each);
+    if (at >= matrices * each)
+        return;
+    const unsigned matrix = at / each;
+    unsigned r0, c0;
+    step_tile<C::TP, C::TQ, kSymmetric>(at - matrix * each, row_tiles, col_tiles, r0, c0);
+    const f16 *p = pm.p + matrix * pm.matrix, *q = qm.p + matrix * qm.matrix;
+    typename C::P::Feed pf[2];
+    typename C::Q::Feed qf[2];
+#pragma unroll
+    for (int n = 0; n < 2; ++n) {
+        pf[n].start({{p + n * ((size_t)pm.rows * pm.cols), pm.cols, nullptr, 0, pm.rows, (int)pm.cols}, c0});
+        qf[n].start({{q + n * ((size_t)qm.rows * qm.cols), qm.cols, nullptr, 0, qm.rows, (int)qm.cols}, r0});
+    }
+    const unsigned lds0 = lds_byte(lds);
+    // a step's loads; behind the last step they bring what lies there, or zeros, and nothing reads it
+    auto bring = [&](unsigned to) {
+#pragma unroll
+        for (int n = 0; n < 2; ++n) {
+#pragma unroll
+            for (int i = 0; i < C::P::kShare; ++i)
+                pf[n].piece(i, lds0 + to + n * C::kStage);
+#pragma unroll
+            for (int i = 0; i < C::Q::kShare; ++i)
+                qf[n].piece(i, lds0 + to + n * C::kStage + C::P::kBytes);
+            pf[n].advance();
+            qf[n].advance();
+        }
+    };
+    bring(0);
+    bring(kStage);
+    const int wave = uniform(threadIdx.x >> 6);
+    const int fp = (wave % C::WP) * C::FP, fq = (wave / C::WP) * C::FQ;
+    f32x4 acc[C::FP][C::FQ] = {};
+    unsigned stage = 0;
+#pragma unroll 1
+    for (unsigned k = 0; k < qm.cols; k += C::kDepth) {
+        arrived<kLoads>();
+        const char *from = lds + stage;
+        small_product<C::FP, C::FQ, true>(
+            C::kDepth, acc, [&](int plane, int i, int part) { return C::P::fragment(from + plane * C::kStage, fp + i, part); },
+            [&](int plane, int j, int part) { return C::Q::fragment(from + plane * C::kStage + C::P::kBytes, fq + j, part); });
+        stored();  // all waves have read the stage
+        bring(stage);
+        stage ^= kStage;
+    }
+    arrived<0>();
+    write_step<KIND, true, C::FP, C::FQ>(acc, p, out.p + matrix * out.matrix, out.rows, out.cols, r0 + fq * 16, c0 + fp * 16,
+                                         lds + wave * 16 * kPieceRow<f16, COLS>, r0 != c0);
+}
+
+// ---- small matrices, all of it in one launch ----------------------------------------------
+
+// Matrices of up to 128 x 128: a workgroup takes one from its gradient to its parameters,
+// X and S (or Q in its place) in LDS.  Both lie row by row in 64-row tiles: their rows are
+// read as they lie, and X's columns for Q X by transposing reads.
+template <int M_, int N_, bool SPLIT>
+struct Small {
+    static constexpr int M = M_, N = N_, kPlanes = SPLIT ? 2 : 1, kThreads = M == 128 ? 512 : 256;
+    static constexpr int WP = 2, WQ = kThreads / 128, FQ = 2;  // waves over columns and rows, 16-row results of each
+    static_assert(WQ * FQ * 16 == M, "all rows");
+    using X = Tile<f16, N, false, kThreads, false, false, true>;
+    using S = Tile<f16, M, false, kThreads, false, false, true>;
+    static constexpr int kX = M * N * 2, kS = M * M * 2, kLds = kPlanes * (kX + kS);  // bytes
+    static constexpr int kVecs = M * N / 4 / kThreads;  // of a thread
+    // workgroups a compute unit by their LDS
+    static constexpr int kAtOnce = 160 * 1024 / (kLds + 256) < 4 ? 160 * 1024 / (kLds + 256) : 4;
+};
+
+// Four values side by side in a plane of tiles: row r, columns from c on.
+template <class TILE>
+__device__ __forceinline__ unsigned lds_at(int r, int c)
+{
+    return (r >> 6) * TILE::kBytes + TILE::at(r & 63, c >> 3) + (c & 4) * 2;
+}
+template <class TILE, bool SPLIT>
+__device__ __forceinline__ f32x4 read_lds(const char *plane, int plane_bytes, int r, int c)
+{
+    const unsigned at = lds_at<TILE>(r, c);
+    f32x4 v = __builtin_convertvector(*reinterpret_cast<const f16x4 *>(plane + at), f32x4);
+    if (SPLIT)
+        v += __builtin_convertvector(*reinterpret_cast<const f16x4 *>(plane + plane_bytes + at), f32x4);
+    return v;
+}
+template <class TILE, bool SPLIT>
+__device__ __forceinline__ void write_lds(char *plane, int plane_bytes, int r, int c, f32x4 v)
+{
+    const unsigned at = lds_at<TILE>(r, c);
+    const f16x4 hi = __builtin_convertvector(v, f16x4);
+    *reinterpret_cast<f16x4 *>(plane + at) = hi;
+    if (SPLIT)
+        *reinterpret_cast<f16x4 *>(plane + plane_bytes + at) = __builtin_convertvector(v - __builtin_convertvector(hi, f32x4), f16x4);
 }
 
 template <class C, bool SPLIT>
@@ -690,16 +767,51 @@ hipError_t launch_step(const Planes &p, const Planes &q, const Planes &out, unsi
     });
 }
 
+template <class C, int KIND>
+hipError_t launch_pair(const Planes &p, const Planes &q, const Planes &out, unsigned matrices, hipStream_t s)
+{
+    const unsigned long long rows = (out.rows + C::TQ - 1) / C::TQ, cols = (out.cols + C::TP - 1) / C::TP;
+    const unsigned long long all = matrices * (KIND != kApply ? rows * (rows + 1) / 2 : rows * cols);
+    pair_kernel<C, KIND><<<(unsigned)all + kXcds * kRun, C::kThreads, 0, s>>>(p, q, out, matrices);
+    return hipGetLastError();
+}
+
+// Tiles of 64, 128 or 256 rows and columns.  Small ones while there are few, whose loads'
+// waits others fill; from 512 of depth on 256 where their rounds of 256 workgroups cost less
+// than those of 128 (two at once a compute unit, or split one): a large one takes as long as
+// 1.65 small ones, split 3.4.  us of S, Q and Q X with 64, 128 and 256 (matrices of m x n):
+//   float32  24 of 300 x 701        15, 12, 27.4     22, 17, 28.8    54, 42, 51
+//            8 of 512 x 512         14, 15, 15       18, 21, 19      46, 58, 59
+//            16 of 512 x 1,024      30, 23, 48       30, 22, 41      76, 60, 64
+//            2 of 2,048 x 2,048     82, 86, 128      100, 105, 104   140, 154, 156
+//            16 of 1,024 x 1,024    87, 96, 155      90, 101, 125    101, 117, 125
+//            8 of 2,048 x 4,096     556, 302, 1,001  494, 282, 839   590, 340, 723
+//   bf16     24 of 300 x 701        10.8, 8.4, 16.4  15.0, 13.0, 13.6  25, 23, 25
+//            8 of 512 x 512         9.3, 9.8, 9.4    12.6, 15.0, 12.7  22, 29, 27
+//            16 of 512 x 1,024      21, 15, 26       20, 16, 18      32, 31, 30
+//            2 of 2,048 x 2,048     53, 55, 72       39, 42, 44      52, 62, 61
+//            16 of 1,024 x 1,024    53, 59, 88       40, 49, 49      36, 46, 47
+//            8 of 2,048 x 4,096     372, 168, 701    193, 120, 322   206, 134, 271
+//            16 of 2,048 x 4,096    -                385, 240, 644   308, 199, 515
 template <int KIND, bool SPLIT>
 hipError_t step(const Planes &p, const Planes &q, const Planes &out, unsigned matrices, hipStream_t s)
 {
     constexpr bool kDeep = KIND != kApply;
-    const unsigned long long large = (unsigned long long)matrices * ((out.rows + 255) / 256) * ((out.cols + 255) / 256);
-    if (large >= 256)
+    auto tiles = [&](unsigned size) {
+        const unsigned long long rows = (out.rows + size - 1) / size, cols = (out.cols + size - 1) / size;
+        return matrices * (kDeep ? rows * (rows + 1) / 2 : rows * cols);
+    };
+    const bool small = out.rows <= 64 || tiles(64) < (kDeep ? (SPLIT ? 3000 : 512) : 1000);
+    const unsigned long long at_once = SPLIT ? 256 : 512;
+    const double large = (SPLIT ? 3.4 : 1.65) * (double)((tiles(256) + 255) / 256);
+    if (!small && q.cols >= 512 && large <= (double)((tiles(128) + at_once - 1) / at_once))
         return launch_step<Product<f16, 256, 256, 4, 2, kDeep, true, false, true>, KIND, SPLIT>(p, q, out, matrices, s);
-    if (out.rows > 64)
-        return launch_step<Product<f16, 128, 128, 2, 2, kDeep, true, false, true>, KIND, SPLIT>(p, q, out, matrices, s);
-    return launch_step<Product<f16, 64, 64, 2, 2, kDeep, true, false, true>, KIND, SPLIT>(p, q, out, matrices, s);
+    if constexpr (SPLIT)
+        return small ? launch_pair<Product<f16, 64, 64, 2, 2, kDeep, true, false, true>, KIND>(p, q, out, matrices, s)
+                     : launch_pair<Product<f16, 128, 128, 2, 4, kDeep, true, false, true>, KIND>(p, q, out, matrices, s);
+    else
+        return small ? launch_step<Product<f16, 64, 64, 2, 2, kDeep, true, false, true>, KIND, false>(p, q, out, matrices, s)
+                     : launch_step<Product<f16, 128, 128, 2, 2, kDeep, true, false, true>, KIND, false>(p, q, out, matrices, s);
 }
 
 template <bool SPLIT>
