@@ -186,33 +186,42 @@ __global__ __launch_bounds__(kSortThreads) void digit_place_kernel(const int *id
     __shared__ unsigned tmp[kWaves];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const unsigned digits = 1u << bits;
-    for (int w = 0; w < kWaves; ++w)
-        for (unsigned d = threadIdx.x; d < digits; d += kSortThreads)
-            hist[w][d] = 0;
-    __syncthreads();
     const unsigned first = blockIdx.x * kSortBlock + wave * (64 * kLaneKeys) + lane;
-    unsigned key[kLaneKeys];
+    // all loads before anything waits: a thread has kShare digits side by side
+    unsigned key[kLaneKeys], value[kLaneKeys], total[kShare], before[kShare], sum = 0;
 #pragma unroll
     for (int i = 0; i < kLaneKeys; ++i) {
         const unsigned p = first + i * 64;
-        key[i] = p < samples ? (keys ? keys[p] : key_of(ids[p], rows)) : 0u;
-        if (p < samples)
-            atomicAdd(&hist[wave][key[i] >> shift & (digits - 1)], 1u);
+        key[i] = p < samples ? (keys ? keys[p] : (unsigned)ids[p]) : 0u;
+        value[i] = p < samples && values ? values[p] : p;
     }
-    // samples of smaller digits; a thread has kShare digits side by side
-    unsigned total[kShare], sum = 0;
 #pragma unroll
     for (int j = 0; j < kShare; ++j) {
         const unsigned d = threadIdx.x * kShare + j;
         total[j] = d < digits ? totals[d] : 0;
-        sum += total[j];
+        before[j] = d < digits ? counts[(size_t)d * gridDim.x + blockIdx.x] : 0;
     }
-    unsigned start = scan<kSortThreads>(sum, tmp);  // its barriers are behind the counting
+    for (int w = 0; w < kWaves; ++w)
+        for (unsigned d = threadIdx.x; d < digits; d += kSortThreads)
+            hist[w][d] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kLaneKeys; ++i) {
+        if (!keys)
+            key[i] = key_of((int)key[i], rows);
+        if (first + i * 64 < samples)
+            atomicAdd(&hist[wave][key[i] >> shift & (digits - 1)], 1u);
+    }
+#pragma unroll
+    for (int j = 0; j < kShare; ++j)
+        sum += total[j];
+    unsigned start = scan<kSortThreads>(sum, tmp);  // samples of smaller digits; its barriers are behind the counting
 #pragma unroll
     for (int j = 0; j < kShare; ++j) {
         const unsigned d = threadIdx.x * kShare + j;
         if (d < digits) {
-            unsigned at = start + counts[(size_t)d * gridDim.x + blockIdx.x];
+            unsigned at = start + before[j];
+#pragma unroll
             for (int w = 0; w < kWaves; ++w) {
                 const unsigned c = hist[w][d];
                 hist[w][d] = at;
@@ -232,7 +241,7 @@ __global__ __launch_bounds__(kSortThreads) void digit_place_kernel(const int *id
             if (rank == 0)
                 mine[digit] = at + __popcll(same);
             out_keys[at] = key[i];
-            out_values[at] = values ? values[p] : p;
+            out_values[at] = value[i];
         }
     }
 }
@@ -307,126 +316,26 @@ __global__ __launch_bounds__(kOneThreads) void sort_one_kernel(const int *ids, u
 
 // ---- sums ------------------------------------------------------------------------
 // The sorted list in pieces of kPiece entries, a group of lanes each.  A run of one key
-// that lies within a piece is a row of the result.  A run that goes on in the next piece,
-// or came from the one before, is a part: at most one of each kind a piece, which make a
-// sorted list of their own, two places a piece, some empty.  That is summed the same way
-// until there is one piece.
+// that lies within a piece is a row of the result.  Of a run that goes on in the next
+// piece its beginning is kept as the piece's trail, and what came from the piece before as
+// its lead; where a run began, its trail and the leads behind are joined.
 
 constexpr unsigned kNone = 0xFFFFFFFFu;
 constexpr unsigned kPiece = 32;
+constexpr int kLeastLanes = 2;  // log2 of a group's: the entries of a workgroup's pieces lie in LDS
 
-// What a run's part is: key, and whether the run began before it and goes on behind it.
-struct Part {
-    unsigned key;
-    unsigned before, behind;
+// Of a piece: the key of its trail, or kNone, and whether its lead goes on behind it.
+struct Ends {
+    unsigned trail, lead_goes_on;
 };
-
-// FIRST: entries are samples (sorted keys, values: places of their rows), else parts.
-template <class T, int V, bool FIRST, bool PAST>
-__global__ __launch_bounds__(256) void sum_runs_kernel(const unsigned *keys, const unsigned *values, const Part *parts,
-                                                       const T *from, long long stride, unsigned entries, unsigned rows, int D,
-                                                       float scale, float *out, Part *out_parts, float *out_rows,
-                                                       int group_log2)
-{
-    constexpr unsigned kAhead = 4;
-    const unsigned piece = blockIdx.x * (256 >> group_log2) + (threadIdx.x >> group_log2);
-    const unsigned first = piece * kPiece;
-    if (first >= entries)
-        return;
-    const unsigned last = entries - first < kPiece ? entries : first + kPiece;
-    const int c = (int)(blockIdx.y << group_log2) + ((int)threadIdx.x & ((1 << group_log2) - 1));
-    const int vecs = (D + V - 1) / V;
-    const bool in = c < vecs, tells = c == 0;
-    const int e = V > 1 ? vec_at<V>(c < vecs ? c : 0, D) : (in ? c : 0);
-    float sum[V];
-    bool open = false, began_before = false, used[2] = {false, false};
-    unsigned run = kNone;
-    auto flush = [&](bool behind) {
-        if (!began_before && !behind) {
-            Vec<float, V> x;
-#pragma unroll
-            for (int k = 0; k < V; ++k)
-                x.v[k] = sum[k] * scale;
-            if (in)
-                store_vec<float, V, PAST>(out + (size_t)run * D + e, x);
-        } else {
-            const unsigned slot = 2 * piece + (began_before ? 0 : 1);
-            Vec<float, V> x;
-#pragma unroll
-            for (int k = 0; k < V; ++k)
-                x.v[k] = sum[k];
-            if (in)
-                store_vec<float, V, false>(out_rows + (size_t)slot * D + e, x);
-            if (tells)
-                out_parts[slot] = {run, began_before, behind};
-            used[began_before ? 0 : 1] = true;
-        }
-        open = false;
-    };
-    bool goes_on = false;
-    for (unsigned i0 = first; i0 < last; i0 += kAhead) {
-        unsigned key[kAhead];
-        bool before[kAhead], behind[kAhead];
-        Vec<T, V> x[kAhead];
-#pragma unroll
-        for (unsigned j = 0; j < kAhead; ++j) {
-            const unsigned i = i0 + j;
-            key[j] = kNone;
-            if (i >= last)
-                continue;
-            if constexpr (FIRST) {
-                const unsigned k = keys[i];
-                if (k >= rows)
-                    continue;
-                key[j] = k;
-                before[j] = i > 0 && keys[i - 1] == k;
-                behind[j] = i + 1 < entries && keys[i + 1] == k;
-                x[j] = load_vec<T, V, PAST>(from + (long long)values[i] * stride + e);
-            } else {
-                const Part p = parts[i];
-                key[j] = p.key;
-                before[j] = p.before;
-                behind[j] = p.behind;
-                if (p.key != kNone)
-                    x[j] = load_vec<T, V, false>(from + (long long)i * stride + e);
-            }
-        }
-#pragma unroll
-        for (unsigned j = 0; j < kAhead; ++j) {
-            if (key[j] == kNone)
-                continue;
-            if (!open) {
-                open = true;
-                run = key[j];
-                began_before = before[j];
-#pragma unroll
-                for (int k = 0; k < V; ++k)
-                    sum[k] = (float)x[j].v[k];
-            } else {
-#pragma unroll
-                for (int k = 0; k < V; ++k)
-                    sum[k] += (float)x[j].v[k];
-            }
-            goes_on = behind[j];
-            if (!goes_on)
-                flush(false);
-        }
-    }
-    if (open)
-        flush(true);
-    if (tells && out_parts)
-        for (int s = 0; s < 2; ++s)
-            if (!used[s])
-                out_parts[2 * piece + s] = {kNone, 0, 0};
-}
 
 // Zeros for the rows that no sample has: a wave takes 64 rows, looks each up in the
 // sorted keys, and writes the absent ones.
 template <bool PAST>
-__global__ __launch_bounds__(256) void absent_rows_kernel(const unsigned *keys, unsigned samples, unsigned rows, int D, float *out)
+__device__ __forceinline__ void absent_rows(unsigned block, const unsigned *keys, unsigned samples, unsigned rows, int D, float *out)
 {
     const int lane = threadIdx.x & 63;
-    const unsigned long long v0 = ((unsigned long long)blockIdx.x * 4 + (threadIdx.x >> 6)) * 64;
+    const unsigned long long v0 = ((unsigned long long)block * 4 + (threadIdx.x >> 6)) * 64;
     if (v0 >= rows)
         return;
     const unsigned long long v = v0 + lane;
@@ -452,6 +361,241 @@ __global__ __launch_bounds__(256) void absent_rows_kernel(const unsigned *keys, 
                 row[c] = 0.0f;
         }
     }
+}
+
+template <int V>
+__device__ __forceinline__ void add(float (&sum)[V], const Vec<float, V> &x)
+{
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+        sum[k] += x.v[k];
+}
+template <int V, bool PAST>
+__device__ __forceinline__ void write_sum(float *to, const float (&sum)[V], float scale)
+{
+    Vec<float, V> x;
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+        x.v[k] = sum[k] * scale;
+    store_vec<float, V, PAST>(to, x);
+}
+
+// The first sum_blocks workgroups of a column of them sum; those behind write the absent
+// rows.
+template <class T, int V, bool PAST>
+__global__ __launch_bounds__(256) void sum_kernel(const unsigned *keys, const unsigned *values, const T *from, long long stride,
+                                                  unsigned samples, unsigned rows, int D, float scale, float *out, Ends *ends,
+                                                  float *leads, float *trails, int group_log2, unsigned sum_blocks)
+{
+    constexpr int kAhead = 8;
+    constexpr unsigned kMostEntries = (256u >> kLeastLanes) * kPiece;
+    __shared__ unsigned key_of_entry[kMostEntries + 2];  // one before and one behind
+    __shared__ unsigned row_of_entry[kMostEntries];
+    if (blockIdx.x >= sum_blocks) {
+        if (blockIdx.y == 0)
+            absent_rows<PAST>(blockIdx.x - sum_blocks, keys, samples, rows, D, out);
+        return;
+    }
+    const unsigned entries = (256u >> group_log2) * kPiece, first = blockIdx.x * entries;
+    for (unsigned i = threadIdx.x; i < entries + 2; i += 256) {
+        const unsigned at = first + i - 1;  // in front of the first: beyond any list
+        key_of_entry[i] = at < samples ? keys[at] : kNone;
+        if (i < entries && first + i < samples)
+            row_of_entry[i] = values[first + i];
+    }
+    __syncthreads();
+    const unsigned group = threadIdx.x >> group_log2, piece = blockIdx.x * (256u >> group_log2) + group;
+    const unsigned *key = key_of_entry + group * kPiece + 1, *row = row_of_entry + group * kPiece;
+    if (first + group * kPiece >= samples)
+        return;
+    const int c = (int)(blockIdx.y << group_log2) + ((int)threadIdx.x & ((1 << group_log2) - 1));
+    const int vecs = (D + V - 1) / V;
+    const bool in = c < vecs;
+    const int e = V > 1 ? vec_at<V>(in ? c : 0, D) : (in ? c : 0);
+    Ends mine = {kNone, 0};
+    float sum[V];
+    bool led = key[-1] == key[0];  // the run came from the piece before
+    for (unsigned i0 = 0; i0 < kPiece; i0 += kAhead) {
+        if (key[i0] >= rows)
+            break;
+        Vec<T, V> x[kAhead];
+#pragma unroll
+        for (unsigned j = 0; j < kAhead; ++j)
+            if (key[i0 + j] < rows)
+                x[j] = load_vec<T, V, PAST>(from + (long long)row[i0 + j] * stride + e);
+#pragma unroll
+        for (unsigned j = 0; j < kAhead; ++j) {
+            const unsigned i = i0 + j, k = key[i];
+            if (k >= rows)
+                continue;
+            if (i == 0 || key[(int)i - 1] != k)
+#pragma unroll
+                for (int n = 0; n < V; ++n)
+                    sum[n] = (float)x[j].v[n];
+            else
+#pragma unroll
+                for (int n = 0; n < V; ++n)
+                    sum[n] += (float)x[j].v[n];
+            const bool goes_on = key[i + 1] == k;
+            if (goes_on && i + 1 < kPiece)
+                continue;
+            if (led) {
+                mine.lead_goes_on = goes_on;
+                if (in)
+                    write_sum<V, false>(leads + (size_t)piece * D + e, sum, 1.0f);
+                led = false;
+            } else if (goes_on) {
+                mine.trail = k;
+                if (in)
+                    write_sum<V, false>(trails + (size_t)piece * D + e, sum, 1.0f);
+            } else if (in) {
+                write_sum<V, PAST>(out + (size_t)k * D + e, sum, scale);
+            }
+        }
+    }
+    if (c == 0)
+        ends[piece] = mine;
+}
+
+// A group takes a piece, and the run that began in it and goes on: alone where it ends
+// within as many pieces as the group has lanes, else the whole workgroup, whose groups
+// take the parts in turn.
+template <int V>
+__global__ __launch_bounds__(256) void join_kernel(const Ends *ends, const float *leads, const float *trails, unsigned pieces, int D,
+                                                   float scale, float *out, int group_log2)
+{
+    constexpr int kAhead = 8;
+    __shared__ unsigned char long_runs[256];
+    __shared__ float sums[256][V];
+    __shared__ unsigned last;
+    const unsigned lanes = 1u << group_log2, groups = 256u >> group_log2;
+    const unsigned group = threadIdx.x >> group_log2, lane = threadIdx.x & (lanes - 1), first = blockIdx.x * groups;
+    const int c = (int)(blockIdx.y * lanes + lane), vecs = (D + V - 1) / V;
+    const bool in = c < vecs;
+    const int e = V > 1 ? vec_at<V>(in ? c : 0, D) : (in ? c : 0);
+    // parts 0, 1, ...: the trail of a piece, the lead of the next, and so on; those from `from`
+    // on, `step` apart, below `parts`
+    auto sum_of = [&](unsigned piece, unsigned from, unsigned step, unsigned parts, float(&sum)[V]) {
+        for (unsigned i0 = from; i0 < parts; i0 += kAhead * step) {
+            Vec<float, V> x[kAhead];
+#pragma unroll
+            for (unsigned j = 0; j < kAhead; ++j) {
+                const unsigned i = i0 + j * step;
+                if (i < parts)
+                    x[j] = load_vec<float, V, false>((i ? leads + (size_t)(piece + i) * D : trails + (size_t)piece * D) + e);
+            }
+#pragma unroll
+            for (unsigned j = 0; j < kAhead; ++j)
+                if (i0 + j * step < parts)
+                    add<V>(sum, x[j]);
+        }
+    };
+    const unsigned piece = first + group;
+    const unsigned key = piece < pieces ? ends[piece].trail : kNone;
+    const bool ends_here = key != kNone && (piece + 1 + lane >= pieces || !ends[piece + 1 + lane].lead_goes_on);
+    const unsigned long long all = __ballot(ends_here);
+    const unsigned long long of_group = (all >> (threadIdx.x & 63 & ~(lanes - 1))) & (lanes == 64 ? ~0ull : (1ull << lanes) - 1);
+    if (key != kNone && of_group) {
+        float sum[V] = {};
+        sum_of(piece, 0, 1, (unsigned)__builtin_ctzll(of_group) + 2, sum);
+        if (in)
+            write_sum<V, false>(out + (size_t)key * D + e, sum, scale);
+    }
+    if (lane == 0)
+        long_runs[group] = key != kNone && !of_group;
+    __syncthreads();
+    for (unsigned g = 0; g < groups; ++g) {
+        if (!long_runs[g])
+            continue;
+        const unsigned from = first + g;
+        if (threadIdx.x == 0)
+            last = kNone;
+        __syncthreads();
+        for (unsigned at = from + 1; at < pieces && last == kNone; at += 256) {  // where its last lead is
+            const unsigned i = at + threadIdx.x;
+            const bool is_last = i < pieces && !ends[i].lead_goes_on;
+            __syncthreads();  // all have seen last
+            if (is_last)
+                atomicMin(&last, i);
+            __syncthreads();
+        }
+        float sum[V] = {};
+        sum_of(from, group, groups, (last < pieces ? last : pieces - 1) - from + 1, sum);
+#pragma unroll
+        for (int k = 0; k < V; ++k)
+            sums[threadIdx.x][k] = sum[k];
+        __syncthreads();
+        if (group == 0) {
+            for (unsigned i = 1; i < groups; ++i)
+#pragma unroll
+                for (int k = 0; k < V; ++k)
+                    sum[k] += sums[i * lanes + lane][k];
+            if (in)
+                write_sum<V, false>(out + (size_t)ends[from].trail * D + e, sum, scale);
+        }
+        __syncthreads();
+    }
+}
+
+// Few samples in one launch: a workgroup takes some rows, notes the samples that are
+// theirs, in order, and sums them row by row, a group of lanes each.
+constexpr unsigned kFewSamples = 256;
+template <class T, int V>
+__global__ __launch_bounds__(256) void few_kernel(const int *ids, const T *from, long long stride, unsigned samples, unsigned rows, int D,
+                                                  float scale, float *out, int group_log2, unsigned rows_each)
+{
+    constexpr int kAhead = 4;
+    __shared__ unsigned of_wave[4];
+    __shared__ unsigned row_of[kFewSamples], sample_of[kFewSamples];
+    const unsigned v0 = blockIdx.x * rows_each, here = rows - v0 < rows_each ? rows - v0 : rows_each;
+    const int id = threadIdx.x < samples ? ids[threadIdx.x] : -1;
+    const bool mine = (unsigned)id >= v0 && (unsigned)id - v0 < here;
+    const unsigned long long ballot = __ballot(mine);
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    if (lane == 0)
+        of_wave[wave] = __popcll(ballot);
+    __syncthreads();
+    unsigned at = __popcll(ballot & ((1ull << lane) - 1)), count = 0;
+    for (int w = 0; w < 4; ++w) {
+        if (w < wave)
+            at += of_wave[w];
+        count += of_wave[w];
+    }
+    if (mine) {
+        row_of[at] = (unsigned)id - v0;
+        sample_of[at] = threadIdx.x;
+    }
+    __syncthreads();
+    const unsigned groups = 256u >> group_log2, lanes = 1u << group_log2;
+    const int vecs = (D + V - 1) / V;
+    for (unsigned v = threadIdx.x >> group_log2; v < here; v += groups)
+        for (int c = (int)(threadIdx.x & (lanes - 1)); c < vecs; c += (int)lanes) {
+            const int e = V > 1 ? vec_at<V>(c, D) : c;
+            float sum[V] = {};
+            for (unsigned i = 0; i < count;) {
+                unsigned found[kAhead], n = 0;  // the next samples of this row
+                for (; i < count && n < kAhead; ++i)
+                    if (row_of[i] == v) {
+#pragma unroll
+                        for (unsigned j = 0; j < kAhead; ++j)
+                            if (j == n)
+                                found[j] = sample_of[i];
+                        ++n;
+                    }
+                Vec<T, V> x[kAhead];
+#pragma unroll
+                for (unsigned j = 0; j < kAhead; ++j)
+                    if (j < n)
+                        x[j] = load_vec<T, V, false>(from + (long long)found[j] * stride + e);
+#pragma unroll
+                for (unsigned j = 0; j < kAhead; ++j)
+                    if (j < n)
+#pragma unroll
+                        for (int k = 0; k < V; ++k)
+                            sum[k] += (float)x[j].v[k];
+            }
+            write_sum<V, false>(out + (size_t)(v0 + v) * D + e, sum, scale);
+        }
 }
 
 // ---- launches --------------------------------------------------------------------
@@ -506,10 +650,9 @@ Digits digits_of(unsigned rows)
 
 size_t whole(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
-// The workspace: two lists of keys and values, the sort's counts, and the parts of the
-// sums' levels, of which two are alive at a time.
+// The workspace: two lists of keys and values, the sort's counts, and the pieces' parts.
 struct Places {
-    size_t list, counts, parts, part_rows, parts2, part_rows2, end;
+    size_t list, counts, ends, leads, trails, end;
 };
 Places places_of(unsigned samples, unsigned rows, int dim)
 {
@@ -521,26 +664,51 @@ Places places_of(unsigned samples, unsigned rows, int dim)
         return here;
     };
     p.list = take(0);
+    if (samples <= kFewSamples) {
+        p.counts = p.ends = p.leads = p.trails = p.end = 0;
+        return p;
+    }
     at += 4 * whole((size_t)samples * 4);
     const Digits d = digits_of(rows);
     p.counts = take(samples > kOneBlock ? (((size_t)blocks_of(samples, kSortBlock) + 1) << d.bits) * 4 : 0);
-    const size_t first = 2 * (size_t)blocks_of(samples, kPiece), second = 2 * (size_t)blocks_of(first, kPiece);
-    p.parts = take(first * sizeof(Part));
-    p.part_rows = take(first * dim * sizeof(float));
-    p.parts2 = take(second * sizeof(Part));
-    p.part_rows2 = take(second * dim * sizeof(float));
+    const size_t pieces = blocks_of(samples, kPiece);
+    p.ends = take(pieces * sizeof(Ends));
+    p.leads = take(pieces * dim * sizeof(float));
+    p.trails = take(pieces * dim * sizeof(float));
     p.end = at;
     return p;
 }
 
-template <class T, int V, bool FIRST, bool PAST>
-hipError_t sum_runs(const unsigned *keys, const unsigned *values, const Part *parts, const T *from, long long stride,
-                    unsigned entries, unsigned rows, int dim, float scale, float *out, Part *out_parts, float *out_rows, hipStream_t s)
+template <class T, int V>
+hipError_t few(Rows dout, const int *ids, unsigned samples, unsigned rows, int dim, float scale, float *out, hipStream_t s)
 {
-    const int vecs = (dim + V - 1) / V, g = group_log2(vecs);
-    const unsigned pieces = blocks_of(entries, kPiece);
-    sum_runs_kernel<T, V, FIRST, PAST><<<dim3(blocks_of(pieces, 256 >> g), blocks_of(vecs, 1 << g)), 256, 0, s>>>(
-        keys, values, parts, from, stride, entries, rows, dim, scale, out, out_parts, out_rows, g);
+    const int g = group_log2((dim + V - 1) / V);
+    // rows of a workgroup: a few for each group, and more where there are too many workgroups
+    unsigned each = (256u >> g) * 4;
+    if (blocks_of(rows, each) > 4096)
+        each = blocks_of(rows, 4096);
+    few_kernel<T, V><<<blocks_of(rows, each), 256, 0, s>>>(ids, static_cast<const T *>(dout.p), dout.stride, samples, rows, dim, scale,
+                                                           out, g, each);
+    return hipGetLastError();
+}
+
+template <class T, int V, bool PAST>
+hipError_t sums(const unsigned *keys, const unsigned *values, Rows dout, unsigned samples, unsigned rows, int dim, float scale, float *out,
+                Ends *ends, float *leads, float *trails, hipStream_t s)
+{
+    const int vecs = (dim + V - 1) / V, least = group_log2(vecs), g = least < kLeastLanes ? kLeastLanes : least;
+    const unsigned pieces = blocks_of(samples, kPiece), blocks = blocks_of(pieces, 256 >> g);
+    sum_kernel<T, V, PAST><<<dim3(blocks + blocks_of(rows, 256), blocks_of(vecs, 1 << g)), 256, 0, s>>>(
+        keys, values, static_cast<const T *>(dout.p), dout.stride, samples, rows, dim, scale, out, ends, leads, trails, g, blocks);
+    return hipGetLastError();
+}
+
+template <int V>
+hipError_t join(const Ends *ends, const float *leads, const float *trails, unsigned pieces, int dim, float scale, float *out, hipStream_t s)
+{
+    const int vecs = (dim + V - 1) / V, least = group_log2(vecs), g = least < kLeastLanes ? kLeastLanes : least;
+    join_kernel<V><<<dim3(blocks_of(pieces, 256 >> g), blocks_of(vecs, 1 << g)), 256, 0, s>>>(ends, leads, trails, pieces, dim, scale, out,
+                                                                                         g);
     return hipGetLastError();
 }
 
@@ -549,6 +717,8 @@ hipError_t backward(Rows dout, const int *ids, unsigned samples, unsigned rows, 
                     hipStream_t s)
 {
     constexpr int V = 16 / sizeof(T);
+    if (samples <= kFewSamples)
+        return dim < V ? few<T, 1>(dout, ids, samples, rows, dim, scale, out, s) : few<T, V>(dout, ids, samples, rows, dim, scale, out, s);
     const Places at = places_of(samples, rows, dim);
     const size_t list = whole((size_t)samples * 4);
     unsigned *keys[2], *values[2];
@@ -573,44 +743,25 @@ hipError_t backward(Rows dout, const int *ids, unsigned samples, unsigned rows, 
         }
         now ^= 1;  // the last one written
         e = hipGetLastError();
-    } else if (samples > 0) {
+    } else {
         sort_one_kernel<<<1, kOneThreads, 0, s>>>(ids, samples, rows, d.key_bits, keys[0], values[0]);
         e = hipGetLastError();
     }
     if (e != hipSuccess)
         return e;
-    const bool past = whole_lines(out, dim, dim, 4);
-    const unsigned blocks = blocks_of(rows, 256);
-    if (past)
-        absent_rows_kernel<true><<<blocks, 256, 0, s>>>(keys[now], samples, rows, dim, out);
-    else
-        absent_rows_kernel<false><<<blocks, 256, 0, s>>>(keys[now], samples, rows, dim, out);
-    e = hipGetLastError();
-    if (e != hipSuccess || samples == 0)
-        return e;
-    Part *parts[2] = {reinterpret_cast<Part *>(ws + at.parts), reinterpret_cast<Part *>(ws + at.parts2)};
-    float *part_rows[2] = {reinterpret_cast<float *>(ws + at.part_rows), reinterpret_cast<float *>(ws + at.part_rows2)};
-    const T *from = static_cast<const T *>(dout.p);
-    const bool lines = past && whole_lines(from, dout.stride, dim, sizeof(T));
+    Ends *ends = reinterpret_cast<Ends *>(ws + at.ends);
+    float *leads = reinterpret_cast<float *>(ws + at.leads), *trails = reinterpret_cast<float *>(ws + at.trails);
+    const unsigned *k = keys[now], *v = values[now];
     if (dim < V)
-        e = sum_runs<T, 1, true, false>(keys[now], values[now], nullptr, from, dout.stride, samples, rows, dim, scale, out, parts[0],
-                                        part_rows[0], s);
-    else if (lines)
-        e = sum_runs<T, V, true, true>(keys[now], values[now], nullptr, from, dout.stride, samples, rows, dim, scale, out, parts[0],
-                                       part_rows[0], s);
+        e = sums<T, 1, false>(k, v, dout, samples, rows, dim, scale, out, ends, leads, trails, s);
+    else if (whole_lines(out, dim, dim, 4) && whole_lines(dout.p, dout.stride, dim, sizeof(T)))
+        e = sums<T, V, true>(k, v, dout, samples, rows, dim, scale, out, ends, leads, trails, s);
     else
-        e = sum_runs<T, V, true, false>(keys[now], values[now], nullptr, from, dout.stride, samples, rows, dim, scale, out, parts[0],
-                                        part_rows[0], s);
-    unsigned pieces = blocks_of(samples, kPiece);
-    for (int level = 0; e == hipSuccess && pieces > 1; ++level) {
-        const unsigned entries = 2 * pieces;
-        pieces = blocks_of(entries, kPiece);
-        Part *const in = parts[level & 1], *const to = parts[~level & 1];
-        float *const in_rows = part_rows[level & 1], *const to_rows = part_rows[~level & 1];
-        e = dim < 4 ? sum_runs<float, 1, false, false>(nullptr, nullptr, in, in_rows, dim, entries, rows, dim, scale, out, to, to_rows, s)
-                    : sum_runs<float, 4, false, false>(nullptr, nullptr, in, in_rows, dim, entries, rows, dim, scale, out, to, to_rows, s);
-    }
-    return e;
+        e = sums<T, V, false>(k, v, dout, samples, rows, dim, scale, out, ends, leads, trails, s);
+    const unsigned pieces = blocks_of(samples, kPiece);
+    if (e != hipSuccess || pieces == 1)
+        return e;
+    return dim < 4 ? join<1>(ends, leads, trails, pieces, dim, scale, out, s) : join<4>(ends, leads, trails, pieces, dim, scale, out, s);
 }
 
 }  // namespace
