@@ -29,14 +29,23 @@ hipError_t gated(const LinearShape &sh, Rows x, const void *w, const float *bias
         return launch_rows<Product<T, 64, 32, 2, 1, true, true, false, false, false, 4, true>>(p, mw, mx, bias, act, y, O, depth,
                                                                                             s, pre);
     const bool alone = goes_alone(mw) && goes_alone(mx);
-    if constexpr (sizeof(T) == 2)
-        if (alone && depth >= 512 && large_tiles(p, 2 * O))
+    if constexpr (sizeof(T) == 2) {
+        // large tiles as in large_tiles, from a depth of 256 on; in both sizes a wave has 64
+        // columns, whole lines.  us, rows of bf16 with gates and ups kept, 256 and 128: 256 to
+        // 256 on 262,139 156, 169, on 65,536 41, 40; 320 to 512 on 65,536 79, 82; 1,024 to
+        // 1,024 on 32,768 144, 170; waves of 32 columns in tiles of 128: 203, 41, 84, 166
+        if (alone && depth >= 256 && large_tiles(p, 2 * O))
             return launch_rows<Product<T, 256, 256, 2, 4, true, true, false, true, false, 1, true>>(p, mw, mx, bias, act, y, O,
                                                                                                  depth, s, pre);
-    if (wide_tile<T>(2 * O)) {
-        if (alone)
-            return launch_rows<Product<T, 128, 128, 2, 2, true, true, false, true, false, 1, true>>(p, mw, mx, bias, act, y, O,
+        if (alone && wide_tile<T>(2 * O))
+            return launch_rows<Product<T, 128, 128, 1, 4, true, true, false, true, false, 1, true>>(p, mw, mx, bias, act, y, O,
                                                                                                  depth, s, pre);
+    }
+    if (wide_tile<T>(2 * O)) {
+        if constexpr (sizeof(T) == 4)
+            if (alone)
+                return launch_rows<Product<T, 128, 128, 2, 2, true, true, false, true, false, 1, true>>(p, mw, mx, bias, act, y,
+                                                                                                     O, depth, s, pre);
         return launch_rows<Product<T, 128, 128, 2, 2, true, true, false, false, false, 1, true>>(p, mw, mx, bias, act, y, O,
                                                                                               depth, s, pre);
     }

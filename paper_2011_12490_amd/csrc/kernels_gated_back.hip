@@ -115,6 +115,212 @@ __global__ __launch_bounds__(256) void gate_gradient_kernel(Problem p, const T *
     }
 }
 
+// ---- narrow layers, all gradients in one pass over the rows --------------------------
+
+// bf16 layers of at most 128 to 2 x 128: as narrow_kernel, a workgroup a compute unit keeps
+// its head's weights in LDS and its part of dW in registers and goes through a stretch of the
+// head's rows, RT at a time, the next ones' loads under way.  dz is made on the way from the
+// registers to LDS, where both products read it: dx by rows, dW by columns.
+template <int TI_, int TO_>
+struct GatedNarrow {
+    using T = __bf16;
+    static constexpr int TI = TI_, TO = TO_, kThreads = 512, RT = 64, V = Type<T>::kVec;
+    using X = Tile<T, TI, false, kThreads, false, false, true>;
+    using Z = Tile<T, TO, false, kThreads, false, false, true>;  // dg, and du
+    static_assert(X::D == RT && Z::D == RT, "a tile of rows a step");
+    static constexpr int FP = TI / 32, FQ = 2 * TO / 64;  // dW: 2 waves over fan_in, 4 over gates and ups
+    static constexpr int FX = TI / 32;                    // dx: 4 waves over rows, 2 over fan_in
+    static constexpr int kWeights = 2 * TO / RT;          // tiles of RT outputs
+    static constexpr int kZ = 0, kX = kZ + 2 * Z::kBytes, kW = kX + X::kBytes, kOut = kW + kWeights * X::kBytes;
+    static constexpr int kRowsOfThreads = kThreads / Z::kPerRow;
+    static constexpr int kSums = kRowsOfThreads * (2 * TO + 1) * 4;
+    static constexpr int kAll = kOut + 8 * 16 * kPieceRow<T, FX * 16>, kLds = kAll > kSums ? kAll : kSums;
+};
+
+template <class C>
+__global__ __launch_bounds__(C::kThreads, 2) void gated_narrow_kernel(Problem p, Matrix<__bf16> w, Matrix<__bf16> dy, Matrix<__bf16> pre,
+                                                                      int act, Matrix<__bf16> x, __bf16 *dx, long long dxs, float *dw,
+                                                                      float *db, unsigned stretch)
+{
+    using T = __bf16;
+    using X = typename C::X;
+    using Z = typename C::Z;
+    constexpr int V = C::V;
+    __shared__ __attribute__((aligned(16))) char lds[C::kLds];
+    __shared__ unsigned before[kMaxHeads + 1];
+    const int I = p.fan_in, O = p.fan_out, lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    count_tiles(p, stretch, before);
+    const unsigned places = uniform(before[p.heads]), place = blockIdx.x;
+    if (place >= places) {  // rows without a head: zeros
+        const unsigned headless = bound(p, p.heads);
+        const unsigned long long from = headless + (unsigned long long)(place - places) * stretch;
+        if (dx)
+            for (unsigned long long r = from + wave; r < from + stretch && r < p.rows; r += C::kThreads / 64)
+                for (int c = lane; c < I; c += 64)
+                    dx[r * dxs + c] = (T)0.0f;
+        return;
+    }
+    const RowTile t = head_tile(p, before, place, stretch);
+    typename X::Source xs = {x, 0};
+    typename Z::Source ys = {dy, 0}, gs = {pre, 0}, us = {pre, 0};
+    us.m.p += O;
+    xs.m.p += t.first * x.stride;
+    ys.m.p += t.first * dy.stride;
+    gs.m.p += t.first * pre.stride;
+    us.m.p += t.first * pre.stride;
+    gs.m.cols = us.m.cols = O;
+    xs.m.rows = ys.m.rows = gs.m.rows = us.m.rows = t.last - t.first;
+    typename X::S sx;
+    typename Z::S sy, sg, su;
+    auto load = [&](unsigned k) {
+        Z::load(sg, gs, k);
+        Z::load(su, us, k);
+        Z::load(sy, ys, k);
+        X::load(sx, xs, k);
+    };
+    if (dx) {
+#pragma unroll
+        for (int i = 0; i < C::kWeights; ++i) {
+            typename X::S sw;
+            const int half = i * C::RT / C::TO, k = i * C::RT % C::TO;
+            typename X::Source ws = {w, 0};
+            ws.m.p += t.head * ((size_t)2 * I * O) + (size_t)half * I * O;
+            ws.m.rows = O;
+            X::load(sw, ws, k);
+            X::settle(sw, ws, k);
+            X::store(sw, lds + C::kW + i * X::kBytes);
+        }
+    }
+    load(0);
+    float g_sums[V], u_sums[V];
+#pragma unroll
+    for (int k = 0; k < V; ++k)
+        g_sums[k] = u_sums[k] = 0.0f;
+    f32x4 acc[C::FP][C::FQ] = {};
+    const int fp = wave % 2 * C::FP, fq = wave / 2 * C::FQ;  // of dW; results fq on are of the ups from TO / 16 on
+    const int fr = wave / 2, fc = wave % 2 * C::FX;          // of dx
+    char *mine = lds + C::kOut + wave * 16 * kPieceRow<T, C::FX * 16>;
+    constexpr int kOfHalf = C::TO / 16;
+    const char *const z_of_dw = lds + C::kZ + (fq >= kOfHalf ? Z::kBytes : 0);
+    const int fz = fq >= kOfHalf ? fq - kOfHalf : fq;
+#pragma unroll 1
+    for (unsigned k = 0; k < t.last - t.first; k += C::RT) {
+        stored();
+        Z::settle(sg, gs, k);
+        Z::settle(su, us, k);
+        Z::settle(sy, ys, k);
+        X::settle(sx, xs, k);
+        X::store(sx, lds + C::kX);
+#pragma unroll
+        for (int j = 0; j < Z::kShare; ++j) {
+            union Piece {
+                u32x4 v;
+                T e[V];
+            };
+            const Piece y = {sy.x[j]}, g = {sg.x[j]}, u = {su.x[j]};
+            Piece dg, du;
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                float value, slope;
+                act_and_slope<T>((float)g.e[e], act, value, slope);
+                const float a = (float)y.e[e] * (float)u.e[e] * slope, b = (float)y.e[e] * value;
+                g_sums[e] += a;
+                u_sums[e] += b;
+                dg.e[e] = (T)a;
+                du.e[e] = (T)b;
+            }
+            *reinterpret_cast<u32x4 *>(lds + C::kZ + (threadIdx.x + j * C::kThreads) * 16) = dg.v;
+            *reinterpret_cast<u32x4 *>(lds + C::kZ + Z::kBytes + (threadIdx.x + j * C::kThreads) * 16) = du.v;
+        }
+        stored();
+        if (k + C::RT < t.last - t.first)
+            load(k + C::RT);
+        if (dx) {
+            f32x4 rows[C::FX] = {};
+#pragma unroll
+            for (int half = 0; half < 2; ++half)
+#pragma unroll
+                for (int part = 0; part < C::TO / 32; ++part) {
+                    const u32x4 q = Z::row_fragment(lds + C::kZ + half * Z::kBytes, fr, part);
+#pragma unroll
+                    for (int i = 0; i < C::FX; ++i)
+                        rows[i] = multiply(X::fragment(lds + C::kW + (half * C::TO / C::RT + part / 2) * X::kBytes, fc + i, part & 1),
+                                           q, rows[i], T{});
+                }
+            write_16_rows<T, C::FX * 16>(rows, mine, t.first + k + fr * 16, t.last, fc * 16, I, dx, dxs);
+        }
+        if (dw)
+#pragma unroll
+            for (int part = 0; part < C::RT / 32; ++part) {
+                u32x4 q[C::FQ];
+#pragma unroll
+                for (int j = 0; j < C::FQ; ++j)
+                    q[j] = Z::fragment(z_of_dw, fz + j, part);
+#pragma unroll
+                for (int i = 0; i < C::FP; ++i) {
+                    const u32x4 f = X::fragment(lds + C::kX, fp + i, part);
+#pragma unroll
+                    for (int j = 0; j < C::FQ; ++j)
+                        acc[i][j] = multiply(f, q[j], acc[i][j], T{});
+                }
+            }
+    }
+    if (dw) {
+        float *to = dw + (size_t)place * 2 * O * I + (fq >= kOfHalf ? (size_t)O * I : 0);
+#pragma unroll
+        for (int j = 0; j < C::FQ; ++j) {
+            const int m = (fz + j) * 16 + (lane & 15);
+#pragma unroll
+            for (int i = 0; i < C::FP; ++i) {
+                const int n = (fp + i) * 16 + (lane >> 4) * 4;
+                if (m < O && n < I)
+                    write_piece(to + ((size_t)m * I + n), __builtin_bit_cast(u32x4, acc[i][j]), I - n, 0.0f);
+            }
+        }
+    }
+    if (db) {
+        float(*part)[2 * C::TO + 1] = reinterpret_cast<float(*)[2 * C::TO + 1]>(lds);
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < V; ++e) {
+            part[Z::my_row()][Z::my_col() + e] = g_sums[e];
+            part[Z::my_row()][C::TO + Z::my_col() + e] = u_sums[e];
+        }
+        __syncthreads();
+        for (int i = threadIdx.x; i < 2 * C::TO; i += C::kThreads) {
+            float v = 0.0f;
+            for (int r = 0; r < C::kRowsOfThreads; ++r)
+                v += part[r][i];
+            const int half = i / C::TO, o = i % C::TO;
+            if (o < O)
+                db[((size_t)place * 2 + half) * O + o] = v;
+        }
+    }
+}
+
+template <int TI, int TO>
+hipError_t gated_narrow(const Problem &p, const Matrix<__bf16> &w, const Matrix<__bf16> &dy, const Matrix<__bf16> &pre, int act,
+                        const Matrix<__bf16> &x, Rows dx, __bf16 *dw, float *db, char *workspace, hipStream_t s)
+{
+    using C = GatedNarrow<TI, TO>;
+    const Split split = narrow_split(p.rows, p.heads, p.fan_in, p.fan_out, true);
+    float *wparts = reinterpret_cast<float *>(workspace);
+    float *bparts = wparts + (size_t)split.places * 2 * p.fan_out * p.fan_in;
+    gated_narrow_kernel<C><<<split.places + 1, C::kThreads, 0, s>>>(p, w, dy, pre, act, x, static_cast<__bf16 *>(const_cast<void *>(dx.p)),
+                                                                    dx.stride, dw ? wparts : nullptr, db ? bparts : nullptr, split.stretch);
+    const hipError_t e = hipGetLastError();
+    const Problem both = {p.offsets, p.rows, p.heads, p.fan_in, 2 * p.fan_out};
+    return e != hipSuccess || (!dw && !db) ? e : launch_sums(both, split, wparts, dw, bparts, db, s);
+}
+
+bool is_gated_narrow(int fan_in, int fan_out, bool bf16) { return bf16 && fan_in <= 128 && fan_out <= 128; }
+size_t gated_narrow_bytes(unsigned rows, int heads, int fan_in, int fan_out)
+{
+    return (size_t)narrow_split(rows, heads, fan_in, fan_out, true).places * 2 * fan_out * ((size_t)fan_in + 1) * sizeof(float);
+}
+
+// ---- launches --------------------------------------------------------------------------
+
 // Stretches of the pass over the rows: about 2,048 workgroups.
 struct Stretches {
     int log_lanes;
@@ -150,6 +356,21 @@ hipError_t gated_backward(const LinearShape &sh, Rows dy, Rows pre, Rows x, cons
     constexpr bool bf16 = sizeof(T) == 2;
     const Problem p = {sh.offsets, sh.rows, sh.heads, sh.fan_in, 2 * sh.fan_out};
     const bool rows = sh.rows > 0;
+    const Matrix<T> mw = {static_cast<const T *>(w), sh.fan_in, nullptr, 0, (unsigned)p.fan_out, sh.fan_in};
+    Matrix<T> mx = {static_cast<const T *>(x.p), x.stride, nullptr, 0, sh.rows, sh.fan_in};
+    if constexpr (bf16)
+        if (rows && is_gated_narrow(sh.fan_in, sh.fan_out, bf16)) {
+            const Problem one = {sh.offsets, sh.rows, sh.heads, sh.fan_in, sh.fan_out};
+            const Matrix<T> my = {static_cast<const T *>(dy.p), dy.stride, nullptr, 0, sh.rows, sh.fan_out};
+            const Matrix<T> mp = {static_cast<const T *>(pre.p), pre.stride, nullptr, 0, sh.rows, sh.fan_out};
+            if (!dw)  // nothing needs x
+                mx = {my.p, my.stride, nullptr, 0, my.rows, my.cols < mx.cols ? my.cols : mx.cols};
+            if (sh.fan_in <= 64)
+                return sh.fan_out <= 64 ? gated_narrow<64, 64>(one, mw, my, mp, act, mx, dx, dw, db, workspace, s)
+                                        : gated_narrow<64, 128>(one, mw, my, mp, act, mx, dx, dw, db, workspace, s);
+            return sh.fan_out <= 64 ? gated_narrow<128, 64>(one, mw, my, mp, act, mx, dx, dw, db, workspace, s)
+                                    : gated_narrow<128, 128>(one, mw, my, mp, act, mx, dx, dw, db, workspace, s);
+        }
     float *parts = reinterpret_cast<float *>(workspace);
     workspace += sums_bytes(sh.rows, sh.heads, sh.fan_out, bf16);
     T *dz = dx.p || dw ? reinterpret_cast<T *>(workspace) : nullptr;
@@ -168,8 +389,6 @@ hipError_t gated_backward(const LinearShape &sh, Rows dy, Rows pre, Rows x, cons
     if (e != hipSuccess || !dz)
         return e;
     const Matrix<T> mz = {dz, dz_stride(sh.fan_out), nullptr, 0, sh.rows, p.fan_out};
-    const Matrix<T> mw = {static_cast<const T *>(w), sh.fan_in, nullptr, 0, (unsigned)p.fan_out, sh.fan_in};
-    const Matrix<T> mx = {static_cast<const T *>(x.p), x.stride, nullptr, 0, sh.rows, sh.fan_in};
     if constexpr (bf16)
         if (rows && dx.p && dw && goes_alone(mz) && goes_alone(mw) && goes_alone(mx) && gradients_together(p))
             return launch_gradients<Product<T, 256, 256, 4, 2, false, true, false, true>,
@@ -188,6 +407,8 @@ hipError_t gated_backward(const LinearShape &sh, Rows dy, Rows pre, Rows x, cons
 
 size_t heads_gated_workspace_bytes(unsigned rows, int heads, int fan_in, int fan_out, bool bf16)
 {
+    if (rows > 0 && is_gated_narrow(fan_in, fan_out, bf16))
+        return gated_narrow_bytes(rows, heads, fan_in, fan_out);
     return sums_bytes(rows, heads, fan_out, bf16) + dz_bytes(rows, fan_out, bf16) +
            parts_bytes(rows, heads, fan_in, 2 * fan_out, bf16);
 }

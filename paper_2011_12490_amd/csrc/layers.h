@@ -479,7 +479,9 @@ struct Shallow {
     using X = Tile<T, RT, true, kThreads, MASK>;
     static constexpr int FP = 4;  // a wave's: 64 outputs of 16 rows
     static constexpr int kRowBytes = 64 * (int)sizeof(T) + 16;
-    static constexpr int kX = STEPS * W::kBytes, kOut = kX + STEPS * X::kBytes, kLds = kOut + 8 * 16 * kRowBytes;
+    static constexpr int kX = STEPS * W::kBytes, kOut = kX + STEPS * X::kBytes;
+    // results on their way out; a gated layer's float ones go from the registers
+    static constexpr int kLds = kOut + (PAIR && sizeof(T) == 4 ? 16 : 8 * 16 * kRowBytes);
     // workgroups a compute unit: by LDS, and 4 waves a SIMD
     static constexpr int kAtOnce = 2 * (kLds + 4096) <= 160 * 1024 ? 2 : 1;
 };
