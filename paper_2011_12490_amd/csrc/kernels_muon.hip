@@ -406,13 +406,74 @@ __global__ __launch_bounds__(C::kThreads, 2) void step_kernel(Planes pm, Planes 
     arrived<0>();
 }
 
-// acc[i][j] = sum over `depth` of P's and Q's 16-row results: P_READ, Q_READ (plane,
-// result, 32 deep part) give the matrix unit's operands.
-template <int FP, int FQ, bool SPLIT, class PRead, class QRead>
-__device__ __forceinline__ void small_product(int depth, f32x4 (&acc)[FP][FQ], PRead p_read, QRead q_read)
+// Two results side by side of 16 rows, as 16-byte chunks of a row: a lane of quarter q gets
+// chunk q / 2 of result q % 2 from its own half and that of the lane 16 on, or back.
+__device__ __forceinline__ void swap_halves(u32x4 &x)
 {
-#pragma unroll 2
-    for (int part = 0; part < depth / 32; ++part) {
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+        const auto both = __builtin_amdgcn_permlane16_swap(x[k], x[2 + k], false, false);
+        x[k] = both[0];
+        x[2 + k] = both[1];
+    }
+}
+__device__ __forceinline__ u32x4 as_halves(f32x4 a, f32x4 b)
+{
+    return __builtin_bit_cast(u32x4, __builtin_convertvector(__builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7), f16x8));
+}
+__device__ __forceinline__ void from_halves(u32x4 x, f32x4 &a, f32x4 &b)
+{
+    typedef float f32x8 __attribute__((ext_vector_type(8)));
+    const f32x8 v = __builtin_convertvector(__builtin_bit_cast(f16x8, x), f32x8);
+    a = __builtin_shufflevector(v, v, 0, 1, 2, 3);
+    b = __builtin_shufflevector(v, v, 4, 5, 6, 7);
+}
+// Where: row `row` of a plane of tiles, results f and f + 1.
+template <class TILE>
+__device__ __forceinline__ unsigned pair_at(int row, int f)
+{
+    const int quarter = (threadIdx.x & 63) >> 4;
+    return (row >> 6) * TILE::kBytes + TILE::at(row & 63, 2 * (f + (quarter & 1)) + (quarter >> 1));
+}
+template <class TILE, bool SPLIT>
+__device__ __forceinline__ void write_pair(char *plane, int plane_bytes, int row, int f, f32x4 a, f32x4 b)
+{
+    const unsigned at = pair_at<TILE>(row, f);
+    u32x4 hi = as_halves(a, b);
+    if (SPLIT) {
+        f32x4 c, d;
+        from_halves(hi, c, d);
+        u32x4 lo = as_halves(a - c, b - d);
+        swap_halves(lo);
+        *reinterpret_cast<u32x4 *>(plane + plane_bytes + at) = lo;
+    }
+    swap_halves(hi);
+    *reinterpret_cast<u32x4 *>(plane + at) = hi;
+}
+template <class TILE, bool SPLIT>
+__device__ __forceinline__ void read_pair(const char *plane, int plane_bytes, int row, int f, f32x4 &a, f32x4 &b)
+{
+    const unsigned at = pair_at<TILE>(row, f);
+    u32x4 hi = *reinterpret_cast<const u32x4 *>(plane + at);
+    swap_halves(hi);
+    from_halves(hi, a, b);
+    if (SPLIT) {
+        u32x4 lo = *reinterpret_cast<const u32x4 *>(plane + plane_bytes + at);
+        swap_halves(lo);
+        f32x4 c, d;
+        from_halves(lo, c, d);
+        a += c;
+        b += d;
+    }
+}
+
+// acc[i][j] = sum over DEPTH of P's and Q's 16-row results: P_READ, Q_READ (plane,
+// result, 32 deep part) give the matrix unit's operands.
+template <int FP, int FQ, bool SPLIT, int DEPTH, class PRead, class QRead>
+__device__ __forceinline__ void small_product(f32x4 (&acc)[FP][FQ], PRead p_read, QRead q_read)
+{
+#pragma unroll
+    for (int part = 0; part < DEPTH / 32; ++part) {
         u32x4 p[FP], q[FQ];
 #pragma unroll
         for (int j = 0; j < FQ; ++j)
@@ -498,8 +559,8 @@ __global__ __launch_bounds__(C::kThreads, 2) void pair_kernel(Planes pm, Planes 
     for (unsigned k = 0; k < qm.cols; k += C::kDepth) {
         arrived<kLoads>();
         const char *from = lds + stage;
-        small_product<C::FP, C::FQ, true>(
-            C::kDepth, acc, [&](int plane, int i, int part) { return C::P::fragment(from + plane * C::kStage, fp + i, part); },
+        small_product<C::FP, C::FQ, true, C::kDepth>(
+            acc, [&](int plane, int i, int part) { return C::P::fragment(from + plane * C::kStage, fp + i, part); },
             [&](int plane, int j, int part) { return C::Q::fragment(from + plane * C::kStage + C::P::kBytes, fq + j, part); });
         stored();  // all waves have read the stage
         bring(stage);
@@ -630,7 +691,7 @@ __global__ __launch_bounds__(C::kThreads, C::kAtOnce *C::kThreads / 256) void sm
     }
     __syncthreads();
     const int wp = wave % C::WP, fq = wave / C::WP * FQ;
-    const int row = fq * 16 + (lane & 15), col = (lane >> 4) * 4;  // of the wave's first result; the next 16 on
+    const int row = fq * 16 + (lane & 15);  // of the wave's first results; the next 16 on
     auto x_rows = [&](int first) {
         return [=](int plane, int i, int part) {
             const int f = first + i;
@@ -647,30 +708,32 @@ __global__ __launch_bounds__(C::kThreads, C::kAtOnce *C::kThreads / 256) void sm
     for (int n = 0; n < st.iterations; ++n) {
         {
             f32x4 acc[FS][FQ] = {};
-            small_product<FS, FQ, SPLIT>(C::N, acc, x_rows(wp * FS), x_rows(fq));
+            small_product<FS, FQ, SPLIT, C::N>(acc, x_rows(wp * FS), x_rows(fq));
 #pragma unroll
-            for (int i = 0; i < FS; ++i)
+            for (int i = 0; i < FS; i += 2)
 #pragma unroll
                 for (int j = 0; j < FQ; ++j)
-                    write_lds<S, SPLIT>(sq, C::kS, row + j * 16, (wp * FS + i) * 16 + col, acc[i][j] * (1.0f / kUnit));
+                    write_pair<S, SPLIT>(sq, C::kS, row + j * 16, wp * FS + i, acc[i][j] * (1.0f / kUnit), acc[i + 1][j] * (1.0f / kUnit));
         }
         __syncthreads();
         {
             f32x4 acc[FS][FQ] = {};
-            small_product<FS, FQ, SPLIT>(C::M, acc, s_rows(wp * FS), s_rows(fq));
+            small_product<FS, FQ, SPLIT, C::M>(acc, s_rows(wp * FS), s_rows(fq));
 #pragma unroll
-            for (int i = 0; i < FS; ++i)
+            for (int i = 0; i < FS; i += 2)
 #pragma unroll
                 for (int j = 0; j < FQ; ++j) {
-                    const f32x4 old = read_lds<S, SPLIT>(sq, C::kS, row + j * 16, (wp * FS + i) * 16 + col);
-                    acc[i][j] = acc[i][j] * (kC / kUnit) + old * kB;
+                    f32x4 a, b;
+                    read_pair<S, SPLIT>(sq, C::kS, row + j * 16, wp * FS + i, a, b);
+                    acc[i][j] = acc[i][j] * (kC / kUnit) + a * kB;
+                    acc[i + 1][j] = acc[i + 1][j] * (kC / kUnit) + b * kB;
                 }
             __syncthreads();
 #pragma unroll
-            for (int i = 0; i < FS; ++i)
+            for (int i = 0; i < FS; i += 2)
 #pragma unroll
                 for (int j = 0; j < FQ; ++j)
-                    write_lds<S, SPLIT>(sq, C::kS, row + j * 16, (wp * FS + i) * 16 + col, acc[i][j]);
+                    write_pair<S, SPLIT>(sq, C::kS, row + j * 16, wp * FS + i, acc[i][j], acc[i + 1][j]);
         }
         __syncthreads();
         {
@@ -678,20 +741,22 @@ __global__ __launch_bounds__(C::kThreads, C::kAtOnce *C::kThreads / 256) void sm
             auto x_columns = [&](int plane, int i, int part) {
                 return X::fragment(x + plane * C::kX + (part >> 1) * X::kBytes, wp * FX + i, part & 1);
             };
-            small_product<FX, FQ, SPLIT>(C::M, acc, x_columns, s_rows(fq));
+            small_product<FX, FQ, SPLIT, C::M>(acc, x_columns, s_rows(fq));
 #pragma unroll
-            for (int i = 0; i < FX; ++i)
+            for (int i = 0; i < FX; i += 2)
 #pragma unroll
                 for (int j = 0; j < FQ; ++j) {
-                    const f32x4 old = read_lds<X, SPLIT>(x, C::kX, row + j * 16, (wp * FX + i) * 16 + col);
-                    acc[i][j] = acc[i][j] * (1.0f / kUnit) + old * kA;
+                    f32x4 a, b;
+                    read_pair<X, SPLIT>(x, C::kX, row + j * 16, wp * FX + i, a, b);
+                    acc[i][j] = acc[i][j] * (1.0f / kUnit) + a * kA;
+                    acc[i + 1][j] = acc[i + 1][j] * (1.0f / kUnit) + b * kA;
                 }
             __syncthreads();
 #pragma unroll
-            for (int i = 0; i < FX; ++i)
+            for (int i = 0; i < FX; i += 2)
 #pragma unroll
                 for (int j = 0; j < FQ; ++j)
-                    write_lds<X, SPLIT>(x, C::kX, row + j * 16, (wp * FX + i) * 16 + col, acc[i][j]);
+                    write_pair<X, SPLIT>(x, C::kX, row + j * 16, wp * FX + i, acc[i][j], acc[i + 1][j]);
         }
         __syncthreads();
     }

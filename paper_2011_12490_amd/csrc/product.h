@@ -271,7 +271,9 @@ __device__ __forceinline__ void stored() { asm volatile("s_waitcnt lgkmcnt(0)\n\
 // transpose.  A thread brings kShare chunks, all of the same columns.
 // PAIR: a deep tile of rows of two halves of a matrix, 16 of the first and 16 of the
 // second in turn, so that a wave has both results of a column in the same lanes.
-// BOTH: not deep, but read (row_fragment) and written by rows as much as by columns.
+// BOTH: not deep, but read (row_fragment) and written by rows as much as by columns: b128
+// reads and transposing ones without bank conflicts in either form, b128 writes of 16 rows
+// 8 cycles with TILE 128, 16 without.
 constexpr int kChunks = 8;
 template <class T, int TILE, bool DEEP, int THREADS, bool MASK, bool PAIR = false, bool BOTH = false>
 struct Tile {
@@ -293,8 +295,10 @@ struct Tile {
     {
         if (DEEP)
             return r >> 1 & 7;
-        if (sizeof(T) == 2)  // in pairs of chunks: rows 0-3 and 8-11 are read at once; BOTH: within a pair by the others
-            return (TILE == 64 ? (r >> 1 & 1) | (r >> 2 & 2) : (r & 3) | (r >> 1 & 4)) << 1 | (BOTH ? r >> 2 & 1 : 0);
+        if (BOTH)  // 8 lanes write 16 bytes at a time, within 128: rows 0-7 differ in their lowest bits
+            return TILE == 64 ? (r & 3) | (r >> 1 & 4) : (r & 3) << 1 | ((r << 1 ^ r) & 8) | (r >> 2 & 1);
+        if (sizeof(T) == 2)  // in pairs of chunks: rows 0-3 and 8-11 are read at once
+            return (TILE == 64 ? (r >> 1 & 1) | (r >> 2 & 2) : (r & 3) | (r >> 1 & 4)) << 1;
         return kRowStep % 16 == 0 ? ((r & 3) | (r >> 1 & 4)) << 1 : 0;
     }
     static __device__ __forceinline__ unsigned my_thread() { return threadIdx.x % THREADS; }  // of a team
