@@ -12,24 +12,68 @@ namespace derf {
 
 namespace {
 
-// act(g) and its slope.
+// dg = dy u act'(g) and du = dy act(g) of a piece of a row; the activation is chosen once
+// for all of it, so that its elements' instructions interleave.
 template <class T>
-__device__ __forceinline__ void act_and_slope(float g, int act, float &value, float &slope)
+struct Grads {
+    static constexpr int V = Type<T>::kVec;
+    float g[V], u[V];
+};
+template <class T>
+__device__ __forceinline__ Grads<T> gradients_of(u32x4 dy, u32x4 gate, u32x4 up, int act)
 {
+    constexpr int V = Type<T>::kVec;
+    union Piece {
+        u32x4 v;
+        T e[V];
+    };
+    const Piece y = {dy}, g = {gate}, u = {up};
+    Grads<T> d;
     if (act == DERF_ACT_RELU) {
-        value = g < 0.0f ? 0.0f : g;
-        slope = g > 0.0f ? 1.0f : 0.0f;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const float x = (float)g.e[k];
+            d.g[k] = (float)y.e[k] * (float)u.e[k] * (x > 0.0f ? 1.0f : 0.0f);
+            d.u[k] = (float)y.e[k] * (x < 0.0f ? 0.0f : x);
+        }
     } else if (act == DERF_ACT_GELU) {
-        const float part = below(g);
-        value = g * part;
-        slope = part + g * 0.39894228f * exp_of(-0.5f * g * g, T{});
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const float x = (float)g.e[k], part = below(x);
+            d.g[k] = (float)y.e[k] * (float)u.e[k] * (part + x * 0.39894228f * exp_of(-0.5f * x * x, T{}));
+            d.u[k] = (float)y.e[k] * (x * part);
+        }
+    } else if (act == DERF_ACT_SILU) {
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const float x = (float)g.e[k], part = logistic(x, T{}), both = (float)y.e[k] * part;
+            d.g[k] = both * (float)u.e[k] * (1.0f + x * (1.0f - part));  // x (1 - part): 2^-24 |x| off, beside 1
+            d.u[k] = both * x;
+        }
     } else {
-        const float e = exp_of(-g, T{});
-        const float part = sizeof(T) == 2 ? __builtin_amdgcn_rcpf(1.0f + e) : 1.0f / (1.0f + e);
-        const float rest = e < 1e30f ? e * part : 1.0f;  // 1 - part, without its cancellation
-        value = act == DERF_ACT_SILU ? g * part : part;
-        slope = act == DERF_ACT_SILU ? part * (1.0f + g * rest) : part * rest;
+#pragma unroll
+        for (int k = 0; k < V; ++k) {
+            const float e = exp_of(-(float)g.e[k], T{});
+            const float part = sizeof(T) == 2 ? __builtin_amdgcn_rcpf(1.0f + e) : 1.0f / (1.0f + e);
+            const float rest = e < 1e30f ? e * part : 1.0f;  // 1 - part, without its cancellation
+            d.g[k] = (float)y.e[k] * (float)u.e[k] * (part * rest);
+            d.u[k] = (float)y.e[k] * part;
+        }
     }
+    return d;
+}
+// V values rounded.
+template <class T>
+__device__ __forceinline__ u32x4 rounded(const float (&v)[Type<T>::kVec])
+{
+    union {
+        u32x4 v;
+        T e[Type<T>::kVec];
+    } piece;
+#pragma unroll
+    for (int k = 0; k < Type<T>::kVec; ++k)
+        piece.e[k] = (T)v[k];
+    return piece.v;
 }
 
 // V elements from a row's column on, `left` of which are the row's.
@@ -73,27 +117,16 @@ __global__ __launch_bounds__(256) void gate_gradient_kernel(Problem p, const T *
     if (left > 0)
 #pragma unroll 2
         for (unsigned r = t.first + threadIdx.x / lanes; r < t.last; r += rows) {
-            union Piece {
-                u32x4 v;
-                T e[V];
-            };
-            const Piece y = {read_piece(dy + (r * dys + c), left)};
-            const Piece g = {read_piece(pre + (r * pres + c), left)};
-            const Piece u = {read_piece(pre + (r * pres + O + c), left)};
-            Piece dg, du;
+            const u32x4 y = read_piece(dy + (r * dys + c), left), g = read_piece(pre + (r * pres + c), left);
+            const Grads<T> d = gradients_of<T>(y, g, read_piece(pre + (r * pres + O + c), left), act);
 #pragma unroll
             for (int k = 0; k < V; ++k) {
-                float value, slope;
-                act_and_slope<T>((float)g.e[k], act, value, slope);
-                const float a = (float)y.e[k] * (float)u.e[k] * slope, b = (float)y.e[k] * value;
-                dg_sum[k] += a;
-                du_sum[k] += b;
-                dg.e[k] = (T)a;
-                du.e[k] = (T)b;
+                dg_sum[k] += d.g[k];
+                du_sum[k] += d.u[k];
             }
             if (dz) {
-                write_piece(dz + (r * dzs + c), dg.v, left, T{});
-                write_piece(dz + (r * dzs + O + c), du.v, left, T{});
+                write_piece(dz + (r * dzs + c), rounded<T>(d.g), left, T{});
+                write_piece(dz + (r * dzs + O + c), rounded<T>(d.u), left, T{});
             }
         }
     if (!parts)
@@ -213,24 +246,14 @@ __global__ __launch_bounds__(C::kThreads, 2) void gated_narrow_kernel(Problem p,
         X::store(sx, lds + C::kX);
 #pragma unroll
         for (int j = 0; j < Z::kShare; ++j) {
-            union Piece {
-                u32x4 v;
-                T e[V];
-            };
-            const Piece y = {sy.x[j]}, g = {sg.x[j]}, u = {su.x[j]};
-            Piece dg, du;
+            const Grads<T> d = gradients_of<T>(sy.x[j], sg.x[j], su.x[j], act);
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                float value, slope;
-                act_and_slope<T>((float)g.e[e], act, value, slope);
-                const float a = (float)y.e[e] * (float)u.e[e] * slope, b = (float)y.e[e] * value;
-                g_sums[e] += a;
-                u_sums[e] += b;
-                dg.e[e] = (T)a;
-                du.e[e] = (T)b;
+                g_sums[e] += d.g[e];
+                u_sums[e] += d.u[e];
             }
-            *reinterpret_cast<u32x4 *>(lds + C::kZ + (threadIdx.x + j * C::kThreads) * 16) = dg.v;
-            *reinterpret_cast<u32x4 *>(lds + C::kZ + Z::kBytes + (threadIdx.x + j * C::kThreads) * 16) = du.v;
+            *reinterpret_cast<u32x4 *>(lds + C::kZ + (threadIdx.x + j * C::kThreads) * 16) = rounded<T>(d.g);
+            *reinterpret_cast<u32x4 *>(lds + C::kZ + Z::kBytes + (threadIdx.x + j * C::kThreads) * 16) = rounded<T>(d.u);
         }
         stored();
         if (k + C::RT < t.last - t.first)

@@ -65,7 +65,7 @@ __device__ __forceinline__ void write_rows(const RowTile &t, int n0, int width, 
 
 // ---- gated layers: their result ---------------------------------------------------
 
-// act(g) and, for the gradient, its slope.  bf16 rows take the exponential and the
+// Of act(g), and for the gradient its slope.  bf16 rows take the exponential and the
 // reciprocal of the hardware (a unit in the last place of float each, and the
 // exponent's rounding, 2^-24 |g| of the value): far below bf16's half step of 2^-9.
 __device__ __forceinline__ float exp_of(float x, float) { return expf(x); }
@@ -73,26 +73,31 @@ __device__ __forceinline__ float exp_of(float x, __bf16) { return __builtin_amdg
 __device__ __forceinline__ float logistic(float g, float) { return 1.0f / (1.0f + expf(-g)); }
 __device__ __forceinline__ float logistic(float g, __bf16 t) { return __builtin_amdgcn_rcpf(1.0f + exp_of(-g, t)); }
 __device__ __forceinline__ float below(float g) { return 0.5f * erfcf(g * -0.70710678f); }  // of the normal distribution
-template <class T>
-__device__ __forceinline__ f32x4 activate(f32x4 g, int act)
+// v = act(g) u for N vectors; the activation is chosen once for all, so that their
+// instructions interleave.
+template <class T, int N>
+__device__ __forceinline__ void activate(const f32x4 (&g)[N], const f32x4 (&u)[N], int act, f32x4 (&v)[N])
 {
-    f32x4 v;
     if (act == DERF_ACT_RELU) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            v[k] = g[k] < 0.0f ? 0.0f : g[k];
+        for (int i = 0; i < 4 * N; ++i)
+            v[i / 4][i % 4] = g[i / 4][i % 4] < 0.0f ? 0.0f : g[i / 4][i % 4];
     } else if (act == DERF_ACT_GELU) {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            v[k] = g[k] * below(g[k]);
+        for (int i = 0; i < 4 * N; ++i)
+            v[i / 4][i % 4] = g[i / 4][i % 4] * below(g[i / 4][i % 4]);
     } else {
 #pragma unroll
-        for (int k = 0; k < 4; ++k)
-            v[k] = logistic(g[k], T{});
+        for (int i = 0; i < 4 * N; ++i)
+            v[i / 4][i % 4] = logistic(g[i / 4][i % 4], T{});
         if (act == DERF_ACT_SILU)
-            v = v * g;
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                v[i] *= g[i];
     }
-    return v;
+#pragma unroll
+    for (int i = 0; i < N; ++i)
+        v[i] *= u[i];
 }
 
 // Of 16 rows: gates in the even results of acc, ups in the odd ones.  y = act(gate) up,
@@ -112,8 +117,8 @@ __device__ __forceinline__ void write_gated(const f32x4 (&acc)[2 * PAIRS], const
             g[i] += *reinterpret_cast<const f32x4 *>(gate_bias + e);
             u[i] += *reinterpret_cast<const f32x4 *>(up_bias + e);
         }
-        v[i] = activate<T>(g[i], act) * u[i];
     }
+    activate<T, PAIRS>(g, u, act, v);
     write_16_rows<T, PAIRS * 16>(v, mine, row0, last, n0, width, y, ys);
     if (pre) {
         write_16_rows<T, PAIRS * 16>(g, mine, row0, last, n0, width, pre, pres);
