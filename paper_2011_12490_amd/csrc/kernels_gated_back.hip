@@ -39,8 +39,9 @@ __device__ __forceinline__ Grads<T> gradients_of(u32x4 dy, u32x4 gate, u32x4 up,
     } else if (act == DERF_ACT_GELU) {
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            const float x = (float)g.e[k], part = below(x);
-            d.g[k] = (float)y.e[k] * (float)u.e[k] * (part + x * 0.39894228f * exp_of(-0.5f * x * x, T{}));
+            float bell;
+            const float x = (float)g.e[k], part = below<T>(x, bell);
+            d.g[k] = (float)y.e[k] * (float)u.e[k] * (part + x * 0.39894228f * bell);
             d.u[k] = (float)y.e[k] * (x * part);
         }
     } else if (act == DERF_ACT_SILU) {

@@ -72,7 +72,25 @@ __device__ __forceinline__ float exp_of(float x, float) { return expf(x); }
 __device__ __forceinline__ float exp_of(float x, __bf16) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
 __device__ __forceinline__ float logistic(float g, float) { return 1.0f / (1.0f + expf(-g)); }
 __device__ __forceinline__ float logistic(float g, __bf16 t) { return __builtin_amdgcn_rcpf(1.0f + exp_of(-g, t)); }
-__device__ __forceinline__ float below(float g) { return 0.5f * erfcf(g * -0.70710678f); }  // of the normal distribution
+// The normal distribution's share below g, and bell = exp(-g^2 / 2).  For x >= 0
+// erfc(x) exp(x^2) / 2 is t P(t) with t = 1 / (1 + 0.45 x), P of degree 9 fitted to least
+// relative error over t in (0, 1] (3.2e-8; 6 x 2^-24 with float32's roundings): a third of
+// the instructions of erfcf.  Layer of 63 to 128 on 98,301 rows of float32 GELU_US us with it,
+// 57 with erfcf.
+template <class T>
+__device__ __forceinline__ float below(float g, float &bell)
+{
+    constexpr float kP[10] = {0.126942664f, 0.126941577f, 0.114135817f, 0.0876260847f, 0.0599751174f,
+                              -0.0111786677f, 0.0711999312f, -0.150290668f, 0.095343627f, -0.0206954815f};
+    bell = exp_of(-0.5f * g * g, T{});
+    const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(g), 0.318198052f, 1.0f));
+    float v = kP[9];
+#pragma unroll
+    for (int k = 8; k >= 0; --k)
+        v = fmaf(v, t, kP[k]);
+    v *= t * bell;
+    return g < 0.0f ? v : 1.0f - v;
+}
 // v = act(g) u for N vectors; the activation is chosen once for all, so that their
 // instructions interleave.
 template <class T, int N>
@@ -84,8 +102,10 @@ __device__ __forceinline__ void activate(const f32x4 (&g)[N], const f32x4 (&u)[N
             v[i / 4][i % 4] = g[i / 4][i % 4] < 0.0f ? 0.0f : g[i / 4][i % 4];
     } else if (act == DERF_ACT_GELU) {
 #pragma unroll
-        for (int i = 0; i < 4 * N; ++i)
-            v[i / 4][i % 4] = g[i / 4][i % 4] * below(g[i / 4][i % 4]);
+        for (int i = 0; i < 4 * N; ++i) {
+            float bell;
+            v[i / 4][i % 4] = g[i / 4][i % 4] * below<T>(g[i / 4][i % 4], bell);
+        }
     } else {
 #pragma unroll
         for (int i = 0; i < 4 * N; ++i)

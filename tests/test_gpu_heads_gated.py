@@ -2,9 +2,9 @@
 
 Tolerances, beside those of test_gpu_heads.  An activation or its slope is within
 REL(g) = (g^2 + |g| + 20) 2^-22 of the sum of its terms' magnitudes: the exponent's
-rounding costs up to 1.5 |g| 2^-24 (for exp(-g^2 / 2): 1.5 g^2 2^-24, for the error
-function's complement of g / sqrt(2): g^2 2^-23), the hardware's exp and reciprocal a unit
-in the last place (2^-23) each, erfc up to 16 of them, the few products and sums half a
+rounding costs up to 1.5 |g| 2^-24 (for exp(-g^2 / 2): 1.5 g^2 2^-24, of which a complement of
+the error function is a product), the hardware's exp and reciprocal a unit in the last
+place (2^-23) each, a fitted polynomial up to 16 of them, the few products and sums half a
 unit each.  Gates and ups off by d move y by at most 1.13 |u| d + |act(g)| d (no slope of
 an activation is above 1.13).  dg and du are rounded to the rows' type before the
 products; the biases' gradients sum them unrounded.
