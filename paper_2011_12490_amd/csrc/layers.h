@@ -75,8 +75,8 @@ __device__ __forceinline__ float logistic(float g, __bf16 t) { return __builtin_
 // The normal distribution's share below g, and bell = exp(-g^2 / 2).  For x >= 0
 // erfc(x) exp(x^2) / 2 is t P(t) with t = 1 / (1 + 0.45 x), P of degree 9 fitted to least
 // relative error over t in (0, 1] (3.2e-8; 6 x 2^-24 with float32's roundings): a third of
-// the instructions of erfcf.  Layer of 63 to 128 on 98,301 rows of float32 GELU_US us with it,
-// 57 with erfcf.
+// the instructions of erfcf.  A layer of 63 to 128 on 98,301 rows of float32: 60 us, 66 with
+// erfcf.
 template <class T>
 __device__ __forceinline__ float below(float g, float &bell)
 {
@@ -122,7 +122,7 @@ __device__ __forceinline__ void activate(const f32x4 (&g)[N], const f32x4 (&u)[N
 
 // Of 16 rows: gates in the even results of acc, ups in the odd ones.  y = act(gate) up,
 // and, where `pre` is wanted, both as they are, the ups `width` columns behind the gates.
-template <class T, int PAIRS>
+template <class T, int PAIRS, bool STAGE = sizeof(T) == 2>
 __device__ __forceinline__ void write_gated(const f32x4 (&acc)[2 * PAIRS], const float *gate_bias, const float *up_bias, int act,
                                             char *mine, unsigned row0, unsigned last, int n0, int width, T *y, long long ys,
                                             T *pre, long long pres)
@@ -139,10 +139,10 @@ __device__ __forceinline__ void write_gated(const f32x4 (&acc)[2 * PAIRS], const
         }
     }
     activate<T, PAIRS>(g, u, act, v);
-    write_16_rows<T, PAIRS * 16>(v, mine, row0, last, n0, width, y, ys);
+    write_16_rows<T, PAIRS * 16, STAGE>(v, mine, row0, last, n0, width, y, ys);
     if (pre) {
-        write_16_rows<T, PAIRS * 16>(g, mine, row0, last, n0, width, pre, pres);
-        write_16_rows<T, PAIRS * 16>(u, mine, row0, last, n0, width, pre + width, pres);
+        write_16_rows<T, PAIRS * 16, STAGE>(g, mine, row0, last, n0, width, pre, pres);
+        write_16_rows<T, PAIRS * 16, STAGE>(u, mine, row0, last, n0, width, pre + width, pres);
     }
 }
 
@@ -503,10 +503,9 @@ struct Shallow {
     using W = Tile<T, TO, DEEP_W, kThreads, false, PAIR>;
     using X = Tile<T, RT, true, kThreads, MASK>;
     static constexpr int FP = 4;  // a wave's: 64 outputs of 16 rows
-    static constexpr int kRowBytes = 64 * (int)sizeof(T) + 16;
+    static constexpr int kRowBytes = (PAIR ? 32 : 64) * (int)sizeof(T) + 16;
     static constexpr int kX = STEPS * W::kBytes, kOut = kX + STEPS * X::kBytes;
-    // results on their way out; a gated layer's float ones go from the registers
-    static constexpr int kLds = kOut + (PAIR && sizeof(T) == 4 ? 16 : 8 * 16 * kRowBytes);
+    static constexpr int kLds = kOut + 8 * 16 * kRowBytes;
     // workgroups a compute unit: by LDS, and 4 waves a SIMD
     static constexpr int kAtOnce = 2 * (kLds + 4096) <= 160 * 1024 ? 2 : 1;
 };
@@ -592,7 +591,7 @@ __global__ __launch_bounds__(C::kThreads, 2 * C::kAtOnce) void shallow_kernel(Pr
                     acc[f] = multiply(C::W::fragment(lds + i * C::W::kBytes, fp + f, part), q, acc[f], T{});
             }
         if constexpr (C::kPair) {
-            write_gated<T, C::FP / 2>(acc, biases + fp * 8, biases + C::kCols + fp * 8, act, mine, t.first + r0 + fq * 16,
+            write_gated<T, C::FP / 2, true>(acc, biases + fp * 8, biases + C::kCols + fp * 8, act, mine, t.first + r0 + fq * 16,
                                       t.last, n0 + fp * 8, O, y, ys, pre, pres);
             continue;
         }

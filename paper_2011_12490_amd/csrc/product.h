@@ -858,14 +858,14 @@ __device__ __forceinline__ void write_result(T *to, u32x4 v, int left, bool past
 // `width`: lane 16 h + l has, of row l, columns 4 h + (0 .. 3) of each 16.  bf16 through
 // the wave's place in LDS (kPieceRow a row), for pieces of 16 bytes.
 template <class T, int COLS>
-constexpr int kPieceRow = sizeof(T) == 2 ? COLS * 2 + 16 : 1;
-template <class T, int COLS>
+constexpr int kPieceRow = COLS * (int)sizeof(T) + 16;
+template <class T, int COLS, bool STAGE = sizeof(T) == 2>
 __device__ __forceinline__ void write_16_rows(const f32x4 (&v)[COLS / 16], char *mine, unsigned row0, unsigned last, int n0,
                                               int width, T *y, long long ys)
 {
     constexpr int V = Type<T>::kVec, kPieces = COLS / V;  // of a row
     const int lane = threadIdx.x & 63;
-    if constexpr (sizeof(T) == 4) {
+    if constexpr (!STAGE) {
         const unsigned row = row0 + (lane & 15);
 #pragma unroll
         for (int i = 0; i < COLS / 16; ++i) {
