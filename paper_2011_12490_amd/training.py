@@ -14,6 +14,10 @@ the trained field is the renderer's hard partition.
 
     python -m paper_2011_12490_amd.training        # fits a small analytic field
 
+The hidden layers' weights may instead go along orthogonalised directions
+(optimizer="muon").  ``GatedTrainer`` trains heads that the renderer does not have: of
+gated layers, on samples of many images with a code for each (``--gated``).
+
 torch does what is a few values a sample (distances, encodings, activations,
 the loss); the rows' way and all products run in libderf.so.
 """
@@ -50,13 +54,16 @@ class HeadTrainer:
 
     weights: float32 [K, derf_weights_count(arch)] (host), the start; precision
     "bf16" or "fp32": of the rows and the layers' weights; state_bits: of the
-    moments (AdamW)."""
+    moments (AdamW); optimizer "adamw", or "muon" for the hidden layers' weights
+    (rate muon_lr), the rest with AdamW."""
 
     def __init__(self, sites, arch: scenes.HeadArch, weights, precision: str = "bf16", top_k: int = 2,
                  beta: float = 20.0, lr: float = 5e-4, weight_decay: float = 0.0, state_bits: int = 32,
-                 device="cuda:0"):
+                 device="cuda:0", optimizer: str = "adamw", muon_lr: float = 0.02):
         if precision not in ("bf16", "fp32"):
             raise ValueError("precision is %r, not bf16 or fp32" % (precision,))
+        if optimizer not in ("adamw", "muon"):
+            raise ValueError("optimizer is %r, not adamw or muon" % (optimizer,))
         self.arch, self.precision, self.beta = arch, precision, float(beta)
         self.device = torch.device(device)
         self.dtype = torch.bfloat16 if precision == "bf16" else torch.float32
@@ -82,9 +89,16 @@ class HeadTrainer:
         self.rows_weight = [w.to(torch.bfloat16) for w in self.weight] if precision == "bf16" else self.weight
         self.weight_grad = [torch.zeros_like(w) for w in self.weight]
         self.bias_grad = [torch.zeros_like(b) for b in self.bias]
-        copies = list(self.rows_weight) + [None] * len(self.bias) if precision == "bf16" else None
-        self.optimizer = heads.AdamW(self.weight + self.bias, self.weight_grad + self.bias_grad, lr=lr,
-                                     weight_decay=weight_decay, state_bits=state_bits, copies=copies)
+        along = [optimizer == "muon" and "hidden" in name for name in self.names]
+        pick = lambda tensors, which: [t for t, a in zip(tensors, along) if a == which]  # noqa: E731
+        copies = self.rows_weight if precision == "bf16" else [None] * len(self.weight)
+        self.muon = None
+        if any(along):
+            self.muon = heads.Muon(pick(self.weight, True), pick(self.weight_grad, True), lr=muon_lr,
+                                   weight_decay=weight_decay, copies=pick(copies, True))
+        self.optimizer = heads.AdamW(pick(self.weight, False) + self.bias, pick(self.weight_grad, False) + self.bias_grad,
+                                     lr=lr, weight_decay=weight_decay, state_bits=state_bits,
+                                     copies=pick(copies, False) + [None] * len(self.bias))
         self._kept = None
 
     def _linear(self, name, x, relu):
@@ -150,6 +164,8 @@ class HeadTrainer:
         off = self.forward(x, d) - target
         self.backward(off * (2.0 / off.numel()))
         self.optimizer.step()
+        if self.muon is not None:
+            self.muon.step()
         return off.square().mean()
 
     def packed(self) -> np.ndarray:
@@ -163,6 +179,100 @@ class HeadTrainer:
         """A renderer of the heads as they are, on the trainer's device."""
         with torch.cuda.device(self.device):
             return derf.Renderer(self.host_sites, self.arch, self.packed(), self.precision)
+
+
+class GatedTrainer:
+    """Heads of gated layers on samples of many images, their optimizers and one
+    training step.
+
+    A sample's input is gamma(x), gamma(d) and its image's code; each head has `depth`
+    gated layers of `width` and a linear layer to density and colour, which are
+    mixed as in HeadTrainer.  The gated layers' weights go along orthogonalised
+    directions (muon_lr), the rest with AdamW (lr)."""
+
+    def __init__(self, sites, images: int, code_dim: int = 16, width: int = 64, depth: int = 2, pos_freqs: int = 6,
+                 dir_freqs: int = 2, act: str = "silu", precision: str = "bf16", top_k: int = 2, beta: float = 20.0,
+                 lr: float = 2e-3, muon_lr: float = 0.02, seed: int = 0, device="cuda:0"):
+        if precision not in ("bf16", "fp32"):
+            raise ValueError("precision is %r, not bf16 or fp32" % (precision,))
+        if images < 1 or code_dim < 1 or width < 1 or depth < 1:
+            raise ValueError("need images, code_dim, width and depth of at least 1")
+        sites = np.ascontiguousarray(sites, np.float32).reshape(-1, 3)
+        if not 1 <= top_k <= min(len(sites), heads.MAX_TOP_K):
+            raise ValueError("top_k is %d for %d heads" % (top_k, len(sites)))
+        self.device, self.act, self.precision = torch.device(device), act, precision
+        self.sites = torch.from_numpy(sites).to(self.device)
+        self.num_heads, self.images, self.top_k, self.beta = len(sites), images, top_k, float(beta)
+        self.pos_freqs, self.dir_freqs, self.code_dim = pos_freqs, dir_freqs, code_dim
+        self.dtype = torch.bfloat16 if precision == "bf16" else torch.float32
+        rng, K = np.random.default_rng(seed), self.num_heads
+        new = lambda *shape: torch.zeros(shape, dtype=torch.float32, device=self.device)  # noqa: E731
+
+        def start(*shape):
+            bound = np.sqrt(3.0 / shape[-1])
+            return torch.from_numpy(rng.uniform(-bound, bound, shape).astype(np.float32)).to(self.device)
+
+        fans = [6 + 6 * (pos_freqs + dir_freqs) + code_dim] + [width] * (depth - 1)
+        self.code_scale = float(code_dim) ** 0.5  # codes of small values, inputs of ordinary ones
+        self.codes, self.codes_grad = start(images, code_dim) / self.code_scale, new(images, code_dim)
+        self.weight = [start(K, 2, width, fan_in) for fan_in in fans]
+        self.bias, self.bias_grad = [new(K, 2, width) for _ in fans], [new(K, 2, width) for _ in fans]
+        self.out_weight, self.out_weight_grad = start(K, 4, width), new(K, 4, width)
+        self.out_bias, self.out_bias_grad = new(K, 4), new(K, 4)
+        rows = (lambda t: t.to(self.dtype)) if precision == "bf16" else (lambda t: t)
+        self.rows_weight, self.rows_out, self.rows_codes = [rows(w) for w in self.weight], rows(self.out_weight), rows(self.codes)
+        self.weight_grad = [torch.zeros_like(w) for w in self.rows_weight]
+        as_matrices = lambda tensors: [t.view(2 * K, t.shape[2], t.shape[3]) for t in tensors]  # noqa: E731
+        copied = precision == "bf16"
+        self.muon = heads.Muon(as_matrices(self.weight), as_matrices(self.weight_grad), lr=muon_lr,
+                               copies=as_matrices(self.rows_weight) if copied else None)
+        self.optimizer = heads.AdamW([self.codes, self.out_weight, self.out_bias] + self.bias,
+                                     [self.codes_grad, self.out_weight_grad, self.out_bias_grad] + self.bias_grad, lr=lr,
+                                     weight_decay=0.0,
+                                     copies=[self.rows_codes, self.rows_out] + [None] * (1 + depth) if copied else None)
+        self._kept = None
+
+    def forward(self, x: torch.Tensor, d: torch.Tensor, image: torch.Tensor) -> torch.Tensor:
+        """Density and colour of samples at x seen along d (float32 [T, 3] each) in images
+        (int32 [T]): float32 [T, 4].  What the gradients need is kept until the next call."""
+        ids, mix = nearest_sites(x, self.sites, self.top_k, self.beta)
+        routing = heads.route(ids, self.num_heads)
+        unit = d / d.norm(dim=1, keepdim=True)
+        codes = heads.lookup(self.rows_codes, image, self.code_scale)
+        h = heads.dispatch(torch.cat([encode(x, self.pos_freqs).to(self.dtype), encode(unit, self.dir_freqs).to(self.dtype),
+                                      codes], dim=1), routing)
+        inputs, pre = [], []
+        for w, b in zip(self.rows_weight, self.bias):
+            inputs.append(h)
+            h, kept = heads.gated(h, w, b, routing.offsets, self.act, keep=True)
+            pre.append(kept)
+        logits = heads.linear(h, self.rows_out, self.out_bias, routing.offsets).float()
+        out = torch.cat([logits[:, :1].clamp_min(0), torch.sigmoid(logits[:, 1:])], dim=1)
+        self._kept = dict(routing=routing, mix=mix, image=image, inputs=inputs, pre=pre, last=h, out=out)
+        return heads.combine(out, routing, mix)
+
+    def backward(self, dout: torch.Tensor) -> None:
+        """Gradients of every parameter from those of forward's result ([T, 4])."""
+        kept = self._kept
+        routing, out = kept["routing"], kept["out"]
+        rows, _ = heads.combine_backward(dout.contiguous(), None, routing, kept["mix"])
+        slope = torch.cat([(out[:, :1] > 0).float(), out[:, 1:] * (1 - out[:, 1:])], dim=1)
+        dh, _, _ = heads.linear_backward((rows * slope).to(self.dtype), kept["last"], self.rows_out, routing.offsets,
+                                         out_weight=self.out_weight_grad, out_bias=self.out_bias_grad)
+        for l in reversed(range(len(self.weight))):
+            dh, _, _ = heads.gated_backward(dh, kept["pre"][l], kept["inputs"][l], self.rows_weight[l], routing.offsets,
+                                            self.act, out_weight=self.weight_grad[l], out_bias=self.bias_grad[l])
+        dx = heads.dispatch_backward(dh, routing)
+        heads.lookup_backward(dx[:, dx.shape[1] - self.code_dim:], kept["image"], self.images, self.code_scale,
+                              out=self.codes_grad)
+
+    def step(self, x: torch.Tensor, d: torch.Tensor, image: torch.Tensor, target: torch.Tensor) -> torch.Tensor:
+        """One step on the mean squared error to target ([T, 4]); returns it."""
+        off = self.forward(x, d, image) - target
+        self.backward(off * (2.0 / off.numel()))
+        self.optimizer.step()
+        self.muon.step()
+        return off.square().mean()
 
 
 def start_weights(num_heads: int, arch: scenes.HeadArch, seed: int) -> np.ndarray:
@@ -186,17 +296,39 @@ def analytic_field(x: torch.Tensor, d: torch.Tensor) -> torch.Tensor:
 
 
 def fit(steps: int = 300, samples: int = 8192, num_heads: int = 8, arch: scenes.HeadArch = scenes.ARCH_TINY,
-        precision: str = "bf16", state_bits: int = 32, top_k: int = 2, lr: float = 2e-3, seed: int = 0, say=None):
+        precision: str = "bf16", state_bits: int = 32, top_k: int = 2, lr: float = 2e-3, seed: int = 0, say=None,
+        optimizer: str = "adamw"):
     """Fits heads to the analytic field; returns the trainer and every step's error."""
     rng = np.random.default_rng(seed)
     trainer = HeadTrainer(rng.uniform(-0.8, 0.8, (num_heads, 3)), arch, start_weights(num_heads, arch, seed + 1),
-                          precision, top_k, lr=lr, state_bits=state_bits)
+                          precision, top_k, lr=lr, state_bits=state_bits, optimizer=optimizer)
     g = torch.Generator(device=trainer.device).manual_seed(seed)
     errors = []
     for i in range(steps):
         x = torch.rand((samples, 3), generator=g, device=trainer.device) * 2 - 1
         d = torch.randn((samples, 3), generator=g, device=trainer.device)
         errors.append(trainer.step(x, d, analytic_field(x, d)))
+        if say and (i % 50 == 0 or i == steps - 1):
+            say("step %d: mean squared error %.5f" % (i, float(errors[-1])))
+    return trainer, torch.stack(errors).cpu().numpy()
+
+
+def fit_images(steps: int = 300, samples: int = 8192, num_heads: int = 8, images: int = 50, precision: str = "bf16",
+               top_k: int = 2, seed: int = 0, say=None):
+    """Fits gated heads to the analytic field as seen in images of different tints; returns
+    the trainer and every step's error."""
+    rng = np.random.default_rng(seed)
+    trainer = GatedTrainer(rng.uniform(-0.8, 0.8, (num_heads, 3)), images, precision=precision, top_k=top_k, seed=seed)
+    g = torch.Generator(device=trainer.device).manual_seed(seed)
+    tint = 0.6 + 0.4 * torch.rand((images, 3), generator=g, device=trainer.device)
+    errors = []
+    for i in range(steps):
+        x = torch.rand((samples, 3), generator=g, device=trainer.device) * 2 - 1
+        d = torch.randn((samples, 3), generator=g, device=trainer.device)
+        image = torch.randint(0, images, (samples,), generator=g, device=trainer.device, dtype=torch.int32)
+        target = analytic_field(x, d)
+        target[:, 1:] *= tint[image.long()]
+        errors.append(trainer.step(x, d, image, target))
         if say and (i % 50 == 0 or i == steps - 1):
             say("step %d: mean squared error %.5f" % (i, float(errors[-1])))
     return trainer, torch.stack(errors).cpu().numpy()
@@ -210,8 +342,14 @@ def main() -> None:
     ap.add_argument("--precision", choices=("bf16", "fp32"), default="bf16")
     ap.add_argument("--state-bits", type=int, choices=(8, 32), default=32)
     ap.add_argument("--top-k", type=int, default=2)
+    ap.add_argument("--optimizer", choices=("adamw", "muon"), default="adamw", help="of the hidden layers' weights")
+    ap.add_argument("--gated", action="store_true", help="heads of gated layers and a code for each image; renders nothing")
     a = ap.parse_args()
-    trainer, _ = fit(a.steps, a.samples, a.heads, precision=a.precision, state_bits=a.state_bits, top_k=a.top_k, say=print)
+    if a.gated:
+        fit_images(a.steps, a.samples, a.heads, precision=a.precision, top_k=a.top_k, say=print)
+        return
+    trainer, _ = fit(a.steps, a.samples, a.heads, precision=a.precision, state_bits=a.state_bits, top_k=a.top_k, say=print,
+                     optimizer=a.optimizer)
     cfg = scenes.CONFIGS["tiny"]
     rays_o, rays_d = scenes.make_rays(cfg)
     o, d = torch.from_numpy(rays_o).to(trainer.device), torch.from_numpy(rays_d).to(trainer.device)
