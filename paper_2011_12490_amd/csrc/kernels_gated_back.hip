@@ -418,13 +418,20 @@ hipError_t gated_backward(const LinearShape &sh, Rows dy, Rows pre, Rows x, cons
             return launch_gradients<Product<T, 256, 256, 4, 2, false, true, false, true>,
                                     Product<T, 256, 256, 4, 2, false, false, false, true, true>>(p, mw, mz, mx, dx, dw,
                                                                                                (float *)nullptr, s);
-    if (rows && dw && is_narrow(p.fan_in, p.fan_out))
-        return narrow<T, false>(p, mw, mz, mx, dx, dw, nullptr, workspace, s);
+    if constexpr (!bf16)
+        if (rows && is_narrow(p.fan_in, p.fan_out)) {
+            if (!dw)  // nothing needs x
+                mx = {mz.p, mz.stride, nullptr, 0, mz.rows, mz.cols < mx.cols ? mz.cols : mx.cols};
+            return narrow<T, false>(p, mw, mz, mx, dx, dw, nullptr, workspace, s);
+        }
     if (rows && dx.p)
-        e = rows_product<T, false, false>(p, mw, mz, nullptr, false, dx, sh.fan_in, p.fan_out, s);
+        e = rows_product<T, false, false, false>(p, mw, mz, nullptr, false, dx, sh.fan_in, p.fan_out, s);
     if (e != hipSuccess || !dw)
         return e;
-    return weights_product<T, false>(p, mz, mx, dw, (float *)nullptr, workspace, s);
+    // without rows narrow layers come here too: what is theirs is zeros
+    if (!rows)
+        return launch_sums(p, Split{256, (unsigned)sh.heads}, (const float *)nullptr, dw, nullptr, nullptr, s);
+    return weights_product<T, false, T, !bf16>(p, mz, mx, dw, (float *)nullptr, workspace, s);
 }
 
 }  // namespace

@@ -844,7 +844,7 @@ hipError_t launch_pair(const Planes &p, const Planes &q, const Planes &out, unsi
 // Tiles of 64, 128 or 256 rows and columns.  Small ones while there are few, whose loads'
 // waits others fill; from 512 of depth on 256 where their rounds of 256 workgroups cost less
 // than those of 128 (two at once a compute unit, or split one): a large one takes as long as
-// 1.65 small ones, split 3.4.  us of S, Q and Q X with 64, 128 and 256 (matrices of m x n):
+// 1.65 small ones, split 3.4 (but for split S and Q, where they are no faster).  us of S, Q and Q X with 64, 128 and 256 (matrices of m x n):
 //   float32  24 of 300 x 701        15, 12, 27.4     22, 17, 28.8    54, 42, 51
 //            8 of 512 x 512         14, 15, 15       18, 21, 19      46, 58, 59
 //            16 of 512 x 1,024      30, 23, 48       30, 22, 41      76, 60, 64
@@ -868,9 +868,11 @@ hipError_t step(const Planes &p, const Planes &q, const Planes &out, unsigned ma
     };
     const bool small = out.rows <= 64 || tiles(64) < (kDeep ? (SPLIT ? 3000 : 512) : 1000);
     const unsigned long long at_once = SPLIT ? 256 : 512;
-    const double large = (SPLIT ? 3.4 : 1.65) * (double)((tiles(256) + 255) / 256);
-    if (!small && q.cols >= 512 && large <= (double)((tiles(128) + at_once - 1) / at_once))
-        return launch_step<Product<f16, 256, 256, 4, 2, kDeep, true, false, true>, KIND, SPLIT>(p, q, out, matrices, s);
+    if constexpr (!SPLIT || !kDeep) {
+        const double large = (SPLIT ? 3.4 : 1.65) * (double)((tiles(256) + 255) / 256);
+        if (!small && q.cols >= 512 && large <= (double)((tiles(128) + at_once - 1) / at_once))
+            return launch_step<Product<f16, 256, 256, 4, 2, kDeep, true, false, true>, KIND, SPLIT>(p, q, out, matrices, s);
+    }
     if constexpr (SPLIT)
         return small ? launch_pair<Product<f16, 64, 64, 2, 2, kDeep, true, false, true>, KIND>(p, q, out, matrices, s)
                      : launch_pair<Product<f16, 128, 128, 2, 4, kDeep, true, false, true>, KIND>(p, q, out, matrices, s);

@@ -1112,16 +1112,18 @@ bool few_rows(const Problem &p, int width, int depth)
     return tiles <= (sizeof(T) == 4 && depth >= 256 ? 640 : 256);
 }
 
-// The rows' product with tiles for its width.
-template <class T, bool DEEP_W, bool MASK>
+// The rows' product with tiles for its width.  NARROW: shallow products of at most 64
+// columns come here (not those of gated layers, whose narrow ones have a kernel of their own).
+template <class T, bool DEEP_W, bool MASK, bool NARROW = true>
 hipError_t rows_product(const Problem &p, const Matrix<T> &w, const Matrix<T> &x, const float *bias,
                         bool relu, Rows y, int width, int depth, hipStream_t s)
 {
     if (is_shallow<T, DEEP_W>(p, w, x, width, depth)) {
         const bool past = past_caches(static_cast<const T *>(y.p), y.stride, width);
-        if (width <= 64)
-            return past ? shallow<T, 64, DEEP_W, MASK, true>(p, w, x, bias, relu, y, width, s)
-                        : shallow<T, 64, DEEP_W, MASK, false>(p, w, x, bias, relu, y, width, s);
+        if constexpr (NARROW)
+            if (width <= 64)
+                return past ? shallow<T, 64, DEEP_W, MASK, true>(p, w, x, bias, relu, y, width, s)
+                            : shallow<T, 64, DEEP_W, MASK, false>(p, w, x, bias, relu, y, width, s);
         return past ? shallow<T, 128, DEEP_W, MASK, true>(p, w, x, bias, relu, y, width, s)
                     : shallow<T, 128, DEEP_W, MASK, false>(p, w, x, bias, relu, y, width, s);
     }
@@ -1197,10 +1199,13 @@ hipError_t launch_weights(const Problem &p, const Matrix<typename C::T> &dz,
             weights_kernel<C, To><<<groups, C::kThreads, 0, s>>>(p, dz, x, to_w, to_b, split.stretch, split.places, row_tiles, col_tiles, from);
         });
     };
-    if (!partial)
+    // tiles of 256 x 256 are taken from 256 of them on: at least 512 of 128 x 128, and no stretches
+    if (C::TP == 256 || !partial)
         return launch(dw, db);
-    const hipError_t e = launch(dw ? wparts : nullptr, db ? bparts : nullptr);
-    return e != hipSuccess ? e : launch_sums(p, split, wparts, dw, bparts, db, s);
+    if constexpr (C::TP != 256) {
+        const hipError_t e = launch(dw ? wparts : nullptr, db ? bparts : nullptr);
+        return e != hipSuccess ? e : launch_sums(p, split, wparts, dw, bparts, db, s);
+    }
 }
 
 // 256 x 256 tiles from 256 of them on, one a compute unit.  dW and db, us with large and
@@ -1208,7 +1213,7 @@ hipError_t launch_weights(const Problem &p, const Matrix<typename C::T> &dz,
 // 1,024 on 16,384 of 8 (128) 115, 70; 512 to 512 on 65,536 of 16 (64) 111, 80; at the line
 // small ones would win: 1,024 to 2,048 on 16,384 of 8 119, 101; 1,024 to 1,024 on 65,536 of
 // 16 387, 271.
-template <class T, bool MASK, class W>
+template <class T, bool MASK, class W, bool NARROW = true>
 hipError_t weights_product(const Problem &p, const Matrix<T> &dz, const Matrix<T> &x, W *dw,
                            float *db, char *workspace, hipStream_t s)
 {
@@ -1229,7 +1234,9 @@ hipError_t weights_product(const Problem &p, const Matrix<T> &dz, const Matrix<T
         return launch_weights<Product<T, 64, 128, 2, 2, false, false, MASK, false, true>>(p, dz, x, dw, db, workspace, s);
     if (wide_i)
         return launch_weights<Product<T, 128, 64, 2, 2, false, false, MASK, false, true>>(p, dz, x, dw, db, workspace, s);
-    return launch_weights<Product<T, 64, 64, 2, 2, false, false, MASK, false, true>>(p, dz, x, dw, db, workspace, s);
+    if constexpr (NARROW)
+        return launch_weights<Product<T, 64, 64, 2, 2, false, false, MASK, false, true>>(p, dz, x, dw, db, workspace, s);
+    return hipErrorInvalidValue;  // no call: bf16 gated layers of at most 64 to 2 x 32 are narrow
 }
 
 // Layers that narrow_kernel takes, and its stretches: a workgroup for each, as

@@ -25,6 +25,14 @@ ACTS = list(heads.ACTIVATIONS)
 CASES = LINEAR_CASES + [([16000, 16700], 9, 512, 1024, 0, 0), ([9000, 300], 3, 64, 64, 0, 0), ([70000], 0, 128, 128, 0, 0),
                         ([40000, 10], 6, 30, 24, 1, 1)]
 
+# More kernels' cases: counts by head, rows without a head, fan_in, fan_out.  Shallow layers of
+# every depth and both widths (odd ones, which do not go to LDS by themselves), rows' gradients
+# of shallow ones, weights' of many heads as wholes, and narrow results of middling rows
+MORE = [([20000, 0, 13000], 7, I, O) for I in (20, 63, 90, 127, 155, 191, 255, 319) for O in (24, 130)]
+MORE += [([32000, 1000], 5, 190, 60), ([32000, 1000], 5, 192, 16), ([32000, 1000], 0, 192, 60), ([32000, 1000], 0, 190, 30),
+         ([32000, 1000], 0, 256, 30), ([32000, 1000], 0, 190, 16), ([20] * 64, 3, 256, 256), ([20] * 200, 0, 40, 140), ([5] * 256, 2, 200, 20), ([9000, 300], 3, 400, 24),
+         ([3000, 900], 0, 100, 50), ([3000, 900], 0, 128, 64)]
+
 
 def near(got, want, size, n, rel):
     """size: the products' magnitudes summed; rel: what their factors are off by, of size."""
@@ -83,7 +91,7 @@ def check_gated(y, pre, x, w, b, offsets, act, I):
 
 
 @pytest.mark.parametrize("dtype", [FP32, BF16])
-@pytest.mark.parametrize("at,case", list(enumerate(CASES)))
+@pytest.mark.parametrize("at,case", list(enumerate(CASES + [c + (0, 0) for c in MORE])))
 def test_gated(at, case, dtype):
     counts, tail, I, O, pad, shift = case
     x, w, b, offsets, _ = gated_layer(*case, dtype, I + O)
@@ -109,7 +117,7 @@ def test_every_activation(act, dtype):
 
 
 @pytest.mark.parametrize("dtype", [FP32, BF16])
-@pytest.mark.parametrize("at,case", list(enumerate(CASES)))
+@pytest.mark.parametrize("at,case", list(enumerate(CASES + [c + (0, 0) for c in MORE])))
 def test_gated_gradients(at, case, dtype):
     counts, tail, I, O, pad, shift = case
     x, w, _, offsets, g = gated_layer(*case, dtype, I + 7 * O)

@@ -1,0 +1,78 @@
+"""Which kernels the gated layers, the table lookups and the orthogonalised updates launch,
+without a GPU (tests/more_forms_driver.cpp runs the library's own choice and writes
+kernels down by name): the GPU tests' cases reach every one, so that a rule that moves
+takes no kernel out of their sight."""
+import os
+import shutil
+import subprocess
+
+import pytest
+
+import test_gpu_heads_gated as gated
+import test_gpu_lookup as lookup
+import test_gpu_muon as muon
+from paper_2011_12490_amd import build
+
+UNITS = ["kernels_gated", "kernels_gated_back", "kernels_lookup", "kernels_muon"]
+
+
+def line(name, *numbers):
+    return " ".join([name] + [str(int(n)) for n in numbers])
+
+
+def calls_of_the_tests():
+    calls = []
+    for bf16 in (0, 1):
+        for counts, tail, I, O, pad, shift in gated.CASES:
+            at = (bf16, sum(counts) + tail, len(counts), I, O, pad, shift)
+            calls += [line("gated", *at, keep) for keep in (0, 1)] + [line("backward", *at, outputs) for outputs in (6, 7)]
+        for counts, tail, I, O in gated.MORE:
+            at = (bf16, sum(counts) + tail, len(counts), I, O, 0, 0)
+            calls += [line("gated", *at, 1)] + [line("backward", *at, outputs) for outputs in (6, 7)]
+        for T, V, D, pad, shift, _ in lookup.CASES:
+            calls += [line("lookup", bf16, T, V, D, pad, shift), line("gradient", bf16, T, V, D, pad, shift)]
+        for K, O, I in muon.SHAPES:
+            calls.append(line("matrices", 1 - bf16, K, O, I))
+    return calls
+
+
+@pytest.fixture(scope="module")
+def launched(tmp_path_factory):
+    """All kernels' names, and those that each of some calls launches."""
+    cxx = shutil.which("g++")
+    if cxx is None:
+        pytest.skip("no g++")
+    objects = [os.path.join(build.BUILD, unit + ".o") for unit in UNITS]
+    if not all(os.path.exists(o) for o in objects):
+        build.build()
+    exe = str(tmp_path_factory.mktemp("forms") / "more_forms")
+    rocm = os.path.join(os.path.dirname(os.path.dirname(os.path.realpath(build.HIPCC))), "include")
+    subprocess.run([cxx, "-std=c++17", "-O1", "-Wall", "-D__HIP_PLATFORM_AMD__", "-I" + rocm,
+                    "-I" + os.path.join(build.ROOT, "include"), "-I" + build.CSRC,
+                    os.path.join(build.ROOT, "tests", "more_forms_driver.cpp")] + objects + ["-o", exe], check=True)
+
+    def run(calls):
+        r = subprocess.run([exe], input="\n".join(calls), capture_output=True, text=True, timeout=60, check=True)
+        head, *per_call = r.stdout.split("call\n")
+        assert len(per_call) == len(calls)
+        names = [[row[4:] for row in part.splitlines() if row.startswith("ran ")] for part in per_call]
+        return {row[4:] for row in head.splitlines() if row.startswith("has ")}, names
+
+    return run
+
+
+def test_the_gpu_tests_reach_every_kernel(launched):
+    kernels, per_call = launched(calls_of_the_tests())
+    assert len(kernels) > 60
+    ran = {name for names in per_call for name in names}
+    assert ran <= kernels
+    assert not kernels - ran, "no test runs:\n" + "\n".join(sorted(kernels - ran))
+
+
+def test_launches_of_ordinary_calls(launched):
+    """How many launches a call takes: what a small call's time is made of."""
+    calls = [line("gated", 1, 16, 16, 64, 64, 0, 0, 1), line("backward", 1, 500, 4, 128, 128, 0, 0, 7),
+             line("lookup", 0, 64, 500, 48, 0, 0), line("gradient", 0, 64, 500, 48, 0, 0), line("gradient", 0, 5000, 500, 48, 0, 0),
+             line("gradient", 0, 50000, 500, 48, 0, 0), line("matrices", 1, 144, 128, 128), line("matrices", 1, 3, 300, 700)]
+    _, names = launched(calls)
+    assert [len(n) for n in names] == [1, 2, 1, 1, 3, 5, 1, 18]
