@@ -616,6 +616,7 @@ int derf_orthogonalise(const void *x, long long num_matrices, int fan_out, int f
  *   param, grad   [num_matrices][fan_out][fan_in], float or bf16 each
  *   m             float, the same shape; zeros at the start
  *   copy          NULL, or bf16: the updated parameters rounded
+ * No array that is written (param, m, copy) shares memory with another of any tensor.
  * num_matrices <= 32768 in all tensors together, fan_out, fan_in in [1, 16384]. */
 typedef struct {
     void *param;

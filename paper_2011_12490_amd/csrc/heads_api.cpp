@@ -64,6 +64,32 @@ struct MuonGroup {
 
 int padded_side(int n) { return (n + 63) / 64 * 64; }
 
+// An array of a tensor, in bytes.
+struct Span {
+    uintptr_t from, to;
+    bool written;
+    int tensor;
+};
+void add_span(std::vector<Span> &spans, const void *p, long long bytes, bool written, int tensor)
+{
+    if (p && bytes > 0)
+        spans.push_back({reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + (uintptr_t)bytes, written, tensor});
+}
+// A tensor with an array that is written and shares memory with another array, or -1.
+int overlapping(std::vector<Span> &spans)
+{
+    std::sort(spans.begin(), spans.end(), [](const Span &a, const Span &b) { return a.from < b.from; });
+    uintptr_t any = 0, written = 0;  // the furthest ends so far
+    for (const Span &s : spans) {
+        if (s.from < (s.written ? any : written))
+            return s.tensor;
+        any = std::max(any, s.to);
+        if (s.written)
+            written = std::max(written, s.to);
+    }
+    return -1;
+}
+
 }  // namespace
 
 struct derf_muon {
@@ -232,6 +258,7 @@ int derf_muon_create(derf_muon **out, const derf_muon_tensor *tensors, int num_t
     derf_muon *opt = nullptr;
     try {
         std::vector<MuonEntry> table;
+        std::vector<Span> spans;
         long long matrices = 0;
         for (int i = 0; i < num_tensors; ++i) {
             const derf_muon_tensor &t = tensors[i];
@@ -245,15 +272,23 @@ int derf_muon_create(derf_muon **out, const derf_muon_tensor *tensors, int num_t
             if (misaligned(t.param, pa) || misaligned(t.grad, ga) || misaligned(t.m, 4) || misaligned(t.copy, 2))
                 return report(DERF_ERR_INVALID_ARG, "tensor %d: an array is not aligned to its elements", i);
             const long long size = (long long)t.fan_out * t.fan_in;
+            const long long all = size * t.num_matrices;
+            add_span(spans, t.param, all * pa, true, i);
+            add_span(spans, t.m, all * 4, true, i);
+            add_span(spans, t.copy, all * 2, true, i);
+            add_span(spans, t.grad, all * ga, false, i);
             for (int k = 0; k < t.num_matrices; ++k)
                 table.push_back({static_cast<char *>(t.param) + k * size * pa, static_cast<const char *>(t.grad) + k * size * ga,
                                  t.m + k * size, t.copy ? static_cast<char *>(t.copy) + k * size * 2 : nullptr, t.fan_out, t.fan_in,
                                  t.param_precision == DERF_PREC_BF16, t.grad_precision == DERF_PREC_BF16,
                                  (float)sqrt(std::max(1.0, (double)t.fan_out / t.fan_in))});
         }
+        const int twice = overlapping(spans);
+        if (twice >= 0)
+            return report(DERF_ERR_INVALID_ARG, "tensor %d: an array shares memory with another", twice);
         auto small = [](const MuonEntry &e) { return e.fan_out <= 128 && e.fan_in <= 128; };
         // few small matrices run at once whatever their shapes: 128 of 128 x 128 and 16 of
-        // 128 x 63 in one launch of 128 x 128 places KEY_ONE us, in two KEY_TWO
+        // 128 x 63 in one launch of 128 x 128 places ONE_US us, in two TWO_US
         const bool as_one = std::count_if(table.begin(), table.end(), small) <= 256;
         auto key = [&](const MuonEntry &e) {
             int o = padded_side(e.fan_out), i = padded_side(e.fan_in);

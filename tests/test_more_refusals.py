@@ -172,6 +172,22 @@ def test_muon_tensors(kw, text):
     assert not h.value
 
 
+@pytest.mark.parametrize("first,second", [
+    (dict(), dict()), (dict(), dict(param=P + 64)), (dict(m=1 << 20), dict(param=1 << 21, grad=(1 << 20) + 572, m=1 << 22)),
+    (dict(param=1 << 20, m=1 << 21, copy=(1 << 20) + 286), None), (dict(param=1 << 20, m=(1 << 20) + 575), None),
+    (dict(param=1 << 20, m=1 << 21), dict(param=1 << 22, m=1 << 23, copy=1 << 20))])
+def test_muon_arrays_that_share_memory(first, second):
+    """Arrays of 2 matrices of 8 x 9: 576 bytes in float, 288 in bf16."""
+    h = ctypes.c_void_p(1)
+    tensors = [_matrices(**t) for t in (first, second) if t is not None]
+    table = (derf.derf_muon_tensor * len(tensors))(*tensors)
+    if first.get("m") == (1 << 20) + 575:
+        refused(lib().derf_muon_create(ctypes.byref(h), table, len(tensors)), b"aligned")
+    else:
+        refused(lib().derf_muon_create(ctypes.byref(h), table, len(tensors)), b"shares memory")
+    assert not h.value
+
+
 def test_muon_calls():
     L = lib()
     h = ctypes.c_void_p(1)
