@@ -40,22 +40,22 @@ __device__ __forceinline__ Grads<T> gradients_of(u32x4 dy, u32x4 gate, u32x4 up,
 #pragma unroll
         for (int k = 0; k < V; ++k) {
             float bell;
-            const float x = (float)g.e[k], part = below<T>(x, bell);
+            const float x = (float)g.e[k], part = below(x, bell);
             d.g[k] = (float)y.e[k] * (float)u.e[k] * (part + x * 0.39894228f * bell);
             d.u[k] = (float)y.e[k] * (x * part);
         }
     } else if (act == DERF_ACT_SILU) {
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            const float x = (float)g.e[k], part = logistic(x, T{}), both = (float)y.e[k] * part;
+            const float x = (float)g.e[k], part = logistic(x), both = (float)y.e[k] * part;
             d.g[k] = both * (float)u.e[k] * (1.0f + x * (1.0f - part));  // x (1 - part): 2^-24 |x| off, beside 1
             d.u[k] = both * x;
         }
     } else {
 #pragma unroll
         for (int k = 0; k < V; ++k) {
-            const float e = exp_of(-(float)g.e[k], T{});
-            const float part = sizeof(T) == 2 ? __builtin_amdgcn_rcpf(1.0f + e) : 1.0f / (1.0f + e);
+            const float e = exp_of(-(float)g.e[k]);
+            const float part = __builtin_amdgcn_rcpf(1.0f + e);
             const float rest = e < 1e30f ? e * part : 1.0f;  // 1 - part, without its cancellation
             d.g[k] = (float)y.e[k] * (float)u.e[k] * (part * rest);
             d.u[k] = (float)y.e[k] * part;
@@ -151,32 +151,36 @@ __global__ __launch_bounds__(256) void gate_gradient_kernel(Problem p, const T *
 
 // ---- narrow layers, all gradients in one pass over the rows --------------------------
 
-// bf16 layers of at most 128 to 2 x 128: as narrow_kernel, a workgroup a compute unit keeps
-// its head's weights in LDS and its part of dW in registers and goes through a stretch of the
-// head's rows, RT at a time, the next ones' loads under way.  dz is made on the way from the
-// registers to LDS, where both products read it: dx by rows, dW by columns.
-template <int TI_, int TO_>
+// Layers of at most 128 to 2 x 128 (float: where one of both is at most 64, whose weights
+// fit): as narrow_kernel, a workgroup a compute unit keeps its head's weights in LDS and its
+// part of dW in registers and goes through a stretch of the head's rows, RT at a time, the
+// next ones' loads under way.  dz is made on the way from the registers to LDS, where both
+// products read it: dx by rows, dW by columns.
+template <class T_, int TI_, int TO_>
 struct GatedNarrow {
-    using T = __bf16;
-    static constexpr int TI = TI_, TO = TO_, kThreads = 512, RT = 64, V = Type<T>::kVec;
-    using X = Tile<T, TI, false, kThreads, false, false, true>;
-    using Z = Tile<T, TO, false, kThreads, false, false, true>;  // dg, and du
-    static_assert(X::D == RT && Z::D == RT, "a tile of rows a step");
+    using T = T_;
+    static constexpr int TI = TI_, TO = TO_, kThreads = 512, V = Type<T>::kVec;
+    static constexpr bool kBoth = sizeof(T) == 2;
+    using X = Tile<T, TI, false, kThreads, false, false, kBoth>;
+    using Z = Tile<T, TO, false, kThreads, false, false, kBoth>;  // dg, and du
+    static constexpr int RT = X::D, kSpan = RT / 2;               // rows of a step, a fragment's depth
+    static_assert(Z::D == RT, "a tile of rows a step");
     static constexpr int FP = TI / 32, FQ = 2 * TO / 64;  // dW: 2 waves over fan_in, 4 over gates and ups
-    static constexpr int FX = TI / 32;                    // dx: 4 waves over rows, 2 over fan_in
-    static constexpr int kWeights = 2 * TO / RT;          // tiles of RT outputs
+    static constexpr int kRowGroups = RT / 16, kColGroups = 8 / kRowGroups, FX = TI / 16 / kColGroups;  // dx
+    static constexpr int kWeights = 2 * TO / RT;  // tiles of RT outputs
     static constexpr int kZ = 0, kX = kZ + 2 * Z::kBytes, kW = kX + X::kBytes, kOut = kW + kWeights * X::kBytes;
     static constexpr int kRowsOfThreads = kThreads / Z::kPerRow;
     static constexpr int kSums = kRowsOfThreads * (2 * TO + 1) * 4;
-    static constexpr int kAll = kOut + 8 * 16 * kPieceRow<T, FX * 16>, kLds = kAll > kSums ? kAll : kSums;
+    static constexpr int kAll = kOut + (sizeof(T) == 2 ? 8 * 16 * kPieceRow<T, FX * 16> : 0), kLds = kAll > kSums ? kAll : kSums;
 };
 
 template <class C>
-__global__ __launch_bounds__(C::kThreads, 2) void gated_narrow_kernel(Problem p, Matrix<__bf16> w, Matrix<__bf16> dy, Matrix<__bf16> pre,
-                                                                      int act, Matrix<__bf16> x, __bf16 *dx, long long dxs, float *dw,
-                                                                      float *db, unsigned stretch)
+__global__ __launch_bounds__(C::kThreads, 2) void gated_narrow_kernel(Problem p, Matrix<typename C::T> w, Matrix<typename C::T> dy,
+                                                                      Matrix<typename C::T> pre, int act, Matrix<typename C::T> x,
+                                                                      typename C::T *dx, long long dxs, float *dw, float *db,
+                                                                      unsigned stretch)
 {
-    using T = __bf16;
+    using T = typename C::T;
     using X = typename C::X;
     using Z = typename C::Z;
     constexpr int V = C::V;
@@ -232,7 +236,7 @@ __global__ __launch_bounds__(C::kThreads, 2) void gated_narrow_kernel(Problem p,
         g_sums[k] = u_sums[k] = 0.0f;
     f32x4 acc[C::FP][C::FQ] = {};
     const int fp = wave % 2 * C::FP, fq = wave / 2 * C::FQ;  // of dW; results fq on are of the ups from TO / 16 on
-    const int fr = wave / 2, fc = wave % 2 * C::FX;          // of dx
+    const int fr = wave / C::kColGroups, fc = wave % C::kColGroups * C::FX;  // of dx
     char *mine = lds + C::kOut + wave * 16 * kPieceRow<T, C::FX * 16>;
     constexpr int kOfHalf = C::TO / 16;
     const char *const z_of_dw = lds + C::kZ + (fq >= kOfHalf ? Z::kBytes : 0);
@@ -264,18 +268,18 @@ __global__ __launch_bounds__(C::kThreads, 2) void gated_narrow_kernel(Problem p,
 #pragma unroll
             for (int half = 0; half < 2; ++half)
 #pragma unroll
-                for (int part = 0; part < C::TO / 32; ++part) {
+                for (int part = 0; part < C::TO / C::kSpan; ++part) {
                     const u32x4 q = Z::row_fragment(lds + C::kZ + half * Z::kBytes, fr, part);
 #pragma unroll
                     for (int i = 0; i < C::FX; ++i)
-                        rows[i] = multiply(X::fragment(lds + C::kW + (half * C::TO / C::RT + part / 2) * X::kBytes, fc + i, part & 1),
+                        rows[i] = multiply(X::fragment(lds + C::kW + (half * C::TO + part * C::kSpan) / C::RT * X::kBytes, fc + i, part & 1),
                                            q, rows[i], T{});
                 }
             write_16_rows<T, C::FX * 16>(rows, mine, t.first + k + fr * 16, t.last, fc * 16, I, dx, dxs);
         }
         if (dw)
 #pragma unroll
-            for (int part = 0; part < C::RT / 32; ++part) {
+            for (int part = 0; part < 2; ++part) {
                 u32x4 q[C::FQ];
 #pragma unroll
                 for (int j = 0; j < C::FQ; ++j)
@@ -322,22 +326,25 @@ __global__ __launch_bounds__(C::kThreads, 2) void gated_narrow_kernel(Problem p,
     }
 }
 
-template <int TI, int TO>
-hipError_t gated_narrow(const Problem &p, const Matrix<__bf16> &w, const Matrix<__bf16> &dy, const Matrix<__bf16> &pre, int act,
-                        const Matrix<__bf16> &x, Rows dx, __bf16 *dw, float *db, char *workspace, hipStream_t s)
+template <class T, int TI, int TO>
+hipError_t gated_narrow(const Problem &p, const Matrix<T> &w, const Matrix<T> &dy, const Matrix<T> &pre, int act,
+                        const Matrix<T> &x, Rows dx, T *dw, float *db, char *workspace, hipStream_t s)
 {
-    using C = GatedNarrow<TI, TO>;
+    using C = GatedNarrow<T, TI, TO>;
     const Split split = narrow_split(p.rows, p.heads, p.fan_in, p.fan_out, true);
     float *wparts = reinterpret_cast<float *>(workspace);
     float *bparts = wparts + (size_t)split.places * 2 * p.fan_out * p.fan_in;
-    gated_narrow_kernel<C><<<split.places + 1, C::kThreads, 0, s>>>(p, w, dy, pre, act, x, static_cast<__bf16 *>(const_cast<void *>(dx.p)),
+    gated_narrow_kernel<C><<<split.places + 1, C::kThreads, 0, s>>>(p, w, dy, pre, act, x, static_cast<T *>(const_cast<void *>(dx.p)),
                                                                     dx.stride, dw ? wparts : nullptr, db ? bparts : nullptr, split.stretch);
     const hipError_t e = hipGetLastError();
     const Problem both = {p.offsets, p.rows, p.heads, p.fan_in, 2 * p.fan_out};
     return e != hipSuccess || (!dw && !db) ? e : launch_sums(both, split, wparts, dw, bparts, db, s);
 }
 
-bool is_gated_narrow(int fan_in, int fan_out, bool bf16) { return bf16 && fan_in <= 128 && fan_out <= 128; }
+bool is_gated_narrow(int fan_in, int fan_out, bool bf16)
+{
+    return fan_in <= 128 && fan_out <= 128 && (bf16 || fan_in <= 64 || fan_out <= 64);
+}
 size_t gated_narrow_bytes(unsigned rows, int heads, int fan_in, int fan_out)
 {
     return (size_t)narrow_split(rows, heads, fan_in, fan_out, true).places * 2 * fan_out * ((size_t)fan_in + 1) * sizeof(float);
@@ -382,19 +389,20 @@ hipError_t gated_backward(const LinearShape &sh, Rows dy, Rows pre, Rows x, cons
     const bool rows = sh.rows > 0;
     const Matrix<T> mw = {static_cast<const T *>(w), sh.fan_in, nullptr, 0, (unsigned)p.fan_out, sh.fan_in};
     Matrix<T> mx = {static_cast<const T *>(x.p), x.stride, nullptr, 0, sh.rows, sh.fan_in};
-    if constexpr (bf16)
-        if (rows && is_gated_narrow(sh.fan_in, sh.fan_out, bf16)) {
-            const Problem one = {sh.offsets, sh.rows, sh.heads, sh.fan_in, sh.fan_out};
-            const Matrix<T> my = {static_cast<const T *>(dy.p), dy.stride, nullptr, 0, sh.rows, sh.fan_out};
-            const Matrix<T> mp = {static_cast<const T *>(pre.p), pre.stride, nullptr, 0, sh.rows, sh.fan_out};
-            if (!dw)  // nothing needs x
-                mx = {my.p, my.stride, nullptr, 0, my.rows, my.cols < mx.cols ? my.cols : mx.cols};
-            if (sh.fan_in <= 64)
-                return sh.fan_out <= 64 ? gated_narrow<64, 64>(one, mw, my, mp, act, mx, dx, dw, db, workspace, s)
-                                        : gated_narrow<64, 128>(one, mw, my, mp, act, mx, dx, dw, db, workspace, s);
-            return sh.fan_out <= 64 ? gated_narrow<128, 64>(one, mw, my, mp, act, mx, dx, dw, db, workspace, s)
-                                    : gated_narrow<128, 128>(one, mw, my, mp, act, mx, dx, dw, db, workspace, s);
-        }
+    if (rows && is_gated_narrow(sh.fan_in, sh.fan_out, bf16)) {
+        const Problem one = {sh.offsets, sh.rows, sh.heads, sh.fan_in, sh.fan_out};
+        const Matrix<T> my = {static_cast<const T *>(dy.p), dy.stride, nullptr, 0, sh.rows, sh.fan_out};
+        const Matrix<T> mp = {static_cast<const T *>(pre.p), pre.stride, nullptr, 0, sh.rows, sh.fan_out};
+        if (!dw)  // nothing needs x
+            mx = {my.p, my.stride, nullptr, 0, my.rows, my.cols < mx.cols ? my.cols : mx.cols};
+        if (sh.fan_in <= 64)
+            return sh.fan_out <= 64 ? gated_narrow<T, 64, 64>(one, mw, my, mp, act, mx, dx, dw, db, workspace, s)
+                                    : gated_narrow<T, 64, 128>(one, mw, my, mp, act, mx, dx, dw, db, workspace, s);
+        if (sh.fan_out <= 64)
+            return gated_narrow<T, 128, 64>(one, mw, my, mp, act, mx, dx, dw, db, workspace, s);
+        if constexpr (bf16)
+            return gated_narrow<T, 128, 128>(one, mw, my, mp, act, mx, dx, dw, db, workspace, s);
+    }
     float *parts = reinterpret_cast<float *>(workspace);
     workspace += sums_bytes(sh.rows, sh.heads, sh.fan_out, bf16);
     T *dz = dx.p || dw ? reinterpret_cast<T *>(workspace) : nullptr;
@@ -418,12 +426,6 @@ hipError_t gated_backward(const LinearShape &sh, Rows dy, Rows pre, Rows x, cons
             return launch_gradients<Product<T, 256, 256, 4, 2, false, true, false, true>,
                                     Product<T, 256, 256, 4, 2, false, false, false, true, true>>(p, mw, mz, mx, dx, dw,
                                                                                                (float *)nullptr, s);
-    if constexpr (!bf16)
-        if (rows && is_narrow(p.fan_in, p.fan_out)) {
-            if (!dw)  // nothing needs x
-                mx = {mz.p, mz.stride, nullptr, 0, mz.rows, mz.cols < mx.cols ? mz.cols : mx.cols};
-            return narrow<T, false>(p, mw, mz, mx, dx, dw, nullptr, workspace, s);
-        }
     if (rows && dx.p)
         e = rows_product<T, false, false, false>(p, mw, mz, nullptr, false, dx, sh.fan_in, p.fan_out, s);
     if (e != hipSuccess || !dw)

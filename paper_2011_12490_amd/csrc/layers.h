@@ -65,24 +65,20 @@ __device__ __forceinline__ void write_rows(const RowTile &t, int n0, int width, 
 
 // ---- gated layers: their result ---------------------------------------------------
 
-// Of act(g), and for the gradient its slope.  bf16 rows take the exponential and the
-// reciprocal of the hardware (a unit in the last place of float each, and the
-// exponent's rounding, 2^-24 |g| of the value): far below bf16's half step of 2^-9.
-__device__ __forceinline__ float exp_of(float x, float) { return expf(x); }
-__device__ __forceinline__ float exp_of(float x, __bf16) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
-__device__ __forceinline__ float logistic(float g, float) { return 1.0f / (1.0f + expf(-g)); }
-__device__ __forceinline__ float logistic(float g, __bf16 t) { return __builtin_amdgcn_rcpf(1.0f + exp_of(-g, t)); }
+// Of act(g), and for the gradient its slope.  The hardware's exponential and reciprocal: a
+// unit in the last place of float each, and the exponent's rounding, 2^-24 |g| of the value.
+__device__ __forceinline__ float exp_of(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504f); }
+__device__ __forceinline__ float logistic(float g) { return __builtin_amdgcn_rcpf(1.0f + exp_of(-g)); }
 // The normal distribution's share below g, and bell = exp(-g^2 / 2).  For x >= 0
 // erfc(x) exp(x^2) / 2 is t P(t) with t = 1 / (1 + 0.45 x), P of degree 9 fitted to least
 // relative error over t in (0, 1] (3.2e-8; 6 x 2^-24 with float32's roundings): a third of
 // the instructions of erfcf.  A layer of 63 to 128 on 98,301 rows of float32: 60 us, 66 with
 // erfcf.
-template <class T>
 __device__ __forceinline__ float below(float g, float &bell)
 {
     constexpr float kP[10] = {0.126942664f, 0.126941577f, 0.114135817f, 0.0876260847f, 0.0599751174f,
                               -0.0111786677f, 0.0711999312f, -0.150290668f, 0.095343627f, -0.0206954815f};
-    bell = exp_of(-0.5f * g * g, T{});
+    bell = exp_of(-0.5f * g * g);
     const float t = __builtin_amdgcn_rcpf(fmaf(fabsf(g), 0.318198052f, 1.0f));
     float v = kP[9];
 #pragma unroll
@@ -93,7 +89,7 @@ __device__ __forceinline__ float below(float g, float &bell)
 }
 // v = act(g) u for N vectors; the activation is chosen once for all, so that their
 // instructions interleave.
-template <class T, int N>
+template <int N>
 __device__ __forceinline__ void activate(const f32x4 (&g)[N], const f32x4 (&u)[N], int act, f32x4 (&v)[N])
 {
     if (act == DERF_ACT_RELU) {
@@ -104,12 +100,12 @@ __device__ __forceinline__ void activate(const f32x4 (&g)[N], const f32x4 (&u)[N
 #pragma unroll
         for (int i = 0; i < 4 * N; ++i) {
             float bell;
-            v[i / 4][i % 4] = g[i / 4][i % 4] * below<T>(g[i / 4][i % 4], bell);
+            v[i / 4][i % 4] = g[i / 4][i % 4] * below(g[i / 4][i % 4], bell);
         }
     } else {
 #pragma unroll
         for (int i = 0; i < 4 * N; ++i)
-            v[i / 4][i % 4] = logistic(g[i / 4][i % 4], T{});
+            v[i / 4][i % 4] = logistic(g[i / 4][i % 4]);
         if (act == DERF_ACT_SILU)
 #pragma unroll
             for (int i = 0; i < N; ++i)
@@ -138,7 +134,7 @@ __device__ __forceinline__ void write_gated(const f32x4 (&acc)[2 * PAIRS], const
             u[i] += *reinterpret_cast<const f32x4 *>(up_bias + e);
         }
     }
-    activate<T, PAIRS>(g, u, act, v);
+    activate<PAIRS>(g, u, act, v);
     write_16_rows<T, PAIRS * 16, STAGE>(v, mine, row0, last, n0, width, y, ys);
     if (pre) {
         write_16_rows<T, PAIRS * 16, STAGE>(g, mine, row0, last, n0, width, pre, pres);
