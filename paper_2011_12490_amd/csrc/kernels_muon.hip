@@ -472,7 +472,7 @@ __device__ __forceinline__ void read_pair(const char *plane, int plane_bytes, in
 template <int FP, int FQ, bool SPLIT, int DEPTH, class PRead, class QRead>
 __device__ __forceinline__ void small_product(f32x4 (&acc)[FP][FQ], PRead p_read, QRead q_read)
 {
-#pragma unroll
+#pragma unroll 4
     for (int part = 0; part < DEPTH / 32; ++part) {
         u32x4 p[FP], q[FQ];
 #pragma unroll
@@ -573,45 +573,49 @@ __global__ __launch_bounds__(C::kThreads, 2) void pair_kernel(Planes pm, Planes 
 
 // ---- small matrices, all of it in one launch ----------------------------------------------
 
-// Matrices of up to 128 x 128: a workgroup takes one from its gradient to its parameters,
-// X and S (or Q in its place) in LDS.  Both lie row by row in 64-row tiles: their rows are
-// read as they lie, and X's columns for Q X by transposing reads.
+// Matrices that fit: a workgroup takes one from its gradient to its parameters, X and S (or
+// Q in its place) in LDS.  Both lie in tiles of 64 rows by up to 128 columns, X's by blocks
+// of columns: their rows are read as they lie, and X's columns for Q X by transposing reads.
 template <int M_, int N_, bool SPLIT>
 struct Small {
-    static constexpr int M = M_, N = N_, kPlanes = SPLIT ? 2 : 1, kThreads = M == 128 ? 512 : 256;
-    static constexpr int WP = 2, WQ = kThreads / 128, FQ = 2;  // waves over columns and rows, 16-row results of each
+    static constexpr int M = M_, N = N_, kPlanes = SPLIT ? 2 : 1, kThreads = M == 128 || N > 128 ? 512 : 256;
+    static constexpr int WP = 2, WQ = kThreads / 128, FQ = M / 16 / WQ;  // waves over columns and rows, 16-row results of each
     static_assert(WQ * FQ * 16 == M, "all rows");
-    using X = Tile<f16, N, false, kThreads, false, false, true>;
+    static constexpr int kBlock = N < 128 ? N : 128;  // columns
+    using X = Tile<f16, kBlock, false, kThreads, false, false, true>;
     using S = Tile<f16, M, false, kThreads, false, false, true>;
+    static constexpr int kXBlock = M / 64 * X::kBytes;
     static constexpr int kX = M * N * 2, kS = M * M * 2, kLds = kPlanes * (kX + kS);  // bytes
     static constexpr int kVecs = M * N / 4 / kThreads;  // of a thread
-    // workgroups a compute unit by their LDS
-    static constexpr int kAtOnce = 160 * 1024 / (kLds + 256) < 4 ? 160 * 1024 / (kLds + 256) : 4;
+    // workgroups a compute unit: by their LDS, and by registers: 128 of a lane, of long rows 256
+    static constexpr int kByLds = 160 * 1024 / (kLds + 256), kByRegisters = N > 256 ? 1 : 1024 / kThreads;
+    static constexpr int kAtOnce = kByLds < kByRegisters ? kByLds : kByRegisters;
 };
 
 // Four values side by side in a plane of tiles: row r, columns from c on.
-template <class TILE>
+template <class C>
 __device__ __forceinline__ unsigned lds_at(int r, int c)
 {
-    return (r >> 6) * TILE::kBytes + TILE::at(r & 63, c >> 3) + (c & 4) * 2;
+    using TILE = typename C::X;
+    return c / C::kBlock * C::kXBlock + (r >> 6) * TILE::kBytes + TILE::at(r & 63, c % C::kBlock >> 3) + (c & 4) * 2;
 }
-template <class TILE, bool SPLIT>
-__device__ __forceinline__ f32x4 read_lds(const char *plane, int plane_bytes, int r, int c)
+template <class C, bool SPLIT>
+__device__ __forceinline__ f32x4 read_lds(const char *plane, int r, int c)
 {
-    const unsigned at = lds_at<TILE>(r, c);
+    const unsigned at = lds_at<C>(r, c);
     f32x4 v = __builtin_convertvector(*reinterpret_cast<const f16x4 *>(plane + at), f32x4);
     if (SPLIT)
-        v += __builtin_convertvector(*reinterpret_cast<const f16x4 *>(plane + plane_bytes + at), f32x4);
+        v += __builtin_convertvector(*reinterpret_cast<const f16x4 *>(plane + C::kX + at), f32x4);
     return v;
 }
-template <class TILE, bool SPLIT>
-__device__ __forceinline__ void write_lds(char *plane, int plane_bytes, int r, int c, f32x4 v)
+template <class C, bool SPLIT>
+__device__ __forceinline__ void write_lds(char *plane, int r, int c, f32x4 v)
 {
-    const unsigned at = lds_at<TILE>(r, c);
+    const unsigned at = lds_at<C>(r, c);
     const f16x4 hi = __builtin_convertvector(v, f16x4);
     *reinterpret_cast<f16x4 *>(plane + at) = hi;
     if (SPLIT)
-        *reinterpret_cast<f16x4 *>(plane + plane_bytes + at) = __builtin_convertvector(v - __builtin_convertvector(hi, f32x4), f16x4);
+        *reinterpret_cast<f16x4 *>(plane + C::kX + at) = __builtin_convertvector(v - __builtin_convertvector(hi, f32x4), f16x4);
 }
 
 template <class C, bool SPLIT>
@@ -676,12 +680,12 @@ __global__ __launch_bounds__(C::kThreads, C::kAtOnce *C::kThreads / 256) void sm
             for (int e = 0; e < 4; ++e)
                 v[e] = (float)((double)u[k][e] * inverse) * kUnit;
             if (!tall) {
-                write_lds<X, SPLIT>(x, C::kX, o, i, v);
+                write_lds<C, SPLIT>(x, o, i, v);
                 continue;
             }
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                f16 *to = reinterpret_cast<f16 *>(x + lds_at<X>(i + e, o)) + (o & 3);
+                f16 *to = reinterpret_cast<f16 *>(x + lds_at<C>(i + e, o)) + (o & 3);
                 const f16 hi = (f16)v[e];
                 to[0] = hi;
                 if (SPLIT)
@@ -694,8 +698,9 @@ __global__ __launch_bounds__(C::kThreads, C::kAtOnce *C::kThreads / 256) void sm
     const int row = fq * 16 + (lane & 15);  // of the wave's first results; the next 16 on
     auto x_rows = [&](int first) {
         return [=](int plane, int i, int part) {
+            constexpr int kParts = C::kBlock / 32;  // of a block
             const int f = first + i;
-            return X::row_fragment(x + plane * C::kX + (f >> 2) * X::kBytes, f & 3, part);
+            return X::row_fragment(x + plane * C::kX + part / kParts * C::kXBlock + (f >> 2) * X::kBytes, f & 3, part % kParts);
         };
     };
     auto s_rows = [&](int first) {
@@ -739,7 +744,9 @@ __global__ __launch_bounds__(C::kThreads, C::kAtOnce *C::kThreads / 256) void sm
         {
             f32x4 acc[FX][FQ] = {};
             auto x_columns = [&](int plane, int i, int part) {
-                return X::fragment(x + plane * C::kX + (part >> 1) * X::kBytes, wp * FX + i, part & 1);
+                constexpr int kOfBlock = C::kBlock / 16;
+                const int f = wp * FX + i;
+                return X::fragment(x + plane * C::kX + f / kOfBlock * C::kXBlock + (part >> 1) * X::kBytes, f % kOfBlock, part & 1);
             };
             small_product<FX, FQ, SPLIT, C::M>(acc, x_columns, s_rows(fq));
 #pragma unroll
@@ -747,7 +754,8 @@ __global__ __launch_bounds__(C::kThreads, C::kAtOnce *C::kThreads / 256) void sm
 #pragma unroll
                 for (int j = 0; j < FQ; ++j) {
                     f32x4 a, b;
-                    read_pair<X, SPLIT>(x, C::kX, row + j * 16, wp * FX + i, a, b);
+                    const int f = wp * FX + i, block = f / (C::kBlock / 16);
+                    read_pair<X, SPLIT>(x + block * C::kXBlock, C::kX, row + j * 16, f % (C::kBlock / 16), a, b);
                     acc[i][j] = acc[i][j] * (1.0f / kUnit) + a * kA;
                     acc[i + 1][j] = acc[i + 1][j] * (1.0f / kUnit) + b * kA;
                 }
@@ -755,8 +763,10 @@ __global__ __launch_bounds__(C::kThreads, C::kAtOnce *C::kThreads / 256) void sm
 #pragma unroll
             for (int i = 0; i < FX; i += 2)
 #pragma unroll
-                for (int j = 0; j < FQ; ++j)
-                    write_pair<X, SPLIT>(x, C::kX, row + j * 16, wp * FX + i, acc[i][j], acc[i + 1][j]);
+                for (int j = 0; j < FQ; ++j) {
+                    const int f = wp * FX + i, block = f / (C::kBlock / 16);
+                    write_pair<X, SPLIT>(x + block * C::kXBlock, C::kX, row + j * 16, f % (C::kBlock / 16), acc[i][j], acc[i + 1][j]);
+                }
         }
         __syncthreads();
     }
@@ -771,11 +781,11 @@ __global__ __launch_bounds__(C::kThreads, C::kAtOnce *C::kThreads / 256) void sm
         if (tall)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                const f16 *from = reinterpret_cast<const f16 *>(x + lds_at<X>(i + e, o)) + (o & 3);
+                const f16 *from = reinterpret_cast<const f16 *>(x + lds_at<C>(i + e, o)) + (o & 3);
                 v[e] = (float)from[0] + (SPLIT ? (float)from[C::kX / 2] : 0.0f);
             }
         else
-            v = read_lds<X, SPLIT>(x, C::kX, o, i);
+            v = read_lds<C, SPLIT>(x, o, i);
         v *= 1.0f / kUnit;
         const long long at = (long long)o * t.fan_in + i;
         if (st.updates)
@@ -881,6 +891,25 @@ hipError_t step(const Planes &p, const Planes &q, const Planes &out, unsigned ma
                      : launch_step<Product<f16, 128, 128, 2, 2, kDeep, true, false, true>, KIND, false>(p, q, out, matrices, s);
 }
 
+// Whether a matrix's X and S fit a compute unit's LDS.
+bool is_small(const Sizes &z, bool split)
+{
+    return z.m == 64 ? z.n <= 512 : z.m == 128 && z.n <= (split ? 128 : 256);
+}
+template <bool SPLIT>
+hipError_t small(const MuonSet &set, unsigned matrices, const Sizes &z, const MuonStep &st, hipStream_t s)
+{
+    if (z.m == 128) {
+        if constexpr (!SPLIT)
+            if (z.n > 128)
+                return launch_small<128, 256, false>(set, matrices, st, s);
+        return launch_small<128, 128, SPLIT>(set, matrices, st, s);
+    }
+    if (z.n > 128)
+        return z.n > 256 ? launch_small<64, 512, SPLIT>(set, matrices, st, s) : launch_small<64, 256, SPLIT>(set, matrices, st, s);
+    return z.n > 64 ? launch_small<64, 128, SPLIT>(set, matrices, st, s) : launch_small<64, 64, SPLIT>(set, matrices, st, s);
+}
+
 template <bool SPLIT>
 hipError_t orthogonalise(const MuonSet &set, unsigned matrices, const Sizes &z, const MuonStep &st, char *ws,
                          hipStream_t s)
@@ -921,7 +950,7 @@ hipError_t orthogonalise(const MuonSet &set, unsigned matrices, const Sizes &z, 
 size_t muon_workspace_bytes(int fan_out, int fan_in, bool split, unsigned matrices)
 {
     const Sizes z = sizes_of(fan_out, fan_in, split);
-    if (z.n <= 128)
+    if (is_small(z, split))
         return 0;  // all in LDS
     return whole(z.squares * matrices) + 2 * whole(z.x * matrices) + 2 * whole(z.s * matrices);
 }
@@ -930,13 +959,8 @@ hipError_t launch_muon(const MuonSet &set, unsigned matrices, int fan_out, int f
                        const MuonStep &st, void *workspace, hipStream_t s)
 {
     const Sizes z = sizes_of(fan_out, fan_in, split);
-    if (z.n <= 128) {
-        if (z.m == 128)
-            return split ? launch_small<128, 128, true>(set, matrices, st, s) : launch_small<128, 128, false>(set, matrices, st, s);
-        if (z.n == 128)
-            return split ? launch_small<64, 128, true>(set, matrices, st, s) : launch_small<64, 128, false>(set, matrices, st, s);
-        return split ? launch_small<64, 64, true>(set, matrices, st, s) : launch_small<64, 64, false>(set, matrices, st, s);
-    }
+    if (is_small(z, split))
+        return split ? small<true>(set, matrices, z, st, s) : small<false>(set, matrices, z, st, s);
     char *ws = static_cast<char *>(workspace);
     return split ? orthogonalise<true>(set, matrices, z, st, ws, s)
                  : orthogonalise<false>(set, matrices, z, st, ws, s);

@@ -141,14 +141,14 @@ def test_orthogonalise_arrays():
     L = lib()
 
     def call(x=P, n=5, out=P, ws=P, size=1 << 50):
-        return L.derf_orthogonalise(x, 3, 400, 50, n, 0, out, ws, size, None)
+        return L.derf_orthogonalise(x, 3, 400, 500, n, 0, out, ws, size, None)
 
     refused(call(x=None), b"null x")
     refused(call(x=P + 2), b"x is not aligned")
     refused(call(n=0), b"iterations")
     refused(call(n=21), b"iterations")
     refused(call(out=None), b"null out")
-    need = L.derf_orthogonalise_workspace(3, 400, 50, 0)
+    need = L.derf_orthogonalise_workspace(3, 400, 500, 0)
     refused(call(size=need - 1), b"workspace")
     refused(call(ws=P + 8), b"workspace")
     assert L.derf_orthogonalise(None, 0, 40, 50, 5, 0, None, None, 1 << 30, None) == derf.DERF_OK
