@@ -1,0 +1,163 @@
+"""What the gated layers, lookups and orthogonalised updates take at their edges: rows
+behind 2^32 bytes, one row of a wide buffer, two calls at once, the same rows twice,
+tensors that autograd follows, and a run of them all in one graph."""
+import pytest
+import torch
+
+from paper_2011_12490_amd import heads
+from test_gpu_heads import BF16, FP32, far_rows, gen, rand
+from test_gpu_heads_gated import gated_layer
+from test_gpu_heads_limits import one_row
+
+pytestmark = pytest.mark.gpu
+
+
+def near(a, c, most):
+    """Sums of the same products in another order: 2^-24 for each of up to 4,608 products of
+    magnitudes that add up to less than `most`; and a rounding to bf16 to either side."""
+    bound = 4608 * 2.0 ** -24 * most + (2.0 ** -7 if a.dtype == BF16 else 2.0 ** -23) * c.double().abs()
+    assert bool(((a.double() - c.double()).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("dtype,stride", [(BF16, 1 << 20), (FP32, (1 << 19) + 1)])
+@pytest.mark.parametrize("I,O", [(40, 72), (150, 136)])
+def test_rows_beyond_32_bits(dtype, stride, I, O):
+    R = 2304
+    x, w, b, offsets, g = gated_layer([1000, R - 1000], 0, I, O, 0, 0, dtype, 5)
+    y, pre = heads.gated(x, w, b, offsets, "gelu", keep=True)
+    dy = rand(g, R, O).to(dtype)
+    want = heads.gated_backward(dy, pre, x, w, offsets, "gelu")
+    far = lambda n: far_rows(R, n, stride, dtype)  # noqa: E731
+    fx = far(I).copy_(x)
+    fy, fpre = heads.gated(fx, w, b, offsets, "gelu", out=far(O), out_pre=far(2 * O))
+    near(fy, y, 100)
+    near(fpre, pre, 20)
+    del fx
+    fpre.copy_(pre)
+    fx = far(I).copy_(x)
+    got = heads.gated_backward(dy, fpre, fx, w, offsets, "gelu", out_x=far(I))
+    near(got[0], want[0], 100)
+    near(got[1], want[1], 1000)
+    near(got[2], want[2], 1000)
+
+
+@pytest.mark.parametrize("dtype", [FP32, BF16])
+def test_one_row_of_a_wide_buffer(dtype):
+    x, w, b, offsets, g = gated_layer([0, 1], 0, 40, 72, 0, 0, dtype, 1)
+    y, pre = heads.gated(x, w, b, offsets, keep=True)
+    dy = rand(g, 1, 72).to(dtype)
+    for a, c in zip(heads.gated(one_row(x), w, b, offsets, out=one_row(torch.zeros_like(y)), out_pre=one_row(torch.zeros_like(pre))), (y, pre)):
+        assert torch.equal(a, c)
+    for a, c in zip(heads.gated_backward(one_row(dy), one_row(pre), one_row(x), w, offsets, out_x=one_row(x)),
+                    heads.gated_backward(dy, pre, x, w, offsets)):
+        assert torch.equal(a, c)
+    ids = torch.tensor([0], dtype=torch.int32, device="cuda")
+    assert torch.equal(heads.lookup(one_row(x), ids, 2.0), 2 * x)
+    assert torch.equal(heads.lookup_backward(one_row(x), ids, 1, 2.0), 2 * x.float())
+
+
+def test_two_calls_at_once():
+    """On two streams, each with its own workspace."""
+    x, w, b, offsets, g = gated_layer([3000, 0, 6000], 40, 160, 96, 0, 0, BF16, 4)
+    x[-40:] = 0
+    dy, table = rand(g, x.shape[0], 96).to(BF16), rand(g, 300, 96)
+    ids = torch.randint(0, 300, (x.shape[0],), generator=g, device="cuda", dtype=torch.int32)
+    matrices = rand(g, 6, 200, 300)
+
+    def run():
+        y, pre = heads.gated(x, w, b, offsets, keep=True)
+        return (y, pre) + heads.gated_backward(dy, pre, x, w, offsets) + (
+            heads.lookup(table, ids), heads.lookup_backward(dy, ids, 300), heads.orthogonalise(matrices))
+
+    want = run()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = []
+    for s in streams:
+        s.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(s):
+            got.append([run() for _ in range(3)])
+    for s in streams:
+        s.synchronize()
+    for runs in got:
+        for outs in runs:
+            assert all(torch.equal(a, c) for a, c in zip(outs, want))
+
+
+def test_a_run_of_them_in_a_graph():
+    """Lookup, gated layers, their gradients and the table's, recorded together; the updates' direction
+    too, and the step itself beside the replays."""
+    x, w, b, offsets, g = gated_layer([500, 300, 0], 0, 48, 64, 0, 0, BF16, 6)
+    table = rand(g, 90, 48).to(BF16)
+    ids = torch.randint(-1, 90, (800,), generator=g, device="cuda", dtype=torch.int32)
+    dy = rand(g, 800, 64).to(BF16)
+    others = [(torch.randint(-1, 90, (800,), generator=g, device="cuda", dtype=torch.int32), rand(g, 800, 64).to(BF16)) for _ in range(3)]
+
+    def run():
+        rows = heads.lookup(table, ids, 1.5)
+        y, pre = heads.gated(rows, w, b, offsets, keep=True)
+        dx, dw, db = heads.gated_backward(dy, pre, rows, w, offsets)
+        return y, dw, db, heads.lookup_backward(dx, ids, 90, 1.5), heads.orthogonalise(dw.view(6, 64, 48))
+
+    run()
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        captured = run()
+    for new_ids, new_dy in others:
+        ids.copy_(new_ids)
+        dy.copy_(new_dy)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, c) for a, c in zip(captured, run()))
+
+
+def test_a_padded_batch():
+    """Samples without a row and rows without a head, of any content, change nothing for the others."""
+    x, w, b, offsets, g = gated_layer([70, 50], 8, 24, 40, 0, 0, FP32, 7)
+    y, pre = heads.gated(x, w, b, offsets, keep=True)
+    clean = x.clone()
+    clean[-8:] = 0
+    assert torch.equal(heads.gated(clean, w, b, offsets)[0], y) and not bool(y[-8:].any())
+    dy = rand(g, 128, 40)
+    want = heads.gated_backward(dy, pre, clean, w, offsets)
+    dy[-8:], pre[-8:] = float("inf"), float("nan")
+    for a, c in zip(heads.gated_backward(dy, pre, x, w, offsets), want):
+        assert torch.equal(a, c)
+    ids = torch.cat([torch.arange(120, device="cuda") % 7, torch.full((8,), -1, device="cuda")]).int()
+    assert torch.equal(heads.lookup_backward(dy, ids, 7), heads.lookup_backward(dy[:120], ids[:120], 7))
+
+
+def test_tensors_that_autograd_follows():
+    x, w, b, offsets, g = gated_layer([5, 6], 0, 8, 12, 0, 0, FP32, 1)
+    y, pre = heads.gated(x, w, b, offsets, keep=True)
+    table, ids = rand(g, 4, 8), torch.zeros(11, dtype=torch.int32, device="cuda")
+    leaf = lambda t: t.clone().requires_grad_()  # noqa: E731
+    calls = [lambda f: heads.gated(f(x), w, b, offsets), lambda f: heads.gated(x, f(w), b, offsets), lambda f: heads.gated(x, w, f(b), offsets),
+             lambda f: heads.gated_backward(f(y), pre, x, w, offsets), lambda f: heads.gated_backward(y, f(pre), x, w, offsets),
+             lambda f: heads.lookup(f(table), ids), lambda f: heads.lookup_backward(f(x), ids, 4), lambda f: heads.orthogonalise(f(table))]
+    for call in calls:
+        with pytest.raises(ValueError, match="requires a gradient"):
+            call(leaf)
+        with torch.no_grad():
+            call(leaf)
+    # the optimizer's parameters may be leaves, as AdamW's
+    p = leaf(table)
+    heads.Muon([p], [rand(g, 4, 8)], lr=0.1).step()
+    assert p.requires_grad and not torch.equal(p.detach(), table)
+
+
+def test_a_backward_pass_in_a_graph_beside_live_autograd():
+    """Recorded while autograd holds a graph of the same weights: nothing here is autograd's."""
+    x, w, b, offsets, g = gated_layer([50, 30], 0, 16, 24, 0, 0, FP32, 3)
+    leaf = w.clone().requires_grad_()
+    loss = (leaf * leaf).sum()
+    y, pre = heads.gated(x, leaf.detach(), b, offsets, keep=True)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        grads = heads.gated_backward(y, pre, x, leaf.detach(), offsets)
+    graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, c) for a, c in zip(grads, heads.gated_backward(y, pre, x, leaf.detach(), offsets)))
+    loss.backward()
+    assert torch.equal(leaf.grad, 2 * w)
