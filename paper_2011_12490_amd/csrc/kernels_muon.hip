@@ -578,9 +578,10 @@ __global__ __launch_bounds__(C::kThreads, 2) void pair_kernel(Planes pm, Planes 
 // of columns: their rows are read as they lie, and X's columns for Q X by transposing reads.
 template <int M_, int N_, bool SPLIT>
 struct Small {
-    static constexpr int M = M_, N = N_, kPlanes = SPLIT ? 2 : 1, kThreads = M == 128 || N > 128 ? 512 : 256;
-    static constexpr int WP = 2, WQ = kThreads / 128, FQ = M / 16 / WQ;  // waves over columns and rows, 16-row results of each
-    static_assert(WQ * FQ * 16 == M, "all rows");
+    static constexpr int M = M_, N = N_, kPlanes = SPLIT ? 2 : 1, kThreads = M == 128 ? 1024 : N > 128 ? 512 : 256;
+    static constexpr int WP = M == 128 ? 4 : 2, WQ = kThreads / 64 / WP;  // waves over columns and rows
+    static constexpr int FQ = M / 16 / WQ, FS = M / 16 / WP, FX = N / 16 / WP;  // 16-row results of each: rows, columns of S and X
+    static_assert(WQ * FQ * 16 == M && FS % 2 == 0, "all rows, and columns in pairs");
     static constexpr int kBlock = N < 128 ? N : 128;  // columns
     using X = Tile<f16, kBlock, false, kThreads, false, false, true>;
     using S = Tile<f16, M, false, kThreads, false, false, true>;
@@ -623,7 +624,7 @@ __global__ __launch_bounds__(C::kThreads, C::kAtOnce *C::kThreads / 256) void sm
 {
     using X = typename C::X;
     using S = typename C::S;
-    constexpr int FQ = C::FQ, FS = C::M / 32, FX = C::N / 32;  // results of a wave: rows, columns of S, columns of X
+    constexpr int FQ = C::FQ, FS = C::FS, FX = C::FX;
     __shared__ __attribute__((aligned(16))) char lds[C::kLds];
     __shared__ double sums[C::kThreads / 64];
     char *const x = lds, *const sq = lds + C::kPlanes * C::kX;
