@@ -578,7 +578,7 @@ __global__ __launch_bounds__(C::kThreads, 2) void pair_kernel(Planes pm, Planes 
 // of columns: their rows are read as they lie, and X's columns for Q X by transposing reads.
 template <int M_, int N_, bool SPLIT>
 struct Small {
-    static constexpr int M = M_, N = N_, kPlanes = SPLIT ? 2 : 1, kThreads = M == 128 ? 1024 : N > 128 ? 512 : 256;
+    static constexpr int M = M_, N = N_, kPlanes = SPLIT ? 2 : 1, kThreads = M == 128 ? 1024 : 512;
     static constexpr int WP = M == 128 ? 4 : 2, WQ = kThreads / 64 / WP;  // waves over columns and rows
     static constexpr int FQ = M / 16 / WQ, FS = M / 16 / WP, FX = N / 16 / WP;  // 16-row results of each: rows, columns of S and X
     static_assert(WQ * FQ * 16 == M && FS % 2 == 0, "all rows, and columns in pairs");
