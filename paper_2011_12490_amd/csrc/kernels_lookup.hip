@@ -7,6 +7,8 @@
 // without atomics, whatever the ids.  All of it moves bytes.
 #include "ops_internal.h"
 
+#include <type_traits>
+
 namespace derf {
 
 namespace {
@@ -93,10 +95,10 @@ __global__ __launch_bounds__(256) void lookup_kernel(const T *table, long long s
 // without a row has the key `rows`, behind all others.  Up to kOneBlock samples one
 // workgroup takes all passes, its samples in registers and LDS.
 
-constexpr int kLaneKeys = 8;
+constexpr int kOneKeys = 8;
 constexpr int kSortThreads = 256, kOneThreads = 1024;
-constexpr unsigned kSortBlock = kSortThreads * kLaneKeys, kOneBlock = kOneThreads * kLaneKeys;
-constexpr int kMostBits = 10, kOneBits = 8;  // of a digit
+constexpr unsigned kOneBlock = kOneThreads * kOneKeys;
+constexpr int kMostBits = 10;  // of a digit
 
 __device__ __forceinline__ unsigned key_of(int id, unsigned rows) { return (unsigned)id < rows ? (unsigned)id : rows; }
 
@@ -122,7 +124,8 @@ __device__ __forceinline__ unsigned scan(unsigned x, unsigned *tmp)
     return before + incl - x;
 }
 
-// keys: null in the first pass, which takes them from ids.
+// KEYS: of a lane.  keys: null in the first pass, which takes them from ids.
+template <int KEYS>
 __global__ __launch_bounds__(kSortThreads) void digit_count_kernel(const int *ids, const unsigned *keys, unsigned samples,
                                                                    unsigned rows, int shift, int bits, unsigned *counts)
 {
@@ -132,8 +135,8 @@ __global__ __launch_bounds__(kSortThreads) void digit_count_kernel(const int *id
         hist[d] = 0;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kLaneKeys; ++i) {
-        const unsigned p = blockIdx.x * kSortBlock + i * kSortThreads + threadIdx.x;
+    for (int i = 0; i < KEYS; ++i) {
+        const unsigned p = blockIdx.x * (kSortThreads * KEYS) + i * kSortThreads + threadIdx.x;
         if (p < samples)
             atomicAdd(&hist[(keys ? keys[p] : key_of(ids[p], rows)) >> shift & (digits - 1)], 1u);
     }
@@ -176,6 +179,7 @@ __device__ __forceinline__ unsigned long long same_digit(unsigned digit, int bit
     return same;
 }
 
+template <int KEYS>
 __global__ __launch_bounds__(kSortThreads) void digit_place_kernel(const int *ids, const unsigned *keys, const unsigned *values,
                                                                    unsigned samples, unsigned rows, int shift, int bits,
                                                                    const unsigned *counts, const unsigned *totals,
@@ -186,11 +190,11 @@ __global__ __launch_bounds__(kSortThreads) void digit_place_kernel(const int *id
     __shared__ unsigned tmp[kWaves];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     const unsigned digits = 1u << bits;
-    const unsigned first = blockIdx.x * kSortBlock + wave * (64 * kLaneKeys) + lane;
+    const unsigned first = blockIdx.x * (kSortThreads * KEYS) + wave * (64 * KEYS) + lane;
     // all loads before anything waits: a thread has kShare digits side by side
-    unsigned key[kLaneKeys], value[kLaneKeys], total[kShare], before[kShare], sum = 0;
+    unsigned key[KEYS], value[KEYS], total[kShare], before[kShare], sum = 0;
 #pragma unroll
-    for (int i = 0; i < kLaneKeys; ++i) {
+    for (int i = 0; i < KEYS; ++i) {
         const unsigned p = first + i * 64;
         key[i] = p < samples ? (keys ? keys[p] : (unsigned)ids[p]) : 0u;
         value[i] = p < samples && values ? values[p] : p;
@@ -206,7 +210,7 @@ __global__ __launch_bounds__(kSortThreads) void digit_place_kernel(const int *id
             hist[w][d] = 0;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kLaneKeys; ++i) {
+    for (int i = 0; i < KEYS; ++i) {
         if (!keys)
             key[i] = key_of((int)key[i], rows);
         if (first + i * 64 < samples)
@@ -233,7 +237,7 @@ __global__ __launch_bounds__(kSortThreads) void digit_place_kernel(const int *id
     __syncthreads();
     volatile unsigned *mine = hist[wave];
 #pragma unroll
-    for (int i = 0; i < kLaneKeys; ++i) {
+    for (int i = 0; i < KEYS; ++i) {
         const unsigned p = first + i * 64, digit = key[i] >> shift & (digits - 1);
         const unsigned long long same = same_digit(digit, bits, p < samples);
         if (p < samples) {
@@ -246,38 +250,41 @@ __global__ __launch_bounds__(kSortThreads) void digit_place_kernel(const int *id
     }
 }
 
+static_assert(kOneThreads == 1 << kMostBits, "a thread a digit");
 // All passes of up to kOneBlock samples.
-__global__ __launch_bounds__(kOneThreads) void sort_one_kernel(const int *ids, unsigned samples, unsigned rows, int key_bits,
+__global__ __launch_bounds__(kOneThreads) void sort_one_kernel(const int *ids, unsigned samples, unsigned rows, int key_bits, int bits,
                                                                unsigned *out_keys, unsigned *out_values)
 {
-    constexpr int kWaves = kOneThreads / 64, kDigits = 1 << kOneBits;
-    __shared__ unsigned hist[kWaves][kDigits];
+    constexpr int kWaves = kOneThreads / 64;
+    __shared__ unsigned hist[kWaves][1 << kMostBits];
     __shared__ unsigned tmp[kWaves];
     __shared__ unsigned sorted[2][kOneBlock];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-    const unsigned first = wave * (64 * kLaneKeys) + lane;
-    unsigned key[kLaneKeys], value[kLaneKeys];
+    const unsigned digits = 1u << bits;
+    const unsigned first = wave * (64 * kOneKeys) + lane;
+    unsigned key[kOneKeys], value[kOneKeys];
 #pragma unroll
-    for (int i = 0; i < kLaneKeys; ++i) {
+    for (int i = 0; i < kOneKeys; ++i) {
         const unsigned p = first + i * 64;
         key[i] = p < samples ? key_of(ids[p], rows) : 0u;
         value[i] = p;
     }
-    for (int shift = 0; shift < key_bits; shift += kOneBits) {
-        for (unsigned i = threadIdx.x; i < kWaves * kDigits; i += kOneThreads)
-            hist[0][i] = 0;
+    for (int shift = 0; shift < key_bits; shift += bits) {
+        for (int w = 0; w < kWaves; ++w)
+            if (threadIdx.x < digits)
+                hist[w][threadIdx.x] = 0;
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kLaneKeys; ++i)
+        for (int i = 0; i < kOneKeys; ++i)
             if (first + i * 64 < samples)
-                atomicAdd(&hist[wave][key[i] >> shift & (kDigits - 1)], 1u);
+                atomicAdd(&hist[wave][key[i] >> shift & (digits - 1)], 1u);
         __syncthreads();
         unsigned count = 0;
-        if (threadIdx.x < kDigits)
+        if (threadIdx.x < digits)
             for (int w = 0; w < kWaves; ++w)
                 count += hist[w][threadIdx.x];
         unsigned at = scan<kOneThreads>(count, tmp);
-        if (threadIdx.x < kDigits)
+        if (threadIdx.x < digits)
             for (int w = 0; w < kWaves; ++w) {
                 const unsigned c = hist[w][threadIdx.x];
                 hist[w][threadIdx.x] = at;
@@ -286,10 +293,10 @@ __global__ __launch_bounds__(kOneThreads) void sort_one_kernel(const int *ids, u
         __syncthreads();
         volatile unsigned *mine = hist[wave];
 #pragma unroll
-        for (int i = 0; i < kLaneKeys; ++i) {
+        for (int i = 0; i < kOneKeys; ++i) {
             const bool in = first + i * 64 < samples;
-            const unsigned digit = key[i] >> shift & (kDigits - 1);
-            const unsigned long long same = same_digit(digit, kOneBits, in);
+            const unsigned digit = key[i] >> shift & (digits - 1);
+            const unsigned long long same = same_digit(digit, bits, in);
             if (in) {
                 const unsigned rank = __popcll(same & ((1ull << lane) - 1)), to = mine[digit] + rank;
                 if (rank == 0)
@@ -300,14 +307,14 @@ __global__ __launch_bounds__(kOneThreads) void sort_one_kernel(const int *ids, u
         }
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < kLaneKeys; ++i)
+        for (int i = 0; i < kOneKeys; ++i)
             if (first + i * 64 < samples) {
                 key[i] = sorted[0][first + i * 64];
                 value[i] = sorted[1][first + i * 64];
             }
     }
 #pragma unroll
-    for (int i = 0; i < kLaneKeys; ++i)
+    for (int i = 0; i < kOneKeys; ++i)
         if (first + i * 64 < samples) {
             out_keys[first + i * 64] = key[i];
             out_values[first + i * 64] = value[i];
@@ -349,6 +356,20 @@ __device__ __forceinline__ void absent_rows(unsigned block, const unsigned *keys
     }
     const bool absent = v < rows && !(lo < samples && keys[lo] == v);
     unsigned long long todo = __ballot(absent);
+    if (D <= 64) {  // short rows: all 64 of them side by side
+        float *first = out + (size_t)v0 * D;
+        if (D % 4 == 0) {
+            const int vecs = D / 4;
+            for (int i = lane; i < 64 * vecs; i += 64)
+                if (todo >> (i / vecs) & 1)
+                    *reinterpret_cast<Any16 *>(first + i * 4) = u32x4{0, 0, 0, 0};
+        } else {
+            for (int i = lane; i < 64 * D; i += 64)
+                if (todo >> (i / D) & 1)
+                    first[i] = 0.0f;
+        }
+        return;
+    }
     while (todo) {
         const int l = __builtin_ctzll(todo);
         todo &= todo - 1;
@@ -650,6 +671,11 @@ Digits digits_of(unsigned rows)
 
 size_t whole(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
+// Samples of a block of the sort: 1,024, or 2,048 where there are blocks for all of the chip.
+// The gradient's us with 1,024 and 2,048: 15,000 samples of 23 rows 29, 31; 70,000 of 8,612
+// 41, 46; 262,144 of 1,000 40, 41; 524,288 of 200,000 340, 333; 1,000,000 of 500,000 159, 154.
+unsigned sort_block(unsigned samples) { return samples < 256u * 8 * kSortThreads ? 4 * kSortThreads : 8 * kSortThreads; }
+
 // The workspace: two lists of keys and values, the sort's counts, and the pieces' parts.
 struct Places {
     size_t list, counts, ends, leads, trails, end;
@@ -670,7 +696,7 @@ Places places_of(unsigned samples, unsigned rows, int dim)
     }
     at += 4 * whole((size_t)samples * 4);
     const Digits d = digits_of(rows);
-    p.counts = take(samples > kOneBlock ? (((size_t)blocks_of(samples, kSortBlock) + 1) << d.bits) * 4 : 0);
+    p.counts = take(samples > kOneBlock ? (((size_t)blocks_of(samples, sort_block(samples)) + 1) << d.bits) * 4 : 0);
     const size_t pieces = blocks_of(samples, kPiece);
     p.ends = take(pieces * sizeof(Ends));
     p.leads = take(pieces * dim * sizeof(float));
@@ -730,21 +756,28 @@ hipError_t backward(Rows dout, const int *ids, unsigned samples, unsigned rows, 
     hipError_t e = hipSuccess;
     int now = 0;
     if (samples > kOneBlock) {
-        const unsigned blocks = blocks_of(samples, kSortBlock);
+        const unsigned blocks = blocks_of(samples, sort_block(samples));
         unsigned *counts = reinterpret_cast<unsigned *>(ws + at.counts), *totals = counts + ((size_t)blocks << d.bits);
         for (int pass = 0; pass < d.passes; ++pass) {
             const unsigned *k = pass ? keys[now ^ 1] : nullptr, *v = pass ? values[now ^ 1] : nullptr;
             const int shift = pass * d.bits;
-            digit_count_kernel<<<blocks, kSortThreads, 0, s>>>(ids, k, samples, rows, shift, d.bits, counts);
-            digit_scan_kernel<<<1u << d.bits, kSortThreads, 0, s>>>(counts, blocks, totals);
-            digit_place_kernel<<<blocks, kSortThreads, 0, s>>>(ids, k, v, samples, rows, shift, d.bits, counts, totals, keys[now],
-                                                               values[now]);
+            auto launch = [&](auto keys_each) {
+                constexpr int KEYS = decltype(keys_each)::value;
+                digit_count_kernel<KEYS><<<blocks, kSortThreads, 0, s>>>(ids, k, samples, rows, shift, d.bits, counts);
+                digit_scan_kernel<<<1u << d.bits, kSortThreads, 0, s>>>(counts, blocks, totals);
+                digit_place_kernel<KEYS><<<blocks, kSortThreads, 0, s>>>(ids, k, v, samples, rows, shift, d.bits, counts, totals,
+                                                                         keys[now], values[now]);
+            };
+            if (sort_block(samples) == 4 * kSortThreads)
+                launch(std::integral_constant<int, 4>{});
+            else
+                launch(std::integral_constant<int, 8>{});
             now ^= 1;
         }
         now ^= 1;  // the last one written
         e = hipGetLastError();
     } else {
-        sort_one_kernel<<<1, kOneThreads, 0, s>>>(ids, samples, rows, d.key_bits, keys[0], values[0]);
+        sort_one_kernel<<<1, kOneThreads, 0, s>>>(ids, samples, rows, d.key_bits, d.bits, keys[0], values[0]);
         e = hipGetLastError();
     }
     if (e != hipSuccess)
