@@ -14,9 +14,13 @@
 // lose no more than they do in float32 (on matrices of 512 to 1,024 of normal values
 // 2.1e-6 of the result's norm off, 1.9e-6 in float32).  a X is added in float32: with a in
 // Q's diagonal the matrix units' sums, whose roundings are those of their largest terms,
-// lose twice as much.  bf16 updates, whose own rounding
-// is 2^-9, take the first halves alone: 11 bits, 0.2 to 3e-3 off where bf16 products would
-// be 0.2 to 3e-2 off.
+// lose twice as much.  bf16 updates, whose own rounding is 2^-9 (1.65e-3 of a matrix's norm),
+// multiply the first halves alone: 11 bits.  X itself keeps both, since a X takes what a step
+// loses of the small singular values' part to 3.4 times as much in the next: the results,
+// rounding included, are 2.0 to 2.6e-3 off (8 x 8 to 1,000 x 1,000), with X in 11 bits too up to
+// 8e-3, with bf16 products about ten times that.  In memory X keeps both for all but the last
+// two steps, after which nothing grows much: as exact, and of 2,048 x 4,096 matrices' last
+// products 564 us where both take 680.
 #include "product.h"
 
 namespace derf {
@@ -165,14 +169,14 @@ __device__ __forceinline__ double inverse_norm(const double *squares, unsigned c
 
 constexpr int kTurnRow = 68;  // floats
 
-// The planes of a matrix: rows x cols fp16 each, the rests behind the rounded values.
+// The planes of a matrix: rows x cols fp16 each, the rests (X's always, S's and Q's where
+// split) behind the rounded values.
 struct Planes {
     f16 *p;
     long long matrix;  // values from a matrix to the next
     unsigned rows, cols;
 };
 
-template <bool SPLIT>
 __global__ __launch_bounds__(256) void start_kernel(const MuonSet set, MuonStep st, const double *squares,
                                                     unsigned chunks, Planes x)
 {
@@ -220,14 +224,12 @@ __global__ __launch_bounds__(256) void start_kernel(const MuonSet set, MuonStep 
         }
         const size_t at = (size_t)(r0 + r) * x.cols + c0 + c;
         *reinterpret_cast<f16x4 *>(out + at) = hi;
-        if (SPLIT)
-            *reinterpret_cast<f16x4 *>(out + (size_t)x.rows * x.cols + at) = lo;
+        *reinterpret_cast<f16x4 *>(out + (size_t)x.rows * x.cols + at) = lo;
     }
 }
 
 // The parameters' step along X, or X itself as the result (no parameters).
-template <bool SPLIT>
-__global__ __launch_bounds__(256) void finish_kernel(const MuonSet set, MuonStep st, Planes x)
+__global__ __launch_bounds__(256) void finish_kernel(const MuonSet set, MuonStep st, Planes x, bool rest)
 {
     __shared__ __attribute__((aligned(16))) float tile[64][kTurnRow];
     const MuonEntry t = entry_of(set, blockIdx.z);
@@ -241,7 +243,7 @@ __global__ __launch_bounds__(256) void finish_kernel(const MuonSet set, MuonStep
         const int r = k * 16 + threadIdx.x / 16;
         const size_t at = (size_t)(r0 + r) * x.cols + c0 + c;
         f32x4 v = __builtin_convertvector(*reinterpret_cast<const f16x4 *>(in + at), f32x4);
-        if (SPLIT)
+        if (rest)
             v += __builtin_convertvector(*reinterpret_cast<const f16x4 *>(in + (size_t)x.rows * x.cols + at), f32x4);
         v *= 1.0f / kUnit;
         if (tall)
@@ -275,8 +277,8 @@ enum Kind { kGram, kSquare, kApply };
 
 // A wave's results, from row r and column c on, to both planes of `to` [rows][cols], with
 // what they are added to (was: S or X).  mirror: those of a symmetric matrix to the place
-// above the diagonal too.
-template <int KIND, bool SPLIT, int FP, int FQ>
+// above the diagonal too.  RESTS: 1 what they are added to has both planes, 2 `to` gets both.
+template <int KIND, int RESTS, int FP, int FQ>
 __device__ __forceinline__ void write_step(const f32x4 (&acc)[FP][FQ], const f16 *was, f16 *to, unsigned rows, unsigned cols, unsigned r,
                                            unsigned c, char *mine, bool mirror)
 {
@@ -293,7 +295,7 @@ __device__ __forceinline__ void write_step(const f32x4 (&acc)[FP][FQ], const f16
             if (KIND != kGram && row < rows && col < cols) {
                 const size_t at = (size_t)row * cols + col;
                 f32x4 old = __builtin_convertvector(*reinterpret_cast<const f16x4 *>(was + at), f32x4);
-                if (SPLIT)
+                if (RESTS & 1)
                     old += __builtin_convertvector(*reinterpret_cast<const f16x4 *>(was + rest + at), f32x4);
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
@@ -302,7 +304,7 @@ __device__ __forceinline__ void write_step(const f32x4 (&acc)[FP][FQ], const f16
             lo[i] = v[i] - __builtin_convertvector(__builtin_convertvector(v[i], f16x4), f32x4);
         }
         write_16_rows<f16, FP * 16>(v, mine, r + j * 16, rows, c, cols, to, cols);
-        if (SPLIT)
+        if (RESTS & 2)
             write_16_rows<f16, FP * 16>(lo, mine, r + j * 16, rows, c, cols, to + rest, cols);
         if (KIND != kApply && mirror)
 #pragma unroll
@@ -312,7 +314,7 @@ __device__ __forceinline__ void write_step(const f32x4 (&acc)[FP][FQ], const f16
                     const unsigned col = c + i * 16 + (lane >> 4) * 4 + k;
                     if (row < rows && col < cols) {
                         to[(size_t)col * cols + row] = (f16)v[i][k];
-                        if (SPLIT)
+                        if (RESTS & 2)
                             to[rest + (size_t)col * cols + row] = (f16)lo[i][k];
                     }
                 }
@@ -342,9 +344,9 @@ __device__ __forceinline__ void step_tile(unsigned in, unsigned row_tiles, unsig
 // c S S (Square: P, Q = S; both results symmetric: tiles on and below the diagonal are
 // computed and written to both places), X = a X + Q X (Apply: P = X, depth down its
 // columns).
-// SPLIT: the product of the rounded values, and those of each with the other's rest, one
-// after the other into the same registers.
-template <class C, int KIND, bool SPLIT>
+// SPLIT: the products of each operand's rests with the other's rounded values, then of
+// those, one after the other into the same registers.
+template <class C, int KIND, bool SPLIT, int RESTS>
 __global__ __launch_bounds__(C::kThreads, 2) void step_kernel(Planes pm, Planes qm, Planes out, unsigned matrices)
 {
     constexpr bool kSymmetric = KIND != kApply;
@@ -370,9 +372,9 @@ __global__ __launch_bounds__(C::kThreads, 2) void step_kernel(Planes pm, Planes 
             if (!tile_at(ahead, matrix, r0, c0))
                 continue;
             const f16 *p = pm.p + matrix * pm.matrix, *q = qm.p + matrix * qm.matrix;
-            if (pass == 1)
+            if (SPLIT && pass == 0)  // the small ones first
                 p += (size_t)pm.rows * pm.cols;
-            if (pass == 2)
+            if (SPLIT && pass == 1)
                 q += (size_t)qm.rows * qm.cols;
             const typename C::P::Source ps = {{p, pm.cols, nullptr, 0, pm.rows, (int)pm.cols}, c0};
             const typename C::Q::Source qs = {{q, qm.cols, nullptr, 0, qm.rows, (int)qm.cols}, r0};
@@ -400,7 +402,7 @@ __global__ __launch_bounds__(C::kThreads, 2) void step_kernel(Planes pm, Planes 
 #pragma unroll 1
             for (unsigned k = 0; k < depth; k += C::kDepth)
                 pipe.step(acc, next_tile, [](auto &) {});
-        write_step<KIND, SPLIT, C::FP, C::FQ>(acc, pm.p + matrix * pm.matrix, out.p + matrix * out.matrix, out.rows, out.cols, r0 + wq,
+        write_step<KIND, RESTS, C::FP, C::FQ>(acc, pm.p + matrix * pm.matrix, out.p + matrix * out.matrix, out.rows, out.cols, r0 + wq,
                                               c0 + wp, mine, r0 != c0);
     }
     arrived<0>();
@@ -467,10 +469,12 @@ __device__ __forceinline__ void read_pair(const char *plane, int plane_bytes, in
     }
 }
 
-// acc[i][j] = sum over DEPTH of P's and Q's 16-row results: P_READ, Q_READ (plane,
-// result, 32 deep part) give the matrix unit's operands.
+// acc[i][j] += sum over DEPTH of P's and Q's 16-row results: p_read, q_read (plane, result, 32
+// deep part) give the matrix unit's operands.  SPLIT: products with a rest go to `rest`: beside
+// the others their last bits would be lost to each of the sum's roundings (300 x 701: 2.1e-6
+// of the norm off, 1.5e-6 with sums of their own).
 template <int FP, int FQ, bool SPLIT, int DEPTH, class PRead, class QRead>
-__device__ __forceinline__ void small_product(f32x4 (&acc)[FP][FQ], PRead p_read, QRead q_read)
+__device__ __forceinline__ void small_product(f32x4 (&acc)[FP][FQ], f32x4 (&rest)[FP][FQ], PRead p_read, QRead q_read)
 {
 #pragma unroll 4
     for (int part = 0; part < DEPTH / 32; ++part) {
@@ -487,15 +491,15 @@ __device__ __forceinline__ void small_product(f32x4 (&acc)[FP][FQ], PRead p_read
             for (int j = 0; j < FQ; ++j)
                 acc[i][j] = multiply(p[i], q[j], acc[i][j], f16{});
         if (SPLIT) {
-            u32x4 rest[FQ];
+            u32x4 low[FQ];
 #pragma unroll
             for (int j = 0; j < FQ; ++j)
-                rest[j] = q_read(1, j, part);
+                low[j] = q_read(1, j, part);
 #pragma unroll
             for (int i = 0; i < FP; ++i)
 #pragma unroll
                 for (int j = 0; j < FQ; ++j)
-                    acc[i][j] = multiply(p[i], rest[j], acc[i][j], f16{});
+                    rest[i][j] = multiply(p[i], low[j], rest[i][j], f16{});
 #pragma unroll
             for (int i = 0; i < FP; ++i)
                 p[i] = p_read(1, i, part);
@@ -503,9 +507,19 @@ __device__ __forceinline__ void small_product(f32x4 (&acc)[FP][FQ], PRead p_read
             for (int i = 0; i < FP; ++i)
 #pragma unroll
                 for (int j = 0; j < FQ; ++j)
-                    acc[i][j] = multiply(p[i], q[j], acc[i][j], f16{});
+                    rest[i][j] = multiply(p[i], q[j], rest[i][j], f16{});
         }
     }
+}
+template <int FP, int FQ, bool SPLIT>
+__device__ __forceinline__ void add_rest(f32x4 (&acc)[FP][FQ], const f32x4 (&rest)[FP][FQ])
+{
+    if (SPLIT)
+#pragma unroll
+        for (int i = 0; i < FP; ++i)
+#pragma unroll
+            for (int j = 0; j < FQ; ++j)
+                acc[i][j] += rest[i][j];
 }
 
 // The same for split matrices of few tiles, one a workgroup: a step brings both planes of
@@ -553,21 +567,22 @@ __global__ __launch_bounds__(C::kThreads, 2) void pair_kernel(Planes pm, Planes 
     bring(kStage);
     const int wave = uniform(threadIdx.x >> 6);
     const int fp = (wave % C::WP) * C::FP, fq = (wave / C::WP) * C::FQ;
-    f32x4 acc[C::FP][C::FQ] = {};
+    f32x4 acc[C::FP][C::FQ] = {}, rest[C::FP][C::FQ] = {};
     unsigned stage = 0;
 #pragma unroll 1
     for (unsigned k = 0; k < qm.cols; k += C::kDepth) {
         arrived<kLoads>();
         const char *from = lds + stage;
         small_product<C::FP, C::FQ, true, C::kDepth>(
-            acc, [&](int plane, int i, int part) { return C::P::fragment(from + plane * C::kStage, fp + i, part); },
+            acc, rest, [&](int plane, int i, int part) { return C::P::fragment(from + plane * C::kStage, fp + i, part); },
             [&](int plane, int j, int part) { return C::Q::fragment(from + plane * C::kStage + C::P::kBytes, fq + j, part); });
         stored();  // all waves have read the stage
         bring(stage);
         stage ^= kStage;
     }
     arrived<0>();
-    write_step<KIND, true, C::FP, C::FQ>(acc, p, out.p + matrix * out.matrix, out.rows, out.cols, r0 + fq * 16, c0 + fp * 16,
+    add_rest<C::FP, C::FQ, true>(acc, rest);
+    write_step<KIND, 3, C::FP, C::FQ>(acc, p, out.p + matrix * out.matrix, out.rows, out.cols, r0 + fq * 16, c0 + fp * 16,
                                          lds + wave * 16 * kPieceRow<f16, COLS>, r0 != c0);
 }
 
@@ -578,7 +593,7 @@ __global__ __launch_bounds__(C::kThreads, 2) void pair_kernel(Planes pm, Planes 
 // of columns: their rows are read as they lie, and X's columns for Q X by transposing reads.
 template <int M_, int N_, bool SPLIT>
 struct Small {
-    static constexpr int M = M_, N = N_, kPlanes = SPLIT ? 2 : 1, kThreads = M == 128 ? 1024 : 512;
+    static constexpr int M = M_, N = N_, kPlanes = SPLIT ? 2 : 1 /* of S */, kThreads = M == 128 ? 1024 : 512;
     static constexpr int WP = M == 128 ? 4 : 2, WQ = kThreads / 64 / WP;  // waves over columns and rows
     static constexpr int FQ = M / 16 / WQ, FS = M / 16 / WP, FX = N / 16 / WP;  // 16-row results of each: rows, columns of S and X
     static_assert(WQ * FQ * 16 == M && FS % 2 == 0, "all rows, and columns in pairs");
@@ -586,7 +601,7 @@ struct Small {
     using X = Tile<f16, kBlock, false, kThreads, false, false, true>;
     using S = Tile<f16, M, false, kThreads, false, false, true>;
     static constexpr int kXBlock = M / 64 * X::kBytes;
-    static constexpr int kX = M * N * 2, kS = M * M * 2, kLds = kPlanes * (kX + kS);  // bytes
+    static constexpr int kX = M * N * 2, kS = M * M * 2, kLds = 2 * kX + kPlanes * kS;  // bytes
     static constexpr int kVecs = M * N / 4 / kThreads;  // of a thread
     // workgroups a compute unit: by their LDS, and by registers: 128 of a lane, of long rows 256
     static constexpr int kByLds = 160 * 1024 / (kLds + 256), kByRegisters = N > 256 ? 1 : 1024 / kThreads;
@@ -600,23 +615,21 @@ __device__ __forceinline__ unsigned lds_at(int r, int c)
     using TILE = typename C::X;
     return c / C::kBlock * C::kXBlock + (r >> 6) * TILE::kBytes + TILE::at(r & 63, c % C::kBlock >> 3) + (c & 4) * 2;
 }
-template <class C, bool SPLIT>
+template <class C>
 __device__ __forceinline__ f32x4 read_lds(const char *plane, int r, int c)
 {
     const unsigned at = lds_at<C>(r, c);
     f32x4 v = __builtin_convertvector(*reinterpret_cast<const f16x4 *>(plane + at), f32x4);
-    if (SPLIT)
-        v += __builtin_convertvector(*reinterpret_cast<const f16x4 *>(plane + C::kX + at), f32x4);
+    v += __builtin_convertvector(*reinterpret_cast<const f16x4 *>(plane + C::kX + at), f32x4);
     return v;
 }
-template <class C, bool SPLIT>
+template <class C>
 __device__ __forceinline__ void write_lds(char *plane, int r, int c, f32x4 v)
 {
     const unsigned at = lds_at<C>(r, c);
     const f16x4 hi = __builtin_convertvector(v, f16x4);
     *reinterpret_cast<f16x4 *>(plane + at) = hi;
-    if (SPLIT)
-        *reinterpret_cast<f16x4 *>(plane + C::kX + at) = __builtin_convertvector(v - __builtin_convertvector(hi, f32x4), f16x4);
+    *reinterpret_cast<f16x4 *>(plane + C::kX + at) = __builtin_convertvector(v - __builtin_convertvector(hi, f32x4), f16x4);
 }
 
 template <class C, bool SPLIT>
@@ -627,7 +640,7 @@ __global__ __launch_bounds__(C::kThreads, C::kAtOnce *C::kThreads / 256) void sm
     constexpr int FQ = C::FQ, FS = C::FS, FX = C::FX;
     __shared__ __attribute__((aligned(16))) char lds[C::kLds];
     __shared__ double sums[C::kThreads / 64];
-    char *const x = lds, *const sq = lds + C::kPlanes * C::kX;
+    char *const x = lds, *const sq = lds + 2 * C::kX;
     const MuonEntry t = entry_of(set, blockIdx.x);
     const bool tall = t.fan_out > t.fan_in;
     const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
@@ -681,7 +694,7 @@ __global__ __launch_bounds__(C::kThreads, C::kAtOnce *C::kThreads / 256) void sm
             for (int e = 0; e < 4; ++e)
                 v[e] = (float)((double)u[k][e] * inverse) * kUnit;
             if (!tall) {
-                write_lds<C, SPLIT>(x, o, i, v);
+                write_lds<C>(x, o, i, v);
                 continue;
             }
 #pragma unroll
@@ -689,8 +702,7 @@ __global__ __launch_bounds__(C::kThreads, C::kAtOnce *C::kThreads / 256) void sm
                 f16 *to = reinterpret_cast<f16 *>(x + lds_at<C>(i + e, o)) + (o & 3);
                 const f16 hi = (f16)v[e];
                 to[0] = hi;
-                if (SPLIT)
-                    to[C::kX / 2] = (f16)(v[e] - (float)hi);
+                to[C::kX / 2] = (f16)(v[e] - (float)hi);
             }
         }
     }
@@ -713,8 +725,9 @@ __global__ __launch_bounds__(C::kThreads, C::kAtOnce *C::kThreads / 256) void sm
 #pragma unroll 1
     for (int n = 0; n < st.iterations; ++n) {
         {
-            f32x4 acc[FS][FQ] = {};
-            small_product<FS, FQ, SPLIT, C::N>(acc, x_rows(wp * FS), x_rows(fq));
+            f32x4 acc[FS][FQ] = {}, rest[FS][FQ] = {};
+            small_product<FS, FQ, SPLIT, C::N>(acc, rest, x_rows(wp * FS), x_rows(fq));
+            add_rest<FS, FQ, SPLIT>(acc, rest);
 #pragma unroll
             for (int i = 0; i < FS; i += 2)
 #pragma unroll
@@ -723,8 +736,9 @@ __global__ __launch_bounds__(C::kThreads, C::kAtOnce *C::kThreads / 256) void sm
         }
         __syncthreads();
         {
-            f32x4 acc[FS][FQ] = {};
-            small_product<FS, FQ, SPLIT, C::M>(acc, s_rows(wp * FS), s_rows(fq));
+            f32x4 acc[FS][FQ] = {}, rest[FS][FQ] = {};
+            small_product<FS, FQ, SPLIT, C::M>(acc, rest, s_rows(wp * FS), s_rows(fq));
+            add_rest<FS, FQ, SPLIT>(acc, rest);
 #pragma unroll
             for (int i = 0; i < FS; i += 2)
 #pragma unroll
@@ -743,20 +757,22 @@ __global__ __launch_bounds__(C::kThreads, C::kAtOnce *C::kThreads / 256) void sm
         }
         __syncthreads();
         {
-            f32x4 acc[FX][FQ] = {};
+            f32x4 acc[FX][FQ] = {}, more[FX][FQ] = {};
+            auto &rest = FX * FQ > 8 ? acc : more;  // two parts of depth only, and no registers for more
             auto x_columns = [&](int plane, int i, int part) {
                 constexpr int kOfBlock = C::kBlock / 16;
                 const int f = wp * FX + i;
                 return X::fragment(x + plane * C::kX + f / kOfBlock * C::kXBlock + (part >> 1) * X::kBytes, f % kOfBlock, part & 1);
             };
-            small_product<FX, FQ, SPLIT, C::M>(acc, x_columns, s_rows(fq));
+            small_product<FX, FQ, SPLIT, C::M>(acc, rest, x_columns, s_rows(fq));
+            add_rest<FX, FQ, SPLIT && FX * FQ <= 8>(acc, rest);
 #pragma unroll
             for (int i = 0; i < FX; i += 2)
 #pragma unroll
                 for (int j = 0; j < FQ; ++j) {
                     f32x4 a, b;
                     const int f = wp * FX + i, block = f / (C::kBlock / 16);
-                    read_pair<X, SPLIT>(x + block * C::kXBlock, C::kX, row + j * 16, f % (C::kBlock / 16), a, b);
+                    read_pair<X, true>(x + block * C::kXBlock, C::kX, row + j * 16, f % (C::kBlock / 16), a, b);
                     acc[i][j] = acc[i][j] * (1.0f / kUnit) + a * kA;
                     acc[i + 1][j] = acc[i + 1][j] * (1.0f / kUnit) + b * kA;
                 }
@@ -766,7 +782,7 @@ __global__ __launch_bounds__(C::kThreads, C::kAtOnce *C::kThreads / 256) void sm
 #pragma unroll
                 for (int j = 0; j < FQ; ++j) {
                     const int f = wp * FX + i, block = f / (C::kBlock / 16);
-                    write_pair<X, SPLIT>(x + block * C::kXBlock, C::kX, row + j * 16, f % (C::kBlock / 16), acc[i][j], acc[i + 1][j]);
+                    write_pair<X, true>(x + block * C::kXBlock, C::kX, row + j * 16, f % (C::kBlock / 16), acc[i][j], acc[i + 1][j]);
                 }
         }
         __syncthreads();
@@ -783,10 +799,10 @@ __global__ __launch_bounds__(C::kThreads, C::kAtOnce *C::kThreads / 256) void sm
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const f16 *from = reinterpret_cast<const f16 *>(x + lds_at<C>(i + e, o)) + (o & 3);
-                v[e] = (float)from[0] + (SPLIT ? (float)from[C::kX / 2] : 0.0f);
+                v[e] = (float)from[0] + (float)from[C::kX / 2];
             }
         else
-            v = read_lds<C, SPLIT>(x, o, i);
+            v = read_lds<C>(x, o, i);
         v *= 1.0f / kUnit;
         const long long at = (long long)o * t.fan_in + i;
         if (st.updates)
@@ -828,18 +844,18 @@ Sizes sizes_of(int fan_out, int fan_in, bool split)
     z.chunk = (unsigned)(chunk < 4096 ? 4096 : chunk);
     z.chunks = (unsigned)((all + z.chunk - 1) / z.chunk);
     z.squares = z.chunks * sizeof(double);
-    z.x = all * (split ? 4 : 2);
+    z.x = all * 4;
     z.s = (size_t)z.m * z.m * (split ? 4 : 2);
     return z;
 }
 
-template <class C, int KIND, bool SPLIT>
+template <class C, int KIND, bool SPLIT, int RESTS>
 hipError_t launch_step(const Planes &p, const Planes &q, const Planes &out, unsigned matrices, hipStream_t s)
 {
     const unsigned long long rows = (out.rows + C::TQ - 1) / C::TQ, cols = (out.cols + C::TP - 1) / C::TP;
     const unsigned long long all = matrices * (KIND != kApply ? rows * (rows + 1) / 2 : rows * cols);
     return launch_for<C>(all, [&](unsigned groups, unsigned) {
-        step_kernel<C, KIND, SPLIT><<<groups, C::kThreads, 0, s>>>(p, q, out, matrices);
+        step_kernel<C, KIND, SPLIT, RESTS><<<groups, C::kThreads, 0, s>>>(p, q, out, matrices);
     });
 }
 
@@ -869,7 +885,7 @@ hipError_t launch_pair(const Planes &p, const Planes &q, const Planes &out, unsi
 //            16 of 1,024 x 1,024    53, 59, 88       40, 49, 49      36, 46, 47
 //            8 of 2,048 x 4,096     372, 168, 701    193, 120, 322   206, 134, 271
 //            16 of 2,048 x 4,096    -                385, 240, 644   308, 199, 515
-template <int KIND, bool SPLIT>
+template <int KIND, bool SPLIT, int RESTS>
 hipError_t step(const Planes &p, const Planes &q, const Planes &out, unsigned matrices, hipStream_t s)
 {
     constexpr bool kDeep = KIND != kApply;
@@ -882,30 +898,26 @@ hipError_t step(const Planes &p, const Planes &q, const Planes &out, unsigned ma
     if constexpr (!SPLIT || !kDeep) {
         const double large = (SPLIT ? 3.4 : 1.65) * (double)((tiles(256) + 255) / 256);
         if (!small && q.cols >= 512 && large <= (double)((tiles(128) + at_once - 1) / at_once))
-            return launch_step<Product<f16, 256, 256, 4, 2, kDeep, true, false, true>, KIND, SPLIT>(p, q, out, matrices, s);
+            return launch_step<Product<f16, 256, 256, 4, 2, kDeep, true, false, true>, KIND, SPLIT, RESTS>(p, q, out, matrices, s);
     }
     if constexpr (SPLIT)
         return small ? launch_pair<Product<f16, 64, 64, 2, 2, kDeep, true, false, true>, KIND>(p, q, out, matrices, s)
                      : launch_pair<Product<f16, 128, 128, 2, 4, kDeep, true, false, true>, KIND>(p, q, out, matrices, s);
     else
-        return small ? launch_step<Product<f16, 64, 64, 2, 2, kDeep, true, false, true>, KIND, false>(p, q, out, matrices, s)
-                     : launch_step<Product<f16, 128, 128, 2, 2, kDeep, true, false, true>, KIND, false>(p, q, out, matrices, s);
+        return small ? launch_step<Product<f16, 64, 64, 2, 2, kDeep, true, false, true>, KIND, false, RESTS>(p, q, out, matrices, s)
+                     : launch_step<Product<f16, 128, 128, 2, 2, kDeep, true, false, true>, KIND, false, RESTS>(p, q, out, matrices, s);
 }
 
 // Whether a matrix's X and S fit a compute unit's LDS.
-bool is_small(const Sizes &z, bool split)
+bool is_small(const Sizes &z)
 {
-    return z.m == 64 ? z.n <= 512 : z.m == 128 && z.n <= (split ? 128 : 256);
+    return z.m == 64 ? z.n <= 512 : z.m == 128 && z.n == 128;
 }
 template <bool SPLIT>
 hipError_t small(const MuonSet &set, unsigned matrices, const Sizes &z, const MuonStep &st, hipStream_t s)
 {
-    if (z.m == 128) {
-        if constexpr (!SPLIT)
-            if (z.n > 128)
-                return launch_small<128, 256, false>(set, matrices, st, s);
+    if (z.m == 128)
         return launch_small<128, 128, SPLIT>(set, matrices, st, s);
-    }
     if (z.n > 128)
         return z.n > 256 ? launch_small<64, 512, SPLIT>(set, matrices, st, s) : launch_small<64, 256, SPLIT>(set, matrices, st, s);
     return z.n > 64 ? launch_small<64, 128, SPLIT>(set, matrices, st, s) : launch_small<64, 64, SPLIT>(set, matrices, st, s);
@@ -928,21 +940,29 @@ hipError_t orthogonalise(const MuonSet &set, unsigned matrices, const Sizes &z, 
     const Planes gram = planes(z.s, z.m, z.m), poly = planes(z.s, z.m, z.m);
     momentum_kernel<<<dim3(z.chunks, matrices), 256, 0, s>>>(set, st, z.chunk, squares);
     const dim3 tiles(z.n / 64, z.m / 64, matrices);
-    start_kernel<SPLIT><<<tiles, 256, 0, s>>>(set, st, squares, z.chunks, x);
+    start_kernel<<<tiles, 256, 0, s>>>(set, st, squares, z.chunks, x);
     hipError_t e = hipGetLastError();
     for (int i = 0; i < st.iterations && e == hipSuccess; ++i) {
-        e = step<kGram, SPLIT>(x, x, gram, matrices, s);
+        constexpr int kRests = SPLIT ? 3 : 0;
+        e = step<kGram, SPLIT, kRests>(x, x, gram, matrices, s);
         if (e == hipSuccess)
-            e = step<kSquare, SPLIT>(gram, gram, poly, matrices, s);
-        if (e == hipSuccess)
-            e = step<kApply, SPLIT>(x, poly, y, matrices, s);
+            e = step<kSquare, SPLIT, kRests>(gram, gram, poly, matrices, s);
+        if (e != hipSuccess)
+            break;
+        const int left = st.iterations - i;
+        if (SPLIT || left > 3)
+            e = step<kApply, SPLIT, 3>(x, poly, y, matrices, s);
+        else if (left == 3)
+            e = step<kApply, SPLIT, SPLIT ? 3 : 1>(x, poly, y, matrices, s);
+        else
+            e = step<kApply, SPLIT, kRests>(x, poly, y, matrices, s);
         const Planes was = x;
         x = y;
         y = was;
     }
     if (e != hipSuccess)
         return e;
-    finish_kernel<SPLIT><<<tiles, 256, 0, s>>>(set, st, x);
+    finish_kernel<<<tiles, 256, 0, s>>>(set, st, x, SPLIT);
     return hipGetLastError();
 }
 
@@ -951,7 +971,7 @@ hipError_t orthogonalise(const MuonSet &set, unsigned matrices, const Sizes &z, 
 size_t muon_workspace_bytes(int fan_out, int fan_in, bool split, unsigned matrices)
 {
     const Sizes z = sizes_of(fan_out, fan_in, split);
-    if (is_small(z, split))
+    if (is_small(z))
         return 0;  // all in LDS
     return whole(z.squares * matrices) + 2 * whole(z.x * matrices) + 2 * whole(z.s * matrices);
 }
@@ -960,7 +980,7 @@ hipError_t launch_muon(const MuonSet &set, unsigned matrices, int fan_out, int f
                        const MuonStep &st, void *workspace, hipStream_t s)
 {
     const Sizes z = sizes_of(fan_out, fan_in, split);
-    if (is_small(z, split))
+    if (is_small(z))
         return split ? small<true>(set, matrices, z, st, s) : small<false>(set, matrices, z, st, s);
     char *ws = static_cast<char *>(workspace);
     return split ? orthogonalise<true>(set, matrices, z, st, ws, s)

@@ -1,10 +1,11 @@
 """Orthogonalised updates on the GPU against the iteration in float64.
 
-Tolerances are of norms (Frobenius), for each matrix.  The kernels' operands carry 22 bits
-(float32: two fp16 values) or 11 (bf16: one), sums are float32.  A plain float32 iteration
-has operands of 24 bits and the same sums, so what its roundings make of a matrix, the
-kernels' make 4 or 2^13 times as large; that much of the plain iteration's own error is
-allowed, and 2^-22 or 2^-11 for a matrix that it gets exactly.  Roundings r_k of a step reach
+Tolerances are of norms (Frobenius), for each matrix.  bf16: what the steps lose is no more than
+half a step of the result's type, 2^-8 of the norm, beside the result's own rounding.
+float32: the kernels' operands carry 22 bits (two fp16 values), sums are float32.  A plain
+float32 iteration has operands of 24 bits and the same sums, so what its roundings make of a
+matrix, the kernels' make 4 times as large; that much of the plain iteration's own error is
+allowed, and 2^-22 for a matrix that it gets exactly.  Roundings r_k of a step reach
 the result as a sum of D_k r_k with the matrix's own sensitivities D_k, the same for both.
 Over many singular values a sum of squares of such sums is near its mean; of a matrix of few
 values one sample can be next to nothing (a 1 x 1 matrix of 1 comes out 3e-8 off in float32
@@ -55,9 +56,9 @@ def direction(u, dtype, iterations=5):
         off = iterated(y, iterations).double() - iterated(x * (1 + j * 2.0 ** -18), iterations)
         of = torch.maximum(off.square().sum((-2, -1)).sqrt(), torch.as_tensor(of, dtype=torch.float64, device="cuda"))
     norm = want.square().sum((-2, -1)).sqrt()
-    bits = 2 if dtype == FP32 else 13
+    far = 4 * of + 2.0 ** -22 * norm if dtype == FP32 else 2.0 ** -8 * norm
     floor = A ** iterations * 2.0 ** -37 * (u.shape[-2] * u.shape[-1]) ** 0.5
-    return want.mT if u.shape[-2] > u.shape[-1] else want, 2.0 ** bits * of + 2.0 ** (bits - 24) * norm + floor
+    return want.mT if u.shape[-2] > u.shape[-1] else want, far + floor
 
 
 def spread(g, *shape):
