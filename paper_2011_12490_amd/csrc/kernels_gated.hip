@@ -32,8 +32,11 @@ hipError_t gated(const LinearShape &sh, Rows x, const void *w, const float *bias
     if constexpr (sizeof(T) == 2) {
         // large tiles as in large_tiles, from a depth of 256 on; in both sizes a wave has 64
         // columns, whole lines.  us, rows of bf16 with gates and ups kept, 256 and 128: 256 to
-        // 256 on 262,139 156, 169, on 65,536 41, 40; 320 to 512 on 65,536 79, 82; 1,024 to
-        // 1,024 on 32,768 144, 170; waves of 32 columns in tiles of 128: 203, 41, 84, 166
+        // 256 on 262,139 146, 148 (197 past weights in LDS), on 65,536 41, 40; 320 to 512 on
+        // 65,536 88, 82; 1,024 to 1,024 on 32,768 144 to 163, 159 to 170 (two cards); 2,048 to
+        // 4,096 on 32,768 1,036, 1,245.  262,139 rows of 256 to 256 move 537 MB: 3.7 TB/s, the
+        // four steps of a tile's loads waiting for its results' stores; wide ones are bound by
+        // the matrix units' power (1,060 TFLOP/s)
         if (alone && depth >= 256 && large_tiles(p, 2 * O))
             return launch_rows<Product<T, 256, 256, 2, 4, true, true, false, true, false, 1, true>>(p, mw, mx, bias, act, y, O,
                                                                                                  depth, s, pre);

@@ -53,7 +53,9 @@ __device__ __forceinline__ int vec_at(int c, int D)
 }
 
 // ---- rows out of the table ------------------------------------------------------
-// A group of 2^group_log2 lanes a row, four rows under way.
+// A group of 2^group_log2 lanes a row, four rows under way.  Bound by its bytes: 524,288 rows
+// of 512 bf16 values out of 200,000 in 154 us, 537 MB written and 257 read (5.2 TB/s); whole
+// lines past the caches (through them 174 us).
 template <class T, int V, bool PAST>
 __global__ __launch_bounds__(256) void lookup_kernel(const T *table, long long stride, const int *ids, long long samples,
                                                      long long rows, int D, float scale, T *out, long long os, int group_log2)
@@ -93,7 +95,9 @@ __global__ __launch_bounds__(256) void lookup_kernel(const T *table, long long s
 // those of smaller digits, plus those of its digit in earlier blocks, in earlier waves
 // of its block and in earlier lanes, which are matched by ballots: stable.  A sample
 // without a row has the key `rows`, behind all others.  Up to kOneBlock samples one
-// workgroup takes all passes, its samples in registers and LDS.
+// workgroup takes all passes, its samples in registers and LDS (the gradient's us so and in
+// launches, rows of 48: 500 samples of 500 rows 20, 23; 8,192 of 500 23, 25; of 100,000 33, 40).
+// Bound by a launch's waits: 524,288 samples of 200,000 rows take two passes of 21 us.
 
 constexpr int kOneKeys = 8;
 constexpr int kSortThreads = 256, kOneThreads = 1024;
@@ -325,7 +329,8 @@ __global__ __launch_bounds__(kOneThreads) void sort_one_kernel(const int *ids, u
 // The sorted list in pieces of kPiece entries, a group of lanes each.  A run of one key
 // that lies within a piece is a row of the result.  Of a run that goes on in the next
 // piece its beginning is kept as the piece's trail, and what came from the piece before as
-// its lead; where a run began, its trail and the leads behind are joined.
+// its lead; where a run began, its trail and the leads behind are joined.  Bound by its
+// bytes: 524,288 samples of 512 bf16 values into 200,000 rows, 947 MB, in 194 us (4.9 TB/s).
 
 constexpr unsigned kNone = 0xFFFFFFFFu;
 constexpr unsigned kPiece = 32;
@@ -559,7 +564,8 @@ __global__ __launch_bounds__(256) void join_kernel(const Ends *ends, const float
 }
 
 // Few samples in one launch: a workgroup takes some rows, notes the samples that are
-// theirs, in order, and sums them row by row, a group of lanes each.
+// theirs, in order, and sums them row by row, a group of lanes each.  us so and sorted, rows
+// of 48: 64 samples of 500 rows 8, 19; 256 of 500 16, 20, of 20,000 7, 24.
 constexpr unsigned kFewSamples = 256;
 template <class T, int V>
 __global__ __launch_bounds__(256) void few_kernel(const int *ids, const T *from, long long stride, unsigned samples, unsigned rows, int D,
@@ -785,9 +791,14 @@ hipError_t backward(Rows dout, const int *ids, unsigned samples, unsigned rows, 
     Ends *ends = reinterpret_cast<Ends *>(ws + at.ends);
     float *leads = reinterpret_cast<float *>(ws + at.leads), *trails = reinterpret_cast<float *>(ws + at.trails);
     const unsigned *k = keys[now], *v = values[now];
+    // Past the caches where they would not hold it all (256 MB).  us with and without: bf16
+    // 131,072 samples of 50,000 rows of 512 (237 MB) 81, 68; 262,144 of 100,000 (473 MB) 145, 150;
+    // 524,288 of 200,000 (946 MB) 250, 268; float32 65,536 of 20,000 (175 MB) 60, 55; 131,072 of
+    // 50,000 (371 MB) 101, 109.
+    const bool past = ((size_t)samples * sizeof(T) + (size_t)rows * 4) * dim > (256u << 20);
     if (dim < V)
         e = sums<T, 1, false>(k, v, dout, samples, rows, dim, scale, out, ends, leads, trails, s);
-    else if (whole_lines(out, dim, dim, 4) && whole_lines(dout.p, dout.stride, dim, sizeof(T)))
+    else if (past && whole_lines(out, dim, dim, 4) && whole_lines(dout.p, dout.stride, dim, sizeof(T)))
         e = sums<T, V, true>(k, v, dout, samples, rows, dim, scale, out, ends, leads, trails, s);
     else
         e = sums<T, V, false>(k, v, dout, samples, rows, dim, scale, out, ends, leads, trails, s);

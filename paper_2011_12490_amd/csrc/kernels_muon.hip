@@ -591,6 +591,9 @@ __global__ __launch_bounds__(C::kThreads, 2) void pair_kernel(Planes pm, Planes 
 // Matrices that fit: a workgroup takes one from its gradient to its parameters, X and S (or
 // Q in its place) in LDS.  Both lie in tiles of 64 rows by up to 128 columns, X's by blocks
 // of columns: their rows are read as they lie, and X's columns for Q X by transposing reads.
+// Bound by waits: a step's three products follow each other, with a barrier after each, and a
+// compute unit holds one matrix of 128 rows.  144 of 128 x 128 (float32) 58 us, in steps
+// through memory 327; 24 of 64 x 256 30, 85.
 template <int M_, int N_, bool SPLIT>
 struct Small {
     static constexpr int M = M_, N = N_, kPlanes = SPLIT ? 2 : 1 /* of S */, kThreads = M == 128 ? 1024 : 512;
@@ -871,20 +874,23 @@ hipError_t launch_pair(const Planes &p, const Planes &q, const Planes &out, unsi
 // Tiles of 64, 128 or 256 rows and columns.  Small ones while there are few, whose loads'
 // waits others fill; from 512 of depth on 256 where their rounds of 256 workgroups cost less
 // than those of 128 (two at once a compute unit, or split one): a large one takes as long as
-// 1.65 small ones, split 3.4 (but for split S and Q, where they are no faster).  us of S, Q and Q X with 64, 128 and 256 (matrices of m x n):
-//   float32  24 of 300 x 701        15, 12, 27.4     22, 17, 28.8    54, 42, 51
-//            8 of 512 x 512         14, 15, 15       18, 21, 19      46, 58, 59
-//            16 of 512 x 1,024      30, 23, 48       30, 22, 41      76, 60, 64
-//            2 of 2,048 x 2,048     82, 86, 128      100, 105, 104   140, 154, 156
-//            16 of 1,024 x 1,024    87, 96, 155      90, 101, 125    101, 117, 125
-//            8 of 2,048 x 4,096     556, 302, 1,001  494, 282, 839   590, 340, 723
-//   bf16     24 of 300 x 701        10.8, 8.4, 16.4  15.0, 13.0, 13.6  25, 23, 25
-//            8 of 512 x 512         9.3, 9.8, 9.4    12.6, 15.0, 12.7  22, 29, 27
-//            16 of 512 x 1,024      21, 15, 26       20, 16, 18      32, 31, 30
-//            2 of 2,048 x 2,048     53, 55, 72       39, 42, 44      52, 62, 61
-//            16 of 1,024 x 1,024    53, 59, 88       40, 49, 49      36, 46, 47
-//            8 of 2,048 x 4,096     372, 168, 701    193, 120, 322   206, 134, 271
-//            16 of 2,048 x 4,096    -                385, 240, 644   308, 199, 515
+// 1.65 small ones, split 3.4 (but for split S and Q, where they are no faster: 8 of 2,048 x
+// 4,096 494, 282 with 128, 592, 340 with 256).  us of S, Q and Q X with 64, 128 and 256
+// (matrices of m x n; bf16's Q X the mean of its steps):
+//   float32  24 of 300 x 701        16, 12, 28       22, 17, 30       Q X 51
+//            8 of 512 x 512         14, 15, 15       18, 21, 19       59
+//            16 of 512 x 1,024      30, 22, 49       30, 22, 41       65
+//            2 of 2,048 x 2,048     82, 85, 131      101, 108, 108    157
+//            16 of 1,024 x 1,024    86, 94, 158      92, 103, 129     124
+//            8 of 2,048 x 4,096     562, 306, 1,040  499, 284, 857    744
+//   bf16     24 of 300 x 701        10.5, 8.3, 18    15.5, 12.7, 18   25, 23, 32
+//            8 of 512 x 512         8.8, 10.2, 10.5  12.7, 15, 15     22, 30, 34
+//            16 of 512 x 1,024      21, 15, 29       19, 16, 23       32, 31, 37
+//            2 of 2,048 x 2,048     52, 55, 75       41, 45, 52       53, 63, 69
+//            16 of 1,024 x 1,024    53, 59, 92       42, 49, 59       38, 48, 57
+//            8 of 2,048 x 4,096     384, 165, 750    197, 124, 365    206, 135, 309
+// The last round of large tiles as quarters (16 of 2,048 x 4,096, 2.25 rounds) gains 1 %: the
+// matrix units' power, not their number, bounds these.
 template <int KIND, bool SPLIT, int RESTS>
 hipError_t step(const Planes &p, const Planes &q, const Planes &out, unsigned matrices, hipStream_t s)
 {
