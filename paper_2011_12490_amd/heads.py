@@ -16,6 +16,10 @@ Sec. 3.2 is
     dx = dispatch_backward(dx0, r)
     optimizer.step()
 
+gated and gated_backward take the place of linear in heads of gated layers, lookup brings
+the samples' rows of a table (a code for each image) and lookup_backward their gradients,
+and Muon takes hidden layers' weights where AdamW takes the rest.
+
 Argument checks and marshalling only; all work is done by libderf.so, on torch's
 current stream of the tensors' device.  Tensors are float32 or bfloat16, of any
 row stride (the layers': below 2^21 elements), on one GPU; what does not fit, and
