@@ -340,6 +340,35 @@ __device__ __forceinline__ void step_tile(unsigned in, unsigned row_tiles, unsig
     }
 }
 
+// Which tiles a workgroup takes.  A matrix's tiles go to 2^parts XCDs (eight share an L2 of
+// their own each): the same ones in every product, so that what they wrote and read is in
+// their L2 still.  parts < 0: tiles in order, by runs (by_xcd).
+struct Spread {
+    unsigned matrices, each;  // tiles of a matrix
+    int parts;
+};
+__host__ __device__ inline unsigned chunk_of(const Spread &sp) { return (sp.each + (1u << sp.parts) - 1) >> sp.parts; }
+// Workgroups' numbers end here.
+__host__ __device__ inline unsigned long long spread_end(const Spread &sp)
+{
+    if (sp.parts < 0)
+        return (unsigned long long)sp.matrices * sp.each + kXcds * kRun;  // runs_end is not above it
+    return (((unsigned long long)sp.matrices << sp.parts) + kXcds - 1) / kXcds * chunk_of(sp) * kXcds;
+}
+__device__ __forceinline__ bool tile_of(const Spread &sp, unsigned b, unsigned &matrix, unsigned &tile)
+{
+    if (sp.parts < 0) {
+        const unsigned at = by_xcd(b, sp.matrices * sp.each);
+        matrix = at / sp.each;
+        tile = at - matrix * sp.each;
+        return matrix < sp.matrices;
+    }
+    const unsigned chunk = chunk_of(sp), j = b / kXcds, xcd = b % kXcds, round = j / chunk;
+    matrix = (round * kXcds + xcd) >> sp.parts;
+    tile = (xcd & ((1u << sp.parts) - 1)) * chunk + j - round * chunk;
+    return matrix < sp.matrices && tile < sp.each;
+}
+
 // out = a product of P and Q for each matrix: S = X X^T (Gram: P, Q = X), Q = b S +
 // c S S (Square: P, Q = S; both results symmetric: tiles on and below the diagonal are
 // computed and written to both places), X = a X + Q X (Apply: P = X, depth down its
@@ -347,22 +376,20 @@ __device__ __forceinline__ void step_tile(unsigned in, unsigned row_tiles, unsig
 // SPLIT: the products of each operand's rests with the other's rounded values, then of
 // those, one after the other into the same registers.
 template <class C, int KIND, bool SPLIT, int RESTS>
-__global__ __launch_bounds__(C::kThreads, 2) void step_kernel(Planes pm, Planes qm, Planes out, unsigned matrices)
+__global__ __launch_bounds__(C::kThreads, 2) void step_kernel(Planes pm, Planes qm, Planes out, Spread sp)
 {
     constexpr bool kSymmetric = KIND != kApply;
     constexpr int kPasses = SPLIT ? 3 : 1, COLS = C::FP * 16;
     __shared__ __attribute__((aligned(16))) char lds[C::kLds];
     __shared__ __attribute__((aligned(16))) char results[C::WP * C::WQ * 16 * kPieceRow<f16, COLS>];
     const unsigned row_tiles = (out.rows + C::TQ - 1) / C::TQ, col_tiles = (out.cols + C::TP - 1) / C::TP;
-    const unsigned each = kSymmetric ? row_tiles * (row_tiles + 1) / 2 : row_tiles * col_tiles;
-    const unsigned all = matrices * each, end = runs_end(all), depth = qm.cols;
+    const unsigned end = sp.parts < 0 ? runs_end(sp.matrices * sp.each) : (unsigned)spread_end(sp), depth = qm.cols;
     static_assert(!kSymmetric || C::TP == C::TQ, "square tiles");
     auto tile_at = [&](unsigned b, unsigned &matrix, unsigned &r0, unsigned &c0) {
-        const unsigned at = by_xcd(b, all);
-        if (at >= all)
+        unsigned tile;
+        if (!tile_of(sp, b, matrix, tile))
             return false;
-        matrix = at / each;
-        step_tile<C::TP, C::TQ, kSymmetric>(at - matrix * each, row_tiles, col_tiles, r0, c0);
+        step_tile<C::TP, C::TQ, kSymmetric>(tile, row_tiles, col_tiles, r0, c0);
         return true;
     };
     unsigned ahead = blockIdx.x, pass = 0;
@@ -526,20 +553,17 @@ __device__ __forceinline__ void add_rest(f32x4 (&acc)[FP][FQ], const f32x4 (&res
 // both operands, so that it has three products to do while the next ones' loads are under
 // way, where the passes of step_kernel have one and wait.
 template <class C, int KIND>
-__global__ __launch_bounds__(C::kThreads, 2) void pair_kernel(Planes pm, Planes qm, Planes out, unsigned matrices)
+__global__ __launch_bounds__(C::kThreads, 2) void pair_kernel(Planes pm, Planes qm, Planes out, Spread sp)
 {
     constexpr bool kSymmetric = KIND != kApply;
     constexpr int kStage = 2 * C::kStage, kLoads = 2 * C::kLoads, COLS = C::FP * 16;
     __shared__ __attribute__((aligned(16))) char lds[2 * kStage];
     static_assert(C::WP * C::WQ * 16 * kPieceRow<f16, COLS> <= 2 * kStage, "results take the stages' place");
     const unsigned row_tiles = (out.rows + C::TQ - 1) / C::TQ, col_tiles = (out.cols + C::TP - 1) / C::TP;
-    const unsigned each = kSymmetric ? row_tiles * (row_tiles + 1) / 2 : row_tiles * col_tiles;
-    const unsigned at = by_xcd(blockIdx.x, matrices * each);
-    if (at >= matrices * each)
+    unsigned matrix, tile, r0, c0;
+    if (!tile_of(sp, blockIdx.x, matrix, tile))
         return;
-    const unsigned matrix = at / each;
-    unsigned r0, c0;
-    step_tile<C::TP, C::TQ, kSymmetric>(at - matrix * each, row_tiles, col_tiles, r0, c0);
+    step_tile<C::TP, C::TQ, kSymmetric>(tile, row_tiles, col_tiles, r0, c0);
     const f16 *p = pm.p + matrix * pm.matrix, *q = qm.p + matrix * qm.matrix;
     typename C::P::Feed pf[2];
     typename C::Q::Feed qf[2];
@@ -852,22 +876,41 @@ Sizes sizes_of(int fan_out, int fan_in, bool split)
     return z;
 }
 
+// A matrix on as few XCDs as take no more rounds than all would, but for large tiles, whose
+// matrices an L2 does not hold; at_once: workgroups a compute unit.  A call's us so and in
+// order: float32, 24 of 300 x 701 287, 302; 8 of 512 x 512 192, 234; 4 of 1,024 x 1,024 447, 483;
+// one of 300 x 300 112, 116; bf16, 24 of 300 x 701 198, 204; 16 of 2,048 x 4,096 6,160, 6,100.
+template <class C, int KIND>
+Spread spread(const Planes &out, unsigned matrices, unsigned at_once)
+{
+    const unsigned rows = (out.rows + C::TQ - 1) / C::TQ, cols = (out.cols + C::TP - 1) / C::TP;
+    Spread sp = {matrices, KIND != kApply ? rows * (rows + 1) / 2 : rows * cols, 0};
+    const unsigned long long slots = 32 * at_once, all = (unsigned long long)matrices * sp.each;
+    const unsigned long long rounds = ((all + kXcds - 1) / kXcds + slots - 1) / slots;
+    for (; C::TQ < 256 && sp.parts < 4; ++sp.parts)
+        if ((spread_end(sp) / kXcds + slots - 1) / slots <= rounds)
+            return sp;
+    sp.parts = -1;
+    return sp;
+}
+
 template <class C, int KIND, bool SPLIT, int RESTS>
 hipError_t launch_step(const Planes &p, const Planes &q, const Planes &out, unsigned matrices, hipStream_t s)
 {
-    const unsigned long long rows = (out.rows + C::TQ - 1) / C::TQ, cols = (out.cols + C::TP - 1) / C::TP;
-    const unsigned long long all = matrices * (KIND != kApply ? rows * (rows + 1) / 2 : rows * cols);
-    return launch_for<C>(all, [&](unsigned groups, unsigned) {
-        step_kernel<C, KIND, SPLIT, RESTS><<<groups, C::kThreads, 0, s>>>(p, q, out, matrices);
+    const Spread sp = spread<C, KIND>(out, matrices, C::kThreads >= 512 ? 1 : 2);
+    return launch_for<C>(spread_end(sp), [&](unsigned groups, unsigned) {
+        step_kernel<C, KIND, SPLIT, RESTS><<<groups, C::kThreads, 0, s>>>(p, q, out, sp);
     });
 }
 
 template <class C, int KIND>
 hipError_t launch_pair(const Planes &p, const Planes &q, const Planes &out, unsigned matrices, hipStream_t s)
 {
-    const unsigned long long rows = (out.rows + C::TQ - 1) / C::TQ, cols = (out.cols + C::TP - 1) / C::TP;
-    const unsigned long long all = matrices * (KIND != kApply ? rows * (rows + 1) / 2 : rows * cols);
-    pair_kernel<C, KIND><<<(unsigned)all + kXcds * kRun, C::kThreads, 0, s>>>(p, q, out, matrices);
+    const Spread sp = spread<C, KIND>(out, matrices, C::kThreads >= 512 ? 1 : 2);
+    const unsigned long long end = spread_end(sp);
+    if (end >= 1ull << 31)  // more than any memory holds
+        return hipErrorInvalidConfiguration;
+    pair_kernel<C, KIND><<<(unsigned)end, C::kThreads, 0, s>>>(p, q, out, sp);
     return hipGetLastError();
 }
 

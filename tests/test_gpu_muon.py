@@ -87,12 +87,13 @@ def test_orthogonalise(K, O, I, dtype):
     check(heads.orthogonalise(x[0]), want[0], far[0])  # a matrix, alone
 
 
-def test_every_number_of_iterations():
+@pytest.mark.parametrize("dtype", [FP32, BF16])
+def test_every_number_of_iterations(dtype):
     g = gen(1)
-    for shape in ((2, 70, 150), (2, 60, 64)):
-        x = spread(g, *shape)
-        for n in (1, 2, 3, 8):
-            check(heads.orthogonalise(x, n), *direction(x.double(), FP32, n))
+    for shape in ((2, 70, 150), (2, 60, 64), (3, 300, 200)):
+        x = spread(g, *shape).to(dtype)
+        for n in (1, 2, 3, 4, 8):
+            check(heads.orthogonalise(x, n), *direction(x.double(), dtype, n))
 
 
 def test_singular_values_come_near_one_and_directions_stay():
