@@ -23,6 +23,8 @@
 // products 564 us where both take 680.
 #include "product.h"
 
+#include <algorithm>
+
 namespace derf {
 
 namespace {
@@ -275,49 +277,103 @@ __global__ __launch_bounds__(256) void finish_kernel(const MuonSet set, MuonStep
 
 enum Kind { kGram, kSquare, kApply };
 
-// A wave's results, from row r and column c on, to both planes of `to` [rows][cols], with
-// what they are added to (was: S or X).  mirror: those of a symmetric matrix to the place
-// above the diagonal too.  RESTS: 1 what they are added to has both planes, 2 `to` gets both.
+// What a wave's results are added to (S or X): read at once where the registers hold it all,
+// else row by row of results (all of it before the product, beside the first loads: 5 us of
+// 280 more).  RESTS: 1 it has both planes.
 template <int KIND, int RESTS, int FP, int FQ>
-__device__ __forceinline__ void write_step(const f32x4 (&acc)[FP][FQ], const f16 *was, f16 *to, unsigned rows, unsigned cols, unsigned r,
-                                           unsigned c, char *mine, bool mirror)
-{
-    const int lane = threadIdx.x & 63;
-    const size_t rest = (size_t)rows * cols;
-#pragma unroll
-    for (int j = 0; j < FQ; ++j) {
+struct Was {
+    static constexpr bool kAll = FP * FQ * (RESTS & 1 ? 2 : 1) <= 16;
+    static constexpr int kRows = kAll ? FQ : 1;
+    f16x4 hi[kRows][FP], lo[kRows][FP];
+    __device__ __forceinline__ void read_row(const f16 *from, unsigned rows, unsigned cols, unsigned r, unsigned c, int j)
+    {
+        const int lane = threadIdx.x & 63;
         const unsigned row = r + j * 16 + (lane & 15);
-        f32x4 v[FP], lo[FP];
 #pragma unroll
         for (int i = 0; i < FP; ++i) {
             const unsigned col = c + i * 16 + (lane >> 4) * 4;
-            v[i] = acc[i][j] * (1.0f / kUnit);
-            if (KIND != kGram && row < rows && col < cols) {
-                const size_t at = (size_t)row * cols + col;
-                f32x4 old = __builtin_convertvector(*reinterpret_cast<const f16x4 *>(was + at), f32x4);
+            f16x4 &h = hi[j % kRows][i], &l = lo[j % kRows][i];
+            h = l = f16x4{};
+            if (row < rows && col < cols) {
+                const f16 *at = from + ((size_t)row * cols + col);
+                h = *reinterpret_cast<const f16x4 *>(at);
                 if (RESTS & 1)
-                    old += __builtin_convertvector(*reinterpret_cast<const f16x4 *>(was + rest + at), f32x4);
+                    l = *reinterpret_cast<const f16x4 *>(at + (size_t)rows * cols);
+            }
+        }
+    }
+    __device__ __forceinline__ void read(const f16 *from, unsigned rows, unsigned cols, unsigned r, unsigned c)
+    {
+        if (kAll && KIND != kGram)
+#pragma unroll
+            for (int j = 0; j < FQ; ++j)
+                read_row(from, rows, cols, r, c, j);
+    }
+};
+
+// 16 rows of results (as write_16_rows) of a symmetric matrix to their columns' rows: turned
+// in the wave's place in LDS, 8 rows a piece, a column's two pieces in turn.
+template <int FP>
+__device__ __forceinline__ void write_turned(const f32x4 (&v)[FP], char *mine, unsigned row0, unsigned c, f16 *to, unsigned size)
+{
+    const int lane = threadIdx.x & 63;
+    auto place = [](int col, int piece) { return col * 32 + (piece ^ (col >> 2 & 1)) * 16; };
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < FP; ++i)
+#pragma unroll
+        for (int k = 0; k < 4; ++k)
+            *reinterpret_cast<f16 *>(mine + place(i * 16 + (lane >> 4) * 4 + k, lane >> 3 & 1) + (lane & 7) * 2) = (f16)v[i][k];
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int n = 0; n < FP * 32; n += 64) {
+        const int col = (n + lane) >> 1, piece = lane & 1;
+        const u32x4 x = *reinterpret_cast<const u32x4 *>(mine + place(col, piece));
+        const unsigned row = row0 + piece * 8;
+        if (row < size && c + col < size)  // both are multiples of 64
+            *reinterpret_cast<u32x4 *>(to + ((size_t)(c + col) * size + row)) = x;
+    }
+    __builtin_amdgcn_wave_barrier();
+}
+
+// A wave's results, from row r and column c on, to `to` [rows][cols].  mirror: those of a
+// symmetric matrix to the place above the diagonal too.  RESTS: 2 `to` gets both planes.
+// PAST: past the caches; small matrices' products are read from them.
+template <int KIND, int RESTS, bool PAST, int FP, int FQ>
+__device__ __forceinline__ void write_step(const f32x4 (&acc)[FP][FQ], Was<KIND, RESTS, FP, FQ> &was, const f16 *from, f16 *to, unsigned rows,
+                                           unsigned cols, unsigned r, unsigned c, char *mine, bool mirror)
+{
+    const size_t rest = (size_t)rows * cols;
+#pragma unroll
+    for (int j = 0; j < FQ; ++j) {
+        f32x4 v[FP], lo[FP];
+        if (KIND != kGram && !was.kAll)
+            was.read_row(from, rows, cols, r, c, j);
+#pragma unroll
+        for (int i = 0; i < FP; ++i) {
+            v[i] = acc[i][j] * (1.0f / kUnit);
+            if (KIND != kGram) {
+                f32x4 old = __builtin_convertvector(was.hi[j % was.kRows][i], f32x4);
+                if (RESTS & 1)
+                    old += __builtin_convertvector(was.lo[j % was.kRows][i], f32x4);
 #pragma unroll
                 for (int k = 0; k < 4; ++k)
                     v[i][k] = KIND == kSquare ? fmaf(kC, v[i][k], kB * old[k]) : fmaf(kA, old[k], v[i][k]);
             }
-            lo[i] = v[i] - __builtin_convertvector(__builtin_convertvector(v[i], f16x4), f32x4);
+            // rounded once, for all that take it: from a sum's fused multiply-add a second
+            // conversion may round to another value, whose rest this is not
+            const f32x4 hi = __builtin_convertvector(__builtin_convertvector(v[i], f16x4), f32x4);
+            lo[i] = v[i] - hi;
+            v[i] = hi;
         }
-        write_16_rows<f16, FP * 16>(v, mine, r + j * 16, rows, c, cols, to, cols);
+        write_16_rows<f16, FP * 16, true, PAST>(v, mine, r + j * 16, rows, c, cols, to, cols);
         if (RESTS & 2)
-            write_16_rows<f16, FP * 16>(lo, mine, r + j * 16, rows, c, cols, to + rest, cols);
-        if (KIND != kApply && mirror)
-#pragma unroll
-            for (int i = 0; i < FP; ++i)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const unsigned col = c + i * 16 + (lane >> 4) * 4 + k;
-                    if (row < rows && col < cols) {
-                        to[(size_t)col * cols + row] = (f16)v[i][k];
-                        if (RESTS & 2)
-                            to[rest + (size_t)col * cols + row] = (f16)lo[i][k];
-                    }
-                }
+            write_16_rows<f16, FP * 16, true, PAST>(lo, mine, r + j * 16, rows, c, cols, to + rest, cols);
+        if (KIND != kApply && mirror) {
+            write_turned<FP>(v, mine, r + j * 16, c, to, rows);
+            if (RESTS & 2)
+                write_turned<FP>(lo, mine, r + j * 16, c, to + rest, rows);
+        }
     }
 }
 
@@ -429,8 +485,11 @@ __global__ __launch_bounds__(C::kThreads, 2) void step_kernel(Planes pm, Planes 
 #pragma unroll 1
             for (unsigned k = 0; k < depth; k += C::kDepth)
                 pipe.step(acc, next_tile, [](auto &) {});
-        write_step<KIND, RESTS, C::FP, C::FQ>(acc, pm.p + matrix * pm.matrix, out.p + matrix * out.matrix, out.rows, out.cols, r0 + wq,
-                                              c0 + wp, mine, r0 != c0);
+        const f16 *from = pm.p + matrix * pm.matrix;
+        Was<KIND, RESTS, C::FP, C::FQ> was;
+        was.read(from, out.rows, out.cols, r0 + wq, c0 + wp);
+        write_step<KIND, RESTS, (C::TP >= 256), C::FP, C::FQ>(acc, was, from, out.p + matrix * out.matrix, out.rows, out.cols, r0 + wq, c0 + wp, mine,
+                                              r0 != c0);
     }
     arrived<0>();
 }
@@ -587,10 +646,10 @@ __global__ __launch_bounds__(C::kThreads, 2) void pair_kernel(Planes pm, Planes 
             qf[n].advance();
         }
     };
-    bring(0);
-    bring(kStage);
     const int wave = uniform(threadIdx.x >> 6);
     const int fp = (wave % C::WP) * C::FP, fq = (wave / C::WP) * C::FQ;
+    bring(0);
+    bring(kStage);
     f32x4 acc[C::FP][C::FQ] = {}, rest[C::FP][C::FQ] = {};
     unsigned stage = 0;
 #pragma unroll 1
@@ -604,10 +663,12 @@ __global__ __launch_bounds__(C::kThreads, 2) void pair_kernel(Planes pm, Planes 
         bring(stage);
         stage ^= kStage;
     }
+    Was<KIND, 3, C::FP, C::FQ> was;
+    was.read(p, out.rows, out.cols, r0 + fq * 16, c0 + fp * 16);
     arrived<0>();
     add_rest<C::FP, C::FQ, true>(acc, rest);
-    write_step<KIND, 3, C::FP, C::FQ>(acc, p, out.p + matrix * out.matrix, out.rows, out.cols, r0 + fq * 16, c0 + fp * 16,
-                                         lds + wave * 16 * kPieceRow<f16, COLS>, r0 != c0);
+    write_step<KIND, 3, false, C::FP, C::FQ>(acc, was, p, out.p + matrix * out.matrix, out.rows, out.cols, r0 + fq * 16, c0 + fp * 16,
+                                      lds + wave * 16 * kPieceRow<f16, COLS>, r0 != c0);
 }
 
 // ---- small matrices, all of it in one launch ----------------------------------------------
@@ -914,26 +975,26 @@ hipError_t launch_pair(const Planes &p, const Planes &q, const Planes &out, unsi
     return hipGetLastError();
 }
 
-// Tiles of 64, 128 or 256 rows and columns.  Small ones while there are few, whose loads'
-// waits others fill; from 512 of depth on 256 where their rounds of 256 workgroups cost less
-// than those of 128 (two at once a compute unit, or split one): a large one takes as long as
-// 1.65 small ones, split 3.4 (but for split S and Q, where they are no faster: 8 of 2,048 x
-// 4,096 494, 282 with 128, 592, 340 with 256).  us of S, Q and Q X with 64, 128 and 256
-// (matrices of m x n; bf16's Q X the mean of its steps):
-//   float32  24 of 300 x 701        16, 12, 28       22, 17, 30       Q X 51
-//            8 of 512 x 512         14, 15, 15       18, 21, 19       59
-//            16 of 512 x 1,024      30, 22, 49       30, 22, 41       65
-//            2 of 2,048 x 2,048     82, 85, 131      101, 108, 108    157
-//            16 of 1,024 x 1,024    86, 94, 158      92, 103, 129     124
-//            8 of 2,048 x 4,096     562, 306, 1,040  499, 284, 857    744
-//   bf16     24 of 300 x 701        10.5, 8.3, 18    15.5, 12.7, 18   25, 23, 32
-//            8 of 512 x 512         8.8, 10.2, 10.5  12.7, 15, 15     22, 30, 34
-//            16 of 512 x 1,024      21, 15, 29       19, 16, 23       32, 31, 37
-//            2 of 2,048 x 2,048     52, 55, 75       41, 45, 52       53, 63, 69
-//            16 of 1,024 x 1,024    53, 59, 92       42, 49, 59       38, 48, 57
-//            8 of 2,048 x 4,096     384, 165, 750    197, 124, 365    206, 135, 309
-// The last round of large tiles as quarters (16 of 2,048 x 4,096, 2.25 rounds) gains 1 %: the
-// matrix units' power, not their number, bounds these.
+// Tiles of 64, 128 or 256 rows and columns, by the rounds that they take of the workgroups that
+// run at once (512 of 64; 512 of 128, split 256; 256 of 256).  A round of 128 takes as long as
+// 1.5 to 1.9 of 64 (split S and Q up to 2, while there are few); from 2,048 of depth on one of
+// 256 as long as 1.6 to 2 of 128, split 3.4 (but for split S and Q, where they are no
+// faster: 8 of 2,048 x 4,096 494, 282 with 128, 592, 340 with 256).  us of S, Q and Q X with 64,
+// 128 and 256 (matrices of m x n; bf16's Q X the mean of its steps):
+//   float32  24 of 300 x 701        14, 11, 25       20, 17, 29       Q X 55
+//            8 of 512 x 512         11, 13, 13       16, 20, 18       62
+//            16 of 512 x 1,024      26, 20, 43       28, 22, 40       68
+//            4 of 1,024 x 1,024     29, 32, 40       28, 32, 32       92
+//            2 of 2,048 x 2,048     84, 87, 132      91, 98, 101      151
+//            16 of 1,024 x 1,024    84, 92, 154      82, 94, 121      124
+//            8 of 2,048 x 4,096     652, 311, 1,112  493, 266, 936    726
+//   bf16     24 of 300 x 701        10.1, 7.8, 17.6  12.6, 10.8, 16   25, 23, 31
+//            8 of 512 x 512         7.4, 8.4, 9.7    9.8, 11.4, 13    23, 29, 33
+//            16 of 512 x 1,024      20, 13.5, 28     16, 12.8, 20     33, 31, 36
+//            2 of 2,048 x 2,048     50, 52, 74       36, 40, 46       54, 63, 66
+//            16 of 1,024 x 1,024    44, 48, 83       33, 38, 53       39, 48, 56
+//            8 of 2,048 x 4,096     397, 156, 615    188, 99, 366     208, 133, 297
+//            16 of 2,048 x 4,096    -                330, 188, -      312, 202, 564
 template <int KIND, bool SPLIT, int RESTS>
 hipError_t step(const Planes &p, const Planes &q, const Planes &out, unsigned matrices, hipStream_t s)
 {
@@ -942,11 +1003,11 @@ hipError_t step(const Planes &p, const Planes &q, const Planes &out, unsigned ma
         const unsigned long long rows = (out.rows + size - 1) / size, cols = (out.cols + size - 1) / size;
         return matrices * (kDeep ? rows * (rows + 1) / 2 : rows * cols);
     };
-    const bool small = out.rows <= 64 || tiles(64) < (kDeep ? (SPLIT ? 3000 : 512) : 1000);
-    const unsigned long long at_once = SPLIT ? 256 : 512;
+    auto rounds = [&](unsigned size, unsigned at_once) { return (double)((tiles(size) + at_once - 1) / at_once); };
+    const double middle = rounds(128, SPLIT ? 256 : 512);
+    const bool small = out.rows <= 64 || rounds(64, 512) <= std::max(1.7 * middle, SPLIT && kDeep ? 2.0 : 0.0);
     if constexpr (!SPLIT || !kDeep) {
-        const double large = (SPLIT ? 3.4 : 1.65) * (double)((tiles(256) + 255) / 256);
-        if (!small && q.cols >= 512 && large <= (double)((tiles(128) + at_once - 1) / at_once))
+        if (!small && q.cols >= 2048 && (SPLIT ? 3.4 : 1.65) * rounds(256, 256) <= middle)
             return launch_step<Product<f16, 256, 256, 4, 2, kDeep, true, false, true>, KIND, SPLIT, RESTS>(p, q, out, matrices, s);
     }
     if constexpr (SPLIT)

@@ -856,10 +856,11 @@ __device__ __forceinline__ void write_result(T *to, u32x4 v, int left, bool past
 
 // 16 rows from row0 on of a wave's COLS results from column n0 on, below `last` and
 // `width`: lane 16 h + l has, of row l, columns 4 h + (0 .. 3) of each 16.  bf16 through
-// the wave's place in LDS (kPieceRow a row), for pieces of 16 bytes.
+// the wave's place in LDS (kPieceRow a row), for pieces of 16 bytes.  PAST: past the caches
+// where whole lines allow it.
 template <class T, int COLS>
 constexpr int kPieceRow = COLS * (int)sizeof(T) + 16;
-template <class T, int COLS, bool STAGE = sizeof(T) == 2>
+template <class T, int COLS, bool STAGE = sizeof(T) == 2, bool PAST = true>
 __device__ __forceinline__ void write_16_rows(const f32x4 (&v)[COLS / 16], char *mine, unsigned row0, unsigned last, int n0,
                                               int width, T *y, long long ys)
 {
@@ -875,7 +876,7 @@ __device__ __forceinline__ void write_16_rows(const f32x4 (&v)[COLS / 16], char 
         }
         return;
     }
-    const bool past = COLS * sizeof(T) >= 128 && past_caches(y, ys, width);
+    const bool past = PAST && COLS * sizeof(T) >= 128 && past_caches(y, ys, width);
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
     for (int i = 0; i < COLS / 16; ++i)
