@@ -96,7 +96,7 @@ __global__ __launch_bounds__(256) void lookup_kernel(const T *table, long long s
 // of its block and in earlier lanes, which are matched by ballots: stable.  A sample
 // without a row has the key `rows`, behind all others.  Up to kOneBlock samples one
 // workgroup takes all passes, its samples in registers and LDS (the gradient's us so and in
-// launches, rows of 48: 500 samples of 500 rows 20, 23; 8,192 of 500 23, 25; of 100,000 33, 40).
+// launches, rows of 48: 2,000 samples of 500 rows 21, 23; 8,192 of 500 22, 23; of 100,000 33, 38).
 // Bound by a launch's waits: 524,288 samples of 200,000 rows take two passes of 21 us.
 
 constexpr int kOneKeys = 8;
@@ -254,6 +254,49 @@ __global__ __launch_bounds__(kSortThreads) void digit_place_kernel(const int *id
     }
 }
 
+// Up to kRanked samples: a sample's place is the number of samples with smaller keys, or the
+// same one and before it, counted for 256 samples a workgroup against all of them in LDS, a
+// quarter of them by each of four threads.  Half as many where the digits are one pass.  The
+// gradient's us so and by digits, rows of 48: 500 samples of 500 rows 18.5, 20.5; 1,000 of 500 23,
+// 21, of 100,000 25, 29.
+constexpr unsigned kRanked = 1024;
+__global__ __launch_bounds__(1024) void rank_kernel(const int *ids, unsigned samples, unsigned rows, unsigned *out_keys,
+                                                    unsigned *out_values)
+{
+    __shared__ u32x4 keys[kRanked / 4];
+    __shared__ unsigned parts[3][256];
+    unsigned *const key_of_sample = reinterpret_cast<unsigned *>(keys);
+    const unsigned fours = (samples + 255) / 256 * 64, own = blockIdx.x * 64;
+    if (threadIdx.x < fours * 4)
+        key_of_sample[threadIdx.x] = threadIdx.x < samples ? key_of(ids[threadIdx.x], rows) : 0xFFFFFFFFu;  // behind all
+    __syncthreads();
+    const unsigned t = threadIdx.x & 255, quarter = threadIdx.x >> 8, i = own * 4 + t, mine = key_of_sample[i];
+    const unsigned from = quarter * (fours / 4), to = from + fours / 4;
+    unsigned place = 0;
+    auto between = [&](unsigned a, unsigned b, auto &&counts) {
+        a = a > from ? a : from;
+        b = b < to ? b : to;
+#pragma unroll 8
+        for (unsigned j = a; j < b; ++j) {
+            const u32x4 k = keys[j];
+#pragma unroll
+            for (unsigned e = 0; e < 4; ++e)
+                place += counts(k[e], j * 4 + e);
+        }
+    };
+    between(0, own, [&](unsigned k, unsigned) { return (unsigned)(k <= mine); });
+    between(own, own + 64, [&](unsigned k, unsigned at) { return (unsigned)(k < mine) | ((unsigned)(k == mine) & (unsigned)(at < i)); });
+    between(own + 64, fours, [&](unsigned k, unsigned) { return (unsigned)(k < mine); });
+    if (quarter)
+        parts[quarter - 1][t] = place;
+    __syncthreads();
+    if (quarter == 0 && i < samples) {
+        place += parts[0][t] + parts[1][t] + parts[2][t];
+        out_keys[place] = mine;
+        out_values[place] = i;
+    }
+}
+
 static_assert(kOneThreads == 1 << kMostBits, "a thread a digit");
 // All passes of up to kOneBlock samples.
 __global__ __launch_bounds__(kOneThreads) void sort_one_kernel(const int *ids, unsigned samples, unsigned rows, int key_bits, int bits,
@@ -341,17 +384,18 @@ struct Ends {
     unsigned trail, lead_goes_on;
 };
 
-// Zeros for the rows that no sample has: a wave takes 64 rows, looks each up in the
-// sorted keys, and writes the absent ones.
+// Zeros for the rows that no sample has: a wave takes rows_each of up to 64, looks each up in
+// the sorted keys, and writes the absent ones.
 template <bool PAST>
-__device__ __forceinline__ void absent_rows(unsigned block, const unsigned *keys, unsigned samples, unsigned rows, int D, float *out)
+__device__ __forceinline__ void absent_rows(unsigned block, const unsigned *keys, unsigned samples, unsigned rows, int D, float *out,
+                                            int rows_each)
 {
     const int lane = threadIdx.x & 63;
-    const unsigned long long v0 = ((unsigned long long)block * 4 + (threadIdx.x >> 6)) * 64;
+    const unsigned long long v0 = ((unsigned long long)block * 4 + (threadIdx.x >> 6)) * rows_each;
     if (v0 >= rows)
         return;
-    const unsigned long long v = v0 + lane;
-    unsigned lo = 0, hi = samples;  // the first key that is not below v
+    const unsigned long long v = lane < rows_each ? v0 + lane : rows;
+    unsigned lo = 0, hi = v < rows ? samples : 0;  // the first key that is not below v
     while (lo < hi) {
         const unsigned mid = lo + (hi - lo) / 2;
         if (keys[mid] < v)
@@ -361,15 +405,15 @@ __device__ __forceinline__ void absent_rows(unsigned block, const unsigned *keys
     }
     const bool absent = v < rows && !(lo < samples && keys[lo] == v);
     unsigned long long todo = __ballot(absent);
-    if (D <= 64) {  // short rows: all 64 of them side by side
+    if (D <= 64) {  // short rows: all of them side by side
         float *first = out + (size_t)v0 * D;
         if (D % 4 == 0) {
             const int vecs = D / 4;
-            for (int i = lane; i < 64 * vecs; i += 64)
+            for (int i = lane; i < rows_each * vecs; i += 64)
                 if (todo >> (i / vecs) & 1)
                     *reinterpret_cast<Any16 *>(first + i * 4) = u32x4{0, 0, 0, 0};
         } else {
-            for (int i = lane; i < 64 * D; i += 64)
+            for (int i = lane; i < rows_each * D; i += 64)
                 if (todo >> (i / D) & 1)
                     first[i] = 0.0f;
         }
@@ -411,7 +455,7 @@ __device__ __forceinline__ void write_sum(float *to, const float (&sum)[V], floa
 template <class T, int V, bool PAST>
 __global__ __launch_bounds__(256) void sum_kernel(const unsigned *keys, const unsigned *values, const T *from, long long stride,
                                                   unsigned samples, unsigned rows, int D, float scale, float *out, Ends *ends,
-                                                  float *leads, float *trails, int group_log2, unsigned sum_blocks)
+                                                  float *leads, float *trails, int group_log2, unsigned sum_blocks, int rows_each)
 {
     constexpr int kAhead = 8;
     constexpr unsigned kMostEntries = (256u >> kLeastLanes) * kPiece;
@@ -419,7 +463,7 @@ __global__ __launch_bounds__(256) void sum_kernel(const unsigned *keys, const un
     __shared__ unsigned row_of_entry[kMostEntries];
     if (blockIdx.x >= sum_blocks) {
         if (blockIdx.y == 0)
-            absent_rows<PAST>(blockIdx.x - sum_blocks, keys, samples, rows, D, out);
+            absent_rows<PAST>(blockIdx.x - sum_blocks, keys, samples, rows, D, out, rows_each);
         return;
     }
     const unsigned entries = (256u >> group_log2) * kPiece, first = blockIdx.x * entries;
@@ -483,20 +527,21 @@ __global__ __launch_bounds__(256) void sum_kernel(const unsigned *keys, const un
         ends[piece] = mine;
 }
 
-// A group takes a piece, and the run that began in it and goes on: alone where it ends
-// within as many pieces as the group has lanes, else the whole workgroup, whose groups
-// take the parts in turn.
+// A wave takes a piece, and the run that began in it and goes on: alone where it ends within
+// 64 more pieces, else the whole workgroup.  2^row_log2 lanes have a row, or 64 of its vectors,
+// and the lanes that are left share the run's parts.  262,144 samples of 1,000 rows of 48 6 us,
+// a million of 3 rows of 8 19.
 template <int V>
-__global__ __launch_bounds__(256) void join_kernel(const Ends *ends, const float *leads, const float *trails, unsigned pieces, int D,
-                                                   float scale, float *out, int group_log2)
+__global__ __launch_bounds__(256) void join_kernel(const unsigned *keys, unsigned samples, const Ends *ends, const float *leads,
+                                                   const float *trails, unsigned pieces, int D, float scale, float *out,
+                                                   int row_log2)
 {
     constexpr int kAhead = 8;
-    __shared__ unsigned char long_runs[256];
-    __shared__ float sums[256][V];
-    __shared__ unsigned last;
-    const unsigned lanes = 1u << group_log2, groups = 256u >> group_log2;
-    const unsigned group = threadIdx.x >> group_log2, lane = threadIdx.x & (lanes - 1), first = blockIdx.x * groups;
-    const int c = (int)(blockIdx.y * lanes + lane), vecs = (D + V - 1) / V;
+    __shared__ unsigned char long_runs[4];
+    __shared__ float sums[3][64][V];
+    const unsigned of_row = 1u << row_log2, subs = 64u >> row_log2;
+    const unsigned wave = threadIdx.x >> 6, lane = threadIdx.x & 63, sub = lane >> row_log2, first = blockIdx.x * 4;
+    const int c = (int)(blockIdx.y * of_row + (lane & (of_row - 1))), vecs = (D + V - 1) / V;
     const bool in = c < vecs;
     const int e = V > 1 ? vec_at<V>(in ? c : 0, D) : (in ? c : 0);
     // parts 0, 1, ...: the trail of a piece, the lead of the next, and so on; those from `from`
@@ -516,48 +561,54 @@ __global__ __launch_bounds__(256) void join_kernel(const Ends *ends, const float
                     add<V>(sum, x[j]);
         }
     };
-    const unsigned piece = first + group;
+    auto join_subs = [&](float(&sum)[V]) {
+        for (unsigned off = of_row; off < 64; off <<= 1)
+#pragma unroll
+            for (int k = 0; k < V; ++k)
+                sum[k] += __shfl_xor(sum[k], off);
+    };
+    const unsigned piece = first + wave;
     const unsigned key = piece < pieces ? ends[piece].trail : kNone;
     const bool ends_here = key != kNone && (piece + 1 + lane >= pieces || !ends[piece + 1 + lane].lead_goes_on);
     const unsigned long long all = __ballot(ends_here);
-    const unsigned long long of_group = (all >> (threadIdx.x & 63 & ~(lanes - 1))) & (lanes == 64 ? ~0ull : (1ull << lanes) - 1);
-    if (key != kNone && of_group) {
+    if (all) {
         float sum[V] = {};
-        sum_of(piece, 0, 1, (unsigned)__builtin_ctzll(of_group) + 2, sum);
-        if (in)
+        sum_of(piece, sub, subs, (unsigned)__builtin_ctzll(all) + 2, sum);
+        join_subs(sum);
+        if (in && sub == 0)
             write_sum<V, false>(out + (size_t)key * D + e, sum, scale);
     }
     if (lane == 0)
-        long_runs[group] = key != kNone && !of_group;
+        long_runs[wave] = key != kNone && !all;
     __syncthreads();
-    for (unsigned g = 0; g < groups; ++g) {
-        if (!long_runs[g])
+    for (unsigned w = 0; w < 4; ++w) {
+        if (!long_runs[w])
             continue;
-        const unsigned from = first + g;
-        if (threadIdx.x == 0)
-            last = kNone;
-        __syncthreads();
-        for (unsigned at = from + 1; at < pieces && last == kNone; at += 256) {  // where its last lead is
-            const unsigned i = at + threadIdx.x;
-            const bool is_last = i < pieces && !ends[i].lead_goes_on;
-            __syncthreads();  // all have seen last
-            if (is_last)
-                atomicMin(&last, i);
-            __syncthreads();
+        const unsigned from = first + w;
+        // its last sample: keys[lo] is its key, keys[hi] is not
+        const unsigned run = ends[from].trail;
+        unsigned lo = (from + 1) * kPiece, hi = samples;
+        while (hi - lo > 1) {
+            const unsigned step = (hi - lo + 255) / 256, at = (threadIdx.x + 1) * step;
+            const unsigned below = __syncthreads_count(at < hi - lo && keys[lo + at] == run);
+            lo += below * step;
+            hi = hi - lo < step ? hi : lo + step;
         }
         float sum[V] = {};
-        sum_of(from, group, groups, (last < pieces ? last : pieces - 1) - from + 1, sum);
+        sum_of(from, wave * subs + sub, 4 * subs, lo / kPiece - from + 1, sum);
+        join_subs(sum);
+        if (wave)
 #pragma unroll
-        for (int k = 0; k < V; ++k)
-            sums[threadIdx.x][k] = sum[k];
+            for (int k = 0; k < V; ++k)
+                sums[wave - 1][lane][k] = sum[k];
         __syncthreads();
-        if (group == 0) {
-            for (unsigned i = 1; i < groups; ++i)
+        if (wave == 0) {
+            for (unsigned i = 0; i < 3; ++i)
 #pragma unroll
                 for (int k = 0; k < V; ++k)
-                    sum[k] += sums[i * lanes + lane][k];
-            if (in)
-                write_sum<V, false>(out + (size_t)ends[from].trail * D + e, sum, scale);
+                    sum[k] += sums[i][lane][k];
+            if (in && sub == 0)
+                write_sum<V, false>(out + (size_t)run * D + e, sum, scale);
         }
         __syncthreads();
     }
@@ -565,7 +616,7 @@ __global__ __launch_bounds__(256) void join_kernel(const Ends *ends, const float
 
 // Few samples in one launch: a workgroup takes some rows, notes the samples that are
 // theirs, in order, and sums them row by row, a group of lanes each.  us so and sorted, rows
-// of 48: 64 samples of 500 rows 8, 19; 256 of 500 16, 20, of 20,000 7, 24.
+// of 48: 64 samples of 500 rows 8, 15; 256 of 500 15.7, 15.8, of 20,000 7, 16.
 constexpr unsigned kFewSamples = 256;
 template <class T, int V>
 __global__ __launch_bounds__(256) void few_kernel(const int *ids, const T *from, long long stride, unsigned samples, unsigned rows, int D,
@@ -730,17 +781,22 @@ hipError_t sums(const unsigned *keys, const unsigned *values, Rows dout, unsigne
 {
     const int vecs = (dim + V - 1) / V, least = group_log2(vecs), g = least < kLeastLanes ? kLeastLanes : least;
     const unsigned pieces = blocks_of(samples, kPiece), blocks = blocks_of(pieces, 256 >> g);
-    sum_kernel<T, V, PAST><<<dim3(blocks + blocks_of(rows, 256), blocks_of(vecs, 1 << g)), 256, 0, s>>>(
-        keys, values, static_cast<const T *>(dout.p), dout.stride, samples, rows, dim, scale, out, ends, leads, trails, g, blocks);
+    int rows_each = 64;  // of a wave that writes absent rows, fewer where there are few waves
+    while (rows_each > 4 && rows / rows_each < 2048)
+        rows_each /= 2;
+    sum_kernel<T, V, PAST><<<dim3(blocks + blocks_of(rows, 4 * rows_each), blocks_of(vecs, 1 << g)), 256, 0, s>>>(
+        keys, values, static_cast<const T *>(dout.p), dout.stride, samples, rows, dim, scale, out, ends, leads, trails, g, blocks,
+        rows_each);
     return hipGetLastError();
 }
 
 template <int V>
-hipError_t join(const Ends *ends, const float *leads, const float *trails, unsigned pieces, int dim, float scale, float *out, hipStream_t s)
+hipError_t join(const unsigned *keys, unsigned samples, const Ends *ends, const float *leads, const float *trails, unsigned pieces,
+                int dim, float scale, float *out, hipStream_t s)
 {
-    const int vecs = (dim + V - 1) / V, least = group_log2(vecs), g = least < kLeastLanes ? kLeastLanes : least;
-    join_kernel<V><<<dim3(blocks_of(pieces, 256 >> g), blocks_of(vecs, 1 << g)), 256, 0, s>>>(ends, leads, trails, pieces, dim, scale, out,
-                                                                                         g);
+    const int vecs = (dim + V - 1) / V, g = group_log2(vecs);
+    join_kernel<V><<<dim3(blocks_of(pieces, 4), blocks_of(vecs, 1 << g)), 256, 0, s>>>(keys, samples, ends, leads, trails, pieces, dim, scale,
+                                                                                               out, g);
     return hipGetLastError();
 }
 
@@ -783,7 +839,10 @@ hipError_t backward(Rows dout, const int *ids, unsigned samples, unsigned rows, 
         now ^= 1;  // the last one written
         e = hipGetLastError();
     } else {
-        sort_one_kernel<<<1, kOneThreads, 0, s>>>(ids, samples, rows, d.key_bits, d.bits, keys[0], values[0]);
+        if (samples <= kRanked && (samples <= kRanked / 2 || d.passes > 1))
+            rank_kernel<<<blocks_of(samples, 256), 1024, 0, s>>>(ids, samples, rows, keys[0], values[0]);
+        else
+            sort_one_kernel<<<1, kOneThreads, 0, s>>>(ids, samples, rows, d.key_bits, d.bits, keys[0], values[0]);
         e = hipGetLastError();
     }
     if (e != hipSuccess)
@@ -805,7 +864,8 @@ hipError_t backward(Rows dout, const int *ids, unsigned samples, unsigned rows, 
     const unsigned pieces = blocks_of(samples, kPiece);
     if (e != hipSuccess || pieces == 1)
         return e;
-    return dim < 4 ? join<1>(ends, leads, trails, pieces, dim, scale, out, s) : join<4>(ends, leads, trails, pieces, dim, scale, out, s);
+    return dim < 4 ? join<1>(k, samples, ends, leads, trails, pieces, dim, scale, out, s)
+                   : join<4>(k, samples, ends, leads, trails, pieces, dim, scale, out, s);
 }
 
 }  // namespace

@@ -23,7 +23,8 @@ CASES = [  # samples, rows, dim, pad, shift, how ids are drawn
     (12000, 2000, 2050, 0, 0, "masked"), (200000, 17, 20, 0, 0, "one"), (65536, 40, 256, 0, 0, "sorted"), (256, 9, 734, 0, 0, "skewed"), (257, 9, 734, 0, 0, "skewed"),
     (200, 100000, 64, 0, 0, "masked"), (1500, 20000, 360, 0, 0, "masked"), (300000, 2, 130, 0, 0, "masked"), (5000, 4, 33, 1, 1, "one"),
     (70000, 3000, 8, 0, 0, "sorted"), (600000, 700, 3, 0, 0, "skewed"), (9000, (1 << 21) + 5, 3, 0, 0, "even"),
-    (280001, 5000, 512, 0, 0, "masked")]
+    (280001, 5000, 512, 0, 0, "masked"), (512, 9, 33, 0, 0, "masked"), (513, 1024, 850, 1, 0, "skewed"), (1024, 70000, 8, 0, 0, "masked"),
+    (1024, 1, 3, 0, 0, "even"), (400, 3000, 1, 0, 0, "one"), (1024, 40000, 70, 0, 0, "one"), (900000, 2, 4, 0, 0, "skewed")]
 
 
 def ids_of(g, T, V, how):
