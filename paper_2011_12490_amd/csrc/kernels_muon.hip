@@ -720,12 +720,106 @@ __device__ __forceinline__ void write_lds(char *plane, int r, int c, f32x4 v)
     *reinterpret_cast<f16x4 *>(plane + C::kX + at) = __builtin_convertvector(v - __builtin_convertvector(hi, f32x4), f16x4);
 }
 
+// The products, a wave's part of each: rows from 16 fq on, results from wp FS or wp FX on.
+template <class C>
+struct Part {
+    const int lane = threadIdx.x & 63, wave = uniform(threadIdx.x >> 6);
+    const int wp = wave % C::WP, fq = wave / C::WP * C::FQ;
+    const int row = fq * 16 + (lane & 15);  // of the wave's first results; the next 16 on
+};
+template <class C>
+__device__ __forceinline__ auto s_rows(const char *sq, int first)
+{
+    return [=](int plane, int i, int part) {
+        using S = typename C::S;
+        const int f = first + i;
+        return S::row_fragment(sq + plane * C::kS + (f >> 2) * S::kBytes, f & 3, part);
+    };
+}
+// S's sums: X X^T is added.
+template <class C, bool SPLIT>
+__device__ __forceinline__ void small_gram(const char *x, f32x4 (&acc)[C::FS][C::FQ], f32x4 (&rest)[C::FS][C::FQ])
+{
+    const Part<C> my;
+    auto x_rows = [&](int first) {
+        return [=](int plane, int i, int part) {
+            using X = typename C::X;
+            constexpr int kParts = C::kBlock / 32;  // of a block
+            const int f = first + i;
+            return X::row_fragment(x + plane * C::kX + part / kParts * C::kXBlock + (f >> 2) * X::kBytes, f & 3, part % kParts);
+        };
+    };
+    small_product<C::FS, C::FQ, SPLIT, C::N>(acc, rest, x_rows(my.wp * C::FS), x_rows(my.fq));
+}
+// Sums times `times` to S's (or Q's) place.
+template <class C, bool SPLIT>
+__device__ __forceinline__ void write_small(char *sq, const f32x4 (&acc)[C::FS][C::FQ], float times)
+{
+    const Part<C> my;
+#pragma unroll
+    for (int i = 0; i < C::FS; i += 2)
+#pragma unroll
+        for (int j = 0; j < C::FQ; ++j)
+            write_pair<typename C::S, SPLIT>(sq, C::kS, my.row + j * 16, my.wp * C::FS + i, acc[i][j] * times, acc[i + 1][j] * times);
+}
+// S becomes Q.
+template <class C, bool SPLIT>
+__device__ __forceinline__ void small_square(char *sq)
+{
+    const Part<C> my;
+    f32x4 acc[C::FS][C::FQ] = {}, rest[C::FS][C::FQ] = {};
+    small_product<C::FS, C::FQ, SPLIT, C::M>(acc, rest, s_rows<C>(sq, my.wp * C::FS), s_rows<C>(sq, my.fq));
+    add_rest<C::FS, C::FQ, SPLIT>(acc, rest);
+#pragma unroll
+    for (int i = 0; i < C::FS; i += 2)
+#pragma unroll
+        for (int j = 0; j < C::FQ; ++j) {
+            f32x4 a, b;
+            read_pair<typename C::S, SPLIT>(sq, C::kS, my.row + j * 16, my.wp * C::FS + i, a, b);
+            acc[i][j] = acc[i][j] * (kC / kUnit) + a * kB;
+            acc[i + 1][j] = acc[i + 1][j] * (kC / kUnit) + b * kB;
+        }
+    __syncthreads();
+    write_small<C, SPLIT>(sq, acc, 1.0f);
+}
+// X becomes a X + Q X.
+template <class C, bool SPLIT>
+__device__ __forceinline__ void small_apply(char *x, const char *sq)
+{
+    using X = typename C::X;
+    constexpr int FX = C::FX, FQ = C::FQ, kOfBlock = C::kBlock / 16;
+    const Part<C> my;
+    f32x4 acc[FX][FQ] = {}, more[FX][FQ] = {};
+    auto &rest = FX * FQ > 8 ? acc : more;  // two parts of depth only, and no registers for more
+    auto x_columns = [&](int plane, int i, int part) {
+        const int f = my.wp * FX + i;
+        return X::fragment(x + plane * C::kX + f / kOfBlock * C::kXBlock + (part >> 1) * X::kBytes, f % kOfBlock, part & 1);
+    };
+    small_product<FX, FQ, SPLIT, C::M>(acc, rest, x_columns, s_rows<C>(sq, my.fq));
+    add_rest<FX, FQ, SPLIT && FX * FQ <= 8>(acc, rest);
+#pragma unroll
+    for (int i = 0; i < FX; i += 2)
+#pragma unroll
+        for (int j = 0; j < FQ; ++j) {
+            f32x4 a, b;
+            const int f = my.wp * FX + i;
+            read_pair<X, true>(x + f / kOfBlock * C::kXBlock, C::kX, my.row + j * 16, f % kOfBlock, a, b);
+            acc[i][j] = acc[i][j] * (1.0f / kUnit) + a * kA;
+            acc[i + 1][j] = acc[i + 1][j] * (1.0f / kUnit) + b * kA;
+        }
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < FX; i += 2)
+#pragma unroll
+        for (int j = 0; j < FQ; ++j) {
+            const int f = my.wp * FX + i;
+            write_pair<X, true>(x + f / kOfBlock * C::kXBlock, C::kX, my.row + j * 16, f % kOfBlock, acc[i][j], acc[i + 1][j]);
+        }
+}
+
 template <class C, bool SPLIT>
 __global__ __launch_bounds__(C::kThreads, C::kAtOnce *C::kThreads / 256) void small_kernel(const MuonSet set, MuonStep st)
 {
-    using X = typename C::X;
-    using S = typename C::S;
-    constexpr int FQ = C::FQ, FS = C::FS, FX = C::FX;
     __shared__ __attribute__((aligned(16))) char lds[C::kLds];
     __shared__ double sums[C::kThreads / 64];
     char *const x = lds, *const sq = lds + 2 * C::kX;
@@ -795,84 +889,18 @@ __global__ __launch_bounds__(C::kThreads, C::kAtOnce *C::kThreads / 256) void sm
         }
     }
     __syncthreads();
-    const int wp = wave % C::WP, fq = wave / C::WP * FQ;
-    const int row = fq * 16 + (lane & 15);  // of the wave's first results; the next 16 on
-    auto x_rows = [&](int first) {
-        return [=](int plane, int i, int part) {
-            constexpr int kParts = C::kBlock / 32;  // of a block
-            const int f = first + i;
-            return X::row_fragment(x + plane * C::kX + part / kParts * C::kXBlock + (f >> 2) * X::kBytes, f & 3, part % kParts);
-        };
-    };
-    auto s_rows = [&](int first) {
-        return [=](int plane, int i, int part) {
-            const int f = first + i;
-            return S::row_fragment(sq + plane * C::kS + (f >> 2) * S::kBytes, f & 3, part);
-        };
-    };
 #pragma unroll 1
     for (int n = 0; n < st.iterations; ++n) {
         {
-            f32x4 acc[FS][FQ] = {}, rest[FS][FQ] = {};
-            small_product<FS, FQ, SPLIT, C::N>(acc, rest, x_rows(wp * FS), x_rows(fq));
-            add_rest<FS, FQ, SPLIT>(acc, rest);
-#pragma unroll
-            for (int i = 0; i < FS; i += 2)
-#pragma unroll
-                for (int j = 0; j < FQ; ++j)
-                    write_pair<S, SPLIT>(sq, C::kS, row + j * 16, wp * FS + i, acc[i][j] * (1.0f / kUnit), acc[i + 1][j] * (1.0f / kUnit));
+            f32x4 acc[C::FS][C::FQ] = {}, rest[C::FS][C::FQ] = {};
+            small_gram<C, SPLIT>(x, acc, rest);
+            add_rest<C::FS, C::FQ, SPLIT>(acc, rest);
+            write_small<C, SPLIT>(sq, acc, 1.0f / kUnit);
         }
         __syncthreads();
-        {
-            f32x4 acc[FS][FQ] = {}, rest[FS][FQ] = {};
-            small_product<FS, FQ, SPLIT, C::M>(acc, rest, s_rows(wp * FS), s_rows(fq));
-            add_rest<FS, FQ, SPLIT>(acc, rest);
-#pragma unroll
-            for (int i = 0; i < FS; i += 2)
-#pragma unroll
-                for (int j = 0; j < FQ; ++j) {
-                    f32x4 a, b;
-                    read_pair<S, SPLIT>(sq, C::kS, row + j * 16, wp * FS + i, a, b);
-                    acc[i][j] = acc[i][j] * (kC / kUnit) + a * kB;
-                    acc[i + 1][j] = acc[i + 1][j] * (kC / kUnit) + b * kB;
-                }
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < FS; i += 2)
-#pragma unroll
-                for (int j = 0; j < FQ; ++j)
-                    write_pair<S, SPLIT>(sq, C::kS, row + j * 16, wp * FS + i, acc[i][j], acc[i + 1][j]);
-        }
+        small_square<C, SPLIT>(sq);
         __syncthreads();
-        {
-            f32x4 acc[FX][FQ] = {}, more[FX][FQ] = {};
-            auto &rest = FX * FQ > 8 ? acc : more;  // two parts of depth only, and no registers for more
-            auto x_columns = [&](int plane, int i, int part) {
-                constexpr int kOfBlock = C::kBlock / 16;
-                const int f = wp * FX + i;
-                return X::fragment(x + plane * C::kX + f / kOfBlock * C::kXBlock + (part >> 1) * X::kBytes, f % kOfBlock, part & 1);
-            };
-            small_product<FX, FQ, SPLIT, C::M>(acc, rest, x_columns, s_rows(fq));
-            add_rest<FX, FQ, SPLIT && FX * FQ <= 8>(acc, rest);
-#pragma unroll
-            for (int i = 0; i < FX; i += 2)
-#pragma unroll
-                for (int j = 0; j < FQ; ++j) {
-                    f32x4 a, b;
-                    const int f = wp * FX + i, block = f / (C::kBlock / 16);
-                    read_pair<X, true>(x + block * C::kXBlock, C::kX, row + j * 16, f % (C::kBlock / 16), a, b);
-                    acc[i][j] = acc[i][j] * (1.0f / kUnit) + a * kA;
-                    acc[i + 1][j] = acc[i + 1][j] * (1.0f / kUnit) + b * kA;
-                }
-            __syncthreads();
-#pragma unroll
-            for (int i = 0; i < FX; i += 2)
-#pragma unroll
-                for (int j = 0; j < FQ; ++j) {
-                    const int f = wp * FX + i, block = f / (C::kBlock / 16);
-                    write_pair<X, true>(x + block * C::kXBlock, C::kX, row + j * 16, f % (C::kBlock / 16), acc[i][j], acc[i + 1][j]);
-                }
-        }
+        small_apply<C, SPLIT>(x, sq);
         __syncthreads();
     }
     const float rate = st.rate * t.size;
@@ -899,6 +927,104 @@ __global__ __launch_bounds__(C::kThreads, C::kAtOnce *C::kThreads / 256) void sm
         if (t.copy)
             write4(t.copy, true, at, v, here);
     }
+}
+
+// ---- matrices of up to 128 rows that do not fit -------------------------------------------
+
+// A step in two launches: this one takes columns of X, `per` pieces of 128 of them a
+// workgroup, through Q X and the next S's part of those columns, as small_kernel does;
+// sum_parts_kernel sums the parts.  S is the same for all of a matrix's workgroups, each of
+// which squares it for itself.  apply: there is an S; gram: there is a next step.  Bound by a
+// launch's chain of waits (S, its square, Q X, the next S, about 8 us); a call's us so and by the
+// products of large matrices, float32 and bf16: 22 of 11 x 1,924 95, 182 and 87, 145; 51 of 123 x
+// 1,545 245, 299 and 203, 235; 70 of 96 x 200 128, 136 and 108, 118; 16 of 128 x 16,384 516, 1,252 and
+// 410, 1,030; 1,000 of 64 x 600 556, 979 and 454, 655.
+template <class C, bool SPLIT>
+__global__ __launch_bounds__(C::kThreads, C::kAtOnce *C::kThreads / 256) void columns_kernel(Planes xm, const f16 *s, float *parts,
+                                                                                              unsigned per, bool apply, bool gram)
+{
+    constexpr int M = C::M;
+    static_assert(C::N == 128 && C::kBlock == 128, "a piece");
+    __shared__ __attribute__((aligned(16))) char lds[C::kLds];
+    char *const x = lds, *const sq = lds + 2 * C::kX;
+    const size_t plane = (size_t)xm.rows * xm.cols;
+    f16 *const from = xm.p + blockIdx.y * xm.matrix;
+    const unsigned pieces = (xm.cols + 127) / 128, first = blockIdx.x * per, last = first + per < pieces ? first + per : pieces;
+    if (apply) {
+        const f16 *mine = s + blockIdx.y * (size_t)(M * M * C::kPlanes);
+        for (int i = threadIdx.x; i < C::kPlanes * M * M / 8; i += C::kThreads) {
+            const int r = i / (M / 8) % M, c = i % (M / 8);
+            using S = typename C::S;
+            *reinterpret_cast<u32x4 *>(sq + i / (M * M / 8) * C::kS + (r >> 6) * S::kBytes + S::at(r & 63, c)) =
+                *reinterpret_cast<const u32x4 *>(mine + (size_t)i * 8);
+        }
+    }
+    // 16 bytes of both planes: in LDS, and in memory, where the columns are X's
+    auto each = [&](unsigned piece, auto &&what) {
+#pragma unroll
+        for (int i = threadIdx.x; i < 2 * M * 16; i += C::kThreads) {
+            const int r = i / 16 % M, c = i % 16, low = i / (M * 16);
+            using X = typename C::X;
+            const unsigned col = piece * 128 + c * 8;
+            what(x + low * C::kX + (r >> 6) * X::kBytes + X::at(r & 63, c), from + low * plane + ((size_t)r * xm.cols + col), col < xm.cols);
+        }
+    };
+    auto load = [&](char *to, const f16 *at, bool there) {
+        *reinterpret_cast<u32x4 *>(to) = there ? *reinterpret_cast<const u32x4 *>(at) : u32x4{};
+    };
+    f32x4 acc[C::FS][C::FQ] = {}, rest[C::FS][C::FQ] = {};
+    each(first, load);
+    __syncthreads();
+    if (apply) {
+        small_square<C, SPLIT>(sq);
+        __syncthreads();
+    }
+#pragma unroll 1
+    for (unsigned piece = first; piece < last; ++piece) {
+        if (piece != first) {
+            __syncthreads();
+            each(piece, load);
+            __syncthreads();
+        }
+        if (apply) {
+            small_apply<C, SPLIT>(x, sq);
+            __syncthreads();
+            each(piece, [&](const char *value, f16 *to, bool there) {
+                if (there)
+                    *reinterpret_cast<u32x4 *>(to) = *reinterpret_cast<const u32x4 *>(value);
+            });
+        }
+        if (gram)
+            small_gram<C, SPLIT>(x, acc, rest);
+    }
+    if (!gram)
+        return;
+    add_rest<C::FS, C::FQ, SPLIT>(acc, rest);
+    const Part<C> my;
+    float *to = parts + ((size_t)blockIdx.y * gridDim.x + blockIdx.x) * (M * M);
+#pragma unroll
+    for (int i = 0; i < C::FS; ++i)
+#pragma unroll
+        for (int j = 0; j < C::FQ; ++j)
+            *reinterpret_cast<f32x4 *>(to + (my.row + j * 16) * M + (my.wp * C::FS + i) * 16 + (my.lane >> 4) * 4) = acc[i][j];
+}
+
+// S of each matrix from its parts, four values a thread.
+template <bool SPLIT>
+__global__ __launch_bounds__(256) void sum_parts_kernel(const float *parts, unsigned count, unsigned size, f16 *s)
+{
+    const unsigned i = (blockIdx.x * 256 + threadIdx.x) * 4;
+    const float *from = parts + (size_t)blockIdx.y * count * size + i;
+    f32x4 sum = {};
+#pragma unroll 8
+    for (unsigned n = 0; n < count; ++n)
+        sum += *reinterpret_cast<const f32x4 *>(from + (size_t)n * size);
+    sum *= 1.0f / kUnit;
+    f16 *to = s + (size_t)blockIdx.y * size * (SPLIT ? 2 : 1) + i;
+    const f16x4 hi = __builtin_convertvector(sum, f16x4);
+    *reinterpret_cast<f16x4 *>(to) = hi;
+    if (SPLIT)
+        *reinterpret_cast<f16x4 *>(to + size) = __builtin_convertvector(sum - __builtin_convertvector(hi, f32x4), f16x4);
 }
 
 // ---- launches --------------------------------------------------------------------------
@@ -1005,7 +1131,7 @@ hipError_t step(const Planes &p, const Planes &q, const Planes &out, unsigned ma
     };
     auto rounds = [&](unsigned size, unsigned at_once) { return (double)((tiles(size) + at_once - 1) / at_once); };
     const double middle = rounds(128, SPLIT ? 256 : 512);
-    const bool small = out.rows <= 64 || rounds(64, 512) <= std::max(1.7 * middle, SPLIT && kDeep ? 2.0 : 0.0);
+    const bool small = rounds(64, 512) <= std::max(1.7 * middle, SPLIT && kDeep ? 2.0 : 0.0);
     if constexpr (!SPLIT || !kDeep) {
         if (!small && q.cols >= 2048 && (SPLIT ? 3.4 : 1.65) * rounds(256, 256) <= middle)
             return launch_step<Product<f16, 256, 256, 4, 2, kDeep, true, false, true>, KIND, SPLIT, RESTS>(p, q, out, matrices, s);
@@ -1033,6 +1159,36 @@ hipError_t small(const MuonSet &set, unsigned matrices, const Sizes &z, const Mu
     return z.n > 64 ? launch_small<64, 128, SPLIT>(set, matrices, st, s) : launch_small<64, 64, SPLIT>(set, matrices, st, s);
 }
 
+// Matrices of up to 128 rows that do not fit: pieces of 128 columns, and how many a workgroup
+// takes so that as many run as at once can: 512, or 256 of 128 rows (51 of 123 x 1,545 245 us, 297
+// with 512).
+bool is_long(const Sizes &z) { return z.m <= 128 && !is_small(z); }
+struct Pieces {
+    unsigned per, parts;
+};
+Pieces pieces_of(const Sizes &z, unsigned matrices)
+{
+    const unsigned pieces = (z.n + 127) / 128, want = matrices ? (z.m == 64 ? 512 : 256) / matrices : 1, parts = want < 1 ? 1 : want < pieces ? want : pieces;
+    const unsigned per = (pieces + parts - 1) / parts;
+    return {per, (pieces + per - 1) / per};
+}
+size_t parts_bytes(const Sizes &z, unsigned matrices)
+{
+    return whole((size_t)matrices * pieces_of(z, matrices).parts * z.m * z.m * sizeof(float));
+}
+template <int M, bool SPLIT>
+hipError_t columns(const Planes &x, unsigned matrices, const Sizes &z, int iterations, f16 *gram, float *parts, hipStream_t s)
+{
+    using C = Small<M, 128, SPLIT>;
+    const Pieces p = pieces_of(z, matrices);
+    for (int i = 0; i <= iterations; ++i) {
+        columns_kernel<C, SPLIT><<<dim3(p.parts, matrices), C::kThreads, 0, s>>>(x, gram, parts, p.per, i > 0, i < iterations);
+        if (i < iterations)
+            sum_parts_kernel<SPLIT><<<dim3(M * M / 1024, matrices), 256, 0, s>>>(parts, p.parts, M * M, gram);
+    }
+    return hipGetLastError();
+}
+
 template <bool SPLIT>
 hipError_t orthogonalise(const MuonSet &set, unsigned matrices, const Sizes &z, const MuonStep &st, char *ws,
                          hipStream_t s)
@@ -1046,7 +1202,23 @@ hipError_t orthogonalise(const MuonSet &set, unsigned matrices, const Sizes &z, 
     auto planes = [&](size_t bytes, unsigned rows, unsigned cols) {
         return Planes{reinterpret_cast<f16 *>(take(bytes)), (long long)(bytes / sizeof(f16)), rows, cols};
     };
-    Planes x = planes(z.x, z.m, z.n), y = planes(z.x, z.m, z.n);
+    Planes x = planes(z.x, z.m, z.n);
+    if (is_long(z)) {
+        f16 *gram = reinterpret_cast<f16 *>(take(z.s));
+        float *parts = reinterpret_cast<float *>(ws);
+        momentum_kernel<<<dim3(z.chunks, matrices), 256, 0, s>>>(set, st, z.chunk, squares);
+        const dim3 tiles(z.n / 64, z.m / 64, matrices);
+        start_kernel<<<tiles, 256, 0, s>>>(set, st, squares, z.chunks, x);
+        hipError_t e = hipGetLastError();
+        if (e == hipSuccess)
+            e = z.m == 64 ? columns<64, SPLIT>(x, matrices, z, st.iterations, gram, parts, s)
+                          : columns<128, SPLIT>(x, matrices, z, st.iterations, gram, parts, s);
+        if (e != hipSuccess)
+            return e;
+        finish_kernel<<<tiles, 256, 0, s>>>(set, st, x, true);
+        return hipGetLastError();
+    }
+    Planes y = planes(z.x, z.m, z.n);
     const Planes gram = planes(z.s, z.m, z.m), poly = planes(z.s, z.m, z.m);
     momentum_kernel<<<dim3(z.chunks, matrices), 256, 0, s>>>(set, st, z.chunk, squares);
     const dim3 tiles(z.n / 64, z.m / 64, matrices);
@@ -1083,7 +1255,8 @@ size_t muon_workspace_bytes(int fan_out, int fan_in, bool split, unsigned matric
     const Sizes z = sizes_of(fan_out, fan_in, split);
     if (is_small(z))
         return 0;  // all in LDS
-    return whole(z.squares * matrices) + 2 * whole(z.x * matrices) + 2 * whole(z.s * matrices);
+    const size_t both = whole(z.squares * matrices) + whole(z.x * matrices) + whole(z.s * matrices);
+    return both + (is_long(z) ? parts_bytes(z, matrices) : whole(z.x * matrices) + whole(z.s * matrices));
 }
 
 hipError_t launch_muon(const MuonSet &set, unsigned matrices, int fan_out, int fan_in, bool split,

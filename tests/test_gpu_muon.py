@@ -32,7 +32,7 @@ SHAPES = [  # matrices, fan_out, fan_in
     (1, 1, 1), (3, 1, 9), (2, 9, 1), (5, 8, 8), (1, 64, 64), (3, 63, 65), (2, 65, 64), (7, 128, 63), (16, 128, 128), (4, 100, 127),
     (2, 128, 129), (2, 129, 128), (3, 64, 155), (2, 30, 700), (2, 700, 30), (2, 300, 701), (2, 701, 300), (1, 256, 256), (1, 257, 512),
     (40, 192, 192), (70, 96, 200), (1, 1000, 1500), (9, 520, 512), (70, 260, 500), (300, 20, 30),
-    (16, 1024, 1024), (24, 1024, 1024), (7, 2048, 2048),
+    (16, 1024, 1024), (24, 1024, 1024), (7, 2048, 2048), (130, 70, 300), (600, 9, 600), (90, 1500, 100), (1, 16384, 3), (2, 5, 16383),
     (3, 64, 512), (2, 512, 33), (5, 20, 257), (2, 64, 513), (3, 250, 60), (2, 130, 64), (4, 100, 250), (2, 256, 128), (3, 128, 257), (2, 60, 900)]
 
 
