@@ -184,7 +184,7 @@ def test_a_head_whose_gradient_is_not_finite_hurts_no_other():
 def test_same_bits_on_a_stream_and_from_a_graph():
     """Eager, on another stream, and captured: twice into graphs that have workspaces of their own."""
     g = gen(6)
-    for shape, dtype in (((3, 200, 130), FP32), ((5, 128, 100), BF16), ((2, 128, 128), FP32)):
+    for shape, dtype in (((3, 200, 130), FP32), ((5, 128, 100), BF16), ((2, 128, 128), FP32), ((4, 100, 250), FP32), ((2, 900, 60), BF16)):
         x = spread(g, *shape).to(dtype)
         want = heads.orthogonalise(x)
         assert torch.equal(heads.orthogonalise(x), want)
