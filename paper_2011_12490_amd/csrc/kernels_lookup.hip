@@ -614,17 +614,20 @@ __global__ __launch_bounds__(256) void join_kernel(const unsigned *keys, unsigne
     }
 }
 
-// Few samples in one launch: a workgroup takes some rows, notes the samples that are
-// theirs, in order, and sums them row by row, a group of lanes each.  us so and sorted, rows
-// of 48: 64 samples of 500 rows 8, 15; 256 of 500 15.7, 15.8, of 20,000 7, 16.
+// Few samples in one launch: a workgroup takes some rows and columns, notes the samples that
+// are its rows', in order, and sums them row by row, a group of lanes each, kAhead entries of
+// its list at a time.  Bound by a launch's waits, and with many samples of a row by the pieces'
+// loads, one after the other: 64 samples of 500 rows of 48 values 3.4 us, 256 samples of one of
+// them 28 (bf16 54; sorted 14 and 17).
 constexpr unsigned kFewSamples = 256;
 template <class T, int V>
 __global__ __launch_bounds__(256) void few_kernel(const int *ids, const T *from, long long stride, unsigned samples, unsigned rows, int D,
                                                   float scale, float *out, int group_log2, unsigned rows_each)
 {
-    constexpr int kAhead = 4;
+    constexpr unsigned kAhead = 16;
+    static_assert(kFewSamples % kAhead == 0, "whole pieces of the list");
     __shared__ unsigned of_wave[4];
-    __shared__ unsigned row_of[kFewSamples], sample_of[kFewSamples];
+    __shared__ __attribute__((aligned(16))) unsigned row_of[kFewSamples], sample_of[kFewSamples];
     const unsigned v0 = blockIdx.x * rows_each, here = rows - v0 < rows_each ? rows - v0 : rows_each;
     const int id = threadIdx.x < samples ? ids[threadIdx.x] : -1;
     const bool mine = (unsigned)id >= v0 && (unsigned)id - v0 < here;
@@ -639,41 +642,35 @@ __global__ __launch_bounds__(256) void few_kernel(const int *ids, const T *from,
             at += of_wave[w];
         count += of_wave[w];
     }
+    if (threadIdx.x >= count)
+        row_of[threadIdx.x] = kNone;
     if (mine) {
         row_of[at] = (unsigned)id - v0;
         sample_of[at] = threadIdx.x;
     }
     __syncthreads();
     const unsigned groups = 256u >> group_log2, lanes = 1u << group_log2;
-    const int vecs = (D + V - 1) / V;
-    for (unsigned v = threadIdx.x >> group_log2; v < here; v += groups)
-        for (int c = (int)(threadIdx.x & (lanes - 1)); c < vecs; c += (int)lanes) {
-            const int e = V > 1 ? vec_at<V>(c, D) : c;
-            float sum[V] = {};
-            for (unsigned i = 0; i < count;) {
-                unsigned found[kAhead], n = 0;  // the next samples of this row
-                for (; i < count && n < kAhead; ++i)
-                    if (row_of[i] == v) {
+    const int c = (int)(blockIdx.y * lanes + (threadIdx.x & (lanes - 1)));
+    if (c >= (D + V - 1) / V)
+        return;
+    const int e = V > 1 ? vec_at<V>(c, D) : c;
+    for (unsigned v = threadIdx.x >> group_log2; v < here; v += groups) {
+        float sum[V] = {};
+        for (unsigned i = 0; i < count; i += kAhead) {
+            Vec<T, V> x[kAhead];
 #pragma unroll
-                        for (unsigned j = 0; j < kAhead; ++j)
-                            if (j == n)
-                                found[j] = sample_of[i];
-                        ++n;
-                    }
-                Vec<T, V> x[kAhead];
+            for (unsigned j = 0; j < kAhead; ++j)
+                if (row_of[i + j] == v)
+                    x[j] = load_vec<T, V, false>(from + (long long)sample_of[i + j] * stride + e);
 #pragma unroll
-                for (unsigned j = 0; j < kAhead; ++j)
-                    if (j < n)
-                        x[j] = load_vec<T, V, false>(from + (long long)found[j] * stride + e);
+            for (unsigned j = 0; j < kAhead; ++j)
+                if (row_of[i + j] == v)
 #pragma unroll
-                for (unsigned j = 0; j < kAhead; ++j)
-                    if (j < n)
-#pragma unroll
-                        for (int k = 0; k < V; ++k)
-                            sum[k] += (float)x[j].v[k];
-            }
-            write_sum<V, false>(out + (size_t)(v0 + v) * D + e, sum, scale);
+                    for (int k = 0; k < V; ++k)
+                        sum[k] += (float)x[j].v[k];
         }
+        write_sum<V, false>(out + (size_t)(v0 + v) * D + e, sum, scale);
+    }
 }
 
 // ---- launches --------------------------------------------------------------------
@@ -726,6 +723,17 @@ Digits digits_of(unsigned rows)
     return {passes, (key_bits + passes - 1) / passes, key_bits};
 }
 
+// Whether few samples go in one launch: while those of a workgroup's rows, as many as ids
+// spread evenly bring, are no more than 96.  us so and sorted, float32 (and bf16), 256 samples: of
+// 2 rows of 48 29, 13 (55, 17), of 9 of 48 24, 14 (51, 18), of 9 of 256 12, 14 (27, 17), of 50 of
+// 48 10, 15 (20, 19), of 500 of 8 8, 17 (16, 19), of 500 of 1,024 4, 17 (4, 20); 128: of 2 of 48
+// 16, 13 (29, 17), of 50 of 48 6, 15 (13, 19); 64 of 2 of 48 9, 14 (15, 17).
+bool is_few(unsigned samples, unsigned rows, int dim)
+{
+    const unsigned each = 256u >> group_log2((dim + 3) / 4);  // bf16's workgroups have twice as many
+    return samples <= kFewSamples && (unsigned long long)samples * (each < rows ? each : rows) <= 96ull * rows;
+}
+
 size_t whole(size_t bytes) { return (bytes + 255) / 256 * 256; }
 
 // Samples of a block of the sort: 1,024, or 2,048 where there are blocks for all of the chip.
@@ -747,7 +755,7 @@ Places places_of(unsigned samples, unsigned rows, int dim)
         return here;
     };
     p.list = take(0);
-    if (samples <= kFewSamples) {
+    if (is_few(samples, rows, dim)) {
         p.counts = p.ends = p.leads = p.trails = p.end = 0;
         return p;
     }
@@ -765,13 +773,13 @@ Places places_of(unsigned samples, unsigned rows, int dim)
 template <class T, int V>
 hipError_t few(Rows dout, const int *ids, unsigned samples, unsigned rows, int dim, float scale, float *out, hipStream_t s)
 {
-    const int g = group_log2((dim + V - 1) / V);
-    // rows of a workgroup: a few for each group, and more where there are too many workgroups
-    unsigned each = (256u >> g) * 4;
+    const int vecs = (dim + V - 1) / V, g = group_log2(vecs);
+    // rows of a workgroup: one for each group, and more where there are too many workgroups
+    unsigned each = 256u >> g;
     if (blocks_of(rows, each) > 4096)
         each = blocks_of(rows, 4096);
-    few_kernel<T, V><<<blocks_of(rows, each), 256, 0, s>>>(ids, static_cast<const T *>(dout.p), dout.stride, samples, rows, dim, scale,
-                                                           out, g, each);
+    few_kernel<T, V><<<dim3(blocks_of(rows, each), blocks_of(vecs, 1 << g)), 256, 0, s>>>(
+        ids, static_cast<const T *>(dout.p), dout.stride, samples, rows, dim, scale, out, g, each);
     return hipGetLastError();
 }
 
@@ -805,7 +813,7 @@ hipError_t backward(Rows dout, const int *ids, unsigned samples, unsigned rows, 
                     hipStream_t s)
 {
     constexpr int V = 16 / sizeof(T);
-    if (samples <= kFewSamples)
+    if (is_few(samples, rows, dim))
         return dim < V ? few<T, 1>(dout, ids, samples, rows, dim, scale, out, s) : few<T, V>(dout, ids, samples, rows, dim, scale, out, s);
     const Places at = places_of(samples, rows, dim);
     const size_t list = whole((size_t)samples * 4);

@@ -148,3 +148,24 @@ def test_python_refusals():
                  lambda: heads.lookup_backward(dout, ids, 5, out=dout)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("dtype", [FP32, BF16])
+@pytest.mark.parametrize("D", [1, 3, 48, 77, 1030])
+def test_few_samples(D, dtype):
+    """Up to 256 samples, on both sides of the choice between one launch and the sort: one row for
+    all, runs, more columns than a workgroup's, tables of more rows than groups."""
+    g = gen(D)
+    for T in (15, 16, 17, 95, 96, 97, 255, 256):
+        for V in (1, 2, 9, 130, 6000):
+            for how in ("masked", "one", "sorted"):
+                ids = ids_of(g, T, V, how)
+                dout = rand(g, T, D).to(dtype)
+                has = (ids >= 0) & (ids < V)
+                dout[~has] = float("nan")
+                got = heads.lookup_backward(dout, ids, V, 0.3, out=torch.full((V, D), 7.0, device="cuda"))
+                at, rows = ids[has].long(), dout[has].double()
+                want, size = (torch.zeros(V, D, dtype=torch.float64, device="cuda").index_add_(0, at, x) for x in (rows, rows.abs()))
+                n = torch.bincount(at, minlength=V)[:, None]
+                bound = (2 * n + 8) * 2.0 ** -24 * 0.3 * size + 2.0 ** -130
+                assert bool(((got.double() - float(np.float32(0.3)) * want).abs() <= bound).all()), (T, V, how)

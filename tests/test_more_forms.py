@@ -76,3 +76,18 @@ def test_launches_of_ordinary_calls(launched):
              line("gradient", 0, 50000, 500, 48, 0, 0), line("matrices", 1, 144, 128, 128), line("matrices", 1, 3, 300, 700)]
     _, names = launched(calls)
     assert [len(n) for n in names] == [1, 2, 1, 1, 3, 5, 1, 18]
+
+
+def test_few_samples_of_few_rows_are_sorted(launched):
+    """The gradient of up to 256 samples: one launch while their rows spread over many workgroups,
+    sorted where a workgroup would go through them all one after the other."""
+    sizes = [(T, V, D) for T in (1, 64, 96) for V in (1, 2, 9, 500) for D in (3, 48, 1024)] + [
+        (256, 500, 48), (256, 500, 1024), (256, 20000, 8), (200, 100000, 64)]
+    spread = len(sizes)
+    sizes += [(T, V, D) for T in (128, 256) for V in (1, 2) for D in (3, 48, 256, 1024)] + [(256, 9, 48), (256, 50, 8)]
+    for bf16 in (0, 1):
+        _, names = launched([line("gradient", bf16, T, V, D, 0, 0) for T, V, D in sizes])
+        for size, kernels in zip(sizes[:spread], names[:spread]):
+            assert len(kernels) == 1 and "few_kernel" in kernels[0], size
+        for size, kernels in zip(sizes[spread:], names[spread:]):
+            assert len(kernels) > 1 and not any("few_kernel" in k for k in kernels), size
