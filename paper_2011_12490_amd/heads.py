@@ -26,7 +26,8 @@ row stride (the layers': below 2^21 elements), on one GPU; what does not fit, an
 what the library itself refuses, raises ValueError before any GPU work.  An out=
 tensor shares no memory with the call's other tensors.  No autograd graph is
 recorded: while autograd records (torch.is_grad_enabled()), a tensor that requires a
-gradient is refused, but for the optimizer's, since its gradient would be lost.
+gradient is refused, but for the optimizer's, since its gradient would be lost; a
+tensor with a forward-mode tangent is refused everywhere, for the same reason.
 """
 from __future__ import annotations
 
@@ -35,6 +36,7 @@ import functools
 from typing import List, NamedTuple, Optional, Sequence
 
 import torch
+from torch.autograd import forward_ad
 
 from . import derf
 
@@ -97,6 +99,12 @@ def _no_graph(x, name) -> None:
                          "torch.no_grad()" % name)
 
 
+def _no_tangent(x, name) -> None:
+    """Refuse a tensor with a forward-mode tangent, which the results would be without."""
+    if forward_ad.unpack_dual(x).tangent is not None:
+        raise ValueError("%s has a forward-mode tangent, which the result would not have: pass its primal" % name)
+
+
 def _array(x, name, dtype, shape, device=None, leaf=False) -> None:
     """Check a contiguous GPU array of a given type and shape; leaf: autograd may follow it."""
     if not isinstance(x, torch.Tensor):
@@ -111,6 +119,8 @@ def _array(x, name, dtype, shape, device=None, leaf=False) -> None:
         raise ValueError("%s must be contiguous" % name)
     if x.requires_grad and not leaf:
         _no_graph(x, name)
+    if forward_ad._current_level >= 0:  # tangents are there within a level only
+        _no_tangent(x, name)
 
 
 def _rows(x, name, shape=None, dtype=None, device=None) -> int:
@@ -131,6 +141,8 @@ def _rows(x, name, shape=None, dtype=None, device=None) -> int:
         raise ValueError("%s: the elements of a row must lie side by side" % name)
     if x.requires_grad:
         _no_graph(x, name)
+    if forward_ad._current_level >= 0:
+        _no_tangent(x, name)
     if size[0] <= 1:  # no next row
         return size[1]
     if stride < size[1]:

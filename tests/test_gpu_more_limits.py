@@ -3,6 +3,7 @@ behind 2^32 bytes, one row of a wide buffer, two calls at once, the same rows tw
 tensors that autograd follows, and a run of them all in one graph."""
 import pytest
 import torch
+from torch.autograd import forward_ad
 
 from paper_2011_12490_amd import heads
 from test_gpu_heads import BF16, FP32, far_rows, gen, rand
@@ -161,3 +162,26 @@ def test_a_backward_pass_in_a_graph_beside_live_autograd():
     assert all(torch.equal(a, c) for a, c in zip(grads, heads.gated_backward(y, pre, x, leaf.detach(), offsets)))
     loss.backward()
     assert torch.equal(leaf.grad, 2 * w)
+
+
+def test_tensors_with_forward_mode_tangents():
+    """Refused, also where nothing records a graph: the results would silently be without them."""
+    x, w, b, offsets, g = gated_layer([5, 6], 0, 8, 12, 0, 0, FP32, 1)
+    y, pre = heads.gated(x, w, b, offsets, keep=True)
+    table, ids = rand(g, 4, 8), torch.zeros(11, dtype=torch.int32, device="cuda")
+    p, m = rand(g, 4, 8), torch.zeros(4, 8, device="cuda")
+    optimizers = [heads.Muon([p], [table]), heads.AdamW([p], [table])]
+    one = torch.ones(1, device="cuda")
+    plain = [lambda f: heads.gated(f(x), w, b, offsets), lambda f: heads.gated(x, f(w), b, offsets), lambda f: heads.gated(x, w, f(b), offsets),
+             lambda f: heads.gated_backward(f(y), pre, x, w, offsets), lambda f: heads.gated_backward(y, f(pre), x, w, offsets),
+             lambda f: heads.lookup(f(table), ids), lambda f: heads.lookup_backward(f(x), ids, 4), lambda f: heads.orthogonalise(f(table)),
+             lambda f: heads.linear(f(x), w[:, 0].contiguous(), b[:, 0].contiguous(), offsets),
+             lambda f: heads.Muon([p], [f(table)]), lambda f: heads.Muon([f(p)], [table], m=[m]),
+             lambda f: optimizers[0].step(f(one)), lambda f: optimizers[1].step(grad_scale=f(one))]
+    with forward_ad.dual_level():
+        for call in plain:
+            for mode in (torch.enable_grad, torch.no_grad):
+                with mode(), pytest.raises(ValueError, match="tangent"):
+                    call(lambda t: forward_ad.make_dual(t, torch.ones_like(t)))
+            call(lambda t: t)  # without one, within a level
+            call(lambda t: forward_ad.unpack_dual(forward_ad.make_dual(t, torch.ones_like(t))).primal)

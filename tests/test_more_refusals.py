@@ -6,6 +6,7 @@ import subprocess
 
 import pytest
 import torch
+from torch.autograd import forward_ad
 
 from paper_2011_12490_amd import derf, heads
 
@@ -231,3 +232,15 @@ def test_muon_refuses_host_tensors():
     for call in (lambda: heads.orthogonalise(x), lambda: heads.Muon([x], [x])):
         with pytest.raises(ValueError):
             call()
+
+
+def test_forward_mode_tangents():
+    x = torch.zeros((4, 8))
+    heads._no_tangent(x, "x")
+    with forward_ad.dual_level():
+        dual = forward_ad.make_dual(x, torch.ones_like(x))
+        heads._no_tangent(x, "x")
+        heads._no_tangent(forward_ad.unpack_dual(dual).primal, "x")
+        for t in (dual, dual[1:], dual * 2):
+            with pytest.raises(ValueError, match="y has a forward-mode tangent"):
+                heads._no_tangent(t, "y")
