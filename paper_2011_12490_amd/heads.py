@@ -105,6 +105,13 @@ def _no_tangent(x, name) -> None:
         raise ValueError("%s has a forward-mode tangent, which the result would not have: pass its primal" % name)
 
 
+def _not_negated(x, name) -> None:
+    """Refuse a view whose sign torch has yet to change (the imaginary part of a conjugate): its
+    memory holds other values.  Only single values a row pass the checks of strides so."""
+    if x.is_neg():
+        raise ValueError("%s is a lazily negated view: call resolve_neg() on it" % name)
+
+
 def _array(x, name, dtype, shape, device=None, leaf=False) -> None:
     """Check a contiguous GPU array of a given type and shape; leaf: autograd may follow it."""
     if not isinstance(x, torch.Tensor):
@@ -117,6 +124,8 @@ def _array(x, name, dtype, shape, device=None, leaf=False) -> None:
         raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(x.shape)))
     if not x.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
+    if x.numel() == 1:
+        _not_negated(x, name)
     if x.requires_grad and not leaf:
         _no_graph(x, name)
     if forward_ad._current_level >= 0:  # tangents are there within a level only
@@ -139,6 +148,8 @@ def _rows(x, name, shape=None, dtype=None, device=None) -> int:
     stride, step = x.stride()
     if step != 1 and size[1] > 1:
         raise ValueError("%s: the elements of a row must lie side by side" % name)
+    if size[1] == 1:
+        _not_negated(x, name)
     if x.requires_grad:
         _no_graph(x, name)
     if forward_ad._current_level >= 0:

@@ -185,3 +185,20 @@ def test_tensors_with_forward_mode_tangents():
                     call(lambda t: forward_ad.make_dual(t, torch.ones_like(t)))
             call(lambda t: t)  # without one, within a level
             call(lambda t: forward_ad.unpack_dual(forward_ad.make_dual(t, torch.ones_like(t))).primal)
+
+
+def test_views_that_torch_has_yet_to_negate():
+    """The imaginary part of a conjugate: memory of the other sign.  Refused, and right once resolved."""
+    z = torch.complex(torch.zeros(3, 1, device="cuda"), torch.tensor([[1.0], [2.0], [3.0]], device="cuda")).conj()
+    table, one = z.imag, z[0, 0:1].imag
+    ids = torch.tensor([2, 0], dtype=torch.int32, device="cuda")
+    p, m = torch.ones(4, 8, device="cuda"), torch.zeros(4, 8, device="cuda")
+    muon = heads.Muon([p], [torch.ones(4, 8, device="cuda")], m=[m])
+    for call in (lambda f: heads.lookup(f(table), ids), lambda f: heads.lookup_backward(f(table)[:2], ids, 3),
+                 lambda f: heads.lookup(z.real, ids, out=f(table)[:2]), lambda f: heads.orthogonalise(f(one)[None]),
+                 lambda f: muon.step(f(one))):
+        with pytest.raises(ValueError, match="negated"):
+            call(lambda t: t)
+        call(lambda t: t.resolve_neg().clone())
+    assert heads.lookup(table.resolve_neg(), ids).flatten().tolist() == [-3.0, -1.0]
+    assert float(m[0, 0]) == -1.0  # a step whose gradients were scaled by -1
