@@ -396,8 +396,9 @@ int derf_reset_stats(derf_handle *h);
  * derf_adamw_create allocates and waits, derf_adamw_step refuses a capturing stream,
  * derf_adamw_destroy waits).  A workspace belongs to the caller, holds nothing between
  * calls, and is 16-byte aligned.  Outputs overlap neither inputs nor each other (the
- * optimizer's arrays are updated in place).  Results do not depend on the run: every
- * sum has a fixed order.
+ * optimizer's arrays are updated in place; columns of one buffer, side by side, do not
+ * overlap): the gated layers, lookups and derf_orthogonalise refuse arrays that do.
+ * Results do not depend on the run: every sum has a fixed order.
  *   precision    a derf_precision: the type of the rows (float or bf16)
  *   *_stride     elements from a row to the next, >= the row length; rows need
  *                the alignment of their type only (rows and strides that are
@@ -595,7 +596,7 @@ void derf_adamw_destroy(derf_adamw *opt);
  * fan_in) and (a, b, c) = (3.4445, -4.7750, 2.0315), which brings the singular values
  * near 1 (five iterations: those above a few hundredths of the norm into about
  * [0.7, 1.2]) and keeps the directions.
- *   x, out   [num_matrices][fan_out][fan_in] of one type, contiguous
+ *   x, out   [num_matrices][fan_out][fan_in] of one type, contiguous; out may be x
  *   float: as exact as the iteration in fp32; bf16: products of 11 bits, sums in fp32.
  *   Entries of X count down to 2^-36 (a norm far below 1e-7 leaves smaller ones)
  *   workspace  derf_orthogonalise_workspace(...) bytes (-1 for invalid sizes)

@@ -130,6 +130,11 @@ int derf_heads_gated(const void *x, long long x_stride, const void *w, const flo
     TRY(check_layer_rows("y", y, y_stride, fan_out, precision));
     if (pre)
         TRY(check_layer_rows("pre", pre, pre_stride, 2 * fan_out, precision));
+    TRY(check_apart({rows_area("y", y, num_rows, y_stride, fan_out, precision),
+                     rows_area("pre", pre, num_rows, pre_stride, 2 * fan_out, precision)},
+                    {rows_area("x", x, num_rows, x_stride, fan_in, precision),
+                     rows_area("w", w, num_heads * 2LL * fan_out, fan_in, fan_in, precision),
+                     array_area("bias", bias, num_heads * 8LL * fan_out), array_area("offsets", offsets, (num_heads + 1) * 4LL)}));
     const LinearShape sh = {offsets, (unsigned)num_rows, num_heads, fan_in, fan_out};
     return launched(launch_heads_gated(sh, {x, x_stride}, w, bias, act, precision == DERF_PREC_BF16, {y, y_stride},
                                        {pre, pre_stride}, static_cast<hipStream_t>(hip_stream)),
@@ -169,8 +174,17 @@ int derf_heads_gated_backward(const void *dy, long long dy_stride, const void *p
     if (out_bias)
         TRY(check_array("out_bias", out_bias, 4));
     TRY(check_array("offsets", offsets, 4));
-    TRY(check_workspace(workspace, workspace_bytes,
-                        derf_heads_gated_workspace(num_rows, num_heads, fan_in, fan_out, precision)));
+    const long long need = derf_heads_gated_workspace(num_rows, num_heads, fan_in, fan_out, precision);
+    TRY(check_workspace(workspace, workspace_bytes, need));
+    const long long weights = num_heads * 2LL * fan_out;
+    TRY(check_apart({rows_area("out_x", out_x, num_rows, out_x_stride, fan_in, precision),
+                     rows_area("out_w", out_w, weights, fan_in, fan_in, precision), array_area("out_bias", out_bias, weights * 4),
+                     array_area("workspace", workspace, need)},
+                    {rows_area("dy", dy, num_rows, dy_stride, fan_out, precision),
+                     rows_area("pre", pre, num_rows, pre_stride, 2 * fan_out, precision),
+                     rows_area("x", out_w ? x : nullptr, num_rows, x_stride, fan_in, precision),
+                     rows_area("w", out_x ? w : nullptr, weights, fan_in, fan_in, precision),
+                     array_area("offsets", offsets, (num_heads + 1) * 4LL)}));
     const LinearShape sh = {offsets, (unsigned)num_rows, num_heads, fan_in, fan_out};
     return launched(launch_heads_gated_backward(sh, {dy, dy_stride}, {pre, pre_stride}, {x, x_stride}, w, act,
                                                 precision == DERF_PREC_BF16, {out_x, out_x_stride}, out_w, out_bias,
@@ -188,6 +202,8 @@ int derf_lookup(const void *table, long long table_stride, const int *ids, long 
     TRY(check_rows("table", table, table_stride, dim, precision));
     TRY(check_array("ids", ids, 4));
     TRY(check_rows("out", out, out_stride, dim, precision));
+    TRY(check_apart({rows_area("out", out, num_samples, out_stride, dim, precision)},
+                    {rows_area("table", table, num_rows, table_stride, dim, precision), array_area("ids", ids, num_samples * 4)}));
     return launched(launch_lookup({table, table_stride}, ids, num_samples, num_rows, dim, scale, precision == DERF_PREC_BF16,
                                   {out, out_stride}, static_cast<hipStream_t>(hip_stream)),
                     "derf_lookup");
@@ -211,7 +227,10 @@ int derf_lookup_backward(const void *dout, long long dout_stride, const int *ids
         TRY(check_array("ids", ids, 4));
     }
     TRY(check_array("out", out, 4));
-    TRY(check_workspace(workspace, workspace_bytes, derf_lookup_workspace(num_samples, num_rows, dim)));
+    const long long need = derf_lookup_workspace(num_samples, num_rows, dim);
+    TRY(check_workspace(workspace, workspace_bytes, need));
+    TRY(check_apart({rows_area("out", out, num_rows, dim, dim, DERF_PREC_FP32), array_area("workspace", workspace, need)},
+                    {rows_area("dout", dout, num_samples, dout_stride, dim, precision), array_area("ids", ids, num_samples * 4)}));
     return launched(launch_lookup_backward({dout, dout_stride}, ids, (unsigned)num_samples, (unsigned)num_rows, dim, scale,
                                            precision == DERF_PREC_BF16, out, workspace, static_cast<hipStream_t>(hip_stream)),
                     "derf_lookup_backward");
@@ -240,7 +259,12 @@ int derf_orthogonalise(const void *x, long long num_matrices, int fan_out, int f
     const bool bf16 = precision == DERF_PREC_BF16;
     TRY(check_array("x", x, bf16 ? 2 : 4));
     TRY(check_array("out", out, bf16 ? 2 : 4));
-    TRY(check_workspace(workspace, workspace_bytes, derf_orthogonalise_workspace(num_matrices, fan_out, fan_in, precision)));
+    const long long need = derf_orthogonalise_workspace(num_matrices, fan_out, fan_in, precision);
+    TRY(check_workspace(workspace, workspace_bytes, need));
+    // x itself is read before any of it is written
+    const Area from = rows_area("x", x, num_matrices * fan_out, fan_in, fan_in, precision);
+    TRY(check_apart({rows_area("out", out, num_matrices * fan_out, fan_in, fan_in, precision), array_area("workspace", workspace, need)},
+                    {x == out ? Area{} : from}));
     const MuonSet set = {nullptr, 0, {out, x, nullptr, nullptr, fan_out, fan_in, bf16, bf16, 1.0f}};
     const MuonStep st = {0.0f, 1.0f, 0.0f, 0, 0, 0, iterations, nullptr};
     return launched(launch_muon(set, (unsigned)num_matrices, fan_out, fan_in, !bf16, st, workspace,

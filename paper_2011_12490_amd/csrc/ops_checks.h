@@ -2,6 +2,9 @@
 #pragma once
 #include "ops_internal.h"
 
+#include <algorithm>
+#include <initializer_list>
+
 namespace derf {
 
 namespace {
@@ -97,6 +100,72 @@ int check_workspace(const void *p, long long have, long long need)
         return report(DERF_ERR_INVALID_ARG, "workspace of %lld bytes, %lld needed", have, need);
     if (need > 0 && (!p || misaligned(p, 16)))
         return report(DERF_ERR_INVALID_ARG, "workspace is null or not 16-byte aligned");
+    return DERF_OK;
+}
+
+// Rows of an array in memory, in bytes; p null: none.
+struct Area {
+    const char *name;
+    const void *p;
+    long long rows, row, stride;
+};
+Area rows_area(const char *name, const void *p, long long rows, long long stride, long long dim, int precision)
+{
+    const int bytes = precision == DERF_PREC_BF16 ? 2 : 4;
+    return {name, p, dim > 0 ? rows : 0, dim * bytes, stride * bytes};
+}
+Area array_area(const char *name, const void *p, long long bytes) { return {name, p, bytes > 0 ? 1 : 0, bytes, bytes}; }
+
+typedef __int128 Wide;
+// The sum of floor((a i + b) / m) over i in [0, n), a, b >= 0: whole parts taken out, what is
+// left counted along the other axis, as Euclid's algorithm goes.
+Wide floor_sum(Wide n, Wide m, Wide a, Wide b)
+{
+    Wide sum = 0;
+    while (n > 0) {
+        sum += n * (n - 1) / 2 * (a / m) + n * (b / m);
+        a %= m;
+        b %= m;
+        const Wide top = a * n + b;
+        n = top / m;
+        b = top % m;
+        std::swap(a, m);
+    }
+    return sum;
+}
+
+// Whether a byte is in a row of both.  Row i of one begins at x = i sa - d behind the other's
+// first, and has bytes of its rows j with x - lb < j sb < x + la: floor((x + la - 1) / sb) -
+// floor((x - lb) / sb) of them, all of which, or their neighbours, are there while x is within
+// (-la, (nb - 1) sb + lb).
+bool share_memory(const Area &one, const Area &other)
+{
+    if (!one.p || !other.p || one.rows <= 0 || other.rows <= 0)
+        return false;
+    const Wide la = one.row, lb = other.row, na = one.rows, nb = other.rows;
+    const Wide sa = na > 1 ? one.stride : one.row, sb = nb > 1 ? other.stride : other.row;
+    const Wide d = (Wide) reinterpret_cast<uintptr_t>(other.p) - (Wide) reinterpret_cast<uintptr_t>(one.p);
+    const Wide end_a = (na - 1) * sa + la, end_b = (nb - 1) * sb + lb;
+    if (d >= end_a || -d >= end_b)
+        return false;
+    const Wide from = d < la ? 0 : (d - la) / sa + 1, to = std::min(na, (end_b + d + sa - 1) / sa);
+    if (from >= to)
+        return false;
+    const Wide x = from * sa - d, up = ((la + lb) / sb + 1) * sb;  // no operand below zero
+    return floor_sum(to - from, sb, sa, x + la - 1 + up) > floor_sum(to - from, sb, sa, x - lb + up);
+}
+
+// What is written shares memory neither with what is read nor with each other.
+int check_apart(std::initializer_list<Area> written, std::initializer_list<Area> read)
+{
+    for (const Area *w = written.begin(); w != written.end(); ++w) {
+        for (const Area &r : read)
+            if (share_memory(*w, r))
+                return report(DERF_ERR_INVALID_ARG, "%s overlaps %s", w->name, r.name);
+        for (const Area *v = w + 1; v != written.end(); ++v)
+            if (share_memory(*w, *v))
+                return report(DERF_ERR_INVALID_ARG, "%s overlaps %s", w->name, v->name);
+    }
     return DERF_OK;
 }
 

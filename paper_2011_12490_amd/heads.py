@@ -24,10 +24,11 @@ Argument checks and marshalling only; all work is done by libderf.so, on torch's
 current stream of the tensors' device.  Tensors are float32 or bfloat16, of any
 row stride (the layers': below 2^21 elements), on one GPU; what does not fit, and
 what the library itself refuses, raises ValueError before any GPU work.  An out=
-tensor shares no memory with the call's other tensors.  No autograd graph is
-recorded: while autograd records (torch.is_grad_enabled()), a tensor that requires a
-gradient is refused, but for the optimizer's, since its gradient would be lost; a
-tensor with a forward-mode tangent is refused everywhere, for the same reason.
+tensor shares no memory with the call's other tensors (gated layers, lookups and
+orthogonalise check that).  No autograd graph is recorded: while autograd records
+(torch.is_grad_enabled()), a tensor that requires a gradient is refused, but for the
+optimizer's, since its gradient would be lost; a tensor with a forward-mode tangent is
+refused everywhere, for the same reason.
 """
 from __future__ import annotations
 
@@ -541,7 +542,7 @@ def orthogonalise(x: torch.Tensor, iterations: int = 5, out: Optional[torch.Tens
     """x's matrices (the last two dimensions) with their singular values brought near 1 and
     their directions kept (derf_orthogonalise): float32 as exactly as the iteration in
     float32, bfloat16 through products of 11 bits.  x: contiguous, [fan_out, fan_in] or
-    [heads, fan_out, fan_in]; out: another tensor of its shape and type."""
+    [heads, fan_out, fan_in]; out: x, or another tensor of its shape and type."""
     if not isinstance(x, torch.Tensor) or x.dim() not in (2, 3) or x.dtype not in _PRECISION:
         raise ValueError("x must be a float32 or bfloat16 tensor [fan_out, fan_in] or [heads, fan_out, fan_in]")
     _array(x, "x", x.dtype, x.shape)

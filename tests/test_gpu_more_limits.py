@@ -202,3 +202,30 @@ def test_views_that_torch_has_yet_to_negate():
         call(lambda t: t.resolve_neg().clone())
     assert heads.lookup(table.resolve_neg(), ids).flatten().tolist() == [-3.0, -1.0]
     assert float(m[0, 0]) == -1.0  # a step whose gradients were scaled by -1
+
+
+@pytest.mark.parametrize("dtype", [FP32, BF16])
+@pytest.mark.parametrize("K,O,I", [(5, 40, 60), (3, 200, 128), (2, 90, 400), (3, 300, 200)])
+def test_orthogonalise_in_place(K, O, I, dtype):
+    x = rand(gen(2), K, O, I).to(dtype)
+    want = heads.orthogonalise(x)
+    assert heads.orthogonalise(x, out=x) is x and torch.equal(x, want)
+
+
+def test_outputs_that_share_memory():
+    x, w, b, offsets, g = gated_layer([70, 50], 8, 24, 24, 0, 0, BF16, 7)
+    wide = torch.zeros(128, 24 * 4 + 3, dtype=BF16, device="cuda")
+    part = lambda at, n: wide[:, at:at + n]  # noqa: E731
+    part(0, 24).copy_(x)
+    y, pre = heads.gated(x, w, b, offsets, keep=True)
+    # columns side by side in one buffer do not overlap
+    got = heads.gated(part(0, 24), w, b, offsets, out=part(24, 24), out_pre=part(48, 48))
+    assert torch.equal(got[0], y) and torch.equal(got[1], pre) and not bool(wide[:, 96:].any())
+    dy, table, ids = rand(g, 128, 24).to(BF16), rand(g, 24, 24), torch.zeros(24, dtype=torch.int32, device="cuda")
+    for call in (lambda: heads.gated(x, w, b, offsets, out=x), lambda: heads.gated(part(0, 24), w, b, offsets, out=part(23, 24)),
+                 lambda: heads.gated(x, w, b, offsets, out=part(24, 24), out_pre=part(47, 48)),
+                 lambda: heads.gated_backward(dy, pre, x, w, offsets, out_x=dy), lambda: heads.gated_backward(dy, pre, x, w, offsets, out_weight=w),
+                 lambda: heads.lookup(table, ids, out=table), lambda: heads.lookup_backward(table, ids, 24, out=table),
+                 lambda: heads.orthogonalise(table[:12], out=table[6:18])):
+        with pytest.raises(ValueError, match="overlaps"):
+            call()
