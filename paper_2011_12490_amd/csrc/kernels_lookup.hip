@@ -54,8 +54,7 @@ __device__ __forceinline__ int vec_at(int c, int D)
 
 // ---- rows out of the table ------------------------------------------------------
 // A group of 2^group_log2 lanes a row, four rows under way.  Bound by its bytes: 524,288 rows
-// of 512 bf16 values out of 200,000 in 154 us, 537 MB written and 257 read (5.2 TB/s); whole
-// lines past the caches (through them 174 us).
+// of 512 bf16 values out of 200,000 in 154 us, 537 MB written and 257 read (5.2 TB/s).
 template <class T, int V, bool PAST>
 __global__ __launch_bounds__(256) void lookup_kernel(const T *table, long long stride, const int *ids, long long samples,
                                                      long long rows, int D, float scale, T *out, long long os, int group_log2)
@@ -707,7 +706,12 @@ hipError_t lookup_of(Rows table, const int *ids, long long samples, long long ro
     constexpr int V = 16 / sizeof(T);
     if (dim < V)
         return lookup<T, 1, false>(table, ids, samples, rows, dim, scale, out, s);
-    if (whole_lines(out.p, out.stride, dim, sizeof(T)))
+    // Whole lines past the caches where these would not hold the result (256 MB) for the operator
+    // that reads it.  us past them and through them, and so with a concatenation behind: bf16
+    // rows of 512 of 20,000, 65,536 samples (67 MB) 20, 21 and 72, 53; 131,072 38, 40 and 138,
+    // 112; 262,144 73, 76 and 290, 305; 524,288 146, 158 and 568, 589; float32 rows of 64 of 1,000,
+    // 524,288 samples (134 MB) 27, 23 and 152, 145; rows of 512, 131,072 samples 76, 78 and 208, 220.
+    if (whole_lines(out.p, out.stride, dim, sizeof(T)) && (unsigned long long)samples * dim * sizeof(T) >= (256ull << 20))
         return lookup<T, V, true>(table, ids, samples, rows, dim, scale, out, s);
     return lookup<T, V, false>(table, ids, samples, rows, dim, scale, out, s);
 }

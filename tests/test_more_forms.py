@@ -91,3 +91,12 @@ def test_few_samples_of_few_rows_are_sorted(launched):
             assert len(kernels) == 1 and "few_kernel" in kernels[0], size
         for size, kernels in zip(sizes[spread:], names[spread:]):
             assert len(kernels) > 1 and not any("few_kernel" in k for k in kernels), size
+
+
+def test_lookups_that_the_caches_hold_stay_there(launched):
+    """Results of whole lines go past the caches only from 256 MB on."""
+    sizes = [(0, 65536, 512), (1, 65536, 512), (1, 262143, 512), (0, 1000, 64), (1, 262144, 512), (0, 131072, 512), (0, 1 << 20, 64)]
+    kernels, names = launched([line("lookup", bf16, T, 1000, D, 0, 0) for bf16, T, D in sizes])
+    past = {k for k in kernels if "lookup_kernel" in k and "Lb1E" in k}
+    assert len(past) == 2
+    assert [n[0] in past for n in names] == [False] * 4 + [True] * 3
