@@ -30,14 +30,16 @@ hipError_t gated(const LinearShape &sh, Rows x, const void *w, const float *bias
                                                                                             s, pre);
     const bool alone = goes_alone(mw) && goes_alone(mx);
     if constexpr (sizeof(T) == 2) {
-        // large tiles as in large_tiles, from a depth of 256 on; in both sizes a wave has 64
-        // columns, whole lines.  us, rows of bf16 with gates and ups kept, 256 and 128: 256 to
-        // 256 on 262,139 146, 148 (197 past weights in LDS), on 65,536 41, 40; 320 to 512 on
-        // 65,536 88, 82; 1,024 to 1,024 on 32,768 144 to 163, 159 to 170 (two cards); 2,048 to
-        // 4,096 on 32,768 1,036, 1,245.  262,139 rows of 256 to 256 move 537 MB: 3.7 TB/s, the
-        // four steps of a tile's loads waiting for its results' stores; wide ones are bound by
-        // the matrix units' power (1,060 TFLOP/s)
-        if (alone && depth >= 256 && large_tiles(p, 2 * O))
+        // large tiles as in large_tiles, and from a depth of 256 to 512 only where they leave little
+        // of their last round empty (their gain there is less); in both sizes a wave has 64
+        // columns, whole lines.  us, rows of bf16 with gates and ups kept, 256 and 128: 256 to 256
+        // on 262,139 130, 136, on 131,072 76, 69; 320 to 512 on 65,536 80, 77 (64 heads 91, 81), on
+        // 131,072 148, 150; 384 to 384 131, 126; 448 to 640 on 65,536 122, 116; 512 to 512 103, 99;
+        // 768 to 768 188, 194; 1,024 to 1,024 on 32,768 152, 155; 2,048 to 2,048 on 16,384 256, 281;
+        // 2,048 to 4,096 on 32,768 1,003, 1,224.  262,139 rows of 256 to 256 move 537 MB: 4.1 TB/s (197
+        // us past weights in LDS), the four steps of a tile's loads waiting for its results'
+        // stores; wide ones are bound by the matrix units' power (1,096 TFLOP/s)
+        if (alone && depth >= 256 && large_tiles(p, 2 * O, depth < 512 ? 4.25 : 4.6))
             return launch_rows<Product<T, 256, 256, 2, 4, true, true, false, true, false, 1, true>>(p, mw, mx, bias, act, y, O,
                                                                                                  depth, s, pre);
         if (alone && wide_tile<T>(2 * O))

@@ -1022,13 +1022,14 @@ hipError_t launch_rows(const Problem &p, const Matrix<typename C::T> &w,
 // larger part of the whole.  us with large and small tiles: 4,096 rows of 2,048 to
 // 4,096 100, 89; 32,768 of 1,024 to 1,024 92, 85; 65,536 of 1,024 to 1,024 179,
 // 207; 65,536 of 512 to 1,024 103, 107; and 262,144 of 256 to 256, where the depth
-// is too short to pay for a large tile's start, 84, 75.
-bool large_tiles(const Problem &p, int width)
+// is too short to pay for a large tile's start, 84, 75.  worth: eight rounds of large tiles in
+// rounds of small ones.
+bool large_tiles(const Problem &p, int width, double worth = 4.6)
 {
     constexpr unsigned kCus = 256;
     const unsigned long long large = (p.rows / 256ull + p.heads / 2) * tiles_of(width, 256);
     const unsigned long long small = (p.rows / 128ull + p.heads / 2) * tiles_of(width, 128);
-    return 8 * ((large + kCus - 1) / kCus) <= 4.6 * ((small + 2 * kCus - 1) / (2 * kCus));
+    return 8 * ((large + kCus - 1) / kCus) <= worth * ((small + 2 * kCus - 1) / (2 * kCus));
 }
 
 template <class C>

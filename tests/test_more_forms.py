@@ -100,3 +100,14 @@ def test_lookups_that_the_caches_hold_stay_there(launched):
     past = {k for k in kernels if "lookup_kernel" in k and "Lb1E" in k}
     assert len(past) == 2
     assert [n[0] in past for n in names] == [False] * 4 + [True] * 3
+
+
+def test_gated_layers_of_large_tiles(launched):
+    """Tiles of 256 as the layers' rule takes them; of 256 to 512 deep ones where few of them are
+    left over for the last round."""
+    small = [(131072, 16, 256, 256), (65536, 8, 320, 512), (65536, 64, 320, 512), (131072, 16, 384, 384), (65536, 16, 448, 640),
+             (4096, 8, 2048, 2048)]
+    large = [(262139, 16, 256, 256), (131072, 16, 320, 512), (65536, 16, 768, 768), (16384, 8, 2048, 2048)]
+    _, names = launched([line("gated", 1, *size, 0, 0, 1) for size in small + large])
+    assert [len(n) for n in names] == [1] * 10
+    assert ["Li256ELi256E" in n[0] for n in names] == [False] * 6 + [True] * 4, names
