@@ -5,6 +5,8 @@ import pytest
 import torch
 
 from paper_2011_12490_amd import heads, scenes, training
+from test_gpu_heads import FP32
+from test_gpu_muon import check, formula
 
 pytestmark = pytest.mark.gpu
 
@@ -135,3 +137,54 @@ def test_fits_run():
         assert np.isfinite(errors).all()
     _, errors = training.fit(steps=3, samples=512, num_heads=3, optimizer="muon")
     assert np.isfinite(errors).all()
+
+
+def adamw_formula(p, g, m, v, step, lr):
+    """AdamW's parameters after a step in float64, without decay, and how far float32 may be: three
+    roundings of the first moment's terms, 16 of the update (the second moment's sums, a root, a
+    quotient), two of the parameter."""
+    p, g, m, v = (t.double() for t in (p, g, m.reshape(p.shape), v.reshape(p.shape)))
+    size, m = 0.9 * m.abs() + 0.1 * g.abs(), 0.9 * m + 0.1 * g
+    root = ((0.999 * v + 0.001 * g * g) / (1 - 0.999 ** step)).sqrt() + 1e-8
+    rate = lr / (1 - 0.9 ** step) / root
+    return p - rate * m, 2.0 ** -24 * (rate * (3 * size + 16 * m.abs()) + 2 * p.abs()) + lr * 2.0 ** -30
+
+
+def check_steps(t, run, adamw, muon, lr, muon_lr):
+    """adamw, muon: pairs of a parameter and the gradient that belongs to it, in the optimizers' order.
+    Three steps of run(), each against the formulas on the state before it."""
+    assert len(t.optimizer.params) == len(adamw) and len(t.muon.params) == len(muon)
+    for step in range(1, 4):
+        was = [(p.clone(), t.optimizer.m[i].clone(), t.optimizer.v[i].clone()) for i, (p, _) in enumerate(adamw)]
+        before = [(p.clone(), t.muon.m[i].clone()) for i, (p, _) in enumerate(muon)]
+        run()
+        for (p, grad), (old, m, v) in zip(adamw, was):
+            assert bool(grad.any())
+            want, far = adamw_formula(old, grad, m, v, step, lr)
+            assert bool(((p.double() - want).abs() <= far).all())
+        for (p, grad), (old, m) in zip(muon, before):
+            assert bool(grad.any())
+            shape = m.shape
+            _, want, far = formula(old.view(shape), grad.view(shape), m, 1.0, muon_lr, 0.95, True, 0.0, FP32)
+            check(p.view(shape), want, far, 3 * 2.0 ** -24 * want.square().sum((-2, -1)).sqrt())
+
+
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+def test_gated_steps_follow_their_own_gradients(precision):
+    """Every parameter moves by its optimizer's formula along the gradient that the backward pass left."""
+    t, x, d, image, target = trainer_and_batch(precision)
+    adamw = [(t.codes, t.codes_grad), (t.out_weight, t.out_weight_grad), (t.out_bias, t.out_bias_grad)] + list(zip(t.bias, t.bias_grad))
+    check_steps(t, lambda: t.step(x, d, image, target), adamw, list(zip(t.weight, t.weight_grad)), 2e-3, 0.02)
+
+
+@pytest.mark.parametrize("precision", ["fp32", "bf16"])
+def test_steps_with_muon_follow_their_own_gradients(precision):
+    rng = np.random.default_rng(5)
+    arch = scenes.ARCH_TINY
+    t = training.HeadTrainer(rng.uniform(-1, 1, (3, 3)), arch, training.start_weights(3, arch, 2), precision, optimizer="muon")
+    g = torch.Generator(device="cuda").manual_seed(1)
+    x, d = torch.rand(900, 3, generator=g, device="cuda") * 2 - 1, torch.randn(900, 3, generator=g, device="cuda")
+    pairs = list(zip(t.weight, t.weight_grad))
+    hidden = ["hidden" in n for n in t.names]
+    adamw = [p for p, h in zip(pairs, hidden) if not h] + list(zip(t.bias, t.bias_grad))
+    check_steps(t, lambda: t.step(x, d, training.analytic_field(x, d)), adamw, [p for p, h in zip(pairs, hidden) if h], 5e-4, 0.02)
