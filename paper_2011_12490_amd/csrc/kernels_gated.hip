@@ -47,6 +47,8 @@ hipError_t gated(const LinearShape &sh, Rows x, const void *w, const float *bias
                                                                                                  depth, s, pre);
     }
     if (wide_tile<T>(2 * O)) {
+        // float32, all kept: 256 to 256 on 65,536 rows 164 us (its products alone 114), 1,024 to
+        // 1,024 on 32,768 1,058 (910): matrix units, 65 % busy
         if constexpr (sizeof(T) == 4)
             if (alone)
                 return launch_rows<Product<T, 128, 128, 2, 2, true, true, false, true, false, 1, true>>(p, mw, mx, bias, act, y,

@@ -5,7 +5,10 @@
 //
 // and the rest is the gradient of a linear layer of 2 fan_out outputs without an
 // activation: dx = W^T dz, dW = dz^T x, db = sum dz.  One pass over the rows makes dz
-// in the rows' type for the products, and sums db from its float32 values.
+// in the rows' type for the products, and sums db from its float32 values.  In bf16 that
+// rounding, half a step, is as large as the results' own: dx and dW are 2.3e-3 of their norm
+// off, 1.7e-3 without it.  A second plane with dz's rest would make two products of each one,
+// and the products bound the wide layers (52 % of the matrix units' cycles, at their power).
 #include "layers.h"
 
 namespace derf {
@@ -428,6 +431,7 @@ hipError_t gated_backward(const LinearShape &sh, Rows dy, Rows pre, Rows x, cons
             return launch_gradients<Product<T, 256, 256, 4, 2, false, true, false, true>,
                                     Product<T, 256, 256, 4, 2, false, false, false, true, true>>(p, mw, mz, mx, dx, dw,
                                                                                                (float *)nullptr, s);
+    // float32: 256 to 256 on 65,536 rows 394 us: dz 61, dx 178, dW 204 (each product alone 114)
     if (rows && dx.p)
         e = rows_product<T, false, false, false>(p, mw, mz, nullptr, false, dx, sh.fan_in, p.fan_out, s);
     if (e != hipSuccess || !dw)

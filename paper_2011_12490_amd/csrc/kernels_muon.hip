@@ -10,15 +10,18 @@
 // The products run on the fp16 matrix units.  All singular values stay below 1.21, so no
 // entry of X, S or Q is above 3.5 in magnitude, and they are held as fp16 values of 2^12
 // times themselves, far from fp16's limits.  For float32 updates each is held as two
-// fp16 values, the rounded one and the rest (22 bits), and a product is three: the steps
-// lose no more than they do in float32 (on matrices of 512 to 1,024 of normal values
-// 2.1e-6 of the result's norm off, 1.9e-6 in float32).  a X is added in float32: with a in
-// Q's diagonal the matrix units' sums, whose roundings are those of their largest terms,
-// lose twice as much.  bf16 updates, whose own rounding is 2^-9 (1.65e-3 of a matrix's norm),
-// multiply the first halves alone: 11 bits.  X itself keeps both, since a X takes what a step
-// loses of the small singular values' part to 3.4 times as much in the next: the results,
-// rounding included, are 2.0 to 2.6e-3 off (8 x 8 to 1,000 x 1,000), with X in 11 bits too up to
-// 8e-3, with bf16 products about ten times that.  In memory X keeps both for all but the last
+// fp16 values, the rounded one and the rest (22 bits), and a product is three.  Float32's
+// operands have 24 bits, and its sums lose more the longer they are.  Off in 1e-6 of the
+// result's norm (root mean square, normal values) here and by plain products in float32:
+// 8 x 8 1.05, 0.77; 16 x 16 0.83, 0.75; 32 x 96 1.64, 1.25; 64 x 64 0.85, 1.19; 64 x 512 1.84,
+// 1.64; 128 x 128 0.81, 1.42; 300 x 701 1.35, 2.40; 1,024 x 1,024 1.19, 3.07.  a X is added in
+// float32: with a in Q's diagonal the matrix units' sums, whose roundings are those of their
+// largest terms, lose twice as much.  bf16 updates, whose own rounding is 2^-9 (1.65e-3 of a
+// matrix's norm), multiply the first halves alone: 11 bits, whatever the gradient's type.  X
+// itself keeps both, since a X takes what a step loses of the small singular values' part to
+// 3.4 times as much in the next: the results, rounding included, are 2.0e-3 (1,024 x 1,024) to
+// 3.2e-3 (8 x 8; one of 2,000 5.7e-3) off, with X in 11 bits too up to 8e-3, with bf16 products
+// about ten times that.  In memory X keeps both for all but the last
 // two steps, after which nothing grows much: as exact, and of 2,048 x 4,096 matrices' last
 // products 564 us where both take 680.
 #include "product.h"
@@ -677,8 +680,8 @@ __global__ __launch_bounds__(C::kThreads, 2) void pair_kernel(Planes pm, Planes 
 // Q in its place) in LDS.  Both lie in tiles of 64 rows by up to 128 columns, X's by blocks
 // of columns: their rows are read as they lie, and X's columns for Q X by transposing reads.
 // Bound by waits: a step's three products follow each other, with a barrier after each, and a
-// compute unit holds one matrix of 128 rows.  144 of 128 x 128 (float32) 58 us, in steps
-// through memory 327; 24 of 64 x 256 30, 85.
+// compute unit holds one matrix of 128 rows.  A step of 144 of 128 x 128 (float32) 58 us, in
+// steps through memory 327; orthogonalised alone 46, in bf16 28; 24 of 64 x 256 30, 85 (bf16 24).
 template <int M_, int N_, bool SPLIT>
 struct Small {
     static constexpr int M = M_, N = N_, kPlanes = SPLIT ? 2 : 1 /* of S */, kThreads = M == 128 ? 1024 : 512;
@@ -1121,6 +1124,9 @@ hipError_t launch_pair(const Planes &p, const Planes &q, const Planes &out, unsi
 //            16 of 1,024 x 1,024    44, 48, 83       33, 38, 53       39, 48, 56
 //            8 of 2,048 x 4,096     397, 156, 615    188, 99, 366     208, 133, 297
 //            16 of 2,048 x 4,096    -                330, 188, -      312, 202, 564
+// Calls: 8 of 2,048 x 4,096 7,885 us in float32 (the products at the library's rate 6,950), 24 of
+// 300 x 701 257, in bf16 183 (58 % of S's wave cycles waiting, matrix units 5 % busy); a step of 112
+// of 256 x 256 in float32 383.
 template <int KIND, bool SPLIT, int RESTS>
 hipError_t step(const Planes &p, const Planes &q, const Planes &out, unsigned matrices, hipStream_t s)
 {
