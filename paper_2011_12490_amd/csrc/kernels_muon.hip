@@ -17,11 +17,14 @@
 // 1.64; 128 x 128 0.81, 1.42; 300 x 701 1.35, 2.40; 1,024 x 1,024 1.19, 3.07.  a X is added in
 // float32: with a in Q's diagonal the matrix units' sums, whose roundings are those of their
 // largest terms, lose twice as much.  bf16 updates, whose own rounding is 2^-9 (1.65e-3 of a
-// matrix's norm), multiply the first halves alone: 11 bits, whatever the gradient's type.  X
+// matrix's norm), multiply the first halves alone: 11 bits, whatever the gradient's type (but
+// where a side is below 8: exact_products in heads_api.cpp).  X
 // itself keeps both, since a X takes what a step loses of the small singular values' part to
 // 3.4 times as much in the next: the results, rounding included, are 2.0e-3 (1,024 x 1,024) to
-// 3.2e-3 (8 x 8; one of 2,000 5.7e-3) off, with X in 11 bits too up to 8e-3, with bf16 products
-// about ten times that.  In memory X keeps both for all but the last
+// 3.2e-3 (8 x 8; one of 20,000 6.2e-3) off, with X in 11 bits too up to 8e-3, with bf16 products
+// about ten times that.  Where few singular values make up a matrix they do not average: one by
+// itself is 3 to 5e-3 off as a rule and up to 3.3e-2 (two million of them in an emulation), 128 x 200
+// matrices of rank 3 4.1e-3, one of 400 1.0e-2.  In memory X keeps both for all but the last
 // two steps, after which nothing grows much: as exact, and of 2,048 x 4,096 matrices' last
 // products 564 us where both take 680.
 #include "product.h"

@@ -541,7 +541,8 @@ class AdamW:
 def orthogonalise(x: torch.Tensor, iterations: int = 5, out: Optional[torch.Tensor] = None) -> torch.Tensor:
     """x's matrices (the last two dimensions) with their singular values brought near 1 and
     their directions kept (derf_orthogonalise): float32 through products of 22 bits, about
-    as exactly as the iteration in float32, bfloat16 through products of 11 bits.  x: contiguous, [fan_out, fan_in] or
+    as exactly as the iteration in float32, bfloat16 through products of 11 bits (22 where a
+    side is below 8).  x: contiguous, [fan_out, fan_in] or
     [heads, fan_out, fan_in]; out: x, or another tensor of its shape and type."""
     if not isinstance(x, torch.Tensor) or x.dim() not in (2, 3) or x.dtype not in _PRECISION:
         raise ValueError("x must be a float32 or bfloat16 tensor [fan_out, fan_in] or [heads, fan_out, fan_in]")

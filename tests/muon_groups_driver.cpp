@@ -108,7 +108,7 @@ hipError_t launch_muon(const MuonSet &set, unsigned matrices, int fan_out, int f
         const int o = padded(e.fan_out), i = padded(e.fan_in), m = std::min(fan_out, fan_in), n = std::max(fan_out, fan_in);
         expect(std::min(o, i) <= m && std::max(o, i) <= n, "the launch's shape holds the matrix");
         expect((o <= 128 && i <= 128) || (std::min(o, i) == m && std::max(o, i) == n), "a large one's is its own");
-        expect(split == !e.param_bf16, "exactness by the parameters' type");
+        expect(split == (!e.param_bf16 || std::min(e.fan_out, e.fan_in) < 8), "exactness by the parameters' type and the shorter side");
         launched.push_back(e);
     }
     return hipSuccess;
@@ -196,9 +196,20 @@ int main()
     t.add(200, 8, 8);
     t.add(56, 65, 65);
     t.add(200, 8, 8, DERF_PREC_BF16);
-    t.add(56, 3, 128, DERF_PREC_BF16);
+    t.add(56, 8, 128, DERF_PREC_BF16);
     l = step(t);
     expect(l.size() == 2 && is(l[0], 256, 64, 128, false) && is(l[1], 256, 128, 128), "256 of each type in two launches");
+    // few rows or columns go with the exact ones
+    t = {};
+    t.add(2, 8, 128, DERF_PREC_BF16);
+    t.add(3, 7, 128, DERF_PREC_BF16);
+    t.add(4, 100, 7, DERF_PREC_BF16);
+    t.add(5, 64, 64);
+    t.add(2, 7, 700, DERF_PREC_BF16);
+    t.add(2, 8, 700, DERF_PREC_BF16);
+    l = step(t);
+    expect(l.size() == 4 && is(l[0], 2, 64, 128, false) && is(l[1], 12, 64, 128) && is(l[2], 2, 64, 704, false) && is(l[3], 2, 64, 704),
+           "by exactness, then shape");
     // places are as large as the largest of each side asks for
     t = {};
     t.add(2, 128, 3);

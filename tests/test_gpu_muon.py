@@ -240,3 +240,17 @@ def test_python_refusals():
                  lambda: heads.Muon([x], [x]).step(grad_scale=vector)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("K,O,I", [(4000, 1, 4), (4000, 2, 2), (4000, 2, 9), (4000, 4, 4), (2000, 40, 3), (2000, 7, 7), (300, 5, 130),
+                                   (200, 1, 700), (100, 900, 6)])
+def test_bf16_matrices_of_few_rows(K, O, I):
+    """Few singular values, whose roundings do not average: as near as float32's, but for the result's own rounding."""
+    x = rand(gen(O + I), K, O, I).to(BF16)
+    want, far = direction(x.double(), FP32)
+    check(heads.orthogonalise(x), want, far)
+    p = torch.zeros(K, O, I, dtype=BF16, device="cuda")
+    heads.Muon([p], [x], lr=1.0, momentum=0.0).step()
+    # p - size X: one more rounding in float32
+    size = math.sqrt(max(1.0, O / I))
+    check(p, -size * want, size * far, 2.0 ** -23 * size * want.square().sum((-2, -1)).sqrt())
