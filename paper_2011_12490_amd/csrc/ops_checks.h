@@ -103,20 +103,33 @@ int check_workspace(const void *p, long long have, long long need)
     return DERF_OK;
 }
 
-// Rows of an array in memory, in bytes; p null: none.
+typedef __int128 Wide;
+
+// Rows of an array in memory, in bytes; p null or no rows: none.
 struct Area {
-    const char *name;
-    const void *p;
-    long long rows, row, stride;
+    const char *name = "";
+    const void *p = nullptr;
+    long long rows = 0, row = 0, stride = 0;
+    uintptr_t from = 0, to = 0;  // of all
+
+    Area() = default;
+    Area(const char *name_, const void *p_, long long rows_, long long row_, long long stride_)
+        : name(name_), p(p_), rows(row_ > 0 ? rows_ : 0), row(row_), stride(rows > 1 ? stride_ : row_)
+    {
+        if (!p || rows <= 0)
+            return;
+        from = reinterpret_cast<uintptr_t>(p);
+        const Wide end = from + (Wide)(rows - 1) * stride + row;
+        to = end < (Wide)UINTPTR_MAX ? (uintptr_t)end : UINTPTR_MAX;
+    }
 };
 Area rows_area(const char *name, const void *p, long long rows, long long stride, long long dim, int precision)
 {
     const int bytes = precision == DERF_PREC_BF16 ? 2 : 4;
-    return {name, p, dim > 0 ? rows : 0, dim * bytes, stride * bytes};
+    return {name, p, rows, dim * bytes, stride * bytes};
 }
-Area array_area(const char *name, const void *p, long long bytes) { return {name, p, bytes > 0 ? 1 : 0, bytes, bytes}; }
+Area array_area(const char *name, const void *p, long long bytes) { return {name, p, 1, bytes, bytes}; }
 
-typedef __int128 Wide;
 // The sum of floor((a i + b) / m) over i in [0, n), a, b >= 0: whole parts taken out, what is
 // left counted along the other axis, as Euclid's algorithm goes.
 Wide floor_sum(Wide n, Wide m, Wide a, Wide b)
@@ -140,14 +153,10 @@ Wide floor_sum(Wide n, Wide m, Wide a, Wide b)
 // (-la, (nb - 1) sb + lb).
 bool share_memory(const Area &one, const Area &other)
 {
-    if (!one.p || !other.p || one.rows <= 0 || other.rows <= 0)
+    if (one.from >= other.to || other.from >= one.to)  // as most are; or one is none
         return false;
-    const Wide la = one.row, lb = other.row, na = one.rows, nb = other.rows;
-    const Wide sa = na > 1 ? one.stride : one.row, sb = nb > 1 ? other.stride : other.row;
-    const Wide d = (Wide) reinterpret_cast<uintptr_t>(other.p) - (Wide) reinterpret_cast<uintptr_t>(one.p);
-    const Wide end_a = (na - 1) * sa + la, end_b = (nb - 1) * sb + lb;
-    if (d >= end_a || -d >= end_b)
-        return false;
+    const Wide la = one.row, lb = other.row, na = one.rows, nb = other.rows, sa = one.stride, sb = other.stride;
+    const Wide d = (Wide)other.from - (Wide)one.from, end_b = (nb - 1) * sb + lb;
     const Wide from = d < la ? 0 : (d - la) / sa + 1, to = std::min(na, (end_b + d + sa - 1) / sa);
     if (from >= to)
         return false;

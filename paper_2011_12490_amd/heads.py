@@ -125,7 +125,7 @@ def _array(x, name, dtype, shape, device=None, leaf=False) -> None:
         raise ValueError("%s must have shape %s, got %s" % (name, tuple(shape), tuple(x.shape)))
     if not x.is_contiguous():
         raise ValueError("%s must be contiguous" % name)
-    if x.numel() == 1:
+    if shape and shape[-1] == 1 and x.numel() == 1:
         _not_negated(x, name)
     if x.requires_grad and not leaf:
         _no_graph(x, name)

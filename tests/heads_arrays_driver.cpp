@@ -109,8 +109,11 @@ void against_bytes()
     };
     for (int n = 0; n < 400000; ++n) {
         Area a = area(), b = area();
-        if (n % 2)  // columns of one buffer
-            a.stride = b.stride = std::max(a.stride, b.stride);
+        if (n % 2) {  // columns of one buffer
+            const long long stride = std::max(a.stride, b.stride);
+            a = {"", a.p, a.rows, a.row, stride};
+            b = {"", b.p, b.rows, b.row, stride};
+        }
         const bool want = by_bytes(a, b);
         ++both[want];
         if (share_memory(a, b) != want || share_memory(b, a) != want) {
@@ -123,16 +126,16 @@ void against_bytes()
     expect(both[0] > 50000 && both[1] > 50000, "both answers are met");
     // large ones: 2^31 rows far apart, and the same one byte on
     const Area far = {"", at(1 << 20), (1LL << 31) - 1, 1000, 1LL << 14}, beside = {"", at((1 << 20) + 1000), (1LL << 31) - 1, 15384, 1LL << 14};
-    Area on = beside;
     expect(!share_memory(far, beside) && !share_memory(beside, far), "rows between rows");
-    on.p = at((1 << 20) + 999);
+    const Area on = {"", at((1 << 20) + 999), beside.rows, beside.row, beside.stride};
     expect(share_memory(far, on) && share_memory(on, far), "one byte of each");
-    on = {"", at((1 << 20) + 1000), 1 << 20, 8, (1LL << 14) + 1};  // one byte on with every row
-    expect(share_memory(far, on), "the last of the gap's rows");
-    on.rows = 15376;  // row i ends at 1008 + i, the next far one begins at 16384
-    expect(!share_memory(far, on), "none yet");
-    on.rows = 15378;
-    expect(share_memory(far, on), "the first");
+    auto moving = [](long long rows) { return Area{"", at((1 << 20) + 1000), rows, 8, (1LL << 14) + 1}; };  // one byte on with every row
+    expect(share_memory(far, moving(1 << 20)), "the last of the gap's rows");
+    expect(!share_memory(far, moving(15376)), "none yet");  // row i ends at 1008 + i, the next far one begins at 16384
+    expect(share_memory(far, moving(15378)), "the first");
+    // more than any memory holds: no sum may turn over
+    expect(share_memory(Area{"", at(64), 1LL << 30, 8, 1LL << 42}, Area{"", at(1LL << 47), 4, 1 << 20, 1 << 20}), "beyond 64 bits");
+    expect(!share_memory(Area{"", at(64), 0, 8, 8}, far) && !share_memory(far, Area{"", nullptr, 5, 1 << 30, 1 << 30}), "no rows, no array");
 }
 
 // Arguments that lie far apart, but for one.
