@@ -569,7 +569,9 @@ class Muon:
     read from these tensors at every step.  copies: bfloat16 tensors (or None in the place
     of one) that receive the updated parameters rounded.  m: the momentum, float32 tensors
     of the parameters' shapes, used in place; zeros unless given.  The optimizer holds its
-    workspace: its steps go on one stream, or are waited for.  Biases and other vectors
+    workspace until close(): about 5 to 17 bytes a value of the matrices of one padded
+    shape, at most 8 GiB (or what one matrix needs), beside torch's allocator; none for
+    matrices of up to 64 x 512 or 128 x 128.  Its steps go on one stream, or are waited for.  Biases and other vectors
     belong to AdamW."""
 
     def __init__(self, params: Sequence[torch.Tensor], grads: Sequence[torch.Tensor], lr: float = 0.02,
