@@ -619,9 +619,10 @@ __global__ __launch_bounds__(256) void join_kernel(const unsigned *keys, unsigne
 
 // Few samples in one launch: a workgroup takes some rows and columns, notes the samples that
 // are its rows', in order, and sums them row by row, a group of lanes each, kAhead entries of
-// its list at a time.  Bound by a launch's waits, and with many samples of a row by the pieces'
-// loads, one after the other: 64 samples of 500 rows of 48 values 3.4 us, 256 samples of one of
-// them 28 (bf16 54; sorted 14 and 17).
+// its list at a time; rows without a sample, and workgroups, are told apart before.  Bound by a
+// launch's waits, and with many samples of a row by the pieces' loads, one after the other: 64
+// samples of 500 rows of 48 values 3.7 us, 256 samples of one of them 29 (bf16 56; sorted 14 and
+// 17); or by the bytes of a large table: 13 samples of 992,618 rows of 65 33 us, 258 MB.
 constexpr unsigned kFewSamples = 256;
 template <class T, int V>
 __global__ __launch_bounds__(256) void few_kernel(const int *ids, const T *from, long long stride, unsigned samples, unsigned rows, int D,
@@ -631,6 +632,9 @@ __global__ __launch_bounds__(256) void few_kernel(const int *ids, const T *from,
     static_assert(kFewSamples % kAhead == 0, "whole pieces of the list");
     __shared__ unsigned of_wave[4];
     __shared__ __attribute__((aligned(16))) unsigned row_of[kFewSamples], sample_of[kFewSamples];
+    __shared__ unsigned met[32];  // a bit for each row, by its number's lowest ten
+    if (threadIdx.x < 32)
+        met[threadIdx.x] = 0;
     const unsigned v0 = blockIdx.x * rows_each, here = rows - v0 < rows_each ? rows - v0 : rows_each;
     const int id = threadIdx.x < samples ? ids[threadIdx.x] : -1;
     const bool mine = (unsigned)id >= v0 && (unsigned)id - v0 < here;
@@ -645,11 +649,21 @@ __global__ __launch_bounds__(256) void few_kernel(const int *ids, const T *from,
             at += of_wave[w];
         count += of_wave[w];
     }
+    if (count == 0) {  // zeros side by side, shared by the workgroups of these rows
+        float *first = out + (size_t)v0 * D;
+        const size_t all = (size_t)here * D;
+        for (size_t i = blockIdx.y * 256u + threadIdx.x; i < all / 4; i += gridDim.y * 256u)
+            *reinterpret_cast<Any16 *>(first + i * 4) = u32x4{0, 0, 0, 0};
+        if (blockIdx.y == 0 && threadIdx.x < all % 4)
+            first[all / 4 * 4 + threadIdx.x] = 0.0f;
+        return;
+    }
     if (threadIdx.x >= count)
         row_of[threadIdx.x] = kNone;
     if (mine) {
         row_of[at] = (unsigned)id - v0;
         sample_of[at] = threadIdx.x;
+        atomicOr(&met[row_of[at] >> 5 & 31], 1u << (row_of[at] & 31));
     }
     __syncthreads();
     const unsigned groups = 256u >> group_log2, lanes = 1u << group_log2;
@@ -659,7 +673,8 @@ __global__ __launch_bounds__(256) void few_kernel(const int *ids, const T *from,
     const int e = V > 1 ? vec_at<V>(c, D) : c;
     for (unsigned v = threadIdx.x >> group_log2; v < here; v += groups) {
         float sum[V] = {};
-        for (unsigned i = 0; i < count; i += kAhead) {
+        const unsigned end = met[v >> 5 & 31] >> (v & 31) & 1 ? count : 0;  // most rows have no sample
+        for (unsigned i = 0; i < end; i += kAhead) {
             Vec<T, V> x[kAhead];
 #pragma unroll
             for (unsigned j = 0; j < kAhead; ++j)
