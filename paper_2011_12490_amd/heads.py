@@ -114,10 +114,11 @@ def _not_negated(x, name) -> None:
 
 
 def _array(x, name, dtype, shape, device=None, leaf=False) -> None:
-    """Check a contiguous GPU array of a given type and shape; leaf: autograd may follow it."""
+    """Check a contiguous GPU array of a given type and shape; leaf: autograd may follow it.
+    device: a GPU, but for an optimizer's tensors (leaf)."""
     if not isinstance(x, torch.Tensor):
         raise ValueError("%s must be a torch tensor" % name)
-    if not x.is_cuda or (device is not None and x.device != device):
+    if ((device is None or leaf) and not x.is_cuda) or (device is not None and x.device != device):
         raise ValueError("%s must be a tensor on %s" % (name, device or "a GPU"))
     if x.dtype != dtype:
         raise ValueError("%s must be %s, got %s" % (name, dtype, x.dtype))
@@ -135,10 +136,10 @@ def _array(x, name, dtype, shape, device=None, leaf=False) -> None:
 
 def _rows(x, name, shape=None, dtype=None, device=None) -> int:
     """Check an array of rows (elements of a row side by side, rows any distance
-    apart that does not make them overlap); returns that distance."""
+    apart that does not make them overlap); returns that distance.  device: a GPU."""
     if not isinstance(x, torch.Tensor):
         raise ValueError("%s must be a torch tensor" % name)
-    if not x.is_cuda or (device is not None and x.device != device):
+    if x.device != device if device is not None else not x.is_cuda:
         raise ValueError("%s must be a tensor on %s" % (name, device or "a GPU"))
     if x.dtype not in _PRECISION or (dtype is not None and x.dtype != dtype):
         raise ValueError("%s must be %s, got %s" % (name, dtype or "float32 or bfloat16", x.dtype))
